@@ -529,6 +529,183 @@ litevlm_status_t litevlm_select_score_noalloc(int32_t num_q_heads, int32_t num_k
                                               float q_scale, float k_scale, float* scores, int32_t* err_d,
                                               litevlm_stream_t stream);
 
+/*
+ * The 4-bit K/V cache of the decoder that runs behind the selection (Design
+ * section, Speculative Decoding Head: K/V rows feed the KV cache): rows appended,
+ * attention that reads them, eviction, and the verification of drafted tokens.
+ * A handle's num_q_heads, num_kv_heads, head_dim and qk_dtype are those of the
+ * model's decoder layers; max_batch bounds the batch of every call; the totals of
+ * the handle bound nothing here.
+ *
+ * Format. A cache is a pool of pages owned by the caller. A page holds, for every
+ * key head, page_size rows of K and of V. A row of d channels is d/2 bytes of
+ * e2m1 codes (channel 2i in the low four bits of byte i, channel 2i+1 in the high
+ * ones; sign, two exponent bits, one mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6)
+ * and d/16 bytes of e4m3 scales, one for every 16 channels. Channel j stands for
+ *     e2m1(code_j) * e4m3(scale_(j/16)) * k_scale (v_scale).
+ *   k_codes, v_codes    device [num_pages][num_kv_heads][page_size][d/2]
+ *   k_scales, v_scales  device [num_pages][num_kv_heads][page_size][d/16]
+ *   page_size           a power of two in [16, 256]
+ *   k_scale, v_scale    in [2^-60, 2^60]
+ * all four 16-byte aligned. A weight for every slot, float [num_pages][page_size],
+ * says how much attention the token has received; it is an argument of its own.
+ *
+ * A request's tokens lie in the pages of its table row, in order: position p in
+ * slot p % page_size of page table[b][p / page_size].
+ *   table       device int32 [batch][table_width]; entries behind the last page
+ *               that a request's tokens need are not used
+ *   seq_lens    device int32 [batch], the tokens that each request has
+ * Lengths and tables are read on the device only, so that a captured graph can be
+ * replayed as they change. What a kernel finds there is checked before use: a
+ * length outside [0, table_width * page_size] (or beyond max_len, where a call has
+ * it) is cut to it, and tokens whose table entry is not in [0, num_pages) are
+ * skipped; both set LITEVLM_ERR_DEVICE_BOUNDS for litevlm_select_check_device.
+ * Two calls that write to the same pages, or one that reads what another writes,
+ * are ordered by the caller (one stream does).
+ */
+typedef struct {
+    void* k_codes;
+    void* k_scales;
+    void* v_codes;
+    void* v_scales;
+    int32_t num_pages;
+    int32_t page_size;
+    float k_scale;
+    float v_scale;
+} litevlm_cache_t;
+
+/*
+ * Appends rows: token t of request b goes to position seq_lens[b] + t. In fp32,
+ * for every 16 channels:
+ *     y = x * in_scale / k_scale (v_scale);  s = e4m3(max |y| / 6), at most 448
+ *     code = e2m1(y / s), rounded to nearest, a tie to the even code, at most +-6
+ * A scale of 0 gives codes 0; a NaN in the block makes its scale NaN.
+ *   batch            0 <= batch <= max_batch
+ *   k, v             device [src_rows][num_kv_heads][d] of the handle's element type,
+ *                    16-byte aligned; row r starts k_row_stride (v_row_stride)
+ *                    elements behind row r-1 (>= num_kv_heads * d, a multiple of
+ *                    16 bytes), so K and V may be parts of one fused projection
+ *   src_rows         rows of k and v
+ *   row_idx          device int32 [sum T_b] or NULL: the source row of every new token
+ *                    (litevlm_select_topk's kept_idx puts the kept rows into the cache
+ *                    with no gather in between); NULL: token r of the call has row r
+ *   new_offsets_d/h  int32 [batch+1] prefix of T_b, the new tokens of each request
+ *   k_in_scale, v_in_scale  e4m3: the codes' per-tensor scales (> 0, finite); bf16: 1
+ *   weights          device float [num_pages][page_size] or NULL: set to 0 for the new tokens
+ *   k_stored, v_stored  device bf16 [sum T_b][num_kv_heads][d] or NULL, 16-byte
+ *                    aligned: the values that the cache now holds for the new rows
+ *                    (rounded to bf16; exact where the scale is a power of two)
+ *   new_lens         device int32 [batch]: seq_lens[b] + T_b (not more than the
+ *                    table row holds); not the array seq_lens
+ * A row whose position or source row is out of range is skipped (DEVICE_BOUNDS).
+ * Errors: INVALID_ARG for sizes, pointers, strides or scales outside the above;
+ * WORKSPACE for a batch beyond max_batch.
+ */
+litevlm_status_t litevlm_select_cache_append(litevlm_select_t handle, int32_t batch, const litevlm_cache_t* cache,
+                                             const int32_t* table, int32_t table_width, const int32_t* seq_lens,
+                                             const void* k, int64_t k_row_stride, const void* v,
+                                             int64_t v_row_stride, int64_t src_rows, const int32_t* row_idx,
+                                             const int32_t* new_offsets_d, const int32_t* new_offsets_h,
+                                             float k_in_scale, float v_in_scale, float* weights, void* k_stored,
+                                             void* v_stored, int32_t* new_lens, litevlm_stream_t stream);
+
+/*
+ * Attention of the last tokens of every request over its cache. Query i of the
+ * T_b queries of request b stands at position n_b - T_b + i (n_b = seq_lens[b],
+ * the queries' own tokens appended before) and sees the positions up to its own:
+ *     s[h][i][j] = q_scale * k_scale * (q[i,h,:] . k[j, h / G, :]) / sqrt(d),  j <= n_b - T_b + i
+ *     p[h][i][:] = softmax_j;  out[i,h,:] = sum_j p[h][i][j] * v[j, h / G, :]
+ *     weights_out[slot of j] = weights_in[slot of j] + (1 / Hq) * sum_h sum_i p[h][i][j]
+ * A query that sees no key gives zeros and adds no weight. What lies behind a
+ * request's last token does not matter, whatever its bytes are.
+ *   q                device [sum T_b][Hq][d] of the handle's element type, 16-byte
+ *                    aligned, row stride as in litevlm_select_cache_append
+ *   q_offsets_d/h    int32 [batch+1] prefix of T_b (T_b = 1: a decoding step; T_b = 0:
+ *                    the request takes no part)
+ *   max_len          a bound of the lengths, 0 <= max_len <= table_width * page_size:
+ *                    it sizes the launch and the workspace
+ *   q_scale          e4m3: the codes' per-tensor scale; bf16: 1
+ *   weights_in/out   device float [num_pages][page_size], both or neither. The same
+ *                    array: weights are added up in place. Two arrays: the sums go to
+ *                    weights_out for every token of every request of the call, other
+ *                    slots are left as they were (a speculative pass whose weights
+ *                    may have to be forgotten)
+ *   out              device bf16 [sum T_b][Hq][d], 16-byte aligned
+ *   workspace        device, at least the bytes that
+ *                    litevlm_select_cache_attend_workspace gives for the same batch,
+ *                    offsets and max_len, 256-byte aligned; used only by this call
+ *                    until it has run. Calls that may run at the same time (two
+ *                    captured graphs among them) need a workspace each.
+ * Softmax statistics, sums and weights are fp32; probabilities are rounded to f16 for
+ * the product with V. The weights are added in a fixed order (the same inputs give
+ * the same bits).
+ * Errors: as for litevlm_select_cache_append; WORKSPACE for a workspace that is too
+ * small; UNSUPPORTED where Hkv x row tiles of the longest request passes 65535.
+ */
+litevlm_status_t litevlm_select_cache_attend_workspace(litevlm_select_t handle, int32_t batch,
+                                                       const int32_t* q_offsets_h, int32_t max_len, int64_t* bytes);
+litevlm_status_t litevlm_select_cache_attend(litevlm_select_t handle, int32_t batch, const litevlm_cache_t* cache,
+                                             const int32_t* table, int32_t table_width, const int32_t* seq_lens,
+                                             const void* q, int64_t q_row_stride, const int32_t* q_offsets_d,
+                                             const int32_t* q_offsets_h, int32_t max_len, float q_scale,
+                                             const float* weights_in, float* weights_out, void* out,
+                                             void* workspace, int64_t workspace_bytes, litevlm_stream_t stream);
+
+/*
+ * Cuts every request back to `budget` tokens by accumulated attention weight. A
+ * request of n_b > budget tokens keeps its first `sink`, its last `recent`, and of
+ * the others those with the largest weights until budget are kept (the order of
+ * litevlm_select_topk: NaN below every number, -0 equals +0, ties to the lower
+ * position); one of n_b <= budget keeps all. Kept rows of K, V and weights move,
+ * in order and byte for byte, to the front of the table row.
+ *   max_len      a bound of the lengths, as above
+ *   budget       >= 1; sink, recent >= 0; sink + recent <= budget
+ *   to_table     device int32 [batch][to_width] or NULL. NULL: rows move within the
+ *                request's own pages (no page belongs to two of the batch's requests).
+ *                Else they move to these pages, which hold min(budget, max_len) tokens a
+ *                request and are none that the call reads: the old pages stay as they
+ *                are (they may be shared)
+ *   weights      device float [num_pages][page_size]
+ *   kept_idx     device int32 [batch][budget]: the kept positions, ascending; -1 behind
+ *                the last
+ *   new_lens     device int32 [batch]: min(n_b, budget); not the array seq_lens
+ * Errors: as above.
+ */
+litevlm_status_t litevlm_select_cache_evict(litevlm_select_t handle, int32_t batch, const litevlm_cache_t* cache,
+                                            const int32_t* table, int32_t table_width, const int32_t* seq_lens,
+                                            int32_t max_len, int32_t budget, int32_t sink, int32_t recent,
+                                            const int32_t* to_table, int32_t to_width, float* weights,
+                                            int32_t* kept_idx, int32_t* new_lens, litevlm_stream_t stream);
+
+/*
+ * Verification of drafted tokens (Design section, Speculative Decoding Head): draft
+ * t of a request, token x with the draft model's probability q and the target's p,
+ * is accepted while u_accept * q < p (exact products). Behind the accepted drafts
+ * one more token is sampled with u_sample: from max(p - q, 0) of the refused
+ * draft's rows, or, where every draft was accepted or no entry of p - q is above 0,
+ * from p. Sampling takes the lowest token i with weight w_i > 0 whose running sum
+ * passes u_sample times the sum of all; the last with w_i > 0 where none does;
+ * -1 where no weight is above 0. NaN counts as 0.
+ *   vocab            entries of a probability row, >= 1
+ *   prob_bf16        0: float rows; 1: bf16 rows
+ *   draft_tokens     device int32 [sum T_b]
+ *   draft_offsets_d/h  int32 [batch+1] prefix of T_b (0 allowed)
+ *   target_probs     device [sum T_b + batch][vocab]: T_b + 1 rows a request
+ *   draft_probs      device [sum T_b][vocab], or NULL: the drafts were certain of their
+ *                    tokens (q = 1 there, 0 elsewhere)
+ *   u_accept         device float [sum T_b], u_sample device float [batch], in [0, 1)
+ *   accepted         device int32 [batch]
+ *   tokens           device int32 [sum T_b + batch]: request b's accepted drafts, the
+ *                    sampled token, then -1, from row draft_offsets[b] + b on
+ * A drafted token outside [0, vocab) is refused (DEVICE_BOUNDS). Needs none of the
+ * handle's head sizes. Errors: INVALID_ARG / WORKSPACE as above.
+ */
+litevlm_status_t litevlm_select_verify(litevlm_select_t handle, int32_t batch, int32_t vocab, int32_t prob_bf16,
+                                       const int32_t* draft_tokens, const int32_t* draft_offsets_d,
+                                       const int32_t* draft_offsets_h, const void* target_probs,
+                                       const void* draft_probs, const float* u_accept, const float* u_sample,
+                                       int32_t* accepted, int32_t* tokens, litevlm_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

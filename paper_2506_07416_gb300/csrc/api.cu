@@ -1240,6 +1240,363 @@ litevlm_status_t litevlm_select_set_wait_budget(litevlm_select_t h, int64_t cycl
 }  // extern "C"
 
 // ----------------------------------------------------------------------------
+// The 4-bit cache and the verification of drafts
+// ----------------------------------------------------------------------------
+namespace {
+
+// The handle's device current for the length of a call (the caller's is restored).
+struct OnDevice {
+    int before = -1;
+    cudaError_t e;
+    explicit OnDevice(int device)
+    {
+        e = cudaGetDevice(&before);
+        if (e == cudaSuccess && before != device) e = cudaSetDevice(device);
+        else before = -1;
+    }
+    ~OnDevice()
+    {
+        if (before >= 0) cudaSetDevice(before);
+    }
+};
+
+bool in_range(float scale) { return scale >= 0x1p-60f && scale <= 0x1p60f; }
+
+litevlm_status_t start_call(litevlm_select_t h, int32_t batch)
+{
+    h->last_error.clear();
+    h->last_launches = 0;
+    if (batch < 0) return fail(h, LITEVLM_ERR_INVALID_ARG, "batch must be >= 0");
+    if (batch > h->cfg.max_batch) return fail(h, LITEVLM_ERR_WORKSPACE, "batch exceeds max_batch");
+    if (batch > 65535) return fail(h, LITEVLM_ERR_UNSUPPORTED, "batches of more than 65535 requests");
+    return LITEVLM_OK;
+}
+
+// Checks a cache and a table; fills the kernels' view of them and `limit`, the tokens a table row holds.
+litevlm_status_t cache_pages(litevlm_select_t h, const litevlm_cache_t* c, const int32_t* table, int32_t table_width,
+                             const int32_t* seq_lens, lvs::CachePages* out, int32_t* limit)
+{
+    if (!c) return fail(h, LITEVLM_ERR_INVALID_ARG, "cache is NULL");
+    if (!c->k_codes || !c->k_scales || !c->v_codes || !c->v_scales || !table || !seq_lens)
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "a device pointer is NULL");
+    if (!aligned16(c->k_codes) || !aligned16(c->k_scales) || !aligned16(c->v_codes) || !aligned16(c->v_scales))
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "the cache's tensors must be 16-byte aligned");
+    if (c->num_pages < 1) return fail(h, LITEVLM_ERR_INVALID_ARG, "num_pages must be >= 1");
+    const int32_t ps = c->page_size;
+    if (ps < 16 || ps > 256 || (ps & (ps - 1)) != 0)
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "page_size must be a power of two in [16, 256]");
+    if (!in_range(c->k_scale) || !in_range(c->v_scale))
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "k_scale and v_scale must be in [2^-60, 2^60]");
+    if (table_width < 1 || (int64_t)table_width * ps > INT32_MAX - 65536)
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "table_width must be >= 1 and its pages hold less than 2^31 - 2^16 tokens");
+    out->codes[0] = static_cast<uint8_t*>(c->k_codes);
+    out->codes[1] = static_cast<uint8_t*>(c->v_codes);
+    out->scales[0] = static_cast<uint8_t*>(c->k_scales);
+    out->scales[1] = static_cast<uint8_t*>(c->v_scales);
+    out->scale[0] = c->k_scale;
+    out->scale[1] = c->v_scale;
+    out->num_pages = c->num_pages;
+    out->page_shift = 0;
+    while ((1 << out->page_shift) < ps) ++out->page_shift;
+    out->hkv = h->cfg.num_kv_heads;
+    if (out->hkv > 65535) return fail(h, LITEVLM_ERR_UNSUPPORTED, "more than 65535 key heads");
+    out->table = table;
+    out->width = table_width;
+    *limit = table_width * ps;
+    return LITEVLM_OK;
+}
+
+// Rows [.][heads][d] of the handle's element type that start `stride` elements apart.
+litevlm_status_t check_rows(litevlm_select_t h, const void* p, int64_t stride, int32_t heads, float scale, const char* name)
+{
+    const bool fp8 = h->cfg.qk_dtype == LITEVLM_FP8_E4M3;
+    if (!p) return fail(h, LITEVLM_ERR_INVALID_ARG, std::string(name) + " is NULL");
+    if (!aligned16(p)) return fail(h, LITEVLM_ERR_INVALID_ARG, std::string(name) + " must be 16-byte aligned");
+    if (stride < (int64_t)heads * h->cfg.head_dim || stride % (fp8 ? 16 : 8) != 0)
+        return fail(h, LITEVLM_ERR_INVALID_ARG,
+                    std::string(name) + "'s row stride must cover a row and be a multiple of 16 bytes");
+    if (fp8 ? !(scale > 0.f) || isinf(scale) : scale != 1.f)
+        return fail(h, LITEVLM_ERR_INVALID_ARG,
+                    std::string(name) + (fp8 ? "'s scale must be finite and > 0" : "'s scale must be 1 for bf16"));
+    return LITEVLM_OK;
+}
+
+// Largest count of an offsets mirror.
+int32_t max_count(const int32_t* off, int32_t batch)
+{
+    int32_t m = 0;
+    for (int32_t b = 0; b < batch; ++b) m = std::max(m, off[b + 1] - off[b]);
+    return m;
+}
+
+int64_t round256(int64_t bytes) { return (bytes + 255) & ~(int64_t)255; }
+
+// Workspace of an attention call: the chunks' sums and statistics, and the rows' lse.
+struct AttendSpace {
+    int64_t part_o, part_ml, lse, total;
+};
+AttendSpace attend_space(const lvs::AttendPlan& plan, int64_t rows, int head_dim)
+{
+    AttendSpace s{};
+    const int64_t parts = plan.chunks > 1 ? rows * plan.chunks : 0;
+    s.part_ml = round256(parts * head_dim * 4);
+    s.lse = s.part_ml + round256(parts * 8);
+    s.total = s.lse + round256(rows * 4);
+    return s;
+}
+
+litevlm_status_t attend_plan(litevlm_select_t h, int32_t batch, const int32_t* q_offsets_h, int32_t max_len,
+                             lvs::AttendPlan* plan, int64_t* total, int* max_rows)
+{
+    const litevlm_select_config_t& c = h->cfg;
+    litevlm_status_t s = check_offsets(h, q_offsets_h, batch, INT32_MAX, "q_offsets", total);
+    if (s != LITEVLM_OK) return s;
+    if (max_len < 0) return fail(h, LITEVLM_ERR_INVALID_ARG, "max_len must be >= 0");
+    const int64_t group = c.num_q_heads / c.num_kv_heads;
+    const int64_t rows = max_count(q_offsets_h, batch) * group;
+    if (rows > INT32_MAX / 2 || (int64_t)c.num_kv_heads * ((rows + 7) / 8) > 65535)
+        return fail(h, LITEVLM_ERR_UNSUPPORTED, "num_kv_heads x rows of the longest request / 8 exceeds 65535");
+    *max_rows = (int)rows;
+    *plan = lvs::plan_cache_attend(batch, c.num_kv_heads, *max_rows, max_len, h->num_sms);
+    return LITEVLM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+litevlm_status_t litevlm_select_cache_append(litevlm_select_t h, int32_t batch, const litevlm_cache_t* cache,
+                                             const int32_t* table, int32_t table_width, const int32_t* seq_lens,
+                                             const void* k, int64_t k_row_stride, const void* v,
+                                             int64_t v_row_stride, int64_t src_rows, const int32_t* row_idx,
+                                             const int32_t* new_offsets_d, const int32_t* new_offsets_h,
+                                             float k_in_scale, float v_in_scale, float* weights, void* k_stored,
+                                             void* v_stored, int32_t* new_lens, litevlm_stream_t stream)
+{
+    const CallRange range_(__func__);
+    if (!h) return LITEVLM_ERR_INVALID_ARG;
+    litevlm_status_t s = start_call(h, batch);
+    if (s != LITEVLM_OK) return s;
+    int64_t rows = 0;
+    s = check_offsets(h, new_offsets_h, batch, INT32_MAX, "new_offsets", &rows);
+    if (s != LITEVLM_OK || batch == 0) return s;
+    lvs::AppendArgs a{};
+    s = cache_pages(h, cache, table, table_width, seq_lens, &a.cache, &a.limit);
+    if (s != LITEVLM_OK) return s;
+    if (!new_offsets_d || !new_lens) return fail(h, LITEVLM_ERR_INVALID_ARG, "a device pointer is NULL");
+    if (new_lens == seq_lens) return fail(h, LITEVLM_ERR_INVALID_ARG, "new_lens must not be the array seq_lens");
+    if (src_rows < 0 || (!row_idx && src_rows < rows))
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "k and v have fewer rows than the call appends");
+    if (rows > 0) {
+        s = check_rows(h, k, k_row_stride, h->cfg.num_kv_heads, k_in_scale, "k");
+        if (s == LITEVLM_OK) s = check_rows(h, v, v_row_stride, h->cfg.num_kv_heads, v_in_scale, "v");
+        if (s != LITEVLM_OK) return s;
+        if ((k_stored && !aligned16(k_stored)) || (v_stored && !aligned16(v_stored)))
+            return fail(h, LITEVLM_ERR_INVALID_ARG, "k_stored and v_stored must be 16-byte aligned");
+    }
+    s = debug_mirror(h, new_offsets_d, new_offsets_h, (int64_t)batch + 1, "new_offsets", stream);
+    if (s != LITEVLM_OK) return s;
+    a.src[0] = k;
+    a.src[1] = v;
+    a.stride[0] = k_row_stride;
+    a.stride[1] = v_row_stride;
+    a.row_idx = row_idx;
+    a.src_rows = src_rows;
+    a.rows = rows;
+    a.lens = seq_lens;
+    a.off = new_offsets_d;
+    a.batch = batch;
+    a.in_scale[0] = k_in_scale;
+    a.in_scale[1] = v_in_scale;
+    a.inv_scale[0] = 1.f / cache->k_scale;
+    a.inv_scale[1] = 1.f / cache->v_scale;
+    a.stored[0] = static_cast<__nv_bfloat16*>(k_stored);
+    a.stored[1] = static_cast<__nv_bfloat16*>(v_stored);
+    a.weights = weights;
+    a.new_lens = new_lens;
+    a.err = h->err_d;
+    const OnDevice on(h->device);
+    cudaError_t e = on.e;
+    if (e == cudaSuccess)
+        e = lvs::launch_cache_append(a, h->cfg.head_dim, h->cfg.qk_dtype == LITEVLM_FP8_E4M3, h->num_sms,
+                                     (cudaStream_t)stream);
+    if (e != cudaSuccess) return cuda_fail(h, e, "cache_append launch");
+    h->last_launches = 1;
+    return LITEVLM_OK;
+}
+
+litevlm_status_t litevlm_select_cache_attend_workspace(litevlm_select_t h, int32_t batch, const int32_t* q_offsets_h,
+                                                       int32_t max_len, int64_t* bytes)
+{
+    const CallRange range_(__func__);
+    if (!h) return LITEVLM_ERR_INVALID_ARG;
+    litevlm_status_t s = start_call(h, batch);
+    if (s != LITEVLM_OK) return s;
+    if (!bytes) return fail(h, LITEVLM_ERR_INVALID_ARG, "bytes is NULL");
+    lvs::AttendPlan plan;
+    int64_t total = 0;
+    int max_rows = 0;
+    s = attend_plan(h, batch, q_offsets_h, max_len, &plan, &total, &max_rows);
+    if (s == LITEVLM_OK) *bytes = attend_space(plan, total * h->cfg.num_q_heads, h->cfg.head_dim).total;
+    return s;
+}
+
+litevlm_status_t litevlm_select_cache_attend(litevlm_select_t h, int32_t batch, const litevlm_cache_t* cache,
+                                             const int32_t* table, int32_t table_width, const int32_t* seq_lens,
+                                             const void* q, int64_t q_row_stride, const int32_t* q_offsets_d,
+                                             const int32_t* q_offsets_h, int32_t max_len, float q_scale,
+                                             const float* weights_in, float* weights_out, void* out,
+                                             void* workspace, int64_t workspace_bytes, litevlm_stream_t stream)
+{
+    const CallRange range_(__func__);
+    if (!h) return LITEVLM_ERR_INVALID_ARG;
+    litevlm_status_t s = start_call(h, batch);
+    if (s != LITEVLM_OK) return s;
+    const litevlm_select_config_t& c = h->cfg;
+    lvs::AttendPlan plan;
+    int64_t total = 0;
+    int max_rows = 0;
+    s = attend_plan(h, batch, q_offsets_h, max_len, &plan, &total, &max_rows);
+    if (s != LITEVLM_OK || batch == 0) return s;
+    lvs::AttendArgs a{};
+    int32_t holds = 0;
+    s = cache_pages(h, cache, table, table_width, seq_lens, &a.cache, &holds);
+    if (s != LITEVLM_OK) return s;
+    if (max_len > holds) return fail(h, LITEVLM_ERR_INVALID_ARG, "max_len exceeds table_width * page_size");
+    if (!q_offsets_d) return fail(h, LITEVLM_ERR_INVALID_ARG, "a device pointer is NULL");
+    if (!weights_in != !weights_out)
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "weights_in and weights_out are given together");
+    if (total > 0) {
+        s = check_rows(h, q, q_row_stride, c.num_q_heads, q_scale, "q");
+        if (s != LITEVLM_OK) return s;
+        if (!out || !aligned16(out)) return fail(h, LITEVLM_ERR_INVALID_ARG, "out must be 16-byte aligned and not NULL");
+    }
+    const AttendSpace space = attend_space(plan, total * c.num_q_heads, c.head_dim);
+    if (workspace_bytes < space.total || (space.total > 0 && !workspace))
+        return fail(h, LITEVLM_ERR_WORKSPACE, "the workspace must hold " + std::to_string(space.total) + " bytes");
+    if (reinterpret_cast<uintptr_t>(workspace) & 255u)
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "the workspace must be 256-byte aligned");
+    s = debug_mirror(h, q_offsets_d, q_offsets_h, (int64_t)batch + 1, "q_offsets", stream);
+    if (s != LITEVLM_OK) return s;
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    a.q = q;
+    a.q_stride = q_row_stride;
+    a.q_off = q_offsets_d;
+    a.lens = seq_lens;
+    a.batch = batch;
+    a.hq = c.num_q_heads;
+    a.group = c.num_q_heads / c.num_kv_heads;
+    a.limit = max_len;
+    a.c_log2 = (float)((double)q_scale * (double)cache->k_scale / sqrt((double)c.head_dim) * 1.4426950408889634);
+    a.chunk = plan.chunk;
+    a.chunks = plan.chunks;
+    a.out = static_cast<__nv_bfloat16*>(out);
+    a.part_o = reinterpret_cast<float*>(ws + space.part_o);
+    a.part_ml = reinterpret_cast<float2*>(ws + space.part_ml);
+    a.lse = weights_out ? reinterpret_cast<float*>(ws + space.lse) : nullptr;
+    a.weights_in = weights_in;
+    a.weights_out = weights_out;
+    a.err = h->err_d;
+    const OnDevice on(h->device);
+    cudaError_t e = on.e;
+    int32_t launches = 0;
+    if (e == cudaSuccess)
+        e = lvs::launch_cache_attend(a, plan, c.head_dim, c.qk_dtype == LITEVLM_FP8_E4M3, max_rows, total, max_len,
+                                     (cudaStream_t)stream, &launches);
+    if (e != cudaSuccess) return cuda_fail(h, e, "cache_attend launch");
+    h->last_launches = launches;
+    return LITEVLM_OK;
+}
+
+litevlm_status_t litevlm_select_cache_evict(litevlm_select_t h, int32_t batch, const litevlm_cache_t* cache,
+                                            const int32_t* table, int32_t table_width, const int32_t* seq_lens,
+                                            int32_t max_len, int32_t budget, int32_t sink, int32_t recent,
+                                            const int32_t* to_table, int32_t to_width, float* weights,
+                                            int32_t* kept_idx, int32_t* new_lens, litevlm_stream_t stream)
+{
+    const CallRange range_(__func__);
+    if (!h) return LITEVLM_ERR_INVALID_ARG;
+    litevlm_status_t s = start_call(h, batch);
+    if (s != LITEVLM_OK) return s;
+    if (budget < 1) return fail(h, LITEVLM_ERR_INVALID_ARG, "budget must be >= 1");
+    if (sink < 0 || recent < 0 || (int64_t)sink + recent > budget)
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "sink and recent must be >= 0 and sink + recent <= budget");
+    if (batch == 0) return LITEVLM_OK;
+    lvs::EvictArgs a{};
+    int32_t holds = 0;
+    s = cache_pages(h, cache, table, table_width, seq_lens, &a.cache, &holds);
+    if (s != LITEVLM_OK) return s;
+    if (max_len < 0 || max_len > holds)
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "max_len must be in [0, table_width * page_size]");
+    if (to_table && (to_width < 1 || (int64_t)to_width * cache->page_size < std::min(budget, max_len)))
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "to_width pages must hold min(budget, max_len) tokens");
+    if (!weights || !kept_idx || !new_lens) return fail(h, LITEVLM_ERR_INVALID_ARG, "a device pointer is NULL");
+    if (new_lens == seq_lens) return fail(h, LITEVLM_ERR_INVALID_ARG, "new_lens must not be the array seq_lens");
+    a.lens = seq_lens;
+    a.batch = batch;
+    a.limit = max_len;
+    a.budget = budget;
+    a.sink = sink;
+    a.recent = recent;
+    a.to_table = to_table ? to_table : table;
+    a.to_width = to_table ? to_width : table_width;
+    a.weights = weights;
+    a.kept = kept_idx;
+    a.new_lens = new_lens;
+    a.err = h->err_d;
+    const OnDevice on(h->device);
+    cudaError_t e = on.e;
+    int32_t launches = 0;
+    if (e == cudaSuccess)
+        e = lvs::launch_cache_evict(a, h->cfg.head_dim, h->num_sms, (cudaStream_t)stream, &launches);
+    if (e != cudaSuccess) return cuda_fail(h, e, "cache_evict launch");
+    h->last_launches = launches;
+    return LITEVLM_OK;
+}
+
+litevlm_status_t litevlm_select_verify(litevlm_select_t h, int32_t batch, int32_t vocab, int32_t prob_bf16,
+                                       const int32_t* draft_tokens, const int32_t* draft_offsets_d,
+                                       const int32_t* draft_offsets_h, const void* target_probs,
+                                       const void* draft_probs, const float* u_accept, const float* u_sample,
+                                       int32_t* accepted, int32_t* tokens, litevlm_stream_t stream)
+{
+    const CallRange range_(__func__);
+    if (!h) return LITEVLM_ERR_INVALID_ARG;
+    litevlm_status_t s = start_call(h, batch);
+    if (s != LITEVLM_OK) return s;
+    if (vocab < 1) return fail(h, LITEVLM_ERR_INVALID_ARG, "vocab must be >= 1");
+    if (prob_bf16 != 0 && prob_bf16 != 1) return fail(h, LITEVLM_ERR_INVALID_ARG, "prob_bf16 must be 0 or 1");
+    int64_t total = 0;
+    s = check_offsets(h, draft_offsets_h, batch, INT32_MAX - 65536, "draft_offsets", &total);
+    if (s != LITEVLM_OK || batch == 0) return s;
+    if (!draft_offsets_d || !target_probs || !u_sample || !accepted || !tokens ||
+        (total > 0 && (!draft_tokens || !u_accept)))
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "a device pointer is NULL");
+    s = debug_mirror(h, draft_offsets_d, draft_offsets_h, (int64_t)batch + 1, "draft_offsets", stream);
+    if (s != LITEVLM_OK) return s;
+    lvs::VerifyArgs a{};
+    a.tokens = draft_tokens;
+    a.off = draft_offsets_d;
+    a.p = target_probs;
+    a.q = draft_probs;
+    a.u = u_accept;
+    a.u_last = u_sample;
+    a.batch = batch;
+    a.vocab = vocab;
+    a.accepted = accepted;
+    a.out = tokens;
+    a.err = h->err_d;
+    const OnDevice on(h->device);
+    cudaError_t e = on.e;
+    if (e == cudaSuccess) e = lvs::launch_verify(a, prob_bf16 == 1, (cudaStream_t)stream);
+    if (e != cudaSuccess) return cuda_fail(h, e, "verify launch");
+    h->last_launches = 1;
+    return LITEVLM_OK;
+}
+
+}  // extern "C"
+
+// ----------------------------------------------------------------------------
 // litevlm_select_score_noalloc: the score kernels with their scratch in
 // static device arrays of this library instead of a handle's workspace.
 //

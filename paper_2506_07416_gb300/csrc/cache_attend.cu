@@ -1,0 +1,650 @@
+// Attention over the 4-bit cache.
+//
+// Query i of the T_b queries of request b stands at position n_b - T_b + i and sees
+// the keys up to it. With s = c * q.k in log2 units, p = 2^(s - lse), lse = log2 sum
+// 2^s: out = sum p v; weight[j] += (1/Hq) sum over heads and queries of p.
+//
+// attend_split_kernel: a CTA takes a key head of a request, a tile of 8, 16 or 32
+// rows (a row is a query with one of the head's query heads) and a chunk of the
+// keys. Its four warps work on their own: a warp copies groups of 16 keys into its
+// ring in shared memory, makes f16 values of codes and scales in registers (exact),
+// and multiplies with the keys as the M rows and the query rows as the N columns
+// (m16n8k16): a tile of 8 rows, the usual one of a single token, then costs no
+// padding. Channels of a contraction may come in any order, so a lane takes the 32
+// (QK) or 16 (PV) neighbouring channels that one load brings. The rows' references
+// move only when a score passes them by 8 (2^8 is well inside f16); sums and
+// statistics are fp32. P is rounded to f16 (11 bits) for the second product, the
+// output once to bf16 (8 bits).
+// attend_join_kernel: the chunks of a row joined under the largest reference.
+// attend_weight_kernel: with every row's lse known, a CTA takes 64 keys of a
+// request, makes their scores again for all heads and adds the probabilities in a
+// fixed order; no atomics.
+
+#include "cache.cuh"
+
+namespace lvs {
+
+namespace {
+
+constexpr int kAttWarps = 4;
+constexpr int kAttThreads = 32 * kAttWarps;
+constexpr int kAttStages = 4;        // groups of a warp's ring
+constexpr float kNoRef = -3.0e38f;   // reference of a row without keys so far
+constexpr float kRefSlack = 8.f;     // a score may pass its row's reference by this
+
+// D += A B: 16 keys (or channels) x 8 rows, f16 operands, fp32 sums
+__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                         uint32_t b1)
+{
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+        "{%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v)
+{
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+
+__device__ __forceinline__ uint32_t pack_h2(float lo, float hi) { return h2_bits(__floats2half2_rn(lo, hi)); }
+
+// A group of 16 keys of one head in shared memory.
+template <int D>
+struct Group {
+    static constexpr int kCodes = 16 * D / 2, kScales = 16 * D / 16;
+    static constexpr int kK = 0, kKs = kCodes, kV = kCodes + kScales, kVs = 2 * kCodes + kScales;
+    static constexpr int kBytes = 2 * (kCodes + kScales);
+};
+
+// Starts the copies of the 16 keys from j0 on (a whole group lies in one page);
+// zeros where the table names no page. K alone where !WITH_V.
+template <int D, bool WITH_V>
+__device__ __forceinline__ void load_group(const CachePages& c, int b, int h, int j0, uint32_t dst, int32_t* err)
+{
+    using G = Group<D>;
+    const int lane = threadIdx.x & 31;
+    const int32_t page = cache_page(c.table, c.width, c.num_pages, c.page_shift, b, j0);
+    const bool ok = page >= 0;
+    if (!ok && lane == 0) atomicOr(err, kErrBounds);
+    const int64_t row = cache_row(ok ? page : 0, c.hkv, h, c.page_shift, j0 & ((1 << c.page_shift) - 1));
+#pragma unroll
+    for (int t = 0; t < (WITH_V ? 2 : 1); ++t) {
+        const uint8_t* codes = c.codes[t] + row * (D / 2);
+        const uint8_t* scales = c.scales[t] + row * (D / 16);
+        const uint32_t d = dst + (t ? G::kV : G::kK), ds = dst + (t ? G::kVs : G::kKs);
+#pragma unroll
+        for (int i = 0; i < G::kCodes / 512; ++i)
+            copy_async16(d + (i * 32 + lane) * 16, codes + (i * 32 + lane) * 16, ok);
+        if (lane < G::kScales / 16) copy_async16(ds + lane * 16, scales + lane * 16, ok);
+    }
+}
+
+// B operands of 8 query rows (columns of the contraction): lane (g, c) holds row
+// g's channels [c * D/4, (c + 1) * D/4) as f16, scaled by a power of two that puts
+// the row's largest magnitude at about 2^10 (no bf16 value that matters to the
+// sums leaves f16's range). `back` receives what undoes the scaling. A row with an
+// infinite or NaN channel has no finite score: it is NaN throughout.
+template <int D, bool FP8>
+__device__ __forceinline__ void load_q(const void* q, int64_t at, bool real, uint32_t (&f)[D / 8], float& back)
+{
+    constexpr int N = D / 4;
+    back = 1.f;
+    if constexpr (FP8) {
+        const uint4* s = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(q) + at);
+#pragma unroll
+        for (int i = 0; i < N / 16; ++i) {
+            const uint4 v = real ? __ldg(s + i) : make_uint4(0u, 0u, 0u, 0u);
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int k = 0; k < 8; ++k) f[i * 8 + k] = h2_bits(e4m3x2_value(w[k / 2] >> (16 * (k & 1))));
+        }
+    } else {
+        float x[N];
+        const uint4* s = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(q) + at);
+        float top = 0.f;
+        bool bad = false;
+#pragma unroll
+        for (int i = 0; i < N / 8; ++i) {
+            const uint4 v = real ? __ldg(s + i) : make_uint4(0u, 0u, 0u, 0u);
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                x[i * 8 + 2 * k] = __uint_as_float(w[k] << 16);
+                x[i * 8 + 2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            top = fmaxf(top, fabsf(x[i]));
+            bad |= !(fabsf(x[i]) <= 3.4028234e38f);
+        }
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const uint32_t any_bad = __ballot_sync(0xffffffffu, bad);
+        bad = (any_bad >> (threadIdx.x & 28)) & 15u;
+        // exponent field of the factor: 127 + 10 - (that of top - 127), at most 2^126
+        const int e = min(264 - (int)(__float_as_uint(top) >> 23), 253);
+        const float up = bad ? __int_as_float(0x7FC00000) : __int_as_float(e << 23);
+        back = __int_as_float((254 - e) << 23);
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) f[i] = pack_h2(x[2 * i] * up, x[2 * i + 1] * up);
+    }
+}
+
+// Scores of a group's 16 keys against the tile's rows: S^T[key][row], unscaled.
+template <int D, int NT, typename QF>
+__device__ __forceinline__ void score_group(const uint8_t* grp, int lane, QF qf, float (&s)[NT][4])
+{
+    using G = Group<D>;
+    const int g = lane >> 2, c = lane & 3;
+    constexpr int WORDS = D / 32;  // words of 8 codes of a lane's D/4 channels
+    uint32_t w0[WORDS], w1[WORDS];
+    __half2 s0[(WORDS + 1) / 2], s1[(WORDS + 1) / 2];
+    if constexpr (D == 128) {
+        const uint4 a = *reinterpret_cast<const uint4*>(grp + G::kK + g * 64 + c * 16);
+        const uint4 b = *reinterpret_cast<const uint4*>(grp + G::kK + (g + 8) * 64 + c * 16);
+        w0[0] = a.x, w0[1] = a.y, w0[2] = a.z, w0[3] = a.w;
+        w1[0] = b.x, w1[1] = b.y, w1[2] = b.z, w1[3] = b.w;
+        const __half2 x = e4m3x2_value(*reinterpret_cast<const uint16_t*>(grp + G::kKs + g * 8 + c * 2));
+        const __half2 y = e4m3x2_value(*reinterpret_cast<const uint16_t*>(grp + G::kKs + (g + 8) * 8 + c * 2));
+        s0[0] = __low2half2(x), s0[1] = __high2half2(x);
+        s1[0] = __low2half2(y), s1[1] = __high2half2(y);
+    } else {
+        const uint2 a = *reinterpret_cast<const uint2*>(grp + G::kK + g * 32 + c * 8);
+        const uint2 b = *reinterpret_cast<const uint2*>(grp + G::kK + (g + 8) * 32 + c * 8);
+        w0[0] = a.x, w0[1] = a.y;
+        w1[0] = b.x, w1[1] = b.y;
+        s0[0] = __low2half2(e4m3x2_value(grp[G::kKs + g * 4 + c]));
+        s1[0] = __low2half2(e4m3x2_value(grp[G::kKs + (g + 8) * 4 + c]));
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[t][i] = 0.f;
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) {  // 4 channels of every lane
+        const int w = k / 2, sc = k / 4;
+        uint32_t a0, a1, a2, a3;
+        if (k & 1) {
+            a0 = h2_bits(__hmul2(e2m1x2_value<2>(w0[w]), s0[sc]));
+            a1 = h2_bits(__hmul2(e2m1x2_value<2>(w1[w]), s1[sc]));
+            a2 = h2_bits(__hmul2(e2m1x2_value<3>(w0[w]), s0[sc]));
+            a3 = h2_bits(__hmul2(e2m1x2_value<3>(w1[w]), s1[sc]));
+        } else {
+            a0 = h2_bits(__hmul2(e2m1x2_value<0>(w0[w]), s0[sc]));
+            a1 = h2_bits(__hmul2(e2m1x2_value<0>(w1[w]), s1[sc]));
+            a2 = h2_bits(__hmul2(e2m1x2_value<1>(w0[w]), s0[sc]));
+            a3 = h2_bits(__hmul2(e2m1x2_value<1>(w1[w]), s1[sc]));
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const uint2 q = qf(t, k);
+            mma16816(s[t], a0, a1, a2, a3, q.x, q.y);
+        }
+    }
+}
+
+// What every CTA of a request's tile needs to know of its rows.
+struct RowTile {
+    int len, t, row0, rows, last0;  // last0: position of the first query
+};
+
+__device__ __forceinline__ RowTile row_tile(const AttendArgs& a, int b, int tile, int per)
+{
+    RowTile r;
+    bool bad;
+    r.len = cache_len(a.lens[b], a.limit, bad);
+    if (bad && threadIdx.x == 0) atomicOr(a.err, kErrBounds);
+    r.t = a.q_off[b + 1] - a.q_off[b];
+    r.row0 = tile * per;
+    r.rows = min(per, r.t * a.group - r.row0);
+    r.last0 = r.len - r.t;
+    return r;
+}
+
+template <int D, int NT, bool FP8>
+__global__ void __launch_bounds__(kAttThreads) attend_split_kernel(const __grid_constant__ AttendArgs a)
+{
+    using G = Group<D>;
+    constexpr int ROWS = 8 * NT;
+    constexpr bool Q_SMEM = NT > 2;  // fragments of 32 rows would take 64 registers
+    constexpr int MT = D / 16;
+    // the rings; behind the loop the same memory takes a row tile of every warp's sums
+    constexpr int kRing = kAttWarps * kAttStages * G::kBytes, kJoin = kAttWarps * 8 * (D + 4) * 4;
+    __shared__ __align__(16) uint8_t ring[kRing > kJoin ? kRing : kJoin];
+    __shared__ float s_m[kAttWarps][ROWS], s_l[kAttWarps][ROWS];
+    __shared__ uint2 q_s[Q_SMEM ? NT * (D / 16) * 32 : 1];
+    __shared__ float back_s[Q_SMEM ? ROWS : 1];
+
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int g = lane >> 2, c = lane & 3;
+    const int b = blockIdx.z, h = blockIdx.y % a.cache.hkv, tile = blockIdx.y / a.cache.hkv;
+    griddep_wait();
+    griddep_launch_dependents();
+    const RowTile rt = row_tile(a, b, tile, ROWS);
+    if (rt.rows <= 0) return;
+    const int q0 = a.q_off[b];
+    const int i_last = (rt.row0 + rt.rows - 1) / a.group;
+    // keys that the tile's last row sees, and this CTA's part of them
+    const int seen = min(rt.len, rt.last0 + i_last + 1);
+    const int k0 = blockIdx.x * a.chunk, k1 = min(seen, k0 + a.chunk);
+    if (k0 >= k1 && blockIdx.x > 0) return;  // (the first chunk of a tile without keys writes its zeros)
+    const int all_see = rt.last0 + rt.row0 / a.group;  // the last key that every row sees
+
+    uint8_t* my = ring + warp * kAttStages * G::kBytes;
+    const uint32_t my_s = smem_u32(my);
+    const int groups = k1 > k0 ? (k1 - k0 + 15) / 16 : 0;
+    const int n_mine = groups > warp ? (groups - warp + kAttWarps - 1) / kAttWarps : 0;
+#pragma unroll
+    for (int i = 0; i < kAttStages - 1; ++i) {
+        if (i < n_mine)
+            load_group<D, true>(a.cache, b, h, k0 + (warp + i * kAttWarps) * 16, my_s + i * G::kBytes, a.err);
+        copy_async_commit();
+    }
+
+    // ---- the tile's rows
+    uint32_t qr[Q_SMEM ? 1 : NT][D / 8];
+    float fac[NT][2];  // log2-unit scale of rows 2c and 2c + 1
+    int vis[NT][2];    // last key they see
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int r = t * 8 + g;
+        const bool real = r < rt.rows;
+        const int row = rt.row0 + (real ? r : 0);
+        const int64_t at = (int64_t)(q0 + row / a.group) * a.q_stride + (int64_t)(h * a.group + row % a.group) * D +
+                           c * (D / 4);
+        float back;
+        if constexpr (Q_SMEM) {
+            if (t % kAttWarps == warp) {
+                uint32_t f[D / 8];
+                load_q<D, FP8>(a.q, at, real, f, back);
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) q_s[(t * (D / 16) + k) * 32 + lane] = make_uint2(f[2 * k], f[2 * k + 1]);
+                if (c == 0) back_s[r] = back;
+            }
+        } else {
+            load_q<D, FP8>(a.q, at, real, qr[t], back);
+            fac[t][0] = a.c_log2 * __shfl_sync(0xffffffffu, back, 8 * c);
+            fac[t][1] = a.c_log2 * __shfl_sync(0xffffffffu, back, 8 * c + 4);
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) vis[t][e] = rt.last0 + (rt.row0 + t * 8 + 2 * c + e) / a.group;
+    }
+    if constexpr (Q_SMEM) {
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            fac[t][0] = a.c_log2 * back_s[t * 8 + 2 * c];
+            fac[t][1] = a.c_log2 * back_s[t * 8 + 2 * c + 1];
+        }
+    }
+    auto qf = [&](int t, int k) -> uint2 {
+        if constexpr (Q_SMEM) return q_s[(t * (D / 16) + k) * 32 + lane];
+        else return make_uint2(qr[t][2 * k], qr[t][2 * k + 1]);
+    };
+
+    float o[NT][MT][4], m[NT][2], l[NT][2];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[t][i][e] = 0.f;
+        m[t][0] = m[t][1] = kNoRef;
+        l[t][0] = l[t][1] = 0.f;
+    }
+
+    bool nan_value = false;
+#pragma unroll 1
+    for (int n = 0; n < n_mine; ++n) {
+        copy_async_wait<kAttStages - 2>();
+        __syncwarp();  // every lane's copies are there, and the group before is no longer read
+        {
+            const int nx = n + kAttStages - 1;
+            if (nx < n_mine)
+                load_group<D, true>(a.cache, b, h, k0 + (warp + nx * kAttWarps) * 16,
+                                    my_s + (nx % kAttStages) * G::kBytes, a.err);
+            copy_async_commit();
+        }
+        const uint8_t* grp = my + (n % kAttStages) * G::kBytes;
+        const int j0 = k0 + (warp + n * kAttWarps) * 16;
+        const bool no_page =
+            cache_page(a.cache.table, a.cache.width, a.cache.num_pages, a.cache.page_shift, b, j0) < 0;
+        float s[NT][4];
+        score_group<D, NT>(grp, lane, qf, s);
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[t][e] *= fac[t][e & 1];
+        if (j0 + 15 > all_see || no_page) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (j0 + g + 8 * (e >> 1) > min(vis[t][e & 1], k1 - 1) || no_page) s[t][e] = -INFINITY;
+        }
+        bool move = false;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) move |= fmaxf(s[t][e], s[t][e + 2]) > m[t][e] + kRefSlack;
+        if (__any_sync(0xffffffffu, move)) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float x = fmaxf(s[t][e], s[t][e + 2]);
+                    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+                    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+                    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+                    const float mn = fmaxf(m[t][e], x);
+                    const float f = ex2(m[t][e] - mn);
+                    m[t][e] = mn;
+                    l[t][e] *= f;
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) {
+                        o[t][i][e] *= f;
+                        o[t][i][e + 2] *= f;
+                    }
+                }
+        }
+        uint32_t pb[NT][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            float p[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) p[e] = ex2(s[t][e] - m[t][e & 1]);
+            l[t][0] += p[0] + p[2];
+            l[t][1] += p[1] + p[3];
+            pb[t][0] = transpose8x8(pack_h2(p[0], p[1]));
+            pb[t][1] = transpose8x8(pack_h2(p[2], p[3]));
+        }
+        // ---- values: lane (g, c) takes keys 2c, 2c+1, 2c+8, 2c+9 and channels [g * D/8, (g + 1) * D/8)
+        constexpr int VW = D / 64;  // words of a lane's channels
+        uint32_t x[4][VW];
+        uint32_t sc[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int key = 2 * c + (e & 1) + 8 * (e >> 1);
+            if constexpr (D == 128) {
+                const uint2 v = *reinterpret_cast<const uint2*>(grp + G::kV + key * 64 + g * 8);
+                x[e][0] = v.x, x[e][1] = v.y;
+                sc[e] = grp[G::kVs + key * 8 + g];
+            } else {
+                x[e][0] = *reinterpret_cast<const uint32_t*>(grp + G::kV + key * 32 + g * 4);
+                sc[e] = grp[G::kVs + key * 4 + g / 2];
+            }
+            // what lies behind the last key may be anything, a NaN scale among it
+            if (j0 + key >= k1) sc[e] = 0u;
+            // a NaN value must not reach the rows that do not see it (0 * NaN): put in at the end
+            if (j0 + key > all_see && (sc[e] & 0x7Fu) == 0x7Fu) {
+                sc[e] = 0u;
+                nan_value = true;
+            }
+        }
+        const __half2 sa = e4m3x2_value(sc[0] | (sc[1] << 8)), sb = e4m3x2_value(sc[2] | (sc[3] << 8));
+#pragma unroll
+        for (int w = 0; w < VW; ++w) {
+            // bytes of (code of the first key, code of the second) for the even and the odd channels
+            const uint32_t lo = 0x0F0F0F0Fu;
+            const uint32_t ae = (x[0][w] & lo) | ((x[1][w] & lo) << 4), ao = ((x[0][w] >> 4) & lo) | (x[1][w] & ~lo);
+            const uint32_t be = (x[2][w] & lo) | ((x[3][w] & lo) << 4), bo = ((x[2][w] >> 4) & lo) | (x[3][w] & ~lo);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t a0 = h2_bits(__hmul2(e2m1x2_value<0>(ae >> (8 * i)), sa));
+                const uint32_t a1 = h2_bits(__hmul2(e2m1x2_value<0>(ao >> (8 * i)), sa));
+                const uint32_t a2 = h2_bits(__hmul2(e2m1x2_value<0>(be >> (8 * i)), sb));
+                const uint32_t a3 = h2_bits(__hmul2(e2m1x2_value<0>(bo >> (8 * i)), sb));
+#pragma unroll
+                for (int t = 0; t < NT; ++t) mma16816(o[t][w * 4 + i], a0, a1, a2, a3, pb[t][0], pb[t][1]);
+            }
+        }
+    }
+    copy_async_wait<0>();
+
+    // ---- the four warps joined, 8 rows at a time
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) l[t][e] += __shfl_xor_sync(0xffffffffu, l[t][e], d);
+            if (g == 0) {
+                s_m[warp][t * 8 + 2 * c + e] = m[t][e];
+                s_l[warp][t * 8 + 2 * c + e] = l[t][e];
+            }
+        }
+    nan_value = __syncthreads_or(nan_value);
+    float* jo = reinterpret_cast<float*>(ring);  // [warp][row][D + 4]
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                jo[(warp * 8 + 2 * c + (e & 1)) * (D + 4) + g * (D / 8) + 2 * i + (e >> 1)] = o[t][i][e];
+        __syncthreads();
+        for (int x = tid; x < 8 * D; x += kAttThreads) {
+            const int r = x / D, ch = x % D;
+            const int row = t * 8 + r;
+            if (row >= rt.rows) continue;
+            float M = kNoRef;
+#pragma unroll
+            for (int w = 0; w < kAttWarps; ++w) M = fmaxf(M, s_m[w][row]);
+            float L = 0.f, O = 0.f;
+#pragma unroll
+            for (int w = 0; w < kAttWarps; ++w) {
+                const float f = ex2(s_m[w][row] - M);
+                L += s_l[w][row] * f;
+                O += jo[(w * 8 + r) * (D + 4) + ch] * f;
+            }
+            const int rr = rt.row0 + row;
+            const int64_t at = (int64_t)(q0 + rr / a.group) * a.hq + h * a.group + rr % a.group;
+            if (nan_value) {
+                for (int j = max(k0, all_see + 1); j < min(k1, rt.last0 + rr / a.group + 1); ++j) {
+                    const int32_t page =
+                        cache_page(a.cache.table, a.cache.width, a.cache.num_pages, a.cache.page_shift, b, j);
+                    if (page < 0) continue;
+                    const int64_t at_row =
+                        cache_row(page, a.cache.hkv, h, a.cache.page_shift, j & ((1 << a.cache.page_shift) - 1));
+                    if ((a.cache.scales[1][at_row * (D / 16) + ch / 16] & 0x7Fu) == 0x7Fu) O = __int_as_float(0x7FC00000);
+                }
+            }
+            if (a.chunks == 1) {
+                // (a row that sees no key is 0; the comparison keeps a NaN sum)
+                a.out[at * D + ch] = __float2bfloat16_rn(L == 0.f ? 0.f : O / L * a.cache.scale[1]);
+                if (a.lse && ch == 0) a.lse[at] = L == 0.f ? INFINITY : M + log2f(L);
+            } else {
+                const int64_t part = at * a.chunks + blockIdx.x;
+                a.part_o[part * D + ch] = O;
+                if (ch == 0) a.part_ml[part] = make_float2(M, L);
+            }
+        }
+    }
+}
+
+// One row a warp: chunks joined under the largest reference.
+template <int D>
+__global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant__ AttendArgs a)
+{
+    const int lane = threadIdx.x & 31;
+    const int b = blockIdx.y;
+    griddep_wait();
+    griddep_launch_dependents();
+    bool bad;
+    const int len = cache_len(a.lens[b], a.limit, bad);
+    const int q0 = a.q_off[b], t = a.q_off[b + 1] - q0;
+    for (int r = blockIdx.x * 4 + (threadIdx.x >> 5); r < t * a.hq; r += gridDim.x * 4) {
+        const int i = r / a.hq;
+        const int64_t at = (int64_t)q0 * a.hq + r;
+        // chunks that the row's tile wrote: at least those with keys of the row
+        const int seen = len - t + i + 1;
+        const int n = seen > 0 ? (seen + a.chunk - 1) / a.chunk : 0;
+        float M = kNoRef;
+        for (int x = lane; x < n; x += 32) M = fmaxf(M, a.part_ml[at * a.chunks + x].x);
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+        float L = 0.f, O[D / 32];
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) O[e] = 0.f;
+        for (int x = 0; x < n; ++x) {
+            const float2 ml = a.part_ml[at * a.chunks + x];
+            const float f = ex2(ml.x - M);
+            L += ml.y * f;
+            const float* p = a.part_o + (at * a.chunks + x) * D + lane * (D / 32);
+            if constexpr (D == 128) {
+                const float4 v = *reinterpret_cast<const float4*>(p);
+                O[0] += v.x * f, O[1] += v.y * f, O[2] += v.z * f, O[3] += v.w * f;
+            } else {
+                const float2 v = *reinterpret_cast<const float2*>(p);
+                O[0] += v.x * f, O[1] += v.y * f;
+            }
+        }
+        const float vs = a.cache.scale[1];
+#pragma unroll
+        for (int e = 0; e < D / 32; e += 2) {
+            const float v0 = L == 0.f ? 0.f : O[e] / L * vs, v1 = L == 0.f ? 0.f : O[e + 1] / L * vs;
+            *reinterpret_cast<__nv_bfloat162*>(a.out + at * D + lane * (D / 32) + e) = __floats2bfloat162_rn(v0, v1);
+        }
+        if (a.lse && lane == 0) a.lse[at] = L == 0.f ? INFINITY : M + log2f(L);
+    }
+}
+
+// A CTA: 64 keys of a request, a warp 16 of them; all key heads, their rows 8 at a time.
+template <int D, bool FP8>
+__global__ void __launch_bounds__(kAttThreads) attend_weight_kernel(const __grid_constant__ AttendArgs a)
+{
+    using G = Group<D>;
+    __shared__ __align__(16) uint8_t ring[kAttWarps][2][G::kBytes / 2];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int g = lane >> 2, c = lane & 3;
+    const int b = blockIdx.y;
+    griddep_wait();
+    griddep_launch_dependents();
+    const RowTile rt = row_tile(a, b, 0, 8);
+    const int j0 = (blockIdx.x * kAttWarps + warp) * 16;
+    if (j0 >= rt.len) return;
+    const int32_t page = cache_page(a.cache.table, a.cache.width, a.cache.num_pages, a.cache.page_shift, b, j0);
+    if (page < 0) return;
+    const int q0 = a.q_off[b], rows = rt.t * a.group;
+    // rows that see a key of the group: the queries from the first that stands at or behind j0
+    const int r_first = max(0, j0 - rt.last0) * a.group;
+    const uint32_t dst = smem_u32(&ring[warp][0][0]);
+    load_group<D, false>(a.cache, b, 0, j0, dst, a.err);
+    copy_async_commit();
+    float sum[2] = {0.f, 0.f};  // of the keys g and g + 8, over the lane's rows
+    for (int h = 0; h < a.cache.hkv; ++h) {
+        if (h + 1 < a.cache.hkv)
+            load_group<D, false>(a.cache, b, h + 1, j0, dst + ((h + 1) & 1) * (G::kBytes / 2), a.err);
+        copy_async_commit();
+        copy_async_wait<1>();
+        __syncwarp();
+        for (int r0 = r_first & ~7; r0 < rows; r0 += 8) {
+            const bool real = r0 + g < rows;
+            const int row = real ? r0 + g : r0;
+            uint32_t q[D / 8];
+            float back;
+            load_q<D, FP8>(a.q, (int64_t)(q0 + row / a.group) * a.q_stride +
+                                    (int64_t)(h * a.group + row % a.group) * D + c * (D / 4),
+                           real, q, back);
+            float s[1][4];
+            score_group<D, 1>(&ring[warp][h & 1][0], lane, [&](int, int k) { return make_uint2(q[2 * k], q[2 * k + 1]); },
+                              s);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float fac = a.c_log2 * __shfl_sync(0xffffffffu, back, 8 * c + 4 * e);
+                const int r = r0 + 2 * c + e;
+                if (r >= rows) continue;
+                const int vis = rt.last0 + r / a.group;
+                const float lse = a.lse[(int64_t)(q0 + r / a.group) * a.hq + h * a.group + r % a.group];
+                if (j0 + g <= vis) sum[0] += ex2(fmaf(s[0][e], fac, -lse));
+                if (j0 + g + 8 <= vis) sum[1] += ex2(fmaf(s[0][e + 2], fac, -lse));
+            }
+        }
+        __syncwarp();
+    }
+    copy_async_wait<0>();
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        sum[e] += __shfl_xor_sync(0xffffffffu, sum[e], 1);
+        sum[e] += __shfl_xor_sync(0xffffffffu, sum[e], 2);
+        const int j = j0 + g + 8 * e;
+        if (c == 0 && j < rt.len) {
+            const int64_t at = ((int64_t)page << a.cache.page_shift) + (j & ((1 << a.cache.page_shift) - 1));
+            a.weights_out[at] = a.weights_in[at] + sum[e] / (float)a.hq;
+        }
+    }
+}
+
+template <int D, bool FP8>
+cudaError_t launch_all(const AttendArgs& a, const AttendPlan& plan, int max_rows, int64_t total_rows, int max_len,
+                       cudaStream_t stream, int32_t* launches)
+{
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1] = {pdl_attribute()};
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    cfg.stream = stream;
+    cudaError_t e = cudaSuccess;
+    if (total_rows > 0) {
+        const int tiles = (max_rows + plan.row_tile - 1) / plan.row_tile;
+        cfg.gridDim = dim3((unsigned)plan.chunks, (unsigned)(tiles * a.cache.hkv), (unsigned)a.batch);
+        cfg.blockDim = dim3(kAttThreads, 1, 1);
+        auto kern = plan.row_tile == 8    ? attend_split_kernel<D, 1, FP8>
+                    : plan.row_tile == 16 ? attend_split_kernel<D, 2, FP8>
+                                          : attend_split_kernel<D, 4, FP8>;
+        e = cudaLaunchKernelEx(&cfg, kern, a);
+        if (e != cudaSuccess) return e;
+        ++*launches;
+        if (plan.chunks > 1) {
+            const int most = max_rows / a.group * a.hq;
+            cfg.gridDim = dim3((unsigned)((most + 3) / 4), (unsigned)a.batch, 1);
+            cfg.blockDim = dim3(128, 1, 1);
+            e = cudaLaunchKernelEx(&cfg, attend_join_kernel<D>, a);
+            if (e != cudaSuccess) return e;
+            ++*launches;
+        }
+    }
+    if (a.weights_out && max_len > 0) {
+        cfg.gridDim = dim3((unsigned)((max_len + 63) / 64), (unsigned)a.batch, 1);
+        cfg.blockDim = dim3(kAttThreads, 1, 1);
+        e = cudaLaunchKernelEx(&cfg, attend_weight_kernel<D, FP8>, a);
+        if (e != cudaSuccess) return e;
+        ++*launches;
+    }
+    return e;
+}
+
+}  // namespace
+
+AttendPlan plan_cache_attend(int batch, int hkv, int max_rows, int64_t max_len, int num_sms)
+{
+    AttendPlan p;
+    p.row_tile = max_rows <= 8 ? 8 : (max_rows <= 16 ? 16 : 32);
+    const int64_t tiles = (max_rows + p.row_tile - 1) / p.row_tile;
+    const int64_t items = (tiles > 0 ? tiles : 1) * hkv * (batch > 0 ? batch : 1);
+    // chunks: enough CTAs for about four on every SM, none shorter than 64 keys
+    int64_t chunks = ((int64_t)num_sms * 4 + items - 1) / items;
+    const int64_t units = max_len > 0 ? (max_len + 63) / 64 : 1;
+    if (chunks > units) chunks = units;
+    const int64_t per = (units + chunks - 1) / chunks;
+    p.chunk = (int32_t)(per * 64);
+    p.chunks = (int32_t)((units + per - 1) / per);
+    return p;
+}
+
+cudaError_t launch_cache_attend(const AttendArgs& a, const AttendPlan& plan, int head_dim, bool fp8, int max_rows,
+                                int64_t total_rows, int max_len, cudaStream_t stream, int32_t* launches)
+{
+    *launches = 0;
+    if (fp8) return launch_all<128, true>(a, plan, max_rows, total_rows, max_len, stream, launches);
+    return head_dim == 128 ? launch_all<128, false>(a, plan, max_rows, total_rows, max_len, stream, launches)
+                           : launch_all<64, false>(a, plan, max_rows, total_rows, max_len, stream, launches);
+}
+
+}  // namespace lvs

@@ -17,12 +17,17 @@
 #include <Python.h>
 #include <stdint.h>
 
-enum { F_SCORE, F_FULL, F_SCORE_TOPK, F_TOPK, F_COMPACT, F_SPLICE, F_PROJECT, F_KEEP, F_COUNT };
+enum { F_SCORE, F_FULL, F_SCORE_TOPK, F_TOPK, F_COMPACT, F_SPLICE, F_PROJECT, F_KEEP,
+       F_APPEND, F_SPACE, F_ATTEND, F_EVICT, F_VERIFY, F_COUNT };
 static const char *const kNames[F_COUNT] = {"score", "score_full_keys", "score_topk", "topk",
-                                            "compact", "splice", "project", "keep_offsets"};
+                                            "compact", "splice", "project", "keep_offsets",
+                                            "cache_append", "cache_attend_workspace", "cache_attend", "cache_evict",
+                                            "verify"};
 /* h handle / stream, i int32, l int64, f float, p pointer, n host int32 array */
 static const char *const kSigs[F_COUNT] = {"hippnppnffph", "hippnppnppnpffph", "hippnppnffppnfppph", "hippnpnfppph",
-                                           "", "hippnppnppnppnlpppph", "hliipppfippifph", ""};
+                                           "", "hippnppnppnppnlpppph", "hliipppfippifph", "",
+                                           "hippipplpllppnffpppph", "", "hippipplpnifpppplh", "hippipiiiipippph",
+                                           "hiiippnpppppph"};
 static void *g_fn[F_COUNT];
 static PyObject *g_host_i32;      /* the binding's conversion of a host offset array */
 static PyObject *g_ndarray;       /* numpy.ndarray */
@@ -252,6 +257,70 @@ static PyObject *f_project(PyObject *self, PyObject *const *args, Py_ssize_t n)
     END
 }
 
+static PyObject *f_append(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    BEGIN(F_APPEND)
+    rc = ((int (*)(P, I, P, P, I, P, P, int64_t, P, int64_t, int64_t, P, P, P, float, float, P, P, P, P, P))
+          g_fn[F_APPEND])(
+        a[0].p, a[1].i, a[2].p, a[3].p, a[4].i, a[5].p, a[6].p, a[7].l, a[8].p, a[9].l, a[10].l, a[11].p,
+        a[12].p, a[13].p, a[14].f, a[15].f, a[16].p, a[17].p, a[18].p, a[19].p, a[20].p);
+    END
+}
+
+static PyObject *f_attend(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    BEGIN(F_ATTEND)
+    rc = ((int (*)(P, I, P, P, I, P, P, int64_t, P, P, I, float, P, P, P, P, int64_t, P))
+          g_fn[F_ATTEND])(
+        a[0].p, a[1].i, a[2].p, a[3].p, a[4].i, a[5].p, a[6].p, a[7].l, a[8].p, a[9].p, a[10].i, a[11].f,
+        a[12].p, a[13].p, a[14].p, a[15].p, a[16].l, a[17].p);
+    END
+}
+
+static PyObject *f_evict(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    BEGIN(F_EVICT)
+    rc = ((int (*)(P, I, P, P, I, P, I, I, I, I, P, I, P, P, P, P))
+          g_fn[F_EVICT])(
+        a[0].p, a[1].i, a[2].p, a[3].p, a[4].i, a[5].p, a[6].i, a[7].i, a[8].i, a[9].i, a[10].p, a[11].i,
+        a[12].p, a[13].p, a[14].p, a[15].p);
+    END
+}
+
+static PyObject *f_verify(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    BEGIN(F_VERIFY)
+    rc = ((int (*)(P, I, I, I, P, P, P, P, P, P, P, P, P, P))
+          g_fn[F_VERIFY])(
+        a[0].p, a[1].i, a[2].i, a[3].i, a[4].p, a[5].p, a[6].p, a[7].p, a[8].p, a[9].p, a[10].p, a[11].p,
+        a[12].p, a[13].p);
+    END
+}
+
+/* attend_bytes(handle, batch, q_offsets_h, max_len): bytes of an attention call's workspace, or -status */
+static PyObject *f_attend_bytes(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    (void)self;
+    if (n != 4) {
+        PyErr_SetString(PyExc_TypeError, "attend_bytes takes four arguments");
+        return NULL;
+    }
+    Held h;
+    h.nbuf = h.nobj = 0;
+    const int32_t *off;
+    uint64_t hd, batch, len;
+    if (as_bits(args[0], 'h', &hd) || as_bits(args[1], 'i', &batch) || as_host_i32(args[2], &h, &off, NULL) ||
+        as_bits(args[3], 'i', &len)) {
+        release(&h);
+        return NULL;
+    }
+    int64_t bytes = 0;
+    const int rc = ((int (*)(P, I, const int32_t *, I, int64_t *))g_fn[F_SPACE])(
+        (P)(uintptr_t)hd, (I)(uint32_t)batch, off, (I)(uint32_t)len, &bytes);
+    release(&h);
+    return PyLong_FromLongLong(rc ? -(long long)rc : (long long)bytes);
+}
+
 /* compact(handle, total_kept, kept_idx, src_rows, srcs, dsts, row_bytes, stream): the three are lists */
 static PyObject *f_compact(PyObject *self, PyObject *const *args, Py_ssize_t n)
 {
@@ -333,6 +402,7 @@ static PyObject *f_bind(PyObject *self, PyObject *const *args, Py_ssize_t n)
     }
     for (int k = 0; k < F_COUNT; ++k) {
         PyObject *v = PyDict_GetItemString(args[0], kNames[k]);
+        if (!v && k > F_KEEP && g_fn[k]) continue; /* these keep the address of an earlier bind */
         if (!v) {
             PyErr_Format(PyExc_KeyError, "%s", kNames[k]);
             return NULL;
@@ -353,7 +423,9 @@ static PyObject *f_bind(PyObject *self, PyObject *const *args, Py_ssize_t n)
 static PyMethodDef kMethods[] = {DEF("bind", f_bind), DEF("score", f_score), DEF("score_full_keys", f_full),
                                  DEF("score_topk", f_score_topk), DEF("topk", f_topk), DEF("compact", f_compact),
                                  DEF("splice", f_splice), DEF("project", f_project),
-                                 DEF("keep_total", f_keep_total), {NULL, NULL, 0, NULL}};
+                                 DEF("keep_total", f_keep_total), DEF("cache_append", f_append),
+                                 DEF("cache_attend", f_attend), DEF("attend_bytes", f_attend_bytes),
+                                 DEF("cache_evict", f_evict), DEF("verify", f_verify), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_fastcall", NULL, -1, kMethods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__fastcall(void)

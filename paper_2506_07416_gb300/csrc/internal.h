@@ -124,6 +124,91 @@ cudaError_t launch_fold_norm(const __nv_bfloat16* w, const float* gamma, __nv_bf
                              int hidden, int num_sms, cudaStream_t stream);
 cudaError_t launch_rope_table(const RopeArgs& a, int num_sms, cudaStream_t stream);
 
+// The 4-bit K/V cache: pages of e2m1 codes and e4m3 scales, for each key head
+// page_size rows (index 0: K, 1: V).
+struct CachePages {
+    uint8_t* codes[2];        // [num_pages][hkv][page_size][d / 2]
+    uint8_t* scales[2];       // [num_pages][hkv][page_size][d / 16]
+    float scale[2];           // one float scale per tensor
+    int32_t num_pages, page_shift, hkv;
+    const int32_t* table;     // [batch][width] pages of each request
+    int32_t width;
+};
+
+// cache_append.cu
+struct AppendArgs {
+    CachePages cache;
+    const void* src[2];       // rows [src_rows][hkv][d], bf16 or e4m3 codes
+    int64_t stride[2];        // elements from a row to the next
+    const int32_t* row_idx;   // source row of each new token (null: token r has row r)
+    int64_t src_rows, rows;
+    const int32_t* lens;      // [batch] tokens cached before the call
+    const int32_t* off;       // [batch+1] prefix of the new tokens
+    int32_t batch, limit;     // limit: tokens a request's pages hold
+    float in_scale[2], inv_scale[2];
+    __nv_bfloat16* stored[2]; // [rows][hkv][d] values that the codes stand for, or null
+    float* weights;           // [num_pages][page_size], 0 for the new tokens; or null
+    int32_t* new_lens;        // [batch]
+    int32_t* err;
+};
+cudaError_t launch_cache_append(const AppendArgs& a, int head_dim, bool fp8, int num_sms, cudaStream_t stream);
+
+// cache_attend.cu
+struct AttendArgs {
+    CachePages cache;
+    const void* q;            // [rows][hq][d] bf16 or e4m3 codes
+    int64_t q_stride;         // elements from a row to the next
+    const int32_t* q_off;     // [batch+1] prefix of the queries
+    const int32_t* lens;      // [batch]
+    int32_t batch, hq, group; // group: query heads of a key head
+    int32_t limit;            // no request is longer
+    float c_log2;             // q_scale * k_scale / sqrt(d) * log2(e)
+    int32_t chunk, chunks;    // keys of a chunk (a multiple of 64), chunks of the longest request
+    __nv_bfloat16* out;       // [rows][hq][d]
+    float* part_o;            // [rows * hq][chunks][d] (chunks > 1)
+    float2* part_ml;          // [rows * hq][chunks] reference and sum
+    float* lse;               // [rows * hq] log2 of the sum of 2^s (with weights)
+    const float* weights_in;  // [num_pages][page_size]
+    float* weights_out;       // null: no weights
+    int32_t* err;
+};
+struct AttendPlan {
+    int32_t row_tile;         // rows (query x head of a key head) of a CTA: 8, 16 or 32
+    int32_t chunk, chunks;
+};
+AttendPlan plan_cache_attend(int batch, int hkv, int max_rows, int64_t max_len, int num_sms);
+cudaError_t launch_cache_attend(const AttendArgs& a, const AttendPlan& plan, int head_dim, bool fp8, int max_rows,
+                                int64_t total_rows, int max_len, cudaStream_t stream, int32_t* launches);
+
+// cache_evict.cu
+struct EvictArgs {
+    CachePages cache;
+    const int32_t* lens;
+    int32_t batch, limit, budget, sink, recent;
+    const int32_t* to_table;  // [batch][to_width] pages that the kept rows move to (the cache's own: in place)
+    int32_t to_width;
+    float* weights;
+    int32_t* kept;            // [batch][budget]
+    int32_t* new_lens;        // [batch]
+    int32_t* err;
+};
+cudaError_t launch_cache_evict(const EvictArgs& a, int head_dim, int num_sms, cudaStream_t stream, int32_t* launches);
+
+// verify.cu
+struct VerifyArgs {
+    const int32_t* tokens;    // [sum T] drafted tokens
+    const int32_t* off;       // [batch+1] prefix of T
+    const void* p;            // [sum T + batch][vocab] the target's probabilities
+    const void* q;            // [sum T][vocab] the draft's, or null (certain of its token)
+    const float* u;           // [sum T]
+    const float* u_last;      // [batch]
+    int32_t batch, vocab;
+    int32_t* accepted;        // [batch]
+    int32_t* out;             // [sum T + batch]
+    int32_t* err;
+};
+cudaError_t launch_verify(const VerifyArgs& a, bool bf16, cudaStream_t stream);
+
 // splice.cu
 struct SpliceArgs {
     const int32_t* sys_off;   // device [batch+1]

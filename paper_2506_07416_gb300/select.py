@@ -28,6 +28,13 @@ STATUS = {0: "OK", 1: "INVALID_ARG", 2: "UNSUPPORTED", 3: "WORKSPACE", 4: "CUDA"
 DTYPES = {"bf16": 0, "e4m3": 1}
 
 
+class Cache(ctypes.Structure):
+    """litevlm_cache_t"""
+    _fields_ = [("k_codes", ctypes.c_void_p), ("k_scales", ctypes.c_void_p), ("v_codes", ctypes.c_void_p),
+                ("v_scales", ctypes.c_void_p), ("num_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("k_scale", ctypes.c_float), ("v_scale", ctypes.c_float)]
+
+
 class LitevlmError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"{STATUS.get(status, status)}: {message}")
@@ -70,11 +77,18 @@ def _load():
     lib.litevlm_select_splice.argtypes = [P, i32, P, P, P, P, P, P, P, P, P, P, P, P, i64, P, P, P, P, P]
     lib.litevlm_select_score_noalloc.argtypes = [i32, i32, i32, i32, i32, P, P, P, P, P, P, f32, f32, P, P, P]
     lib.litevlm_select_keep_offsets.argtypes = [i32, P, P, f32, P]
+    lib.litevlm_select_cache_append.argtypes = [P, i32, P, P, i32, P, P, i64, P, i64, i64, P, P, P, f32, f32, P, P, P,
+                                                P, P]
+    lib.litevlm_select_cache_attend_workspace.argtypes = [P, i32, P, i32, ctypes.POINTER(i64)]
+    lib.litevlm_select_cache_attend.argtypes = [P, i32, P, P, i32, P, P, i64, P, P, i32, f32, P, P, P, P, i64, P]
+    lib.litevlm_select_cache_evict.argtypes = [P, i32, P, P, i32, P, i32, i32, i32, i32, P, i32, P, P, P, P]
+    lib.litevlm_select_verify.argtypes = [P, i32, i32, i32, P, P, P, P, P, P, P, P, P, P]
     lib.litevlm_select_set_wait_budget.argtypes = [P, i64]
     lib.litevlm_select_set_debug_flags.argtypes = [P, i32]
     for fn in ("create", "destroy", "score", "score_full_keys", "topk", "compact", "check_device", "score_plan",
                "score_noalloc", "splice", "views", "fold_norm", "rope_table", "project", "score_topk", "host_view",
-               "keep_offsets", "set_wait_budget", "set_debug_flags"):
+               "keep_offsets", "cache_append", "cache_attend_workspace", "cache_attend", "cache_evict", "verify",
+               "set_wait_budget", "set_debug_flags"):
         getattr(lib, "litevlm_select_" + fn).restype = ctypes.c_int
     return lib
 
@@ -88,7 +102,9 @@ EXPORTS = ["litevlm_select_create", "litevlm_select_destroy", "litevlm_select_la
            "litevlm_select_splice", "litevlm_select_score_full_keys", "litevlm_select_views",
            "litevlm_select_fold_norm", "litevlm_select_rope_table", "litevlm_select_project",
            "litevlm_select_last_launches", "litevlm_select_score_topk", "litevlm_select_host_view",
-           "litevlm_select_keep_offsets", "litevlm_select_set_wait_budget", "litevlm_select_set_debug_flags"]
+           "litevlm_select_keep_offsets", "litevlm_select_cache_append", "litevlm_select_cache_attend_workspace",
+           "litevlm_select_cache_attend", "litevlm_select_cache_evict", "litevlm_select_verify",
+           "litevlm_select_set_wait_budget", "litevlm_select_set_debug_flags"]
 FLAGS = {"auto": 0, "reread": 1, "resident": 2, "resident_1buf": 8, "resident_2buf": 16, "resident_flat": 64}
 # LITEVLM_FLAG_SCORE_SPLIT_QUERIES: resident plans for T > 64 run each head's text rows as two pseudo-heads
 QUERY_SPLIT = {"whole": 0, "split": 128}
@@ -158,7 +174,8 @@ def _load_fastcall():
         raise ImportError(f"_fastcall.so is not built; run __graft_entry__.build() ({e})") from e
     _fastcall.bind({n: ctypes.cast(getattr(LIB, "litevlm_select_" + n), ctypes.c_void_p).value
                     for n in ("score", "score_full_keys", "score_topk", "topk", "compact", "splice", "project",
-                              "keep_offsets")}, _host_i32, np.ndarray, _ctypes_value)
+                              "keep_offsets", "cache_append", "cache_attend_workspace", "cache_attend", "cache_evict",
+                              "verify")}, _host_i32, np.ndarray, _ctypes_value)
     return _fastcall
 
 
@@ -279,6 +296,51 @@ def splice(handle: int, batch: int, sys_rows, sys_offsets_d, sys_offsets_h, vis_
         _check(rc, handle)
 
 
+def cache_append(handle: int, batch: int, cache, table, table_width: int, seq_lens, k, k_row_stride: int, v,
+                 v_row_stride: int, src_rows: int, row_idx, new_offsets_d, new_offsets_h, k_in_scale: float,
+                 v_in_scale: float, weights, k_stored, v_stored, new_lens, stream=None) -> None:
+    """litevlm_select_cache_append; cache: the address of a litevlm_cache_t (KVCache.struct)."""
+    rc = _FC.cache_append(handle, batch, cache, table, table_width, seq_lens, k, k_row_stride, v, v_row_stride, src_rows,
+                          row_idx, new_offsets_d, new_offsets_h, k_in_scale, v_in_scale, weights, k_stored, v_stored,
+                          new_lens, _stream_ptr(stream))
+    if rc:
+        _check(rc, handle)
+
+
+def cache_attend_workspace(handle: int, batch: int, q_offsets_h, max_len: int) -> int:
+    """litevlm_select_cache_attend_workspace: bytes of the workspace of an attention call."""
+    n = _FC.attend_bytes(handle, batch, q_offsets_h, max_len)
+    if n < 0:
+        _check(-n, handle)
+    return n
+
+
+def cache_attend(handle: int, batch: int, cache, table, table_width: int, seq_lens, q, q_row_stride: int, q_offsets_d,
+                 q_offsets_h, max_len: int, q_scale: float, weights_in, weights_out, out, workspace,
+                 workspace_bytes: int, stream=None) -> None:
+    rc = _FC.cache_attend(handle, batch, cache, table, table_width, seq_lens, q, q_row_stride, q_offsets_d, q_offsets_h,
+                          max_len, q_scale, weights_in, weights_out, out, workspace, workspace_bytes,
+                          _stream_ptr(stream))
+    if rc:
+        _check(rc, handle)
+
+
+def cache_evict(handle: int, batch: int, cache, table, table_width: int, seq_lens, max_len: int, budget: int, sink: int,
+                recent: int, to_table, to_width: int, weights, kept_idx, new_lens, stream=None) -> None:
+    rc = _FC.cache_evict(handle, batch, cache, table, table_width, seq_lens, max_len, budget, sink, recent, to_table,
+                         to_width, weights, kept_idx, new_lens, _stream_ptr(stream))
+    if rc:
+        _check(rc, handle)
+
+
+def verify(handle: int, batch: int, vocab: int, prob_bf16: int, draft_tokens, draft_offsets_d, draft_offsets_h,
+           target_probs, draft_probs, u_accept, u_sample, accepted, tokens, stream=None) -> None:
+    rc = _FC.verify(handle, batch, vocab, prob_bf16, draft_tokens, draft_offsets_d, draft_offsets_h, target_probs,
+                    draft_probs, u_accept, u_sample, accepted, tokens, _stream_ptr(stream))
+    if rc:
+        _check(rc, handle)
+
+
 def host_view(handle: int, host_ptr: int) -> int:
     """litevlm_select_host_view: the device address of pinned host memory."""
     out = ctypes.c_void_p()
@@ -344,6 +406,89 @@ def score_plan(handle: int, batch: int, text_offsets_h, seq_offsets_h):
 # convenience object (allocates outputs with torch; still marshalling only)
 # ----------------------------------------------------------------------------
 
+def _refuse(message: str):
+    raise LitevlmError(1, message)
+
+
+def _want(name: str, t, dtype, shape, device: int):
+    """A contiguous CUDA tensor of this type, shape (None: any size) and device, or an error."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device.type != "cuda" or t.device.index != device:
+        _refuse(f"{name} must be a {dtype} tensor on cuda:{device}")
+    if t.dim() != len(shape) or any(w is not None and n != w for n, w in zip(t.shape, shape)):
+        _refuse(f"{name} must have the shape {tuple('any' if w is None else w for w in shape)}, not {tuple(t.shape)}")
+    if not t.is_contiguous():
+        _refuse(f"{name} must be contiguous")
+    return t
+
+
+def _row_stride(name: str, t, dtype, heads: int, d: int, device: int) -> int:
+    """Elements from a row to the next of [rows, heads, d] rows, whose channels and heads lie side by side."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device.type != "cuda" or t.device.index != device:
+        _refuse(f"{name} must be a {dtype} tensor on cuda:{device}")
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != d:
+        _refuse(f"{name} must have the shape (any, {heads}, {d}), not {tuple(t.shape)}")
+    stride = t.stride()
+    if stride[2] != 1 or (heads > 1 and stride[1] != d):
+        _refuse(f"{name}'s heads and channels must lie side by side (only the row stride is free)")
+    return stride[0] if t.shape[0] > 1 else heads * d
+
+
+class KVCache:
+    """The tensors of a 4-bit K/V cache (litevlm_cache_t), uint8 CUDA tensors: codes [pages, Hkv, page_size, d/2],
+    scales [pages, Hkv, page_size, d/16]; weights: float32 [pages, page_size] or None. ``Selector.cache`` makes one."""
+
+    def __init__(self, k_codes, k_scales, v_codes, v_scales, k_scale: float = 1.0, v_scale: float = 1.0, weights=None):
+        import torch
+        if not isinstance(k_codes, torch.Tensor) or k_codes.dim() != 4 or k_codes.device.type != "cuda":
+            _refuse("k_codes must be a CUDA tensor [pages, Hkv, page_size, d/2]")
+        self.num_pages, self.heads, self.page_size = k_codes.shape[:3]
+        self.head_dim = 2 * k_codes.shape[3]
+        self.device = k_codes.device.index
+        codes, scales = tuple(k_codes.shape), (*k_codes.shape[:3], self.head_dim // 16)
+        for name, t, shape in (("k_codes", k_codes, codes), ("v_codes", v_codes, codes), ("k_scales", k_scales, scales),
+                               ("v_scales", v_scales, scales)):
+            _want(name, t, torch.uint8, shape, self.device)
+        if weights is not None:
+            _want("weights", weights, torch.float32, (self.num_pages, self.page_size), self.device)
+        self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
+        self.k_scale, self.v_scale, self.weights = float(k_scale), float(v_scale), weights
+        self._c = Cache(k_codes.data_ptr(), k_scales.data_ptr(), v_codes.data_ptr(), v_scales.data_ptr(),
+                        self.num_pages, self.page_size, self.k_scale, self.v_scale)
+        self.struct = ctypes.addressof(self._c)
+
+
+class _NoContext:
+    def __enter__(self):
+        return None
+
+    def __exit__(self, *a):
+        return False
+
+
+_HERE = _NoContext()
+
+
+def _allocate_on(stream, device: int):
+    """Where a call has a stream of its own, its buffers belong to that stream (the allocator then gives their memory
+    to nobody else before the call's work has run)."""
+    if stream is None:
+        return _HERE
+    import torch
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
+    return torch.cuda.stream(stream)
+
+
+def _stream_on(stream, device: int) -> int:
+    """The raw stream of a call: the one given, or the current one of the tensors' device."""
+    if stream is not None:
+        return _stream_ptr(stream)
+    import torch
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
 class Selector:
     """Owns one handle. Tensors are torch CUDA tensors laid out as in the C header."""
 
@@ -353,6 +498,7 @@ class Selector:
         self.handle = create(max_batch, max_total_visual, max_total_text, num_q_heads, num_kv_heads, head_dim,
                              qk_dtype, score_kernel, query, query_split)
         self.qk_dtype = qk_dtype
+        self.heads, self.kv_heads, self.head_dim = num_q_heads, num_kv_heads, head_dim
 
     def close(self) -> None:
         if self.handle:
@@ -521,6 +667,155 @@ class Selector:
         splice(self.handle, batch, sys_rows, sys_offsets, so, vis_rows, seq_offsets, vo, kept_idx, kept_offsets, ko,
                txt_rows, text_offsets, to, rb, out, off_d, pos, off_h, stream)
         return out[:total], off_d, off_h, pos[:total]
+
+    # ---- the 4-bit K/V cache
+
+    def _cache_call(self, cache, table, seq_lens, batch: int):
+        import torch
+        if not isinstance(cache, KVCache):
+            _refuse("cache must be a KVCache")
+        if cache.heads != self.kv_heads or cache.head_dim != self.head_dim:
+            _refuse(f"the cache has {cache.heads} heads of {cache.head_dim}, the handle {self.kv_heads} of "
+                    f"{self.head_dim}")
+        _want("table", table, torch.int32, (batch, None), cache.device)
+        _want("seq_lens", seq_lens, torch.int32, (batch,), cache.device)
+        return cache.device
+
+    def _element(self):
+        import torch
+        return torch.uint8 if self.qk_dtype == "e4m3" else torch.bfloat16
+
+    def cache(self, num_pages: int, page_size: int, k_scale: float = 1.0, v_scale: float = 1.0, weights: bool = True,
+              device="cuda") -> KVCache:
+        """An empty cache of the handle's head sizes."""
+        import torch
+        shape = (num_pages, self.kv_heads, page_size)
+        c = [torch.zeros((*shape, self.head_dim // n), dtype=torch.uint8, device=device) for n in (2, 16, 2, 16)]
+        w = torch.zeros((num_pages, page_size), dtype=torch.float32, device=device) if weights else None
+        return KVCache(*c, k_scale=k_scale, v_scale=v_scale, weights=w)
+
+    def cache_append(self, cache: KVCache, table, seq_lens, k, v, offsets, rows=None, k_in_scale: float = 1.0,
+                     v_in_scale: float = 1.0, offsets_h=None, stored: bool = False, new_lens=None, stream=None):
+        """Quantises rows into the cache: token t of request b, row offsets[b] + t of k and v [rows, Hkv, d] (or row
+        rows[offsets[b] + t]), to position seq_lens[b] + t of the request's pages; its weight becomes 0. Returns the
+        new lengths, and with ``stored`` also the K and V values that the cache now holds for the rows (bf16)."""
+        import torch
+        off_h = _host_i32(offsets if offsets_h is None else offsets_h)
+        batch, total = len(off_h) - 1, int(off_h[-1])
+        dev = self._cache_call(cache, table, seq_lens, batch)
+        _want("offsets", offsets, torch.int32, (batch + 1,), dev)
+        kind = self._element()
+        k_stride = _row_stride("k", k, kind, self.kv_heads, self.head_dim, dev)
+        v_stride = _row_stride("v", v, kind, self.kv_heads, self.head_dim, dev)
+        if v.shape[0] != k.shape[0]:
+            _refuse("k and v must have the same number of rows")
+        if rows is not None:
+            _want("rows", rows, torch.int32, (total,), dev)
+        with _allocate_on(stream, dev):
+            if new_lens is None:
+                new_lens = torch.empty_like(seq_lens)
+            else:
+                _want("new_lens", new_lens, torch.int32, (batch,), dev)
+            out = [torch.empty((total, self.kv_heads, self.head_dim), dtype=torch.bfloat16, device=k.device)
+                   for _ in "kv"] if stored else (None, None)
+        cache_append(self.handle, batch, cache.struct, table, table.shape[1], seq_lens, k, k_stride, v, v_stride,
+                     k.shape[0], rows, offsets, off_h, k_in_scale, v_in_scale, cache.weights, out[0], out[1], new_lens,
+                     _stream_on(stream, dev))
+        return (new_lens, *out) if stored else new_lens
+
+    def cache_attend(self, cache: KVCache, table, seq_lens, q, offsets, max_len: int, q_scale: float = 1.0,
+                     accumulate: bool = False, weights_out=None, offsets_h=None, out=None, workspace=None, stream=None):
+        """Attention of each request's last tokens (queries [sum T, Hq, d], offsets the prefix of T) over its cache.
+        ``accumulate`` adds every cached token's attention weight (mean over heads, summed over queries) to
+        cache.weights in place; ``weights_out`` takes the sums instead and leaves cache.weights as it is. Returns the
+        bf16 outputs [sum T, Hq, d]. ``workspace``: a uint8 tensor of at least ``cache_attend_workspace`` bytes that no
+        other call in flight uses (made for the call when not given)."""
+        import torch
+        off_h = _host_i32(offsets if offsets_h is None else offsets_h)
+        batch, total = len(off_h) - 1, int(off_h[-1])
+        dev = self._cache_call(cache, table, seq_lens, batch)
+        _want("offsets", offsets, torch.int32, (batch + 1,), dev)
+        stride = _row_stride("q", q, self._element(), self.heads, self.head_dim, dev)
+        if q.shape[0] != total:
+            _refuse(f"q has {q.shape[0]} rows, the offsets {total}")
+        w_in = w_out = None
+        if weights_out is not None or accumulate:
+            if cache.weights is None:
+                _refuse("the cache has no weights")
+            w_in = w_out = cache.weights
+            if weights_out is not None:
+                w_out = _want("weights_out", weights_out, torch.float32, (cache.num_pages, cache.page_size), dev)
+        need = cache_attend_workspace(self.handle, batch, off_h, max_len)
+        with _allocate_on(stream, dev):
+            if out is None:
+                out = torch.empty((total, self.heads, self.head_dim), dtype=torch.bfloat16, device=q.device)
+            else:
+                _want("out", out, torch.bfloat16, (total, self.heads, self.head_dim), dev)
+            if workspace is None:
+                workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+            else:
+                _want("workspace", workspace, torch.uint8, (None,), dev)
+        cache_attend(self.handle, batch, cache.struct, table, table.shape[1], seq_lens, q, stride, offsets, off_h,
+                     max_len, q_scale, w_in, w_out, out, workspace, workspace.shape[0], _stream_on(stream, dev))
+        return out
+
+    def cache_evict(self, cache: KVCache, table, seq_lens, max_len: int, budget: int, sink: int = 0, recent: int = 0,
+                    to_table=None, new_lens=None, kept_idx=None, stream=None):
+        """Cuts every request back to ``budget`` tokens: its first ``sink``, its last ``recent`` and the others of the
+        largest cache.weights stay, in order, at the front of the request's pages (or of the pages of to_table).
+        Returns (kept positions int32 [batch, budget], -1 behind the last; new lengths)."""
+        import torch
+        batch = seq_lens.shape[0] if isinstance(seq_lens, torch.Tensor) and seq_lens.dim() == 1 else -1
+        dev = self._cache_call(cache, table, seq_lens, batch)
+        if cache.weights is None:
+            _refuse("the cache has no weights")
+        if to_table is not None:
+            _want("to_table", to_table, torch.int32, (batch, None), dev)
+        with _allocate_on(stream, dev):
+            if new_lens is None:
+                new_lens = torch.empty_like(seq_lens)
+            else:
+                _want("new_lens", new_lens, torch.int32, (batch,), dev)
+            if kept_idx is None:
+                kept_idx = torch.empty((batch, max(budget, 0)), dtype=torch.int32, device=seq_lens.device)
+            else:
+                _want("kept_idx", kept_idx, torch.int32, (batch, budget), dev)
+        cache_evict(self.handle, batch, cache.struct, table, table.shape[1], seq_lens, max_len, budget, sink, recent,
+                    to_table, 0 if to_table is None else to_table.shape[1], cache.weights, kept_idx, new_lens,
+                    _stream_on(stream, dev))
+        return kept_idx, new_lens
+
+    def verify(self, draft_tokens, target_probs, u_accept, u_sample, offsets, draft_probs=None, offsets_h=None,
+               accepted=None, tokens=None, stream=None):
+        """Verifies drafted tokens (int32 [sum T]) against the target's probabilities [sum T + B, vocab] (float32 or
+        bf16; draft_probs [sum T, vocab] likewise, None: the drafts were certain). Returns (accepted drafts of every
+        request, tokens [sum T + B]: request b's accepted drafts, the sampled token, then -1, from offsets[b] + b)."""
+        import torch
+        off_h = _host_i32(offsets if offsets_h is None else offsets_h)
+        batch, total = len(off_h) - 1, int(off_h[-1])
+        if not isinstance(target_probs, torch.Tensor) or target_probs.device.type != "cuda" or \
+                target_probs.dim() != 2 or target_probs.dtype not in (torch.float32, torch.bfloat16):
+            _refuse("target_probs must be a float32 or bf16 CUDA tensor [sum T + batch, vocab]")
+        dev, kind, vocab = target_probs.device.index, target_probs.dtype, target_probs.shape[1]
+        _want("target_probs", target_probs, kind, (total + batch, None), dev)
+        _want("draft_tokens", draft_tokens, torch.int32, (total,), dev)
+        _want("u_accept", u_accept, torch.float32, (total,), dev)
+        _want("u_sample", u_sample, torch.float32, (batch,), dev)
+        _want("offsets", offsets, torch.int32, (batch + 1,), dev)
+        if draft_probs is not None:
+            _want("draft_probs", draft_probs, kind, (total, vocab), dev)
+        with _allocate_on(stream, dev):
+            if accepted is None:
+                accepted = torch.empty(batch, dtype=torch.int32, device=target_probs.device)
+            else:
+                _want("accepted", accepted, torch.int32, (batch,), dev)
+            if tokens is None:
+                tokens = torch.empty(total + batch, dtype=torch.int32, device=target_probs.device)
+            else:
+                _want("tokens", tokens, torch.int32, (total + batch,), dev)
+        verify(self.handle, batch, vocab, int(kind == torch.bfloat16), draft_tokens, offsets, off_h, target_probs,
+               draft_probs, u_accept, u_sample, accepted, tokens, _stream_on(stream, dev))
+        return accepted, tokens
 
     def check_device(self, stream=None) -> None:
         check_device(self.handle, stream)
