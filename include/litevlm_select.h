@@ -633,7 +633,8 @@ litevlm_status_t litevlm_select_cache_append(litevlm_select_t handle, int32_t ba
  *   out              device bf16 [sum T_b][Hq][d], 16-byte aligned
  *   workspace        device, at least the bytes that
  *                    litevlm_select_cache_attend_workspace gives for the same batch,
- *                    offsets and max_len, 256-byte aligned; used only by this call
+ *                    offsets and max_len (weights: 1 for a call with weights, which
+ *                    needs more), 256-byte aligned; used only by this call
  *                    until it has run. Calls that may run at the same time (two
  *                    captured graphs among them) need a workspace each.
  * Softmax statistics, sums and weights are fp32; probabilities are rounded to f16 for
@@ -643,7 +644,8 @@ litevlm_status_t litevlm_select_cache_append(litevlm_select_t handle, int32_t ba
  * small; UNSUPPORTED where Hkv x row tiles of the longest request passes 65535.
  */
 litevlm_status_t litevlm_select_cache_attend_workspace(litevlm_select_t handle, int32_t batch,
-                                                       const int32_t* q_offsets_h, int32_t max_len, int64_t* bytes);
+                                                       const int32_t* q_offsets_h, int32_t max_len, int32_t weights,
+                                                       int64_t* bytes);
 litevlm_status_t litevlm_select_cache_attend(litevlm_select_t handle, int32_t batch, const litevlm_cache_t* cache,
                                              const int32_t* table, int32_t table_width, const int32_t* seq_lens,
                                              const void* q, int64_t q_row_stride, const int32_t* q_offsets_d,

@@ -1333,15 +1333,18 @@ int64_t round256(int64_t bytes) { return (bytes + 255) & ~(int64_t)255; }
 
 // Workspace of an attention call: the chunks' sums and statistics, and the rows' lse.
 struct AttendSpace {
-    int64_t part_o, part_ml, lse, total;
+    int64_t part_o, part_ml, lse, logits, total;
 };
-AttendSpace attend_space(const lvs::AttendPlan& plan, int64_t rows, int head_dim)
+int64_t logit_stride(int32_t max_len) { return ((int64_t)max_len + 31) & ~(int64_t)31; }
+AttendSpace attend_space(const lvs::AttendPlan& plan, int64_t rows, int head_dim, int64_t tile_rows, int32_t max_len,
+                         bool weights)
 {
     AttendSpace s{};
     const int64_t parts = plan.chunks > 1 ? rows * plan.chunks : 0;
     s.part_ml = round256(parts * head_dim * 4);
     s.lse = s.part_ml + round256(parts * 8);
-    s.total = s.lse + round256(rows * 4);
+    s.logits = s.lse + (weights ? round256(rows * 4) : 0);
+    s.total = s.logits + (weights && plan.logits ? round256(tile_rows * logit_stride(max_len) * 4) : 0);
     return s;
 }
 
@@ -1426,7 +1429,7 @@ litevlm_status_t litevlm_select_cache_append(litevlm_select_t h, int32_t batch, 
 }
 
 litevlm_status_t litevlm_select_cache_attend_workspace(litevlm_select_t h, int32_t batch, const int32_t* q_offsets_h,
-                                                       int32_t max_len, int64_t* bytes)
+                                                       int32_t max_len, int32_t weights, int64_t* bytes)
 {
     const CallRange range_(__func__);
     if (!h) return LITEVLM_ERR_INVALID_ARG;
@@ -1437,7 +1440,10 @@ litevlm_status_t litevlm_select_cache_attend_workspace(litevlm_select_t h, int32
     int64_t total = 0;
     int max_rows = 0;
     s = attend_plan(h, batch, q_offsets_h, max_len, &plan, &total, &max_rows);
-    if (s == LITEVLM_OK) *bytes = attend_space(plan, total * h->cfg.num_q_heads, h->cfg.head_dim).total;
+    if (s == LITEVLM_OK)
+        *bytes = attend_space(plan, total * h->cfg.num_q_heads, h->cfg.head_dim,
+                              (int64_t)batch * h->cfg.num_kv_heads * max_rows, max_len, weights != 0)
+                     .total;
     return s;
 }
 
@@ -1471,7 +1477,8 @@ litevlm_status_t litevlm_select_cache_attend(litevlm_select_t h, int32_t batch, 
         if (s != LITEVLM_OK) return s;
         if (!out || !aligned16(out)) return fail(h, LITEVLM_ERR_INVALID_ARG, "out must be 16-byte aligned and not NULL");
     }
-    const AttendSpace space = attend_space(plan, total * c.num_q_heads, c.head_dim);
+    const AttendSpace space = attend_space(plan, total * c.num_q_heads, c.head_dim,
+                                           (int64_t)batch * c.num_kv_heads * max_rows, max_len, weights_out != nullptr);
     if (workspace_bytes < space.total || (space.total > 0 && !workspace))
         return fail(h, LITEVLM_ERR_WORKSPACE, "the workspace must hold " + std::to_string(space.total) + " bytes");
     if (reinterpret_cast<uintptr_t>(workspace) & 255u)
@@ -1494,6 +1501,9 @@ litevlm_status_t litevlm_select_cache_attend(litevlm_select_t h, int32_t batch, 
     a.part_o = reinterpret_cast<float*>(ws + space.part_o);
     a.part_ml = reinterpret_cast<float2*>(ws + space.part_ml);
     a.lse = weights_out ? reinterpret_cast<float*>(ws + space.lse) : nullptr;
+    a.logits = weights_out && plan.logits ? reinterpret_cast<float*>(ws + space.logits) : nullptr;
+    a.max_rows = max_rows;
+    a.logit_stride = logit_stride(max_len);
     a.weights_in = weights_in;
     a.weights_out = weights_out;
     a.err = h->err_d;

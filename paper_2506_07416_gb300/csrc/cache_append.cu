@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const __grid_con
             uint32_t o[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float2 f = __half22float2(e2m1x2_value<0>(w[i / 4] >> (8 * (i & 3))));
+                const float2 f = __half22float2(e2m1x2_value(w[i / 4] >> (8 * (i & 3))));
                 const __nv_bfloat162 p = __floats2bfloat162_rn(f.x * s * scale, f.y * s * scale);
                 o[i] = *reinterpret_cast<const uint32_t*>(&p);
             }

@@ -7,7 +7,7 @@
 // attend_split_kernel: a CTA takes a key head of a request, a tile of 8, 16 or 32
 // rows (a row is a query with one of the head's query heads) and a chunk of the
 // keys. Its four warps work on their own: a warp copies groups of 16 keys into its
-// ring in shared memory, makes f16 values of codes and scales in registers (exact),
+// ring in shared memory (two groups at a time), makes f16 values of codes and scales in registers (exact),
 // and multiplies with the keys as the M rows and the query rows as the N columns
 // (m16n8k16): a tile of 8 rows, the usual one of a single token, then costs no
 // padding. Channels of a contraction may come in any order, so a lane takes the 32
@@ -15,10 +15,15 @@
 // move only when a score passes them by 8 (2^8 is well inside f16); sums and
 // statistics are fp32. P is rounded to f16 (11 bits) for the second product, the
 // output once to bf16 (8 bits).
-// attend_join_kernel: the chunks of a row joined under the largest reference.
-// attend_weight_kernel: with every row's lse known, a CTA takes 64 keys of a
-// request, makes their scores again for all heads and adds the probabilities in a
-// fixed order; no atomics.
+// attend_finish_kernel: the chunks of a row joined under the largest reference, and
+// the weights of calls of up to 32 rows a key head, whose scores the first kernel has
+// kept: 4 bytes a row and key written and read, mostly in L2.
+// attend_weight_kernel: the weights of calls of more rows: with every row's lse known,
+// a CTA takes 128 keys of a request and makes their scores again for all heads.
+// Either adds the probabilities in a fixed order; no atomics.
+
+#include <algorithm>
+#include <type_traits>
 
 #include "cache.cuh"
 
@@ -28,7 +33,7 @@ namespace {
 
 constexpr int kAttWarps = 4;
 constexpr int kAttThreads = 32 * kAttWarps;
-constexpr int kAttStages = 4;        // groups of a warp's ring
+constexpr int kAttStages = 3;        // spans of 32 keys of a warp's ring
 constexpr float kNoRef = -3.0e38f;   // reference of a row without keys so far
 constexpr float kRefSlack = 8.f;     // a score may pass its row's reference by this
 
@@ -60,27 +65,32 @@ struct Group {
     static constexpr int kBytes = 2 * (kCodes + kScales);
 };
 
-// Starts the copies of the 16 keys from j0 on (a whole group lies in one page);
-// zeros where the table names no page. K alone where !WITH_V.
+// Starts a warp's copies of the two groups of 16 keys from j0 on, of K (and of V where
+// WITH_V) of head h: lanes 0 to 15 copy the first group, the others the second. A group
+// lies in one page; `page` is the lane's (-1: zeros).
 template <int D, bool WITH_V>
-__device__ __forceinline__ void load_group(const CachePages& c, int b, int h, int j0, uint32_t dst, int32_t* err)
+__device__ __forceinline__ void load_span(const CachePages& c, int32_t page, int h, int j0, uint32_t dst)
 {
     using G = Group<D>;
-    const int lane = threadIdx.x & 31;
-    const int32_t page = cache_page(c.table, c.width, c.num_pages, c.page_shift, b, j0);
+    constexpr int BYTES = WITH_V ? G::kBytes : G::kBytes / 2;
+    const int lane = threadIdx.x & 31, l = lane & 15, half = lane >> 4;
     const bool ok = page >= 0;
-    if (!ok && lane == 0) atomicOr(err, kErrBounds);
-    const int64_t row = cache_row(ok ? page : 0, c.hkv, h, c.page_shift, j0 & ((1 << c.page_shift) - 1));
+    const int64_t row =
+        cache_row(ok ? page : 0, c.hkv, h, c.page_shift, (j0 + 16 * half) & ((1 << c.page_shift) - 1));
+    dst += half * BYTES + l * 16;
+    const uint8_t* k = c.codes[0] + row * (D / 2) + l * 16;
 #pragma unroll
-    for (int t = 0; t < (WITH_V ? 2 : 1); ++t) {
-        const uint8_t* codes = c.codes[t] + row * (D / 2);
-        const uint8_t* scales = c.scales[t] + row * (D / 16);
-        const uint32_t d = dst + (t ? G::kV : G::kK), ds = dst + (t ? G::kVs : G::kKs);
+    for (int i = 0; i < G::kCodes / 256; ++i) copy_async16(dst + G::kK + i * 256, k + i * 256, ok);
+    if constexpr (WITH_V) {
+        const uint8_t* v = c.codes[1] + row * (D / 2) + l * 16;
 #pragma unroll
-        for (int i = 0; i < G::kCodes / 512; ++i)
-            copy_async16(d + (i * 32 + lane) * 16, codes + (i * 32 + lane) * 16, ok);
-        if (lane < G::kScales / 16) copy_async16(ds + lane * 16, scales + lane * 16, ok);
+        for (int i = 0; i < G::kCodes / 256; ++i) copy_async16(dst + G::kV + i * 256, v + i * 256, ok);
     }
+    // scales: the first lanes those of K, the next those of V
+    constexpr int SL = G::kScales / 16;
+    const int t = l / SL;
+    if (t < (WITH_V ? 2 : 1))
+        copy_async16(dst + (t ? G::kVs - SL * 16 : G::kKs), c.scales[t] + row * (D / 16) + (l - t * SL) * 16, ok);
 }
 
 // B operands of 8 query rows (columns of the contraction): lane (g, c) holds row
@@ -166,25 +176,23 @@ __device__ __forceinline__ void score_group(const uint8_t* grp, int lane, QF qf,
 #pragma unroll
         for (int i = 0; i < 4; ++i) s[t][i] = 0.f;
 #pragma unroll
-    for (int k = 0; k < D / 16; ++k) {  // 4 channels of every lane
-        const int w = k / 2, sc = k / 4;
-        uint32_t a0, a1, a2, a3;
-        if (k & 1) {
-            a0 = h2_bits(__hmul2(e2m1x2_value<2>(w0[w]), s0[sc]));
-            a1 = h2_bits(__hmul2(e2m1x2_value<2>(w1[w]), s1[sc]));
-            a2 = h2_bits(__hmul2(e2m1x2_value<3>(w0[w]), s0[sc]));
-            a3 = h2_bits(__hmul2(e2m1x2_value<3>(w1[w]), s1[sc]));
-        } else {
-            a0 = h2_bits(__hmul2(e2m1x2_value<0>(w0[w]), s0[sc]));
-            a1 = h2_bits(__hmul2(e2m1x2_value<0>(w1[w]), s1[sc]));
-            a2 = h2_bits(__hmul2(e2m1x2_value<1>(w0[w]), s0[sc]));
-            a3 = h2_bits(__hmul2(e2m1x2_value<1>(w1[w]), s1[sc]));
+    for (int w = 0; w < WORDS; ++w) {  // 8 channels of every lane, two contractions of 16
+        __half2 x[4], y[4];
+        e2m1x8_value(w0[w], x);
+        e2m1x8_value(w1[w], y);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i] = __hmul2(x[i], s0[w / 2]);
+            y[i] = __hmul2(y[i], s1[w / 2]);
         }
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const uint2 q = qf(t, k);
-            mma16816(s[t], a0, a1, a2, a3, q.x, q.y);
-        }
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const uint2 q = qf(t, 2 * w + e);
+                mma16816(s[t], h2_bits(x[2 * e]), h2_bits(y[2 * e]), h2_bits(x[2 * e + 1]), h2_bits(y[2 * e + 1]), q.x,
+                         q.y);
+            }
     }
 }
 
@@ -206,6 +214,9 @@ __device__ __forceinline__ RowTile row_tile(const AttendArgs& a, int b, int tile
     return r;
 }
 
+template <int D>
+constexpr int kRingBytes = kAttWarps * kAttStages * 2 * Group<D>::kBytes;
+
 template <int D, int NT, bool FP8>
 __global__ void __launch_bounds__(kAttThreads) attend_split_kernel(const __grid_constant__ AttendArgs a)
 {
@@ -214,8 +225,9 @@ __global__ void __launch_bounds__(kAttThreads) attend_split_kernel(const __grid_
     constexpr bool Q_SMEM = NT > 2;  // fragments of 32 rows would take 64 registers
     constexpr int MT = D / 16;
     // the rings; behind the loop the same memory takes a row tile of every warp's sums
-    constexpr int kRing = kAttWarps * kAttStages * G::kBytes, kJoin = kAttWarps * 8 * (D + 4) * 4;
-    __shared__ __align__(16) uint8_t ring[kRing > kJoin ? kRing : kJoin];
+    constexpr int kRing = kRingBytes<D>, kJoin = kAttWarps * 8 * (D + 4) * 4;
+    static_assert(kRing >= kJoin, "the sums fit the rings");
+    extern __shared__ __align__(16) uint8_t ring[];
     __shared__ float s_m[kAttWarps][ROWS], s_l[kAttWarps][ROWS];
     __shared__ uint2 q_s[Q_SMEM ? NT * (D / 16) * 32 : 1];
     __shared__ float back_s[Q_SMEM ? ROWS : 1];
@@ -235,16 +247,29 @@ __global__ void __launch_bounds__(kAttThreads) attend_split_kernel(const __grid_
     if (k0 >= k1 && blockIdx.x > 0) return;  // (the first chunk of a tile without keys writes its zeros)
     const int all_see = rt.last0 + rt.row0 / a.group;  // the last key that every row sees
 
-    uint8_t* my = ring + warp * kAttStages * G::kBytes;
+    constexpr int SPAN = 2 * G::kBytes;
+    uint8_t* my = ring + warp * kAttStages * SPAN;
     const uint32_t my_s = smem_u32(my);
-    const int groups = k1 > k0 ? (k1 - k0 + 15) / 16 : 0;
-    const int n_mine = groups > warp ? (groups - warp + kAttWarps - 1) / kAttWarps : 0;
+    const int spans = k1 > k0 ? (k1 - k0 + 31) / 32 : 0;
+    const int n_mine = spans > warp ? (spans - warp + kAttWarps - 1) / kAttWarps : 0;
+    // page of the lane's group of the warp's n-th span (-1: none; no keys from k1 on are copied)
+    auto page_of = [&](int n) -> int32_t {
+        const int j = k0 + (warp + n * kAttWarps) * 32 + (lane & 16);
+        if (j >= k1) return -1;
+        const int32_t p = cache_page(a.cache.table, a.cache.width, a.cache.num_pages, a.cache.page_shift, b, j);
+        if (p < 0 && (lane & 15) == 0) atomicOr(a.err, kErrBounds);
+        return p;
+    };
+    // whether the lane's group has a page, a bit for every span on its way, the last one's lowest
+    uint32_t named = 0;
 #pragma unroll
     for (int i = 0; i < kAttStages - 1; ++i) {
-        if (i < n_mine)
-            load_group<D, true>(a.cache, b, h, k0 + (warp + i * kAttWarps) * 16, my_s + i * G::kBytes, a.err);
+        const int32_t page = page_of(i);
+        if (i < n_mine) load_span<D, true>(a.cache, page, h, k0 + (warp + i * kAttWarps) * 32, my_s + i * SPAN);
         copy_async_commit();
+        named = named << 1 | (page >= 0);
     }
+    int32_t next_page = page_of(kAttStages - 1);  // (read a span ahead: nothing waits for the table)
 
     // ---- the tile's rows
     uint32_t qr[Q_SMEM ? 1 : NT][D / 8];
@@ -298,34 +323,31 @@ __global__ void __launch_bounds__(kAttThreads) attend_split_kernel(const __grid_
         l[t][0] = l[t][1] = 0.f;
     }
 
+    float* logits = a.logits + (((int64_t)b * a.cache.hkv + h) * a.max_rows + rt.row0 + 2 * c) * a.logit_stride;
     bool nan_value = false;
-#pragma unroll 1
-    for (int n = 0; n < n_mine; ++n) {
-        copy_async_wait<kAttStages - 2>();
-        __syncwarp();  // every lane's copies are there, and the group before is no longer read
-        {
-            const int nx = n + kAttStages - 1;
-            if (nx < n_mine)
-                load_group<D, true>(a.cache, b, h, k0 + (warp + nx * kAttWarps) * 16,
-                                    my_s + (nx % kAttStages) * G::kBytes, a.err);
-            copy_async_commit();
-        }
-        const uint8_t* grp = my + (n % kAttStages) * G::kBytes;
-        const int j0 = k0 + (warp + n * kAttWarps) * 16;
-        const bool no_page =
-            cache_page(a.cache.table, a.cache.width, a.cache.num_pages, a.cache.page_shift, b, j0) < 0;
+
+    // a group of 16 keys from j0 on; CHECK: some of the rows do not see all of them
+    auto group = [&](const uint8_t* grp, int j0, bool there, auto check) {
+        constexpr bool CHECK = decltype(check)::value;
         float s[NT][4];
         score_group<D, NT>(grp, lane, qf, s);
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[t][e] *= fac[t][e & 1];
-        if (j0 + 15 > all_see || no_page) {
+            for (int e = 0; e < 4; ++e) {
+                s[t][e] *= fac[t][e & 1];
+                if (CHECK && (!there || j0 + g + 8 * (e >> 1) > min(vis[t][e & 1], k1 - 1))) s[t][e] = -INFINITY;
+            }
+        if (a.logits) {
+            float* to = logits + j0 + g;
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (j0 + g + 8 * (e >> 1) > min(vis[t][e & 1], k1 - 1) || no_page) s[t][e] = -INFINITY;
+                for (int e = 0; e < 2; ++e)
+                    if (t * 8 + 2 * c + e < rt.rows) {
+                        __stcg(to + (t * 8 + e) * a.logit_stride, s[t][e]);
+                        __stcg(to + (t * 8 + e) * a.logit_stride + 8, s[t][e + 2]);
+                    }
         }
         bool move = false;
 #pragma unroll
@@ -378,12 +400,14 @@ __global__ void __launch_bounds__(kAttThreads) attend_split_kernel(const __grid_
                 x[e][0] = *reinterpret_cast<const uint32_t*>(grp + G::kV + key * 32 + g * 4);
                 sc[e] = grp[G::kVs + key * 4 + g / 2];
             }
-            // what lies behind the last key may be anything, a NaN scale among it
-            if (j0 + key >= k1) sc[e] = 0u;
-            // a NaN value must not reach the rows that do not see it (0 * NaN): put in at the end
-            if (j0 + key > all_see && (sc[e] & 0x7Fu) == 0x7Fu) {
-                sc[e] = 0u;
-                nan_value = true;
+            if constexpr (CHECK) {
+                // what lies behind the last key may be anything, a NaN scale among it
+                if (j0 + key >= k1) sc[e] = 0u;
+                // a NaN value must not reach the rows that do not see it (0 * NaN): put in at the end
+                if (j0 + key > all_see && (sc[e] & 0x7Fu) == 0x7Fu) {
+                    sc[e] = 0u;
+                    nan_value = true;
+                }
             }
         }
         const __half2 sa = e4m3x2_value(sc[0] | (sc[1] << 8)), sb = e4m3x2_value(sc[2] | (sc[3] << 8));
@@ -391,17 +415,48 @@ __global__ void __launch_bounds__(kAttThreads) attend_split_kernel(const __grid_
         for (int w = 0; w < VW; ++w) {
             // bytes of (code of the first key, code of the second) for the even and the odd channels
             const uint32_t lo = 0x0F0F0F0Fu;
-            const uint32_t ae = (x[0][w] & lo) | ((x[1][w] & lo) << 4), ao = ((x[0][w] >> 4) & lo) | (x[1][w] & ~lo);
-            const uint32_t be = (x[2][w] & lo) | ((x[3][w] & lo) << 4), bo = ((x[2][w] >> 4) & lo) | (x[3][w] & ~lo);
+            const uint32_t ae = (x[0][w] & lo) | ((x[1][w] << 4) & ~lo), ao = ((x[0][w] >> 4) & lo) | (x[1][w] & ~lo);
+            const uint32_t be = (x[2][w] & lo) | ((x[3][w] << 4) & ~lo), bo = ((x[2][w] >> 4) & lo) | (x[3][w] & ~lo);
+            __half2 a0[4], a1[4], a2[4], a3[4];
+            e2m1x8_value(ae, a0);
+            e2m1x8_value(ao, a1);
+            e2m1x8_value(be, a2);
+            e2m1x8_value(bo, a3);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const uint32_t a0 = h2_bits(__hmul2(e2m1x2_value<0>(ae >> (8 * i)), sa));
-                const uint32_t a1 = h2_bits(__hmul2(e2m1x2_value<0>(ao >> (8 * i)), sa));
-                const uint32_t a2 = h2_bits(__hmul2(e2m1x2_value<0>(be >> (8 * i)), sb));
-                const uint32_t a3 = h2_bits(__hmul2(e2m1x2_value<0>(bo >> (8 * i)), sb));
+                const uint32_t f0 = h2_bits(__hmul2(a0[i], sa)), f1 = h2_bits(__hmul2(a1[i], sa));
+                const uint32_t f2 = h2_bits(__hmul2(a2[i], sb)), f3 = h2_bits(__hmul2(a3[i], sb));
 #pragma unroll
-                for (int t = 0; t < NT; ++t) mma16816(o[t][w * 4 + i], a0, a1, a2, a3, pb[t][0], pb[t][1]);
+                for (int t = 0; t < NT; ++t) mma16816(o[t][w * 4 + i], f0, f1, f2, f3, pb[t][0], pb[t][1]);
             }
+        }
+    };
+
+    int stage = 0;
+#pragma unroll 1
+    for (int n = 0; n < n_mine; ++n) {
+        copy_async_wait<kAttStages - 2>();
+        __syncwarp();  // every lane's copies are there, and the span before is no longer read
+        const int j0 = k0 + (warp + n * kAttWarps) * 32;
+        const bool mine = named >> (kAttStages - 2) & 1u;  // the lane's group of this span has a page
+        {
+            const int nx = n + kAttStages - 1;
+            const int to = stage == 0 ? kAttStages - 1 : stage - 1;
+            if (nx < n_mine)
+                load_span<D, true>(a.cache, next_page, h, j0 + (kAttStages - 1) * kAttWarps * 32, my_s + to * SPAN);
+            copy_async_commit();
+            named = named << 1 | (next_page >= 0);
+            next_page = page_of(nx + 1);
+        }
+        const uint8_t* span = my + stage * SPAN;
+        stage = stage + 1 == kAttStages ? 0 : stage + 1;
+        const uint32_t there = __ballot_sync(0xffffffffu, mine);
+        if (there == 0xFFFFFFFFu && j0 + 31 <= all_see) {
+            group(span, j0, true, std::false_type{});
+            group(span + G::kBytes, j0 + 16, true, std::false_type{});
+        } else {
+            group(span, j0, there & 1u, std::true_type{});
+            if (j0 + 16 < k1) group(span + G::kBytes, j0 + 16, there >> 16 & 1u, std::true_type{});
         }
     }
     copy_async_wait<0>();
@@ -468,79 +523,214 @@ __global__ void __launch_bounds__(kAttThreads) attend_split_kernel(const __grid_
     }
 }
 
-// One row a warp: chunks joined under the largest reference.
-template <int D>
-__global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant__ AttendArgs a)
+// Log2 of a row's sum of 2^s from its chunks' references and sums, by a warp: the row's
+// reference and sum too.
+__device__ __forceinline__ float2 join_stats(const float2* ml, int n)
 {
     const int lane = threadIdx.x & 31;
+    float M = kNoRef, L = 0.f;
+    for (int x = lane; x < n; x += 32) M = fmaxf(M, __ldcg(ml + x).x);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+    for (int x = lane; x < n; x += 32) {
+        const float2 v = __ldcg(ml + x);
+        L += v.y * ex2(v.x - M);
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) L += __shfl_xor_sync(0xffffffffu, L, d);
+    return make_float2(M, L);
+}
+
+constexpr int kFinishThreads = 512;
+constexpr int kFinishWarps = kFinishThreads / 32;
+constexpr int kFinishKeys = 512;  // keys whose weights a CTA adds: 128 a warp, four warps share the rows
+constexpr int kLogitRows = 2048;  // rows of a request whose scores are kept for the weights
+
+// Sums over the rows [x0, x1) of the probabilities of four neighbouring keys. CHECK: some
+// of the rows do not see all of them.
+template <bool CHECK>
+__device__ __forceinline__ float4 add_weights(const float* s, int64_t stride, const int2* rows, const float* lse, int x0,
+                                              int x1, int j)
+{
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    constexpr int U = 8;
+    for (int x = x0; x < x1; x += U) {
+        float4 v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            v[u] = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+            if (x + u < x1 && (!CHECK || j <= rows[x + u].y))
+                v[u] = __ldcg(reinterpret_cast<const float4*>(s + (int64_t)rows[x + u].x * stride));
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (x + u >= x1) break;
+            const float e = lse[x + u];
+            const int last = CHECK ? rows[x + u].y : 0;
+            sum.x += CHECK && j > last ? 0.f : ex2(v[u].x - e);
+            sum.y += CHECK && j + 1 > last ? 0.f : ex2(v[u].y - e);
+            sum.z += CHECK && j + 2 > last ? 0.f : ex2(v[u].z - e);
+            sum.w += CHECK && j + 3 > last ? 0.f : ex2(v[u].w - e);
+        }
+    }
+    return sum;
+}
+
+// The first `weight_blocks` CTAs of a request add the weights of 512 keys each from the
+// kept scores, over the rows in order; the others join chunks, `row_warps` warps a row.
+// A weight CTA finds the rows' lse from the chunks' statistics by itself, which saves a
+// launch between the two.
+template <int D>
+__global__ void __launch_bounds__(kFinishThreads) attend_finish_kernel(const __grid_constant__ AttendArgs a,
+                                                                       int weight_blocks, int row_warps)
+{
+    extern __shared__ uint8_t rows_s[];
+    // the warps' parts: four weights a lane, or a row of outputs a warp (D <= 128)
+    __shared__ __align__(16) float join_s[kFinishWarps][128];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int b = blockIdx.y;
     griddep_wait();
     griddep_launch_dependents();
     bool bad;
     const int len = cache_len(a.lens[b], a.limit, bad);
     const int q0 = a.q_off[b], t = a.q_off[b + 1] - q0;
-    for (int r = blockIdx.x * 4 + (threadIdx.x >> 5); r < t * a.hq; r += gridDim.x * 4) {
-        const int i = r / a.hq;
-        const int64_t at = (int64_t)q0 * a.hq + r;
-        // chunks that the row's tile wrote: at least those with keys of the row
+    // chunks with keys that query i sees
+    auto chunks_of = [&](int i) -> int {
         const int seen = len - t + i + 1;
-        const int n = seen > 0 ? (seen + a.chunk - 1) / a.chunk : 0;
-        float M = kNoRef;
-        for (int x = lane; x < n; x += 32) M = fmaxf(M, a.part_ml[at * a.chunks + x].x);
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
-        float L = 0.f, O[D / 32];
-#pragma unroll
-        for (int e = 0; e < D / 32; ++e) O[e] = 0.f;
-        for (int x = 0; x < n; ++x) {
-            const float2 ml = a.part_ml[at * a.chunks + x];
-            const float f = ex2(ml.x - M);
-            L += ml.y * f;
-            const float* p = a.part_o + (at * a.chunks + x) * D + lane * (D / 32);
-            if constexpr (D == 128) {
-                const float4 v = *reinterpret_cast<const float4*>(p);
-                O[0] += v.x * f, O[1] += v.y * f, O[2] += v.z * f, O[3] += v.w * f;
+        return seen > 0 ? (seen + a.chunk - 1) / a.chunk : 0;
+    };
+    if ((int)blockIdx.x < weight_blocks) {
+        const int j0 = blockIdx.x * kFinishKeys;
+        if (j0 >= len) return;
+        const int rows = t * a.group, n = rows * a.cache.hkv;
+        float* lse_s = reinterpret_cast<float*>(rows_s);
+        int2* row_s = reinterpret_cast<int2*>(rows_s + (size_t)((n + 1) & ~1) * 4);  // scores' row, last key seen
+        const bool by_warp = a.chunks > 16;
+        for (int x = by_warp ? warp : tid; x < n; x += by_warp ? kFinishWarps : kFinishThreads) {
+            const int h = x / rows, r = x % rows, i = r / a.group;
+            const int64_t at = (int64_t)(q0 + i) * a.hq + h * a.group + r % a.group;
+            float lse;
+            if (a.chunks == 1) {
+                lse = __ldcg(a.lse + at);
             } else {
-                const float2 v = *reinterpret_cast<const float2*>(p);
-                O[0] += v.x * f, O[1] += v.y * f;
+                float2 ml = make_float2(kNoRef, 0.f);
+                if (by_warp) {
+                    ml = join_stats(a.part_ml + at * a.chunks, chunks_of(i));
+                } else {
+                    float2 v[16];
+                    const int m = chunks_of(i);
+#pragma unroll
+                    for (int y = 0; y < 16; ++y)
+                        v[y] = y < m ? __ldcg(a.part_ml + at * a.chunks + y) : make_float2(kNoRef, 0.f);
+#pragma unroll
+                    for (int y = 0; y < 16; ++y) ml.x = fmaxf(ml.x, v[y].x);
+#pragma unroll
+                    for (int y = 0; y < 16; ++y) ml.y += v[y].y * ex2(v[y].x - ml.x);
+                }
+                lse = ml.y == 0.f ? INFINITY : ml.x + log2f(ml.y);
+            }
+            if (!by_warp || lane == 0) {
+                lse_s[x] = lse;
+                row_s[x] = make_int2(h * a.max_rows + r, len - t + i);
             }
         }
-        const float vs = a.cache.scale[1];
-#pragma unroll
-        for (int e = 0; e < D / 32; e += 2) {
-            const float v0 = L == 0.f ? 0.f : O[e] / L * vs, v1 = L == 0.f ? 0.f : O[e + 1] / L * vs;
-            *reinterpret_cast<__nv_bfloat162*>(a.out + at * D + lane * (D / 32) + e) = __floats2bfloat162_rn(v0, v1);
+        __syncthreads();
+        // four neighbouring keys a lane (the scores' rows are padded to a whole number of them)
+        const int part = warp >> 2, per = (n + 3) / 4;
+        const int x0 = min(n, part * per), x1 = min(n, x0 + per);
+        const int j = j0 + (warp & 3) * 128 + 4 * lane;
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (j < len) {
+            const float* s = a.logits + (int64_t)b * a.cache.hkv * a.max_rows * a.logit_stride + j;
+            sum = j0 + kFinishKeys - 1 <= len - t ? add_weights<false>(s, a.logit_stride, row_s, lse_s, x0, x1, j)
+                                                  : add_weights<true>(s, a.logit_stride, row_s, lse_s, x0, x1, j);
         }
-        if (a.lse && lane == 0) a.lse[at] = L == 0.f ? INFINITY : M + log2f(L);
+        float4* sums = reinterpret_cast<float4*>(&join_s[0][0]);  // [part][128 lanes of the tile]
+        sums[warp * 32 + lane] = sum;
+        __syncthreads();
+        if (part != 0 || j >= len) return;
+#pragma unroll
+        for (int p = 1; p < 4; ++p) {
+            const float4 v = sums[(warp + 4 * p) * 32 + lane];
+            sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
+        }
+        const int32_t page = cache_page(a.cache.table, a.cache.width, a.cache.num_pages, a.cache.page_shift, b, j);
+        if (page < 0) return;
+        const int64_t at = ((int64_t)page << a.cache.page_shift) + (j & ((1 << a.cache.page_shift) - 1));
+        const float add[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (j + e < len) a.weights_out[at + e] = a.weights_in[at + e] + add[e] / (float)a.hq;
+        return;
     }
+    const int part = warp % row_warps;
+    const int r = (blockIdx.x - weight_blocks) * (kFinishWarps / row_warps) + warp / row_warps;
+    const bool real = r < t * a.hq;
+    const int64_t at = (int64_t)q0 * a.hq + (real ? r : 0);
+    const int n = real ? chunks_of(r / a.hq) : 0;
+    const float2 ml = join_stats(a.part_ml + at * a.chunks, n);
+    const float M = ml.x, L = ml.y;
+    float O[D / 32];
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e) O[e] = 0.f;
+#pragma unroll 4
+    for (int x = part; x < n; x += row_warps) {
+        const float f = ex2(__ldcg(a.part_ml + at * a.chunks + x).x - M);
+        const float* p = a.part_o + (at * a.chunks + x) * D + lane * (D / 32);
+        if constexpr (D == 128) {
+            const float4 v = __ldcg(reinterpret_cast<const float4*>(p));
+            O[0] += v.x * f, O[1] += v.y * f, O[2] += v.z * f, O[3] += v.w * f;
+        } else {
+            const float2 v = __ldcg(reinterpret_cast<const float2*>(p));
+            O[0] += v.x * f, O[1] += v.y * f;
+        }
+    }
+    if (row_warps > 1) {
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) join_s[warp][lane * (D / 32) + e] = O[e];
+        __syncthreads();
+        if (part != 0) return;
+        for (int w = 1; w < row_warps; ++w)
+#pragma unroll
+            for (int e = 0; e < D / 32; ++e) O[e] += join_s[warp + w][lane * (D / 32) + e];
+    }
+    if (!real) return;
+    const float vs = a.cache.scale[1];
+#pragma unroll
+    for (int e = 0; e < D / 32; e += 2) {
+        const float v0 = L == 0.f ? 0.f : O[e] / L * vs, v1 = L == 0.f ? 0.f : O[e + 1] / L * vs;
+        *reinterpret_cast<__nv_bfloat162*>(a.out + at * D + lane * (D / 32) + e) = __floats2bfloat162_rn(v0, v1);
+    }
+    if (a.lse && lane == 0) a.lse[at] = L == 0.f ? INFINITY : M + log2f(L);
 }
 
-// A CTA: 64 keys of a request, a warp 16 of them; all key heads, their rows 8 at a time.
+// A CTA: 128 keys of a request, a warp 32 of them; all key heads, their rows 8 at a time.
 template <int D, bool FP8>
 __global__ void __launch_bounds__(kAttThreads) attend_weight_kernel(const __grid_constant__ AttendArgs a)
 {
     using G = Group<D>;
-    __shared__ __align__(16) uint8_t ring[kAttWarps][2][G::kBytes / 2];
+    constexpr int HALF = G::kBytes / 2;  // a group's K
+    __shared__ __align__(16) uint8_t ring[kAttWarps][2][2 * HALF];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int g = lane >> 2, c = lane & 3;
     const int b = blockIdx.y;
     griddep_wait();
     griddep_launch_dependents();
     const RowTile rt = row_tile(a, b, 0, 8);
-    const int j0 = (blockIdx.x * kAttWarps + warp) * 16;
+    const int j0 = (blockIdx.x * kAttWarps + warp) * 32;
     if (j0 >= rt.len) return;
-    const int32_t page = cache_page(a.cache.table, a.cache.width, a.cache.num_pages, a.cache.page_shift, b, j0);
-    if (page < 0) return;
+    const int my_j = j0 + (lane & 16);
+    const int32_t page =
+        my_j < rt.len ? cache_page(a.cache.table, a.cache.width, a.cache.num_pages, a.cache.page_shift, b, my_j) : -1;
     const int q0 = a.q_off[b], rows = rt.t * a.group;
-    // rows that see a key of the group: the queries from the first that stands at or behind j0
+    // rows that see a key of the span: the queries from the first that stands at or behind j0
     const int r_first = max(0, j0 - rt.last0) * a.group;
     const uint32_t dst = smem_u32(&ring[warp][0][0]);
-    load_group<D, false>(a.cache, b, 0, j0, dst, a.err);
+    load_span<D, false>(a.cache, page, 0, j0, dst);
     copy_async_commit();
-    float sum[2] = {0.f, 0.f};  // of the keys g and g + 8, over the lane's rows
+    float sum[2][2] = {{0.f, 0.f}, {0.f, 0.f}};  // of the groups' keys g and g + 8, over the lane's rows
     for (int h = 0; h < a.cache.hkv; ++h) {
-        if (h + 1 < a.cache.hkv)
-            load_group<D, false>(a.cache, b, h + 1, j0, dst + ((h + 1) & 1) * (G::kBytes / 2), a.err);
+        if (h + 1 < a.cache.hkv) load_span<D, false>(a.cache, page, h + 1, j0, dst + ((h + 1) & 1) * 2 * HALF);
         copy_async_commit();
         copy_async_wait<1>();
         __syncwarp();
@@ -552,9 +742,11 @@ __global__ void __launch_bounds__(kAttThreads) attend_weight_kernel(const __grid
             load_q<D, FP8>(a.q, (int64_t)(q0 + row / a.group) * a.q_stride +
                                     (int64_t)(h * a.group + row % a.group) * D + c * (D / 4),
                            real, q, back);
-            float s[1][4];
-            score_group<D, 1>(&ring[warp][h & 1][0], lane, [&](int, int k) { return make_uint2(q[2 * k], q[2 * k + 1]); },
-                              s);
+            float s[2][1][4];
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+                score_group<D, 1>(&ring[warp][h & 1][x * HALF], lane,
+                                  [&](int, int k) { return make_uint2(q[2 * k], q[2 * k + 1]); }, s[x]);
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const float fac = a.c_log2 * __shfl_sync(0xffffffffu, back, 8 * c + 4 * e);
@@ -562,21 +754,28 @@ __global__ void __launch_bounds__(kAttThreads) attend_weight_kernel(const __grid
                 if (r >= rows) continue;
                 const int vis = rt.last0 + r / a.group;
                 const float lse = a.lse[(int64_t)(q0 + r / a.group) * a.hq + h * a.group + r % a.group];
-                if (j0 + g <= vis) sum[0] += ex2(fmaf(s[0][e], fac, -lse));
-                if (j0 + g + 8 <= vis) sum[1] += ex2(fmaf(s[0][e + 2], fac, -lse));
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int y = 0; y < 2; ++y)
+                        if (j0 + 16 * x + 8 * y + g <= vis) sum[x][y] += ex2(fmaf(s[x][0][e + 2 * y], fac, -lse));
             }
         }
         __syncwarp();
     }
     copy_async_wait<0>();
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        sum[e] += __shfl_xor_sync(0xffffffffu, sum[e], 1);
-        sum[e] += __shfl_xor_sync(0xffffffffu, sum[e], 2);
-        const int j = j0 + g + 8 * e;
-        if (c == 0 && j < rt.len) {
-            const int64_t at = ((int64_t)page << a.cache.page_shift) + (j & ((1 << a.cache.page_shift) - 1));
-            a.weights_out[at] = a.weights_in[at] + sum[e] / (float)a.hq;
+    for (int x = 0; x < 2; ++x) {
+        const int32_t p = __shfl_sync(0xffffffffu, page, 16 * x);
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+            sum[x][y] += __shfl_xor_sync(0xffffffffu, sum[x][y], 1);
+            sum[x][y] += __shfl_xor_sync(0xffffffffu, sum[x][y], 2);
+            const int j = j0 + 16 * x + 8 * y + g;
+            if (c == 0 && j < rt.len && p >= 0) {
+                const int64_t at = ((int64_t)p << a.cache.page_shift) + (j & ((1 << a.cache.page_shift) - 1));
+                a.weights_out[at] = a.weights_in[at] + sum[x][y] / (float)a.hq;
+            }
         }
     }
 }
@@ -598,20 +797,29 @@ cudaError_t launch_all(const AttendArgs& a, const AttendPlan& plan, int max_rows
         auto kern = plan.row_tile == 8    ? attend_split_kernel<D, 1, FP8>
                     : plan.row_tile == 16 ? attend_split_kernel<D, 2, FP8>
                                           : attend_split_kernel<D, 4, FP8>;
-        e = cudaLaunchKernelEx(&cfg, kern, a);
+        cfg.dynamicSmemBytes = kRingBytes<D>;
+        e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes<D>);
+        if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, kern, a);
         if (e != cudaSuccess) return e;
         ++*launches;
-        if (plan.chunks > 1) {
-            const int most = max_rows / a.group * a.hq;
-            cfg.gridDim = dim3((unsigned)((most + 3) / 4), (unsigned)a.batch, 1);
-            cfg.blockDim = dim3(128, 1, 1);
-            e = cudaLaunchKernelEx(&cfg, attend_join_kernel<D>, a);
-            if (e != cudaSuccess) return e;
-            ++*launches;
-        }
+        cfg.dynamicSmemBytes = 0;
     }
-    if (a.weights_out && max_len > 0) {
-        cfg.gridDim = dim3((unsigned)((max_len + 63) / 64), (unsigned)a.batch, 1);
+    const int weight_blocks = a.logits ? (max_len + kFinishKeys - 1) / kFinishKeys : 0;
+    const int most = max_rows / a.group * a.hq;  // rows of the longest request
+    const int row_warps = plan.chunks <= 4 ? 1 : (plan.chunks <= 16 ? 4 : kFinishWarps);
+    const int join_rows = kFinishWarps / row_warps;  // of a CTA
+    const int join_blocks = total_rows > 0 && plan.chunks > 1 ? (most + join_rows - 1) / join_rows : 0;
+    if (weight_blocks + join_blocks > 0) {
+        cfg.gridDim = dim3((unsigned)(weight_blocks + join_blocks), (unsigned)a.batch, 1);
+        cfg.blockDim = dim3(kFinishThreads, 1, 1);
+        cfg.dynamicSmemBytes = a.logits ? (size_t)(most + 2) * 12 : 0;
+        e = cudaLaunchKernelEx(&cfg, attend_finish_kernel<D>, a, weight_blocks, row_warps);
+        if (e != cudaSuccess) return e;
+        ++*launches;
+        cfg.dynamicSmemBytes = 0;
+    }
+    if (a.weights_out && !a.logits && max_len > 0) {
+        cfg.gridDim = dim3((unsigned)((max_len + 127) / 128), (unsigned)a.batch, 1);
         cfg.blockDim = dim3(kAttThreads, 1, 1);
         e = cudaLaunchKernelEx(&cfg, attend_weight_kernel<D, FP8>, a);
         if (e != cudaSuccess) return e;
@@ -628,13 +836,17 @@ AttendPlan plan_cache_attend(int batch, int hkv, int max_rows, int64_t max_len, 
     p.row_tile = max_rows <= 8 ? 8 : (max_rows <= 16 ? 16 : 32);
     const int64_t tiles = (max_rows + p.row_tile - 1) / p.row_tile;
     const int64_t items = (tiles > 0 ? tiles : 1) * hkv * (batch > 0 ? batch : 1);
-    // chunks: enough CTAs for about four on every SM, none shorter than 64 keys
-    int64_t chunks = ((int64_t)num_sms * 4 + items - 1) / items;
+    // chunks where the batch alone gives fewer than four CTAs an SM: up to sixteen for every SM
+    // (requests differ in length), none shorter than 64 keys, nor than 512 unless that leaves
+    // fewer than four CTAs an SM
     const int64_t units = max_len > 0 ? (max_len + 63) / 64 : 1;
+    const int64_t few = ((int64_t)num_sms * 4 + items - 1) / items, many = ((int64_t)num_sms * 16 + items - 1) / items;
+    int64_t chunks = few == 1 ? 1 : std::min(many, std::max(few, units / 8));
     if (chunks > units) chunks = units;
     const int64_t per = (units + chunks - 1) / chunks;
     p.chunk = (int32_t)(per * 64);
     p.chunks = (int32_t)((units + per - 1) / per);
+    p.logits = max_rows > 0 && max_rows <= 32 && (int64_t)max_rows * hkv <= kLogitRows;
     return p;
 }
 

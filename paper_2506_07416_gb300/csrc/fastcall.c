@@ -297,26 +297,26 @@ static PyObject *f_verify(PyObject *self, PyObject *const *args, Py_ssize_t n)
     END
 }
 
-/* attend_bytes(handle, batch, q_offsets_h, max_len): bytes of an attention call's workspace, or -status */
+/* attend_bytes(handle, batch, q_offsets_h, max_len, weights): bytes of an attention call's workspace, or -status */
 static PyObject *f_attend_bytes(PyObject *self, PyObject *const *args, Py_ssize_t n)
 {
     (void)self;
-    if (n != 4) {
-        PyErr_SetString(PyExc_TypeError, "attend_bytes takes four arguments");
+    if (n != 5) {
+        PyErr_SetString(PyExc_TypeError, "attend_bytes takes five arguments");
         return NULL;
     }
     Held h;
     h.nbuf = h.nobj = 0;
     const int32_t *off;
-    uint64_t hd, batch, len;
+    uint64_t hd, batch, len, weights;
     if (as_bits(args[0], 'h', &hd) || as_bits(args[1], 'i', &batch) || as_host_i32(args[2], &h, &off, NULL) ||
-        as_bits(args[3], 'i', &len)) {
+        as_bits(args[3], 'i', &len) || as_bits(args[4], 'i', &weights)) {
         release(&h);
         return NULL;
     }
     int64_t bytes = 0;
-    const int rc = ((int (*)(P, I, const int32_t *, I, int64_t *))g_fn[F_SPACE])(
-        (P)(uintptr_t)hd, (I)(uint32_t)batch, off, (I)(uint32_t)len, &bytes);
+    const int rc = ((int (*)(P, I, const int32_t *, I, I, int64_t *))g_fn[F_SPACE])(
+        (P)(uintptr_t)hd, (I)(uint32_t)batch, off, (I)(uint32_t)len, (I)(uint32_t)weights, &bytes);
     release(&h);
     return PyLong_FromLongLong(rc ? -(long long)rc : (long long)bytes);
 }

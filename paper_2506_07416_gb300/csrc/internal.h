@@ -168,6 +168,9 @@ struct AttendArgs {
     float* part_o;            // [rows * hq][chunks][d] (chunks > 1)
     float2* part_ml;          // [rows * hq][chunks] reference and sum
     float* lse;               // [rows * hq] log2 of the sum of 2^s (with weights)
+    float* logits;            // [batch][hkv][max_rows][logit_stride] scores in log2 units, or null
+    int32_t max_rows;         // rows (query x head of a key head) of the longest request
+    int64_t logit_stride;
     const float* weights_in;  // [num_pages][page_size]
     float* weights_out;       // null: no weights
     int32_t* err;
@@ -175,6 +178,7 @@ struct AttendArgs {
 struct AttendPlan {
     int32_t row_tile;         // rows (query x head of a key head) of a CTA: 8, 16 or 32
     int32_t chunk, chunks;
+    bool logits;              // the weights are made from kept scores
 };
 AttendPlan plan_cache_attend(int batch, int hkv, int max_rows, int64_t max_len, int num_sms);
 cudaError_t launch_cache_attend(const AttendArgs& a, const AttendPlan& plan, int head_dim, bool fp8, int max_rows,

@@ -79,7 +79,7 @@ def _load():
     lib.litevlm_select_keep_offsets.argtypes = [i32, P, P, f32, P]
     lib.litevlm_select_cache_append.argtypes = [P, i32, P, P, i32, P, P, i64, P, i64, i64, P, P, P, f32, f32, P, P, P,
                                                 P, P]
-    lib.litevlm_select_cache_attend_workspace.argtypes = [P, i32, P, i32, ctypes.POINTER(i64)]
+    lib.litevlm_select_cache_attend_workspace.argtypes = [P, i32, P, i32, i32, ctypes.POINTER(i64)]
     lib.litevlm_select_cache_attend.argtypes = [P, i32, P, P, i32, P, P, i64, P, P, i32, f32, P, P, P, P, i64, P]
     lib.litevlm_select_cache_evict.argtypes = [P, i32, P, P, i32, P, i32, i32, i32, i32, P, i32, P, P, P, P]
     lib.litevlm_select_verify.argtypes = [P, i32, i32, i32, P, P, P, P, P, P, P, P, P, P]
@@ -307,9 +307,9 @@ def cache_append(handle: int, batch: int, cache, table, table_width: int, seq_le
         _check(rc, handle)
 
 
-def cache_attend_workspace(handle: int, batch: int, q_offsets_h, max_len: int) -> int:
+def cache_attend_workspace(handle: int, batch: int, q_offsets_h, max_len: int, weights: bool = True) -> int:
     """litevlm_select_cache_attend_workspace: bytes of the workspace of an attention call."""
-    n = _FC.attend_bytes(handle, batch, q_offsets_h, max_len)
+    n = _FC.attend_bytes(handle, batch, q_offsets_h, max_len, weights)
     if n < 0:
         _check(-n, handle)
     return n
@@ -745,7 +745,7 @@ class Selector:
             w_in = w_out = cache.weights
             if weights_out is not None:
                 w_out = _want("weights_out", weights_out, torch.float32, (cache.num_pages, cache.page_size), dev)
-        need = cache_attend_workspace(self.handle, batch, off_h, max_len)
+        need = cache_attend_workspace(self.handle, batch, off_h, max_len, w_out is not None)
         with _allocate_on(stream, dev):
             if out is None:
                 out = torch.empty((total, self.heads, self.head_dim), dtype=torch.bfloat16, device=q.device)

@@ -77,7 +77,7 @@ def test_calls_need_a_handle():
     assert L.litevlm_select_cache_append(None, 1, None, None, 1, None, None, 0, None, 0, 0, None, None, None, 1.0, 1.0,
                                          None, None, None, None, None) == 1
     n = ctypes.c_int64(-7)
-    assert L.litevlm_select_cache_attend_workspace(None, 1, None, 1, ctypes.byref(n)) == 1 and n.value == -7
+    assert L.litevlm_select_cache_attend_workspace(None, 1, None, 1, 1, ctypes.byref(n)) == 1 and n.value == -7
     assert L.litevlm_select_cache_attend(None, 1, None, None, 1, None, None, 0, None, None, 1, 1.0, None, None, None,
                                          None, 0, None) == 1
     assert L.litevlm_select_cache_evict(None, 1, None, None, 1, None, 1, 1, 0, 0, None, 0, None, None, None, None) == 1
