@@ -1336,15 +1336,16 @@ struct AttendSpace {
     int64_t part_o, part_ml, lse, logits, total;
 };
 int64_t logit_stride(int32_t max_len) { return ((int64_t)max_len + 31) & ~(int64_t)31; }
-AttendSpace attend_space(const lvs::AttendPlan& plan, int64_t rows, int head_dim, int64_t tile_rows, int32_t max_len,
-                         bool weights)
+// rows: of the call (query x head); head_rows: key heads x rows of the longest request
+AttendSpace attend_space(const lvs::AttendPlan& plan, int64_t rows, int head_dim, int64_t head_rows, int32_t batch,
+                         int32_t max_len, bool weights)
 {
     AttendSpace s{};
-    const int64_t parts = plan.chunks > 1 ? rows * plan.chunks : 0;
+    const int64_t parts = plan.slots * head_rows;
     s.part_ml = round256(parts * head_dim * 4);
     s.lse = s.part_ml + round256(parts * 8);
     s.logits = s.lse + (weights ? round256(rows * 4) : 0);
-    s.total = s.logits + (weights && plan.logits ? round256(tile_rows * logit_stride(max_len) * 4) : 0);
+    s.total = s.logits + (weights && plan.logits ? round256(batch * head_rows * logit_stride(max_len) * 4) : 0);
     return s;
 }
 
@@ -1442,7 +1443,7 @@ litevlm_status_t litevlm_select_cache_attend_workspace(litevlm_select_t h, int32
     s = attend_plan(h, batch, q_offsets_h, max_len, &plan, &total, &max_rows);
     if (s == LITEVLM_OK)
         *bytes = attend_space(plan, total * h->cfg.num_q_heads, h->cfg.head_dim,
-                              (int64_t)batch * h->cfg.num_kv_heads * max_rows, max_len, weights != 0)
+                              (int64_t)h->cfg.num_kv_heads * max_rows, batch, max_len, weights != 0)
                      .total;
     return s;
 }
@@ -1478,7 +1479,7 @@ litevlm_status_t litevlm_select_cache_attend(litevlm_select_t h, int32_t batch, 
         if (!out || !aligned16(out)) return fail(h, LITEVLM_ERR_INVALID_ARG, "out must be 16-byte aligned and not NULL");
     }
     const AttendSpace space = attend_space(plan, total * c.num_q_heads, c.head_dim,
-                                           (int64_t)batch * c.num_kv_heads * max_rows, max_len, weights_out != nullptr);
+                                           (int64_t)c.num_kv_heads * max_rows, batch, max_len, weights_out != nullptr);
     if (workspace_bytes < space.total || (space.total > 0 && !workspace))
         return fail(h, LITEVLM_ERR_WORKSPACE, "the workspace must hold " + std::to_string(space.total) + " bytes");
     if (reinterpret_cast<uintptr_t>(workspace) & 255u)
@@ -1495,8 +1496,8 @@ litevlm_status_t litevlm_select_cache_attend(litevlm_select_t h, int32_t batch, 
     a.group = c.num_q_heads / c.num_kv_heads;
     a.limit = max_len;
     a.c_log2 = (float)((double)q_scale * (double)cache->k_scale / sqrt((double)c.head_dim) * 1.4426950408889634);
-    a.chunk = plan.chunk;
-    a.chunks = plan.chunks;
+    a.slots = plan.slots;
+    a.num_sms = h->num_sms;
     a.out = static_cast<__nv_bfloat16*>(out);
     a.part_o = reinterpret_cast<float*>(ws + space.part_o);
     a.part_ml = reinterpret_cast<float2*>(ws + space.part_ml);

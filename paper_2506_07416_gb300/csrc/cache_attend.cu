@@ -33,9 +33,12 @@ namespace {
 
 constexpr int kAttWarps = 4;
 constexpr int kAttThreads = 32 * kAttWarps;
-constexpr int kAttStages = 3;        // spans of 32 keys of a warp's ring
+constexpr int kAttStages = 2;        // spans of 32 keys of a warp's ring
 constexpr float kNoRef = -3.0e38f;   // reference of a row without keys so far
 constexpr float kRefSlack = 8.f;     // a score may pass its row's reference by this
+// of a single row, whose p * scale * 2^5 is at most 2^2 * 448 * 2^5 = 57344, inside f16; the
+// factor keeps small scales' products above f16's lower end
+constexpr float kRefSlack1 = 2.f, kBoost1 = 32.f;
 
 // D += A B: 16 keys (or channels) x 8 rows, f16 operands, fp32 sums
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -113,35 +116,27 @@ __device__ __forceinline__ void load_q(const void* q, int64_t at, bool real, uin
             for (int k = 0; k < 8; ++k) f[i * 8 + k] = h2_bits(e4m3x2_value(w[k / 2] >> (16 * (k & 1))));
         }
     } else {
-        float x[N];
+        uint32_t w[N / 2];
         const uint4* s = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(q) + at);
-        float top = 0.f;
-        bool bad = false;
 #pragma unroll
         for (int i = 0; i < N / 8; ++i) {
             const uint4 v = real ? __ldg(s + i) : make_uint4(0u, 0u, 0u, 0u);
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                x[i * 8 + 2 * k] = __uint_as_float(w[k] << 16);
-                x[i * 8 + 2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
-            }
+            w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
         }
+        // the largest magnitude's bits (as integers they order the magnitudes, NaN above infinity above the rest)
+        uint32_t top = 0u;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            top = fmaxf(top, fabsf(x[i]));
-            bad |= !(fabsf(x[i]) <= 3.4028234e38f);
-        }
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        const uint32_t any_bad = __ballot_sync(0xffffffffu, bad);
-        bad = (any_bad >> (threadIdx.x & 28)) & 15u;
+        for (int i = 0; i < N / 2; ++i) top = __vmaxu2(top, w[i] & 0x7FFF7FFFu);
+        top = max(top & 0xFFFFu, top >> 16);
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
         // exponent field of the factor: 127 + 10 - (that of top - 127), at most 2^126
-        const int e = min(264 - (int)(__float_as_uint(top) >> 23), 253);
-        const float up = bad ? __int_as_float(0x7FC00000) : __int_as_float(e << 23);
+        const int e = min(264 - (int)(top >> 7), 253);
+        const float up = __int_as_float(top >= 0x7F80u ? 0x7FC00000 : e << 23);
         back = __int_as_float((254 - e) << 23);
 #pragma unroll
-        for (int i = 0; i < N / 2; ++i) f[i] = pack_h2(x[2 * i] * up, x[2 * i + 1] * up);
+        for (int i = 0; i < N / 2; ++i)
+            f[i] = pack_h2(__uint_as_float(w[i] << 16) * up, __uint_as_float(w[i] & 0xFFFF0000u) * up);
     }
 }
 
@@ -199,6 +194,9 @@ __device__ __forceinline__ void score_group(const uint8_t* grp, int lane, QF qf,
 // What every CTA of a request's tile needs to know of its rows.
 struct RowTile {
     int len, t, row0, rows, last0;  // last0: position of the first query
+    int group;
+    // query of a row (a row's head is its key head's first plus the rest)
+    __device__ __forceinline__ int query(int row) const { return t == 1 ? 0 : row / group; }
 };
 
 __device__ __forceinline__ RowTile row_tile(const AttendArgs& a, int b, int tile, int per)
@@ -211,15 +209,62 @@ __device__ __forceinline__ RowTile row_tile(const AttendArgs& a, int b, int tile
     r.row0 = tile * per;
     r.rows = min(per, r.t * a.group - r.row0);
     r.last0 = r.len - r.t;
+    r.group = a.group;
     return r;
+}
+
+// How the keys are split, found by a warp from the lengths on the device: equal chunks, as
+// short as they may be while all requests together have at most a.slots of them (the CTAs
+// that run at once), so that neither lengths that differ nor a max_len far above them leave
+// SMs without work. Of 32 candidate lengths from the mean on, in steps of an eighth of it,
+// the first that fits is taken. Requests without queries take no part.
+__device__ __forceinline__ int keys_of(const AttendArgs& a, int b)
+{
+    bool bad;
+    const int n = cache_len(__ldg(a.lens + b), a.limit, bad);
+    return __ldg(a.q_off + b + 1) > __ldg(a.q_off + b) ? n : 0;
+}
+__device__ __forceinline__ int chunks_of(int keys, int chunk) { return (int)(((unsigned)keys + chunk - 1) / (unsigned)chunk); }
+__device__ __forceinline__ int chunk_keys(const AttendArgs& a)
+{
+    if (a.batch == 1) return max(64, (chunks_of(keys_of(a, 0), a.slots) + 63) & ~63);
+    const int lane = threadIdx.x & 31;
+    long long total = 0;
+    for (int b = lane; b < a.batch; b += 32) total += keys_of(a, b);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
+    const long long mean = (total + a.slots - 1) / a.slots;
+    const int mine = (int)min((long long)INT32_MAX / 2, (mean + mean * lane / 8 + 63) & ~63ll);
+    const unsigned c = (unsigned)max(mine, 64);
+    long long count = 0;
+    for (int b = 0; b < a.batch; ++b) count += ((unsigned)keys_of(a, b) + c - 1) / c;
+    const uint32_t fits = __ballot_sync(0xffffffffu, count <= a.slots);
+    return fits ? (int)__shfl_sync(0xffffffffu, c, __ffs(fits) - 1) : (a.limit + 63) & ~63;
+}
+// Chunks of the requests before b.
+__device__ __forceinline__ int chunks_before(const AttendArgs& a, int b, int chunk)
+{
+    int n = 0;
+    for (int x = threadIdx.x & 31; x < b; x += 32) n += chunks_of(keys_of(a, x), chunk);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) n += __shfl_xor_sync(0xffffffffu, n, d);
+    return n;
 }
 
 template <int D>
 constexpr int kRingBytes = kAttWarps * kAttStages * 2 * Group<D>::kBytes;
 
-template <int D, int NT, bool FP8>
+// NT: tiles of 8 rows of a CTA; 0: a single row (a decoded token of a head with keys of its
+// own). The eight columns of the contractions, of which a single row would use one, then
+// take the scales, which costs no multiplication of the values: column n of QK holds the
+// row's channels of scale block n alone, and the score is the sum of the columns times the
+// key's scales; column n of PV holds p times the scales of block n, and the channels of
+// block n are read from column n.
+template <int D, int NT_, bool FP8>
 __global__ void __launch_bounds__(kAttThreads) attend_split_kernel(const __grid_constant__ AttendArgs a)
 {
+    constexpr bool SINGLE = NT_ == 0;
+    constexpr int NT = SINGLE ? 1 : NT_;
     using G = Group<D>;
     constexpr int ROWS = 8 * NT;
     constexpr bool Q_SMEM = NT > 2;  // fragments of 32 rows would take 64 registers
@@ -234,18 +279,31 @@ __global__ void __launch_bounds__(kAttThreads) attend_split_kernel(const __grid_
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int g = lane >> 2, c = lane & 3;
-    const int b = blockIdx.z, h = blockIdx.y % a.cache.hkv, tile = blockIdx.y / a.cache.hkv;
+    const int h = blockIdx.y % a.cache.hkv, tile = blockIdx.y / a.cache.hkv;
     griddep_wait();
     griddep_launch_dependents();
+    // the request, and its part of the keys: all, or the chunk of this CTA's slot
+    int b = blockIdx.z, chunk = INT32_MAX / 2, k0 = 0;
+    if (a.slots > 0) {
+        chunk = chunk_keys(a);
+        int at = blockIdx.x;
+        for (b = 0; b < a.batch; ++b) {
+            const int n = chunks_of(keys_of(a, b), chunk);
+            if (at < n) break;
+            at -= n;
+        }
+        if (b == a.batch) return;
+        k0 = at * chunk;
+    }
     const RowTile rt = row_tile(a, b, tile, ROWS);
     if (rt.rows <= 0) return;
     const int q0 = a.q_off[b];
-    const int i_last = (rt.row0 + rt.rows - 1) / a.group;
+    const int i_last = rt.query(rt.row0 + rt.rows - 1);
     // keys that the tile's last row sees, and this CTA's part of them
     const int seen = min(rt.len, rt.last0 + i_last + 1);
-    const int k0 = blockIdx.x * a.chunk, k1 = min(seen, k0 + a.chunk);
-    if (k0 >= k1 && blockIdx.x > 0) return;  // (the first chunk of a tile without keys writes its zeros)
-    const int all_see = rt.last0 + rt.row0 / a.group;  // the last key that every row sees
+    const int k1 = min(seen, k0 + chunk);
+    if (k0 >= k1 && a.slots > 0) return;  // (without chunks the tile's zeros are written here, else by the join)
+    const int all_see = rt.last0 + rt.query(rt.row0);  // the last key that every row sees
 
     constexpr int SPAN = 2 * G::kBytes;
     uint8_t* my = ring + warp * kAttStages * SPAN;
@@ -280,8 +338,9 @@ __global__ void __launch_bounds__(kAttThreads) attend_split_kernel(const __grid_
         const int r = t * 8 + g;
         const bool real = r < rt.rows;
         const int row = rt.row0 + (real ? r : 0);
-        const int64_t at = (int64_t)(q0 + row / a.group) * a.q_stride + (int64_t)(h * a.group + row % a.group) * D +
-                           c * (D / 4);
+        const int i = rt.query(row);
+        const int64_t at =
+            (int64_t)(q0 + i) * a.q_stride + (int64_t)(h * a.group + row - i * a.group) * D + c * (D / 4);
         float back;
         if constexpr (Q_SMEM) {
             if (t % kAttWarps == warp) {
@@ -292,12 +351,17 @@ __global__ void __launch_bounds__(kAttThreads) attend_split_kernel(const __grid_
                 if (c == 0) back_s[r] = back;
             }
         } else {
-            load_q<D, FP8>(a.q, at, real, qr[t], back);
+            load_q<D, FP8>(a.q, at, SINGLE || real, qr[t], back);
+            if constexpr (SINGLE) {  // (every lane has read row 0; lane (g, c) keeps what lies in block g)
+#pragma unroll
+                for (int k = 0; k < D / 8; ++k)
+                    if (D == 128 ? g != 2 * c + k / 8 : g != c) qr[0][k] = 0u;
+            }
             fac[t][0] = a.c_log2 * __shfl_sync(0xffffffffu, back, 8 * c);
             fac[t][1] = a.c_log2 * __shfl_sync(0xffffffffu, back, 8 * c + 4);
         }
 #pragma unroll
-        for (int e = 0; e < 2; ++e) vis[t][e] = rt.last0 + (rt.row0 + t * 8 + 2 * c + e) / a.group;
+        for (int e = 0; e < 2; ++e) vis[t][e] = rt.last0 + rt.query(rt.row0 + t * 8 + 2 * c + e);
     }
     if constexpr (Q_SMEM) {
         __syncthreads();
@@ -326,9 +390,118 @@ __global__ void __launch_bounds__(kAttThreads) attend_split_kernel(const __grid_
     float* logits = a.logits + (((int64_t)b * a.cache.hkv + h) * a.max_rows + rt.row0 + 2 * c) * a.logit_stride;
     bool nan_value = false;
 
+    // a group of 16 keys from j0 on, for a single row
+    auto group1 = [&](const uint8_t* grp, int j0, bool there, auto check) {
+        constexpr bool CHECK = decltype(check)::value;
+        constexpr int WORDS = D / 32;
+        float s[4] = {0.f, 0.f, 0.f, 0.f};
+        float ks[2][2];  // scales of the keys g and g + 8 in the blocks 2c and 2c + 1
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int at = G::kKs + (g + 8 * e) * (D / 16) + 2 * c;
+            const float2 f = __half22float2(e4m3x2_value(*reinterpret_cast<const uint16_t*>(grp + (D == 128 || c < 2 ? at : 0))));
+            ks[e][0] = D == 128 || c < 2 ? f.x : 0.f;
+            ks[e][1] = D == 128 || c < 2 ? f.y : 0.f;
+        }
+        uint32_t w0[WORDS], w1[WORDS];
+        if constexpr (D == 128) {
+            const uint4 x = *reinterpret_cast<const uint4*>(grp + G::kK + g * 64 + c * 16);
+            const uint4 y = *reinterpret_cast<const uint4*>(grp + G::kK + (g + 8) * 64 + c * 16);
+            w0[0] = x.x, w0[1] = x.y, w0[2] = x.z, w0[3] = x.w;
+            w1[0] = y.x, w1[1] = y.y, w1[2] = y.z, w1[3] = y.w;
+        } else {
+            const uint2 x = *reinterpret_cast<const uint2*>(grp + G::kK + g * 32 + c * 8);
+            const uint2 y = *reinterpret_cast<const uint2*>(grp + G::kK + (g + 8) * 32 + c * 8);
+            w0[0] = x.x, w0[1] = x.y;
+            w1[0] = y.x, w1[1] = y.y;
+        }
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) {
+            __half2 x[4], y[4];
+            e2m1x8_value(w0[w], x);
+            e2m1x8_value(w1[w], y);
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                mma16816(s, h2_bits(x[2 * e]), h2_bits(y[2 * e]), h2_bits(x[2 * e + 1]), h2_bits(y[2 * e + 1]),
+                         qr[0][4 * w + 2 * e], qr[0][4 * w + 2 * e + 1]);
+        }
+        float z[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            z[e] = fmaf(s[2 * e], ks[e][0], s[2 * e + 1] * ks[e][1]);
+            z[e] += __shfl_xor_sync(0xffffffffu, z[e], 1);
+            z[e] += __shfl_xor_sync(0xffffffffu, z[e], 2);
+            z[e] *= fac[0][0];
+            if (CHECK && (!there || j0 + g + 8 * e >= k1)) z[e] = -INFINITY;
+        }
+        if (a.logits && c == 0) {
+            __stcg(logits + j0 + g, z[0]);
+            __stcg(logits + j0 + g + 8, z[1]);
+        }
+        if (__any_sync(0xffffffffu, fmaxf(z[0], z[1]) > m[0][0] + kRefSlack1)) {
+            float x = fmaxf(z[0], z[1]);
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+            const float mn = fmaxf(m[0][0], x);
+            const float f = ex2(m[0][0] - mn);
+            m[0][0] = mn;
+            l[0][0] *= f;
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[0][i][e] *= f;
+        }
+        const float p0 = ex2(z[0] - m[0][0]), p1 = ex2(z[1] - m[0][0]);
+        l[0][0] += p0 + p1;
+        // probabilities of the lane's keys of the second product (2c, 2c+1, 2c+8, 2c+9)
+        float pk[4];
+        pk[0] = __shfl_sync(0xffffffffu, p0, 8 * c);
+        pk[1] = __shfl_sync(0xffffffffu, p0, 8 * c + 4);
+        pk[2] = __shfl_sync(0xffffffffu, p1, 8 * c);
+        pk[3] = __shfl_sync(0xffffffffu, p1, 8 * c + 4);
+        constexpr int VW = D / 64;
+        uint32_t x[4][VW], sc[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int key = 2 * c + (e & 1) + 8 * (e >> 1);
+            if constexpr (D == 128) {
+                const uint2 v = *reinterpret_cast<const uint2*>(grp + G::kV + key * 64 + g * 8);
+                x[e][0] = v.x, x[e][1] = v.y;
+                sc[e] = grp[G::kVs + key * 8 + g];
+            } else {
+                x[e][0] = *reinterpret_cast<const uint32_t*>(grp + G::kV + key * 32 + g * 4);
+                sc[e] = grp[G::kVs + key * 4 + g / 2];
+            }
+            if (CHECK && j0 + key >= k1) sc[e] = 0u;  // (bytes behind the last key may be anything)
+        }
+        const float2 sa = __half22float2(e4m3x2_value(sc[0] | (sc[1] << 8)));
+        const float2 sb = __half22float2(e4m3x2_value(sc[2] | (sc[3] << 8)));
+        const uint32_t b0 = pack_h2(pk[0] * (sa.x * kBoost1), pk[1] * (sa.y * kBoost1));
+        const uint32_t b1 = pack_h2(pk[2] * (sb.x * kBoost1), pk[3] * (sb.y * kBoost1));
+#pragma unroll
+        for (int w = 0; w < VW; ++w) {
+            const uint32_t lo = 0x0F0F0F0Fu;
+            const uint32_t ae = (x[0][w] & lo) | ((x[1][w] << 4) & ~lo), ao = ((x[0][w] >> 4) & lo) | (x[1][w] & ~lo);
+            const uint32_t be = (x[2][w] & lo) | ((x[3][w] << 4) & ~lo), bo = ((x[2][w] >> 4) & lo) | (x[3][w] & ~lo);
+            __half2 a0[4], a1[4], a2[4], a3[4];
+            e2m1x8_value(ae, a0);
+            e2m1x8_value(ao, a1);
+            e2m1x8_value(be, a2);
+            e2m1x8_value(bo, a3);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                mma16816(o[0][w * 4 + i], h2_bits(a0[i]), h2_bits(a1[i]), h2_bits(a2[i]), h2_bits(a3[i]), b0, b1);
+        }
+    };
+
     // a group of 16 keys from j0 on; CHECK: some of the rows do not see all of them
     auto group = [&](const uint8_t* grp, int j0, bool there, auto check) {
         constexpr bool CHECK = decltype(check)::value;
+        if constexpr (SINGLE) {
+            group1(grp, j0, there, check);
+            return;
+        }
         float s[NT][4];
         score_group<D, NT>(grp, lane, qf, s);
 #pragma unroll
@@ -477,17 +650,27 @@ __global__ void __launch_bounds__(kAttThreads) attend_split_kernel(const __grid_
     float* jo = reinterpret_cast<float*>(ring);  // [warp][row][D + 4]
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        __syncthreads();
+        const int rows = min(8, rt.rows - t * 8);
+        if (rows <= 0) break;
+        if (t > 0) __syncthreads();
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+        for (int e = 0; e < 2; ++e)
+            if (!SINGLE && 2 * c + e < rows) {
+                float* to = jo + (warp * 8 + 2 * c + e) * (D + 4) + g * (D / 8);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                jo[(warp * 8 + 2 * c + (e & 1)) * (D + 4) + g * (D / 8) + 2 * i + (e >> 1)] = o[t][i][e];
+                for (int i = 0; i < MT; ++i) *reinterpret_cast<float2*>(to + 2 * i) = make_float2(o[t][i][e], o[t][i][e + 2]);
+            }
+        if (SINGLE && c == g >> 1) {  // column g holds the channels of lane g
+            float* to = jo + warp * 8 * (D + 4) + g * (D / 8);
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+                *reinterpret_cast<float2*>(to + 2 * i) =
+                    g & 1 ? make_float2(o[0][i][1], o[0][i][3]) : make_float2(o[0][i][0], o[0][i][2]);
+        }
         __syncthreads();
-        for (int x = tid; x < 8 * D; x += kAttThreads) {
+        for (int x = tid; x < rows * D; x += kAttThreads) {
             const int r = x / D, ch = x % D;
             const int row = t * 8 + r;
-            if (row >= rt.rows) continue;
             float M = kNoRef;
 #pragma unroll
             for (int w = 0; w < kAttWarps; ++w) M = fmaxf(M, s_m[w][row]);
@@ -498,10 +681,11 @@ __global__ void __launch_bounds__(kAttThreads) attend_split_kernel(const __grid_
                 L += s_l[w][row] * f;
                 O += jo[(w * 8 + r) * (D + 4) + ch] * f;
             }
-            const int rr = rt.row0 + row;
-            const int64_t at = (int64_t)(q0 + rr / a.group) * a.hq + h * a.group + rr % a.group;
+            if constexpr (SINGLE) O *= 1.f / kBoost1;
+            const int rr = rt.row0 + row, i = rt.query(rr);
+            const int64_t at = (int64_t)(q0 + i) * a.hq + h * a.group + rr - i * a.group;
             if (nan_value) {
-                for (int j = max(k0, all_see + 1); j < min(k1, rt.last0 + rr / a.group + 1); ++j) {
+                for (int j = max(k0, all_see + 1); j < min(k1, rt.last0 + i + 1); ++j) {
                     const int32_t page =
                         cache_page(a.cache.table, a.cache.width, a.cache.num_pages, a.cache.page_shift, b, j);
                     if (page < 0) continue;
@@ -510,12 +694,12 @@ __global__ void __launch_bounds__(kAttThreads) attend_split_kernel(const __grid_
                     if ((a.cache.scales[1][at_row * (D / 16) + ch / 16] & 0x7Fu) == 0x7Fu) O = __int_as_float(0x7FC00000);
                 }
             }
-            if (a.chunks == 1) {
+            if (a.slots == 0) {
                 // (a row that sees no key is 0; the comparison keeps a NaN sum)
                 a.out[at * D + ch] = __float2bfloat16_rn(L == 0.f ? 0.f : O / L * a.cache.scale[1]);
                 if (a.lse && ch == 0) a.lse[at] = L == 0.f ? INFINITY : M + log2f(L);
             } else {
-                const int64_t part = at * a.chunks + blockIdx.x;
+                const int64_t part = ((int64_t)blockIdx.x * a.cache.hkv + h) * a.max_rows + rr;
                 a.part_o[part * D + ch] = O;
                 if (ch == 0) a.part_ml[part] = make_float2(M, L);
             }
@@ -523,22 +707,34 @@ __global__ void __launch_bounds__(kAttThreads) attend_split_kernel(const __grid_
     }
 }
 
-// Log2 of a row's sum of 2^s from its chunks' references and sums, by a warp: the row's
-// reference and sum too.
-__device__ __forceinline__ float2 join_stats(const float2* ml, int n)
+// Reference and sum of a row from those of its n chunks (`step` apart), by a warp.
+__device__ __forceinline__ float2 join_stats(const float2* ml, int64_t step, int n)
 {
     const int lane = threadIdx.x & 31;
     float M = kNoRef, L = 0.f;
-    for (int x = lane; x < n; x += 32) M = fmaxf(M, __ldcg(ml + x).x);
+    constexpr int U = 4;
+    for (int x0 = 0; x0 < n; x0 += 32 * U) {
+        float2 v[U];
+        float mx = M;
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
-    for (int x = lane; x < n; x += 32) {
-        const float2 v = __ldcg(ml + x);
-        L += v.y * ex2(v.x - M);
+        for (int u = 0; u < U; ++u) {
+            const int x = x0 + u * 32 + lane;
+            v[u] = x < n ? __ldcg(ml + x * step) : make_float2(kNoRef, 0.f);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) mx = fmaxf(mx, v[u].x);
+        L *= ex2(M - mx);
+        M = mx;
+#pragma unroll
+        for (int u = 0; u < U; ++u) L += v[u].y * ex2(v[u].x - M);
     }
+    float top = M;
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+    L *= ex2(M - top);
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) L += __shfl_xor_sync(0xffffffffu, L, d);
-    return make_float2(M, L);
+    return make_float2(top, L);
 }
 
 constexpr int kFinishThreads = 512;
@@ -576,13 +772,13 @@ __device__ __forceinline__ float4 add_weights(const float* s, int64_t stride, co
     return sum;
 }
 
-// The first `weight_blocks` CTAs of a request add the weights of 512 keys each from the
-// kept scores, over the rows in order; the others join chunks, `row_warps` warps a row.
+// The first `join_blocks` CTAs of a request join its rows' chunks, `row_warps` warps a row;
+// the others add weights from the kept scores, 512 keys at a time, over the rows in order.
 // A weight CTA finds the rows' lse from the chunks' statistics by itself, which saves a
 // launch between the two.
 template <int D>
 __global__ void __launch_bounds__(kFinishThreads) attend_finish_kernel(const __grid_constant__ AttendArgs a,
-                                                                       int weight_blocks, int row_warps)
+                                                                       int join_blocks, int row_warps)
 {
     extern __shared__ uint8_t rows_s[];
     // the warps' parts: four weights a lane, or a row of outputs a warp (D <= 128)
@@ -594,34 +790,41 @@ __global__ void __launch_bounds__(kFinishThreads) attend_finish_kernel(const __g
     bool bad;
     const int len = cache_len(a.lens[b], a.limit, bad);
     const int q0 = a.q_off[b], t = a.q_off[b + 1] - q0;
+    int chunk = INT32_MAX / 2, slot0 = 0;
+    if (a.slots > 0 && t > 0) {
+        chunk = chunk_keys(a);
+        slot0 = chunks_before(a, b, chunk);
+    }
+    const int64_t step = (int64_t)a.cache.hkv * a.max_rows;  // from a chunk's statistics to the next's
     // chunks with keys that query i sees
-    auto chunks_of = [&](int i) -> int {
+    auto chunks_seen = [&](int i) -> int {
         const int seen = len - t + i + 1;
-        return seen > 0 ? (seen + a.chunk - 1) / a.chunk : 0;
+        return seen > 0 ? chunks_of(seen, chunk) : 0;
     };
-    if ((int)blockIdx.x < weight_blocks) {
-        const int j0 = blockIdx.x * kFinishKeys;
-        if (j0 >= len) return;
+    if ((int)blockIdx.x >= join_blocks) {
         const int rows = t * a.group, n = rows * a.cache.hkv;
+        const int tiles = (len + kFinishKeys - 1) / kFinishKeys;
+        int tile = blockIdx.x - join_blocks;
+        if (tile >= tiles) return;
         float* lse_s = reinterpret_cast<float*>(rows_s);
         int2* row_s = reinterpret_cast<int2*>(rows_s + (size_t)((n + 1) & ~1) * 4);  // scores' row, last key seen
-        const bool by_warp = a.chunks > 16;
+        const int most = t > 0 ? chunks_seen(t - 1) : 0;
+        const bool by_warp = most > 16;
         for (int x = by_warp ? warp : tid; x < n; x += by_warp ? kFinishWarps : kFinishThreads) {
             const int h = x / rows, r = x % rows, i = r / a.group;
-            const int64_t at = (int64_t)(q0 + i) * a.hq + h * a.group + r % a.group;
             float lse;
-            if (a.chunks == 1) {
-                lse = __ldcg(a.lse + at);
+            if (a.slots == 0) {
+                lse = __ldcg(a.lse + (int64_t)(q0 + i) * a.hq + h * a.group + r % a.group);
             } else {
+                const float2* from = a.part_ml + ((int64_t)slot0 * a.cache.hkv + h) * a.max_rows + r;
                 float2 ml = make_float2(kNoRef, 0.f);
                 if (by_warp) {
-                    ml = join_stats(a.part_ml + at * a.chunks, chunks_of(i));
+                    ml = join_stats(from, step, chunks_seen(i));
                 } else {
                     float2 v[16];
-                    const int m = chunks_of(i);
+                    const int m = chunks_seen(i);
 #pragma unroll
-                    for (int y = 0; y < 16; ++y)
-                        v[y] = y < m ? __ldcg(a.part_ml + at * a.chunks + y) : make_float2(kNoRef, 0.f);
+                    for (int y = 0; y < 16; ++y) v[y] = y < m ? __ldcg(from + y * step) : make_float2(kNoRef, 0.f);
 #pragma unroll
                     for (int y = 0; y < 16; ++y) ml.x = fmaxf(ml.x, v[y].x);
 #pragma unroll
@@ -635,48 +838,54 @@ __global__ void __launch_bounds__(kFinishThreads) attend_finish_kernel(const __g
             }
         }
         __syncthreads();
-        // four neighbouring keys a lane (the scores' rows are padded to a whole number of them)
         const int part = warp >> 2, per = (n + 3) / 4;
         const int x0 = min(n, part * per), x1 = min(n, x0 + per);
-        const int j = j0 + (warp & 3) * 128 + 4 * lane;
-        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (j < len) {
-            const float* s = a.logits + (int64_t)b * a.cache.hkv * a.max_rows * a.logit_stride + j;
-            sum = j0 + kFinishKeys - 1 <= len - t ? add_weights<false>(s, a.logit_stride, row_s, lse_s, x0, x1, j)
-                                                  : add_weights<true>(s, a.logit_stride, row_s, lse_s, x0, x1, j);
-        }
-        float4* sums = reinterpret_cast<float4*>(&join_s[0][0]);  // [part][128 lanes of the tile]
-        sums[warp * 32 + lane] = sum;
-        __syncthreads();
-        if (part != 0 || j >= len) return;
+        for (; tile < tiles; tile += gridDim.x - join_blocks) {
+            // four neighbouring keys a lane (the scores' rows are padded to a whole number of them)
+            const int j0 = tile * kFinishKeys, j = j0 + (warp & 3) * 128 + 4 * lane;
+            int32_t page = -1;
+            if (part == 0 && j < len)
+                page = cache_page(a.cache.table, a.cache.width, a.cache.num_pages, a.cache.page_shift, b, j);
+            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (j < len) {
+                const float* s = a.logits + (int64_t)b * a.cache.hkv * a.max_rows * a.logit_stride + j;
+                sum = j0 + kFinishKeys - 1 <= len - t ? add_weights<false>(s, a.logit_stride, row_s, lse_s, x0, x1, j)
+                                                      : add_weights<true>(s, a.logit_stride, row_s, lse_s, x0, x1, j);
+            }
+            float4* sums = reinterpret_cast<float4*>(&join_s[0][0]);  // [part][128 lanes of the tile]
+            sums[warp * 32 + lane] = sum;
+            __syncthreads();
+            if (page >= 0) {
+                const int64_t at = ((int64_t)page << a.cache.page_shift) + (j & ((1 << a.cache.page_shift) - 1));
 #pragma unroll
-        for (int p = 1; p < 4; ++p) {
-            const float4 v = sums[(warp + 4 * p) * 32 + lane];
-            sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
-        }
-        const int32_t page = cache_page(a.cache.table, a.cache.width, a.cache.num_pages, a.cache.page_shift, b, j);
-        if (page < 0) return;
-        const int64_t at = ((int64_t)page << a.cache.page_shift) + (j & ((1 << a.cache.page_shift) - 1));
-        const float add[4] = {sum.x, sum.y, sum.z, sum.w};
+                for (int p = 1; p < 4; ++p) {
+                    const float4 v = sums[(warp + 4 * p) * 32 + lane];
+                    sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
+                }
+                const float add[4] = {sum.x, sum.y, sum.z, sum.w};
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (j + e < len) a.weights_out[at + e] = a.weights_in[at + e] + add[e] / (float)a.hq;
+                for (int e = 0; e < 4; ++e)
+                    if (j + e < len) a.weights_out[at + e] = a.weights_in[at + e] + add[e] / (float)a.hq;
+            }
+            __syncthreads();
+        }
         return;
     }
     const int part = warp % row_warps;
-    const int r = (blockIdx.x - weight_blocks) * (kFinishWarps / row_warps) + warp / row_warps;
+    const int r = blockIdx.x * (kFinishWarps / row_warps) + warp / row_warps;  // query and head
     const bool real = r < t * a.hq;
-    const int64_t at = (int64_t)q0 * a.hq + (real ? r : 0);
-    const int n = real ? chunks_of(r / a.hq) : 0;
-    const float2 ml = join_stats(a.part_ml + at * a.chunks, n);
+    const int i = real ? r / a.hq : 0, hq = real ? r % a.hq : 0, h = hq / a.group;
+    const int n = real ? chunks_seen(i) : 0;
+    const int64_t from = ((int64_t)slot0 * a.cache.hkv + h) * a.max_rows + i * a.group + hq - h * a.group;
+    const float2 ml = join_stats(a.part_ml + from, step, n);
     const float M = ml.x, L = ml.y;
     float O[D / 32];
 #pragma unroll
     for (int e = 0; e < D / 32; ++e) O[e] = 0.f;
 #pragma unroll 4
     for (int x = part; x < n; x += row_warps) {
-        const float f = ex2(__ldcg(a.part_ml + at * a.chunks + x).x - M);
-        const float* p = a.part_o + (at * a.chunks + x) * D + lane * (D / 32);
+        const float f = ex2(__ldcg(a.part_ml + from + x * step).x - M);
+        const float* p = a.part_o + (from + x * step) * D + lane * (D / 32);
         if constexpr (D == 128) {
             const float4 v = __ldcg(reinterpret_cast<const float4*>(p));
             O[0] += v.x * f, O[1] += v.y * f, O[2] += v.z * f, O[3] += v.w * f;
@@ -695,6 +904,7 @@ __global__ void __launch_bounds__(kFinishThreads) attend_finish_kernel(const __g
             for (int e = 0; e < D / 32; ++e) O[e] += join_s[warp + w][lane * (D / 32) + e];
     }
     if (!real) return;
+    const int64_t at = (int64_t)q0 * a.hq + r;
     const float vs = a.cache.scale[1];
 #pragma unroll
     for (int e = 0; e < D / 32; e += 2) {
@@ -792,9 +1002,11 @@ cudaError_t launch_all(const AttendArgs& a, const AttendPlan& plan, int max_rows
     cudaError_t e = cudaSuccess;
     if (total_rows > 0) {
         const int tiles = (max_rows + plan.row_tile - 1) / plan.row_tile;
-        cfg.gridDim = dim3((unsigned)plan.chunks, (unsigned)(tiles * a.cache.hkv), (unsigned)a.batch);
+        cfg.gridDim = plan.slots > 0 ? dim3((unsigned)plan.slots, (unsigned)(tiles * a.cache.hkv), 1)
+                                     : dim3(1, (unsigned)(tiles * a.cache.hkv), (unsigned)a.batch);
         cfg.blockDim = dim3(kAttThreads, 1, 1);
-        auto kern = plan.row_tile == 8    ? attend_split_kernel<D, 1, FP8>
+        auto kern = max_rows == 1         ? attend_split_kernel<D, 0, FP8>
+                    : plan.row_tile == 8  ? attend_split_kernel<D, 1, FP8>
                     : plan.row_tile == 16 ? attend_split_kernel<D, 2, FP8>
                                           : attend_split_kernel<D, 4, FP8>;
         cfg.dynamicSmemBytes = kRingBytes<D>;
@@ -804,16 +1016,20 @@ cudaError_t launch_all(const AttendArgs& a, const AttendPlan& plan, int max_rows
         ++*launches;
         cfg.dynamicSmemBytes = 0;
     }
-    const int weight_blocks = a.logits ? (max_len + kFinishKeys - 1) / kFinishKeys : 0;
     const int most = max_rows / a.group * a.hq;  // rows of the longest request
-    const int row_warps = plan.chunks <= 4 ? 1 : (plan.chunks <= 16 ? 4 : kFinishWarps);
+    // warps of a row by the chunks that a request has where all are alike
+    const int chunks = (plan.slots + a.batch - 1) / a.batch;
+    const int row_warps = chunks <= 4 ? 1 : (chunks <= 16 ? 4 : kFinishWarps);
     const int join_rows = kFinishWarps / row_warps;  // of a CTA
-    const int join_blocks = total_rows > 0 && plan.chunks > 1 ? (most + join_rows - 1) / join_rows : 0;
+    const int join_blocks = total_rows > 0 && plan.slots > 0 ? (most + join_rows - 1) / join_rows : 0;
+    // a CTA for every 512 keys, as many as run at once
+    const int weight_blocks =
+        a.logits ? std::min((max_len + kFinishKeys - 1) / kFinishKeys, std::max(1, 3 * a.num_sms / a.batch)) : 0;
     if (weight_blocks + join_blocks > 0) {
         cfg.gridDim = dim3((unsigned)(weight_blocks + join_blocks), (unsigned)a.batch, 1);
         cfg.blockDim = dim3(kFinishThreads, 1, 1);
         cfg.dynamicSmemBytes = a.logits ? (size_t)(most + 2) * 12 : 0;
-        e = cudaLaunchKernelEx(&cfg, attend_finish_kernel<D>, a, weight_blocks, row_warps);
+        e = cudaLaunchKernelEx(&cfg, attend_finish_kernel<D>, a, join_blocks, row_warps);
         if (e != cudaSuccess) return e;
         ++*launches;
         cfg.dynamicSmemBytes = 0;
@@ -835,17 +1051,16 @@ AttendPlan plan_cache_attend(int batch, int hkv, int max_rows, int64_t max_len, 
     AttendPlan p;
     p.row_tile = max_rows <= 8 ? 8 : (max_rows <= 16 ? 16 : 32);
     const int64_t tiles = (max_rows + p.row_tile - 1) / p.row_tile;
-    const int64_t items = (tiles > 0 ? tiles : 1) * hkv * (batch > 0 ? batch : 1);
-    // chunks where the batch alone gives fewer than four CTAs an SM: up to sixteen for every SM
-    // (requests differ in length), none shorter than 64 keys, nor than 512 unless that leaves
-    // fewer than four CTAs an SM
-    const int64_t units = max_len > 0 ? (max_len + 63) / 64 : 1;
-    const int64_t few = ((int64_t)num_sms * 4 + items - 1) / items, many = ((int64_t)num_sms * 16 + items - 1) / items;
-    int64_t chunks = few == 1 ? 1 : std::min(many, std::max(few, units / 8));
-    if (chunks > units) chunks = units;
-    const int64_t per = (units + chunks - 1) / chunks;
-    p.chunk = (int32_t)(per * 64);
-    p.chunks = (int32_t)((units + per - 1) / per);
+    const int64_t per_key = (tiles > 0 ? tiles : 1) * hkv;  // CTAs for every chunk
+    const int64_t items = per_key * (batch > 0 ? batch : 1);
+    // Four CTAs run on an SM. Where the batch has fewer than two for every one of these places,
+    // the keys are split over that many CTAs; else a CTA takes all keys of its rows.
+    const int64_t places = (int64_t)num_sms * 4;
+    p.slots = 0;
+    if (max_len > 64 && items < 2 * places) {
+        const int64_t units = (max_len + 63) / 64 * (batch > 0 ? batch : 1);
+        p.slots = (int32_t)std::min(units, std::max((int64_t)batch, places / per_key));
+    }
     p.logits = max_rows > 0 && max_rows <= 32 && (int64_t)max_rows * hkv <= kLogitRows;
     return p;
 }

@@ -163,10 +163,11 @@ struct AttendArgs {
     int32_t batch, hq, group; // group: query heads of a key head
     int32_t limit;            // no request is longer
     float c_log2;             // q_scale * k_scale / sqrt(d) * log2(e)
-    int32_t chunk, chunks;    // keys of a chunk (a multiple of 64), chunks of the longest request
+    int32_t slots;            // chunks that the requests' keys are split into, all together (0: not split)
+    int32_t num_sms;
     __nv_bfloat16* out;       // [rows][hq][d]
-    float* part_o;            // [rows * hq][chunks][d] (chunks > 1)
-    float2* part_ml;          // [rows * hq][chunks] reference and sum
+    float* part_o;            // [slots][hkv][max_rows][d] sums of a chunk's rows
+    float2* part_ml;          // [slots][hkv][max_rows] their references and sums of 2^s
     float* lse;               // [rows * hq] log2 of the sum of 2^s (with weights)
     float* logits;            // [batch][hkv][max_rows][logit_stride] scores in log2 units, or null
     int32_t max_rows;         // rows (query x head of a key head) of the longest request
@@ -177,7 +178,7 @@ struct AttendArgs {
 };
 struct AttendPlan {
     int32_t row_tile;         // rows (query x head of a key head) of a CTA: 8, 16 or 32
-    int32_t chunk, chunks;
+    int32_t slots;
     bool logits;              // the weights are made from kept scores
 };
 AttendPlan plan_cache_attend(int batch, int hkv, int max_rows, int64_t max_len, int num_sms);
