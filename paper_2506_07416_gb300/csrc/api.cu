@@ -1599,7 +1599,7 @@ litevlm_status_t litevlm_select_verify(litevlm_select_t h, int32_t batch, int32_
     a.err = h->err_d;
     const OnDevice on(h->device);
     cudaError_t e = on.e;
-    if (e == cudaSuccess) e = lvs::launch_verify(a, prob_bf16 == 1, (cudaStream_t)stream);
+    if (e == cudaSuccess) e = lvs::launch_verify(a, prob_bf16 == 1, h->num_sms, (cudaStream_t)stream);
     if (e != cudaSuccess) return cuda_fail(h, e, "verify launch");
     h->last_launches = 1;
     return LITEVLM_OK;

@@ -1010,8 +1010,8 @@ cudaError_t launch_all(const AttendArgs& a, const AttendPlan& plan, int max_rows
                     : plan.row_tile == 16 ? attend_split_kernel<D, 2, FP8>
                                           : attend_split_kernel<D, 4, FP8>;
         cfg.dynamicSmemBytes = kRingBytes<D>;
-        e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes<D>);
-        if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, kern, a);
+        static_assert(kRingBytes<D> + 10 * 1024 <= 48 * 1024, "no more shared memory than a launch has without asking");
+        e = cudaLaunchKernelEx(&cfg, kern, a);
         if (e != cudaSuccess) return e;
         ++*launches;
         cfg.dynamicSmemBytes = 0;

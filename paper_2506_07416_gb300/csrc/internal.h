@@ -212,7 +212,7 @@ struct VerifyArgs {
     int32_t* out;             // [sum T + batch]
     int32_t* err;
 };
-cudaError_t launch_verify(const VerifyArgs& a, bool bf16, cudaStream_t stream);
+cudaError_t launch_verify(const VerifyArgs& a, bool bf16, int num_sms, cudaStream_t stream);
 
 // splice.cu
 struct SpliceArgs {

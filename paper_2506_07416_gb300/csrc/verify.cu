@@ -8,15 +8,16 @@
 // w_i > 0 and w_0 + .. + w_i > u * (w_0 + .. + w_V-1); where no sum passes (u >= 1),
 // the last index with w_i > 0; -1 where there is none. NaN counts as 0.
 //
-// A cluster works on a request: each CTA adds up its part of the row, the CTAs
-// exchange their sums, and the warp whose part holds the index reads its few
-// hundred entries again. Only the one row of p and of q that is sampled is read.
-//   Sums: fp64 is scarce here (2 additions a clock and SM: the largest batch
-// would spend longer adding than reading), and fp32 sums would put the index one
-// entry off in one draw of some dozens (V entries, each with its border). So
-// p - q and the threads' sums are kept as unevaluated pairs of floats, about 48
-// bits, by error-free transformations (Dekker's difference for p >= q >= 0,
-// Knuth's two-sum); warps, CTAs and the search add in fp64.
+// A cluster works on a request: each CTA adds up its part of the row, a sixteenth of it a
+// warp, and the CTAs exchange their sums; the CTA whose part holds the index splits the
+// warp's part that holds it over its sixteen warps again, and one warp searches the
+// hundred entries that are left. Only the one row of p and of q that is sampled is read.
+//   Sums: fp64 is scarce here (2 additions a clock and SM: the largest batch would spend
+// longer adding than reading), and fp32 sums would put the index one entry off in one draw
+// of some dozens (V entries, each with its border). So p - q and the sums of threads and
+// warps are unevaluated pairs of floats, about 48 bits, by error-free transformations
+// (Dekker's difference for p >= q >= 0, Knuth's two-sum); one warp adds the warps' and
+// CTAs' sums in fp64. With every thread adding those, fp64 took 60 of 93 us.
 
 #include "cache.cuh"
 
@@ -35,163 +36,199 @@ __device__ __forceinline__ float prob(const __nv_bfloat16* p, int64_t i) { retur
 __device__ __forceinline__ float2 residual(float p, float q)
 {
     const float w = p - q;
-    if (!(w > 0.f)) return make_float2(0.f, 0.f);
-    return make_float2(w, w <= 3.4028234e38f ? (p - w) - q : 0.f);
+    return make_float2(w > 0.f ? w : 0.f, w > 0.f && w <= 3.4028234e38f ? (p - w) - q : 0.f);
 }
 
-__device__ __forceinline__ double warp_sum(double v)
+// (hi, lo) += (w, e)
+__device__ __forceinline__ void add_pair(float& hi, float& lo, float w, float e)
 {
+    const float s = hi + w, t = s - hi;
+    const float err = (hi - (s - t)) + (w - t) + e;
+    hi = s;
+    lo += s <= 3.4028234e38f ? err : 0.f;  // (an infinite sum has no error)
+}
+
+// What drafts of the row leave of its entry i: MODE 0: p - q, 1: p with the entry x struck out, 2: p
+template <int MODE>
+__device__ __forceinline__ float2 entry(float p, float q, int32_t x, int i)
+{
+    if constexpr (MODE == 0) return residual(p, q);
+    return make_float2(p > 0.f && !(MODE == 1 && i == x) ? p : 0.f, 0.f);
+}
+
+struct VerifyShared {
+    float2 sum[kVerifyWarps];   // the warps' sums
+    int last[kVerifyWarps];     // their last indices with w > 0, or -1
+    double cta_sum;             // read by the cluster
+    int cta_last;
+    int row_last;               // the last index of the whole row
+    int part;                   // the warp whose part holds the index; -1: settled, or another CTA's
+    double before, bar;         // sum before that part, and what the running sum has to pass
+};
+
+// The sixteen parts of [i0, i1): a whole number of 32 entries each.
+__device__ __forceinline__ void part_of(int i0, int i1, int w, int& a, int& b)
+{
+    const int per = ((i1 - i0 + kVerifyWarps - 1) / kVerifyWarps + 31) & ~31;
+    const long long at = (long long)i0 + (long long)w * per;
+    a = (int)(at < i1 ? at : i1);
+    b = i1 - a < per ? i1 : a + per;
+}
+
+// Sums and last positive indices of the warps' parts of [i0, i1), into shared memory.
+template <int MODE, typename T>
+__device__ void part_sums(const T* p, const T* q, int32_t x, int i0, int i1, VerifyShared& sh)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int a, b;
+    part_of(i0, i1, warp, a, b);
+    float hi = 0.f, lo = 0.f;
+    int last = -1;
+    constexpr int U = 8;  // entries of a lane on their way, and as many being added
+    float pn[U], qn[U];
+    auto load = [&](int i) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        for (int k = 0; k < U; ++k) {
+            pn[k] = i + 32 * k < b ? prob(p, i + 32 * k) : 0.f;
+            qn[k] = MODE == 0 && i + 32 * k < b ? prob(q, i + 32 * k) : 0.f;
+        }
+    };
+    load(a + lane);
+#pragma unroll 1
+    for (int i = a + lane; i < b; i += 32 * U) {
+        float pc[U], qc[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) pc[k] = pn[k], qc[k] = qn[k];
+        load(i + 32 * U);
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const float2 w = entry<MODE>(pc[k], qc[k], x, i + 32 * k);
+            add_pair(hi, lo, w.x, w.y);
+            if (w.x > 0.f) last = i + 32 * k;
+        }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const float h2 = __shfl_xor_sync(0xffffffffu, hi, o), l2 = __shfl_xor_sync(0xffffffffu, lo, o);
+        add_pair(hi, lo, h2, l2);
+    }
+    last = __reduce_max_sync(0xffffffffu, last);
+    if (lane == 0) {
+        sh.sum[warp] = make_float2(hi, lo);
+        sh.last[warp] = last;
+    }
+}
+
+// Inclusive sums over the lanes.
+__device__ __forceinline__ double scan(double v, int lanes)
+{
+    const int lane = threadIdx.x & 31;
+    for (int o = 1; o < lanes; o <<= 1) {
+        const double y = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += y;
+    }
     return v;
 }
 
-struct VerifyPart {
-    double sum;
-    int32_t last;  // last index with w > 0, or -1
-    int32_t pad;
-};
-
-// What drafts of the row leave: MODE 0: p - q, 1: p with the entry x struck out, 2: p
-template <int MODE, typename T>
-__device__ __forceinline__ float2 entry(const T* p, const T* q, int32_t x, int i)
-{
-    if constexpr (MODE == 0) return residual(prob(p, i), prob(q, i));
-    const float v = prob(p, i);
-    return make_float2(v > 0.f && !(MODE == 1 && i == x) ? v : 0.f, 0.f);
-}
-
-// Sum and last positive index of the entries [i0, i1) of a warp's part
-template <int MODE, typename T>
-__device__ VerifyPart part_sum(const T* p, const T* q, int32_t x, int i0, int i1)
+// By warp 0: the part of the warps' sums whose running sum from `before` on passes sh.bar (the
+// last with an entry above 0 where rounding lets none pass).
+__device__ __forceinline__ void pick_part(double before, VerifyShared& sh)
 {
     const int lane = threadIdx.x & 31;
-    float hi = 0.f, lo = 0.f;
-    int last = -1;
-    constexpr int U = 8;
-    for (int i = i0 + lane; i < i1; i += 32 * U) {
-        float2 w[U];
-#pragma unroll
-        for (int k = 0; k < U; ++k)
-            w[k] = i + 32 * k < i1 ? entry<MODE>(p, q, x, i + 32 * k) : make_float2(0.f, 0.f);
-#pragma unroll
-        for (int k = 0; k < U; ++k) {
-            const float s = hi + w[k].x, t = s - hi;
-            const float e = (hi - (s - t)) + (w[k].x - t);
-            hi = s;
-            if (s <= 3.4028234e38f) lo += e + w[k].y;
-            if (w[k].x > 0.f) last = i + 32 * k;
-        }
+    const float2 s = lane < kVerifyWarps ? sh.sum[lane] : make_float2(0.f, 0.f);
+    const double v = (double)s.x + (double)s.y, c = before + scan(v, kVerifyWarps);
+    const uint32_t some = __ballot_sync(0xffffffffu, v > 0.0), hit = __ballot_sync(0xffffffffu, v > 0.0 && c > sh.bar);
+    const int w = hit ? __ffs(hit) - 1 : 31 - __clz(some | 1u);
+    if (lane == w) {
+        sh.part = w;
+        sh.before = c - v;
     }
-    VerifyPart r;
-    r.sum = warp_sum((double)hi + (double)lo);
-    r.last = __reduce_max_sync(0xffffffffu, last);
-    r.pad = 0;
-    return r;
 }
 
-// The lowest index of [i0, i1) with w > 0 whose running sum (from `before` on)
-// passes `bar`; the last one with w > 0 where rounding lets none pass.
+// Samples the token of one row; returns whether any entry was above 0. Called by the whole
+// cluster.
 template <int MODE, typename T>
-__device__ int find(const T* p, const T* q, int32_t x, int i0, int i1, double before, double bar)
+__device__ bool sample(const T* p, const T* q, int32_t x, int vocab, float u, VerifyShared& sh, int32_t* out)
 {
-    const int lane = threadIdx.x & 31;
-    int last = -1;
-    for (int base = i0; base < i1; base += 32) {
-        const int i = base + lane;
-        const float2 w = i < i1 ? entry<MODE>(p, q, x, i) : make_float2(0.f, 0.f);
-        double c = (double)w.x + (double)w.y;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const double y = __shfl_up_sync(0xffffffffu, c, o);
-            if (lane >= o) c += y;
-        }
-        c += before;
-        const uint32_t pos = __ballot_sync(0xffffffffu, w.x > 0.f);
-        const uint32_t hit = __ballot_sync(0xffffffffu, w.x > 0.f && c > bar);
-        if (hit) return base + __ffs(hit) - 1;
-        if (pos) last = base + 31 - __clz(pos);
-        before = __shfl_sync(0xffffffffu, c, 31);
-    }
-    return last;
-}
-
-// Samples the token of one row; returns whether any entry was above 0. Called by
-// the whole cluster; `slot`: this CTA's part in shared memory.
-template <int MODE, typename T>
-__device__ bool sample(const T* p, const T* q, int32_t x, int vocab, float u, VerifyPart* parts, VerifyPart* slot,
-                       int32_t* out)
-{
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int rank = (int)cluster_ctarank(), ctas = (int)cluster_nctarank();
-    // parts of a whole number of 32 entries for the cluster's warps
-    const int nw = ctas * kVerifyWarps;
-    const int per = ((vocab + nw - 1) / nw + 31) & ~31;
-    const int64_t at = (int64_t)(rank * kVerifyWarps + warp) * per;
-    const int i0 = (int)(at < vocab ? at : vocab), i1 = (int)(at + per < vocab ? at + per : vocab);
-    const VerifyPart mine = part_sum<MODE>(p, q, x, i0, i1);
-    if (lane == 0) parts[warp] = mine;
+    const int per = ((vocab + ctas - 1) / ctas + 31) & ~31;
+    const long long at = (long long)rank * per;
+    const int i0 = (int)(at < vocab ? at : vocab), i1 = vocab - i0 < per ? vocab : i0 + per;
+    part_sums<MODE>(p, q, x, i0, i1, sh);
     __syncthreads();
-    if (tid == 0) {
-        VerifyPart c{0.0, -1, 0};
-        for (int w = 0; w < kVerifyWarps; ++w) {
-            c.sum += parts[w].sum;
-            c.last = max(c.last, parts[w].last);
+    if (warp == 0) {
+        const float2 s = lane < kVerifyWarps ? sh.sum[lane] : make_float2(0.f, 0.f);
+        const double sum = scan((double)s.x + (double)s.y, kVerifyWarps);
+        const int last = __reduce_max_sync(0xffffffffu, lane < kVerifyWarps ? sh.last[lane] : -1);
+        if (lane == kVerifyWarps - 1) {
+            sh.cta_sum = sum;
+            sh.cta_last = last;
+            sh.part = -1;
         }
-        *slot = c;
     }
     cluster_sync_all();
-    double total = 0.0, before = 0.0;
-    int last = -1;
-    {
-        double sums[kVerifyMaxCluster];
-        const uint32_t addr = smem_u32(slot);
-        for (int r = 0; r < ctas; ++r) {
-            const uint32_t a = mapa_shared(addr, (uint32_t)r);
-            int l;
-            asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(sums[r]) : "r"(a) : "memory");
-            asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(l) : "r"(a + 8) : "memory");
-            last = max(last, l);
-            total += sums[r];
+    if (warp == 0) {
+        double v = 0.0;
+        int last = -1;
+        if (lane < ctas) {
+            const uint32_t r = (uint32_t)lane;
+            asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(mapa_shared(smem_u32(&sh.cta_sum), r)) : "memory");
+            asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(last) : "r"(mapa_shared(smem_u32(&sh.cta_last), r)) : "memory");
         }
-        const double bar = (double)u * total;
-        // the first CTA, then the first of its warps, whose running sum passes the bar
-        double c = 0.0;
-        int cta = -1;
-        for (int r = 0; r < ctas && cta < 0; ++r) {
-            before = c;
-            c += sums[r];
-            if (sums[r] > 0.0 && c > bar) cta = r;
+        const double c = scan(v, kVerifyMaxCluster);
+        const double bar = (double)u * __shfl_sync(0xffffffffu, c, ctas - 1);
+        const uint32_t hit = __ballot_sync(0xffffffffu, lane < ctas && v > 0.0 && c > bar);
+        last = __reduce_max_sync(0xffffffffu, last);
+        const double before = __shfl_sync(0xffffffffu, c - v, rank);
+        if (lane == 0) {
+            sh.row_last = last;
+            sh.bar = bar;
         }
-        if (last >= 0) {
-            if (cta < 0) {
-                if (rank == 0 && tid == 0) *out = last;
-            } else if (cta == rank) {
-                int w = -1;
-                double cw = before, start = before;
-                for (int k = 0; k < kVerifyWarps; ++k) {
-                    start = w < 0 ? cw : start;
-                    cw += parts[k].sum;
-                    if (w < 0 && parts[k].sum > 0.0 && cw > bar) w = k;
+        __syncwarp();
+        if (hit && __ffs(hit) - 1 == rank) pick_part(before, sh);
+        else if (!hit && last >= 0 && rank == 0 && lane == 0) *out = last;
+    }
+    __syncthreads();
+    const int part = sh.part;
+    const double first = sh.before, bar = sh.bar;
+    if (part >= 0) {
+        int a, b;
+        part_of(i0, i1, part, a, b);
+        __syncthreads();  // (everyone has read what the second round overwrites)
+        part_sums<MODE>(p, q, x, a, b, sh);
+        __syncthreads();
+        if (warp == 0) pick_part(first, sh);
+        __syncthreads();
+        if (warp == sh.part) {
+            int s0, s1;
+            part_of(a, b, warp, s0, s1);
+            double before = sh.before;
+            int found = -1;
+            for (int base = s0; base < s1; base += 32) {
+                const int i = base + lane;
+                const float2 w = i < s1 ? entry<MODE>(prob(p, i), MODE == 0 ? prob(q, i) : 0.f, x, i) : make_float2(0.f, 0.f);
+                const double c = before + scan((double)w.x + (double)w.y, 32);
+                const uint32_t pos = __ballot_sync(0xffffffffu, w.x > 0.f);
+                const uint32_t hit = __ballot_sync(0xffffffffu, w.x > 0.f && c > bar);
+                if (pos) found = base + 31 - __clz(pos);
+                if (hit) {
+                    found = base + __ffs(hit) - 1;
+                    break;
                 }
-                if (w < 0) {  // the two orders of addition differ by a last bit: the CTA's last entry
-                    if (tid == 0) *out = slot->last;
-                } else if (w == warp) {
-                    const int f = find<MODE>(p, q, x, i0, i1, start, bar);
-                    if (lane == 0) *out = f;
-                }
+                before = __shfl_sync(0xffffffffu, c, 31);
             }
+            if (lane == 0) *out = found;
         }
     }
-    cluster_sync_all();  // the slots are free, and every CTA stays until its part has been read
-    return last >= 0;
+    cluster_sync_all();  // every CTA stays until its sums have been read
+    return sh.row_last >= 0;
 }
 
 template <typename T>
 __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(const __grid_constant__ VerifyArgs a)
 {
-    __shared__ VerifyPart parts[kVerifyWarps];
-    __shared__ VerifyPart slot;
+    __shared__ VerifyShared sh;
     __shared__ int s_first;
     const int tid = threadIdx.x;
     const int b = blockIdx.y;
@@ -230,19 +267,20 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(const __grid_con
     bool any = false;
     // (every CTA of the cluster takes the same branches; the token is written behind the
     // first cluster barrier, so after the lead CTA's -1)
-    if (acc < n && Q) any = sample<0>(p, q, 0, a.vocab, u, parts, &slot, out + acc);
-    else if (acc < n) any = sample<1>(p, q, a.tokens[t0 + acc], a.vocab, u, parts, &slot, out + acc);
-    if (!any) sample<2>(p, q, 0, a.vocab, u, parts, &slot, out + acc);
+    if (acc < n && Q) any = sample<0>(p, q, 0, a.vocab, u, sh, out + acc);
+    else if (acc < n) any = sample<1>(p, q, a.tokens[t0 + acc], a.vocab, u, sh, out + acc);
+    if (!any) sample<2>(p, q, 0, a.vocab, u, sh, out + acc);
 }
 
 }  // namespace
 
-cudaError_t launch_verify(const VerifyArgs& a, bool bf16, cudaStream_t stream)
+cudaError_t launch_verify(const VerifyArgs& a, bool bf16, int num_sms, cudaStream_t stream)
 {
     if (a.batch <= 0) return cudaSuccess;
-    // a CTA for every 2048 entries, up to a cluster of eight
+    // a CTA for every 2048 entries, up to a cluster of eight, while the batch's CTAs run at once
+    // (two on an SM)
     int ctas = 1;
-    while (ctas < kVerifyMaxCluster && a.vocab > 2048 * ctas) ctas *= 2;
+    while (ctas < kVerifyMaxCluster && a.vocab > 2048 * ctas && 2 * ctas * a.batch <= 2 * num_sms) ctas *= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)ctas, (unsigned)a.batch, 1);
     cfg.blockDim = dim3(kVerifyThreads, 1, 1);

@@ -411,15 +411,15 @@ def _refuse(message: str):
 
 
 def _want(name: str, t, dtype, shape, device: int):
-    """A contiguous CUDA tensor of this type, shape (None: any size) and device, or an error."""
+    """A contiguous CUDA tensor of this type, shape (-1: any size) and device, or an error."""
+    if _FC.fits(t, dtype, device, *shape):
+        return t
     import torch
     if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device.type != "cuda" or t.device.index != device:
         _refuse(f"{name} must be a {dtype} tensor on cuda:{device}")
-    if t.dim() != len(shape) or any(w is not None and n != w for n, w in zip(t.shape, shape)):
-        _refuse(f"{name} must have the shape {tuple('any' if w is None else w for w in shape)}, not {tuple(t.shape)}")
-    if not t.is_contiguous():
-        _refuse(f"{name} must be contiguous")
-    return t
+    if t.dim() != len(shape) or any(w >= 0 and n != w for n, w in zip(t.shape, shape)):
+        _refuse(f"{name} must have the shape {tuple('any' if w < 0 else w for w in shape)}, not {tuple(t.shape)}")
+    _refuse(f"{name} must be contiguous")
 
 
 def _row_stride(name: str, t, dtype, heads: int, d: int, device: int) -> int:
@@ -499,6 +499,7 @@ class Selector:
                              qk_dtype, score_kernel, query, query_split)
         self.qk_dtype = qk_dtype
         self.heads, self.kv_heads, self.head_dim = num_q_heads, num_kv_heads, head_dim
+        self._space = {}  # workspaces of cache_attend by stream
 
     def close(self) -> None:
         if self.handle:
@@ -677,9 +678,21 @@ class Selector:
         if cache.heads != self.kv_heads or cache.head_dim != self.head_dim:
             _refuse(f"the cache has {cache.heads} heads of {cache.head_dim}, the handle {self.kv_heads} of "
                     f"{self.head_dim}")
-        _want("table", table, torch.int32, (batch, None), cache.device)
+        _want("table", table, torch.int32, (batch, -1), cache.device)
         _want("seq_lens", seq_lens, torch.int32, (batch,), cache.device)
         return cache.device
+
+    def _workspace(self, need: int, stream, device):
+        """The handle's own workspace for calls on one stream; a call that is captured, or that has a stream of its
+        own, gets one that nothing else uses."""
+        import torch
+        if stream is not None or torch._C._cuda_isCurrentStreamCapturing():
+            return torch.empty(need, dtype=torch.uint8, device=device)
+        now = torch._C._cuda_getCurrentRawStream(device.index)
+        kept = self._space.get(now)
+        if kept is None or kept.shape[0] < need:
+            kept = self._space[now] = torch.empty(need, dtype=torch.uint8, device=device)
+        return kept
 
     def _element(self):
         import torch
@@ -752,9 +765,9 @@ class Selector:
             else:
                 _want("out", out, torch.bfloat16, (total, self.heads, self.head_dim), dev)
             if workspace is None:
-                workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+                workspace = self._workspace(need, stream, q.device)
             else:
-                _want("workspace", workspace, torch.uint8, (None,), dev)
+                _want("workspace", workspace, torch.uint8, (-1,), dev)
         cache_attend(self.handle, batch, cache.struct, table, table.shape[1], seq_lens, q, stride, offsets, off_h,
                      max_len, q_scale, w_in, w_out, out, workspace, workspace.shape[0], _stream_on(stream, dev))
         return out
@@ -770,7 +783,7 @@ class Selector:
         if cache.weights is None:
             _refuse("the cache has no weights")
         if to_table is not None:
-            _want("to_table", to_table, torch.int32, (batch, None), dev)
+            _want("to_table", to_table, torch.int32, (batch, -1), dev)
         with _allocate_on(stream, dev):
             if new_lens is None:
                 new_lens = torch.empty_like(seq_lens)
@@ -779,7 +792,7 @@ class Selector:
             if kept_idx is None:
                 kept_idx = torch.empty((batch, max(budget, 0)), dtype=torch.int32, device=seq_lens.device)
             else:
-                _want("kept_idx", kept_idx, torch.int32, (batch, budget), dev)
+                _want("kept_idx", kept_idx, torch.int32, (batch, max(budget, 0)), dev)
         cache_evict(self.handle, batch, cache.struct, table, table.shape[1], seq_lens, max_len, budget, sink, recent,
                     to_table, 0 if to_table is None else to_table.shape[1], cache.weights, kept_idx, new_lens,
                     _stream_on(stream, dev))
@@ -797,7 +810,7 @@ class Selector:
                 target_probs.dim() != 2 or target_probs.dtype not in (torch.float32, torch.bfloat16):
             _refuse("target_probs must be a float32 or bf16 CUDA tensor [sum T + batch, vocab]")
         dev, kind, vocab = target_probs.device.index, target_probs.dtype, target_probs.shape[1]
-        _want("target_probs", target_probs, kind, (total + batch, None), dev)
+        _want("target_probs", target_probs, kind, (total + batch, -1), dev)
         _want("draft_tokens", draft_tokens, torch.int32, (total,), dev)
         _want("u_accept", u_accept, torch.float32, (total,), dev)
         _want("u_sample", u_sample, torch.float32, (batch,), dev)
