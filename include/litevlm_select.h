@@ -688,7 +688,7 @@ litevlm_status_t litevlm_select_cache_evict(litevlm_select_t handle, int32_t bat
  * from p. Sampling takes the lowest token i with weight w_i > 0 whose running sum
  * passes u_sample times the sum of all; the last with w_i > 0 where none does;
  * -1 where no weight is above 0. NaN counts as 0.
- *   vocab            entries of a probability row, >= 1
+ *   vocab            entries of a probability row, in [1, 2^30]
  *   prob_bf16        0: float rows; 1: bf16 rows
  *   draft_tokens     device int32 [sum T_b]
  *   draft_offsets_d/h  int32 [batch+1] prefix of T_b (0 allowed)

@@ -1575,7 +1575,7 @@ litevlm_status_t litevlm_select_verify(litevlm_select_t h, int32_t batch, int32_
     if (!h) return LITEVLM_ERR_INVALID_ARG;
     litevlm_status_t s = start_call(h, batch);
     if (s != LITEVLM_OK) return s;
-    if (vocab < 1) return fail(h, LITEVLM_ERR_INVALID_ARG, "vocab must be >= 1");
+    if (vocab < 1 || vocab > (1 << 30)) return fail(h, LITEVLM_ERR_INVALID_ARG, "vocab must be in [1, 2^30]");
     if (prob_bf16 != 0 && prob_bf16 != 1) return fail(h, LITEVLM_ERR_INVALID_ARG, "prob_bf16 must be 0 or 1");
     int64_t total = 0;
     s = check_offsets(h, draft_offsets_h, batch, INT32_MAX - 65536, "draft_offsets", &total);

@@ -9,11 +9,13 @@
 // 32-bit keys in shared memory (protected tokens above all others); a radix select
 // of 4 passes of 8 bits adds up the CTAs' histograms through distributed shared
 // memory, one cluster barrier a pass; two counts in index order give every kept
-// token its place. evict_move_kernel: a CTA moves rows of one head, 16 bytes a
+// token its place. evict_move_kernel: a CTA moves rows of some heads, 16 bytes a
 // thread. In place a CTA moves all of a head's rows, a batch of rows at a time:
 // every load of a batch ends before its first store, and since the kept rows
 // ascend (row i comes from a position >= i), no store touches a row of a later
 // batch.
+
+#include <type_traits>
 
 #include "cache.cuh"
 
@@ -193,32 +195,36 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const __grid_
     cluster_sync_all();  // every CTA stays until its counts have been read
 }
 
-constexpr int kMoveThreads = 256;
-constexpr int kMoveRows = 4;  // rows of a thread in flight
+constexpr int kMoveThreads = 128;
+constexpr int kMoveRows = 2;  // rows of a thread in flight
 
+// Rows [first, first + rows_per_cta) of the heads [h0, h0 + heads_per_cta). Where a row comes
+// from and goes to is the same for every head, so a CTA finds that once and then moves head
+// after head.
 template <int D, bool INPLACE>
-__global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_constant__ EvictArgs a, int rows_per_cta)
+__global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_constant__ EvictArgs a, int rows_per_cta,
+                                                                  int heads_per_cta)
 {
     constexpr int VECS = D / 32;      // 16-byte vectors of a row's codes
     constexpr int LANES = 2 * VECS;   // threads of a row: the vectors of K, then those of V
     constexpr int BATCH = kMoveThreads / LANES * kMoveRows;
+    using Scales = typename std::conditional<D == 128, uint2, uint32_t>::type;  // of a row of one head
     const int e = threadIdx.x % LANES, t = e / VECS, vec = e % VECS;
-    const int h = blockIdx.y, b = blockIdx.z;
+    const int b = blockIdx.z, h0 = blockIdx.y * heads_per_cta, h1 = min(a.cache.hkv, h0 + heads_per_cta);
     const int shift = a.cache.page_shift, smask = (1 << shift) - 1;
     griddep_wait();
     griddep_launch_dependents();
     const int k = a.new_lens[b];
     const int32_t* kept = a.kept + (int64_t)b * a.budget;
     const int first = blockIdx.x * rows_per_cta, end = min(k, first + rows_per_cta);
+    uint8_t* const codes = a.cache.codes[t] + vec * 16;
+    uint8_t* const scales = a.cache.scales[t];
     for (int base = first; base < end; base += BATCH) {
-        uint4 code[kMoveRows];
-        uint2 scale[kMoveRows];
-        float weight[kMoveRows];
-        int64_t to[kMoveRows], to_w[kMoveRows];
+        int64_t from[kMoveRows], to[kMoveRows];  // rows of head 0; -1: nothing to move
 #pragma unroll
         for (int u = 0; u < kMoveRows; ++u) {
             const int i = base + u * (BATCH / kMoveRows) + threadIdx.x / LANES;
-            to[u] = -1;
+            from[u] = to[u] = -1;
             if (i >= end) continue;
             const int j = __ldcg(kept + i);
             if (INPLACE && j == i) continue;
@@ -229,30 +235,40 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_c
                 if (e == 0) atomicOr(a.err, kErrBounds);
                 continue;
             }
-            const int64_t from = cache_row(from_page, a.cache.hkv, h, shift, j & smask);
-            to[u] = cache_row(to_page, a.cache.hkv, h, shift, i & smask);
-            code[u] = *reinterpret_cast<const uint4*>(a.cache.codes[t] + from * (D / 2) + vec * 16);
-            if (vec == 0) {
-                const uint8_t* s = a.cache.scales[t] + from * (D / 16);
-                if constexpr (D == 128) scale[u] = *reinterpret_cast<const uint2*>(s);
-                else scale[u].x = *reinterpret_cast<const uint32_t*>(s);
-            }
-            if (h == 0 && e == 1) {
-                weight[u] = a.weights[((int64_t)from_page << shift) + (j & smask)];
-                to_w[u] = ((int64_t)to_page << shift) + (i & smask);
-            }
+            from[u] = cache_row(from_page, a.cache.hkv, 0, shift, j & smask);
+            to[u] = cache_row(to_page, a.cache.hkv, 0, shift, i & smask);
         }
-        if constexpr (INPLACE) __syncthreads();
+        if (h0 == 0) {
+            float w[kMoveRows];
+            // (slots of the weights: a page has one row of them where it has hkv rows of each head)
+            auto slot = [&](int64_t row) { return ((row >> shift) / a.cache.hkv << shift) + (row & smask); };
+            if (e == 0)
 #pragma unroll
-        for (int u = 0; u < kMoveRows; ++u) {
-            if (to[u] < 0) continue;
-            *reinterpret_cast<uint4*>(a.cache.codes[t] + to[u] * (D / 2) + vec * 16) = code[u];
-            if (vec == 0) {
-                uint8_t* s = a.cache.scales[t] + to[u] * (D / 16);
-                if constexpr (D == 128) *reinterpret_cast<uint2*>(s) = scale[u];
-                else *reinterpret_cast<uint32_t*>(s) = scale[u].x;
+                for (int u = 0; u < kMoveRows; ++u) w[u] = to[u] >= 0 ? a.weights[slot(from[u])] : 0.f;
+            if constexpr (INPLACE) __syncthreads();
+            if (e == 0)
+#pragma unroll
+                for (int u = 0; u < kMoveRows; ++u)
+                    if (to[u] >= 0) a.weights[slot(to[u])] = w[u];
+        }
+#pragma unroll 1
+        for (int h = h0; h < h1; ++h) {
+            uint4 code[kMoveRows];
+            Scales scale[kMoveRows];
+            const int64_t head = (int64_t)h << shift;
+#pragma unroll
+            for (int u = 0; u < kMoveRows; ++u) {
+                if (to[u] < 0) continue;
+                code[u] = __ldcg(reinterpret_cast<const uint4*>(codes + (from[u] + head) * (D / 2)));
+                if (vec == 0) scale[u] = *reinterpret_cast<const Scales*>(scales + (from[u] + head) * (D / 16));
             }
-            if (h == 0 && e == 1) a.weights[to_w[u]] = weight[u];
+            if constexpr (INPLACE) __syncthreads();
+#pragma unroll
+            for (int u = 0; u < kMoveRows; ++u) {
+                if (to[u] < 0) continue;
+                *reinterpret_cast<uint4*>(codes + (to[u] + head) * (D / 2)) = code[u];
+                if (vec == 0) *reinterpret_cast<Scales*>(scales + (to[u] + head) * (D / 16)) = scale[u];
+            }
         }
     }
 }
@@ -293,15 +309,20 @@ cudaError_t launch_cache_evict(const EvictArgs& a, int head_dim, int num_sms, cu
     const int batch_rows = kMoveThreads / (head_dim / 16) * kMoveRows;
     const int rows = inplace ? most : batch_rows;
     if (most <= 0) return cudaSuccess;
+    const int64_t chunks = (most + rows - 1) / rows * (int64_t)a.batch;
+    // heads of a CTA: eight, fewer while that leaves SMs without work
+    int heads = inplace ? 1 : 8;
+    while (heads > 1 && chunks * ((a.cache.hkv + heads - 1) / heads) < 4 * (int64_t)num_sms) heads /= 2;
     cudaLaunchConfig_t mv = {};
-    mv.gridDim = dim3((unsigned)((most + rows - 1) / rows), (unsigned)a.cache.hkv, (unsigned)a.batch);
+    mv.gridDim = dim3((unsigned)((most + rows - 1) / rows), (unsigned)((a.cache.hkv + heads - 1) / heads),
+                      (unsigned)a.batch);
     mv.blockDim = dim3(kMoveThreads, 1, 1);
     mv.stream = stream;
     mv.attrs = attr;
     mv.numAttrs = 1;
     auto kern = head_dim == 128 ? (inplace ? evict_move_kernel<128, true> : evict_move_kernel<128, false>)
                                 : (inplace ? evict_move_kernel<64, true> : evict_move_kernel<64, false>);
-    e = cudaLaunchKernelEx(&mv, kern, a, rows);
+    e = cudaLaunchKernelEx(&mv, kern, a, rows, heads);
     if (e == cudaSuccess) *launches = 2;
     return e;
 }
