@@ -590,7 +590,7 @@ typedef struct {
  *                    (litevlm_select_topk's kept_idx puts the kept rows into the cache
  *                    with no gather in between); NULL: token r of the call has row r
  *   new_offsets_d/h  int32 [batch+1] prefix of T_b, the new tokens of each request
- *   k_in_scale, v_in_scale  e4m3: the codes' per-tensor scales (> 0, finite); bf16: 1
+ *   k_in_scale, v_in_scale  e4m3: the codes' per-tensor scales, in [2^-60, 2^60]; bf16: 1
  *   weights          device float [num_pages][page_size] or NULL: set to 0 for the new tokens
  *   k_stored, v_stored  device bf16 [sum T_b][num_kv_heads][d] or NULL, 16-byte
  *                    aligned: the values that the cache now holds for the new rows

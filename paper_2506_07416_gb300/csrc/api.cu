@@ -1395,6 +1395,8 @@ litevlm_status_t litevlm_select_cache_append(litevlm_select_t h, int32_t batch, 
         s = check_rows(h, k, k_row_stride, h->cfg.num_kv_heads, k_in_scale, "k");
         if (s == LITEVLM_OK) s = check_rows(h, v, v_row_stride, h->cfg.num_kv_heads, v_in_scale, "v");
         if (s != LITEVLM_OK) return s;
+        if (!in_range(k_in_scale) || !in_range(v_in_scale))
+            return fail(h, LITEVLM_ERR_INVALID_ARG, "k_in_scale and v_in_scale must be in [2^-60, 2^60]");
         if ((k_stored && !aligned16(k_stored)) || (v_stored && !aligned16(v_stored)))
             return fail(h, LITEVLM_ERR_INVALID_ARG, "k_stored and v_stored must be 16-byte aligned");
     }
