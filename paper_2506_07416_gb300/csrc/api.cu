@@ -1510,6 +1510,7 @@ litevlm_status_t litevlm_select_cache_attend(litevlm_select_t h, int32_t batch, 
     a.weights_in = weights_in;
     a.weights_out = weights_out;
     a.err = h->err_d;
+    a.wait_budget = h->wait_budget;
     const OnDevice on(h->device);
     cudaError_t e = on.e;
     int32_t launches = 0;

@@ -25,7 +25,7 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "cache.cuh"
+#include "cache_attend.cuh"
 
 namespace lvs {
 
@@ -34,8 +34,6 @@ namespace {
 constexpr int kAttWarps = 4;
 constexpr int kAttThreads = 32 * kAttWarps;
 constexpr int kAttStages = 2;        // spans of 32 keys of a warp's ring
-constexpr float kNoRef = -3.0e38f;   // reference of a row without keys so far
-constexpr float kRefSlack = 8.f;     // a score may pass its row's reference by this
 // of a single row, whose p * scale * 2^5 is at most 2^2 * 448 * 2^5 = 57344, inside f16; the
 // factor keeps small scales' products above f16's lower end
 constexpr float kRefSlack1 = 2.f, kBoost1 = 32.f;
@@ -58,7 +56,6 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t v)
     return r;
 }
 
-__device__ __forceinline__ uint32_t pack_h2(float lo, float hi) { return h2_bits(__floats2half2_rn(lo, hi)); }
 
 // A group of 16 keys of one head in shared memory.
 template <int D>
@@ -189,66 +186,6 @@ __device__ __forceinline__ void score_group(const uint8_t* grp, int lane, QF qf,
                          q.y);
             }
     }
-}
-
-// What every CTA of a request's tile needs to know of its rows.
-struct RowTile {
-    int len, t, row0, rows, last0;  // last0: position of the first query
-    int group;
-    // query of a row (a row's head is its key head's first plus the rest)
-    __device__ __forceinline__ int query(int row) const { return t == 1 ? 0 : row / group; }
-};
-
-__device__ __forceinline__ RowTile row_tile(const AttendArgs& a, int b, int tile, int per)
-{
-    RowTile r;
-    bool bad;
-    r.len = cache_len(a.lens[b], a.limit, bad);
-    if (bad && threadIdx.x == 0) atomicOr(a.err, kErrBounds);
-    r.t = a.q_off[b + 1] - a.q_off[b];
-    r.row0 = tile * per;
-    r.rows = min(per, r.t * a.group - r.row0);
-    r.last0 = r.len - r.t;
-    r.group = a.group;
-    return r;
-}
-
-// How the keys are split, found by a warp from the lengths on the device: equal chunks, as
-// short as they may be while all requests together have at most a.slots of them (the CTAs
-// that run at once), so that neither lengths that differ nor a max_len far above them leave
-// SMs without work. Of 32 candidate lengths from the mean on, in steps of an eighth of it,
-// the first that fits is taken. Requests without queries take no part.
-__device__ __forceinline__ int keys_of(const AttendArgs& a, int b)
-{
-    bool bad;
-    const int n = cache_len(__ldg(a.lens + b), a.limit, bad);
-    return __ldg(a.q_off + b + 1) > __ldg(a.q_off + b) ? n : 0;
-}
-__device__ __forceinline__ int chunks_of(int keys, int chunk) { return (int)(((unsigned)keys + chunk - 1) / (unsigned)chunk); }
-__device__ __forceinline__ int chunk_keys(const AttendArgs& a)
-{
-    if (a.batch == 1) return max(64, (chunks_of(keys_of(a, 0), a.slots) + 63) & ~63);
-    const int lane = threadIdx.x & 31;
-    long long total = 0;
-    for (int b = lane; b < a.batch; b += 32) total += keys_of(a, b);
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
-    const long long mean = (total + a.slots - 1) / a.slots;
-    const int mine = (int)min((long long)INT32_MAX / 2, (mean + mean * lane / 8 + 63) & ~63ll);
-    const unsigned c = (unsigned)max(mine, 64);
-    long long count = 0;
-    for (int b = 0; b < a.batch; ++b) count += ((unsigned)keys_of(a, b) + c - 1) / c;
-    const uint32_t fits = __ballot_sync(0xffffffffu, count <= a.slots);
-    return fits ? (int)__shfl_sync(0xffffffffu, c, __ffs(fits) - 1) : (a.limit + 63) & ~63;
-}
-// Chunks of the requests before b.
-__device__ __forceinline__ int chunks_before(const AttendArgs& a, int b, int chunk)
-{
-    int n = 0;
-    for (int x = threadIdx.x & 31; x < b; x += 32) n += chunks_of(keys_of(a, x), chunk);
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) n += __shfl_xor_sync(0xffffffffu, n, d);
-    return n;
 }
 
 template <int D>
@@ -1002,6 +939,11 @@ cudaError_t launch_all(const AttendArgs& a, const AttendPlan& plan, int max_rows
     cudaError_t e = cudaSuccess;
     if (total_rows > 0) {
         const int tiles = (max_rows + plan.row_tile - 1) / plan.row_tile;
+        if (plan.row_tile == 128) {
+            e = launch_attend_tiles(a, D, FP8, tiles, stream);
+            if (e != cudaSuccess) return e;
+            ++*launches;
+        } else {
         cfg.gridDim = plan.slots > 0 ? dim3((unsigned)plan.slots, (unsigned)(tiles * a.cache.hkv), 1)
                                      : dim3(1, (unsigned)(tiles * a.cache.hkv), (unsigned)a.batch);
         cfg.blockDim = dim3(kAttThreads, 1, 1);
@@ -1015,6 +957,7 @@ cudaError_t launch_all(const AttendArgs& a, const AttendPlan& plan, int max_rows
         if (e != cudaSuccess) return e;
         ++*launches;
         cfg.dynamicSmemBytes = 0;
+        }
     }
     const int most = max_rows / a.group * a.hq;  // rows of the longest request
     // warps of a row by the chunks that a request has where all are alike
@@ -1046,16 +989,18 @@ cudaError_t launch_all(const AttendArgs& a, const AttendPlan& plan, int max_rows
 
 }  // namespace
 
+constexpr int kFewRows = 32;
+
 AttendPlan plan_cache_attend(int batch, int hkv, int max_rows, int64_t max_len, int num_sms)
 {
     AttendPlan p;
-    p.row_tile = max_rows <= 8 ? 8 : (max_rows <= 16 ? 16 : 32);
+    p.row_tile = max_rows <= 8 ? 8 : (max_rows <= 16 ? 16 : (max_rows <= kFewRows ? 32 : 128));
     const int64_t tiles = (max_rows + p.row_tile - 1) / p.row_tile;
     const int64_t per_key = (tiles > 0 ? tiles : 1) * hkv;  // CTAs for every chunk
     const int64_t items = per_key * (batch > 0 ? batch : 1);
-    // Four CTAs run on an SM. Where the batch has fewer than two for every one of these places,
+    // Four CTAs run on an SM (two of the kernel for many rows). Where the batch has fewer than two for every one of these places,
     // the keys are split over that many CTAs; else a CTA takes all keys of its rows.
-    const int64_t places = (int64_t)num_sms * 4;
+    const int64_t places = (int64_t)num_sms * (p.row_tile == 128 ? 2 : 4);
     p.slots = 0;
     if (max_len > 64 && items < 2 * places) {
         const int64_t units = (max_len + 63) / 64 * (batch > 0 ? batch : 1);

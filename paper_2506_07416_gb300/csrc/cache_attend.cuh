@@ -1,0 +1,77 @@
+// What the attention kernels of the 4-bit cache share: the split of the keys, the rows of
+// a CTA, and the units of their sums.
+#pragma once
+
+#include "cache.cuh"
+
+namespace lvs {
+
+constexpr float kNoRef = -3.0e38f;   // reference of a row without keys so far
+constexpr float kRefSlack = 8.f;     // a score may pass its row's reference by this (2^8 is well inside f16)
+
+__device__ __forceinline__ uint32_t pack_h2(float lo, float hi) { return h2_bits(__floats2half2_rn(lo, hi)); }
+
+// How the keys are split, found by a warp from the lengths on the device: equal chunks, as
+// short as they may be while all requests together have at most a.slots of them (the CTAs
+// that run at once), so that neither lengths that differ nor a max_len far above them leave
+// SMs without work. Of 32 candidate lengths from the mean on, in steps of an eighth of it,
+// the first that fits is taken. Requests without queries take no part.
+__device__ __forceinline__ int keys_of(const AttendArgs& a, int b)
+{
+    bool bad;
+    const int n = cache_len(__ldg(a.lens + b), a.limit, bad);
+    return __ldg(a.q_off + b + 1) > __ldg(a.q_off + b) ? n : 0;
+}
+__device__ __forceinline__ int chunks_of(int keys, int chunk) { return (int)(((unsigned)keys + chunk - 1) / (unsigned)chunk); }
+__device__ __forceinline__ int chunk_keys(const AttendArgs& a)
+{
+    if (a.batch == 1) return max(64, (chunks_of(keys_of(a, 0), a.slots) + 63) & ~63);
+    const int lane = threadIdx.x & 31;
+    long long total = 0;
+    for (int b = lane; b < a.batch; b += 32) total += keys_of(a, b);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
+    const long long mean = (total + a.slots - 1) / a.slots;
+    const int mine = (int)min((long long)INT32_MAX / 2, (mean + mean * lane / 8 + 63) & ~63ll);
+    const unsigned c = (unsigned)max(mine, 64);
+    long long count = 0;
+    for (int b = 0; b < a.batch; ++b) count += ((unsigned)keys_of(a, b) + c - 1) / c;
+    const uint32_t fits = __ballot_sync(0xffffffffu, count <= a.slots);
+    return fits ? (int)__shfl_sync(0xffffffffu, c, __ffs(fits) - 1) : (a.limit + 63) & ~63;
+}
+// Chunks of the requests before b.
+__device__ __forceinline__ int chunks_before(const AttendArgs& a, int b, int chunk)
+{
+    int n = 0;
+    for (int x = threadIdx.x & 31; x < b; x += 32) n += chunks_of(keys_of(a, x), chunk);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) n += __shfl_xor_sync(0xffffffffu, n, d);
+    return n;
+}
+
+// What every CTA of a request's tile needs to know of its rows.
+struct RowTile {
+    int len, t, row0, rows, last0;  // last0: position of the first query
+    int group;
+    // query of a row (a row's head is its key head's first plus the rest)
+    __device__ __forceinline__ int query(int row) const { return t == 1 ? 0 : row / group; }
+};
+
+__device__ __forceinline__ RowTile row_tile(const AttendArgs& a, int b, int tile, int per)
+{
+    RowTile r;
+    bool bad;
+    r.len = cache_len(a.lens[b], a.limit, bad);
+    if (bad && threadIdx.x == 0) atomicOr(a.err, kErrBounds);
+    r.t = a.q_off[b + 1] - a.q_off[b];
+    r.row0 = tile * per;
+    r.rows = min(per, r.t * a.group - r.row0);
+    r.last0 = r.len - r.t;
+    r.group = a.group;
+    return r;
+}
+
+// The launch of cache_tile.cu: rows of 128 of a request's, `tiles` of them for the longest.
+cudaError_t launch_attend_tiles(const AttendArgs& a, int head_dim, bool fp8, int tiles, cudaStream_t stream);
+
+}  // namespace lvs

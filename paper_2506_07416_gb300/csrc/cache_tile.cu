@@ -1,0 +1,561 @@
+// Attention over the 4-bit cache for calls of many rows (drafts of grouped heads, chunks of
+// a prompt), on the fifth-generation tensor cores.
+//
+// A CTA takes a key head of a request, 128 rows (a row is a query with one of the head's
+// query heads) and all keys that they see, or one chunk of them, 128 keys at a time:
+//   warps 4-7 make f16 values of codes and scales (exact) and lay them out for the
+//     contractions: K rows with their channels, V transposed, so that both are K-major
+//     128-byte swizzled operands; the next tile's codes are on their way meanwhile;
+//   warp 8 issues S = Q K^T into 128 columns of tensor memory and, once the probabilities
+//     are there, O += P V with P read from tensor memory;
+//   warps 0-3 hold a row a thread: they read S twice (its largest score, then the
+//     exponentials), write P as f16 over S, and keep the row's reference and sum. A
+//     reference moves only when a score passes it by 8; O is then rescaled in place.
+// What bounds it: an SM makes 16 exponentials a clock, a tile of 128 x 128 takes 1024
+// clocks of them, against 512 of contractions, so two CTAs share an SM: while one waits
+// for a contraction the other computes. That needs 256 columns and at most 113 KB each, so
+// operands are not double-buffered and S and P share their columns.
+
+#include "cache_attend.cuh"
+#include "pipe.cuh"
+
+namespace lvs {
+
+namespace {
+
+constexpr int kTileKeys = 128, kTileThreads = 288;
+enum { B_K_FULL, B_V_FULL, B_S_FULL, B_P_FULL, B_PV_DONE, B_DRAIN, B_COUNT };
+
+template <int D>
+struct TileLayout {
+    static constexpr int ATOM = 128 * 128;                 // 128 rows of 64 f16
+    static constexpr int Q = 0;                            // [D / 64] atoms: rows x channels
+    static constexpr int K = Q + D / 64 * ATOM;            // [D / 64] atoms: keys x channels
+    static constexpr int V = K + D / 64 * ATOM;            // [2] halves of the keys: D channels x 64 keys
+    static constexpr int BAR = V + 2 * D * 128;
+    static constexpr int MISC = BAR + 8 * B_COUNT;
+    // at least 77 KB: no more than two CTAs (of 256 columns each) share an SM
+    static constexpr int NEED = MISC + 16 + 1024;
+    static constexpr int ALLOC = NEED > 77 * 1024 ? NEED : 77 * 1024;
+};
+
+// O += P V: A from tensor memory
+__device__ __forceinline__ void mma_f16_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
+                                           uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
+__device__ __forceinline__ void st_shared16(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+
+// Row `row` of the tile as f16 into shared memory, scaled as in the kernel for few rows (a
+// power of two that puts its largest magnitude at about 2^10; NaN throughout where a channel
+// is infinite or NaN). Returns what undoes the scaling.
+template <int D, bool FP8>
+__device__ __forceinline__ float stage_q(const void* q, int64_t at, bool real, uint32_t q_s, int row)
+{
+    auto put = [&](int u, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {  // 8 channels
+        st_shared16(q_s + (u >> 3) * TileLayout<D>::ATOM + row * 128 + (((u & 7) ^ (row & 7)) << 4), a, b, c, d);
+    };
+    if (!real) {
+#pragma unroll 4
+        for (int u = 0; u < D / 8; ++u) put(u, 0u, 0u, 0u, 0u);
+        return 1.f;
+    }
+    if constexpr (FP8) {
+        const uint4* s = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(q) + at);
+#pragma unroll 2
+        for (int i = 0; i < D / 16; ++i) {
+            const uint4 v = __ldg(s + i);
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            uint32_t f[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) f[k] = h2_bits(e4m3x2_value(w[k / 2] >> (16 * (k & 1))));
+            put(2 * i, f[0], f[1], f[2], f[3]);
+            put(2 * i + 1, f[4], f[5], f[6], f[7]);
+        }
+        return 1.f;
+    } else {
+        const uint4* s = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(q) + at);
+        uint32_t top = 0u;
+#pragma unroll 4
+        for (int i = 0; i < D / 8; ++i) {
+            const uint4 v = __ldg(s + i);
+            top = __vmaxu2(__vmaxu2(top, v.x & 0x7FFF7FFFu), __vmaxu2(v.y & 0x7FFF7FFFu, v.z & 0x7FFF7FFFu));
+            top = __vmaxu2(top, v.w & 0x7FFF7FFFu);
+        }
+        top = max(top & 0xFFFFu, top >> 16);
+        const int e = min(264 - (int)(top >> 7), 253);
+        const float up = __int_as_float(top >= 0x7F80u ? 0x7FC00000 : e << 23);
+#pragma unroll 4
+        for (int i = 0; i < D / 8; ++i) {
+            const uint4 v = __ldg(s + i);
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            uint32_t f[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                f[k] = pack_h2(__uint_as_float(w[k] << 16) * up, __uint_as_float(w[k] & 0xFFFF0000u) * up);
+            put(i, f[0], f[1], f[2], f[3]);
+        }
+        return __int_as_float((254 - e) << 23);
+    }
+}
+
+// A thread's part of a tile's K: 32 channels (D = 64: 16) of each of four keys, 8 apart.
+template <int D>
+struct KPart {
+    uint4 code[4];   // D = 64: the first two words
+    uint32_t scale[4];
+};
+// ... and of its V: 8 neighbouring keys, the 16 channels of one scale block.
+struct VPart {
+    uint2 code[8];
+    uint32_t scale[8];
+};
+
+template <int D, bool FP8>
+__global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __grid_constant__ AttendArgs a)
+{
+    using L = TileLayout<D>;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw);
+    const uint32_t base = (raw + 1023u) & ~1023u;
+    uint8_t* smem = smem_raw + (base - raw);
+    auto BAR = [&](int i) { return base + L::BAR + 8 * i; };
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::MISC);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + L::MISC + 4);
+    volatile int* nan_flag = reinterpret_cast<volatile int*>(smem + L::MISC + 8);
+
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int warp = uniform(tid >> 5);
+    const int h = blockIdx.y % a.cache.hkv, tile = blockIdx.y / a.cache.hkv;
+    griddep_wait();
+    griddep_launch_dependents();
+    int b = blockIdx.z, chunk = INT32_MAX / 2, k0 = 0;
+    if (a.slots > 0) {
+        chunk = chunk_keys(a);
+        int at = blockIdx.x;
+        for (b = 0; b < a.batch; ++b) {
+            const int n = chunks_of(keys_of(a, b), chunk);
+            if (at < n) break;
+            at -= n;
+        }
+        if (b == a.batch) return;
+        k0 = at * chunk;
+    }
+    const RowTile rt = row_tile(a, b, tile, 128);
+    if (rt.rows <= 0) return;
+    const int q0 = a.q_off[b];
+    const int seen = min(rt.len, rt.last0 + rt.query(rt.row0 + rt.rows - 1) + 1);
+    const int k1 = min(seen, k0 + chunk);
+    if (k0 >= k1 && a.slots > 0) return;  // (without chunks the tile's zeros are written here, else by the join)
+    const int all_see = rt.last0 + rt.query(rt.row0);  // the last key that every row sees
+    const int n_tiles = uniform(k1 > k0 ? (k1 - k0 + kTileKeys - 1) / kTileKeys : 0);
+    const int live = (rt.rows + 31) / 32;  // softmax warps with rows
+
+    if (tid == 0) {
+        mbar_init(BAR(B_K_FULL), 4);
+        mbar_init(BAR(B_V_FULL), 4);
+        mbar_init(BAR(B_S_FULL), 1);
+        mbar_init(BAR(B_P_FULL), (uint32_t)live);
+        mbar_init(BAR(B_PV_DONE), 1);
+        mbar_init(BAR(B_DRAIN), 1);
+        *abort_flag = 0;
+        *nan_flag = 0;
+        fence_mbar_init_cluster();
+    }
+    if (warp == 8) {
+        tmem_alloc(smem_u32(tmem_slot), 256);
+        tmem_relinquish();
+    }
+    // ---- the rows
+    const int row = rt.row0 + (tid < rt.rows ? tid : 0), query = rt.query(row);
+    float fac = 0.f;
+    if (tid < 128) {
+        const bool real = tid < rt.rows;
+        fac = a.c_log2 * stage_q<D, FP8>(a.q,
+                                         (int64_t)(q0 + query) * a.q_stride +
+                                             (int64_t)(h * a.group + row - query * a.group) * D,
+                                         real, base + L::Q, tid);
+        fence_proxy_async_shared();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = uniform(*tmem_slot);
+    const Ctl ctl{abort_flag, a.err, a.wait_budget};
+    float m = kNoRef, l = 0.f;
+
+    if (warp < 4) {
+        // ---------------------------------------------------------------- softmax: a row a thread
+        if (warp < live) {
+            const uint32_t ts = tmem + ((uint32_t)(warp * 32) << 16), to = ts + 128;
+            const int vis = min(rt.last0 + query, k1 - 1);  // the last key that the row sees here
+            float* logits = a.logits ? a.logits + (((int64_t)b * a.cache.hkv + h) * a.max_rows + row) * a.logit_stride
+                                     : nullptr;
+            const float2 fac2 = make_float2(fac, fac);
+            for (int t = 0; t < n_tiles; ++t) {
+                const int j0 = k0 + t * kTileKeys;
+                // groups of 16 keys without a page are as masked
+                uint32_t gone = 0;
+                {
+                    const int j = j0 + lane * 16;
+                    const bool none = lane < 8 && j < k1 &&
+                                      cache_page(a.cache.table, a.cache.width, a.cache.num_pages, a.cache.page_shift, b, j) < 0;
+                    gone = __ballot_sync(0xffffffffu, none);
+                }
+                const bool check = j0 + kTileKeys > min(k1, all_see + 1) || gone != 0;
+                if (!poll_phase_warp(BAR(B_S_FULL), (uint32_t)t & 1u, ctl)) break;
+                tc_fence_after();
+                // columns of a chunk of 32 that the row sees, as a mask
+                auto mask_of = [&](int c0) -> uint32_t {
+                    const int n = vis - (j0 + c0) + 1;
+                    uint32_t k = n >= 32 ? 0xFFFFFFFFu : (n <= 0 ? 0u : (1u << n) - 1u);
+                    if (gone >> (c0 / 16) & 1u) k &= 0xFFFF0000u;
+                    if (gone >> (c0 / 16 + 1) & 1u) k &= 0x0000FFFFu;
+                    return k;
+                };
+                float mx = -INFINITY;
+#pragma unroll 1
+                for (int c0 = 0; c0 < kTileKeys; c0 += 32) {
+                    float v[32];
+                    tmem_ld32(ts + c0, v);
+                    tmem_wait_ld();
+                    if (check) {
+                        const uint32_t k = mask_of(c0);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = k >> i & 1u ? v[i] : -INFINITY;
+                    }
+                    mx = fmaxf(mx, row_max<32>(v));
+                }
+                mx *= fac;  // (fac > 0)
+                if (__any_sync(0xffffffffu, mx > m + kRefSlack)) {
+                    const float mn = fmaxf(m, mx);
+                    const float f = ex2(m - mn);
+                    m = mn;
+                    l *= f;
+                    if (t > 0) {  // (the product with the last tile's values is done: S came behind it)
+#pragma unroll 1
+                        for (int c0 = 0; c0 < D; c0 += 32) {
+                            float v[32];
+                            tmem_ld32(to + c0, v);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) v[i] *= f;
+                            tmem_st32(to + c0, v);
+                        }
+                        tmem_wait_st();
+                    }
+                }
+                const float2 nm2 = make_float2(-m, -m);
+                float2 s0 = make_float2(0.f, 0.f), s1 = make_float2(0.f, 0.f);
+#pragma unroll 1
+                for (int c0 = 0; c0 < kTileKeys; c0 += 32) {
+                    float v[32];
+                    tmem_ld32(ts + c0, v);
+                    tmem_wait_ld();
+                    if (check) {
+                        const uint32_t k = mask_of(c0);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = k >> i & 1u ? v[i] : -INFINITY;
+                    }
+                    if (logits && tid < rt.rows) {
+                        float4* out = reinterpret_cast<float4*>(logits + j0 + c0);
+                        if (j0 + c0 < k1)
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                __stcg(out + i, make_float4(v[4 * i] * fac, v[4 * i + 1] * fac, v[4 * i + 2] * fac,
+                                                            v[4 * i + 3] * fac));
+                    }
+                    float p[16];
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4) {
+                        const float2 x0 = ffma2(make_float2(v[i], v[i + 1]), fac2, nm2);
+                        const float2 x1 = ffma2(make_float2(v[i + 2], v[i + 3]), fac2, nm2);
+                        const float2 p0 = make_float2(ex2(x0.x), ex2(x0.y)), p1 = make_float2(ex2(x1.x), ex2(x1.y));
+                        s0 = fadd2(s0, p0);
+                        s1 = fadd2(s1, p1);
+                        p[i / 2] = __uint_as_float(pack_h2(p0.x, p0.y));
+                        p[i / 2 + 1] = __uint_as_float(pack_h2(p1.x, p1.y));
+                    }
+                    tmem_st16(ts + c0 / 2, p);
+                }
+                l += (s0.x + s0.y) + (s1.x + s1.y);
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(BAR(B_P_FULL));
+            }
+        }
+    } else if (warp < 8) {
+        // ---------------------------------------------------------------- codes to values
+        const int w = warp - 4;
+        const CachePages& C = a.cache;
+        const int smask = (1 << C.page_shift) - 1;
+        // K: channels [c * D/4, ..) of the keys w * 32 + (lane & 7) + 8 i; V: keys kg * 8 .., block vb
+        const int c = lane >> 3, kr = w * 32 + (lane & 7);
+        const int kg = (lane & 7) + 8 * (lane >> 3 & 1), vb = 2 * w + (lane >> 4);
+        const bool v_part = vb < D / 16;
+        auto page_at = [&](int j) -> int32_t {
+            return j < k1 ? cache_page(C.table, C.width, C.num_pages, C.page_shift, b, j) : -1;
+        };
+        auto report = [&](int32_t page, int j) {
+            if (page < 0 && j < k1) atomicOr(a.err, kErrBounds);
+        };
+        auto load_k = [&](KPart<D>& x, int32_t p0, int32_t p1, int j0) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int32_t page = i < 2 ? p0 : p1;
+                const int j = j0 + kr + 8 * i;
+                x.code[i] = make_uint4(0u, 0u, 0u, 0u);
+                x.scale[i] = 0u;
+                if (page >= 0) {
+                    const int64_t at = cache_row(page, C.hkv, h, C.page_shift, j & smask);
+                    if constexpr (D == 128) {
+                        x.code[i] = __ldg(reinterpret_cast<const uint4*>(C.codes[0] + at * 64 + c * 16));
+                        x.scale[i] = __ldg(reinterpret_cast<const uint16_t*>(C.scales[0] + at * 8 + c * 2));
+                    } else {
+                        const uint2 v = __ldg(reinterpret_cast<const uint2*>(C.codes[0] + at * 32 + c * 8));
+                        x.code[i].x = v.x, x.code[i].y = v.y;
+                        x.scale[i] = __ldg(C.scales[0] + at * 4 + c);
+                    }
+                }
+            }
+        };
+        auto load_v = [&](VPart& x, int32_t page, int j0) {
+            const int64_t at = cache_row(page >= 0 ? page : 0, C.hkv, h, C.page_shift, (j0 + kg * 8) & smask);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                x.code[i] = make_uint2(0u, 0u);
+                x.scale[i] = 0u;
+                if (page >= 0 && v_part) {
+                    x.code[i] = __ldg(reinterpret_cast<const uint2*>(C.codes[1] + (at + i) * (D / 2) + vb * 8));
+                    x.scale[i] = __ldg(C.scales[1] + (at + i) * (D / 16) + vb);
+                }
+            }
+        };
+        // pages of the thread's keys (a group of 16 lies in one), a tile ahead of their loads
+        int32_t pk0 = page_at(k0 + w * 32), pk1 = page_at(k0 + w * 32 + 16), pv = page_at(k0 + kg * 8);
+        KPart<D> kp;
+        VPart vp;
+        if (n_tiles > 0) {
+            if ((lane & 15) == 0) report(lane ? pk1 : pk0, k0 + w * 32 + lane);
+            load_k(kp, pk0, pk1, k0);
+            load_v(vp, pv, k0);
+        }
+        for (int t = 0; t < n_tiles; ++t) {
+            const int j0 = k0 + t * kTileKeys, jn = j0 + kTileKeys;
+            const bool more = t + 1 < n_tiles;
+            if (more) {
+                pk0 = page_at(jn + w * 32);
+                pk1 = page_at(jn + w * 32 + 16);
+                pv = page_at(jn + kg * 8);
+                if ((lane & 15) == 0) report(lane ? pk1 : pk0, jn + w * 32 + lane);
+            }
+            if (t > 0 && !poll_phase_warp(BAR(B_S_FULL), (uint32_t)(t - 1) & 1u, ctl)) break;  // K is free
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int key = kr + 8 * i;
+                const uint32_t words[4] = {kp.code[i].x, kp.code[i].y, kp.code[i].z, kp.code[i].w};
+                const __half2 sc = e4m3x2_value(kp.scale[i]);
+                const __half2 sb[2] = {__low2half2(sc), D == 128 ? __high2half2(sc) : __low2half2(sc)};
+#pragma unroll
+                for (int q = 0; q < D / 32; ++q) {  // 8 channels
+                    __half2 x[4];
+                    e2m1x8_value(words[q], x);
+                    const __half2 s = sb[q / 2];
+                    const int u = c * (D / 32) + q;
+                    st_shared16(base + L::K + (u >> 3) * L::ATOM + key * 128 + (((u & 7) ^ (key & 7)) << 4),
+                                h2_bits(__hmul2(x[0], s)), h2_bits(__hmul2(x[1], s)), h2_bits(__hmul2(x[2], s)),
+                                h2_bits(__hmul2(x[3], s)));
+                }
+            }
+            fence_proxy_async_shared();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(BAR(B_K_FULL));
+            if (more) load_k(kp, pk0, pk1, jn);
+            if (t > 0 && !poll_phase_warp(BAR(B_PV_DONE), (uint32_t)(t - 1) & 1u, ctl)) break;  // V is free
+            if (v_part) {
+                if (j0 + kTileKeys - 1 > all_see) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int j = j0 + kg * 8 + i;
+                        // what lies behind the last key may be anything, a NaN scale among it
+                        if (j >= k1) vp.scale[i] = 0u;
+                        // a NaN value must not reach the rows that do not see it (0 * NaN): put in at the end
+                        if (j > all_see && (vp.scale[i] & 0x7Fu) == 0x7Fu) {
+                            vp.scale[i] = 0u;
+                            *nan_flag = 1;
+                        }
+                    }
+                }
+                __half2 s[4];
+#pragma unroll
+                for (int p = 0; p < 4; ++p) s[p] = e4m3x2_value(vp.scale[2 * p] | (vp.scale[2 * p + 1] << 8));
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {  // 8 channels: even ones from the low codes, odd ones from the high
+                    __half2 ev[4][4], od[4][4];
+                    const uint32_t lo = 0x0F0F0F0Fu;
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) {
+                        const uint32_t x = q ? vp.code[2 * p].y : vp.code[2 * p].x;
+                        const uint32_t y = q ? vp.code[2 * p + 1].y : vp.code[2 * p + 1].x;
+                        e2m1x8_value((x & lo) | ((y << 4) & ~lo), ev[p]);
+                        e2m1x8_value(((x >> 4) & lo) | (y & ~lo), od[p]);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int ch = vb * 16 + q * 8 + i;
+                        uint32_t f[4];
+#pragma unroll
+                        for (int p = 0; p < 4; ++p) f[p] = h2_bits(__hmul2(i & 1 ? od[p][i / 2] : ev[p][i / 2], s[p]));
+                        st_shared16(base + L::V + (kg >> 3) * (D * 128) + ch * 128 + (((kg & 7) ^ (ch & 7)) << 4), f[0],
+                                    f[1], f[2], f[3]);
+                    }
+                }
+            }
+            fence_proxy_async_shared();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(BAR(B_V_FULL));
+            if (more) load_v(vp, pv, jn);
+        }
+    } else {
+        // ---------------------------------------------------------------- contractions
+        const uint32_t idesc_s = idesc_make(128, kTileKeys, 0u), idesc_o = idesc_make(128, D, 0u);
+        for (int t = 0; t < n_tiles; ++t) {
+            const uint32_t ph = (uint32_t)t & 1u;
+            if (!poll_phase_warp(BAR(B_K_FULL), ph, ctl)) break;
+            // S takes the place of the last tile's P
+            if (t > 0 && !poll_phase_warp(BAR(B_PV_DONE), ph ^ 1u, ctl)) break;
+            tc_fence_after();
+            if (elect_one()) {
+#pragma unroll
+                for (int st = 0; st < D / 16; ++st) {
+                    const uint32_t off = (st >> 2) * L::ATOM + (st & 3) * 32;
+                    mma_f16(tmem, sdesc_k_sw128(base + L::Q + off), sdesc_k_sw128(base + L::K + off), idesc_s, st > 0);
+                }
+                mma_commit(BAR(B_S_FULL));
+            }
+            __syncwarp();
+            if (!poll_phase_warp(BAR(B_V_FULL), ph, ctl)) break;
+            if (!poll_phase_warp(BAR(B_P_FULL), ph, ctl)) break;
+            tc_fence_after();
+            if (elect_one()) {
+#pragma unroll
+                for (int st = 0; st < kTileKeys / 16; ++st)
+                    mma_f16_ta(tmem + 128, tmem + st * 8,
+                               sdesc_k_sw128(base + L::V + (st >> 2) * (D * 128) + (st & 3) * 32), idesc_o,
+                               t > 0 || st > 0);
+                mma_commit(BAR(B_PV_DONE));
+            }
+            __syncwarp();
+        }
+        // every contraction issued has ended before tensor memory is read or released, also where
+        // a wait gave up
+        if (elect_one()) mma_commit(BAR(B_DRAIN));
+        __syncwarp();
+        volatile int no_abort = 0;
+        const Ctl drain{&no_abort, a.err, kWaitBudgetCycles};
+        wait_phase(BAR(B_DRAIN), 0u, drain);
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+
+    // ---- the rows' results
+    if (warp < live && !*abort_flag) {
+        const bool real = tid < rt.rows;
+        const uint32_t to = tmem + ((uint32_t)(warp * 32) << 16) + 128;
+        const int64_t at = (int64_t)(q0 + query) * a.hq + h * a.group + row - query * a.group;
+        const int64_t part = ((int64_t)blockIdx.x * a.cache.hkv + h) * a.max_rows + row;
+        const float f = a.slots > 0 ? 1.f : (l == 0.f ? 0.f : a.cache.scale[1] / l);
+#pragma unroll 1
+        for (int c0 = 0; c0 < D; c0 += 32) {
+            float v[32];
+            if (n_tiles > 0) {
+                tmem_ld32(to + c0, v);
+                tmem_wait_ld();
+            } else {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] = 0.f;
+            }
+            if (*nan_flag) {  // values that are NaN, for the rows that see them
+                for (int j = max(k0, all_see + 1); j < min(k1, rt.last0 + query + 1); ++j) {
+                    const int32_t page = cache_page(a.cache.table, a.cache.width, a.cache.num_pages, a.cache.page_shift, b, j);
+                    if (page < 0) continue;
+                    const int64_t r = cache_row(page, a.cache.hkv, h, a.cache.page_shift, j & ((1 << a.cache.page_shift) - 1));
+#pragma unroll
+                    for (int q = 0; q < 2; ++q)
+                        if ((a.cache.scales[1][r * (D / 16) + c0 / 16 + q] & 0x7Fu) == 0x7Fu)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) v[16 * q + i] = __int_as_float(0x7FC00000);
+                }
+            }
+            if (!real) continue;
+            if (a.slots > 0) {
+                float4* out = reinterpret_cast<float4*>(a.part_o + part * D + c0);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) __stcg(out + i, make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]));
+            } else {
+                uint4* out = reinterpret_cast<uint4*>(a.out + at * D + c0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t o[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        // (a row that sees no key is 0, whatever the columns hold)
+                        const __nv_bfloat162 x = __floats2bfloat162_rn(l == 0.f ? 0.f : v[8 * i + 2 * k] * f,
+                                                                       l == 0.f ? 0.f : v[8 * i + 2 * k + 1] * f);
+                        o[k] = *reinterpret_cast<const uint32_t*>(&x);
+                    }
+                    out[i] = make_uint4(o[0], o[1], o[2], o[3]);
+                }
+            }
+        }
+        if (real && a.slots > 0) a.part_ml[part] = make_float2(m, l);
+        if (real && a.slots == 0 && a.lse) a.lse[at] = l == 0.f ? INFINITY : m + log2f(l);
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 8) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 256);
+    }
+}
+
+template <int D, bool FP8>
+cudaError_t launch_variant(const AttendArgs& a, int tiles, cudaStream_t stream)
+{
+    using L = TileLayout<D>;
+    auto kern = attend_tile_kernel<D, FP8>;
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, L::ALLOC);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = a.slots > 0 ? dim3((unsigned)a.slots, (unsigned)(tiles * a.cache.hkv), 1)
+                              : dim3(1, (unsigned)(tiles * a.cache.hkv), (unsigned)a.batch);
+    cfg.blockDim = dim3(kTileThreads, 1, 1);
+    cfg.dynamicSmemBytes = L::ALLOC;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1] = {pdl_attribute()};
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kern, a);
+}
+
+}  // namespace
+
+cudaError_t launch_attend_tiles(const AttendArgs& a, int head_dim, bool fp8, int tiles, cudaStream_t stream)
+{
+    if (fp8) return launch_variant<128, true>(a, tiles, stream);
+    return head_dim == 128 ? launch_variant<128, false>(a, tiles, stream) : launch_variant<64, false>(a, tiles, stream);
+}
+
+}  // namespace lvs

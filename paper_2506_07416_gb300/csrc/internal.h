@@ -175,9 +175,10 @@ struct AttendArgs {
     const float* weights_in;  // [num_pages][page_size]
     float* weights_out;       // null: no weights
     int32_t* err;
+    long long wait_budget;
 };
 struct AttendPlan {
-    int32_t row_tile;         // rows (query x head of a key head) of a CTA: 8, 16 or 32
+    int32_t row_tile;         // rows (query x head of a key head) of a CTA: 8, 16, 32 or 128
     int32_t slots;
     bool logits;              // the weights are made from kept scores
 };

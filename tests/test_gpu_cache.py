@@ -209,7 +209,8 @@ def test_attend_matches_the_definition(select, hq, hkv, d, page, dtype, lens, co
     o, wn, slack, slack_w = ref.attend(c, table, lens, qv, off, hq, w if weights else None)
     got = out.double().cpu().numpy()
     assert np.isfinite(got).all()
-    assert (np.abs(got - o) <= slack).all(), float((np.abs(got - o) / np.maximum(slack, 1e-30)).max())
+    worst = float((np.abs(got - o) / np.maximum(slack, 1e-30)).max())
+    assert worst <= 1.0
     assert (cache.weights.cpu().numpy() == w).all()
     if weights:
         touched = slack_w > 0
@@ -251,10 +252,11 @@ def test_attend_extreme_scores(select):
     s.close()
 
 
-def test_attend_nan_reaches_only_the_rows_that_see_it(select):
+@pytest.mark.parametrize("t", [6, 40])
+def test_attend_nan_reaches_only_the_rows_that_see_it(select, t):
     """A NaN or infinite query channel, a NaN key, a NaN value: rows that do not see them are as without them."""
     rng = np.random.default_rng(6)
-    hq, d, n, t = 4, 128, 100, 6
+    hq, d, n = 4, 128, 100
     table, pool = tables(rng, [n], 16)
     clean = random_pool(rng, pool, 2, 16, d)
     q, qv, _ = make_q(rng, t, hq, d, "bf16")
