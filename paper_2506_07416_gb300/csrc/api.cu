@@ -1361,7 +1361,7 @@ litevlm_status_t attend_plan(litevlm_select_t h, int32_t batch, const int32_t* q
     if (rows > INT32_MAX / 2 || (int64_t)c.num_kv_heads * ((rows + 7) / 8) > 65535)
         return fail(h, LITEVLM_ERR_UNSUPPORTED, "num_kv_heads x rows of the longest request / 8 exceeds 65535");
     *max_rows = (int)rows;
-    *plan = lvs::plan_cache_attend(batch, c.num_kv_heads, *max_rows, max_len, h->num_sms);
+    *plan = lvs::plan_cache_attend(batch, c.num_kv_heads, (int)group, q_offsets_h, max_len, h->num_sms);
     return LITEVLM_OK;
 }
 

@@ -989,24 +989,36 @@ cudaError_t launch_all(const AttendArgs& a, const AttendPlan& plan, int max_rows
 
 }  // namespace
 
-constexpr int kFewRows = 32;
+constexpr int kFewRows = 32;  // rows of a request's key head up to which the kernel for few rows is taken
 
-AttendPlan plan_cache_attend(int batch, int hkv, int max_rows, int64_t max_len, int num_sms)
+AttendPlan plan_cache_attend(int batch, int hkv, int group, const int32_t* q_off, int64_t max_len, int num_sms)
 {
+    int max_t = 0;
+    for (int b = 0; b < batch; ++b) max_t = std::max(max_t, q_off[b + 1] - q_off[b]);
+    const int64_t max_rows = (int64_t)max_t * group;
     AttendPlan p;
     p.row_tile = max_rows <= 8 ? 8 : (max_rows <= 16 ? 16 : (max_rows <= kFewRows ? 32 : 128));
-    const int64_t tiles = (max_rows + p.row_tile - 1) / p.row_tile;
-    const int64_t per_key = (tiles > 0 ? tiles : 1) * hkv;  // CTAs for every chunk
-    const int64_t items = per_key * (batch > 0 ? batch : 1);
-    // Four CTAs run on an SM (two of the kernel for many rows). Where the batch has fewer than two for every one of these places,
-    // the keys are split over that many CTAs; else a CTA takes all keys of its rows.
+    int64_t items = 0;  // CTAs where each takes all keys of its rows
+    for (int b = 0; b < batch; ++b)
+        items += ((int64_t)(q_off[b + 1] - q_off[b]) * group + p.row_tile - 1) / p.row_tile * hkv;
+    // The keys are split into n chunks a request where that fills the GPU better: items * n CTAs of
+    // 1/n of the work run in rounds of as many as fit at once (four on an SM, two of the kernel for
+    // many rows), and every chunk costs the writing and joining of its sums, about a twentieth of
+    // a round.
     const int64_t places = (int64_t)num_sms * (p.row_tile == 128 ? 2 : 4);
-    p.slots = 0;
-    if (max_len > 64 && items < 2 * places) {
-        const int64_t units = (max_len + 63) / 64 * (batch > 0 ? batch : 1);
-        p.slots = (int32_t)std::min(units, std::max((int64_t)batch, places / per_key));
+    const int64_t units = std::max<int64_t>(1, (max_len + 63) / 64);
+    int64_t best = 1;
+    if (items > 0 && items < places) {
+        best = std::min(units, places / items);
+    } else if (items < 3 * places) {  // (from three rounds on the last one's idle places matter little)
+        double cost = 1e30;
+        for (int64_t n = 1; n <= std::min<int64_t>(units, 8); ++n) {
+            const double c = (double)((items * n + places - 1) / places) / (double)n + (n > 1 ? 0.05 * n : 0.0);
+            if (c < cost) cost = c, best = n;
+        }
     }
-    p.logits = max_rows > 0 && max_rows <= 32 && (int64_t)max_rows * hkv <= kLogitRows;
+    p.slots = best > 1 ? (int32_t)std::min<int64_t>(best * batch, 1 << 20) : 0;
+    p.logits = max_rows > 0 && max_rows <= 32 && max_rows * hkv <= kLogitRows;
     return p;
 }
 

@@ -11,6 +11,10 @@
 //   warps 0-3 hold a row a thread: they read S twice (its largest score, then the
 //     exponentials), write P as f16 over S, and keep the row's reference and sum. A
 //     reference moves only when a score passes it by 8; O is then rescaled in place.
+// Of 64 rows or fewer (32) every row stands in two (four) of the 128 places, and each place
+// takes a half (a quarter) of the tile's keys, with zeros for the others in its P: the
+// exponentials of a few rows are then made by four warps and not by one. The places of a
+// row are added up at the end, as the chunks are.
 // What bounds it: an SM makes 16 exponentials a clock, a tile of 128 x 128 takes 1024
 // clocks of them, against 512 of contractions, so two CTAs share an SM: while one waits
 // for a contraction the other computes. That needs 256 columns and at most 113 KB each, so
@@ -34,6 +38,7 @@ struct TileLayout {
     static constexpr int V = K + D / 64 * ATOM;            // [2] halves of the keys: D channels x 64 keys
     static constexpr int BAR = V + 2 * D * 128;
     static constexpr int MISC = BAR + 8 * B_COUNT;
+    static_assert(128 * (D + 4) * 4 + 1024 <= BAR, "the places' sums fit the operands' memory");
     // at least 77 KB: no more than two CTAs (of 256 columns each) share an SM
     static constexpr int NEED = MISC + 16 + 1024;
     static constexpr int ALLOC = NEED > 77 * 1024 ? NEED : 77 * 1024;
@@ -159,7 +164,9 @@ __global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __gr
     if (k0 >= k1 && a.slots > 0) return;  // (without chunks the tile's zeros are written here, else by the join)
     const int all_see = rt.last0 + rt.query(rt.row0);  // the last key that every row sees
     const int n_tiles = uniform(k1 > k0 ? (k1 - k0 + kTileKeys - 1) / kTileKeys : 0);
-    const int live = (rt.rows + 31) / 32;  // softmax warps with rows
+    // places of a row, and softmax warps with rows
+    const int places = rt.rows <= 32 ? 4 : (rt.rows <= 64 ? 2 : 1);
+    const int live = places == 1 ? (rt.rows + 31) / 32 : 4;
 
     if (tid == 0) {
         mbar_init(BAR(B_K_FULL), 4);
@@ -177,10 +184,11 @@ __global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __gr
         tmem_relinquish();
     }
     // ---- the rows
-    const int row = rt.row0 + (tid < rt.rows ? tid : 0), query = rt.query(row);
+    const int place = tid & (128 / places - 1);  // the thread's row of the tile (softmax warps)
+    const bool real = place < rt.rows;
+    const int row = rt.row0 + (real ? place : 0), query = rt.query(row);
     float fac = 0.f;
     if (tid < 128) {
-        const bool real = tid < rt.rows;
         fac = a.c_log2 * stage_q<D, FP8>(a.q,
                                          (int64_t)(q0 + query) * a.q_stride +
                                              (int64_t)(h * a.group + row - query * a.group) * D,
@@ -202,6 +210,11 @@ __global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __gr
             float* logits = a.logits ? a.logits + (((int64_t)b * a.cache.hkv + h) * a.max_rows + row) * a.logit_stride
                                      : nullptr;
             const float2 fac2 = make_float2(fac, fac);
+            // the columns of this place
+            const int own = kTileKeys / places, first = uniform((tid & 127) / own * own * (places > 1)), end = first + own;
+            float zero[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) zero[i] = 0.f;
             for (int t = 0; t < n_tiles; ++t) {
                 const int j0 = k0 + t * kTileKeys;
                 // groups of 16 keys without a page are as masked
@@ -224,9 +237,8 @@ __global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __gr
                     return k;
                 };
                 float mx = -INFINITY;
-#pragma unroll 1
-                for (int c0 = 0; c0 < kTileKeys; c0 += 32) {
-                    float v[32];
+                float v[32];
+                auto read = [&](int c0) {
                     tmem_ld32(ts + c0, v);
                     tmem_wait_ld();
                     if (check) {
@@ -234,6 +246,10 @@ __global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __gr
 #pragma unroll
                         for (int i = 0; i < 32; ++i) v[i] = k >> i & 1u ? v[i] : -INFINITY;
                     }
+                };
+#pragma unroll 1
+                for (int c0 = first; c0 < end; c0 += 32) {
+                    read(c0);
                     mx = fmaxf(mx, row_max<32>(v));
                 }
                 mx *= fac;  // (fac > 0)
@@ -244,13 +260,13 @@ __global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __gr
                     l *= f;
                     if (t > 0) {  // (the product with the last tile's values is done: S came behind it)
 #pragma unroll 1
-                        for (int c0 = 0; c0 < D; c0 += 32) {
-                            float v[32];
-                            tmem_ld32(to + c0, v);
+                        for (int c0 = 0; c0 < D; c0 += 16) {
+                            float x[16];
+                            tmem_ld16(to + c0, x);
                             tmem_wait_ld();
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) v[i] *= f;
-                            tmem_st32(to + c0, v);
+                            for (int i = 0; i < 16; ++i) x[i] *= f;
+                            tmem_st16(to + c0, x);
                         }
                         tmem_wait_st();
                     }
@@ -258,16 +274,9 @@ __global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __gr
                 const float2 nm2 = make_float2(-m, -m);
                 float2 s0 = make_float2(0.f, 0.f), s1 = make_float2(0.f, 0.f);
 #pragma unroll 1
-                for (int c0 = 0; c0 < kTileKeys; c0 += 32) {
-                    float v[32];
-                    tmem_ld32(ts + c0, v);
-                    tmem_wait_ld();
-                    if (check) {
-                        const uint32_t k = mask_of(c0);
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] = k >> i & 1u ? v[i] : -INFINITY;
-                    }
-                    if (logits && tid < rt.rows) {
+                for (int c0 = first; c0 < end; c0 += 32) {
+                    if (own > 32) read(c0);  // (a place of 32 columns still has them)
+                    if (logits && real) {
                         float4* out = reinterpret_cast<float4*>(logits + j0 + c0);
                         if (j0 + c0 < k1)
 #pragma unroll
@@ -289,6 +298,11 @@ __global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __gr
                     tmem_st16(ts + c0 / 2, p);
                 }
                 l += (s0.x + s0.y) + (s1.x + s1.y);
+                if (places > 1) {
+#pragma unroll 1
+                    for (int c0 = 0; c0 < kTileKeys; c0 += 32)
+                        if (c0 < first || c0 >= end) tmem_st16(ts + c0 / 2, zero);
+                }
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
@@ -300,9 +314,14 @@ __global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __gr
         const int w = warp - 4;
         const CachePages& C = a.cache;
         const int smask = (1 << C.page_shift) - 1;
-        // K: channels [c * D/4, ..) of the keys w * 32 + (lane & 7) + 8 i; V: keys kg * 8 .., block vb
+        // K: channels [c * D/4, ..) of the keys w * 32 + (lane & 7) + 8 i; V: keys kg * 8 .., block vb:
+        // a warp's loads then cover whole rows, and the stores of eight neighbouring lanes eight
+        // banks' worth of shared memory. For V these are four groups of keys of two blocks, so
+        // odd blocks take their channels 4 to 7 first (their words are turned by half).
         const int c = lane >> 3, kr = w * 32 + (lane & 7);
-        const int kg = (lane & 7) + 8 * (lane >> 3 & 1), vb = 2 * w + (lane >> 4);
+        const int kg = 4 * w + (lane & 3), vb = lane >> 2, turn = (vb & 1) * 4;
+        const uint32_t v_at = base + L::V + (kg >> 3) * (D * 128) + vb * 16 * 128;
+        const uint32_t v_x = (uint32_t)(turn << 7 | ((kg & 7) ^ turn) << 4);
         const bool v_part = vb < D / 16;
         auto page_at = [&](int j) -> int32_t {
             return j < k1 ? cache_page(C.table, C.width, C.num_pages, C.page_shift, b, j) : -1;
@@ -406,19 +425,19 @@ __global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __gr
                     const uint32_t lo = 0x0F0F0F0Fu;
 #pragma unroll
                     for (int p = 0; p < 4; ++p) {
-                        const uint32_t x = q ? vp.code[2 * p].y : vp.code[2 * p].x;
-                        const uint32_t y = q ? vp.code[2 * p + 1].y : vp.code[2 * p + 1].x;
+                        uint32_t x = q ? vp.code[2 * p].y : vp.code[2 * p].x;
+                        uint32_t y = q ? vp.code[2 * p + 1].y : vp.code[2 * p + 1].x;
+                        x = __funnelshift_l(x, x, 4 * turn);
+                        y = __funnelshift_l(y, y, 4 * turn);
                         e2m1x8_value((x & lo) | ((y << 4) & ~lo), ev[p]);
                         e2m1x8_value(((x >> 4) & lo) | (y & ~lo), od[p]);
                     }
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int ch = vb * 16 + q * 8 + i;
+                    for (int i = 0; i < 8; ++i) {  // channel i ^ turn of the eight
                         uint32_t f[4];
 #pragma unroll
                         for (int p = 0; p < 4; ++p) f[p] = h2_bits(__hmul2(i & 1 ? od[p][i / 2] : ev[p][i / 2], s[p]));
-                        st_shared16(base + L::V + (kg >> 3) * (D * 128) + ch * 128 + (((kg & 7) ^ (ch & 7)) << 4), f[0],
-                                    f[1], f[2], f[3]);
+                        st_shared16(v_at + q * 1024 + ((uint32_t)(i << 7 | i << 4) ^ v_x), f[0], f[1], f[2], f[3]);
                     }
                 }
             }
@@ -471,57 +490,104 @@ __global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __gr
     tc_fence_after();
 
     // ---- the rows' results
-    if (warp < live && !*abort_flag) {
-        const bool real = tid < rt.rows;
-        const uint32_t to = tmem + ((uint32_t)(warp * 32) << 16) + 128;
+    const bool done = !*abort_flag;
+    // values that are NaN, for the rows that see them: whether block x of 16 channels has one
+    auto nan_block = [&](int x, int i) -> bool {
+        for (int j = max(k0, all_see + 1); j < min(k1, rt.last0 + i + 1); ++j) {
+            const int32_t page = cache_page(a.cache.table, a.cache.width, a.cache.num_pages, a.cache.page_shift, b, j);
+            if (page < 0) continue;
+            const int64_t r = cache_row(page, a.cache.hkv, h, a.cache.page_shift, j & ((1 << a.cache.page_shift) - 1));
+            if ((a.cache.scales[1][r * (D / 16) + x] & 0x7Fu) == 0x7Fu) return true;
+        }
+        return false;
+    };
+    const uint32_t to = tmem + ((uint32_t)((warp & 3) * 32) << 16) + 128;
+    if (places == 1 && warp < live && done) {
         const int64_t at = (int64_t)(q0 + query) * a.hq + h * a.group + row - query * a.group;
         const int64_t part = ((int64_t)blockIdx.x * a.cache.hkv + h) * a.max_rows + row;
         const float f = a.slots > 0 ? 1.f : (l == 0.f ? 0.f : a.cache.scale[1] / l);
 #pragma unroll 1
-        for (int c0 = 0; c0 < D; c0 += 32) {
-            float v[32];
+        for (int c0 = 0; c0 < D; c0 += 16) {
+            float v[16];
             if (n_tiles > 0) {
-                tmem_ld32(to + c0, v);
+                tmem_ld16(to + c0, v);
                 tmem_wait_ld();
             } else {
 #pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = 0.f;
-            }
-            if (*nan_flag) {  // values that are NaN, for the rows that see them
-                for (int j = max(k0, all_see + 1); j < min(k1, rt.last0 + query + 1); ++j) {
-                    const int32_t page = cache_page(a.cache.table, a.cache.width, a.cache.num_pages, a.cache.page_shift, b, j);
-                    if (page < 0) continue;
-                    const int64_t r = cache_row(page, a.cache.hkv, h, a.cache.page_shift, j & ((1 << a.cache.page_shift) - 1));
-#pragma unroll
-                    for (int q = 0; q < 2; ++q)
-                        if ((a.cache.scales[1][r * (D / 16) + c0 / 16 + q] & 0x7Fu) == 0x7Fu)
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) v[16 * q + i] = __int_as_float(0x7FC00000);
-                }
+                for (int i = 0; i < 16; ++i) v[i] = 0.f;
             }
             if (!real) continue;
+            if (*nan_flag && nan_block(c0 / 16, query)) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) v[i] = __int_as_float(0x7FC00000);
+            }
             if (a.slots > 0) {
                 float4* out = reinterpret_cast<float4*>(a.part_o + part * D + c0);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) __stcg(out + i, make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]));
+                for (int i = 0; i < 4; ++i) __stcg(out + i, make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]));
             } else {
-                uint4* out = reinterpret_cast<uint4*>(a.out + at * D + c0);
+                uint32_t o[8];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint32_t o[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        // (a row that sees no key is 0, whatever the columns hold)
-                        const __nv_bfloat162 x = __floats2bfloat162_rn(l == 0.f ? 0.f : v[8 * i + 2 * k] * f,
-                                                                       l == 0.f ? 0.f : v[8 * i + 2 * k + 1] * f);
-                        o[k] = *reinterpret_cast<const uint32_t*>(&x);
-                    }
-                    out[i] = make_uint4(o[0], o[1], o[2], o[3]);
+                for (int k = 0; k < 8; ++k) {
+                    // (a row that sees no key is 0, whatever the columns hold)
+                    const __nv_bfloat162 x =
+                        __floats2bfloat162_rn(l == 0.f ? 0.f : v[2 * k] * f, l == 0.f ? 0.f : v[2 * k + 1] * f);
+                    o[k] = *reinterpret_cast<const uint32_t*>(&x);
                 }
+                uint4* out = reinterpret_cast<uint4*>(a.out + at * D + c0);
+                out[0] = make_uint4(o[0], o[1], o[2], o[3]);
+                out[1] = make_uint4(o[4], o[5], o[6], o[7]);
             }
         }
         if (real && a.slots > 0) a.part_ml[part] = make_float2(m, l);
         if (real && a.slots == 0 && a.lse) a.lse[at] = l == 0.f ? INFINITY : m + log2f(l);
+    }
+    if (places > 1 && done) {
+        // the operands' memory is free: the places' sums [128][D + 4], references and sums of 2^s
+        float* sums = reinterpret_cast<float*>(smem);
+        float* refs = sums + 128 * (D + 4);
+        if (warp < 4) {
+#pragma unroll 1
+            for (int c0 = 0; c0 < D; c0 += 16) {
+                float v[16];
+                if (n_tiles > 0) {
+                    tmem_ld16(to + c0, v);
+                    tmem_wait_ld();
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] = 0.f;
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    *reinterpret_cast<float4*>(sums + tid * (D + 4) + c0 + 4 * i) =
+                        make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+            }
+            refs[tid] = m;
+            refs[128 + tid] = l;
+        }
+        __syncthreads();
+        const int step = 128 / places;  // from a place of a row to the next
+        for (int x = tid; x < rt.rows * D; x += kTileThreads) {
+            const int r = x / D, ch = x % D;
+            float M = kNoRef, L = 0.f, O = 0.f;
+            for (int p = 0; p < places; ++p) M = fmaxf(M, refs[r + p * step]);
+            for (int p = 0; p < places; ++p) {
+                const float f = ex2(refs[r + p * step] - M);
+                L += refs[128 + r + p * step] * f;
+                O += sums[(r + p * step) * (D + 4) + ch] * f;
+            }
+            const int rr = rt.row0 + r, i = rt.query(rr);
+            if (*nan_flag && nan_block(ch / 16, i)) O = __int_as_float(0x7FC00000);
+            if (a.slots > 0) {
+                const int64_t part = ((int64_t)blockIdx.x * a.cache.hkv + h) * a.max_rows + rr;
+                __stcg(a.part_o + part * D + ch, O);
+                if (ch == 0) a.part_ml[part] = make_float2(M, L);
+            } else {
+                const int64_t at = (int64_t)(q0 + i) * a.hq + h * a.group + rr - i * a.group;
+                a.out[at * D + ch] = __float2bfloat16_rn(L == 0.f ? 0.f : O / L * a.cache.scale[1]);
+                if (a.lse && ch == 0) a.lse[at] = L == 0.f ? INFINITY : M + log2f(L);
+            }
+        }
     }
     tc_fence_before();
     __syncthreads();
