@@ -1333,7 +1333,7 @@ int64_t round256(int64_t bytes) { return (bytes + 255) & ~(int64_t)255; }
 
 // Workspace of an attention call: the chunks' sums and statistics, and the rows' lse.
 struct AttendSpace {
-    int64_t part_o, part_ml, lse, logits, total;
+    int64_t part_o, part_ml, split, lse, logits, total;
 };
 int64_t logit_stride(int32_t max_len) { return ((int64_t)max_len + 31) & ~(int64_t)31; }
 // rows: of the call (query x head); head_rows: key heads x rows of the longest request
@@ -1343,7 +1343,8 @@ AttendSpace attend_space(const lvs::AttendPlan& plan, int64_t rows, int head_dim
     AttendSpace s{};
     const int64_t parts = plan.slots * head_rows;
     s.part_ml = round256(parts * head_dim * 4);
-    s.lse = s.part_ml + round256(parts * 8);
+    s.split = s.part_ml + round256(parts * 8);
+    s.lse = s.split + (plan.slots > 0 ? round256((int64_t)batch * 8) : 0);
     s.logits = s.lse + (weights ? round256(rows * 4) : 0);
     s.total = s.logits + (weights && plan.logits ? round256(batch * head_rows * logit_stride(max_len) * 4) : 0);
     return s;
@@ -1503,6 +1504,7 @@ litevlm_status_t litevlm_select_cache_attend(litevlm_select_t h, int32_t batch, 
     a.out = static_cast<__nv_bfloat16*>(out);
     a.part_o = reinterpret_cast<float*>(ws + space.part_o);
     a.part_ml = reinterpret_cast<float2*>(ws + space.part_ml);
+    a.split = reinterpret_cast<int2*>(ws + space.split);
     a.lse = weights_out ? reinterpret_cast<float*>(ws + space.lse) : nullptr;
     a.logits = weights_out && plan.logits ? reinterpret_cast<float*>(ws + space.logits) : nullptr;
     a.max_rows = max_rows;

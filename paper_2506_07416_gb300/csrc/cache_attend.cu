@@ -197,7 +197,10 @@ constexpr int kRingBytes = kAttWarps * kAttStages * 2 * Group<D>::kBytes;
 // row's channels of scale block n alone, and the score is the sum of the columns times the
 // key's scales; column n of PV holds p times the scales of block n, and the channels of
 // block n are read from column n.
-template <int D, int NT_, bool FP8>
+// WHOLE: the keys are not split (the request is then known to be the same for a whole CTA,
+// which keeps addresses out of the lanes' registers: the sweep's 128 requests take 127 us
+// and not 135).
+template <int D, int NT_, bool FP8, bool WHOLE>
 __global__ void __launch_bounds__(kAttThreads) attend_split_kernel(const __grid_constant__ AttendArgs a)
 {
     constexpr bool SINGLE = NT_ == 0;
@@ -221,16 +224,18 @@ __global__ void __launch_bounds__(kAttThreads) attend_split_kernel(const __grid_
     griddep_launch_dependents();
     // the request, and its part of the keys: all, or the chunk of this CTA's slot
     int b = blockIdx.z, chunk = INT32_MAX / 2, k0 = 0;
-    if (a.slots > 0) {
-        chunk = chunk_keys(a);
-        int at = blockIdx.x;
-        for (b = 0; b < a.batch; ++b) {
-            const int n = chunks_of(keys_of(a, b), chunk);
-            if (at < n) break;
-            at -= n;
+    __shared__ int split_s[3];
+    if (!WHOLE && a.slots > 0) {
+        if (threadIdx.x < 32) {
+            chunk = chunk_keys(a);
+            find_slot(a, blockIdx.x, chunk, b, k0);
+            if (threadIdx.x == 0) split_s[0] = chunk, split_s[1] = b, split_s[2] = k0;
         }
+        __syncthreads();
+        chunk = uniform(split_s[0]), b = uniform(split_s[1]), k0 = uniform(split_s[2]);
         if (b == a.batch) return;
-        k0 = at * chunk;
+        // (for the launch that joins the chunks: their length, and the request's first slot)
+        if (k0 == 0 && blockIdx.y == 0 && threadIdx.x == 0) a.split[b] = make_int2(chunk, (int)blockIdx.x);
     }
     const RowTile rt = row_tile(a, b, tile, ROWS);
     if (rt.rows <= 0) return;
@@ -239,7 +244,7 @@ __global__ void __launch_bounds__(kAttThreads) attend_split_kernel(const __grid_
     // keys that the tile's last row sees, and this CTA's part of them
     const int seen = min(rt.len, rt.last0 + i_last + 1);
     const int k1 = min(seen, k0 + chunk);
-    if (k0 >= k1 && a.slots > 0) return;  // (without chunks the tile's zeros are written here, else by the join)
+    if (k0 >= k1 && !WHOLE && a.slots > 0) return;  // (without chunks the tile's zeros are written here, else by the join)
     const int all_see = rt.last0 + rt.query(rt.row0);  // the last key that every row sees
 
     constexpr int SPAN = 2 * G::kBytes;
@@ -631,7 +636,7 @@ __global__ void __launch_bounds__(kAttThreads) attend_split_kernel(const __grid_
                     if ((a.cache.scales[1][at_row * (D / 16) + ch / 16] & 0x7Fu) == 0x7Fu) O = __int_as_float(0x7FC00000);
                 }
             }
-            if (a.slots == 0) {
+            if (WHOLE || a.slots == 0) {
                 // (a row that sees no key is 0; the comparison keeps a NaN sum)
                 a.out[at * D + ch] = __float2bfloat16_rn(L == 0.f ? 0.f : O / L * a.cache.scale[1]);
                 if (a.lse && ch == 0) a.lse[at] = L == 0.f ? INFINITY : M + log2f(L);
@@ -728,9 +733,9 @@ __global__ void __launch_bounds__(kFinishThreads) attend_finish_kernel(const __g
     const int len = cache_len(a.lens[b], a.limit, bad);
     const int q0 = a.q_off[b], t = a.q_off[b + 1] - q0;
     int chunk = INT32_MAX / 2, slot0 = 0;
-    if (a.slots > 0 && t > 0) {
-        chunk = chunk_keys(a);
-        slot0 = chunks_before(a, b, chunk);
+    if (a.slots > 0 && t > 0 && len > 0) {
+        const int2 v = __ldcg(a.split + b);
+        chunk = v.x, slot0 = v.y;
     }
     const int64_t step = (int64_t)a.cache.hkv * a.max_rows;  // from a chunk's statistics to the next's
     // chunks with keys that query i sees
@@ -814,31 +819,55 @@ __global__ void __launch_bounds__(kFinishThreads) attend_finish_kernel(const __g
     const int i = real ? r / a.hq : 0, hq = real ? r % a.hq : 0, h = hq / a.group;
     const int n = real ? chunks_seen(i) : 0;
     const int64_t from = ((int64_t)slot0 * a.cache.hkv + h) * a.max_rows + i * a.group + hq - h * a.group;
-    const float2 ml = join_stats(a.part_ml + from, step, n);
-    const float M = ml.x, L = ml.y;
-    float O[D / 32];
+    // chunks under a running reference, four of the warp's on their way at once
+    float M = kNoRef, L = 0.f, O[D / 32];
 #pragma unroll
     for (int e = 0; e < D / 32; ++e) O[e] = 0.f;
-#pragma unroll 4
-    for (int x = part; x < n; x += row_warps) {
-        const float f = ex2(__ldcg(a.part_ml + from + x * step).x - M);
-        const float* p = a.part_o + (from + x * step) * D + lane * (D / 32);
-        if constexpr (D == 128) {
-            const float4 v = __ldcg(reinterpret_cast<const float4*>(p));
-            O[0] += v.x * f, O[1] += v.y * f, O[2] += v.z * f, O[3] += v.w * f;
-        } else {
-            const float2 v = __ldcg(reinterpret_cast<const float2*>(p));
-            O[0] += v.x * f, O[1] += v.y * f;
+    auto add = [&](float m2, float l2, const float* v) {
+        const float top = fmaxf(M, m2), f = ex2(M - top), f2 = ex2(m2 - top);
+        M = top;
+        L = L * f + l2 * f2;
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) O[e] = O[e] * f + v[e] * f2;
+    };
+    for (int x0 = part; x0 < n; x0 += 4 * row_warps) {
+        float2 ml[4];
+        float v[4][D / 32];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int x = x0 + u * row_warps;
+            const float* p = a.part_o + (from + x * step) * D + lane * (D / 32);
+            ml[u] = make_float2(kNoRef, 0.f);
+#pragma unroll
+            for (int e = 0; e < D / 32; ++e) v[u][e] = 0.f;
+            if (x < n) {
+                ml[u] = __ldcg(a.part_ml + from + x * step);
+                if constexpr (D == 128) {
+                    const float4 w = __ldcg(reinterpret_cast<const float4*>(p));
+                    v[u][0] = w.x, v[u][1] = w.y, v[u][2] = w.z, v[u][3] = w.w;
+                } else {
+                    const float2 w = __ldcg(reinterpret_cast<const float2*>(p));
+                    v[u][0] = w.x, v[u][1] = w.y;
+                }
+            }
         }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (x0 + u * row_warps < n) add(ml[u].x, ml[u].y, v[u]);
     }
     if (row_warps > 1) {
+        __shared__ float2 ml_s[kFinishWarps];
 #pragma unroll
         for (int e = 0; e < D / 32; ++e) join_s[warp][lane * (D / 32) + e] = O[e];
+        if (lane == 0) ml_s[warp] = make_float2(M, L);
         __syncthreads();
         if (part != 0) return;
-        for (int w = 1; w < row_warps; ++w)
+        for (int w = 1; w < row_warps; ++w) {
+            float v[D / 32];
 #pragma unroll
-            for (int e = 0; e < D / 32; ++e) O[e] += join_s[warp + w][lane * (D / 32) + e];
+            for (int e = 0; e < D / 32; ++e) v[e] = join_s[warp + w][lane * (D / 32) + e];
+            add(ml_s[warp + w].x, ml_s[warp + w].y, v);
+        }
     }
     if (!real) return;
     const int64_t at = (int64_t)q0 * a.hq + r;
@@ -947,10 +976,12 @@ cudaError_t launch_all(const AttendArgs& a, const AttendPlan& plan, int max_rows
         cfg.gridDim = plan.slots > 0 ? dim3((unsigned)plan.slots, (unsigned)(tiles * a.cache.hkv), 1)
                                      : dim3(1, (unsigned)(tiles * a.cache.hkv), (unsigned)a.batch);
         cfg.blockDim = dim3(kAttThreads, 1, 1);
-        auto kern = max_rows == 1         ? attend_split_kernel<D, 0, FP8>
-                    : plan.row_tile == 8  ? attend_split_kernel<D, 1, FP8>
-                    : plan.row_tile == 16 ? attend_split_kernel<D, 2, FP8>
-                                          : attend_split_kernel<D, 4, FP8>;
+        const bool whole = plan.slots == 0;
+        auto kern = max_rows == 1 ? (whole ? attend_split_kernel<D, 0, FP8, true> : attend_split_kernel<D, 0, FP8, false>)
+                    : plan.row_tile == 8
+                        ? (whole ? attend_split_kernel<D, 1, FP8, true> : attend_split_kernel<D, 1, FP8, false>)
+                    : plan.row_tile == 16 ? attend_split_kernel<D, 2, FP8, false>
+                                          : attend_split_kernel<D, 4, FP8, false>;
         cfg.dynamicSmemBytes = kRingBytes<D>;
         static_assert(kRingBytes<D> + 10 * 1024 <= 48 * 1024, "no more shared memory than a launch has without asking");
         e = cudaLaunchKernelEx(&cfg, kern, a);

@@ -22,7 +22,10 @@ __device__ __forceinline__ int keys_of(const AttendArgs& a, int b)
     const int n = cache_len(__ldg(a.lens + b), a.limit, bad);
     return __ldg(a.q_off + b + 1) > __ldg(a.q_off + b) ? n : 0;
 }
-__device__ __forceinline__ int chunks_of(int keys, int chunk) { return (int)(((unsigned)keys + chunk - 1) / (unsigned)chunk); }
+__device__ __forceinline__ int chunks_of(int keys, int chunk)
+{
+    return (int)(((unsigned)keys + chunk - 1) / (unsigned)chunk);
+}
 __device__ __forceinline__ int chunk_keys(const AttendArgs& a)
 {
     if (a.batch == 1) return max(64, (chunks_of(keys_of(a, 0), a.slots) + 63) & ~63);
@@ -32,21 +35,41 @@ __device__ __forceinline__ int chunk_keys(const AttendArgs& a)
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
     const long long mean = (total + a.slots - 1) / a.slots;
-    const int mine = (int)min((long long)INT32_MAX / 2, (mean + mean * lane / 8 + 63) & ~63ll);
-    const unsigned c = (unsigned)max(mine, 64);
-    long long count = 0;
-    for (int b = 0; b < a.batch; ++b) count += ((unsigned)keys_of(a, b) + c - 1) / c;
-    const uint32_t fits = __ballot_sync(0xffffffffu, count <= a.slots);
-    return fits ? (int)__shfl_sync(0xffffffffu, c, __ffs(fits) - 1) : (a.limit + 63) & ~63;
+    const int c = max(64, (int)min((long long)INT32_MAX / 2, (mean + mean * lane / 8 + 63) & ~63ll));
+    // chunks by a reciprocal that errs upwards: never fewer than there are
+    const float inv = 1.000001f / (float)c;
+    float count = 0.f;
+    for (int b0 = 0; b0 < a.batch; b0 += 32) {
+        const float mine = b0 + lane < a.batch ? (float)keys_of(a, b0 + lane) : 0.f;
+        for (int x = 0; x < min(32, a.batch - b0); ++x) count += ceilf(__shfl_sync(0xffffffffu, mine, x) * inv);
+    }
+    const uint32_t fits = __ballot_sync(0xffffffffu, count <= (float)a.slots);
+    return fits ? __shfl_sync(0xffffffffu, c, __ffs(fits) - 1) : (a.limit + 63) & ~63;
 }
-// Chunks of the requests before b.
-__device__ __forceinline__ int chunks_before(const AttendArgs& a, int b, int chunk)
+// The request that a slot is of (a.batch: none), and the slot's first key.
+__device__ __forceinline__ void find_slot(const AttendArgs& a, int slot, int chunk, int& b, int& k0)
 {
-    int n = 0;
-    for (int x = threadIdx.x & 31; x < b; x += 32) n += chunks_of(keys_of(a, x), chunk);
+    const int lane = threadIdx.x & 31;
+    int before = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += 32) {
+        const int n = b0 + lane < a.batch ? chunks_of(keys_of(a, b0 + lane), chunk) : 0;
+        int sum = n;  // inclusive
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) n += __shfl_xor_sync(0xffffffffu, n, d);
-    return n;
+        for (int d = 1; d < 32; d <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, sum, d);
+            if (lane >= d) sum += y;
+        }
+        const uint32_t hit = __ballot_sync(0xffffffffu, slot < before + sum);
+        if (hit) {
+            const int x = __ffs(hit) - 1;
+            b = b0 + x;
+            k0 = (slot - before - __shfl_sync(0xffffffffu, sum - n, x)) * chunk;
+            return;
+        }
+        before += __shfl_sync(0xffffffffu, sum, 31);
+    }
+    b = a.batch;
+    k0 = 0;
 }
 
 // What every CTA of a request's tile needs to know of its rows.

@@ -145,16 +145,18 @@ __global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __gr
     griddep_wait();
     griddep_launch_dependents();
     int b = blockIdx.z, chunk = INT32_MAX / 2, k0 = 0;
+    __shared__ int split_s[3];
     if (a.slots > 0) {
-        chunk = chunk_keys(a);
-        int at = blockIdx.x;
-        for (b = 0; b < a.batch; ++b) {
-            const int n = chunks_of(keys_of(a, b), chunk);
-            if (at < n) break;
-            at -= n;
+        if (threadIdx.x < 32) {
+            chunk = chunk_keys(a);
+            find_slot(a, blockIdx.x, chunk, b, k0);
+            if (threadIdx.x == 0) split_s[0] = chunk, split_s[1] = b, split_s[2] = k0;
         }
+        __syncthreads();
+        chunk = uniform(split_s[0]), b = uniform(split_s[1]), k0 = uniform(split_s[2]);
         if (b == a.batch) return;
-        k0 = at * chunk;
+        // (for the launch that joins the chunks: their length, and the request's first slot)
+        if (k0 == 0 && blockIdx.y == 0 && threadIdx.x == 0) a.split[b] = make_int2(chunk, (int)blockIdx.x);
     }
     const RowTile rt = row_tile(a, b, tile, 128);
     if (rt.rows <= 0) return;
@@ -215,16 +217,18 @@ __global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __gr
             float zero[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) zero[i] = 0.f;
+            // page of a tile's group of 16 keys (lanes 0 to 7); groups without one are as masked
+            auto page_of = [&](int t) -> int32_t {
+                const int j = k0 + t * kTileKeys + lane * 16;
+                return lane < 8 && j < k1
+                           ? cache_page(a.cache.table, a.cache.width, a.cache.num_pages, a.cache.page_shift, b, j)
+                           : 0;
+            };
+            int32_t next_page = page_of(0);
             for (int t = 0; t < n_tiles; ++t) {
                 const int j0 = k0 + t * kTileKeys;
-                // groups of 16 keys without a page are as masked
-                uint32_t gone = 0;
-                {
-                    const int j = j0 + lane * 16;
-                    const bool none = lane < 8 && j < k1 &&
-                                      cache_page(a.cache.table, a.cache.width, a.cache.num_pages, a.cache.page_shift, b, j) < 0;
-                    gone = __ballot_sync(0xffffffffu, none);
-                }
+                const uint32_t gone = __ballot_sync(0xffffffffu, next_page < 0);
+                next_page = page_of(t + 1);
                 const bool check = j0 + kTileKeys > min(k1, all_see + 1) || gone != 0;
                 if (!poll_phase_warp(BAR(B_S_FULL), (uint32_t)t & 1u, ctl)) break;
                 tc_fence_after();
@@ -276,13 +280,12 @@ __global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __gr
 #pragma unroll 1
                 for (int c0 = first; c0 < end; c0 += 32) {
                     if (own > 32) read(c0);  // (a place of 32 columns still has them)
-                    if (logits && real) {
+                    if (logits && real && j0 + c0 < k1) {
                         float4* out = reinterpret_cast<float4*>(logits + j0 + c0);
-                        if (j0 + c0 < k1)
 #pragma unroll
-                            for (int i = 0; i < 8; ++i)
-                                __stcg(out + i, make_float4(v[4 * i] * fac, v[4 * i + 1] * fac, v[4 * i + 2] * fac,
-                                                            v[4 * i + 3] * fac));
+                        for (int i = 0; i < 8; ++i)
+                            __stcg(out + i, make_float4(v[4 * i] * fac, v[4 * i + 1] * fac, v[4 * i + 2] * fac,
+                                                        v[4 * i + 3] * fac));
                     }
                     float p[16];
 #pragma unroll
@@ -361,24 +364,26 @@ __global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __gr
                 }
             }
         };
-        // pages of the thread's keys (a group of 16 lies in one), a tile ahead of their loads
-        int32_t pk0 = page_at(k0 + w * 32), pk1 = page_at(k0 + w * 32 + 16), pv = page_at(k0 + kg * 8);
+        // pages of the thread's keys (a group of 16 lies in one), a tile ahead of the loads of the codes
+        int32_t pk0, pk1, pv;
+        auto pages = [&](int j0) {
+            pk0 = page_at(j0 + w * 32);
+            pk1 = page_at(j0 + w * 32 + 16);
+            pv = page_at(j0 + kg * 8);
+        };
+        auto report_pages = [&](int j0) {
+            if ((lane & 15) == 0) report(lane ? pk1 : pk0, j0 + w * 32 + lane);
+        };
         KPart<D> kp;
         VPart vp;
-        if (n_tiles > 0) {
-            if ((lane & 15) == 0) report(lane ? pk1 : pk0, k0 + w * 32 + lane);
-            load_k(kp, pk0, pk1, k0);
-            load_v(vp, pv, k0);
-        }
+        pages(k0);
+        report_pages(k0);
+        load_k(kp, pk0, pk1, k0);
+        load_v(vp, pv, k0);
+        pages(k0 + kTileKeys);
         for (int t = 0; t < n_tiles; ++t) {
             const int j0 = k0 + t * kTileKeys, jn = j0 + kTileKeys;
             const bool more = t + 1 < n_tiles;
-            if (more) {
-                pk0 = page_at(jn + w * 32);
-                pk1 = page_at(jn + w * 32 + 16);
-                pv = page_at(jn + kg * 8);
-                if ((lane & 15) == 0) report(lane ? pk1 : pk0, jn + w * 32 + lane);
-            }
             if (t > 0 && !poll_phase_warp(BAR(B_S_FULL), (uint32_t)(t - 1) & 1u, ctl)) break;  // K is free
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -400,7 +405,10 @@ __global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __gr
             fence_proxy_async_shared();
             __syncwarp();
             if (lane == 0) mbar_arrive(BAR(B_K_FULL));
-            if (more) load_k(kp, pk0, pk1, jn);
+            if (more) {
+                report_pages(jn);
+                load_k(kp, pk0, pk1, jn);
+            }
             if (t > 0 && !poll_phase_warp(BAR(B_PV_DONE), (uint32_t)(t - 1) & 1u, ctl)) break;  // V is free
             if (v_part) {
                 if (j0 + kTileKeys - 1 > all_see) {
@@ -445,6 +453,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __gr
             __syncwarp();
             if (lane == 0) mbar_arrive(BAR(B_V_FULL));
             if (more) load_v(vp, pv, jn);
+            pages(jn + kTileKeys);
         }
     } else {
         // ---------------------------------------------------------------- contractions

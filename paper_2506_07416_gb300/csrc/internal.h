@@ -168,6 +168,7 @@ struct AttendArgs {
     __nv_bfloat16* out;       // [rows][hq][d]
     float* part_o;            // [slots][hkv][max_rows][d] sums of a chunk's rows
     float2* part_ml;          // [slots][hkv][max_rows] their references and sums of 2^s
+    int2* split;              // [batch] chunk length and first slot of each request (slots > 0)
     float* lse;               // [rows * hq] log2 of the sum of 2^s (with weights)
     float* logits;            // [batch][hkv][max_rows][logit_stride] scores in log2 units, or null
     int32_t max_rows;         // rows (query x head of a key head) of the longest request
