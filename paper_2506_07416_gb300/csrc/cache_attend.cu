@@ -567,11 +567,13 @@ __global__ void __launch_bounds__(kAttThreads) attend_split_kernel(const __grid_
         stage = stage + 1 == kAttStages ? 0 : stage + 1;
         const uint32_t there = __ballot_sync(0xffffffffu, mine);
         if (there == 0xFFFFFFFFu && j0 + 31 <= all_see) {
-            group(span, j0, true, std::false_type{});
-            group(span + G::kBytes, j0 + 16, true, std::false_type{});
+            // (the code of many rows is long: once, it stays in the instruction cache)
+#pragma unroll(NT > 1 ? 1 : 2)
+            for (int x = 0; x < 2; ++x) group(span + x * G::kBytes, j0 + 16 * x, true, std::false_type{});
         } else {
-            group(span, j0, there & 1u, std::true_type{});
-            if (j0 + 16 < k1) group(span + G::kBytes, j0 + 16, there >> 16 & 1u, std::true_type{});
+#pragma unroll 1
+            for (int x = 0; x < 2; ++x)
+                if (j0 + 16 * x < k1) group(span + x * G::kBytes, j0 + 16 * x, there >> (16 * x) & 1u, std::true_type{});
         }
     }
     copy_async_wait<0>();
@@ -980,8 +982,7 @@ cudaError_t launch_all(const AttendArgs& a, const AttendPlan& plan, int max_rows
         auto kern = max_rows == 1 ? (whole ? attend_split_kernel<D, 0, FP8, true> : attend_split_kernel<D, 0, FP8, false>)
                     : plan.row_tile == 8
                         ? (whole ? attend_split_kernel<D, 1, FP8, true> : attend_split_kernel<D, 1, FP8, false>)
-                    : plan.row_tile == 16 ? attend_split_kernel<D, 2, FP8, false>
-                                          : attend_split_kernel<D, 4, FP8, false>;
+                        : attend_split_kernel<D, 2, FP8, false>;
         cfg.dynamicSmemBytes = kRingBytes<D>;
         static_assert(kRingBytes<D> + 10 * 1024 <= 48 * 1024, "no more shared memory than a launch has without asking");
         e = cudaLaunchKernelEx(&cfg, kern, a);
@@ -1028,7 +1029,7 @@ AttendPlan plan_cache_attend(int batch, int hkv, int group, const int32_t* q_off
     for (int b = 0; b < batch; ++b) max_t = std::max(max_t, q_off[b + 1] - q_off[b]);
     const int64_t max_rows = (int64_t)max_t * group;
     AttendPlan p;
-    p.row_tile = max_rows <= 8 ? 8 : (max_rows <= 16 ? 16 : (max_rows <= kFewRows ? 32 : 128));
+    p.row_tile = max_rows <= 8 ? 8 : (max_rows <= kFewRows ? 16 : 128);
     int64_t items = 0;  // CTAs where each takes all keys of its rows
     for (int b = 0; b < batch; ++b)
         items += ((int64_t)(q_off[b + 1] - q_off[b]) * group + p.row_tile - 1) / p.row_tile * hkv;
@@ -1036,11 +1037,12 @@ AttendPlan plan_cache_attend(int batch, int hkv, int group, const int32_t* q_off
     // 1/n of the work run in rounds of as many as fit at once (four on an SM, two of the kernel for
     // many rows), and every chunk costs the writing and joining of its sums, about a twentieth of
     // a round.
-    const int64_t places = (int64_t)num_sms * (p.row_tile == 128 ? 2 : 4);
+    const int64_t places = (int64_t)num_sms * (p.row_tile == 128 ? 2 : (p.row_tile == 16 ? 3 : 4));
+    const int rounds = p.row_tile == 16 && batch > 1 ? 3 : 1;
     const int64_t units = std::max<int64_t>(1, (max_len + 63) / 64);
     int64_t best = 1;
     if (items > 0 && items < places) {
-        best = std::min(units, places / items);
+        best = std::min(units, rounds * places / items);
     } else if (items < 3 * places) {  // (from three rounds on the last one's idle places matter little)
         double cost = 1e30;
         for (int64_t n = 1; n <= std::min<int64_t>(units, 8); ++n) {
