@@ -970,8 +970,8 @@ cudaError_t launch_all(const AttendArgs& a, const AttendPlan& plan, int max_rows
     cudaError_t e = cudaSuccess;
     if (total_rows > 0) {
         const int tiles = (max_rows + plan.row_tile - 1) / plan.row_tile;
-        if (plan.row_tile == 128) {
-            e = launch_attend_tiles(a, D, FP8, tiles, stream);
+        if (plan.row_tile >= 128) {
+            e = launch_attend_tiles(a, D, FP8, plan.row_tile, tiles, stream);
             if (e != cudaSuccess) return e;
             ++*launches;
         } else {
@@ -1029,7 +1029,7 @@ AttendPlan plan_cache_attend(int batch, int hkv, int group, const int32_t* q_off
     for (int b = 0; b < batch; ++b) max_t = std::max(max_t, q_off[b + 1] - q_off[b]);
     const int64_t max_rows = (int64_t)max_t * group;
     AttendPlan p;
-    p.row_tile = max_rows <= 8 ? 8 : (max_rows <= kFewRows ? 16 : 128);
+    p.row_tile = max_rows <= 8 ? 8 : (max_rows <= kFewRows ? 16 : (max_rows <= 128 ? 128 : 256));
     int64_t items = 0;  // CTAs where each takes all keys of its rows
     for (int b = 0; b < batch; ++b)
         items += ((int64_t)(q_off[b + 1] - q_off[b]) * group + p.row_tile - 1) / p.row_tile * hkv;
@@ -1037,7 +1037,7 @@ AttendPlan plan_cache_attend(int batch, int hkv, int group, const int32_t* q_off
     // 1/n of the work run in rounds of as many as fit at once (four on an SM, two of the kernel for
     // many rows), and every chunk costs the writing and joining of its sums, about a twentieth of
     // a round.
-    const int64_t places = (int64_t)num_sms * (p.row_tile == 128 ? 2 : (p.row_tile == 16 ? 3 : 4));
+    const int64_t places = (int64_t)num_sms * (p.row_tile == 256 ? 1 : (p.row_tile == 128 ? 2 : (p.row_tile == 16 ? 3 : 4)));
     const int rounds = p.row_tile == 16 && batch > 1 ? 3 : 1;
     const int64_t units = std::max<int64_t>(1, (max_len + 63) / 64);
     int64_t best = 1;

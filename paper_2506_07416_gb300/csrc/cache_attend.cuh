@@ -94,7 +94,7 @@ __device__ __forceinline__ RowTile row_tile(const AttendArgs& a, int b, int tile
     return r;
 }
 
-// The launch of cache_tile.cu: rows of 128 of a request's, `tiles` of them for the longest.
-cudaError_t launch_attend_tiles(const AttendArgs& a, int head_dim, bool fp8, int tiles, cudaStream_t stream);
+// The launch of cache_tile.cu: `tiles` tiles of 128 or 256 rows for the longest request.
+cudaError_t launch_attend_tiles(const AttendArgs& a, int head_dim, bool fp8, int row_tile, int tiles, cudaStream_t stream);
 
 }  // namespace lvs

@@ -27,21 +27,30 @@ namespace lvs {
 
 namespace {
 
-constexpr int kTileKeys = 128, kTileThreads = 288;
-enum { B_K_FULL, B_V_FULL, B_S_FULL, B_P_FULL, B_PV_DONE, B_DRAIN, B_COUNT };
+constexpr int kTileKeys = 128;
+// Barriers: operands of a stage written, operands of a stage read (two stages), and for each
+// of two row tiles scores there, probabilities there, their product there.
+enum { B_K_FULL = 0, B_V_FULL = 2, B_K_FREE = 4, B_V_FREE = 6, B_S_FULL = 8, B_P_FULL = 10, B_PV_DONE = 12, B_DRAIN = 14, B_COUNT };
 
-template <int D>
+// Warps of a CTA of NR row tiles: 4 NR for the rows, 4 for the values, 1 for the contractions.
+template <int NR>
+constexpr int kTileThreads = 32 * (4 * NR + 5);
+
+template <int D, int NR>
 struct TileLayout {
     static constexpr int ATOM = 128 * 128;                 // 128 rows of 64 f16
-    static constexpr int Q = 0;                            // [D / 64] atoms: rows x channels
-    static constexpr int K = Q + D / 64 * ATOM;            // [D / 64] atoms: keys x channels
-    static constexpr int V = K + D / 64 * ATOM;            // [2] halves of the keys: D channels x 64 keys
-    static constexpr int BAR = V + 2 * D * 128;
+    static constexpr int STAGES = NR;                      // of K and V
+    static constexpr int ROWS = D / 64 * ATOM;             // a row tile, or a stage of K: [D / 64] atoms
+    static constexpr int VALUES = 2 * D * 128;             // a stage of V: [2] halves of the keys, D channels x 64 keys
+    static constexpr int Q = 0;
+    static constexpr int K = Q + NR * ROWS;
+    static constexpr int V = K + STAGES * ROWS;
+    static constexpr int BAR = V + STAGES * VALUES;
     static constexpr int MISC = BAR + 8 * B_COUNT;
-    static_assert(128 * (D + 4) * 4 + 1024 <= BAR, "the places' sums fit the operands' memory");
-    // at least 77 KB: no more than two CTAs (of 256 columns each) share an SM
-    static constexpr int NEED = MISC + 16 + 1024;
-    static constexpr int ALLOC = NEED > 77 * 1024 ? NEED : 77 * 1024;
+    static_assert(NR > 1 || 128 * (D + 4) * 4 + 1024 <= BAR, "the places' sums fit the operands' memory");
+    // at least 77 KB (115): no more than two CTAs of 256 columns each (one of 512) on an SM
+    static constexpr int NEED = MISC + 16 + 1024, LEAST = NR == 1 ? 77 * 1024 : 115 * 1024;
+    static constexpr int ALLOC = NEED > LEAST ? NEED : LEAST;
 };
 
 // O += P V: A from tensor memory
@@ -68,7 +77,7 @@ template <int D, bool FP8>
 __device__ __forceinline__ float stage_q(const void* q, int64_t at, bool real, uint32_t q_s, int row)
 {
     auto put = [&](int u, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {  // 8 channels
-        st_shared16(q_s + (u >> 3) * TileLayout<D>::ATOM + row * 128 + (((u & 7) ^ (row & 7)) << 4), a, b, c, d);
+        st_shared16(q_s + (u >> 3) * TileLayout<D, 1>::ATOM + row * 128 + (((u & 7) ^ (row & 7)) << 4), a, b, c, d);
     };
     if (!real) {
 #pragma unroll 4
@@ -126,10 +135,11 @@ struct VPart {
     uint32_t scale[8];
 };
 
-template <int D, bool FP8>
-__global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __grid_constant__ AttendArgs a)
+template <int D, bool FP8, int NR>
+__global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile_kernel(const __grid_constant__ AttendArgs a)
 {
-    using L = TileLayout<D>;
+    using L = TileLayout<D, NR>;
+    constexpr int SOFT = 4 * NR, MMA_WARP = SOFT + 4, ST = L::STAGES;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t base = (raw + 1023u) & ~1023u;
@@ -158,7 +168,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __gr
         // (for the launch that joins the chunks: their length, and the request's first slot)
         if (k0 == 0 && blockIdx.y == 0 && threadIdx.x == 0) a.split[b] = make_int2(chunk, (int)blockIdx.x);
     }
-    const RowTile rt = row_tile(a, b, tile, 128);
+    const RowTile rt = row_tile(a, b, tile, 128 * NR);
     if (rt.rows <= 0) return;
     const int q0 = a.q_off[b];
     const int seen = min(rt.len, rt.last0 + rt.query(rt.row0 + rt.rows - 1) + 1);
@@ -167,34 +177,39 @@ __global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __gr
     const int all_see = rt.last0 + rt.query(rt.row0);  // the last key that every row sees
     const int n_tiles = uniform(k1 > k0 ? (k1 - k0 + kTileKeys - 1) / kTileKeys : 0);
     // places of a row, and softmax warps with rows
-    const int places = rt.rows <= 32 ? 4 : (rt.rows <= 64 ? 2 : 1);
+    const int places = NR > 1 ? 1 : (rt.rows <= 32 ? 4 : (rt.rows <= 64 ? 2 : 1));
     const int live = places == 1 ? (rt.rows + 31) / 32 : 4;
+    const int row_tiles = NR > 1 ? uniform((rt.rows + 127) / 128) : 1;
 
     if (tid == 0) {
-        mbar_init(BAR(B_K_FULL), 4);
-        mbar_init(BAR(B_V_FULL), 4);
-        mbar_init(BAR(B_S_FULL), 1);
-        mbar_init(BAR(B_P_FULL), (uint32_t)live);
-        mbar_init(BAR(B_PV_DONE), 1);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(BAR(B_K_FULL + i), 4);
+            mbar_init(BAR(B_V_FULL + i), 4);
+            mbar_init(BAR(B_K_FREE + i), 1);
+            mbar_init(BAR(B_V_FREE + i), 1);
+            mbar_init(BAR(B_S_FULL + i), 1);
+            mbar_init(BAR(B_P_FULL + i), (uint32_t)max(1, min(4, live - 4 * i)));
+            mbar_init(BAR(B_PV_DONE + i), 1);
+        }
         mbar_init(BAR(B_DRAIN), 1);
         *abort_flag = 0;
         *nan_flag = 0;
         fence_mbar_init_cluster();
     }
-    if (warp == 8) {
-        tmem_alloc(smem_u32(tmem_slot), 256);
+    if (warp == MMA_WARP) {
+        tmem_alloc(smem_u32(tmem_slot), 256 * NR);
         tmem_relinquish();
     }
     // ---- the rows
-    const int place = tid & (128 / places - 1);  // the thread's row of the tile (softmax warps)
+    const int place = NR > 1 ? tid : tid & (128 / places - 1);  // the thread's row of the CTA's (softmax warps)
     const bool real = place < rt.rows;
     const int row = rt.row0 + (real ? place : 0), query = rt.query(row);
     float fac = 0.f;
-    if (tid < 128) {
+    if (tid < 128 * NR) {
         fac = a.c_log2 * stage_q<D, FP8>(a.q,
                                          (int64_t)(q0 + query) * a.q_stride +
                                              (int64_t)(h * a.group + row - query * a.group) * D,
-                                         real, base + L::Q, tid);
+                                         real, base + L::Q + (tid >> 7) * L::ROWS, tid & 127);
         fence_proxy_async_shared();
     }
     tc_fence_before();
@@ -204,10 +219,12 @@ __global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __gr
     const Ctl ctl{abort_flag, a.err, a.wait_budget};
     float m = kNoRef, l = 0.f;
 
-    if (warp < 4) {
+    const int rtile = warp >> 2;  // the softmax warps' row tile
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    if (warp < SOFT) {
         // ---------------------------------------------------------------- softmax: a row a thread
         if (warp < live) {
-            const uint32_t ts = tmem + ((uint32_t)(warp * 32) << 16), to = ts + 128;
+            const uint32_t ts = tmem + lanes + 256 * rtile, to = ts + 128;
             const int vis = min(rt.last0 + query, k1 - 1);  // the last key that the row sees here
             float* logits = a.logits ? a.logits + (((int64_t)b * a.cache.hkv + h) * a.max_rows + row) * a.logit_stride
                                      : nullptr;
@@ -230,7 +247,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __gr
                 const uint32_t gone = __ballot_sync(0xffffffffu, next_page < 0);
                 next_page = page_of(t + 1);
                 const bool check = j0 + kTileKeys > min(k1, all_see + 1) || gone != 0;
-                if (!poll_phase_warp(BAR(B_S_FULL), (uint32_t)t & 1u, ctl)) break;
+                if (!poll_phase_warp(BAR(B_S_FULL + rtile), (uint32_t)t & 1u, ctl)) break;
                 tc_fence_after();
                 // columns of a chunk of 32 that the row sees, as a mask
                 auto mask_of = [&](int c0) -> uint32_t {
@@ -240,21 +257,29 @@ __global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __gr
                     if (gone >> (c0 / 16 + 1) & 1u) k &= 0x0000FFFFu;
                     return k;
                 };
+                // the place's columns, STEP at a time from the last on, read for their maximum; the
+                // first STEP are still there when the exponentials are made
+                constexpr int STEP = NR > 1 ? 64 : 32;
                 float mx = -INFINITY;
-                float v[32];
+                float v[STEP];
+                auto mask = [&](int c0, float* x) {
+                    const uint32_t k = mask_of(c0);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) x[i] = k >> i & 1u ? x[i] : -INFINITY;
+                };
                 auto read = [&](int c0) {
-                    tmem_ld32(ts + c0, v);
+#pragma unroll
+                    for (int x = 0; x < STEP; x += 32) tmem_ld32(ts + c0 + x, v + x);
                     tmem_wait_ld();
                     if (check) {
-                        const uint32_t k = mask_of(c0);
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] = k >> i & 1u ? v[i] : -INFINITY;
+                        for (int x = 0; x < STEP; x += 32) mask(c0 + x, v + x);
                     }
                 };
 #pragma unroll 1
-                for (int c0 = first; c0 < end; c0 += 32) {
+                for (int c0 = end - STEP; c0 >= first; c0 -= STEP) {
                     read(c0);
-                    mx = fmaxf(mx, row_max<32>(v));
+                    mx = fmaxf(mx, row_max<STEP>(v));
                 }
                 mx *= fac;  // (fac > 0)
                 if (__any_sync(0xffffffffu, mx > m + kRefSlack)) {
@@ -277,21 +302,19 @@ __global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __gr
                 }
                 const float2 nm2 = make_float2(-m, -m);
                 float2 s0 = make_float2(0.f, 0.f), s1 = make_float2(0.f, 0.f);
-#pragma unroll 1
-                for (int c0 = first; c0 < end; c0 += 32) {
-                    if (own > 32) read(c0);  // (a place of 32 columns still has them)
+                auto chunk_of = [&](int c0, const float* x) {
                     if (logits && real && j0 + c0 < k1) {
                         float4* out = reinterpret_cast<float4*>(logits + j0 + c0);
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
-                            __stcg(out + i, make_float4(v[4 * i] * fac, v[4 * i + 1] * fac, v[4 * i + 2] * fac,
-                                                        v[4 * i + 3] * fac));
+                            __stcg(out + i, make_float4(x[4 * i] * fac, x[4 * i + 1] * fac, x[4 * i + 2] * fac,
+                                                        x[4 * i + 3] * fac));
                     }
                     float p[16];
 #pragma unroll
                     for (int i = 0; i < 32; i += 4) {
-                        const float2 x0 = ffma2(make_float2(v[i], v[i + 1]), fac2, nm2);
-                        const float2 x1 = ffma2(make_float2(v[i + 2], v[i + 3]), fac2, nm2);
+                        const float2 x0 = ffma2(make_float2(x[i], x[i + 1]), fac2, nm2);
+                        const float2 x1 = ffma2(make_float2(x[i + 2], x[i + 3]), fac2, nm2);
                         const float2 p0 = make_float2(ex2(x0.x), ex2(x0.y)), p1 = make_float2(ex2(x1.x), ex2(x1.y));
                         s0 = fadd2(s0, p0);
                         s1 = fadd2(s1, p1);
@@ -299,6 +322,13 @@ __global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __gr
                         p[i / 2 + 1] = __uint_as_float(pack_h2(p1.x, p1.y));
                     }
                     tmem_st16(ts + c0 / 2, p);
+                };
+                // (P of columns c is written to the columns from c / 2 on, which have been read)
+#pragma unroll 1
+                for (int c0 = first; c0 < end; c0 += STEP) {
+                    if (c0 > first) read(c0);
+#pragma unroll
+                    for (int x = 0; x < STEP; x += 32) chunk_of(c0 + x, v + x);
                 }
                 l += (s0.x + s0.y) + (s1.x + s1.y);
                 if (places > 1) {
@@ -309,12 +339,12 @@ __global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __gr
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(BAR(B_P_FULL));
+                if (lane == 0) mbar_arrive(BAR(B_P_FULL + rtile));
             }
         }
-    } else if (warp < 8) {
+    } else if (warp < MMA_WARP) {
         // ---------------------------------------------------------------- codes to values
-        const int w = warp - 4;
+        const int w = warp - SOFT;
         const CachePages& C = a.cache;
         const int smask = (1 << C.page_shift) - 1;
         // K: channels [c * D/4, ..) of the keys w * 32 + (lane & 7) + 8 i; V: keys kg * 8 .., block vb:
@@ -323,7 +353,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __gr
         // odd blocks take their channels 4 to 7 first (their words are turned by half).
         const int c = lane >> 3, kr = w * 32 + (lane & 7);
         const int kg = 4 * w + (lane & 3), vb = lane >> 2, turn = (vb & 1) * 4;
-        const uint32_t v_at = base + L::V + (kg >> 3) * (D * 128) + vb * 16 * 128;
+        const uint32_t v_at = (kg >> 3) * (D * 128) + vb * 16 * 128;
         const uint32_t v_x = (uint32_t)(turn << 7 | ((kg & 7) ^ turn) << 4);
         const bool v_part = vb < D / 16;
         auto page_at = [&](int j) -> int32_t {
@@ -384,7 +414,11 @@ __global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __gr
         for (int t = 0; t < n_tiles; ++t) {
             const int j0 = k0 + t * kTileKeys, jn = j0 + kTileKeys;
             const bool more = t + 1 < n_tiles;
-            if (t > 0 && !poll_phase_warp(BAR(B_S_FULL), (uint32_t)(t - 1) & 1u, ctl)) break;  // K is free
+            // the stage, and the parity of its last use's end
+            const int st = t % ST;
+            const uint32_t past = (uint32_t)(t / ST - 1) & 1u, k_s = base + L::K + st * L::ROWS;
+            const uint32_t v_s = base + L::V + st * L::VALUES;
+            if (t >= ST && !poll_phase_warp(BAR(B_K_FREE + st), past, ctl)) break;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int key = kr + 8 * i;
@@ -397,19 +431,19 @@ __global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __gr
                     e2m1x8_value(words[q], x);
                     const __half2 s = sb[q / 2];
                     const int u = c * (D / 32) + q;
-                    st_shared16(base + L::K + (u >> 3) * L::ATOM + key * 128 + (((u & 7) ^ (key & 7)) << 4),
+                    st_shared16(k_s + (u >> 3) * L::ATOM + key * 128 + (((u & 7) ^ (key & 7)) << 4),
                                 h2_bits(__hmul2(x[0], s)), h2_bits(__hmul2(x[1], s)), h2_bits(__hmul2(x[2], s)),
                                 h2_bits(__hmul2(x[3], s)));
                 }
             }
             fence_proxy_async_shared();
             __syncwarp();
-            if (lane == 0) mbar_arrive(BAR(B_K_FULL));
+            if (lane == 0) mbar_arrive(BAR(B_K_FULL + st));
             if (more) {
                 report_pages(jn);
                 load_k(kp, pk0, pk1, jn);
             }
-            if (t > 0 && !poll_phase_warp(BAR(B_PV_DONE), (uint32_t)(t - 1) & 1u, ctl)) break;  // V is free
+            if (t >= ST && !poll_phase_warp(BAR(B_V_FREE + st), past, ctl)) break;
             if (v_part) {
                 if (j0 + kTileKeys - 1 > all_see) {
 #pragma unroll
@@ -445,47 +479,64 @@ __global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __gr
                         uint32_t f[4];
 #pragma unroll
                         for (int p = 0; p < 4; ++p) f[p] = h2_bits(__hmul2(i & 1 ? od[p][i / 2] : ev[p][i / 2], s[p]));
-                        st_shared16(v_at + q * 1024 + ((uint32_t)(i << 7 | i << 4) ^ v_x), f[0], f[1], f[2], f[3]);
+                        st_shared16(v_s + v_at + q * 1024 + ((uint32_t)(i << 7 | i << 4) ^ v_x), f[0], f[1], f[2], f[3]);
                     }
                 }
             }
             fence_proxy_async_shared();
             __syncwarp();
-            if (lane == 0) mbar_arrive(BAR(B_V_FULL));
+            if (lane == 0) mbar_arrive(BAR(B_V_FULL + st));
             if (more) load_v(vp, pv, jn);
             pages(jn + kTileKeys);
         }
     } else {
         // ---------------------------------------------------------------- contractions
+        // S of row tile r and key tile t, into the place of its last P: behind the product that read it
         const uint32_t idesc_s = idesc_make(128, kTileKeys, 0u), idesc_o = idesc_make(128, D, 0u);
-        for (int t = 0; t < n_tiles; ++t) {
-            const uint32_t ph = (uint32_t)t & 1u;
-            if (!poll_phase_warp(BAR(B_K_FULL), ph, ctl)) break;
-            // S takes the place of the last tile's P
-            if (t > 0 && !poll_phase_warp(BAR(B_PV_DONE), ph ^ 1u, ctl)) break;
+        auto scores = [&](int r, int t) -> bool {
+            const int st = t % ST;
+            if (r == 0 && !poll_phase_warp(BAR(B_K_FULL + st), (uint32_t)(t / ST) & 1u, ctl)) return false;
+            if (t > 0 && !poll_phase_warp(BAR(B_PV_DONE + r), (uint32_t)(t - 1) & 1u, ctl)) return false;
             tc_fence_after();
             if (elect_one()) {
 #pragma unroll
-                for (int st = 0; st < D / 16; ++st) {
-                    const uint32_t off = (st >> 2) * L::ATOM + (st & 3) * 32;
-                    mma_f16(tmem, sdesc_k_sw128(base + L::Q + off), sdesc_k_sw128(base + L::K + off), idesc_s, st > 0);
+                for (int x = 0; x < D / 16; ++x) {
+                    const uint32_t off = (x >> 2) * L::ATOM + (x & 3) * 32;
+                    mma_f16(tmem + 256 * r, sdesc_k_sw128(base + L::Q + r * L::ROWS + off),
+                            sdesc_k_sw128(base + L::K + st * L::ROWS + off), idesc_s, x > 0);
                 }
-                mma_commit(BAR(B_S_FULL));
+                mma_commit(BAR(B_S_FULL + r));
+                if (r == row_tiles - 1) mma_commit(BAR(B_K_FREE + st));
             }
             __syncwarp();
-            if (!poll_phase_warp(BAR(B_V_FULL), ph, ctl)) break;
-            if (!poll_phase_warp(BAR(B_P_FULL), ph, ctl)) break;
+            return true;
+        };
+        // O of row tile r += P of key tile t times its values
+        auto values = [&](int r, int t) -> bool {
+            const int st = t % ST;
+            if (r == 0 && !poll_phase_warp(BAR(B_V_FULL + st), (uint32_t)(t / ST) & 1u, ctl)) return false;
+            if (!poll_phase_warp(BAR(B_P_FULL + r), (uint32_t)t & 1u, ctl)) return false;
             tc_fence_after();
             if (elect_one()) {
 #pragma unroll
-                for (int st = 0; st < kTileKeys / 16; ++st)
-                    mma_f16_ta(tmem + 128, tmem + st * 8,
-                               sdesc_k_sw128(base + L::V + (st >> 2) * (D * 128) + (st & 3) * 32), idesc_o,
-                               t > 0 || st > 0);
-                mma_commit(BAR(B_PV_DONE));
+                for (int x = 0; x < kTileKeys / 16; ++x)
+                    mma_f16_ta(tmem + 256 * r + 128, tmem + 256 * r + x * 8,
+                               sdesc_k_sw128(base + L::V + st * L::VALUES + (x >> 2) * (D * 128) + (x & 3) * 32), idesc_o,
+                               t > 0 || x > 0);
+                mma_commit(BAR(B_PV_DONE + r));
+                if (r == row_tiles - 1) mma_commit(BAR(B_V_FREE + st));
             }
             __syncwarp();
-        }
+            return true;
+        };
+        // while one row tile's scores become probabilities, the other's contractions run
+        bool ok = true;
+        for (int r = 0; r < row_tiles && n_tiles > 0 && ok; ++r) ok = scores(r, 0);
+        for (int t = 0; t < n_tiles && ok; ++t)
+            for (int r = 0; r < row_tiles && ok; ++r) {
+                ok = values(r, t);
+                if (ok && t + 1 < n_tiles) ok = scores(r, t + 1);
+            }
         // every contraction issued has ended before tensor memory is read or released, also where
         // a wait gave up
         if (elect_one()) mma_commit(BAR(B_DRAIN));
@@ -510,8 +561,8 @@ __global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __gr
         }
         return false;
     };
-    const uint32_t to = tmem + ((uint32_t)((warp & 3) * 32) << 16) + 128;
-    if (places == 1 && warp < live && done) {
+    const uint32_t to = tmem + lanes + 256 * (NR > 1 ? rtile : 0) + 128;
+    if (places == 1 && warp < live && done) {  // (live <= 4 NR)
         const int64_t at = (int64_t)(q0 + query) * a.hq + h * a.group + row - query * a.group;
         const int64_t part = ((int64_t)blockIdx.x * a.cache.hkv + h) * a.max_rows + row;
         const float f = a.slots > 0 ? 1.f : (l == 0.f ? 0.f : a.cache.scale[1] / l);
@@ -576,7 +627,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __gr
         }
         __syncthreads();
         const int step = 128 / places;  // from a place of a row to the next
-        for (int x = tid; x < rt.rows * D; x += kTileThreads) {
+        for (int x = tid; x < rt.rows * D; x += kTileThreads<NR>) {
             const int r = x / D, ch = x % D;
             float M = kNoRef, L = 0.f, O = 0.f;
             for (int p = 0; p < places; ++p) M = fmaxf(M, refs[r + p * step]);
@@ -600,23 +651,23 @@ __global__ void __launch_bounds__(kTileThreads, 2) attend_tile_kernel(const __gr
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 8) {
+    if (warp == MMA_WARP) {
         tc_fence_after();
-        tmem_dealloc(tmem, 256);
+        tmem_dealloc(tmem, 256 * NR);
     }
 }
 
-template <int D, bool FP8>
+template <int D, bool FP8, int NR>
 cudaError_t launch_variant(const AttendArgs& a, int tiles, cudaStream_t stream)
 {
-    using L = TileLayout<D>;
-    auto kern = attend_tile_kernel<D, FP8>;
+    using L = TileLayout<D, NR>;
+    auto kern = attend_tile_kernel<D, FP8, NR>;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, L::ALLOC);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = a.slots > 0 ? dim3((unsigned)a.slots, (unsigned)(tiles * a.cache.hkv), 1)
                               : dim3(1, (unsigned)(tiles * a.cache.hkv), (unsigned)a.batch);
-    cfg.blockDim = dim3(kTileThreads, 1, 1);
+    cfg.blockDim = dim3(kTileThreads<NR>, 1, 1);
     cfg.dynamicSmemBytes = L::ALLOC;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1] = {pdl_attribute()};
@@ -627,10 +678,16 @@ cudaError_t launch_variant(const AttendArgs& a, int tiles, cudaStream_t stream)
 
 }  // namespace
 
-cudaError_t launch_attend_tiles(const AttendArgs& a, int head_dim, bool fp8, int tiles, cudaStream_t stream)
+cudaError_t launch_attend_tiles(const AttendArgs& a, int head_dim, bool fp8, int row_tile, int tiles, cudaStream_t stream)
 {
-    if (fp8) return launch_variant<128, true>(a, tiles, stream);
-    return head_dim == 128 ? launch_variant<128, false>(a, tiles, stream) : launch_variant<64, false>(a, tiles, stream);
+    if (row_tile == 256) {
+        if (fp8) return launch_variant<128, true, 2>(a, tiles, stream);
+        return head_dim == 128 ? launch_variant<128, false, 2>(a, tiles, stream)
+                               : launch_variant<64, false, 2>(a, tiles, stream);
+    }
+    if (fp8) return launch_variant<128, true, 1>(a, tiles, stream);
+    return head_dim == 128 ? launch_variant<128, false, 1>(a, tiles, stream)
+                           : launch_variant<64, false, 1>(a, tiles, stream);
 }
 
 }  // namespace lvs

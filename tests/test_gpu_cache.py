@@ -180,6 +180,9 @@ CASES = [
     (2, 2, 64, 16, "bf16", [5000], [1]),                   # many chunks
     (4, 2, 128, 16, "e4m3", [2100, 5], [33, 5]),
     (12, 12, 64, 32, "bf16", [260], [70]),
+    (16, 2, 64, 32, "bf16", [600, 1300, 45], [30, 2, 45]),  # 240 rows: two row tiles, the second of them in part
+    (7, 1, 128, 16, "e4m3", [900, 300], [90, 1]),
+    (8, 2, 128, 256, "bf16", [400, 20, 129], [16, 9, 12]),  # 36 to 64 rows: places of their own
 ]
 
 
