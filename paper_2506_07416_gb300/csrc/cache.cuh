@@ -19,12 +19,6 @@ namespace lvs {
 __device__ __forceinline__ uint32_t h2_bits(__half2 h) { return *reinterpret_cast<uint32_t*>(&h); }
 __device__ __forceinline__ __half2 bits_h2(uint32_t u) { return *reinterpret_cast<__half2*>(&u); }
 
-// Values of two codes in the low byte of w, the low four bits first.
-__device__ __forceinline__ __half2 e2m1x2_value(uint32_t w)
-{
-    return __half2(__nv_cvt_fp4x2_to_halfraw2((__nv_fp4x2_storage_t)w, __NV_E2M1));
-}
-
 // Values of the eight codes of w, byte by byte. The bytes are named to the
 // assembler, which then converts them in place: 50 pairs a clock and SM where
 // shifting each byte down first made it 24, and building f16 from the bits by

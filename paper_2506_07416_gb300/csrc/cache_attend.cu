@@ -207,15 +207,12 @@ __global__ void __launch_bounds__(kAttThreads) attend_split_kernel(const __grid_
     constexpr int NT = SINGLE ? 1 : NT_;
     using G = Group<D>;
     constexpr int ROWS = 8 * NT;
-    constexpr bool Q_SMEM = NT > 2;  // fragments of 32 rows would take 64 registers
     constexpr int MT = D / 16;
     // the rings; behind the loop the same memory takes a row tile of every warp's sums
     constexpr int kRing = kRingBytes<D>, kJoin = kAttWarps * 8 * (D + 4) * 4;
     static_assert(kRing >= kJoin, "the sums fit the rings");
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ float s_m[kAttWarps][ROWS], s_l[kAttWarps][ROWS];
-    __shared__ uint2 q_s[Q_SMEM ? NT * (D / 16) * 32 : 1];
-    __shared__ float back_s[Q_SMEM ? ROWS : 1];
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int g = lane >> 2, c = lane & 3;
@@ -272,7 +269,7 @@ __global__ void __launch_bounds__(kAttThreads) attend_split_kernel(const __grid_
     int32_t next_page = page_of(kAttStages - 1);  // (read a span ahead: nothing waits for the table)
 
     // ---- the tile's rows
-    uint32_t qr[Q_SMEM ? 1 : NT][D / 8];
+    uint32_t qr[NT][D / 8];
     float fac[NT][2];  // log2-unit scale of rows 2c and 2c + 1
     int vis[NT][2];    // last key they see
 #pragma unroll
@@ -284,38 +281,19 @@ __global__ void __launch_bounds__(kAttThreads) attend_split_kernel(const __grid_
         const int64_t at =
             (int64_t)(q0 + i) * a.q_stride + (int64_t)(h * a.group + row - i * a.group) * D + c * (D / 4);
         float back;
-        if constexpr (Q_SMEM) {
-            if (t % kAttWarps == warp) {
-                uint32_t f[D / 8];
-                load_q<D, FP8>(a.q, at, real, f, back);
+        load_q<D, FP8>(a.q, at, SINGLE || real, qr[t], back);
+        if constexpr (SINGLE) {  // (every lane has read row 0; lane (g, c) keeps what lies in block g)
 #pragma unroll
-                for (int k = 0; k < D / 16; ++k) q_s[(t * (D / 16) + k) * 32 + lane] = make_uint2(f[2 * k], f[2 * k + 1]);
-                if (c == 0) back_s[r] = back;
-            }
-        } else {
-            load_q<D, FP8>(a.q, at, SINGLE || real, qr[t], back);
-            if constexpr (SINGLE) {  // (every lane has read row 0; lane (g, c) keeps what lies in block g)
-#pragma unroll
-                for (int k = 0; k < D / 8; ++k)
-                    if (D == 128 ? g != 2 * c + k / 8 : g != c) qr[0][k] = 0u;
-            }
-            fac[t][0] = a.c_log2 * __shfl_sync(0xffffffffu, back, 8 * c);
-            fac[t][1] = a.c_log2 * __shfl_sync(0xffffffffu, back, 8 * c + 4);
+            for (int k = 0; k < D / 8; ++k)
+                if (D == 128 ? g != 2 * c + k / 8 : g != c) qr[0][k] = 0u;
         }
+        fac[t][0] = a.c_log2 * __shfl_sync(0xffffffffu, back, 8 * c);
+        fac[t][1] = a.c_log2 * __shfl_sync(0xffffffffu, back, 8 * c + 4);
 #pragma unroll
         for (int e = 0; e < 2; ++e) vis[t][e] = rt.last0 + rt.query(rt.row0 + t * 8 + 2 * c + e);
     }
-    if constexpr (Q_SMEM) {
-        __syncthreads();
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            fac[t][0] = a.c_log2 * back_s[t * 8 + 2 * c];
-            fac[t][1] = a.c_log2 * back_s[t * 8 + 2 * c + 1];
-        }
-    }
     auto qf = [&](int t, int k) -> uint2 {
-        if constexpr (Q_SMEM) return q_s[(t * (D / 16) + k) * 32 + lane];
-        else return make_uint2(qr[t][2 * k], qr[t][2 * k + 1]);
+        return make_uint2(qr[t][2 * k], qr[t][2 * k + 1]);
     };
 
     float o[NT][MT][4], m[NT][2], l[NT][2];
@@ -1034,9 +1012,9 @@ AttendPlan plan_cache_attend(int batch, int hkv, int group, const int32_t* q_off
     for (int b = 0; b < batch; ++b)
         items += ((int64_t)(q_off[b + 1] - q_off[b]) * group + p.row_tile - 1) / p.row_tile * hkv;
     // The keys are split into n chunks a request where that fills the GPU better: items * n CTAs of
-    // 1/n of the work run in rounds of as many as fit at once (four on an SM, two of the kernel for
-    // many rows), and every chunk costs the writing and joining of its sums, about a twentieth of
-    // a round.
+    // 1/n of the work run in rounds of as many as fit at once (by the kernels' registers and tensor
+    // memory), and the writing and joining of a chunk's sums takes a CTA as long as about five
+    // keys for every four rows.
     const int64_t places = (int64_t)num_sms * (p.row_tile == 256 ? 1 : (p.row_tile == 128 ? 2 : (p.row_tile == 16 ? 3 : 4)));
     const int rounds = p.row_tile == 16 && batch > 1 ? 3 : 1;
     const int64_t units = std::max<int64_t>(1, (max_len + 63) / 64);
@@ -1046,7 +1024,8 @@ AttendPlan plan_cache_attend(int batch, int hkv, int group, const int32_t* q_off
     } else if (items < 3 * places) {  // (from three rounds on the last one's idle places matter little)
         double cost = 1e30;
         for (int64_t n = 1; n <= std::min<int64_t>(units, 8); ++n) {
-            const double c = (double)((items * n + places - 1) / places) / (double)n + (n > 1 ? 0.05 * n : 0.0);
+            const double r = (double)((items * n + places - 1) / places);
+            const double c = r / (double)n + (n > 1 ? r * 1.25 * p.row_tile / (double)std::max<int64_t>(max_len, 1) : 0.0);
             if (c < cost) cost = c, best = n;
         }
     }

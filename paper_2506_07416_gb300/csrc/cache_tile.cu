@@ -11,10 +11,6 @@
 //   warps 0-3 hold a row a thread: they read S twice (its largest score, then the
 //     exponentials), write P as f16 over S, and keep the row's reference and sum. A
 //     reference moves only when a score passes it by 8; O is then rescaled in place.
-// Of 64 rows or fewer (32) every row stands in two (four) of the 128 places, and each place
-// takes a half (a quarter) of the tile's keys, with zeros for the others in its P: the
-// exponentials of a few rows are then made by four warps and not by one. The places of a
-// row are added up at the end, as the chunks are.
 // What bounds it: an SM makes 16 exponentials a clock, a tile of 128 x 128 takes 1024
 // clocks of them, against 512 of contractions, so two CTAs share an SM: while one waits
 // for a contraction the other computes. That needs 256 columns and at most 113 KB each, so
@@ -47,7 +43,6 @@ struct TileLayout {
     static constexpr int V = K + STAGES * ROWS;
     static constexpr int BAR = V + STAGES * VALUES;
     static constexpr int MISC = BAR + 8 * B_COUNT;
-    static_assert(NR > 1 || 128 * (D + 4) * 4 + 1024 <= BAR, "the places' sums fit the operands' memory");
     // at least 77 KB (115): no more than two CTAs of 256 columns each (one of 512) on an SM
     static constexpr int NEED = MISC + 16 + 1024, LEAST = NR == 1 ? 77 * 1024 : 115 * 1024;
     static constexpr int ALLOC = NEED > LEAST ? NEED : LEAST;
@@ -176,9 +171,7 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
     if (k0 >= k1 && a.slots > 0) return;  // (without chunks the tile's zeros are written here, else by the join)
     const int all_see = rt.last0 + rt.query(rt.row0);  // the last key that every row sees
     const int n_tiles = uniform(k1 > k0 ? (k1 - k0 + kTileKeys - 1) / kTileKeys : 0);
-    // places of a row, and softmax warps with rows
-    const int places = NR > 1 ? 1 : (rt.rows <= 32 ? 4 : (rt.rows <= 64 ? 2 : 1));
-    const int live = places == 1 ? (rt.rows + 31) / 32 : 4;
+    const int live = (rt.rows + 31) / 32;  // softmax warps with rows
     const int row_tiles = NR > 1 ? uniform((rt.rows + 127) / 128) : 1;
 
     if (tid == 0) {
@@ -201,9 +194,8 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
         tmem_relinquish();
     }
     // ---- the rows
-    const int place = NR > 1 ? tid : tid & (128 / places - 1);  // the thread's row of the CTA's (softmax warps)
-    const bool real = place < rt.rows;
-    const int row = rt.row0 + (real ? place : 0), query = rt.query(row);
+    const bool real = tid < rt.rows;  // (the softmax warps' threads)
+    const int row = rt.row0 + (real ? tid : 0), query = rt.query(row);
     float fac = 0.f;
     if (tid < 128 * NR) {
         fac = a.c_log2 * stage_q<D, FP8>(a.q,
@@ -229,11 +221,6 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
             float* logits = a.logits ? a.logits + (((int64_t)b * a.cache.hkv + h) * a.max_rows + row) * a.logit_stride
                                      : nullptr;
             const float2 fac2 = make_float2(fac, fac);
-            // the columns of this place
-            const int own = kTileKeys / places, first = uniform((tid & 127) / own * own * (places > 1)), end = first + own;
-            float zero[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) zero[i] = 0.f;
             // page of a tile's group of 16 keys (lanes 0 to 7); groups without one are as masked
             auto page_of = [&](int t) -> int32_t {
                 const int j = k0 + t * kTileKeys + lane * 16;
@@ -257,8 +244,8 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
                     if (gone >> (c0 / 16 + 1) & 1u) k &= 0x0000FFFFu;
                     return k;
                 };
-                // the place's columns, STEP at a time from the last on, read for their maximum; the
-                // first STEP are still there when the exponentials are made
+                // the columns, STEP at a time from the last on, read for their maximum; the first STEP
+                // are still there when the exponentials are made
                 constexpr int STEP = NR > 1 ? 64 : 32;
                 float mx = -INFINITY;
                 float v[STEP];
@@ -277,7 +264,7 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
                     }
                 };
 #pragma unroll 1
-                for (int c0 = end - STEP; c0 >= first; c0 -= STEP) {
+                for (int c0 = kTileKeys - STEP; c0 >= 0; c0 -= STEP) {
                     read(c0);
                     mx = fmaxf(mx, row_max<STEP>(v));
                 }
@@ -325,17 +312,12 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
                 };
                 // (P of columns c is written to the columns from c / 2 on, which have been read)
 #pragma unroll 1
-                for (int c0 = first; c0 < end; c0 += STEP) {
-                    if (c0 > first) read(c0);
+                for (int c0 = 0; c0 < kTileKeys; c0 += STEP) {
+                    if (c0 > 0) read(c0);
 #pragma unroll
                     for (int x = 0; x < STEP; x += 32) chunk_of(c0 + x, v + x);
                 }
                 l += (s0.x + s0.y) + (s1.x + s1.y);
-                if (places > 1) {
-#pragma unroll 1
-                    for (int c0 = 0; c0 < kTileKeys; c0 += 32)
-                        if (c0 < first || c0 >= end) tmem_st16(ts + c0 / 2, zero);
-                }
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
@@ -550,7 +532,6 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
     tc_fence_after();
 
     // ---- the rows' results
-    const bool done = !*abort_flag;
     // values that are NaN, for the rows that see them: whether block x of 16 channels has one
     auto nan_block = [&](int x, int i) -> bool {
         for (int j = max(k0, all_see + 1); j < min(k1, rt.last0 + i + 1); ++j) {
@@ -562,7 +543,7 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
         return false;
     };
     const uint32_t to = tmem + lanes + 256 * (NR > 1 ? rtile : 0) + 128;
-    if (places == 1 && warp < live && done) {  // (live <= 4 NR)
+    if (warp < live && !*abort_flag) {  // (live <= 4 NR)
         const int64_t at = (int64_t)(q0 + query) * a.hq + h * a.group + row - query * a.group;
         const int64_t part = ((int64_t)blockIdx.x * a.cache.hkv + h) * a.max_rows + row;
         const float f = a.slots > 0 ? 1.f : (l == 0.f ? 0.f : a.cache.scale[1] / l);
@@ -601,53 +582,6 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
         }
         if (real && a.slots > 0) a.part_ml[part] = make_float2(m, l);
         if (real && a.slots == 0 && a.lse) a.lse[at] = l == 0.f ? INFINITY : m + log2f(l);
-    }
-    if (places > 1 && done) {
-        // the operands' memory is free: the places' sums [128][D + 4], references and sums of 2^s
-        float* sums = reinterpret_cast<float*>(smem);
-        float* refs = sums + 128 * (D + 4);
-        if (warp < 4) {
-#pragma unroll 1
-            for (int c0 = 0; c0 < D; c0 += 16) {
-                float v[16];
-                if (n_tiles > 0) {
-                    tmem_ld16(to + c0, v);
-                    tmem_wait_ld();
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) v[i] = 0.f;
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    *reinterpret_cast<float4*>(sums + tid * (D + 4) + c0 + 4 * i) =
-                        make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-            }
-            refs[tid] = m;
-            refs[128 + tid] = l;
-        }
-        __syncthreads();
-        const int step = 128 / places;  // from a place of a row to the next
-        for (int x = tid; x < rt.rows * D; x += kTileThreads<NR>) {
-            const int r = x / D, ch = x % D;
-            float M = kNoRef, L = 0.f, O = 0.f;
-            for (int p = 0; p < places; ++p) M = fmaxf(M, refs[r + p * step]);
-            for (int p = 0; p < places; ++p) {
-                const float f = ex2(refs[r + p * step] - M);
-                L += refs[128 + r + p * step] * f;
-                O += sums[(r + p * step) * (D + 4) + ch] * f;
-            }
-            const int rr = rt.row0 + r, i = rt.query(rr);
-            if (*nan_flag && nan_block(ch / 16, i)) O = __int_as_float(0x7FC00000);
-            if (a.slots > 0) {
-                const int64_t part = ((int64_t)blockIdx.x * a.cache.hkv + h) * a.max_rows + rr;
-                __stcg(a.part_o + part * D + ch, O);
-                if (ch == 0) a.part_ml[part] = make_float2(M, L);
-            } else {
-                const int64_t at = (int64_t)(q0 + i) * a.hq + h * a.group + rr - i * a.group;
-                a.out[at * D + ch] = __float2bfloat16_rn(L == 0.f ? 0.f : O / L * a.cache.scale[1]);
-                if (a.lse && ch == 0) a.lse[at] = L == 0.f ? INFINITY : M + log2f(L);
-            }
-        }
     }
     tc_fence_before();
     __syncthreads();

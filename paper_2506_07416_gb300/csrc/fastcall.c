@@ -369,6 +369,48 @@ done:
     return PyBool_FromLong(ok);
 }
 
+/* row_stride(tensor, dtype, device index, heads, d): elements from a row to the next of [rows, heads, d] rows whose heads
+ * and channels lie side by side, on this CUDA device; -1 for anything else */
+static PyObject *g_stride;
+static PyObject *f_row_stride(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    (void)self;
+    if (n != 5) {
+        PyErr_SetString(PyExc_TypeError, "row_stride takes five arguments");
+        return NULL;
+    }
+    long long stride = -1;
+    PyObject *t = args[0], *shape = NULL, *strides = NULL, *r = PyObject_GetAttr(t, g_dtype);
+    if (!r) goto done;
+    Py_DECREF(r);
+    if (r != args[1]) goto done;
+    r = PyObject_CallMethodNoArgs(t, g_get_device);
+    if (!r) goto done;
+    const int here = PyLong_Check(r) && PyLong_AsLong(r) == PyLong_AsLong(args[2]);
+    Py_DECREF(r);
+    if (!here) goto done;
+    shape = PyObject_GetAttr(t, g_shape);
+    strides = shape ? PyObject_CallMethodNoArgs(t, g_stride) : NULL;
+    if (strides && PyTuple_Check(shape) && PyTuple_GET_SIZE(shape) == 3 && PyTuple_Check(strides) &&
+        PyTuple_GET_SIZE(strides) == 3) {
+        long long v[6];
+        for (int k = 0; k < 3; ++k) {
+            v[k] = PyLong_AsLongLong(PyTuple_GET_ITEM(shape, k));
+            v[3 + k] = PyLong_AsLongLong(PyTuple_GET_ITEM(strides, k));
+        }
+        const long long heads = PyLong_AsLongLong(args[3]), d = PyLong_AsLongLong(args[4]);
+        if (v[1] == heads && v[2] == d && v[5] == 1 && (heads == 1 || v[4] == d)) stride = v[0] > 1 ? v[3] : heads * d;
+    }
+done:
+    Py_XDECREF(shape);
+    Py_XDECREF(strides);
+    if (PyErr_Occurred()) { /* no tensor: the caller says what is wrong */
+        PyErr_Clear();
+        stride = -1;
+    }
+    return PyLong_FromLongLong(stride);
+}
+
 /* compact(handle, total_kept, kept_idx, src_rows, srcs, dsts, row_bytes, stream): the three are lists */
 static PyObject *f_compact(PyObject *self, PyObject *const *args, Py_ssize_t n)
 {
@@ -474,7 +516,7 @@ static PyMethodDef kMethods[] = {DEF("bind", f_bind), DEF("score", f_score), DEF
                                  DEF("keep_total", f_keep_total), DEF("cache_append", f_append),
                                  DEF("cache_attend", f_attend), DEF("attend_bytes", f_attend_bytes),
                                  DEF("cache_evict", f_evict), DEF("verify", f_verify),
-                                 DEF("fits", f_fits), {NULL, NULL, 0, NULL}};
+                                 DEF("fits", f_fits), DEF("row_stride", f_row_stride), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_fastcall", NULL, -1, kMethods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__fastcall(void)
@@ -484,5 +526,6 @@ PyMODINIT_FUNC PyInit__fastcall(void)
     g_get_device = PyUnicode_InternFromString("get_device");
     g_shape = PyUnicode_InternFromString("shape");
     g_is_contiguous = PyUnicode_InternFromString("is_contiguous");
-    return g_data_ptr && g_dtype && g_get_device && g_shape && g_is_contiguous ? PyModule_Create(&kModule) : NULL;
+    g_stride = PyUnicode_InternFromString("stride");
+    return g_data_ptr && g_stride && g_dtype && g_get_device && g_shape && g_is_contiguous ? PyModule_Create(&kModule) : NULL;
 }

@@ -424,15 +424,15 @@ def _want(name: str, t, dtype, shape, device: int):
 
 def _row_stride(name: str, t, dtype, heads: int, d: int, device: int) -> int:
     """Elements from a row to the next of [rows, heads, d] rows, whose channels and heads lie side by side."""
+    stride = _FC.row_stride(t, dtype, device, heads, d)
+    if stride >= 0:
+        return stride
     import torch
     if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device.type != "cuda" or t.device.index != device:
         _refuse(f"{name} must be a {dtype} tensor on cuda:{device}")
     if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != d:
         _refuse(f"{name} must have the shape (any, {heads}, {d}), not {tuple(t.shape)}")
-    stride = t.stride()
-    if stride[2] != 1 or (heads > 1 and stride[1] != d):
-        _refuse(f"{name}'s heads and channels must lie side by side (only the row stride is free)")
-    return stride[0] if t.shape[0] > 1 else heads * d
+    _refuse(f"{name}'s heads and channels must lie side by side (only the row stride is free)")
 
 
 class KVCache:
