@@ -461,12 +461,16 @@ litevlm_status_t litevlm_select_set_wait_budget(litevlm_select_t handle, int64_t
  * second CTA stop after three stages in the same way, so that the launch gives
  * up with copies and contractions in flight and its CTAs at different stages;
  * rows are invalid, and check_device reports LITEVLM_ERR_TIMEOUT.
+ * LITEVLM_DEBUG_STALL_ATTEND: in the launches of litevlm_select_cache_attend for many
+ * rows (more than 32 a key head), the values of the second 128 keys (the only ones) are never made,
+ * so that the launch gives up with contractions in flight; the same report.
  * Nothing faults, traps or hangs: each wait is bounded by the budget. flags = 0
  * restores normal operation. Errors: INVALID_ARG for a NULL handle or an
  * unknown flag.
  */
 #define LITEVLM_DEBUG_STALL_SCORE 1
 #define LITEVLM_DEBUG_STALL_PROJECT 4
+#define LITEVLM_DEBUG_STALL_ATTEND 8
 litevlm_status_t litevlm_select_set_debug_flags(litevlm_select_t handle, int32_t flags);
 
 /*

@@ -1222,7 +1222,8 @@ litevlm_status_t litevlm_select_set_debug_flags(litevlm_select_t h, int32_t flag
     const CallRange range_(__func__);
     if (!h) return LITEVLM_ERR_INVALID_ARG;
     h->last_error.clear();
-    if (flags & ~(LITEVLM_DEBUG_STALL_SCORE | LITEVLM_DEBUG_STALL_PROJECT)) return fail(h, LITEVLM_ERR_INVALID_ARG, "unknown debug flag");
+    if (flags & ~(LITEVLM_DEBUG_STALL_SCORE | LITEVLM_DEBUG_STALL_PROJECT | LITEVLM_DEBUG_STALL_ATTEND))
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "unknown debug flag");
     h->debug_flags = flags;
     return LITEVLM_OK;
 }
@@ -1512,6 +1513,7 @@ litevlm_status_t litevlm_select_cache_attend(litevlm_select_t h, int32_t batch, 
     a.weights_in = weights_in;
     a.weights_out = weights_out;
     a.err = h->err_d;
+    a.stall = (h->debug_flags & LITEVLM_DEBUG_STALL_ATTEND) != 0;
     a.wait_budget = h->wait_budget;
     const OnDevice on(h->device);
     cudaError_t e = on.e;

@@ -396,6 +396,7 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
         for (int t = 0; t < n_tiles; ++t) {
             const int j0 = k0 + t * kTileKeys, jn = j0 + kTileKeys;
             const bool more = t + 1 < n_tiles;
+            if (a.stall && t == min(1, n_tiles - 1)) break;
             // the stage, and the parity of its last use's end
             const int st = t % ST;
             const uint32_t past = (uint32_t)(t / ST - 1) & 1u, k_s = base + L::K + st * L::ROWS;

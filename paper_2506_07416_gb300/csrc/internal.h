@@ -175,6 +175,7 @@ struct AttendArgs {
     int64_t logit_stride;
     const float* weights_in;  // [num_pages][page_size]
     float* weights_out;       // null: no weights
+    int32_t stall;            // debug: the second tile's values are never made
     int32_t* err;
     long long wait_budget;
 };

@@ -376,6 +376,7 @@ def set_wait_budget(handle: int, cycles: int) -> None:
 
 DEBUG_STALL_SCORE = 1
 DEBUG_STALL_PROJECT = 4
+DEBUG_STALL_ATTEND = 8
 
 
 def set_debug_flags(handle: int, flags: int) -> None:
