@@ -1337,17 +1337,20 @@ struct AttendSpace {
     int64_t part_o, part_ml, split, lse, logits, total;
 };
 int64_t logit_stride(int32_t max_len) { return ((int64_t)max_len + 31) & ~(int64_t)31; }
-// rows: of the call (query x head); head_rows: key heads x rows of the longest request
-AttendSpace attend_space(const lvs::AttendPlan& plan, int64_t rows, int head_dim, int64_t head_rows, int32_t batch,
-                         int32_t max_len, bool weights)
+int row_tiles(int max_rows) { return (max_rows + 127) / 128; }
+// rows: of the call (query x head); max_rows: of the longest request (query x head of a key head)
+AttendSpace attend_space(const lvs::AttendPlan& plan, int64_t rows, int head_dim, int64_t hkv, int max_rows,
+                         int32_t batch, int32_t max_len, bool weights)
 {
+    const int64_t head_rows = hkv * max_rows, head_tiles = hkv * row_tiles(max_rows);
     AttendSpace s{};
     const int64_t parts = plan.slots * head_rows;
     s.part_ml = round256(parts * head_dim * 4);
     s.split = s.part_ml + round256(parts * 8);
     s.lse = s.split + (plan.slots > 0 ? round256((int64_t)batch * 8) : 0);
     s.logits = s.lse + (weights ? round256(rows * 4) : 0);
-    s.total = s.logits + (weights && plan.logits ? round256(batch * head_rows * logit_stride(max_len) * 4) : 0);
+    const int64_t kept = plan.logits ? head_rows : head_tiles;  // rows of scores, or of their tiles' weights
+    s.total = s.logits + (weights ? round256(batch * kept * logit_stride(max_len) * 4) : 0);
     return s;
 }
 
@@ -1357,7 +1360,8 @@ litevlm_status_t attend_plan(litevlm_select_t h, int32_t batch, const int32_t* q
     const litevlm_select_config_t& c = h->cfg;
     litevlm_status_t s = check_offsets(h, q_offsets_h, batch, INT32_MAX, "q_offsets", total);
     if (s != LITEVLM_OK) return s;
-    if (max_len < 0) return fail(h, LITEVLM_ERR_INVALID_ARG, "max_len must be >= 0");
+    if (max_len < 0 || max_len > (1 << 30))
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "max_len must be in [0, 2^30]");
     const int64_t group = c.num_q_heads / c.num_kv_heads;
     const int64_t rows = max_count(q_offsets_h, batch) * group;
     if (rows > INT32_MAX / 2 || (int64_t)c.num_kv_heads * ((rows + 7) / 8) > 65535)
@@ -1447,7 +1451,7 @@ litevlm_status_t litevlm_select_cache_attend_workspace(litevlm_select_t h, int32
     s = attend_plan(h, batch, q_offsets_h, max_len, &plan, &total, &max_rows);
     if (s == LITEVLM_OK)
         *bytes = attend_space(plan, total * h->cfg.num_q_heads, h->cfg.head_dim,
-                              (int64_t)h->cfg.num_kv_heads * max_rows, batch, max_len, weights != 0)
+                              h->cfg.num_kv_heads, max_rows, batch, max_len, weights != 0)
                      .total;
     return s;
 }
@@ -1483,7 +1487,7 @@ litevlm_status_t litevlm_select_cache_attend(litevlm_select_t h, int32_t batch, 
         if (!out || !aligned16(out)) return fail(h, LITEVLM_ERR_INVALID_ARG, "out must be 16-byte aligned and not NULL");
     }
     const AttendSpace space = attend_space(plan, total * c.num_q_heads, c.head_dim,
-                                           (int64_t)c.num_kv_heads * max_rows, batch, max_len, weights_out != nullptr);
+                                           c.num_kv_heads, max_rows, batch, max_len, weights_out != nullptr);
     if (workspace_bytes < space.total || (space.total > 0 && !workspace))
         return fail(h, LITEVLM_ERR_WORKSPACE, "the workspace must hold " + std::to_string(space.total) + " bytes");
     if (reinterpret_cast<uintptr_t>(workspace) & 255u)
@@ -1508,6 +1512,8 @@ litevlm_status_t litevlm_select_cache_attend(litevlm_select_t h, int32_t batch, 
     a.split = reinterpret_cast<int2*>(ws + space.split);
     a.lse = weights_out ? reinterpret_cast<float*>(ws + space.lse) : nullptr;
     a.logits = weights_out && plan.logits ? reinterpret_cast<float*>(ws + space.logits) : nullptr;
+    a.part_w = weights_out && !plan.logits ? reinterpret_cast<float*>(ws + space.logits) : nullptr;
+    a.row_tiles = row_tiles(max_rows);
     a.max_rows = max_rows;
     a.logit_stride = logit_stride(max_len);
     a.weights_in = weights_in;
@@ -1544,8 +1550,8 @@ litevlm_status_t litevlm_select_cache_evict(litevlm_select_t h, int32_t batch, c
     int32_t holds = 0;
     s = cache_pages(h, cache, table, table_width, seq_lens, &a.cache, &holds);
     if (s != LITEVLM_OK) return s;
-    if (max_len < 0 || max_len > holds)
-        return fail(h, LITEVLM_ERR_INVALID_ARG, "max_len must be in [0, table_width * page_size]");
+    if (max_len < 0 || max_len > holds || max_len > (1 << 30))
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "max_len must be in [0, table_width * page_size] and at most 2^30");
     if (to_table && (to_width < 1 || (int64_t)to_width * cache->page_size < std::min(budget, max_len)))
         return fail(h, LITEVLM_ERR_INVALID_ARG, "to_width pages must hold min(budget, max_len) tokens");
     if (!weights || !kept_idx || !new_lens) return fail(h, LITEVLM_ERR_INVALID_ARG, "a device pointer is NULL");

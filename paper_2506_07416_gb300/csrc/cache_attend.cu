@@ -4,13 +4,14 @@
 // the keys up to it. With s = c * q.k in log2 units, p = 2^(s - lse), lse = log2 sum
 // 2^s: out = sum p v; weight[j] += (1/Hq) sum over heads and queries of p.
 //
-// attend_split_kernel: a CTA takes a key head of a request, a tile of 8, 16 or 32
-// rows (a row is a query with one of the head's query heads) and a chunk of the
-// keys. Its four warps work on their own: a warp copies groups of 16 keys into its
-// ring in shared memory (two groups at a time), makes f16 values of codes and scales in registers (exact),
-// and multiplies with the keys as the M rows and the query rows as the N columns
+// attend_split_kernel, for up to 32 rows a key head (a row is a query with one of the
+// head's query heads; cache_tile.cu has the kernel for more): a CTA takes a key head of
+// a request, a tile of 8 or 16 rows and all keys, or a chunk of them. Its four warps
+// work on their own: a warp copies groups of 16 keys into its ring in shared memory,
+// two groups at a time, makes f16 values of codes and scales in registers (exact), and
+// multiplies with the keys as the M rows and the query rows as the N columns
 // (m16n8k16): a tile of 8 rows, the usual one of a single token, then costs no
-// padding. Channels of a contraction may come in any order, so a lane takes the 32
+// padding, where a contraction of the fifth generation takes 128 rows. Channels of a contraction may come in any order, so a lane takes the 32
 // (QK) or 16 (PV) neighbouring channels that one load brings. The rows' references
 // move only when a score passes them by 8 (2^8 is well inside f16); sums and
 // statistics are fp32. P is rounded to f16 (11 bits) for the second product, the
@@ -18,9 +19,7 @@
 // attend_finish_kernel: the chunks of a row joined under the largest reference, and
 // the weights of calls of up to 32 rows a key head, whose scores the first kernel has
 // kept: 4 bytes a row and key written and read, mostly in L2.
-// attend_weight_kernel: the weights of calls of more rows: with every row's lse known,
-// a CTA takes 128 keys of a request and makes their scores again for all heads.
-// Either adds the probabilities in a fixed order; no atomics.
+// The probabilities of a key are added in a fixed order; no atomics.
 
 #include <algorithm>
 #include <type_traits>
@@ -65,31 +64,28 @@ struct Group {
     static constexpr int kBytes = 2 * (kCodes + kScales);
 };
 
-// Starts a warp's copies of the two groups of 16 keys from j0 on, of K (and of V where
-// WITH_V) of head h: lanes 0 to 15 copy the first group, the others the second. A group
-// lies in one page; `page` is the lane's (-1: zeros).
-template <int D, bool WITH_V>
+// Starts a warp's copies of the two groups of 16 keys from j0 on, of K and V of head h:
+// lanes 0 to 15 copy the first group, the others the second. A group lies in one page;
+// `page` is the lane's (-1: zeros).
+template <int D>
 __device__ __forceinline__ void load_span(const CachePages& c, int32_t page, int h, int j0, uint32_t dst)
 {
     using G = Group<D>;
-    constexpr int BYTES = WITH_V ? G::kBytes : G::kBytes / 2;
     const int lane = threadIdx.x & 31, l = lane & 15, half = lane >> 4;
     const bool ok = page >= 0;
     const int64_t row =
         cache_row(ok ? page : 0, c.hkv, h, c.page_shift, (j0 + 16 * half) & ((1 << c.page_shift) - 1));
-    dst += half * BYTES + l * 16;
+    dst += half * G::kBytes + l * 16;
     const uint8_t* k = c.codes[0] + row * (D / 2) + l * 16;
 #pragma unroll
     for (int i = 0; i < G::kCodes / 256; ++i) copy_async16(dst + G::kK + i * 256, k + i * 256, ok);
-    if constexpr (WITH_V) {
-        const uint8_t* v = c.codes[1] + row * (D / 2) + l * 16;
+    const uint8_t* v = c.codes[1] + row * (D / 2) + l * 16;
 #pragma unroll
-        for (int i = 0; i < G::kCodes / 256; ++i) copy_async16(dst + G::kV + i * 256, v + i * 256, ok);
-    }
+    for (int i = 0; i < G::kCodes / 256; ++i) copy_async16(dst + G::kV + i * 256, v + i * 256, ok);
     // scales: the first lanes those of K, the next those of V
     constexpr int SL = G::kScales / 16;
     const int t = l / SL;
-    if (t < (WITH_V ? 2 : 1))
+    if (t < 2)
         copy_async16(dst + (t ? G::kVs - SL * 16 : G::kKs), c.scales[t] + row * (D / 16) + (l - t * SL) * 16, ok);
 }
 
@@ -262,7 +258,7 @@ __global__ void __launch_bounds__(kAttThreads) attend_split_kernel(const __grid_
 #pragma unroll
     for (int i = 0; i < kAttStages - 1; ++i) {
         const int32_t page = page_of(i);
-        if (i < n_mine) load_span<D, true>(a.cache, page, h, k0 + (warp + i * kAttWarps) * 32, my_s + i * SPAN);
+        if (i < n_mine) load_span<D>(a.cache, page, h, k0 + (warp + i * kAttWarps) * 32, my_s + i * SPAN);
         copy_async_commit();
         named = named << 1 | (page >= 0);
     }
@@ -536,7 +532,7 @@ __global__ void __launch_bounds__(kAttThreads) attend_split_kernel(const __grid_
             const int nx = n + kAttStages - 1;
             const int to = stage == 0 ? kAttStages - 1 : stage - 1;
             if (nx < n_mine)
-                load_span<D, true>(a.cache, next_page, h, j0 + (kAttStages - 1) * kAttWarps * 32, my_s + to * SPAN);
+                load_span<D>(a.cache, next_page, h, j0 + (kAttStages - 1) * kAttWarps * 32, my_s + to * SPAN);
             copy_async_commit();
             named = named << 1 | (next_page >= 0);
             next_page = page_of(nx + 1);
@@ -860,82 +856,6 @@ __global__ void __launch_bounds__(kFinishThreads) attend_finish_kernel(const __g
     if (a.lse && lane == 0) a.lse[at] = L == 0.f ? INFINITY : M + log2f(L);
 }
 
-// A CTA: 128 keys of a request, a warp 32 of them; all key heads, their rows 8 at a time.
-template <int D, bool FP8>
-__global__ void __launch_bounds__(kAttThreads) attend_weight_kernel(const __grid_constant__ AttendArgs a)
-{
-    using G = Group<D>;
-    constexpr int HALF = G::kBytes / 2;  // a group's K
-    __shared__ __align__(16) uint8_t ring[kAttWarps][2][2 * HALF];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int g = lane >> 2, c = lane & 3;
-    const int b = blockIdx.y;
-    griddep_wait();
-    griddep_launch_dependents();
-    const RowTile rt = row_tile(a, b, 0, 8);
-    const int j0 = (blockIdx.x * kAttWarps + warp) * 32;
-    if (j0 >= rt.len) return;
-    const int my_j = j0 + (lane & 16);
-    const int32_t page =
-        my_j < rt.len ? cache_page(a.cache.table, a.cache.width, a.cache.num_pages, a.cache.page_shift, b, my_j) : -1;
-    const int q0 = a.q_off[b], rows = rt.t * a.group;
-    // rows that see a key of the span: the queries from the first that stands at or behind j0
-    const int r_first = max(0, j0 - rt.last0) * a.group;
-    const uint32_t dst = smem_u32(&ring[warp][0][0]);
-    load_span<D, false>(a.cache, page, 0, j0, dst);
-    copy_async_commit();
-    float sum[2][2] = {{0.f, 0.f}, {0.f, 0.f}};  // of the groups' keys g and g + 8, over the lane's rows
-    for (int h = 0; h < a.cache.hkv; ++h) {
-        if (h + 1 < a.cache.hkv) load_span<D, false>(a.cache, page, h + 1, j0, dst + ((h + 1) & 1) * 2 * HALF);
-        copy_async_commit();
-        copy_async_wait<1>();
-        __syncwarp();
-        for (int r0 = r_first & ~7; r0 < rows; r0 += 8) {
-            const bool real = r0 + g < rows;
-            const int row = real ? r0 + g : r0;
-            uint32_t q[D / 8];
-            float back;
-            load_q<D, FP8>(a.q, (int64_t)(q0 + row / a.group) * a.q_stride +
-                                    (int64_t)(h * a.group + row % a.group) * D + c * (D / 4),
-                           real, q, back);
-            float s[2][1][4];
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-                score_group<D, 1>(&ring[warp][h & 1][x * HALF], lane,
-                                  [&](int, int k) { return make_uint2(q[2 * k], q[2 * k + 1]); }, s[x]);
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const float fac = a.c_log2 * __shfl_sync(0xffffffffu, back, 8 * c + 4 * e);
-                const int r = r0 + 2 * c + e;
-                if (r >= rows) continue;
-                const int vis = rt.last0 + r / a.group;
-                const float lse = a.lse[(int64_t)(q0 + r / a.group) * a.hq + h * a.group + r % a.group];
-#pragma unroll
-                for (int x = 0; x < 2; ++x)
-#pragma unroll
-                    for (int y = 0; y < 2; ++y)
-                        if (j0 + 16 * x + 8 * y + g <= vis) sum[x][y] += ex2(fmaf(s[x][0][e + 2 * y], fac, -lse));
-            }
-        }
-        __syncwarp();
-    }
-    copy_async_wait<0>();
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-        const int32_t p = __shfl_sync(0xffffffffu, page, 16 * x);
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-            sum[x][y] += __shfl_xor_sync(0xffffffffu, sum[x][y], 1);
-            sum[x][y] += __shfl_xor_sync(0xffffffffu, sum[x][y], 2);
-            const int j = j0 + 16 * x + 8 * y + g;
-            if (c == 0 && j < rt.len && p >= 0) {
-                const int64_t at = ((int64_t)p << a.cache.page_shift) + (j & ((1 << a.cache.page_shift) - 1));
-                a.weights_out[at] = a.weights_in[at] + sum[x][y] / (float)a.hq;
-            }
-        }
-    }
-}
-
 template <int D, bool FP8>
 cudaError_t launch_all(const AttendArgs& a, const AttendPlan& plan, int max_rows, int64_t total_rows, int max_len,
                        cudaStream_t stream, int32_t* launches)
@@ -988,11 +908,9 @@ cudaError_t launch_all(const AttendArgs& a, const AttendPlan& plan, int max_rows
         cfg.dynamicSmemBytes = 0;
     }
     if (a.weights_out && !a.logits && max_len > 0) {
-        cfg.gridDim = dim3((unsigned)((max_len + 127) / 128), (unsigned)a.batch, 1);
-        cfg.blockDim = dim3(kAttThreads, 1, 1);
-        e = cudaLaunchKernelEx(&cfg, attend_weight_kernel<D, FP8>, a);
+        e = launch_attend_weights(a, D, FP8, max_len, stream);
         if (e != cudaSuccess) return e;
-        ++*launches;
+        *launches += a.row_tiles > 0 ? 2 : 1;
     }
     return e;
 }

@@ -36,11 +36,13 @@ __device__ __forceinline__ int chunk_keys(const AttendArgs& a)
     for (int d = 16; d > 0; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
     const long long mean = (total + a.slots - 1) / a.slots;
     const int c = max(64, (int)min((long long)INT32_MAX / 2, (mean + mean * lane / 8 + 63) & ~63ll));
-    // chunks by a reciprocal that errs upwards: never fewer than there are
-    const float inv = 1.000001f / (float)c;
+    // ceil(n / c) as that of (n - 1/2) / c: below 2^21 keys the product's error cannot reach a
+    // whole number; longer requests count with a margin (never fewer chunks than there are)
+    const float inv = 1.f / (float)c;
     float count = 0.f;
     for (int b0 = 0; b0 < a.batch; b0 += 32) {
-        const float mine = b0 + lane < a.batch ? (float)keys_of(a, b0 + lane) : 0.f;
+        float mine = b0 + lane < a.batch ? (float)keys_of(a, b0 + lane) : 0.f;
+        mine = mine < 2097152.f ? fmaxf(mine - 0.5f, 0.f) : mine * 1.000001f;
         for (int x = 0; x < min(32, a.batch - b0); ++x) count += ceilf(__shfl_sync(0xffffffffu, mine, x) * inv);
     }
     const uint32_t fits = __ballot_sync(0xffffffffu, count <= (float)a.slots);
@@ -96,5 +98,8 @@ __device__ __forceinline__ RowTile row_tile(const AttendArgs& a, int b, int tile
 
 // The launch of cache_tile.cu: `tiles` tiles of 128 or 256 rows for the longest request.
 cudaError_t launch_attend_tiles(const AttendArgs& a, int head_dim, bool fp8, int row_tile, int tiles, cudaStream_t stream);
+
+// The weights of a call of many rows, from their lse.
+cudaError_t launch_attend_weights(const AttendArgs& a, int head_dim, bool fp8, int max_len, cudaStream_t stream);
 
 }  // namespace lvs

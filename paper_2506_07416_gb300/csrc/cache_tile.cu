@@ -118,11 +118,60 @@ __device__ __forceinline__ float stage_q(const void* q, int64_t at, bool real, u
     }
 }
 
-// A thread's part of a tile's K: 32 channels (D = 64: 16) of each of four keys, 8 apart.
+// A thread's part of a tile's K: 32 channels (D = 64: 16) of each of four keys, 8 apart: of warp
+// w of four the channels [c * D/4, ..), c = lane / 8, of the keys w * 32 + lane % 8 + 8 i. A warp's
+// loads then cover whole rows, and the stores of eight neighbouring lanes all banks.
 template <int D>
 struct KPart {
     uint4 code[4];   // D = 64: the first two words
     uint32_t scale[4];
+
+    // from the pages p0 and p1 of the warp's two groups of 16 keys (-1: zeros)
+    __device__ __forceinline__ void load(const CachePages& C, int32_t p0, int32_t p1, int h, int j0, int w)
+    {
+        const int lane = threadIdx.x & 31, c = lane >> 3, smask = (1 << C.page_shift) - 1;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int32_t page = i < 2 ? p0 : p1;
+            code[i] = make_uint4(0u, 0u, 0u, 0u);
+            scale[i] = 0u;
+            if (page >= 0) {
+                const int64_t at =
+                    cache_row(page, C.hkv, h, C.page_shift, (j0 + w * 32 + (lane & 7) + 8 * i) & smask);
+                if constexpr (D == 128) {
+                    code[i] = __ldg(reinterpret_cast<const uint4*>(C.codes[0] + at * 64 + c * 16));
+                    scale[i] = __ldg(reinterpret_cast<const uint16_t*>(C.scales[0] + at * 8 + c * 2));
+                } else {
+                    const uint2 v = __ldg(reinterpret_cast<const uint2*>(C.codes[0] + at * 32 + c * 8));
+                    code[i].x = v.x, code[i].y = v.y;
+                    scale[i] = __ldg(C.scales[0] + at * 4 + c);
+                }
+            }
+        }
+    }
+
+    // as f16 values into a K-major operand of 128 keys
+    __device__ __forceinline__ void store(uint32_t k_s, int w) const
+    {
+        const int lane = threadIdx.x & 31, c = lane >> 3;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int key = w * 32 + (lane & 7) + 8 * i;
+            const uint32_t words[4] = {code[i].x, code[i].y, code[i].z, code[i].w};
+            const __half2 sc = e4m3x2_value(scale[i]);
+            const __half2 sb[2] = {__low2half2(sc), D == 128 ? __high2half2(sc) : __low2half2(sc)};
+#pragma unroll
+            for (int q = 0; q < D / 32; ++q) {  // 8 channels
+                __half2 x[4];
+                e2m1x8_value(words[q], x);
+                const __half2 s = sb[q / 2];
+                const int u = c * (D / 32) + q;
+                st_shared16(k_s + (u >> 3) * (128 * 128) + key * 128 + (((u & 7) ^ (key & 7)) << 4),
+                            h2_bits(__hmul2(x[0], s)), h2_bits(__hmul2(x[1], s)), h2_bits(__hmul2(x[2], s)),
+                            h2_bits(__hmul2(x[3], s)));
+            }
+        }
+    }
 };
 // ... and of its V: 8 neighbouring keys, the 16 channels of one scale block.
 struct VPart {
@@ -329,11 +378,9 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
         const int w = warp - SOFT;
         const CachePages& C = a.cache;
         const int smask = (1 << C.page_shift) - 1;
-        // K: channels [c * D/4, ..) of the keys w * 32 + (lane & 7) + 8 i; V: keys kg * 8 .., block vb:
-        // a warp's loads then cover whole rows, and the stores of eight neighbouring lanes eight
-        // banks' worth of shared memory. For V these are four groups of keys of two blocks, so
-        // odd blocks take their channels 4 to 7 first (their words are turned by half).
-        const int c = lane >> 3, kr = w * 32 + (lane & 7);
+        // V: keys kg * 8 .., block vb: a warp's loads cover whole rows, and the stores of eight
+        // neighbouring lanes, four groups of keys of two blocks, all banks: odd blocks take their
+        // channels 4 to 7 first (their words are turned by half)
         const int kg = 4 * w + (lane & 3), vb = lane >> 2, turn = (vb & 1) * 4;
         const uint32_t v_at = (kg >> 3) * (D * 128) + vb * 16 * 128;
         const uint32_t v_x = (uint32_t)(turn << 7 | ((kg & 7) ^ turn) << 4);
@@ -343,26 +390,6 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
         };
         auto report = [&](int32_t page, int j) {
             if (page < 0 && j < k1) atomicOr(a.err, kErrBounds);
-        };
-        auto load_k = [&](KPart<D>& x, int32_t p0, int32_t p1, int j0) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int32_t page = i < 2 ? p0 : p1;
-                const int j = j0 + kr + 8 * i;
-                x.code[i] = make_uint4(0u, 0u, 0u, 0u);
-                x.scale[i] = 0u;
-                if (page >= 0) {
-                    const int64_t at = cache_row(page, C.hkv, h, C.page_shift, j & smask);
-                    if constexpr (D == 128) {
-                        x.code[i] = __ldg(reinterpret_cast<const uint4*>(C.codes[0] + at * 64 + c * 16));
-                        x.scale[i] = __ldg(reinterpret_cast<const uint16_t*>(C.scales[0] + at * 8 + c * 2));
-                    } else {
-                        const uint2 v = __ldg(reinterpret_cast<const uint2*>(C.codes[0] + at * 32 + c * 8));
-                        x.code[i].x = v.x, x.code[i].y = v.y;
-                        x.scale[i] = __ldg(C.scales[0] + at * 4 + c);
-                    }
-                }
-            }
         };
         auto load_v = [&](VPart& x, int32_t page, int j0) {
             const int64_t at = cache_row(page >= 0 ? page : 0, C.hkv, h, C.page_shift, (j0 + kg * 8) & smask);
@@ -390,7 +417,7 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
         VPart vp;
         pages(k0);
         report_pages(k0);
-        load_k(kp, pk0, pk1, k0);
+        kp.load(C, pk0, pk1, h, k0, w);
         load_v(vp, pv, k0);
         pages(k0 + kTileKeys);
         for (int t = 0; t < n_tiles; ++t) {
@@ -402,29 +429,13 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
             const uint32_t past = (uint32_t)(t / ST - 1) & 1u, k_s = base + L::K + st * L::ROWS;
             const uint32_t v_s = base + L::V + st * L::VALUES;
             if (t >= ST && !poll_phase_warp(BAR(B_K_FREE + st), past, ctl)) break;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int key = kr + 8 * i;
-                const uint32_t words[4] = {kp.code[i].x, kp.code[i].y, kp.code[i].z, kp.code[i].w};
-                const __half2 sc = e4m3x2_value(kp.scale[i]);
-                const __half2 sb[2] = {__low2half2(sc), D == 128 ? __high2half2(sc) : __low2half2(sc)};
-#pragma unroll
-                for (int q = 0; q < D / 32; ++q) {  // 8 channels
-                    __half2 x[4];
-                    e2m1x8_value(words[q], x);
-                    const __half2 s = sb[q / 2];
-                    const int u = c * (D / 32) + q;
-                    st_shared16(k_s + (u >> 3) * L::ATOM + key * 128 + (((u & 7) ^ (key & 7)) << 4),
-                                h2_bits(__hmul2(x[0], s)), h2_bits(__hmul2(x[1], s)), h2_bits(__hmul2(x[2], s)),
-                                h2_bits(__hmul2(x[3], s)));
-                }
-            }
+            kp.store(k_s, w);
             fence_proxy_async_shared();
             __syncwarp();
             if (lane == 0) mbar_arrive(BAR(B_K_FULL + st));
             if (more) {
                 report_pages(jn);
-                load_k(kp, pk0, pk1, jn);
+                kp.load(C, pk0, pk1, h, jn, w);
             }
             if (t >= ST && !poll_phase_warp(BAR(B_V_FREE + st), past, ctl)) break;
             if (v_part) {
@@ -592,6 +603,229 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
     }
 }
 
+// ---------------------------------------------------------------------------------------
+// The weights of calls of many rows. With every row's lse known, a CTA takes 128 rows of a
+// key head and all keys that they see (or a chunk of them), makes their scores again, this
+// time with the keys as the rows of the contraction, and each thread adds up the
+// probabilities of one key over the columns, in order. The sums of a tile of rows are kept
+// for every key; attend_fold_kernel adds those of all tiles and heads, in order. Bound by the
+// exponentials and the contraction, as the first pass, with no second product.
+enum { W_K_FULL = 0, W_K_FREE = 2, W_S_FULL = 4, W_S_FREE = 6, W_DRAIN = 8, W_COUNT };
+
+template <int D>
+struct WeightLayout {
+    static constexpr int ROWS = TileLayout<D, 1>::ROWS;
+    static constexpr int Q = 0, K = ROWS;                   // two stages of K
+    static constexpr int CONST = 3 * ROWS;                  // scale and lse of every row
+    static constexpr int BAR = CONST + 128 * 8;
+    static constexpr int MISC = BAR + 8 * W_COUNT;
+    static constexpr int NEED = MISC + 16 + 1024;           // (at least 77 KB, as above)
+    static constexpr int ALLOC = NEED > 77 * 1024 ? NEED : 77 * 1024;
+};
+
+template <int D, bool FP8>
+__global__ void __launch_bounds__(kTileThreads<1>, 2) attend_weight_kernel(const __grid_constant__ AttendArgs a)
+{
+    using L = WeightLayout<D>;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw);
+    const uint32_t base = (raw + 1023u) & ~1023u;
+    uint8_t* smem = smem_raw + (base - raw);
+    auto BAR = [&](int i) { return base + L::BAR + 8 * i; };
+    float2* row_s = reinterpret_cast<float2*>(smem + L::CONST);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::MISC);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + L::MISC + 4);
+
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int warp = uniform(tid >> 5);
+    const int h = blockIdx.y % a.cache.hkv, tile = blockIdx.y / a.cache.hkv;
+    griddep_wait();
+    griddep_launch_dependents();
+    int b = blockIdx.z, chunk = INT32_MAX / 2, k0 = 0;
+    __shared__ int split_s[3];
+    if (a.slots > 0) {
+        if (threadIdx.x < 32) {
+            chunk = chunk_keys(a);
+            find_slot(a, blockIdx.x, chunk, b, k0);
+            if (threadIdx.x == 0) split_s[0] = chunk, split_s[1] = b, split_s[2] = k0;
+        }
+        __syncthreads();
+        chunk = uniform(split_s[0]), b = uniform(split_s[1]), k0 = uniform(split_s[2]);
+        if (b == a.batch) return;
+    }
+    const RowTile rt = row_tile(a, b, tile, 128);
+    if (rt.rows <= 0) return;
+    const int q0 = a.q_off[b];
+    const int seen = min(rt.len, rt.last0 + rt.query(rt.row0 + rt.rows - 1) + 1);
+    const int k1 = min(seen, k0 + chunk);
+    if (k0 >= k1) return;
+    const int all_see = rt.last0 + rt.query(rt.row0);
+    const int n_tiles = uniform((k1 - k0 + kTileKeys - 1) / kTileKeys);
+
+    if (tid == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(BAR(W_K_FULL + i), 4);
+            mbar_init(BAR(W_K_FREE + i), 1);
+            mbar_init(BAR(W_S_FULL + i), 1);
+            mbar_init(BAR(W_S_FREE + i), 4);
+        }
+        mbar_init(BAR(W_DRAIN), 1);
+        *abort_flag = 0;
+        fence_mbar_init_cluster();
+    }
+    if (warp == 8) {
+        tmem_alloc(smem_u32(tmem_slot), 256);
+        tmem_relinquish();
+    }
+    if (tid < 128) {
+        const bool real = tid < rt.rows;
+        const int row = rt.row0 + (real ? tid : 0), query = rt.query(row), head = h * a.group + row - query * a.group;
+        const float fac = a.c_log2 * stage_q<D, FP8>(a.q, (int64_t)(q0 + query) * a.q_stride + (int64_t)head * D, real,
+                                                     base + L::Q, tid);
+        row_s[tid] = real ? make_float2(fac, -__ldcg(a.lse + (int64_t)(q0 + query) * a.hq + head))
+                          : make_float2(0.f, -INFINITY);  // (no probability)
+        fence_proxy_async_shared();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = uniform(*tmem_slot);
+    const Ctl ctl{abort_flag, a.err, a.wait_budget};
+
+    if (warp < 4) {
+        // ---------------------------------------------------------------- sums: a key a thread
+        float* out = a.part_w + (((int64_t)b * a.cache.hkv + h) * a.row_tiles + tile) * a.logit_stride;
+        const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+        for (int t = 0; t < n_tiles; ++t) {
+            const int st = t & 1, j = k0 + t * kTileKeys + tid;
+            if (!poll_phase_warp(BAR(W_S_FULL + st), (uint32_t)(t >> 1) & 1u, ctl)) break;
+            tc_fence_after();
+            // the first row that sees the key (rows ascend with their queries)
+            const int from = j <= all_see ? 0 : (int)min((int64_t)128, (int64_t)(j - rt.last0) * a.group - rt.row0);
+            float2 sum = make_float2(0.f, 0.f);
+#pragma unroll 1
+            for (int c0 = 0; c0 < 128; c0 += 32) {
+                float v[32];
+                tmem_ld32(tmem + lanes + 128 * st + c0, v);
+                tmem_wait_ld();
+                if (c0 == 96) {  // all have been read
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(BAR(W_S_FREE + st));
+                }
+                const float4* k = reinterpret_cast<const float4*>(row_s + c0);
+                if (k0 + t * kTileKeys + kTileKeys - 1 <= all_see) {
+#pragma unroll
+                    for (int i = 0; i < 32; i += 2) {
+                        const float4 x = k[i / 2];
+                        const float2 e = ffma2(make_float2(v[i], v[i + 1]), make_float2(x.x, x.z), make_float2(x.y, x.w));
+                        sum = fadd2(sum, make_float2(ex2(e.x), ex2(e.y)));
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 32; i += 2) {
+                        const float4 x = k[i / 2];
+                        const float p0 = ex2(fmaf(v[i], x.x, x.y)), p1 = ex2(fmaf(v[i + 1], x.z, x.w));
+                        sum.x += c0 + i >= from ? p0 : 0.f;
+                        sum.y += c0 + i + 1 >= from ? p1 : 0.f;
+                    }
+                }
+            }
+            if (j < k1) __stcg(out + j, sum.x + sum.y);
+        }
+    } else if (warp < 8) {
+        // ---------------------------------------------------------------- codes to values
+        const int w = warp - 4;
+        const CachePages& C = a.cache;
+        auto page_at = [&](int j) -> int32_t {
+            return j < k1 ? cache_page(C.table, C.width, C.num_pages, C.page_shift, b, j) : -1;
+        };
+        KPart<D> kp;
+        int32_t p0 = page_at(k0 + w * 32), p1 = page_at(k0 + w * 32 + 16);
+        kp.load(C, p0, p1, h, k0, w);
+        p0 = page_at(k0 + kTileKeys + w * 32), p1 = page_at(k0 + kTileKeys + w * 32 + 16);
+        for (int t = 0; t < n_tiles; ++t) {
+            const int st = t & 1, jn = k0 + (t + 1) * kTileKeys;
+            if (t >= 2 && !poll_phase_warp(BAR(W_K_FREE + st), (uint32_t)((t >> 1) - 1) & 1u, ctl)) break;
+            kp.store(base + L::K + st * L::ROWS, w);
+            fence_proxy_async_shared();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(BAR(W_K_FULL + st));
+            if (t + 1 < n_tiles) kp.load(C, p0, p1, h, jn, w);
+            p0 = page_at(jn + kTileKeys + w * 32), p1 = page_at(jn + kTileKeys + w * 32 + 16);
+        }
+    } else {
+        // ---------------------------------------------------------------- contractions
+        const uint32_t idesc = idesc_make(128, 128, 0u);
+        for (int t = 0; t < n_tiles; ++t) {
+            const int st = t & 1;
+            if (!poll_phase_warp(BAR(W_K_FULL + st), (uint32_t)(t >> 1) & 1u, ctl)) break;
+            if (t >= 2 && !poll_phase_warp(BAR(W_S_FREE + st), (uint32_t)((t >> 1) - 1) & 1u, ctl)) break;
+            tc_fence_after();
+            if (elect_one()) {
+#pragma unroll
+                for (int x = 0; x < D / 16; ++x) {
+                    const uint32_t off = (x >> 2) * (128 * 128) + (x & 3) * 32;
+                    mma_f16(tmem + 128 * st, sdesc_k_sw128(base + L::K + st * L::ROWS + off),
+                            sdesc_k_sw128(base + L::Q + off), idesc, x > 0);
+                }
+                mma_commit(BAR(W_S_FULL + st));
+                mma_commit(BAR(W_K_FREE + st));
+            }
+            __syncwarp();
+        }
+        if (elect_one()) mma_commit(BAR(W_DRAIN));
+        __syncwarp();
+        volatile int no_abort = 0;
+        const Ctl drain{&no_abort, a.err, kWaitBudgetCycles};
+        wait_phase(BAR(W_DRAIN), 0u, drain);
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 8) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 256);
+    }
+}
+
+// 128 keys of a request a CTA: the sums of all heads' row tiles that see a key, four warps
+// sharing them, then the weights.
+constexpr int kFoldThreads = 512;
+__global__ void __launch_bounds__(kFoldThreads) attend_fold_kernel(const __grid_constant__ AttendArgs a)
+{
+    __shared__ float part_s[4][128];
+    const int b = blockIdx.y, j = blockIdx.x * 128 + (threadIdx.x & 127), part = threadIdx.x >> 7;
+    griddep_wait();
+    griddep_launch_dependents();
+    bool bad;
+    const int len = cache_len(a.lens[b], a.limit, bad);
+    const int t = a.q_off[b + 1] - a.q_off[b], rows = t * a.group;
+    if (blockIdx.x * 128 >= len) return;
+    float sum = 0.f;
+    if (j < len) {
+        // the row tiles from the one on whose last row is the first that sees the key
+        const int tiles = (rows + 127) / 128, query = max(0, j - (len - t));
+        const int first = (int)((int64_t)query * a.group / 128);
+        const float* p = a.part_w + (int64_t)b * a.cache.hkv * a.row_tiles * a.logit_stride + j;
+        const int n = max(0, tiles - first), all = n * a.cache.hkv, per = (all + 3) / 4;
+        const int x0 = min(all, part * per), x1 = min(all, x0 + per);
+        int h = n > 0 ? x0 / n : 0, r = first + (n > 0 ? x0 - h * n : 0);
+#pragma unroll 8
+        for (int x = x0; x < x1; ++x) {
+            sum += __ldcg(p + ((int64_t)h * a.row_tiles + r) * a.logit_stride);
+            if (++r == tiles) r = first, ++h;
+        }
+    }
+    part_s[part][threadIdx.x & 127] = sum;
+    __syncthreads();
+    if (part != 0 || j >= len) return;
+    const int32_t page = cache_page(a.cache.table, a.cache.width, a.cache.num_pages, a.cache.page_shift, b, j);
+    if (page < 0) return;
+    const int64_t at = ((int64_t)page << a.cache.page_shift) + (j & ((1 << a.cache.page_shift) - 1));
+    const float all = ((sum + part_s[1][threadIdx.x]) + part_s[2][threadIdx.x]) + part_s[3][threadIdx.x];
+    a.weights_out[at] = a.weights_in[at] + all / (float)a.hq;
+}
+
 template <int D, bool FP8, int NR>
 cudaError_t launch_variant(const AttendArgs& a, int tiles, cudaStream_t stream)
 {
@@ -623,6 +857,43 @@ cudaError_t launch_attend_tiles(const AttendArgs& a, int head_dim, bool fp8, int
     if (fp8) return launch_variant<128, true, 1>(a, tiles, stream);
     return head_dim == 128 ? launch_variant<128, false, 1>(a, tiles, stream)
                            : launch_variant<64, false, 1>(a, tiles, stream);
+}
+
+namespace {
+
+template <int D, bool FP8>
+cudaError_t launch_weights(const AttendArgs& a, int max_len, cudaStream_t stream)
+{
+    using L = WeightLayout<D>;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1] = {pdl_attribute()};
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    cfg.stream = stream;
+    cudaError_t e = cudaSuccess;
+    if (a.row_tiles > 0) {
+        auto kern = attend_weight_kernel<D, FP8>;
+        e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, L::ALLOC);
+        if (e != cudaSuccess) return e;
+        cfg.gridDim = a.slots > 0 ? dim3((unsigned)a.slots, (unsigned)(a.row_tiles * a.cache.hkv), 1)
+                                  : dim3(1, (unsigned)(a.row_tiles * a.cache.hkv), (unsigned)a.batch);
+        cfg.blockDim = dim3(kTileThreads<1>, 1, 1);
+        cfg.dynamicSmemBytes = L::ALLOC;
+        e = cudaLaunchKernelEx(&cfg, kern, a);
+        if (e != cudaSuccess) return e;
+        cfg.dynamicSmemBytes = 0;
+    }
+    cfg.gridDim = dim3((unsigned)((max_len + 127) / 128), (unsigned)a.batch, 1);
+    cfg.blockDim = dim3(kFoldThreads, 1, 1);
+    return cudaLaunchKernelEx(&cfg, attend_fold_kernel, a);
+}
+
+}  // namespace
+
+cudaError_t launch_attend_weights(const AttendArgs& a, int head_dim, bool fp8, int max_len, cudaStream_t stream)
+{
+    if (fp8) return launch_weights<128, true>(a, max_len, stream);
+    return head_dim == 128 ? launch_weights<128, false>(a, max_len, stream) : launch_weights<64, false>(a, max_len, stream);
 }
 
 }  // namespace lvs

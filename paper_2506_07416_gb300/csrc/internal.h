@@ -173,6 +173,8 @@ struct AttendArgs {
     float* logits;            // [batch][hkv][max_rows][logit_stride] scores in log2 units, or null
     int32_t max_rows;         // rows (query x head of a key head) of the longest request
     int64_t logit_stride;
+    float* part_w;            // [batch][hkv][row_tiles][logit_stride] a row tile's weights (calls of many rows)
+    int32_t row_tiles;        // tiles of 128 rows of the longest request
     const float* weights_in;  // [num_pages][page_size]
     float* weights_out;       // null: no weights
     int32_t stall;            // debug: the second tile's values are never made
@@ -180,7 +182,7 @@ struct AttendArgs {
     long long wait_budget;
 };
 struct AttendPlan {
-    int32_t row_tile;         // rows (query x head of a key head) of a CTA: 8, 16, 32 or 128
+    int32_t row_tile;         // rows (query x head of a key head) of a CTA: 8, 16, 128 or 256
     int32_t slots;
     bool logits;              // the weights are made from kept scores
 };
