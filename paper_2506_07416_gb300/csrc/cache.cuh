@@ -44,6 +44,19 @@ __device__ __forceinline__ __half2 e4m3x2_value(uint32_t w)
     return __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)w, __NV_E4M3));
 }
 
+// Values of the four e4m3 codes of w.
+__device__ __forceinline__ void e4m3x4_value(uint32_t w, __half2 (&v)[2])
+{
+    uint32_t o[2];
+    asm("{\n\t.reg .b16 h0, h1;\n\t"
+        "mov.b32 {h0, h1}, %2;\n\t"
+        "cvt.rn.f16x2.e4m3x2 %0, h0;\n\t"
+        "cvt.rn.f16x2.e4m3x2 %1, h1;\n\t}"
+        : "=r"(o[0]), "=r"(o[1])
+        : "r"(w));
+    v[0] = bits_h2(o[0]), v[1] = bits_h2(o[1]);
+}
+
 // 16 bytes from global to shared memory, asynchronously; zeros where !valid.
 __device__ __forceinline__ void copy_async16(uint32_t dst, const void* src, bool valid)
 {

@@ -119,10 +119,12 @@ __global__ void __launch_bounds__(kAppendThreads, 5) append_kernel(const __grid_
         if constexpr (FP8) {
             const uint32_t w[4] = {now.v[0].x, now.v[0].y, now.v[0].z, now.v[0].w};
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float2 f = __half22float2(e4m3x2_value(w[i / 2] >> (16 * (i & 1))));
-                y[2 * i] = f.x;
-                y[2 * i + 1] = f.y;
+            for (int i = 0; i < 4; ++i) {
+                __half2 v[2];
+                e4m3x4_value(w[i], v);
+                const float2 f = __half22float2(v[0]), g = __half22float2(v[1]);
+                y[4 * i] = f.x, y[4 * i + 1] = f.y;
+                y[4 * i + 2] = g.x, y[4 * i + 3] = g.y;
             }
         } else {
 #pragma unroll
@@ -195,7 +197,7 @@ cudaError_t launch_cache_append(const AppendArgs& a, int head_dim, bool fp8, int
     const int64_t row_groups = (a.rows + rows_per_warp - 1) / rows_per_warp;
     // heads of a warp: all of them once the rows alone fill the GPU
     int per_warp = 1;
-    while (per_warp < a.cache.hkv && row_groups * a.cache.hkv / (2 * per_warp) >= (int64_t)num_sms * 64) per_warp *= 2;
+    while (per_warp < a.cache.hkv && row_groups * a.cache.hkv / (2 * per_warp) >= (int64_t)num_sms * 128) per_warp *= 2;
     const int64_t parts = (a.cache.hkv + per_warp - 1) / per_warp;
     const int64_t warps = row_groups * parts;
     int64_t blocks = (warps * 32 + kAppendThreads - 1) / kAppendThreads;

@@ -106,7 +106,11 @@ __device__ __forceinline__ void load_q(const void* q, int64_t at, bool real, uin
             const uint4 v = real ? __ldg(s + i) : make_uint4(0u, 0u, 0u, 0u);
             const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-            for (int k = 0; k < 8; ++k) f[i * 8 + k] = h2_bits(e4m3x2_value(w[k / 2] >> (16 * (k & 1))));
+            for (int k = 0; k < 4; ++k) {
+                __half2 x[2];
+                e4m3x4_value(w[k], x);
+                f[i * 8 + 2 * k] = h2_bits(x[0]), f[i * 8 + 2 * k + 1] = h2_bits(x[1]);
+            }
         }
     } else {
         uint32_t w[N / 2];

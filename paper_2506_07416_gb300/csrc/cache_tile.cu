@@ -87,7 +87,11 @@ __device__ __forceinline__ float stage_q(const void* q, int64_t at, bool real, u
             const uint32_t w[4] = {v.x, v.y, v.z, v.w};
             uint32_t f[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) f[k] = h2_bits(e4m3x2_value(w[k / 2] >> (16 * (k & 1))));
+            for (int k = 0; k < 4; ++k) {
+                __half2 x[2];
+                e4m3x4_value(w[k], x);
+                f[2 * k] = h2_bits(x[0]), f[2 * k + 1] = h2_bits(x[1]);
+            }
             put(2 * i, f[0], f[1], f[2], f[3]);
             put(2 * i + 1, f[4], f[5], f[6], f[7]);
         }
