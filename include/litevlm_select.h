@@ -565,7 +565,10 @@ litevlm_status_t litevlm_select_score_noalloc(int32_t num_q_heads, int32_t num_k
  * it) is cut to it, and tokens whose table entry is not in [0, num_pages) are
  * skipped; both set LITEVLM_ERR_DEVICE_BOUNDS for litevlm_select_check_device.
  * Two calls that write to the same pages, or one that reads what another writes,
- * are ordered by the caller (one stream does).
+ * are ordered by the caller (one stream does). Requests of a call may share pages
+ * that it only reads (a common prefix under litevlm_select_cache_attend without
+ * weights); no slot that a call writes, weights among them, belongs to two of its
+ * tokens: which of the two is then left there is not defined.
  */
 typedef struct {
     void* k_codes;
@@ -645,7 +648,8 @@ litevlm_status_t litevlm_select_cache_append(litevlm_select_t handle, int32_t ba
  * the product with V. The weights are added in a fixed order (the same inputs give
  * the same bits).
  * Errors: as for litevlm_select_cache_append; WORKSPACE for a workspace that is too
- * small; UNSUPPORTED where Hkv x row tiles of the longest request passes 65535.
+ * small; UNSUPPORTED where Hkv x row tiles of the longest request passes 65535, or the
+ * workspace 2^60 bytes.
  */
 litevlm_status_t litevlm_select_cache_attend_workspace(litevlm_select_t handle, int32_t batch,
                                                        const int32_t* q_offsets_h, int32_t max_len, int32_t weights,

@@ -1366,6 +1366,10 @@ litevlm_status_t attend_plan(litevlm_select_t h, int32_t batch, const int32_t* q
     const int64_t rows = max_count(q_offsets_h, batch) * group;
     if (rows > INT32_MAX / 2 || (int64_t)c.num_kv_heads * ((rows + 7) / 8) > 65535)
         return fail(h, LITEVLM_ERR_UNSUPPORTED, "num_kv_heads x rows of the longest request / 8 exceeds 65535");
+    // the largest part of the workspace: a float for a key of every row (or 128 rows) of every key head
+    if ((double)batch * c.num_kv_heads * (double)std::max<int64_t>(std::min<int64_t>(rows, 32), row_tiles((int)rows)) *
+            ((double)max_len + 32.0) * 4.0 > 0x1p60)
+        return fail(h, LITEVLM_ERR_UNSUPPORTED, "the workspace would pass 2^60 bytes");
     *max_rows = (int)rows;
     *plan = lvs::plan_cache_attend(batch, c.num_kv_heads, (int)group, q_offsets_h, max_len, h->num_sms);
     return LITEVLM_OK;

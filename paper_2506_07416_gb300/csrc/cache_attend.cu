@@ -11,8 +11,9 @@
 // two groups at a time, makes f16 values of codes and scales in registers (exact), and
 // multiplies with the keys as the M rows and the query rows as the N columns
 // (m16n8k16): a tile of 8 rows, the usual one of a single token, then costs no
-// padding, where a contraction of the fifth generation takes 128 rows. Channels of a contraction may come in any order, so a lane takes the 32
-// (QK) or 16 (PV) neighbouring channels that one load brings. The rows' references
+// padding, where a contraction of the fifth generation takes 64 or 128 rows. Channels of a
+// contraction may come in any order, so a lane takes the 32 (QK) or 16 (PV) neighbouring
+// channels that one load brings. The rows' references
 // move only when a score passes them by 8 (2^8 is well inside f16); sums and
 // statistics are fp32. P is rounded to f16 (11 bits) for the second product, the
 // output once to bf16 (8 bits).
@@ -20,6 +21,18 @@
 // the weights of calls of up to 32 rows a key head, whose scores the first kernel has
 // kept: 4 bytes a row and key written and read, mostly in L2.
 // The probabilities of a key are added in a fixed order; no atomics.
+//
+// What bounds it: a byte of codes costs instructions (its conversion to f16 pairs, loads,
+// contractions) beside its 1/6780 ns of memory, and registers limit an SM to 16 (one row, 8
+// rows) or 12 (16 rows) warps. By cases, all with weights:
+//   a token of 128 requests of about 1130, 32 heads (669 MB): 118 us and 10 for the weights;
+//     5.75 TB/s, issue 61%, the integer pipe 62%
+//   a token of four requests of 30 Ki to 131 Ki, 28 / 4 heads (217 MB): 50 + 22 us; 4.5 TB/s, issue 47%
+//   1 to 8 e4m3 queries of 32 requests, 32 / 8 heads (139 MB): 91 + 28 us; 2.6 TB/s with the kept
+//     scores, issue 37%: 12 warps do not cover one another's latencies
+// Dropped: values from codes by masks and shifts (20 pairs a clock and SM; the conversion 50),
+// the weights from K read again (190 us of the first case where the kept scores take 10),
+// tiles of 32 rows (155 us of the third: 255 registers), rings of three spans (no change).
 
 #include <algorithm>
 #include <type_traits>
@@ -697,7 +710,8 @@ __device__ __forceinline__ float4 add_weights(const float* s, int64_t stride, co
 // The first `join_blocks` CTAs of a request join its rows' chunks, `row_warps` warps a row;
 // the others add weights from the kept scores, 512 keys at a time, over the rows in order.
 // A weight CTA finds the rows' lse from the chunks' statistics by itself, which saves a
-// launch between the two.
+// launch between the two. 10 us of the 128-request step; 22 of the four long requests' (16 Ki to
+// 131 Ki keys x 28 rows of kept scores, 47 MB, and 600 chunks of 28 rows), 28 of the drafts' (80 MB).
 template <int D>
 __global__ void __launch_bounds__(kFinishThreads) attend_finish_kernel(const __grid_constant__ AttendArgs a,
                                                                        int join_blocks, int row_warps)
@@ -921,7 +935,13 @@ cudaError_t launch_all(const AttendArgs& a, const AttendPlan& plan, int max_rows
 
 }  // namespace
 
-constexpr int kFewRows = 32;  // rows of a request's key head up to which the kernel for few rows is taken
+// Rows of a request's key head up to which the kernel for few rows is taken. A key costs it less
+// and it splits finer, but it makes a key's values again for every 16 rows; the other makes them once for
+// 128 or 256 rows and takes as long for fewer. 16 requests of 4096 keys, 32 / 8 heads: 12 rows 54 us
+// (other 60), 20 rows 72 (60), 36 rows 93 (60). One of 8000 keys: 20 rows 19.2 (18.8), 36 rows 21.7
+// (19.7). 32 ragged requests of 4 to 32 rows and 0 to 8191 keys: 119 (201). A call's rows are those of its
+// longest request, so the border lies where ragged calls gain more than even ones lose.
+constexpr int kFewRows = 32;
 
 AttendPlan plan_cache_attend(int batch, int hkv, int group, const int32_t* q_off, int64_t max_len, int num_sms)
 {
@@ -929,6 +949,8 @@ AttendPlan plan_cache_attend(int batch, int hkv, int group, const int32_t* q_off
     for (int b = 0; b < batch; ++b) max_t = std::max(max_t, q_off[b + 1] - q_off[b]);
     const int64_t max_rows = (int64_t)max_t * group;
     AttendPlan p;
+    // 128 rows a CTA, or two row tiles that share the K and V that it makes: 192 rows 97 (one) and 76 us
+    // (two), 256 rows 92 and 79.
     p.row_tile = max_rows <= 8 ? 8 : (max_rows <= kFewRows ? 16 : (max_rows <= 128 ? 128 : 256));
     int64_t items = 0;  // CTAs where each takes all keys of its rows
     for (int b = 0; b < batch; ++b)
@@ -938,6 +960,7 @@ AttendPlan plan_cache_attend(int batch, int hkv, int group, const int32_t* q_off
     // memory), and the writing and joining of a chunk's sums takes a CTA as long as about five
     // keys for every four rows.
     const int64_t places = (int64_t)num_sms * (p.row_tile == 256 ? 1 : (p.row_tile == 128 ? 2 : (p.row_tile == 16 ? 3 : 4)));
+    // (three rounds of smaller chunks for 9 to 32 rows, whose requests have different numbers of rows too)
     const int rounds = p.row_tile == 16 && batch > 1 ? 3 : 1;
     const int64_t units = std::max<int64_t>(1, (max_len + 63) / 64);
     int64_t best = 1;
@@ -952,7 +975,7 @@ AttendPlan plan_cache_attend(int batch, int hkv, int group, const int32_t* q_off
         }
     }
     p.slots = best > 1 ? (int32_t)std::min<int64_t>(best * batch, 1 << 20) : 0;
-    p.logits = max_rows > 0 && max_rows <= 32 && max_rows * hkv <= kLogitRows;
+    p.logits = max_rows > 0 && max_rows <= kFewRows && max_rows * hkv <= kLogitRows;
     return p;
 }
 

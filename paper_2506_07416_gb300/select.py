@@ -500,6 +500,8 @@ class Selector:
                              qk_dtype, score_kernel, query, query_split)
         self.qk_dtype = qk_dtype
         self.heads, self.kv_heads, self.head_dim = num_q_heads, num_kv_heads, head_dim
+        import torch
+        self.device = torch.cuda.current_device()  # the one that create() took
         self._space = {}  # workspaces of cache_attend by stream
 
     def close(self) -> None:
@@ -676,6 +678,8 @@ class Selector:
         import torch
         if not isinstance(cache, KVCache):
             _refuse("cache must be a KVCache")
+        if cache.device != self.device:
+            _refuse(f"the cache is on cuda:{cache.device}, the handle on cuda:{self.device}")
         if cache.heads != self.kv_heads or cache.head_dim != self.head_dim:
             _refuse(f"the cache has {cache.heads} heads of {cache.head_dim}, the handle {self.kv_heads} of "
                     f"{self.head_dim}")
@@ -700,9 +704,10 @@ class Selector:
         return torch.uint8 if self.qk_dtype == "e4m3" else torch.bfloat16
 
     def cache(self, num_pages: int, page_size: int, k_scale: float = 1.0, v_scale: float = 1.0, weights: bool = True,
-              device="cuda") -> KVCache:
-        """An empty cache of the handle's head sizes."""
+              device=None) -> KVCache:
+        """An empty cache of the handle's head sizes (on the handle's device)."""
         import torch
+        device = self.device if device is None else device
         shape = (num_pages, self.kv_heads, page_size)
         c = [torch.zeros((*shape, self.head_dim // n), dtype=torch.uint8, device=device) for n in (2, 16, 2, 16)]
         w = torch.zeros((num_pages, page_size), dtype=torch.float32, device=device) if weights else None
@@ -811,6 +816,8 @@ class Selector:
                 target_probs.dim() != 2 or target_probs.dtype not in (torch.float32, torch.bfloat16):
             _refuse("target_probs must be a float32 or bf16 CUDA tensor [sum T + batch, vocab]")
         dev, kind, vocab = target_probs.device.index, target_probs.dtype, target_probs.shape[1]
+        if dev != self.device:
+            _refuse(f"target_probs is on cuda:{dev}, the handle on cuda:{self.device}")
         _want("target_probs", target_probs, kind, (total + batch, -1), dev)
         _want("draft_tokens", draft_tokens, torch.int32, (total,), dev)
         _want("u_accept", u_accept, torch.float32, (total,), dev)

@@ -273,3 +273,28 @@ def test_refusals(select):
     s.check_device()
     att()
     s.check_device()
+
+
+def test_tensors_of_another_device_than_the_handle_s_are_refused(select):
+    rng = np.random.default_rng(8)
+    s, c, w, table, q, _ = setup(select, rng)
+    cache, t, lens, off = to_cache(select, c, w), i32(table), i32([200, 37, 90]), i32([0, 1, 2, 3])
+    k = torch.zeros((3, 2, 128), dtype=torch.bfloat16, device="cuda")
+    p, x, u = torch.full((6, 5), 0.2, device="cuda"), i32([1, 2, 3]), torch.zeros(3, device="cuda")
+    assert s.device == torch.cuda.current_device() and s.cache(2, 16).device == s.device
+    s.device += 1  # (as if the handle had been made there: the check is the host's)
+    for call in (lambda: s.cache_append(cache, t, lens, k, k, off), lambda: s.cache_attend(cache, t, lens, q, off, 200),
+                 lambda: s.cache_evict(cache, t, lens, 200, 20), lambda: s.verify(x, p, u, u, off)):
+        with pytest.raises(select.LitevlmError) as e:
+            call()
+        assert e.value.name == "INVALID_ARG", str(e.value)
+    s.close()
+
+
+def test_a_workspace_beyond_every_size_is_refused(select):
+    s = select.Selector(65535, 8, 8, 65535, 65535, 128, "bf16")
+    off = np.arange(65536, dtype=np.int32)
+    with pytest.raises(select.LitevlmError) as e:
+        select.cache_attend_workspace(s.handle, 65535, off, 1 << 30)
+    assert e.value.name == "UNSUPPORTED", str(e.value)
+    s.close()
