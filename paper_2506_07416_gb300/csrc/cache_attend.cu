@@ -558,8 +558,7 @@ __global__ void __launch_bounds__(kAttThreads) attend_split_kernel(const __grid_
         stage = stage + 1 == kAttStages ? 0 : stage + 1;
         const uint32_t there = __ballot_sync(0xffffffffu, mine);
         if (there == 0xFFFFFFFFu && j0 + 31 <= all_see) {
-            // (the code of many rows is long: once, it stays in the instruction cache)
-#pragma unroll(NT > 1 ? 1 : 2)
+#pragma unroll
             for (int x = 0; x < 2; ++x) group(span + x * G::kBytes, j0 + 16 * x, true, std::false_type{});
         } else {
 #pragma unroll 1
@@ -674,7 +673,12 @@ __device__ __forceinline__ float2 join_stats(const float2* ml, int64_t step, int
 
 constexpr int kFinishThreads = 512;
 constexpr int kFinishWarps = kFinishThreads / 32;
-constexpr int kFinishKeys = 512;  // keys whose weights a CTA adds: 128 a warp, four warps share the rows
+// Warps of a CTA that share a key's rows in adding weights: the fewer, the more keys a CTA takes at a time
+// (128 for each of the others) and the fewer CTAs read the chunks' statistics; the more rows (query and
+// head), the longer a CTA would have. 28 rows (four requests of up to 131 Ki keys): 67 us for the call with 2,
+// 70 with 4, 75 with 8; 32 to 256 rows (32 requests of up to 8191): 125, 119 and 115.5. Where CTAs of 256
+// keys are so few that all run at once, more share too (16 rows, 524 keys: 8.4 us with 2, 7.7 with 8).
+int weight_parts(int rows, int64_t ctas, int num_sms) { return rows <= 64 && ctas > 3 * num_sms ? 2 : 8; }
 constexpr int kLogitRows = 2048;  // rows of a request whose scores are kept for the weights
 
 // Sums over the rows [x0, x1) of the probabilities of four neighbouring keys. CHECK: some
@@ -708,11 +712,11 @@ __device__ __forceinline__ float4 add_weights(const float* s, int64_t stride, co
 }
 
 // The first `join_blocks` CTAs of a request join its rows' chunks, `row_warps` warps a row;
-// the others add weights from the kept scores, 512 keys at a time, over the rows in order.
+// the others add weights from the kept scores, 256 to 1024 keys at a time, over the rows in order.
 // A weight CTA finds the rows' lse from the chunks' statistics by itself, which saves a
-// launch between the two. 10 us of the 128-request step; 22 of the four long requests' (16 Ki to
-// 131 Ki keys x 28 rows of kept scores, 47 MB, and 600 chunks of 28 rows), 28 of the drafts' (80 MB).
-template <int D>
+// launch between the two. 7 us of the 128-request step; 18 of the four long requests' (16 Ki to
+// 131 Ki keys x 28 rows of kept scores, 47 MB, and 600 chunks of 28 rows), 20 of the drafts' (80 MB).
+template <int D, int PARTS>
 __global__ void __launch_bounds__(kFinishThreads) attend_finish_kernel(const __grid_constant__ AttendArgs a,
                                                                        int join_blocks, int row_warps)
 {
@@ -739,7 +743,8 @@ __global__ void __launch_bounds__(kFinishThreads) attend_finish_kernel(const __g
     };
     if ((int)blockIdx.x >= join_blocks) {
         const int rows = t * a.group, n = rows * a.cache.hkv;
-        const int tiles = (len + kFinishKeys - 1) / kFinishKeys;
+        constexpr int across = kFinishWarps / PARTS, keys = 128 * across;
+        const int tiles = (len + keys - 1) / keys;
         int tile = blockIdx.x - join_blocks;
         if (tile >= tiles) return;
         float* lse_s = reinterpret_cast<float*>(rows_s);
@@ -774,61 +779,58 @@ __global__ void __launch_bounds__(kFinishThreads) attend_finish_kernel(const __g
             }
         }
         __syncthreads();
-        const int part = warp >> 2, per = (n + 3) / 4;
+        const int part = warp / across, per = (n + PARTS - 1) / PARTS;
         const int x0 = min(n, part * per), x1 = min(n, x0 + per);
         for (; tile < tiles; tile += gridDim.x - join_blocks) {
             // four neighbouring keys a lane (the scores' rows are padded to a whole number of them)
-            const int j0 = tile * kFinishKeys, j = j0 + (warp & 3) * 128 + 4 * lane;
-            int32_t page = -1;
-            if (part == 0 && j < len)
-                page = cache_page(a.cache.table, a.cache.width, a.cache.num_pages, a.cache.page_shift, b, j);
+            const int j0 = tile * keys, j = j0 + warp % across * 128 + 4 * lane;
+            int64_t at = -1;
+            float before[4];
+            if (part == 0 && j < len) {
+                const int32_t page =
+                    cache_page(a.cache.table, a.cache.width, a.cache.num_pages, a.cache.page_shift, b, j);
+                if (page >= 0) at = ((int64_t)page << a.cache.page_shift) + (j & ((1 << a.cache.page_shift) - 1));
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) before[e] = at >= 0 && j + e < len ? a.weights_in[at + e] : 0.f;
             float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
             if (j < len) {
                 const float* s = a.logits + (int64_t)b * a.cache.hkv * a.max_rows * a.logit_stride + j;
-                sum = j0 + kFinishKeys - 1 <= len - t ? add_weights<false>(s, a.logit_stride, row_s, lse_s, x0, x1, j)
+                sum = j0 + keys - 1 <= len - t ? add_weights<false>(s, a.logit_stride, row_s, lse_s, x0, x1, j)
                                                       : add_weights<true>(s, a.logit_stride, row_s, lse_s, x0, x1, j);
             }
             float4* sums = reinterpret_cast<float4*>(&join_s[0][0]);  // [part][128 lanes of the tile]
             sums[warp * 32 + lane] = sum;
             __syncthreads();
-            if (page >= 0) {
-                const int64_t at = ((int64_t)page << a.cache.page_shift) + (j & ((1 << a.cache.page_shift) - 1));
+            if (at >= 0) {
 #pragma unroll
-                for (int p = 1; p < 4; ++p) {
-                    const float4 v = sums[(warp + 4 * p) * 32 + lane];
+                for (int p = 1; p < PARTS; ++p) {
+                    const float4 v = sums[(warp + across * p) * 32 + lane];
                     sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
                 }
                 const float add[4] = {sum.x, sum.y, sum.z, sum.w};
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (j + e < len) a.weights_out[at + e] = a.weights_in[at + e] + add[e] / (float)a.hq;
+                    if (j + e < len) a.weights_out[at + e] = before[e] + add[e] / (float)a.hq;
             }
             __syncthreads();
         }
         return;
     }
-    const int part = warp % row_warps;
-    const int r = blockIdx.x * (kFinishWarps / row_warps) + warp / row_warps;  // query and head
-    const bool real = r < t * a.hq;
-    const int i = real ? r / a.hq : 0, hq = real ? r % a.hq : 0, h = hq / a.group;
-    const int n = real ? chunks_seen(i) : 0;
-    const int64_t from = ((int64_t)slot0 * a.cache.hkv + h) * a.max_rows + i * a.group + hq - h * a.group;
-    // chunks under a running reference, four of the warp's on their way at once
-    float M = kNoRef, L = 0.f, O[D / 32];
-#pragma unroll
-    for (int e = 0; e < D / 32; ++e) O[e] = 0.f;
-    auto add = [&](float m2, float l2, const float* v) {
-        const float top = fmaxf(M, m2), f = ex2(M - top), f2 = ex2(m2 - top);
-        M = top;
-        L = L * f + l2 * f2;
-#pragma unroll
-        for (int e = 0; e < D / 32; ++e) O[e] = O[e] * f + v[e] * f2;
+    const int part = warp % row_warps, join_rows = kFinishWarps / row_warps, rows = t * a.hq;
+    __shared__ float2 ml_s[kFinishWarps];
+    // where a row (query and head) has its chunks' sums, and how many chunks there are
+    auto place = [&](int r, int64_t& from) -> int {
+        if (r >= rows) return 0;
+        const int i = r / a.hq, hq = r - i * a.hq, h = hq / a.group;
+        from = ((int64_t)slot0 * a.cache.hkv + h) * a.max_rows + i * a.group + hq - h * a.group;
+        return chunks_seen(i);
     };
-    for (int x0 = part; x0 < n; x0 += 4 * row_warps) {
-        float2 ml[4];
-        float v[4][D / 32];
+    // four of the warp's chunks, from x0 on
+    constexpr int U = 4;
+    auto load = [&](int64_t from, int n, int x0, float2 (&ml)[U], float (&v)[U][D / 32]) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < U; ++u) {
             const int x = x0 + u * row_warps;
             const float* p = a.part_o + (from + x * step) * D + lane * (D / 32);
             ml[u] = make_float2(kNoRef, 0.f);
@@ -845,33 +847,59 @@ __global__ void __launch_bounds__(kFinishThreads) attend_finish_kernel(const __g
                 }
             }
         }
+    };
+    int64_t from = 0;
+    int r = blockIdx.x * join_rows + warp / row_warps, n = place(r, from);
+    float2 ml[U];
+    float v[U][D / 32];
+    load(from, n, part, ml, v);
+    const int next_r = join_blocks * join_rows;
+    for (int r0 = blockIdx.x * join_rows; r0 < rows; r0 += next_r, r += next_r) {
+        // chunks under a running reference
+        float M = kNoRef, L = 0.f, O[D / 32];
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-            if (x0 + u * row_warps < n) add(ml[u].x, ml[u].y, v[u]);
-    }
-    if (row_warps > 1) {
-        __shared__ float2 ml_s[kFinishWarps];
+        for (int e = 0; e < D / 32; ++e) O[e] = 0.f;
+        auto add = [&](float m2, float l2, const float* o2) {
+            const float top = fmaxf(M, m2), f = ex2(M - top), f2 = ex2(m2 - top);
+            M = top;
+            L = L * f + l2 * f2;
 #pragma unroll
-        for (int e = 0; e < D / 32; ++e) join_s[warp][lane * (D / 32) + e] = O[e];
-        if (lane == 0) ml_s[warp] = make_float2(M, L);
-        __syncthreads();
-        if (part != 0) return;
-        for (int w = 1; w < row_warps; ++w) {
-            float v[D / 32];
+            for (int e = 0; e < D / 32; ++e) O[e] = O[e] * f + o2[e] * f2;
+        };
+        for (int x0 = part; x0 < n; x0 += U * row_warps) {
+            if (x0 > part) load(from, n, x0, ml, v);
 #pragma unroll
-            for (int e = 0; e < D / 32; ++e) v[e] = join_s[warp + w][lane * (D / 32) + e];
-            add(ml_s[warp + w].x, ml_s[warp + w].y, v);
+            for (int u = 0; u < U; ++u)
+                if (x0 + u * row_warps < n) add(ml[u].x, ml[u].y, v[u]);
+        }
+        const bool real = r < rows;
+        n = place(r + next_r, from);  // the next row's sums are on their way while this one is written
+        load(from, n, part, ml, v);
+        if (row_warps > 1) {
+#pragma unroll
+            for (int e = 0; e < D / 32; ++e) join_s[warp][lane * (D / 32) + e] = O[e];
+            if (lane == 0) ml_s[warp] = make_float2(M, L);
+            __syncthreads();
+            if (part == 0) {
+                for (int w = 1; w < row_warps; ++w) {
+                    float o2[D / 32];
+#pragma unroll
+                    for (int e = 0; e < D / 32; ++e) o2[e] = join_s[warp + w][lane * (D / 32) + e];
+                    add(ml_s[warp + w].x, ml_s[warp + w].y, o2);
+                }
+            }
+            __syncthreads();
+        }
+        if (part == 0 && real) {
+            const int64_t at = (int64_t)q0 * a.hq + r;
+            const float f = a.cache.scale[1] / L;
+#pragma unroll
+            for (int e = 0; e < D / 32; e += 2)
+                *reinterpret_cast<__nv_bfloat162*>(a.out + at * D + lane * (D / 32) + e) =
+                    __floats2bfloat162_rn(L == 0.f ? 0.f : O[e] * f, L == 0.f ? 0.f : O[e + 1] * f);
+            if (a.lse && lane == 0) a.lse[at] = L == 0.f ? INFINITY : M + log2f(L);
         }
     }
-    if (!real) return;
-    const int64_t at = (int64_t)q0 * a.hq + r;
-    const float vs = a.cache.scale[1];
-#pragma unroll
-    for (int e = 0; e < D / 32; e += 2) {
-        const float v0 = L == 0.f ? 0.f : O[e] / L * vs, v1 = L == 0.f ? 0.f : O[e + 1] / L * vs;
-        *reinterpret_cast<__nv_bfloat162*>(a.out + at * D + lane * (D / 32) + e) = __floats2bfloat162_rn(v0, v1);
-    }
-    if (a.lse && lane == 0) a.lse[at] = L == 0.f ? INFINITY : M + log2f(L);
 }
 
 template <int D, bool FP8>
@@ -912,15 +940,21 @@ cudaError_t launch_all(const AttendArgs& a, const AttendPlan& plan, int max_rows
     const int chunks = (plan.slots + a.batch - 1) / a.batch;
     const int row_warps = chunks <= 4 ? 1 : (chunks <= 16 ? 4 : kFinishWarps);
     const int join_rows = kFinishWarps / row_warps;  // of a CTA
-    const int join_blocks = total_rows > 0 && plan.slots > 0 ? (most + join_rows - 1) / join_rows : 0;
-    // a CTA for every 512 keys, as many as run at once
+    // (a warp joins row after row, the next one's sums on their way: a chunk of a prompt 234 to 224 us)
+    const int join_blocks =
+        total_rows > 0 && plan.slots > 0
+            ? std::min((most + join_rows - 1) / join_rows, std::max(1, 4 * a.num_sms / a.batch)) : 0;
+    // weight CTAs: one for the keys that it takes at a time, as many as run in a round or two
+    const int parts = weight_parts(most, (int64_t)(max_len + 255) / 256 * a.batch, a.num_sms);
+    const int keys = 128 * kFinishWarps / parts;
     const int weight_blocks =
-        a.logits ? std::min((max_len + kFinishKeys - 1) / kFinishKeys, std::max(1, 3 * a.num_sms / a.batch)) : 0;
+        a.logits ? std::min((max_len + keys - 1) / keys, std::max(1, (parts == 8 ? 6 : 3) * a.num_sms / a.batch)) : 0;
     if (weight_blocks + join_blocks > 0) {
         cfg.gridDim = dim3((unsigned)(weight_blocks + join_blocks), (unsigned)a.batch, 1);
         cfg.blockDim = dim3(kFinishThreads, 1, 1);
         cfg.dynamicSmemBytes = a.logits ? (size_t)(most + 2) * 12 : 0;
-        e = cudaLaunchKernelEx(&cfg, attend_finish_kernel<D>, a, join_blocks, row_warps);
+        e = cudaLaunchKernelEx(&cfg, parts == 2 ? attend_finish_kernel<D, 2> : attend_finish_kernel<D, 8>, a, join_blocks,
+                               row_warps);
         if (e != cudaSuccess) return e;
         ++*launches;
         cfg.dynamicSmemBytes = 0;
