@@ -214,7 +214,7 @@ constexpr int kRingBytes = kAttWarps * kAttStages * 2 * Group<D>::kBytes;
 // which keeps addresses out of the lanes' registers: the sweep's 128 requests take 127 us
 // and not 135).
 template <int D, int NT_, bool FP8, bool WHOLE>
-__global__ void __launch_bounds__(kAttThreads) attend_split_kernel(const __grid_constant__ AttendArgs a)
+__global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_kernel(const __grid_constant__ AttendArgs a)
 {
     constexpr bool SINGLE = NT_ == 0;
     constexpr int NT = SINGLE ? 1 : NT_;
@@ -282,7 +282,11 @@ __global__ void __launch_bounds__(kAttThreads) attend_split_kernel(const __grid_
     int32_t next_page = page_of(kAttStages - 1);  // (read a span ahead: nothing waits for the table)
 
     // ---- the tile's rows
-    uint32_t qr[NT][D / 8];
+    // of 16 rows in shared memory: the registers go to sums and to contractions on their way (114.6 to 111.4 us
+    // for 1 to 8 queries of 32 requests, 32 / 8 heads; of 8 rows in registers: 68.2 and 69.0 the other way, four long requests)
+    constexpr bool IN_S = NT_ == 2;
+    __shared__ uint2 q_s[IN_S ? NT : 1][IN_S ? D / 16 : 1][32];
+    uint32_t qr[IN_S ? 1 : NT][D / 8];
     float fac[NT][2];  // log2-unit scale of rows 2c and 2c + 1
     int vis[NT][2];    // last key they see
 #pragma unroll
@@ -294,7 +298,13 @@ __global__ void __launch_bounds__(kAttThreads) attend_split_kernel(const __grid_
         const int64_t at =
             (int64_t)(q0 + i) * a.q_stride + (int64_t)(h * a.group + row - i * a.group) * D + c * (D / 4);
         float back;
-        load_q<D, FP8>(a.q, at, SINGLE || real, qr[t], back);
+        load_q<D, FP8>(a.q, at, SINGLE || real, qr[IN_S ? 0 : t], back);
+        if constexpr (IN_S) {
+            if (warp == t) {
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) q_s[t][k][lane] = make_uint2(qr[0][2 * k], qr[0][2 * k + 1]);
+            }
+        }
         if constexpr (SINGLE) {  // (every lane has read row 0; lane (g, c) keeps what lies in block g)
 #pragma unroll
             for (int k = 0; k < D / 8; ++k)
@@ -306,8 +316,10 @@ __global__ void __launch_bounds__(kAttThreads) attend_split_kernel(const __grid_
         for (int e = 0; e < 2; ++e) vis[t][e] = rt.last0 + rt.query(rt.row0 + t * 8 + 2 * c + e);
     }
     auto qf = [&](int t, int k) -> uint2 {
-        return make_uint2(qr[t][2 * k], qr[t][2 * k + 1]);
+        if constexpr (IN_S) return q_s[t][k][lane];
+        else return make_uint2(qr[t][2 * k], qr[t][2 * k + 1]);
     };
+    if constexpr (IN_S) __syncthreads();
 
     float o[NT][MT][4], m[NT][2], l[NT][2];
 #pragma unroll

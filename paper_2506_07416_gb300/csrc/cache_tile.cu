@@ -276,8 +276,6 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
         if (warp < live) {
             const uint32_t ts = tmem + lanes + 256 * rtile, to = ts + 128;
             const int vis = min(rt.last0 + query, k1 - 1);  // the last key that the row sees here
-            float* logits = a.logits ? a.logits + (((int64_t)b * a.cache.hkv + h) * a.max_rows + row) * a.logit_stride
-                                     : nullptr;
             const float2 fac2 = make_float2(fac, fac);
             // page of a tile's group of 16 keys (lanes 0 to 7); groups without one are as masked
             auto page_of = [&](int t) -> int32_t {
@@ -348,13 +346,6 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
                 const float2 nm2 = make_float2(-m, -m);
                 float2 s0 = make_float2(0.f, 0.f), s1 = make_float2(0.f, 0.f);
                 auto chunk_of = [&](int c0, const float* x) {
-                    if (logits && real && j0 + c0 < k1) {
-                        float4* out = reinterpret_cast<float4*>(logits + j0 + c0);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            __stcg(out + i, make_float4(x[4 * i] * fac, x[4 * i + 1] * fac, x[4 * i + 2] * fac,
-                                                        x[4 * i + 3] * fac));
-                    }
                     float p[16];
 #pragma unroll
                     for (int i = 0; i < 32; i += 4) {
