@@ -282,11 +282,7 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
     int32_t next_page = page_of(kAttStages - 1);  // (read a span ahead: nothing waits for the table)
 
     // ---- the tile's rows
-    // of 16 rows in shared memory: the registers go to sums and to contractions on their way (114.6 to 111.4 us
-    // for 1 to 8 queries of 32 requests, 32 / 8 heads; of 8 rows in registers: 68.2 and 69.0 the other way, four long requests)
-    constexpr bool IN_S = NT_ == 2;
-    __shared__ uint2 q_s[IN_S ? NT : 1][IN_S ? D / 16 : 1][32];
-    uint32_t qr[IN_S ? 1 : NT][D / 8];
+    uint32_t qr[NT][D / 8];
     float fac[NT][2];  // log2-unit scale of rows 2c and 2c + 1
     int vis[NT][2];    // last key they see
 #pragma unroll
@@ -298,13 +294,7 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
         const int64_t at =
             (int64_t)(q0 + i) * a.q_stride + (int64_t)(h * a.group + row - i * a.group) * D + c * (D / 4);
         float back;
-        load_q<D, FP8>(a.q, at, SINGLE || real, qr[IN_S ? 0 : t], back);
-        if constexpr (IN_S) {
-            if (warp == t) {
-#pragma unroll
-                for (int k = 0; k < D / 16; ++k) q_s[t][k][lane] = make_uint2(qr[0][2 * k], qr[0][2 * k + 1]);
-            }
-        }
+        load_q<D, FP8>(a.q, at, SINGLE || real, qr[t], back);
         if constexpr (SINGLE) {  // (every lane has read row 0; lane (g, c) keeps what lies in block g)
 #pragma unroll
             for (int k = 0; k < D / 8; ++k)
@@ -316,10 +306,8 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
         for (int e = 0; e < 2; ++e) vis[t][e] = rt.last0 + rt.query(rt.row0 + t * 8 + 2 * c + e);
     }
     auto qf = [&](int t, int k) -> uint2 {
-        if constexpr (IN_S) return q_s[t][k][lane];
-        else return make_uint2(qr[t][2 * k], qr[t][2 * k + 1]);
+        return make_uint2(qr[t][2 * k], qr[t][2 * k + 1]);
     };
-    if constexpr (IN_S) __syncthreads();
 
     float o[NT][MT][4], m[NT][2], l[NT][2];
 #pragma unroll
@@ -440,22 +428,25 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
         }
     };
 
-    // a group of 16 keys from j0 on; CHECK: some of the rows do not see all of them
-    auto group = [&](const uint8_t* grp, int j0, bool there, auto check) {
+    // a span of 32 keys from j0 on, two groups at a time (one after the other: 114 us where this takes 110, 1 to 8
+    // queries of 32 requests, 32 / 8 heads); `there`: their keys that have a page; CHECK: some of
+    // the rows do not see all of them
+    auto span_of = [&](const uint8_t* grp0, int j0, uint32_t there, auto check) {
         constexpr bool CHECK = decltype(check)::value;
-        if constexpr (SINGLE) {
-            group1(grp, j0, there, check);
-            return;
-        }
-        float s[NT][4];
-        score_group<D, NT>(grp, lane, qf, s);
+        float s[2][NT][4];
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int x = 0; x < 2; ++x) score_group<D, NT>(grp0 + x * G::kBytes, lane, qf, s[x]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                s[t][e] *= fac[t][e & 1];
-                if (CHECK && (!there || j0 + g + 8 * (e >> 1) > min(vis[t][e & 1], k1 - 1))) s[t][e] = -INFINITY;
-            }
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[x][t][e] *= fac[t][e & 1];
+                    if (CHECK && (!(there >> (16 * x) & 1u) ||
+                                  j0 + 16 * x + g + 8 * (e >> 1) > min(vis[t][e & 1], k1 - 1)))
+                        s[x][t][e] = -INFINITY;
+                }
         if (a.logits) {
             float* to = logits + j0 + g;
 #pragma unroll
@@ -463,21 +454,25 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
                     if (t * 8 + 2 * c + e < rt.rows) {
-                        __stcg(to + (t * 8 + e) * a.logit_stride, s[t][e]);
-                        __stcg(to + (t * 8 + e) * a.logit_stride + 8, s[t][e + 2]);
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            __stcg(to + (t * 8 + e) * a.logit_stride + 16 * x, s[x][t][e]);
+                            __stcg(to + (t * 8 + e) * a.logit_stride + 16 * x + 8, s[x][t][e + 2]);
+                        }
                     }
         }
         bool move = false;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) move |= fmaxf(s[t][e], s[t][e + 2]) > m[t][e] + kRefSlack;
+            for (int e = 0; e < 2; ++e)
+                move |= fmaxf(fmaxf(s[0][t][e], s[0][t][e + 2]), fmaxf(s[1][t][e], s[1][t][e + 2])) > m[t][e] + kRefSlack;
         if (__any_sync(0xffffffffu, move)) {
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float x = fmaxf(s[t][e], s[t][e + 2]);
+                    float x = fmaxf(fmaxf(s[0][t][e], s[0][t][e + 2]), fmaxf(s[1][t][e], s[1][t][e + 2]));
                     x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
                     x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
                     x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
@@ -492,60 +487,67 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
                     }
                 }
         }
-        uint32_t pb[NT][2];
+        uint32_t pb[2][NT][2];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            float p[4];
+        for (int x = 0; x < 2; ++x)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) p[e] = ex2(s[t][e] - m[t][e & 1]);
-            l[t][0] += p[0] + p[2];
-            l[t][1] += p[1] + p[3];
-            pb[t][0] = transpose8x8(pack_h2(p[0], p[1]));
-            pb[t][1] = transpose8x8(pack_h2(p[2], p[3]));
-        }
-        // ---- values: lane (g, c) takes keys 2c, 2c+1, 2c+8, 2c+9 and channels [g * D/8, (g + 1) * D/8)
-        constexpr int VW = D / 64;  // words of a lane's channels
-        uint32_t x[4][VW];
-        uint32_t sc[4];
+            for (int t = 0; t < NT; ++t) {
+                float p[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int key = 2 * c + (e & 1) + 8 * (e >> 1);
-            if constexpr (D == 128) {
-                const uint2 v = *reinterpret_cast<const uint2*>(grp + G::kV + key * 64 + g * 8);
-                x[e][0] = v.x, x[e][1] = v.y;
-                sc[e] = grp[G::kVs + key * 8 + g];
-            } else {
-                x[e][0] = *reinterpret_cast<const uint32_t*>(grp + G::kV + key * 32 + g * 4);
-                sc[e] = grp[G::kVs + key * 4 + g / 2];
+                for (int e = 0; e < 4; ++e) p[e] = ex2(s[x][t][e] - m[t][e & 1]);
+                l[t][0] += p[0] + p[2];
+                l[t][1] += p[1] + p[3];
+                pb[x][t][0] = transpose8x8(pack_h2(p[0], p[1]));
+                pb[x][t][1] = transpose8x8(pack_h2(p[2], p[3]));
             }
-            if constexpr (CHECK) {
-                // what lies behind the last key may be anything, a NaN scale among it
-                if (j0 + key >= k1) sc[e] = 0u;
-                // a NaN value must not reach the rows that do not see it (0 * NaN): put in at the end
-                if (j0 + key > all_see && (sc[e] & 0x7Fu) == 0x7Fu) {
-                    sc[e] = 0u;
-                    nan_value = true;
+        // ---- values: lane (g, c) takes keys 2c, 2c+1, 2c+8, 2c+9 and channels [g * D/8, (g + 1) * D/8)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const uint8_t* grp = grp0 + x * G::kBytes;
+            constexpr int VW = D / 64;  // words of a lane's channels
+            uint32_t w4[4][VW];
+            uint32_t sc[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int key = 2 * c + (e & 1) + 8 * (e >> 1);
+                if constexpr (D == 128) {
+                    const uint2 v = *reinterpret_cast<const uint2*>(grp + G::kV + key * 64 + g * 8);
+                    w4[e][0] = v.x, w4[e][1] = v.y;
+                    sc[e] = grp[G::kVs + key * 8 + g];
+                } else {
+                    w4[e][0] = *reinterpret_cast<const uint32_t*>(grp + G::kV + key * 32 + g * 4);
+                    sc[e] = grp[G::kVs + key * 4 + g / 2];
+                }
+                if constexpr (CHECK) {
+                    const int at = j0 + 16 * x + key;
+                    // what lies behind the last key may be anything, a NaN scale among it
+                    if (at >= k1) sc[e] = 0u;
+                    // a NaN value must not reach the rows that do not see it (0 * NaN): put in at the end
+                    if (at > all_see && (sc[e] & 0x7Fu) == 0x7Fu) {
+                        sc[e] = 0u;
+                        nan_value = true;
+                    }
                 }
             }
-        }
-        const __half2 sa = e4m3x2_value(sc[0] | (sc[1] << 8)), sb = e4m3x2_value(sc[2] | (sc[3] << 8));
+            const __half2 sa = e4m3x2_value(sc[0] | (sc[1] << 8)), sb = e4m3x2_value(sc[2] | (sc[3] << 8));
 #pragma unroll
-        for (int w = 0; w < VW; ++w) {
-            // bytes of (code of the first key, code of the second) for the even and the odd channels
-            const uint32_t lo = 0x0F0F0F0Fu;
-            const uint32_t ae = (x[0][w] & lo) | ((x[1][w] << 4) & ~lo), ao = ((x[0][w] >> 4) & lo) | (x[1][w] & ~lo);
-            const uint32_t be = (x[2][w] & lo) | ((x[3][w] << 4) & ~lo), bo = ((x[2][w] >> 4) & lo) | (x[3][w] & ~lo);
-            __half2 a0[4], a1[4], a2[4], a3[4];
-            e2m1x8_value(ae, a0);
-            e2m1x8_value(ao, a1);
-            e2m1x8_value(be, a2);
-            e2m1x8_value(bo, a3);
+            for (int w = 0; w < VW; ++w) {
+                // bytes of (code of the first key, code of the second) for the even and the odd channels
+                const uint32_t lo = 0x0F0F0F0Fu;
+                const uint32_t ae = (w4[0][w] & lo) | ((w4[1][w] << 4) & ~lo), ao = ((w4[0][w] >> 4) & lo) | (w4[1][w] & ~lo);
+                const uint32_t be = (w4[2][w] & lo) | ((w4[3][w] << 4) & ~lo), bo = ((w4[2][w] >> 4) & lo) | (w4[3][w] & ~lo);
+                __half2 a0[4], a1[4], a2[4], a3[4];
+                e2m1x8_value(ae, a0);
+                e2m1x8_value(ao, a1);
+                e2m1x8_value(be, a2);
+                e2m1x8_value(bo, a3);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t f0 = h2_bits(__hmul2(a0[i], sa)), f1 = h2_bits(__hmul2(a1[i], sa));
-                const uint32_t f2 = h2_bits(__hmul2(a2[i], sb)), f3 = h2_bits(__hmul2(a3[i], sb));
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t f0 = h2_bits(__hmul2(a0[i], sa)), f1 = h2_bits(__hmul2(a1[i], sa));
+                    const uint32_t f2 = h2_bits(__hmul2(a2[i], sb)), f3 = h2_bits(__hmul2(a3[i], sb));
 #pragma unroll
-                for (int t = 0; t < NT; ++t) mma16816(o[t][w * 4 + i], f0, f1, f2, f3, pb[t][0], pb[t][1]);
+                    for (int t = 0; t < NT; ++t) mma16816(o[t][w * 4 + i], f0, f1, f2, f3, pb[x][t][0], pb[x][t][1]);
+                }
             }
         }
     };
@@ -569,13 +571,20 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
         const uint8_t* span = my + stage * SPAN;
         stage = stage + 1 == kAttStages ? 0 : stage + 1;
         const uint32_t there = __ballot_sync(0xffffffffu, mine);
-        if (there == 0xFFFFFFFFu && j0 + 31 <= all_see) {
+        const bool all = there == 0xFFFFFFFFu && j0 + 31 <= all_see;
+        if constexpr (SINGLE) {
+            if (all) {
 #pragma unroll
-            for (int x = 0; x < 2; ++x) group(span + x * G::kBytes, j0 + 16 * x, true, std::false_type{});
-        } else {
+                for (int x = 0; x < 2; ++x) group1(span + x * G::kBytes, j0 + 16 * x, true, std::false_type{});
+            } else {
 #pragma unroll 1
-            for (int x = 0; x < 2; ++x)
-                if (j0 + 16 * x < k1) group(span + x * G::kBytes, j0 + 16 * x, there >> (16 * x) & 1u, std::true_type{});
+                for (int x = 0; x < 2; ++x)
+                    if (j0 + 16 * x < k1)
+                        group1(span + x * G::kBytes, j0 + 16 * x, there >> (16 * x) & 1u, std::true_type{});
+            }
+        } else {
+            if (all) span_of(span, j0, there, std::false_type{});
+            else span_of(span, j0, there, std::true_type{});
         }
     }
     copy_async_wait<0>();
