@@ -31,7 +31,7 @@ namespace {
 constexpr int kTileKeys = 128;
 // Barriers: operands of a stage written, operands of a stage read (two stages), and for each
 // of two row tiles scores there, probabilities there, their product there.
-enum { B_K_FULL = 0, B_V_FULL = 2, B_K_FREE = 4, B_V_FREE = 6, B_S_FULL = 8, B_P_FULL = 10, B_PV_DONE = 12, B_DRAIN = 14, B_COUNT };
+enum { B_K_FULL = 0, B_V_FULL = 2, B_K_FREE = 4, B_V_FREE = 6, B_S_FULL = 8, B_P_FULL = 10, B_PV_DONE = 12, B_DRAIN = 14, B_Q_FULL = 15, B_COUNT };
 
 // Warps of a CTA of NR row tiles: 4 NR for the rows, 4 for the values, 1 for the contractions.
 template <int NR>
@@ -70,61 +70,66 @@ __device__ __forceinline__ void st_shared16(uint32_t at, uint32_t a, uint32_t b,
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 
-// Row `row` of the tile as f16 into shared memory, scaled as in the kernel for few rows (a
-// power of two that puts its largest magnitude at about 2^10; NaN throughout where a channel
-// is infinite or NaN). Returns what undoes the scaling.
+// 32 rows of the tile (row0 + lane; my_at: where the lane's row starts in q, -1: zeros) as f16 into shared
+// memory, by a warp, scaled as in the kernel for few rows (a power of two that puts a row's largest magnitude at about
+// 2^10; NaN throughout where a channel is infinite or NaN). Returns what undoes the scaling of the lane's row. A
+// row's 16-byte parts go to neighbouring lanes, several rows on their way at once: with a row a lane a
+// CTA's start took so long that a chunk of a prompt was 218 us and not 199.
 template <int D, bool FP8>
-__device__ __forceinline__ float stage_q(const void* q, int64_t at, bool real, uint32_t q_s, int row)
+__device__ __forceinline__ float stage_rows(const void* q, int64_t my_at, uint32_t q_s, int row0)
 {
-    auto put = [&](int u, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {  // 8 channels
-        st_shared16(q_s + (u >> 3) * TileLayout<D, 1>::ATOM + row * 128 + (((u & 7) ^ (row & 7)) << 4), a, b, c, d);
-    };
-    if (!real) {
-#pragma unroll 4
-        for (int u = 0; u < D / 8; ++u) put(u, 0u, 0u, 0u, 0u);
-        return 1.f;
-    }
-    if constexpr (FP8) {
-        const uint4* s = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(q) + at);
-#pragma unroll 2
-        for (int i = 0; i < D / 16; ++i) {
-            const uint4 v = __ldg(s + i);
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-            uint32_t f[8];
+    constexpr int LANES = D * (FP8 ? 1 : 2) / 16, PER = 32 / LANES, STEPS = 32 / PER, U = STEPS < 8 ? STEPS : 8;
+    const int lane = threadIdx.x & 31, sub = lane % LANES;
+    float back = 1.f;
+#pragma unroll 1
+    for (int k0 = 0; k0 < STEPS; k0 += U) {
+        uint4 v[U];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                __half2 x[2];
-                e4m3x4_value(w[k], x);
-                f[2 * k] = h2_bits(x[0]), f[2 * k + 1] = h2_bits(x[1]);
+        for (int u = 0; u < U; ++u) {
+            const int64_t at = __shfl_sync(0xffffffffu, my_at, (k0 + u) * PER + lane / LANES);
+            v[u] = make_uint4(0u, 0u, 0u, 0u);
+            if (at >= 0)
+                v[u] = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(q) + at * (FP8 ? 1 : 2)) + sub);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int row = row0 + (k0 + u) * PER + lane / LANES;
+            auto put = [&](int x, uint32_t f0, uint32_t f1, uint32_t f2, uint32_t f3) {  // 8 channels
+                st_shared16(q_s + (x >> 3) * TileLayout<D, 1>::ATOM + row * 128 + (((x & 7) ^ (row & 7)) << 4), f0, f1, f2,
+                            f3);
+            };
+            const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+            if constexpr (FP8) {
+                uint32_t f[8];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    __half2 x[2];
+                    e4m3x4_value(w[k], x);
+                    f[2 * k] = h2_bits(x[0]), f[2 * k + 1] = h2_bits(x[1]);
+                }
+                put(2 * sub, f[0], f[1], f[2], f[3]);
+                put(2 * sub + 1, f[4], f[5], f[6], f[7]);
+            } else {
+                // the largest magnitude's bits (as integers they order the magnitudes, NaN above infinity above the rest)
+                uint32_t top = __vmaxu2(__vmaxu2(w[0] & 0x7FFF7FFFu, w[1] & 0x7FFF7FFFu),
+                                        __vmaxu2(w[2] & 0x7FFF7FFFu, w[3] & 0x7FFF7FFFu));
+                top = max(top & 0xFFFFu, top >> 16);
+#pragma unroll
+                for (int d = 1; d < LANES; d <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
+                const int e = min(264 - (int)(top >> 7), 253);
+                const float up = __int_as_float(top >= 0x7F80u ? 0x7FC00000 : e << 23);
+                uint32_t f[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    f[k] = pack_h2(__uint_as_float(w[k] << 16) * up, __uint_as_float(w[k] & 0xFFFF0000u) * up);
+                put(sub, f[0], f[1], f[2], f[3]);
+                const float mine =
+                    __shfl_sync(0xffffffffu, __int_as_float((254 - e) << 23), lane % PER * LANES);
+                if (lane / PER == k0 + u) back = mine;
             }
-            put(2 * i, f[0], f[1], f[2], f[3]);
-            put(2 * i + 1, f[4], f[5], f[6], f[7]);
         }
-        return 1.f;
-    } else {
-        const uint4* s = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(q) + at);
-        uint32_t top = 0u;
-#pragma unroll 4
-        for (int i = 0; i < D / 8; ++i) {
-            const uint4 v = __ldg(s + i);
-            top = __vmaxu2(__vmaxu2(top, v.x & 0x7FFF7FFFu), __vmaxu2(v.y & 0x7FFF7FFFu, v.z & 0x7FFF7FFFu));
-            top = __vmaxu2(top, v.w & 0x7FFF7FFFu);
-        }
-        top = max(top & 0xFFFFu, top >> 16);
-        const int e = min(264 - (int)(top >> 7), 253);
-        const float up = __int_as_float(top >= 0x7F80u ? 0x7FC00000 : e << 23);
-#pragma unroll 4
-        for (int i = 0; i < D / 8; ++i) {
-            const uint4 v = __ldg(s + i);
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-            uint32_t f[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                f[k] = pack_h2(__uint_as_float(w[k] << 16) * up, __uint_as_float(w[k] & 0xFFFF0000u) * up);
-            put(i, f[0], f[1], f[2], f[3]);
-        }
-        return __int_as_float((254 - e) << 23);
     }
+    return back;
 }
 
 // A thread's part of a tile's K: 32 channels (D = 64: 16) of each of four keys, 8 apart: of warp
@@ -243,6 +248,7 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
             mbar_init(BAR(B_PV_DONE + i), 1);
         }
         mbar_init(BAR(B_DRAIN), 1);
+        mbar_init(BAR(B_Q_FULL), 4 * (uint32_t)row_tiles);
         *abort_flag = 0;
         *nan_flag = 0;
         fence_mbar_init_cluster();
@@ -251,28 +257,29 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
         tmem_alloc(smem_u32(tmem_slot), 256 * NR);
         tmem_relinquish();
     }
-    // ---- the rows
-    const bool real = tid < rt.rows;  // (the softmax warps' threads)
-    const int row = rt.row0 + (real ? tid : 0), query = rt.query(row);
-    float fac = 0.f;
-    if (tid < 128 * NR) {
-        fac = a.c_log2 * stage_q<D, FP8>(a.q,
-                                         (int64_t)(q0 + query) * a.q_stride +
-                                             (int64_t)(h * a.group + row - query * a.group) * D,
-                                         real, base + L::Q + (tid >> 7) * L::ROWS, tid & 127);
-        fence_proxy_async_shared();
-    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = uniform(*tmem_slot);
     const Ctl ctl{abort_flag, a.err, a.wait_budget};
     float m = kNoRef, l = 0.f;
+    const bool real = tid < rt.rows;  // (the softmax warps' threads)
+    const int row = rt.row0 + (real ? tid : 0), query = rt.query(row);
 
     const int rtile = warp >> 2;  // the softmax warps' row tile
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     if (warp < SOFT) {
         // ---------------------------------------------------------------- softmax: a row a thread
+        float fac = 0.f;
+        if (rtile < row_tiles) {  // (rows that are not there are zeros)
+            const int64_t at =
+                (int64_t)(q0 + query) * a.q_stride + (int64_t)(h * a.group + row - query * a.group) * D;
+            fac = a.c_log2 *
+                  stage_rows<D, FP8>(a.q, real ? at : -1, base + L::Q + rtile * L::ROWS, (warp & 3) * 32);
+            fence_proxy_async_shared();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(BAR(B_Q_FULL));
+        }
         if (warp < live) {
             const uint32_t ts = tmem + lanes + 256 * rtile, to = ts + 128;
             const int vis = min(rt.last0 + query, k1 - 1);  // the last key that the row sees here
@@ -524,7 +531,7 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
             return true;
         };
         // while one row tile's scores become probabilities, the other's contractions run
-        bool ok = true;
+        bool ok = poll_phase_warp(BAR(B_Q_FULL), 0u, ctl);
         for (int r = 0; r < row_tiles && n_tiles > 0 && ok; ++r) ok = scores(r, 0);
         for (int t = 0; t < n_tiles && ok; ++t)
             for (int r = 0; r < row_tiles && ok; ++r) {
@@ -682,8 +689,8 @@ __global__ void __launch_bounds__(kTileThreads<1>, 2) attend_weight_kernel(const
     if (tid < 128) {
         const bool real = tid < rt.rows;
         const int row = rt.row0 + (real ? tid : 0), query = rt.query(row), head = h * a.group + row - query * a.group;
-        const float fac = a.c_log2 * stage_q<D, FP8>(a.q, (int64_t)(q0 + query) * a.q_stride + (int64_t)head * D, real,
-                                                     base + L::Q, tid);
+        const int64_t at = (int64_t)(q0 + query) * a.q_stride + (int64_t)head * D;
+        const float fac = a.c_log2 * stage_rows<D, FP8>(a.q, real ? at : -1, base + L::Q, warp * 32);
         row_s[tid] = real ? make_float2(fac, -__ldcg(a.lse + (int64_t)(q0 + query) * a.hq + head))
                           : make_float2(0.f, -INFINITY);  // (no probability)
         fence_proxy_async_shared();
