@@ -1013,7 +1013,11 @@ AttendPlan plan_cache_attend(int batch, int hkv, int group, const int32_t* q_off
     // The keys are split into n chunks a request where that fills the GPU better: items * n CTAs of
     // 1/n of the work run in rounds of as many as fit at once (by the kernels' registers and tensor
     // memory), and the writing and joining of a chunk's sums takes a CTA as long as about five
-    // keys for every four rows.
+    // keys for every four rows. A CTA of the kernel for many rows, alone on its SM or in a pair, takes as long
+    // as 700 keys to start and to end, and its chunks are joined in as long as 2.3 keys a row; its rounds are between
+    // the whole number and the fraction, as its CTAs' keys differ. (2 x 700 queries over 2048 keys, 32 / 8
+    // heads: whole 73 us, three chunks, as for few rows, 103; 1024 and 777 over up to 8191, 28 / 4 heads: 195 and
+    // 213; 512 over 8192, half the SMs: whole 129, two chunks 80.)
     const int64_t places = (int64_t)num_sms * (p.row_tile == 256 ? 1 : (p.row_tile == 128 ? 2 : (p.row_tile == 16 ? 3 : 4)));
     // (three rounds of smaller chunks for 9 to 32 rows, whose requests have different numbers of rows too)
     const int rounds = p.row_tile == 16 && batch > 1 ? 3 : 1;
@@ -1024,8 +1028,11 @@ AttendPlan plan_cache_attend(int batch, int hkv, int group, const int32_t* q_off
     } else if (items < 3 * places) {  // (from three rounds on the last one's idle places matter little)
         double cost = 1e30;
         for (int64_t n = 1; n <= std::min<int64_t>(units, 8); ++n) {
-            const double r = (double)((items * n + places - 1) / places);
-            const double c = r / (double)n + (n > 1 ? r * 1.25 * p.row_tile / (double)std::max<int64_t>(max_len, 1) : 0.0);
+            const bool many = p.row_tile >= 128;
+            const double whole = (double)((items * n + places - 1) / places);
+            const double r = many ? (whole + (double)(items * n) / (double)places) / 2.0 : whole;
+            const double more = (many ? 700.0 : 0.0) + (n > 1 ? (many ? 2.3 : 1.25) * p.row_tile : 0.0);
+            const double c = r / (double)n + r * more / (double)std::max<int64_t>(max_len, 1);
             if (c < cost) cost = c, best = n;
         }
     }

@@ -73,60 +73,57 @@ __device__ __forceinline__ void st_shared16(uint32_t at, uint32_t a, uint32_t b,
 // 32 rows of the tile (row0 + lane; my_at: where the lane's row starts in q, -1: zeros) as f16 into shared
 // memory, by a warp, scaled as in the kernel for few rows (a power of two that puts a row's largest magnitude at about
 // 2^10; NaN throughout where a channel is infinite or NaN). Returns what undoes the scaling of the lane's row. A
-// row's 16-byte parts go to neighbouring lanes, several rows on their way at once: with a row a lane a
-// CTA's start took so long that a chunk of a prompt was 218 us and not 199.
+// row's 16-byte parts go to neighbouring lanes, all rows on their way at once: with a row a lane a
+// CTA's start took several us more (a chunk of a prompt 218 and not 208 us).
 template <int D, bool FP8>
 __device__ __forceinline__ float stage_rows(const void* q, int64_t my_at, uint32_t q_s, int row0)
 {
-    constexpr int LANES = D * (FP8 ? 1 : 2) / 16, PER = 32 / LANES, STEPS = 32 / PER, U = STEPS < 8 ? STEPS : 8;
+    constexpr int LANES = D * (FP8 ? 1 : 2) / 16, PER = 32 / LANES, STEPS = 32 / PER;
     const int lane = threadIdx.x & 31, sub = lane % LANES;
     float back = 1.f;
-#pragma unroll 1
-    for (int k0 = 0; k0 < STEPS; k0 += U) {
-        uint4 v[U];
+    uint4 v[STEPS];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t at = __shfl_sync(0xffffffffu, my_at, (k0 + u) * PER + lane / LANES);
-            v[u] = make_uint4(0u, 0u, 0u, 0u);
-            if (at >= 0)
-                v[u] = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(q) + at * (FP8 ? 1 : 2)) + sub);
-        }
+    for (int u = 0; u < STEPS; ++u) {
+        const int64_t at = __shfl_sync(0xffffffffu, my_at, u * PER + lane / LANES);
+        v[u] = make_uint4(0u, 0u, 0u, 0u);
+        if (at >= 0)
+            v[u] = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(q) + at * (FP8 ? 1 : 2)) + sub);
+    }
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int row = row0 + (k0 + u) * PER + lane / LANES;
-            auto put = [&](int x, uint32_t f0, uint32_t f1, uint32_t f2, uint32_t f3) {  // 8 channels
-                st_shared16(q_s + (x >> 3) * TileLayout<D, 1>::ATOM + row * 128 + (((x & 7) ^ (row & 7)) << 4), f0, f1, f2,
-                            f3);
-            };
-            const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
-            if constexpr (FP8) {
-                uint32_t f[8];
+    for (int u = 0; u < STEPS; ++u) {
+        const int row = row0 + u * PER + lane / LANES;
+        auto put = [&](int x, uint32_t f0, uint32_t f1, uint32_t f2, uint32_t f3) {  // 8 channels
+            st_shared16(q_s + (x >> 3) * TileLayout<D, 1>::ATOM + row * 128 + (((x & 7) ^ (row & 7)) << 4), f0, f1, f2,
+                        f3);
+        };
+        const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+        if constexpr (FP8) {
+            uint32_t f[8];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    __half2 x[2];
-                    e4m3x4_value(w[k], x);
-                    f[2 * k] = h2_bits(x[0]), f[2 * k + 1] = h2_bits(x[1]);
-                }
-                put(2 * sub, f[0], f[1], f[2], f[3]);
-                put(2 * sub + 1, f[4], f[5], f[6], f[7]);
-            } else {
-                // the largest magnitude's bits (as integers they order the magnitudes, NaN above infinity above the rest)
-                uint32_t top = __vmaxu2(__vmaxu2(w[0] & 0x7FFF7FFFu, w[1] & 0x7FFF7FFFu),
-                                        __vmaxu2(w[2] & 0x7FFF7FFFu, w[3] & 0x7FFF7FFFu));
-                top = max(top & 0xFFFFu, top >> 16);
-#pragma unroll
-                for (int d = 1; d < LANES; d <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
-                const int e = min(264 - (int)(top >> 7), 253);
-                const float up = __int_as_float(top >= 0x7F80u ? 0x7FC00000 : e << 23);
-                uint32_t f[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    f[k] = pack_h2(__uint_as_float(w[k] << 16) * up, __uint_as_float(w[k] & 0xFFFF0000u) * up);
-                put(sub, f[0], f[1], f[2], f[3]);
-                const float mine =
-                    __shfl_sync(0xffffffffu, __int_as_float((254 - e) << 23), lane % PER * LANES);
-                if (lane / PER == k0 + u) back = mine;
+            for (int k = 0; k < 4; ++k) {
+                __half2 x[2];
+                e4m3x4_value(w[k], x);
+                f[2 * k] = h2_bits(x[0]), f[2 * k + 1] = h2_bits(x[1]);
             }
+            put(2 * sub, f[0], f[1], f[2], f[3]);
+            put(2 * sub + 1, f[4], f[5], f[6], f[7]);
+        } else {
+            // the largest magnitude's bits (as integers they order the magnitudes, NaN above infinity above the rest)
+            uint32_t top = __vmaxu2(__vmaxu2(w[0] & 0x7FFF7FFFu, w[1] & 0x7FFF7FFFu),
+                                    __vmaxu2(w[2] & 0x7FFF7FFFu, w[3] & 0x7FFF7FFFu));
+            top = max(top & 0xFFFFu, top >> 16);
+#pragma unroll
+            for (int d = 1; d < LANES; d <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
+            const int e = min(264 - (int)(top >> 7), 253);
+            const float up = __int_as_float(top >= 0x7F80u ? 0x7FC00000 : e << 23);
+            uint32_t f[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                f[k] = pack_h2(__uint_as_float(w[k] << 16) * up, __uint_as_float(w[k] & 0xFFFF0000u) * up);
+            put(sub, f[0], f[1], f[2], f[3]);
+            const float mine =
+                __shfl_sync(0xffffffffu, __int_as_float((254 - e) << 23), lane % PER * LANES);
+            if (lane / PER == u) back = mine;
         }
     }
     return back;
@@ -563,9 +560,11 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
     };
     const uint32_t to = tmem + lanes + 256 * (NR > 1 ? rtile : 0) + 128;
     if (warp < live && !*abort_flag) {  // (live <= 4 NR)
-        const int64_t at = (int64_t)(q0 + query) * a.hq + h * a.group + row - query * a.group;
-        const int64_t part = ((int64_t)blockIdx.x * a.cache.hkv + h) * a.max_rows + row;
-        const float f = a.slots > 0 ? 1.f : (l == 0.f ? 0.f : a.cache.scale[1] / l);
+        // through shared memory (the operands have been read), so that a store covers whole rows: 32 rows of
+        // a warp, padded to keep the lanes' rows in different banks
+        constexpr int PITCH = D + 4;
+        static_assert(NR * 4 * 32 * PITCH * 4 <= L::BAR, "the rows fit the operands' memory");
+        float* mine = reinterpret_cast<float*>(smem) + warp * 32 * PITCH;
 #pragma unroll 1
         for (int c0 = 0; c0 < D; c0 += 16) {
             float v[16];
@@ -576,27 +575,39 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
 #pragma unroll
                 for (int i = 0; i < 16; ++i) v[i] = 0.f;
             }
-            if (!real) continue;
-            if (*nan_flag && nan_block(c0 / 16, query)) {
+            if (real && *nan_flag && nan_block(c0 / 16, query)) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) v[i] = __int_as_float(0x7FC00000);
             }
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+                *reinterpret_cast<float4*>(mine + lane * PITCH + c0 + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+        }
+        __syncwarp();
+        const int64_t at = (int64_t)(q0 + query) * a.hq + h * a.group + row - query * a.group;
+        const int64_t part = ((int64_t)blockIdx.x * a.cache.hkv + h) * a.max_rows + row;
+        const float f = l == 0.f ? 0.f : a.cache.scale[1] / l;
+        const int rows = min(32, rt.rows - warp * 32);
+        constexpr int N = D / 32;  // channels of a lane
+#pragma unroll 4
+        for (int r = 0; r < rows; ++r) {
+            float v[N];
+#pragma unroll
+            for (int i = 0; i < N; i += 2)
+                *reinterpret_cast<float2*>(v + i) = *reinterpret_cast<const float2*>(mine + r * PITCH + lane * N + i);
             if (a.slots > 0) {
-                float4* out = reinterpret_cast<float4*>(a.part_o + part * D + c0);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) __stcg(out + i, make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]));
+                float* out = a.part_o + __shfl_sync(0xffffffffu, part, r) * D + lane * N;
+                if constexpr (N == 4) __stcg(reinterpret_cast<float4*>(out), make_float4(v[0], v[1], v[2], v[3]));
+                else __stcg(reinterpret_cast<float2*>(out), make_float2(v[0], v[1]));
             } else {
-                uint32_t o[8];
+                // (a row that sees no key is 0, whatever the columns hold)
+                const float fr = __shfl_sync(0xffffffffu, f, r);
+                const bool none = __shfl_sync(0xffffffffu, l, r) == 0.f;
+                __nv_bfloat16* out = a.out + __shfl_sync(0xffffffffu, at, r) * D + lane * N;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    // (a row that sees no key is 0, whatever the columns hold)
-                    const __nv_bfloat162 x =
-                        __floats2bfloat162_rn(l == 0.f ? 0.f : v[2 * k] * f, l == 0.f ? 0.f : v[2 * k + 1] * f);
-                    o[k] = *reinterpret_cast<const uint32_t*>(&x);
-                }
-                uint4* out = reinterpret_cast<uint4*>(a.out + at * D + c0);
-                out[0] = make_uint4(o[0], o[1], o[2], o[3]);
-                out[1] = make_uint4(o[4], o[5], o[6], o[7]);
+                for (int i = 0; i < N; i += 2)
+                    *reinterpret_cast<__nv_bfloat162*>(out + i) =
+                        __floats2bfloat162_rn(none ? 0.f : v[i] * fr, none ? 0.f : v[i + 1] * fr);
             }
         }
         if (real && a.slots > 0) a.part_ml[part] = make_float2(m, l);
