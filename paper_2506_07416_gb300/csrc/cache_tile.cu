@@ -206,7 +206,8 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
 
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = uniform(tid >> 5);
-    const int h = blockIdx.y % a.cache.hkv, tile = blockIdx.y / a.cache.hkv;
+    // the last rows, which see the most keys, first: 2048 queries over themselves 63 to 49 us, a chunk of a prompt 195 to 186
+    const int h = blockIdx.y % a.cache.hkv, tile = (gridDim.y - 1 - blockIdx.y) / a.cache.hkv;
     griddep_wait();
     griddep_launch_dependents();
     int b = blockIdx.z, chunk = INT32_MAX / 2, k0 = 0;
@@ -658,7 +659,7 @@ __global__ void __launch_bounds__(kTileThreads<1>, 2) attend_weight_kernel(const
 
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = uniform(tid >> 5);
-    const int h = blockIdx.y % a.cache.hkv, tile = blockIdx.y / a.cache.hkv;
+    const int h = blockIdx.y % a.cache.hkv, tile = (gridDim.y - 1 - blockIdx.y) / a.cache.hkv;
     griddep_wait();
     griddep_launch_dependents();
     int b = blockIdx.z, chunk = INT32_MAX / 2, k0 = 0;
