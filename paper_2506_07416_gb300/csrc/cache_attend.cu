@@ -25,14 +25,16 @@
 // What bounds it: a byte of codes costs instructions (its conversion to f16 pairs, loads,
 // contractions) beside its 1/6780 ns of memory, and registers limit an SM to 16 (one row, 8
 // rows) or 12 (16 rows) warps. By cases, all with weights:
-//   a token of 128 requests of about 1130, 32 heads (669 MB): 118 us and 10 for the weights;
-//     5.75 TB/s, issue 61%, the integer pipe 62%
-//   a token of four requests of 30 Ki to 131 Ki, 28 / 4 heads (217 MB): 50 + 22 us; 4.5 TB/s, issue 47%
-//   1 to 8 e4m3 queries of 32 requests, 32 / 8 heads (139 MB): 91 + 28 us; 2.6 TB/s with the kept
-//     scores, issue 37%: 12 warps do not cover one another's latencies
+//   a token of 128 requests of about 1130, 32 heads (669 MB): 118 us and 7 for the weights;
+//     5.75 TB/s, issue and the integer pipe 57%
+//   a token of four requests of 30 Ki to 131 Ki, 28 / 4 heads (217 MB): 50 + 18 us; 4.5 TB/s, issue 47%
+//   1 to 8 e4m3 queries of 32 requests, 32 / 8 heads (139 MB): 88 + 22 us; 2.7 TB/s with the kept
+//     scores, issue 38%: 12 warps do not cover one another's latencies, and requests of different rows
+//     leave a sixth of the SMs' time idle
 // Dropped: values from codes by masks and shifts (20 pairs a clock and SM; the conversion 50),
 // the weights from K read again (190 us of the first case where the kept scores take 10),
-// tiles of 32 rows (155 us of the third: 255 registers), rings of three spans (no change).
+// tiles of 32 rows (155 us of the third: 255 registers), rings of three spans (no change), two or four chains
+// of contractions a score (no change), 16 warps of 128 registers for tiles of 16 rows (123 us of the third).
 
 #include <algorithm>
 #include <type_traits>
@@ -213,6 +215,7 @@ constexpr int kRingBytes = kAttWarps * kAttStages * 2 * Group<D>::kBytes;
 // WHOLE: the keys are not split (the request is then known to be the same for a whole CTA,
 // which keeps addresses out of the lanes' registers: the sweep's 128 requests take 127 us
 // and not 135).
+// (CTAs of an SM as the plan of the split counts them.)
 template <int D, int NT_, bool FP8, bool WHOLE>
 __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_kernel(const __grid_constant__ AttendArgs a)
 {
@@ -992,10 +995,11 @@ cudaError_t launch_all(const AttendArgs& a, const AttendPlan& plan, int max_rows
 
 // Rows of a request's key head up to which the kernel for few rows is taken. A key costs it less
 // and it splits finer, but it makes a key's values again for every 16 rows; the other makes them once for
-// 128 or 256 rows and takes as long for fewer. 16 requests of 4096 keys, 32 / 8 heads: 12 rows 54 us
-// (other 60), 20 rows 72 (60), 36 rows 93 (60). One of 8000 keys: 20 rows 19.2 (18.8), 36 rows 21.7
-// (19.7). 32 ragged requests of 4 to 32 rows and 0 to 8191 keys: 119 (201). A call's rows are those of its
-// longest request, so the border lies where ragged calls gain more than even ones lose.
+// 128 or 256 rows, takes as long for fewer, and makes the scores twice where weights are wanted. 16 requests of
+// 4096 keys, 32 / 8 heads: 12 rows 53 us (other 50), with weights 63 (95); 20 rows 71 (51), with weights 84
+// (96); 32 rows 79 (51), 97.5 (96). One of 8000 keys: 20 rows 19.6 (19.7). 32 ragged requests of 4 to 32 rows and up to
+// 8200 keys: 88 (128), with weights 111 (243). A call's rows are those of its longest request, so the border
+// lies where ragged calls and those with weights gain more than the others lose.
 constexpr int kFewRows = 32;
 
 AttendPlan plan_cache_attend(int batch, int hkv, int group, const int32_t* q_off, int64_t max_len, int num_sms)

@@ -14,12 +14,15 @@
 //     reference moves only when a score passes it by 8; O is then rescaled in place.
 // What bounds it: the chain of a row tile. The exponentials take at least 1024 clocks of an
 // SM for 128 x 128, each contraction 516, and S, softmax and the product with V follow one
-// another: about 4100 clocks for a tile of 256 rows by 128 keys. So two row tiles are always in flight:
+// another: about 3600 clocks for a tile of 256 rows by 128 keys. So two row tiles are always in flight:
 //   NR = 1, up to 128 rows: two CTAs on an SM, 256 columns and at most 113 KB each, one stage of K and V
 //   NR = 2: one CTA with two row tiles, for which K and V are made once, in two stages
-// (192 rows of 16 requests of 4096 keys: 76 us with NR = 2 and 97 with 1). A chunk of a prompt, 1024
-// and 777 queries of 28 / 4 heads over up to 8191 keys (156 GFLOP): 200 us here and 30 of joining, the tensor
-// pipe active 40% of the time; with the contractions of the warp-wide instructions 617.
+// (192 rows of 16 requests of 4096 keys: 76 us with NR = 2 and 97 with 1). Start and end of a CTA take about as
+// long as seven of those tiles. A chunk of a prompt, 1024 and 777 queries of 28 / 4 heads over up to 8191 keys
+// (156 GFLOP): 186 us, the tensor pipe active half of the time; with the contractions of the warp-wide instructions 617.
+// Dropped for that chunk: P and the product by halves of a tile's keys (233 us where the whole took 224), S by
+// halves too (263), two threads a row (245 against 218), a quarter of the exponentials by a polynomial (241 against
+// 217): a warp's own latencies bound the softmax, and the warps share their SM with those that make the values.
 
 #include "cache_attend.cuh"
 #include "pipe.cuh"
@@ -629,7 +632,7 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
 // probabilities of one key over the columns, in order. The sums of a tile of rows are kept
 // for every key; attend_fold_kernel adds those of all tiles and heads, in order. Bound by the
 // exponentials and the contraction, as the first pass, with no second product: the chunk of a
-// prompt above takes 413 us with weights and 234 without (with rows as the contraction's rows and
+// prompt above takes 366 us with weights and 186 without (with rows as the contraction's rows and
 // sums over lanes about 3 ms).
 enum { W_K_FULL = 0, W_K_FREE = 2, W_S_FULL = 4, W_S_FREE = 6, W_DRAIN = 8, W_COUNT };
 
