@@ -669,7 +669,7 @@ litevlm_status_t litevlm_select_cache_attend(litevlm_select_t handle, int32_t ba
  * position); one of n_b <= budget keeps all. Kept rows of K, V and weights move,
  * in order and byte for byte, to the front of the table row.
  *   max_len      a bound of the lengths, as above
- *   budget       >= 1; sink, recent >= 0; sink + recent <= budget
+ *   budget       in [1, 2^30]; sink, recent >= 0; sink + recent <= budget
  *   to_table     device int32 [batch][to_width] or NULL. NULL: rows move within the
  *                request's own pages (no page belongs to two of the batch's requests).
  *                Else they move to these pages, which hold min(budget, max_len) tokens a

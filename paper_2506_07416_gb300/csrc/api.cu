@@ -1546,7 +1546,7 @@ litevlm_status_t litevlm_select_cache_evict(litevlm_select_t h, int32_t batch, c
     if (!h) return LITEVLM_ERR_INVALID_ARG;
     litevlm_status_t s = start_call(h, batch);
     if (s != LITEVLM_OK) return s;
-    if (budget < 1) return fail(h, LITEVLM_ERR_INVALID_ARG, "budget must be >= 1");
+    if (budget < 1 || budget > (1 << 30)) return fail(h, LITEVLM_ERR_INVALID_ARG, "budget must be in [1, 2^30]");
     if (sink < 0 || recent < 0 || (int64_t)sink + recent > budget)
         return fail(h, LITEVLM_ERR_INVALID_ARG, "sink and recent must be >= 0 and sink + recent <= budget");
     if (batch == 0) return LITEVLM_OK;

@@ -298,3 +298,16 @@ def test_a_workspace_beyond_every_size_is_refused(select):
         select.cache_attend_workspace(s.handle, 65535, off, 1 << 30)
     assert e.value.name == "UNSUPPORTED", str(e.value)
     s.close()
+
+
+def test_a_budget_whose_places_pass_32_bits_is_refused(select):
+    rng = np.random.default_rng(9)
+    s, c, w, table, _, _ = setup(select, rng)
+    cache, t, lens, kept, new = to_cache(select, c, w), i32(table), i32([200, 37, 90]), i32([0] * 3), i32([0] * 3)
+    for budget in ((1 << 30) + 1, 2 ** 31 - 1):  # (refused by the host: kept_idx is far too small for a launch)
+        with pytest.raises(select.LitevlmError) as e:
+            select.cache_evict(s.handle, 3, cache.struct, t, t.shape[1], lens, 200, budget, 0, 0, None, 0, cache.weights,
+                               kept, new, torch.cuda.current_stream().cuda_stream)
+        assert e.value.name == "INVALID_ARG", str(e.value)
+    s.check_device()
+    s.close()
