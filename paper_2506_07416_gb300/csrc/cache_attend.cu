@@ -943,20 +943,20 @@ cudaError_t launch_all(const AttendArgs& a, const AttendPlan& plan, int max_rows
             if (e != cudaSuccess) return e;
             ++*launches;
         } else {
-        cfg.gridDim = plan.slots > 0 ? dim3((unsigned)plan.slots, (unsigned)(tiles * a.cache.hkv), 1)
-                                     : dim3(1, (unsigned)(tiles * a.cache.hkv), (unsigned)a.batch);
-        cfg.blockDim = dim3(kAttThreads, 1, 1);
-        const bool whole = plan.slots == 0;
-        auto kern = max_rows == 1 ? (whole ? attend_split_kernel<D, 0, FP8, true> : attend_split_kernel<D, 0, FP8, false>)
-                    : plan.row_tile == 8
-                        ? (whole ? attend_split_kernel<D, 1, FP8, true> : attend_split_kernel<D, 1, FP8, false>)
-                        : attend_split_kernel<D, 2, FP8, false>;
-        cfg.dynamicSmemBytes = kRingBytes<D>;
-        static_assert(kRingBytes<D> + 10 * 1024 <= 48 * 1024, "no more shared memory than a launch has without asking");
-        e = cudaLaunchKernelEx(&cfg, kern, a);
-        if (e != cudaSuccess) return e;
-        ++*launches;
-        cfg.dynamicSmemBytes = 0;
+            cfg.gridDim = plan.slots > 0 ? dim3((unsigned)plan.slots, (unsigned)(tiles * a.cache.hkv), 1)
+                                         : dim3(1, (unsigned)(tiles * a.cache.hkv), (unsigned)a.batch);
+            cfg.blockDim = dim3(kAttThreads, 1, 1);
+            const bool whole = plan.slots == 0;
+            auto kern = max_rows == 1 ? (whole ? attend_split_kernel<D, 0, FP8, true> : attend_split_kernel<D, 0, FP8, false>)
+                        : plan.row_tile == 8
+                            ? (whole ? attend_split_kernel<D, 1, FP8, true> : attend_split_kernel<D, 1, FP8, false>)
+                            : attend_split_kernel<D, 2, FP8, false>;
+            cfg.dynamicSmemBytes = kRingBytes<D>;
+            static_assert(kRingBytes<D> + 10 * 1024 <= 48 * 1024, "no more shared memory than a launch has without asking");
+            e = cudaLaunchKernelEx(&cfg, kern, a);
+            if (e != cudaSuccess) return e;
+            ++*launches;
+            cfg.dynamicSmemBytes = 0;
         }
     }
     const int most = max_rows / a.group * a.hq;  // rows of the longest request
