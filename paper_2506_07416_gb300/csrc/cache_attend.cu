@@ -303,8 +303,8 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
             for (int k = 0; k < D / 8; ++k)
                 if (D == 128 ? g != 2 * c + k / 8 : g != c) qr[0][k] = 0u;
         }
-        fac[t][0] = a.c_log2 * __shfl_sync(0xffffffffu, back, 8 * c);
-        fac[t][1] = a.c_log2 * __shfl_sync(0xffffffffu, back, 8 * c + 4);
+        fac[t][0] = row_factor(a.c_log2, __shfl_sync(0xffffffffu, back, 8 * c));
+        fac[t][1] = row_factor(a.c_log2, __shfl_sync(0xffffffffu, back, 8 * c + 4));
 #pragma unroll
         for (int e = 0; e < 2; ++e) vis[t][e] = rt.last0 + rt.query(rt.row0 + t * 8 + 2 * c + e);
     }

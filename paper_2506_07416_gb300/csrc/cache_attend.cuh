@@ -9,6 +9,11 @@ namespace lvs {
 constexpr float kNoRef = -3.0e38f;   // reference of a row without keys so far
 constexpr float kRefSlack = 8.f;     // a score may pass its row's reference by this (2^8 is well inside f16)
 
+// What turns a row's products into scores in log2 units (`back` undoes the scaling of its query): not 0, where the
+// factors' product is below 32 bits, as for a query of zeros, whose back is 2^-126. Masked keys have a score of
+// -inf, which 0 would make NaN; at the smallest normal value every 2^s is 1 too (products are below 2^30).
+__device__ __forceinline__ float row_factor(float c_log2, float back) { return fmaxf(c_log2 * back, 0x1p-126f); }
+
 __device__ __forceinline__ uint32_t pack_h2(float lo, float hi) { return h2_bits(__floats2half2_rn(lo, hi)); }
 
 // How the keys are split, found by a warp from the lengths on the device: equal chunks, as

@@ -275,8 +275,8 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
         if (rtile < row_tiles) {  // (rows that are not there are zeros)
             const int64_t at =
                 (int64_t)(q0 + query) * a.q_stride + (int64_t)(h * a.group + row - query * a.group) * D;
-            fac = a.c_log2 *
-                  stage_rows<D, FP8>(a.q, real ? at : -1, base + L::Q + rtile * L::ROWS, (warp & 3) * 32);
+            fac = row_factor(a.c_log2, stage_rows<D, FP8>(a.q, real ? at : -1, base + L::Q + rtile * L::ROWS,
+                                                          (warp & 3) * 32));
             fence_proxy_async_shared();
             __syncwarp();
             if (lane == 0) mbar_arrive(BAR(B_Q_FULL));
@@ -332,7 +332,7 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
                     read(c0);
                     mx = fmaxf(mx, row_max<STEP>(v));
                 }
-                mx *= fac;  // (fac > 0)
+                mx *= fac;  // (fac > 0, see row_factor)
                 if (__any_sync(0xffffffffu, mx > m + kRefSlack)) {
                     const float mn = fmaxf(m, mx);
                     const float f = ex2(m - mn);
@@ -705,7 +705,7 @@ __global__ void __launch_bounds__(kTileThreads<1>, 2) attend_weight_kernel(const
         const bool real = tid < rt.rows;
         const int row = rt.row0 + (real ? tid : 0), query = rt.query(row), head = h * a.group + row - query * a.group;
         const int64_t at = (int64_t)(q0 + query) * a.q_stride + (int64_t)head * D;
-        const float fac = a.c_log2 * stage_rows<D, FP8>(a.q, real ? at : -1, base + L::Q, warp * 32);
+        const float fac = row_factor(a.c_log2, stage_rows<D, FP8>(a.q, real ? at : -1, base + L::Q, warp * 32));
         row_s[tid] = real ? make_float2(fac, -__ldcg(a.lse + (int64_t)(q0 + query) * a.hq + head))
                           : make_float2(0.f, -INFINITY);  // (no probability)
         fence_proxy_async_shared();
