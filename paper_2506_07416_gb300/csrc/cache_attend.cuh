@@ -9,10 +9,20 @@ namespace lvs {
 constexpr float kNoRef = -3.0e38f;   // reference of a row without keys so far
 constexpr float kRefSlack = 8.f;     // a score may pass its row's reference by this (2^8 is well inside f16)
 
-// What turns a row's products into scores in log2 units (`back` undoes the scaling of its query): not 0, where the
-// factors' product is below 32 bits, as for a query of zeros, whose back is 2^-126. Masked keys have a score of
-// -inf, which 0 would make NaN; at the smallest normal value every 2^s is 1 too (products are below 2^30).
-__device__ __forceinline__ float row_factor(float c_log2, float back) { return fmaxf(c_log2 * back, 0x1p-126f); }
+// What turns a row's products into scores in log2 units (`back` undoes the scaling of its query). Not 0, where the
+// factors' product is below 32 bits, as for a query of zeros, whose back is 2^-126: masked keys have a score of
+// -inf, which 0 would make NaN, and at the smallest normal value every 2^s is 1 too. And at most 2^90, so that no
+// score leaves fp32 (products are below 2^30): two sums that differ at all, by 2^-34 or more, are then 2^56
+// apart, and the softmax is as with any larger factor.
+__device__ __forceinline__ float row_factor(float c_log2, float back)
+{
+    return fminf(fmaxf(c_log2 * back, 0x1p-126f), 0x1p90f);
+}
+// Up to this factor a score stays below 2^22, and the rounding of a reference or an lse, by which the kernels with
+// a fused multiplication and subtraction move a whole row, is at most 2^-3. Beyond it they round each score as
+// its row's reference was rounded and subtract then: a reference of 2^33 is rounded by up to 2^9, and 2^512
+// is no number.
+constexpr float kFusedFactor = 0x1p-8f;
 
 __device__ __forceinline__ uint32_t pack_h2(float lo, float hi) { return h2_bits(__floats2half2_rn(lo, hi)); }
 

@@ -24,6 +24,8 @@
 // halves too (263), two threads a row (245 against 218), a quarter of the exponentials by a polynomial (241 against
 // 217): a warp's own latencies bound the softmax, and the warps share their SM with those that make the values.
 
+#include <type_traits>
+
 #include "cache_attend.cuh"
 #include "pipe.cuh"
 
@@ -284,7 +286,6 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
         if (warp < live) {
             const uint32_t ts = tmem + lanes + 256 * rtile, to = ts + 128;
             const int vis = min(rt.last0 + query, k1 - 1);  // the last key that the row sees here
-            const float2 fac2 = make_float2(fac, fac);
             // page of a tile's group of 16 keys (lanes 0 to 7); groups without one are as masked
             auto page_of = [&](int t) -> int32_t {
                 const int j = k0 + t * kTileKeys + lane * 16;
@@ -292,94 +293,104 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
                            ? cache_page(a.cache.table, a.cache.width, a.cache.num_pages, a.cache.page_shift, b, j)
                            : 0;
             };
-            int32_t next_page = page_of(0);
-            for (int t = 0; t < n_tiles; ++t) {
-                const int j0 = k0 + t * kTileKeys;
-                const uint32_t gone = __ballot_sync(0xffffffffu, next_page < 0);
-                next_page = page_of(t + 1);
-                const bool check = j0 + kTileKeys > min(k1, all_see + 1) || gone != 0;
-                if (!poll_phase_warp(BAR(B_S_FULL + rtile), (uint32_t)t & 1u, ctl)) break;
-                tc_fence_after();
-                // columns of a chunk of 32 that the row sees, as a mask
-                auto mask_of = [&](int c0) -> uint32_t {
-                    const int n = vis - (j0 + c0) + 1;
-                    uint32_t k = n >= 32 ? 0xFFFFFFFFu : (n <= 0 ? 0u : (1u << n) - 1u);
-                    if (gone >> (c0 / 16) & 1u) k &= 0xFFFF0000u;
-                    if (gone >> (c0 / 16 + 1) & 1u) k &= 0x0000FFFFu;
-                    return k;
-                };
-                // the columns, STEP at a time from the last on, read for their maximum; the first STEP
-                // are still there when the exponentials are made
-                constexpr int STEP = NR > 1 ? 64 : 32;
-                float mx = -INFINITY;
-                float v[STEP];
-                auto mask = [&](int c0, float* x) {
-                    const uint32_t k = mask_of(c0);
+            auto rows = [&](auto rounded) {  // rounded: the scores, as they are read
+                const float unit = rounded.value ? 1.f : fac;
+                const float2 fac2 = make_float2(unit, unit);
+                int32_t next_page = page_of(0);
+                for (int t = 0; t < n_tiles; ++t) {
+                    const int j0 = k0 + t * kTileKeys;
+                    const uint32_t gone = __ballot_sync(0xffffffffu, next_page < 0);
+                    next_page = page_of(t + 1);
+                    const bool check = j0 + kTileKeys > min(k1, all_see + 1) || gone != 0;
+                    if (!poll_phase_warp(BAR(B_S_FULL + rtile), (uint32_t)t & 1u, ctl)) break;
+                    tc_fence_after();
+                    // columns of a chunk of 32 that the row sees, as a mask
+                    auto mask_of = [&](int c0) -> uint32_t {
+                        const int n = vis - (j0 + c0) + 1;
+                        uint32_t k = n >= 32 ? 0xFFFFFFFFu : (n <= 0 ? 0u : (1u << n) - 1u);
+                        if (gone >> (c0 / 16) & 1u) k &= 0xFFFF0000u;
+                        if (gone >> (c0 / 16 + 1) & 1u) k &= 0x0000FFFFu;
+                        return k;
+                    };
+                    // the columns, STEP at a time from the last on, read for their maximum; the first STEP
+                    // are still there when the exponentials are made
+                    constexpr int STEP = NR > 1 ? 64 : 32;
+                    float mx = -INFINITY;
+                    float v[STEP];
+                    auto mask = [&](int c0, float* x) {
+                        const uint32_t k = mask_of(c0);
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) x[i] = k >> i & 1u ? x[i] : -INFINITY;
-                };
-                auto read = [&](int c0) {
+                        for (int i = 0; i < 32; ++i) x[i] = k >> i & 1u ? x[i] : -INFINITY;
+                    };
+                    auto read = [&](int c0) {
 #pragma unroll
-                    for (int x = 0; x < STEP; x += 32) tmem_ld32(ts + c0 + x, v + x);
-                    tmem_wait_ld();
-                    if (check) {
+                        for (int x = 0; x < STEP; x += 32) tmem_ld32(ts + c0 + x, v + x);
+                        tmem_wait_ld();
+                        if constexpr (rounded.value) {
 #pragma unroll
-                        for (int x = 0; x < STEP; x += 32) mask(c0 + x, v + x);
-                    }
-                };
-#pragma unroll 1
-                for (int c0 = kTileKeys - STEP; c0 >= 0; c0 -= STEP) {
-                    read(c0);
-                    mx = fmaxf(mx, row_max<STEP>(v));
-                }
-                mx *= fac;  // (fac > 0, see row_factor)
-                if (__any_sync(0xffffffffu, mx > m + kRefSlack)) {
-                    const float mn = fmaxf(m, mx);
-                    const float f = ex2(m - mn);
-                    m = mn;
-                    l *= f;
-                    if (t > 0) {  // (the product with the last tile's values is done: S came behind it)
-#pragma unroll 1
-                        for (int c0 = 0; c0 < D; c0 += 16) {
-                            float x[16];
-                            tmem_ld16(to + c0, x);
-                            tmem_wait_ld();
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) x[i] *= f;
-                            tmem_st16(to + c0, x);
+                            for (int i = 0; i < STEP; ++i) v[i] *= fac;
                         }
-                        tmem_wait_st();
-                    }
-                }
-                const float2 nm2 = make_float2(-m, -m);
-                float2 s0 = make_float2(0.f, 0.f), s1 = make_float2(0.f, 0.f);
-                auto chunk_of = [&](int c0, const float* x) {
-                    float p[16];
+                        if (check) {
 #pragma unroll
-                    for (int i = 0; i < 32; i += 4) {
-                        const float2 x0 = ffma2(make_float2(x[i], x[i + 1]), fac2, nm2);
-                        const float2 x1 = ffma2(make_float2(x[i + 2], x[i + 3]), fac2, nm2);
-                        const float2 p0 = make_float2(ex2(x0.x), ex2(x0.y)), p1 = make_float2(ex2(x1.x), ex2(x1.y));
-                        s0 = fadd2(s0, p0);
-                        s1 = fadd2(s1, p1);
-                        p[i / 2] = __uint_as_float(pack_h2(p0.x, p0.y));
-                        p[i / 2 + 1] = __uint_as_float(pack_h2(p1.x, p1.y));
-                    }
-                    tmem_st16(ts + c0 / 2, p);
-                };
-                // (P of columns c is written to the columns from c / 2 on, which have been read)
+                            for (int x = 0; x < STEP; x += 32) mask(c0 + x, v + x);
+                        }
+                    };
 #pragma unroll 1
-                for (int c0 = 0; c0 < kTileKeys; c0 += STEP) {
-                    if (c0 > 0) read(c0);
+                    for (int c0 = kTileKeys - STEP; c0 >= 0; c0 -= STEP) {
+                        read(c0);
+                        mx = fmaxf(mx, row_max<STEP>(v));
+                    }
+                    mx *= unit;  // (> 0, see row_factor)
+                    if (__any_sync(0xffffffffu, mx > m + kRefSlack)) {
+                        const float mn = fmaxf(m, mx);
+                        const float f = ex2(m - mn);
+                        m = mn;
+                        l *= f;
+                        if (t > 0) {  // (the product with the last tile's values is done: S came behind it)
+#pragma unroll 1
+                            for (int c0 = 0; c0 < D; c0 += 16) {
+                                float x[16];
+                                tmem_ld16(to + c0, x);
+                                tmem_wait_ld();
 #pragma unroll
-                    for (int x = 0; x < STEP; x += 32) chunk_of(c0 + x, v + x);
+                                for (int i = 0; i < 16; ++i) x[i] *= f;
+                                tmem_st16(to + c0, x);
+                            }
+                            tmem_wait_st();
+                        }
+                    }
+                    const float2 nm2 = make_float2(-m, -m);
+                    float2 s0 = make_float2(0.f, 0.f), s1 = make_float2(0.f, 0.f);
+                    auto chunk_of = [&](int c0, const float* x) {
+                        float p[16];
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4) {
+                            const float2 x0 = ffma2(make_float2(x[i], x[i + 1]), fac2, nm2);
+                            const float2 x1 = ffma2(make_float2(x[i + 2], x[i + 3]), fac2, nm2);
+                            const float2 p0 = make_float2(ex2(x0.x), ex2(x0.y)), p1 = make_float2(ex2(x1.x), ex2(x1.y));
+                            s0 = fadd2(s0, p0);
+                            s1 = fadd2(s1, p1);
+                            p[i / 2] = __uint_as_float(pack_h2(p0.x, p0.y));
+                            p[i / 2 + 1] = __uint_as_float(pack_h2(p1.x, p1.y));
+                        }
+                        tmem_st16(ts + c0 / 2, p);
+                    };
+                    // (P of columns c is written to the columns from c / 2 on, which have been read)
+#pragma unroll 1
+                    for (int c0 = 0; c0 < kTileKeys; c0 += STEP) {
+                        if (c0 > 0) read(c0);
+#pragma unroll
+                        for (int x = 0; x < STEP; x += 32) chunk_of(c0 + x, v + x);
+                    }
+                    l += (s0.x + s0.y) + (s1.x + s1.y);
+                    tmem_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(BAR(B_P_FULL + rtile));
                 }
-                l += (s0.x + s0.y) + (s1.x + s1.y);
-                tmem_wait_st();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(BAR(B_P_FULL + rtile));
-            }
+            };
+            if (__any_sync(0xffffffffu, fac > kFusedFactor)) rows(std::true_type{});
+            else rows(std::false_type{});
         }
     } else if (warp < MMA_WARP) {
         // ---------------------------------------------------------------- codes to values
@@ -640,7 +651,7 @@ template <int D>
 struct WeightLayout {
     static constexpr int ROWS = TileLayout<D, 1>::ROWS;
     static constexpr int Q = 0, K = ROWS;                   // two stages of K
-    static constexpr int CONST = 3 * ROWS;                  // scale and lse of every row
+    static constexpr int CONST = 3 * ROWS;                  // factor and lse of every row
     static constexpr int BAR = CONST + 128 * 8;
     static constexpr int MISC = BAR + 8 * W_COUNT;
     static constexpr int NEED = MISC + 16 + 1024;           // (at least 77 KB, as above)
@@ -683,7 +694,7 @@ __global__ void __launch_bounds__(kTileThreads<1>, 2) attend_weight_kernel(const
     const int seen = min(rt.len, rt.last0 + rt.query(rt.row0 + rt.rows - 1) + 1);
     const int k1 = min(seen, k0 + chunk);
     if (k0 >= k1) return;
-    const int all_see = rt.last0 + rt.query(rt.row0);
+    int all_see = rt.last0 + rt.query(rt.row0);
     const int n_tiles = uniform((k1 - k0 + kTileKeys - 1) / kTileKeys);
 
     if (tid == 0) {
@@ -701,6 +712,7 @@ __global__ void __launch_bounds__(kTileThreads<1>, 2) attend_weight_kernel(const
         tmem_alloc(smem_u32(tmem_slot), 256);
         tmem_relinquish();
     }
+    bool apart = false;  // a factor beyond kFusedFactor
     if (tid < 128) {
         const bool real = tid < rt.rows;
         const int row = rt.row0 + (real ? tid : 0), query = rt.query(row), head = h * a.group + row - query * a.group;
@@ -708,10 +720,13 @@ __global__ void __launch_bounds__(kTileThreads<1>, 2) attend_weight_kernel(const
         const float fac = row_factor(a.c_log2, stage_rows<D, FP8>(a.q, real ? at : -1, base + L::Q, warp * 32));
         row_s[tid] = real ? make_float2(fac, -__ldcg(a.lse + (int64_t)(q0 + query) * a.hq + head))
                           : make_float2(0.f, -INFINITY);  // (no probability)
+        apart = fac > kFusedFactor;
         fence_proxy_async_shared();
     }
     tc_fence_before();
-    __syncthreads();
+    // (no tile then counts as one that every row sees: the sums of the others round each score, then subtract the
+    // lse. With a branch of its own in the loop the chunk of a prompt took 377 to 380 us, so 373, without 369)
+    if (__syncthreads_or(apart)) all_see = -1;
     tc_fence_after();
     const uint32_t tmem = uniform(*tmem_slot);
     const Ctl ctl{abort_flag, a.err, a.wait_budget};
@@ -749,7 +764,8 @@ __global__ void __launch_bounds__(kTileThreads<1>, 2) attend_weight_kernel(const
 #pragma unroll
                     for (int i = 0; i < 32; i += 2) {
                         const float4 x = k[i / 2];
-                        const float p0 = ex2(fmaf(v[i], x.x, x.y)), p1 = ex2(fmaf(v[i + 1], x.z, x.w));
+                        const float p0 = ex2(__fadd_rn(__fmul_rn(v[i], x.x), x.y));
+                        const float p1 = ex2(__fadd_rn(__fmul_rn(v[i + 1], x.z), x.w));
                         sum.x += c0 + i >= from ? p0 : 0.f;
                         sum.y += c0 + i + 1 >= from ? p1 : 0.f;
                     }

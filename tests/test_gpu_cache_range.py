@@ -57,3 +57,58 @@ def test_zero_queries_and_scales_whose_product_is_below_32_bits(select, hq, hkv,
     g = cache.weights.double().cpu().numpy()
     assert (np.abs(g - wn) <= np.where(slack_w > 0, slack_w, 0)).all()
     s.close()
+
+
+@pytest.mark.parametrize("hq,hkv,d,lens,counts", ROWS)
+@pytest.mark.parametrize("dtype,k_scale,q_scale", [("bf16", 2.0 ** 14, 1.0), ("bf16", 2.0 ** 40, 1.0),
+                                                   ("bf16", 2.0 ** 60, 1.0), ("e4m3", 2.0 ** 60, 1e30)])
+def test_scores_beyond_24_bits(select, hq, hkv, d, lens, counts, dtype, k_scale, q_scale):  # noqa: F811
+    """The largest score takes all of a row where it leads by more than fp32 sums can be off (by 60 in log2 units and by
+    four times (d + 8) 2^-24 of the sum of the products' magnitudes); nowhere is anything but a number."""
+    if dtype == "e4m3" and d == 64:
+        pytest.skip("e4m3 heads have 128 channels")
+    rng = np.random.default_rng(hq + d + 7)
+    table, pool = tables(rng, lens, 16)
+    c = random_pool(rng, pool, hkv, 16, d, k_scale=k_scale)
+    off = offsets(counts)
+    x = rng.standard_normal((int(off[-1]), hq, d))
+    if dtype == "bf16":
+        x[1::3] *= 2.0 ** 60
+        x[2::3] *= 2.0 ** 120
+        q = torch.from_numpy(x).to(torch.bfloat16).cuda()
+        qv = q.double().cpu().numpy()
+    else:
+        q = torch.from_numpy(x).to(torch.float8_e4m3fn).view(torch.uint8).cuda()
+        qv = ref.E4M3[q.cpu().numpy()] * float(np.float32(q_scale))
+    w = np.zeros((pool, 16), np.float32)
+    cache = to_cache(select, c, w)
+    s = select.Selector(len(lens), 8, 8, hq, hkv, d, dtype)
+    out = s.cache_attend(cache, i32(table), i32(lens), q, i32(off), max(lens), q_scale=q_scale, accumulate=True)
+    s.check_device()
+    got, g = out.double().cpu().numpy(), cache.weights.double().cpu().numpy()
+    assert np.isfinite(got).all() and np.isfinite(g).all()
+    sure, most = np.zeros(w.shape), np.zeros(w.shape)
+    led = rows = 0
+    for b, n in enumerate(lens):
+        k, v = (ref.cached_rows(c, table, b, n, y) for y in "kv")
+        for i in range(counts[b]):
+            see = n - counts[b] + i + 1
+            place = table[b][np.arange(see) // 16], np.arange(see) % 16
+            for h in range(hq if see > 0 else 0):
+                kk, qq, rows = k[:see, h // (hq // hkv)], qv[off[b] + i, h], rows + 1
+                z = kk @ qq / math.sqrt(d) * math.log2(math.e)
+                top = int(z.argmax())
+                gap = z[top] - np.max(np.delete(z, top), initial=-np.inf)
+                room = 4 * (d + 8) * 2.0 ** -24 * (np.abs(kk) @ np.abs(qq)).max() / math.sqrt(d) * math.log2(math.e)
+                if gap <= max(60.0, room):
+                    most[place] += 1 / hq
+                    continue
+                led += 1
+                at = place[0][top], place[1][top]
+                sure[at] += 1 / hq
+                most[at] += 1 / hq
+                want = v[top, h // (hq // hkv)]
+                assert (np.abs(got[off[b] + i, h] - want) <= (2.0 ** -8 + 2.0 ** -18) * np.abs(want)).all()
+    assert led > 0.9 * rows
+    assert (g >= sure * (1 - 2.0 ** -18)).all() and (g <= most * (1 + 2.0 ** -18)).all()
+    s.close()
