@@ -48,9 +48,13 @@ namespace {
 constexpr int kAttWarps = 4;
 constexpr int kAttThreads = 32 * kAttWarps;
 constexpr int kAttStages = 2;        // spans of 32 keys of a warp's ring
-// of a single row, whose p * scale * 2^5 is at most 2^2 * 448 * 2^5 = 57344, inside f16; the
-// factor keeps small scales' products above f16's lower end
-constexpr float kRefSlack1 = 2.f, kBoost1 = 32.f;
+// Of a single row p times the scale is rounded to f16, times a power of two that follows the block's largest
+// scale so far: with e at or above the exponent field of that scale (below 1.875 * 2^(e - 7)) and p at most 2^2 the
+// product with 2^(20 - e) stays below 2^16, and what falls below f16's normal range is off by at most 2^-34 of the
+// largest value, whatever the scales' size. (With 2^5 throughout, which suits the largest scale, the smallest lost
+// p below 2^-20.) A larger scale moves e two beyond its field, so that this happens once or twice a warp: 128 requests
+// of about 1130 keys, 32 heads, 126 us so, 128 with e at the field, 125 with 2^5.
+constexpr float kRefSlack1 = 2.f, kBoost1 = 0x1p20f;  // (the factor for e = 0)
 
 // D += A B: 16 keys (or channels) x 8 rows, f16 operands, fp32 sums
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -323,6 +327,11 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
         l[t][0] = l[t][1] = 0.f;
     }
 
+    // SINGLE: the factor of block g of V, and what brings any larger exponent field of a scale, in the four bytes of a
+    // word, to the byte's highest bit: 0x78 - 8 e
+    float boost = kBoost1;
+    uint32_t room = 0x78787878u;
+
     float* logits = a.logits + (((int64_t)b * a.cache.hkv + h) * a.max_rows + rt.row0 + 2 * c) * a.logit_stride;
     bool nan_value = false;
 
@@ -374,7 +383,17 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
             __stcg(logits + j0 + g, z[0]);
             __stcg(logits + j0 + g + 8, z[1]);
         }
-        if (__any_sync(0xffffffffu, fmaxf(z[0], z[1]) > m[0][0] + kRefSlack1)) {
+        // scales of the lane's keys of the second product, a byte each
+        uint32_t scales = 0u;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int key = 2 * c + (e & 1) + 8 * (e >> 1);
+            uint32_t sc = grp[G::kVs + (D == 128 ? key * 8 + g : key * 4 + g / 2)];
+            if (CHECK && j0 + key >= k1) sc = 0u;  // (bytes behind the last key may be anything)
+            scales |= sc << (8 * e);
+        }
+        const bool larger = (((scales + room) | scales) & 0x80808080u) != 0u;
+        if (__any_sync(0xffffffffu, larger || fmaxf(z[0], z[1]) > m[0][0] + kRefSlack1)) {
             float x = fmaxf(z[0], z[1]);
             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
@@ -383,10 +402,25 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
             const float f = ex2(m[0][0] - mn);
             m[0][0] = mn;
             l[0][0] *= f;
+            float f0 = f, f1 = f;  // of the columns 2c and 2c + 1
+            if (__any_sync(0xffffffffu, larger)) {
+                const uint32_t fields = scales & 0x78787878u;
+                uint32_t e8 = max(max(fields & 0xFFu, (fields >> 8) & 0xFFu), max((fields >> 16) & 0xFFu, fields >> 24));
+                e8 = max(e8, __shfl_xor_sync(0xffffffffu, e8, 1));
+                e8 = max(e8, __shfl_xor_sync(0xffffffffu, e8, 2));
+                const uint32_t before = 0x78u - (room & 0xFFu);
+                e8 = e8 > before ? min(e8 + 16u, 0x78u) : before;
+                room = 0x01010101u * (0x78u - e8);
+                boost = __uint_as_float((147u - e8 / 8u) << 23);
+                const float less = __uint_as_float((127u - (e8 - before) / 8u) << 23);
+                f0 *= __shfl_sync(0xffffffffu, less, 8 * c);
+                f1 *= __shfl_sync(0xffffffffu, less, 8 * c + 4);
+            }
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[0][i][e] *= f;
+            for (int i = 0; i < MT; ++i) {
+                o[0][i][0] *= f0, o[0][i][1] *= f1;
+                o[0][i][2] *= f0, o[0][i][3] *= f1;
+            }
         }
         const float p0 = ex2(z[0] - m[0][0]), p1 = ex2(z[1] - m[0][0]);
         l[0][0] += p0 + p1;
@@ -397,24 +431,20 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
         pk[2] = __shfl_sync(0xffffffffu, p1, 8 * c);
         pk[3] = __shfl_sync(0xffffffffu, p1, 8 * c + 4);
         constexpr int VW = D / 64;
-        uint32_t x[4][VW], sc[4];
+        uint32_t x[4][VW];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int key = 2 * c + (e & 1) + 8 * (e >> 1);
             if constexpr (D == 128) {
                 const uint2 v = *reinterpret_cast<const uint2*>(grp + G::kV + key * 64 + g * 8);
                 x[e][0] = v.x, x[e][1] = v.y;
-                sc[e] = grp[G::kVs + key * 8 + g];
             } else {
                 x[e][0] = *reinterpret_cast<const uint32_t*>(grp + G::kV + key * 32 + g * 4);
-                sc[e] = grp[G::kVs + key * 4 + g / 2];
             }
-            if (CHECK && j0 + key >= k1) sc[e] = 0u;  // (bytes behind the last key may be anything)
         }
-        const float2 sa = __half22float2(e4m3x2_value(sc[0] | (sc[1] << 8)));
-        const float2 sb = __half22float2(e4m3x2_value(sc[2] | (sc[3] << 8)));
-        const uint32_t b0 = pack_h2(pk[0] * (sa.x * kBoost1), pk[1] * (sa.y * kBoost1));
-        const uint32_t b1 = pack_h2(pk[2] * (sb.x * kBoost1), pk[3] * (sb.y * kBoost1));
+        const float2 sa = __half22float2(e4m3x2_value(scales & 0xFFFFu)), sb = __half22float2(e4m3x2_value(scales >> 16));
+        const uint32_t b0 = pack_h2(pk[0] * (sa.x * boost), pk[1] * (sa.y * boost));
+        const uint32_t b1 = pack_h2(pk[2] * (sb.x * boost), pk[3] * (sb.y * boost));
 #pragma unroll
         for (int w = 0; w < VW; ++w) {
             const uint32_t lo = 0x0F0F0F0Fu;
@@ -620,10 +650,11 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
             }
         if (SINGLE && c == g >> 1) {  // column g holds the channels of lane g
             float* to = jo + warp * 8 * (D + 4) + g * (D / 8);
+            const float back = 1.f / boost;
 #pragma unroll
             for (int i = 0; i < MT; ++i)
-                *reinterpret_cast<float2*>(to + 2 * i) =
-                    g & 1 ? make_float2(o[0][i][1], o[0][i][3]) : make_float2(o[0][i][0], o[0][i][2]);
+                *reinterpret_cast<float2*>(to + 2 * i) = g & 1 ? make_float2(o[0][i][1] * back, o[0][i][3] * back)
+                                                               : make_float2(o[0][i][0] * back, o[0][i][2] * back);
         }
         __syncthreads();
         for (int x = tid; x < rows * D; x += kAttThreads) {
@@ -639,7 +670,6 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
                 L += s_l[w][row] * f;
                 O += jo[(w * 8 + r) * (D + 4) + ch] * f;
             }
-            if constexpr (SINGLE) O *= 1.f / kBoost1;
             const int rr = rt.row0 + row, i = rt.query(rr);
             const int64_t at = (int64_t)(q0 + i) * a.hq + h * a.group + rr - i * a.group;
             if (nan_value) {

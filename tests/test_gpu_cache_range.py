@@ -112,3 +112,64 @@ def test_scores_beyond_24_bits(select, hq, hkv, d, lens, counts, dtype, k_scale,
     assert led > 0.9 * rows
     assert (g >= sure * (1 - 2.0 ** -18)).all() and (g <= most * (1 + 2.0 ** -18)).all()
     s.close()
+
+
+def strict(slack, n, v_abs):
+    """cache_ref's slack without its term for probabilities below f16's normal range (n 2^-25 of the largest value)."""
+    return slack - n * 2.0 ** -25 * v_abs
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("at", [0, 300])
+def test_a_single_row_over_small_block_scales(select, d, at):  # noqa: F811
+    """One strong key and a flat tail whose probabilities are 2^-20 of its, values with the smallest block scales, in a
+    batch whose keys are not split: a probability's weight does not depend on the size of the scales it meets. What p
+    times the scale may be off by: 2^-11 (its rounding to f16), and 2^-34 of the largest value for a product below
+    f16's normal range. The request's tokens lie in two pages, of which the second is named again and again."""
+    rng = np.random.default_rng(d + at)
+    heads, batch, page, n = 32, 58, 256, 131072 + 300
+    table = np.full((batch, -(-n // page)), 1, np.int32)
+    table[0, at] = 0
+    lens = np.ones(batch, np.int64)
+    lens[0] = n
+    c = random_pool(rng, 2, heads, page, d, k_scale=1.0, v_scale=1.0)
+    c["k_codes"][:] = 0
+    c["k_codes"][0, :, 7] = 0x22  # 1.0 in every channel of the strong key
+    c["k_scales"][:] = 0x38
+    c["v_codes"] &= 0x77          # no negative values: the tail adds up
+    c["v_scales"][:] = 1 + np.arange(d // 16)
+    c["v_codes"][0, :, 7] = 0
+    q = torch.full((batch, heads, d), 20.4 * math.log(2) / math.sqrt(d)).to(torch.bfloat16).cuda()
+    s = select.Selector(batch, 8, 8, heads, heads, d, "bf16")
+    out = s.cache_attend(to_cache(select, c), i32(table), i32(lens), q, i32(np.arange(batch + 1)), n)
+    s.check_device()
+    v = ref.values(c["v_codes"], c["v_scales"], 1.0)  # [page, head, slot, d]
+    strong = math.exp(float(q[0, 0, 0]) * math.sqrt(d))
+    count = np.array([np.bincount(np.arange(n) % page, (table[0][np.arange(n) // page] == x)) for x in (0, 1)])
+    want = np.einsum("ps,phsd->hd", count, v) / (strong + n - 1)
+    delta = (d + 8) * 2.0 ** -24 * math.log(strong)
+    slack = (2.0 ** -8 + 2.0 ** -11 + 2 * delta + 2.0 ** -20) * want + n * 2.0 ** -34 * v.max()
+    assert (np.abs(out[0].double().cpu().numpy() - want) <= slack).all()
+    s.close()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_single_row_over_block_scales_of_every_size(select, d):  # noqa: F811
+    rng = np.random.default_rng(d)
+    lens = [700, 33, 400]
+    table, pool = tables(rng, lens, 32)
+    c = random_pool(rng, pool, 3, 32, d)
+    c["v_scales"] = rng.integers(0, 0x7F, c["v_scales"].shape, dtype=np.uint8)
+    c["v_scales"][:, 1, :, 0] = 0x7E   # the largest throughout
+    c["v_scales"][:, 1, :, 1] = rng.integers(0, 4, c["v_scales"].shape[0::2][:2], dtype=np.uint8)
+    for b, at in ((0, 650), (1, 32), (2, 3)):  # a large one among the smallest
+        c["v_scales"][table[b, at // 32], 1, at % 32, 1] = 0x78
+    q, qv, _ = make_q(rng, 3, 3, d, "bf16")
+    s = select.Selector(3, 8, 8, 3, 3, d, "bf16")
+    out = s.cache_attend(to_cache(select, c), i32(table), i32(lens), q, i32([0, 1, 2, 3]), 700)
+    s.check_device()
+    o, _, slack, _ = ref.attend(c, table, lens, qv, offsets([1, 1, 1]), 3)
+    for b, n in enumerate(lens):
+        top = np.abs(ref.cached_rows(c, table, b, n, "v")).max((0, 2))[:, None]
+        assert (np.abs(out[b].double().cpu().numpy() - o[b]) <= strict(slack[b], n, top) + n * 2.0 ** -34 * top).all()
+    s.close()
