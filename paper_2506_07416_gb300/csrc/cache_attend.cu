@@ -14,7 +14,7 @@
 // padding, where a contraction of the fifth generation takes 64 or 128 rows. Channels of a
 // contraction may come in any order, so a lane takes the 32 (QK) or 16 (PV) neighbouring
 // channels that one load brings. The rows' references
-// move only when a score passes them by 8 (2^8 is well inside f16); sums and
+// move only when a score passes them by 15 (see kRefBelow); sums and
 // statistics are fp32. P is rounded to f16 (11 bits) for the second product, the
 // output once to bf16 (8 bits).
 // attend_finish_kernel: the chunks of a row joined under the largest reference, and
@@ -509,7 +509,7 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
                     x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
                     x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
                     x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-                    const float mn = fmaxf(m[t][e], x);
+                    const float mn = fmaxf(m[t][e], x - kRefBelow);
                     const float f = ex2(m[t][e] - mn);
                     m[t][e] = mn;
                     l[t][e] *= f;

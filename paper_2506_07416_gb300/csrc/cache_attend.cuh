@@ -7,7 +7,11 @@
 namespace lvs {
 
 constexpr float kNoRef = -3.0e38f;   // reference of a row without keys so far
-constexpr float kRefSlack = 8.f;     // a score may pass its row's reference by this (2^8 is well inside f16)
+// A row's reference is put this much below its largest score so far and moves when a score passes it by kRefSlack: a
+// probability in f16, 2^(score - reference), then lies between 2^7 and 2^15 at the largest score and is off by at most
+// 2^-32 of it where it falls below f16's normal range. (With the reference at the largest score 2^-25: a million keys
+// of 2^-25 of the largest, 3% of a row's sum, were lost.)
+constexpr float kRefBelow = 7.f, kRefSlack = 15.f;
 
 // What turns a row's products into scores in log2 units (`back` undoes the scaling of its query). Not 0, where the
 // factors' product is below 32 bits, as for a query of zeros, whose back is 2^-126: masked keys have a score of

@@ -11,7 +11,7 @@
 //     are there, O += P V with P read from tensor memory;
 //   4 NR hold a row a thread: they read S twice (its largest score, then the
 //     exponentials), write P as f16 over S, and keep the row's reference and sum. A
-//     reference moves only when a score passes it by 8; O is then rescaled in place.
+//     reference moves only when a score passes it by 15; O is then rescaled in place.
 // What bounds it: the chain of a row tile. The exponentials take at least 1024 clocks of an
 // SM for 128 x 128, each contraction 516, and S, softmax and the product with V follow one
 // another: about 3600 clocks for a tile of 256 rows by 128 keys. So two row tiles are always in flight:
@@ -342,7 +342,7 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
                     }
                     mx *= unit;  // (> 0, see row_factor)
                     if (__any_sync(0xffffffffu, mx > m + kRefSlack)) {
-                        const float mn = fmaxf(m, mx);
+                        const float mn = fmaxf(m, mx - kRefBelow);
                         const float f = ex2(m - mn);
                         m = mn;
                         l *= f;

@@ -173,3 +173,49 @@ def test_a_single_row_over_block_scales_of_every_size(select, d):  # noqa: F811
         top = np.abs(ref.cached_rows(c, table, b, n, "v")).max((0, 2))[:, None]
         assert (np.abs(out[b].double().cpu().numpy() - o[b]) <= strict(slack[b], n, top) + n * 2.0 ** -34 * top).all()
     s.close()
+
+
+@pytest.mark.parametrize("hq,hkv,d,batch,t", [
+    (256, 32, 128, 58, 1),    # 8 rows a CTA
+    (64, 32, 64, 43, 8),      # 16
+    (256, 32, 128, 32, 8),    # 64
+    (256, 32, 128, 16, 20),   # 160
+])
+def test_a_flat_tail_behind_one_strong_key(select, hq, hkv, d, batch, t):  # noqa: F811
+    """One request of 2^20 tokens among short ones, in a batch whose keys are not split: a tail of probabilities of
+    2^-25.3 of the largest. Its tokens lie in two pages, of which the second is named again and again. Probabilities
+    are rounded to f16 (2^-11), those below its normal range by 2^-32 of the largest."""
+    rng = np.random.default_rng(t)
+    n, page = (1 << 20) + 77, 256
+    table = np.full((batch, -(-n // page)), 1, np.int32)
+    table[0, 0] = 0
+    lens = np.full(batch, t)
+    lens[0] = n
+    c = random_pool(rng, 2, hkv, page, d, k_scale=1.0, v_scale=0.125)
+    c["k_codes"][:] = 0
+    c["k_scales"][:] = 0x38
+    c["k_codes"][0, :, 0] = 0x22
+    c["v_codes"] &= 0x77
+    c["v_codes"][0, :, 0] = 0
+    q = torch.full((batch * t, hq, d), 25.3 * math.log(2) / math.sqrt(d)).to(torch.bfloat16).cuda()
+    s = select.Selector(batch, 8, 8, hq, hkv, d, "bf16")
+    out = s.cache_attend(to_cache(select, c), i32(table), i32(lens), q, i32(offsets([t] * batch)), n)
+    s.check_device()
+    v = ref.values(c["v_codes"], c["v_scales"], c["v_scale"])  # [page, head, slot, d]
+    strong = math.exp(float(q[0, 0, 0]) * math.sqrt(d))
+    pos = np.arange(n)
+    for i in (0, t - 1):
+        see = n - t + i + 1
+        first = min(see, page)
+        slots = np.bincount(pos[page:see] % page, minlength=page)
+        total = v[0, :, :first].sum(1) + np.einsum("s,hsd->hd", slots, v[1])
+        want = np.repeat(total / (strong + see - 1), hq // hkv, 0)
+        got = out[i].double().cpu().numpy()
+        delta = (d + 8) * 2.0 ** -24 * math.log(strong)
+        slack = (2.0 ** -8 + 2.0 ** -11 + 2 * delta + 2.0 ** -20) * want + see * 2.0 ** -32 * np.abs(v).max()
+        assert (np.abs(got - want) <= slack).all(), float((np.abs(got - want) / slack).max())
+    for b in range(1, batch):  # t tokens of the same score: the mean of those seen
+        for i in (0, t - 1):
+            want = np.repeat(v[1, :, :i + 1].mean(1), hq // hkv, 0)
+            assert (np.abs(out[b * t + i].double().cpu().numpy() - want) <= (2.0 ** -8 + 2.0 ** -10) * want + 1e-9).all()
+    s.close()
