@@ -16,6 +16,7 @@
 #include <vector>
 
 #include "../../include/litevlm_select.h"
+#include "cache_index.h"
 #include "internal.h"
 
 #ifdef LITEVLM_NVTX
@@ -1360,7 +1361,7 @@ litevlm_status_t attend_plan(litevlm_select_t h, int32_t batch, const int32_t* q
     const litevlm_select_config_t& c = h->cfg;
     litevlm_status_t s = check_offsets(h, q_offsets_h, batch, INT32_MAX, "q_offsets", total);
     if (s != LITEVLM_OK) return s;
-    if (max_len < 0 || max_len > (1 << 30))
+    if (max_len < 0 || max_len > lvs::kMostKeys)
         return fail(h, LITEVLM_ERR_INVALID_ARG, "max_len must be in [0, 2^30]");
     const int64_t group = c.num_q_heads / c.num_kv_heads;
     const int64_t rows = max_count(q_offsets_h, batch) * group;
@@ -1554,7 +1555,7 @@ litevlm_status_t litevlm_select_cache_evict(litevlm_select_t h, int32_t batch, c
     int32_t holds = 0;
     s = cache_pages(h, cache, table, table_width, seq_lens, &a.cache, &holds);
     if (s != LITEVLM_OK) return s;
-    if (max_len < 0 || max_len > holds || max_len > (1 << 30))
+    if (max_len < 0 || max_len > holds || max_len > lvs::kMostKeys)
         return fail(h, LITEVLM_ERR_INVALID_ARG, "max_len must be in [0, table_width * page_size] and at most 2^30");
     if (to_table && (to_width < 1 || (int64_t)to_width * cache->page_size < std::min(budget, max_len)))
         return fail(h, LITEVLM_ERR_INVALID_ARG, "to_width pages must hold min(budget, max_len) tokens");

@@ -240,7 +240,7 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
     griddep_wait();
     griddep_launch_dependents();
     // the request, and its part of the keys: all, or the chunk of this CTA's slot
-    int b = blockIdx.z, chunk = INT32_MAX / 2, k0 = 0;
+    int b = blockIdx.z, chunk = kMostKeys, k0 = 0;
     __shared__ int split_s[3];
     if (!WHOLE && a.slots > 0) {
         if (threadIdx.x < 32) {
@@ -260,7 +260,7 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
     const int i_last = rt.query(rt.row0 + rt.rows - 1);
     // keys that the tile's last row sees, and this CTA's part of them
     const int seen = min(rt.len, rt.last0 + i_last + 1);
-    const int k1 = min(seen, k0 + chunk);
+    const int k1 = chunk_end(seen, k0, chunk);
     if (k0 >= k1 && !WHOLE && a.slots > 0) return;  // (without chunks the tile's zeros are written here, else by the join)
     const int all_see = rt.last0 + rt.query(rt.row0);  // the last key that every row sees
 
@@ -784,7 +784,7 @@ __global__ void __launch_bounds__(kFinishThreads) attend_finish_kernel(const __g
     bool bad;
     const int len = cache_len(a.lens[b], a.limit, bad);
     const int q0 = a.q_off[b], t = a.q_off[b + 1] - q0;
-    int chunk = INT32_MAX / 2, slot0 = 0;
+    int chunk = kMostKeys, slot0 = 0;
     if (a.slots > 0 && t > 0 && len > 0) {
         const int2 v = __ldcg(a.split + b);
         chunk = v.x, slot0 = v.y;

@@ -54,7 +54,7 @@ __device__ __forceinline__ int chunk_keys(const AttendArgs& a)
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
     const long long mean = (total + a.slots - 1) / a.slots;
-    const int c = max(64, (int)min((long long)INT32_MAX / 2, (mean + mean * lane / 8 + 63) & ~63ll));
+    const int c = max(64, (int)min((long long)kMostKeys, (mean + mean * lane / 8 + 63) & ~63ll));
     // ceil(n / c) as that of (n - 1/2) / c: below 2^21 keys the product's error cannot reach a
     // whole number; longer requests count with a margin (never fewer chunks than there are)
     const float inv = 1.f / (float)c;

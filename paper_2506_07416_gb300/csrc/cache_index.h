@@ -13,6 +13,16 @@
 
 namespace lvs {
 
+// Tokens of the longest request that a call takes; as a chunk's length: all keys, the last of such a request among
+// them (a multiple of the 64 that every chunk is one of).
+constexpr int32_t kMostKeys = 1 << 30;
+
+// Where the chunk of keys from k0 on ends, of the `seen` keys there are (at or below k0: the chunk is empty).
+LVS_HD int32_t chunk_end(int32_t seen, int32_t k0, int32_t chunk)
+{
+    return seen - k0 < chunk ? seen : k0 + chunk;
+}
+
 // Tokens of a request that the kernels may touch: its length cut to
 // [0, limit]. `bad` tells that the length was outside.
 LVS_HD int cache_len(int32_t len, int32_t limit, bool& bad)

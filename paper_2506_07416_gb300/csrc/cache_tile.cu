@@ -215,7 +215,7 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
     const int h = blockIdx.y % a.cache.hkv, tile = (gridDim.y - 1 - blockIdx.y) / a.cache.hkv;
     griddep_wait();
     griddep_launch_dependents();
-    int b = blockIdx.z, chunk = INT32_MAX / 2, k0 = 0;
+    int b = blockIdx.z, chunk = kMostKeys, k0 = 0;
     __shared__ int split_s[3];
     if (a.slots > 0) {
         if (threadIdx.x < 32) {
@@ -233,7 +233,7 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
     if (rt.rows <= 0) return;
     const int q0 = a.q_off[b];
     const int seen = min(rt.len, rt.last0 + rt.query(rt.row0 + rt.rows - 1) + 1);
-    const int k1 = min(seen, k0 + chunk);
+    const int k1 = chunk_end(seen, k0, chunk);
     if (k0 >= k1 && a.slots > 0) return;  // (without chunks the tile's zeros are written here, else by the join)
     const int all_see = rt.last0 + rt.query(rt.row0);  // the last key that every row sees
     const int n_tiles = uniform(k1 > k0 ? (k1 - k0 + kTileKeys - 1) / kTileKeys : 0);
@@ -676,7 +676,7 @@ __global__ void __launch_bounds__(kTileThreads<1>, 2) attend_weight_kernel(const
     const int h = blockIdx.y % a.cache.hkv, tile = (gridDim.y - 1 - blockIdx.y) / a.cache.hkv;
     griddep_wait();
     griddep_launch_dependents();
-    int b = blockIdx.z, chunk = INT32_MAX / 2, k0 = 0;
+    int b = blockIdx.z, chunk = kMostKeys, k0 = 0;
     __shared__ int split_s[3];
     if (a.slots > 0) {
         if (threadIdx.x < 32) {
@@ -692,7 +692,7 @@ __global__ void __launch_bounds__(kTileThreads<1>, 2) attend_weight_kernel(const
     if (rt.rows <= 0) return;
     const int q0 = a.q_off[b];
     const int seen = min(rt.len, rt.last0 + rt.query(rt.row0 + rt.rows - 1) + 1);
-    const int k1 = min(seen, k0 + chunk);
+    const int k1 = chunk_end(seen, k0, chunk);
     if (k0 >= k1) return;
     int all_see = rt.last0 + rt.query(rt.row0);
     const int n_tiles = uniform((k1 - k0 + kTileKeys - 1) / kTileKeys);
