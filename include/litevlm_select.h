@@ -648,8 +648,10 @@ litevlm_status_t litevlm_select_cache_append(litevlm_select_t handle, int32_t ba
  * the product with V. The weights are added in a fixed order (the same inputs give
  * the same bits).
  * Errors: as for litevlm_select_cache_append; WORKSPACE for a workspace that is too
- * small; UNSUPPORTED where Hkv x row tiles of the longest request passes 65535, or the
- * workspace 2^60 bytes.
+ * small; UNSUPPORTED where the workspace passes 2^60 bytes, or Hkv x tiles of rows of the
+ * longest request 65535 (a row is a query with one of the G heads of a key head; a tile has
+ * 256 rows in calls of more than 128, with weights 128: 262016 queries at 32 / 32 heads
+ * with weights).
  */
 litevlm_status_t litevlm_select_cache_attend_workspace(litevlm_select_t handle, int32_t batch,
                                                        const int32_t* q_offsets_h, int32_t max_len, int32_t weights,

@@ -1356,7 +1356,7 @@ AttendSpace attend_space(const lvs::AttendPlan& plan, int64_t rows, int head_dim
 }
 
 litevlm_status_t attend_plan(litevlm_select_t h, int32_t batch, const int32_t* q_offsets_h, int32_t max_len,
-                             lvs::AttendPlan* plan, int64_t* total, int* max_rows)
+                             bool weights, lvs::AttendPlan* plan, int64_t* total, int* max_rows)
 {
     const litevlm_select_config_t& c = h->cfg;
     litevlm_status_t s = check_offsets(h, q_offsets_h, batch, INT32_MAX, "q_offsets", total);
@@ -1365,8 +1365,12 @@ litevlm_status_t attend_plan(litevlm_select_t h, int32_t batch, const int32_t* q
         return fail(h, LITEVLM_ERR_INVALID_ARG, "max_len must be in [0, 2^30]");
     const int64_t group = c.num_q_heads / c.num_kv_heads;
     const int64_t rows = max_count(q_offsets_h, batch) * group;
-    if (rows > INT32_MAX / 2 || (int64_t)c.num_kv_heads * ((rows + 7) / 8) > 65535)
-        return fail(h, LITEVLM_ERR_UNSUPPORTED, "num_kv_heads x rows of the longest request / 8 exceeds 65535");
+    // the grids' second dimension: key heads x row tiles, of the kernel that the plan takes and of the weights' pass
+    const auto ctas = [&](int64_t rows_of_a_cta) { return c.num_kv_heads * ((rows + rows_of_a_cta - 1) / rows_of_a_cta); };
+    if (rows > INT32_MAX / 2 || ctas(lvs::attend_row_tile(rows)) > 65535 ||
+        (weights && !lvs::attend_keeps_scores(rows, c.num_kv_heads) && ctas(128) > 65535))
+        return fail(h, LITEVLM_ERR_UNSUPPORTED,
+                    "num_kv_heads x the longest request's tiles of rows exceeds 65535");
     // the largest part of the workspace: a float for a key of every row (or 128 rows) of every key head
     if ((double)batch * c.num_kv_heads * (double)std::max<int64_t>(std::min<int64_t>(rows, 32), row_tiles((int)rows)) *
             ((double)max_len + 32.0) * 4.0 > 0x1p60)
@@ -1453,7 +1457,7 @@ litevlm_status_t litevlm_select_cache_attend_workspace(litevlm_select_t h, int32
     lvs::AttendPlan plan;
     int64_t total = 0;
     int max_rows = 0;
-    s = attend_plan(h, batch, q_offsets_h, max_len, &plan, &total, &max_rows);
+    s = attend_plan(h, batch, q_offsets_h, max_len, weights != 0, &plan, &total, &max_rows);
     if (s == LITEVLM_OK)
         *bytes = attend_space(plan, total * h->cfg.num_q_heads, h->cfg.head_dim,
                               h->cfg.num_kv_heads, max_rows, batch, max_len, weights != 0)
@@ -1476,7 +1480,7 @@ litevlm_status_t litevlm_select_cache_attend(litevlm_select_t h, int32_t batch, 
     lvs::AttendPlan plan;
     int64_t total = 0;
     int max_rows = 0;
-    s = attend_plan(h, batch, q_offsets_h, max_len, &plan, &total, &max_rows);
+    s = attend_plan(h, batch, q_offsets_h, max_len, weights_out != nullptr, &plan, &total, &max_rows);
     if (s != LITEVLM_OK || batch == 0) return s;
     lvs::AttendArgs a{};
     int32_t holds = 0;

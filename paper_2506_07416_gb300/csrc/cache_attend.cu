@@ -1032,15 +1032,21 @@ cudaError_t launch_all(const AttendArgs& a, const AttendPlan& plan, int max_rows
 // lies where ragged calls and those with weights gain more than the others lose.
 constexpr int kFewRows = 32;
 
+// 128 rows a CTA, or two row tiles that share the K and V that it makes: 192 rows 97 (one) and 72 us
+// (two), 256 rows 92 and 79.
+int attend_row_tile(int64_t max_rows) { return max_rows <= 8 ? 8 : (max_rows <= kFewRows ? 16 : (max_rows <= 128 ? 128 : 256)); }
+bool attend_keeps_scores(int64_t max_rows, int hkv)
+{
+    return max_rows > 0 && max_rows <= kFewRows && max_rows * hkv <= kLogitRows;
+}
+
 AttendPlan plan_cache_attend(int batch, int hkv, int group, const int32_t* q_off, int64_t max_len, int num_sms)
 {
     int max_t = 0;
     for (int b = 0; b < batch; ++b) max_t = std::max(max_t, q_off[b + 1] - q_off[b]);
     const int64_t max_rows = (int64_t)max_t * group;
     AttendPlan p;
-    // 128 rows a CTA, or two row tiles that share the K and V that it makes: 192 rows 97 (one) and 76 us
-    // (two), 256 rows 92 and 79.
-    p.row_tile = max_rows <= 8 ? 8 : (max_rows <= kFewRows ? 16 : (max_rows <= 128 ? 128 : 256));
+    p.row_tile = attend_row_tile(max_rows);
     int64_t items = 0;  // CTAs where each takes all keys of its rows
     for (int b = 0; b < batch; ++b)
         items += ((int64_t)(q_off[b + 1] - q_off[b]) * group + p.row_tile - 1) / p.row_tile * hkv;
@@ -1071,7 +1077,7 @@ AttendPlan plan_cache_attend(int batch, int hkv, int group, const int32_t* q_off
         }
     }
     p.slots = best > 1 ? (int32_t)std::min<int64_t>(best * batch, 1 << 20) : 0;
-    p.logits = max_rows > 0 && max_rows <= kFewRows && max_rows * hkv <= kLogitRows;
+    p.logits = attend_keeps_scores(max_rows, hkv);
     return p;
 }
 

@@ -186,6 +186,8 @@ struct AttendPlan {
     int32_t slots;
     bool logits;              // the weights are made from kept scores
 };
+int attend_row_tile(int64_t max_rows);                   // AttendPlan::row_tile for a longest request of so many rows
+bool attend_keeps_scores(int64_t max_rows, int hkv);     // AttendPlan::logits
 AttendPlan plan_cache_attend(int batch, int hkv, int group, const int32_t* q_off, int64_t max_len, int num_sms);
 cudaError_t launch_cache_attend(const AttendArgs& a, const AttendPlan& plan, int head_dim, bool fp8, int max_rows,
                                 int64_t total_rows, int max_len, cudaStream_t stream, int32_t* launches);

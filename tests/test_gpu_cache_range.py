@@ -219,3 +219,46 @@ def test_a_flat_tail_behind_one_strong_key(select, hq, hkv, d, batch, t):  # noq
             want = np.repeat(v[1, :, :i + 1].mean(1), hq // hkv, 0)
             assert (np.abs(out[b * t + i].double().cpu().numpy() - want) <= (2.0 ** -8 + 2.0 ** -10) * want + 1e-9).all()
     s.close()
+
+
+@pytest.mark.parametrize("weights", [False, True])
+def test_a_prompt_of_16384_queries(select, weights):  # noqa: F811
+    """A call's limit is that of the tiles its kernels take, 256 rows a CTA (128 with weights)."""
+    n, hq, d, page = 16384, 32, 64, 256
+    rng = np.random.default_rng(16)
+    c = random_pool(rng, n // page, hq, page, d)
+    table = np.arange(n // page, dtype=np.int32)[None]
+    cache = to_cache(select, c, np.zeros((n // page, page), np.float32))
+    q, _, _ = make_q(rng, n, hq, d, "bf16")
+    s = select.Selector(1, 8, 8, hq, hq, d, "bf16")
+    out = s.cache_attend(cache, i32(table), i32([n]), q, i32([0, n]), n, accumulate=weights)
+    s.check_device()
+    total = 0.0
+    for h in (0, 31):
+        k, v = (torch.from_numpy(ref.values(c[x + "_codes"][:, h], c[x + "_scales"][:, h], c[x + "_scale"])
+                                 .reshape(n, d)).cuda() for x in "kv")
+        for i in (0, 1, 255, 256, 9000, n - 1):
+            z = k[:i + 1] @ q[i, h].double() / math.sqrt(d)
+            p = torch.softmax(z, 0)
+            want = p @ v[:i + 1]
+            delta = (d + 8) * 2.0 ** -24 * (k[:i + 1].abs() @ q[i, h].double().abs()).max() / math.sqrt(d)
+            slack = 2.0 ** -8 * want.abs() + (2.0 ** -11 + 2 * delta + 2.0 ** -20) * (p @ v[:i + 1].abs()) + \
+                (i + 1) * 2.0 ** -25 * v.abs().max()
+            assert ((out[i, h].double() - want).abs() <= slack).all()
+    if weights:  # every query gives away 1 in all
+        total = float(cache.weights.double().sum())
+        assert abs(total - n) <= n * 2.0 ** -12
+    s.close()
+
+
+def test_the_limits_of_a_call_s_rows(select):  # noqa: F811
+    """65535 CTAs: 255 key heads by 257 tiles of 256 rows, or of 128 where weights are wanted."""
+    s = select.Selector(1, 8, 8, 255, 255, 128, "bf16")
+    space = lambda t, w: select.cache_attend_workspace(s.handle, 1, np.array([0, t], np.int32), 1000, w)  # noqa: E731
+    assert space(257 * 256, False) == 0  # (whole keys: nothing to join)
+    assert space(257 * 128, True) > 0
+    for t, w in ((257 * 256 + 1, False), (257 * 128 + 1, True)):
+        with pytest.raises(select.LitevlmError) as e:
+            space(t, w)
+        assert e.value.name == "UNSUPPORTED", str(e.value)
+    s.close()
