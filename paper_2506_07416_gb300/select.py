@@ -438,7 +438,17 @@ def _row_stride(name: str, t, dtype, heads: int, d: int, device: int) -> int:
 
 class KVCache:
     """The tensors of a 4-bit K/V cache (litevlm_cache_t), uint8 CUDA tensors: codes [pages, Hkv, page_size, d/2],
-    scales [pages, Hkv, page_size, d/16]; weights: float32 [pages, page_size] or None. ``Selector.cache`` makes one."""
+    scales [pages, Hkv, page_size, d/16]; weights: float32 [pages, page_size] or None. ``Selector.cache`` makes one.
+    The calls are given the tensors' addresses and the scales once, so none of them can be assigned to; ``weights`` can."""
+
+    def __setattr__(self, name, value):
+        if name == "weights":
+            if value is not None:
+                import torch
+                _want("weights", value, torch.float32, (self.num_pages, self.page_size), self.device)
+        elif "struct" in self.__dict__:
+            _refuse(f"{name} of a KVCache is fixed: make another one")
+        object.__setattr__(self, name, value)
 
     def __init__(self, k_codes, k_scales, v_codes, v_scales, k_scale: float = 1.0, v_scale: float = 1.0, weights=None):
         import torch
@@ -451,8 +461,6 @@ class KVCache:
         for name, t, shape in (("k_codes", k_codes, codes), ("v_codes", v_codes, codes), ("k_scales", k_scales, scales),
                                ("v_scales", v_scales, scales)):
             _want(name, t, torch.uint8, shape, self.device)
-        if weights is not None:
-            _want("weights", weights, torch.float32, (self.num_pages, self.page_size), self.device)
         self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
         self.k_scale, self.v_scale, self.weights = float(k_scale), float(v_scale), weights
         self._c = Cache(k_codes.data_ptr(), k_scales.data_ptr(), v_codes.data_ptr(), v_scales.data_ptr(),
