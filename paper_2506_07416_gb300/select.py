@@ -510,9 +510,10 @@ class Selector:
         self.heads, self.kv_heads, self.head_dim = num_q_heads, num_kv_heads, head_dim
         import torch
         self.device = torch.cuda.current_device()  # the one that create() took
-        self._space = {}  # workspaces of cache_attend by stream
+        self._space = None  # the stream and the workspace of the last cache_attend
 
     def close(self) -> None:
+        self._space = None
         if self.handle:
             destroy(self.handle)
             self.handle = None
@@ -696,16 +697,16 @@ class Selector:
         return cache.device
 
     def _workspace(self, need: int, stream, device):
-        """The handle's own workspace for calls on one stream; a call that is captured, or that has a stream of its
-        own, gets one that nothing else uses."""
+        """The handle's own workspace for calls on one stream after another (an earlier stream's goes back to the
+        allocator); a call that is captured, or that has a stream of its own, gets one that nothing else uses."""
         import torch
         if stream is not None or torch._C._cuda_isCurrentStreamCapturing():
             return torch.empty(need, dtype=torch.uint8, device=device)
         now = torch._C._cuda_getCurrentRawStream(device.index)
-        kept = self._space.get(now)
-        if kept is None or kept.shape[0] < need:
-            kept = self._space[now] = torch.empty(need, dtype=torch.uint8, device=device)
-        return kept
+        if self._space is None or self._space[0] != now or self._space[1].shape[0] < need:
+            self._space = None
+            self._space = (now, torch.empty(need, dtype=torch.uint8, device=device))
+        return self._space[1]
 
     def _element(self):
         import torch

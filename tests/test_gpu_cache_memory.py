@@ -40,3 +40,28 @@ def test_a_cache_s_tensors_and_scales_are_fixed(select):  # noqa: F811
     assert abs(float(cache.weights.double().sum()) - 1.0) < 1e-5
     s.check_device()
     s.close()
+
+
+def test_a_handle_keeps_one_workspace_and_gives_it_back(select):  # noqa: F811
+    rng = np.random.default_rng(2)
+    n = 60000
+    table, pool = tables(rng, [n], 16)
+    cache = to_cache(select, random_pool(rng, pool, 2, 16, 64), np.zeros((pool, 16), np.float32))
+    s = select.Selector(1, 8, 8, 32, 2, 64, "bf16")
+    q, _, _ = make_q(rng, 2, 32, 64, "bf16")
+    t, lens, off, off_h = i32(table), i32([n]), i32([0, 2]), offsets([2])
+    out = torch.empty((2, 32, 64), dtype=torch.bfloat16, device="cuda")
+    need = select.cache_attend_workspace(s.handle, 1, off_h, n)
+    assert need > 10 << 20
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    streams = [torch.cuda.Stream() for _ in range(4)]
+    for st in streams + streams:
+        with torch.cuda.stream(st):
+            s.cache_attend(cache, t, lens, q, off, n, accumulate=True, offsets_h=off_h, out=out)
+        st.synchronize()
+    held = torch.cuda.memory_allocated() - before
+    assert need <= held < 2 * need
+    s.check_device()
+    s.close()
+    assert torch.cuda.memory_allocated() == before
