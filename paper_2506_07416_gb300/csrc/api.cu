@@ -1339,19 +1339,18 @@ struct AttendSpace {
 };
 int64_t logit_stride(int32_t max_len) { return ((int64_t)max_len + 31) & ~(int64_t)31; }
 int row_tiles(int max_rows) { return (max_rows + 127) / 128; }
-// rows: of the call (query x head); max_rows: of the longest request (query x head of a key head)
+// rows: of the call (query x head of a key head); max_rows: of the longest request
 AttendSpace attend_space(const lvs::AttendPlan& plan, int64_t rows, int head_dim, int64_t hkv, int max_rows,
                          int32_t batch, int32_t max_len, bool weights)
 {
-    const int64_t head_rows = hkv * max_rows, head_tiles = hkv * row_tiles(max_rows);
     AttendSpace s{};
-    const int64_t parts = plan.slots * head_rows;
+    const int64_t parts = plan.slots * hkv * max_rows;
     s.part_ml = round256(parts * head_dim * 4);
     s.split = s.part_ml + round256(parts * 8);
     s.lse = s.split + (plan.slots > 0 ? round256((int64_t)batch * 8) : 0);
-    s.logits = s.lse + (weights ? round256(rows * 4) : 0);
-    const int64_t kept = plan.logits ? head_rows : head_tiles;  // rows of scores, or of their tiles' weights
-    s.total = s.logits + (weights ? round256(batch * kept * logit_stride(max_len) * 4) : 0);
+    s.logits = s.lse + (weights ? round256(rows * hkv * 4) : 0);
+    const int64_t kept = plan.logits ? rows : lvs::tile_at(rows, batch);  // rows of scores, or of their tiles' weights
+    s.total = s.logits + (weights ? round256(hkv * kept * logit_stride(max_len) * 4) : 0);
     return s;
 }
 
@@ -1365,14 +1364,15 @@ litevlm_status_t attend_plan(litevlm_select_t h, int32_t batch, const int32_t* q
         return fail(h, LITEVLM_ERR_INVALID_ARG, "max_len must be in [0, 2^30]");
     const int64_t group = c.num_q_heads / c.num_kv_heads;
     const int64_t rows = max_count(q_offsets_h, batch) * group;
+    const bool kept = lvs::attend_keeps_scores(rows, c.num_kv_heads);
     // the grids' second dimension: key heads x row tiles, of the kernel that the plan takes and of the weights' pass
     const auto ctas = [&](int64_t rows_of_a_cta) { return c.num_kv_heads * ((rows + rows_of_a_cta - 1) / rows_of_a_cta); };
     if (rows > INT32_MAX / 2 || ctas(lvs::attend_row_tile(rows)) > 65535 ||
-        (weights && !lvs::attend_keeps_scores(rows, c.num_kv_heads) && ctas(128) > 65535))
+        (weights && !kept && ctas(128) > 65535))
         return fail(h, LITEVLM_ERR_UNSUPPORTED,
                     "num_kv_heads x the longest request's tiles of rows exceeds 65535");
     // the largest part of the workspace: a float for a key of every row (or 128 rows) of every key head
-    if ((double)batch * c.num_kv_heads * (double)std::max<int64_t>(std::min<int64_t>(rows, 32), row_tiles((int)rows)) *
+    if ((double)c.num_kv_heads * (double)(kept ? *total * group : lvs::tile_at(*total * group, batch)) *
             ((double)max_len + 32.0) * 4.0 > 0x1p60)
         return fail(h, LITEVLM_ERR_UNSUPPORTED, "the workspace would pass 2^60 bytes");
     *max_rows = (int)rows;
@@ -1459,7 +1459,7 @@ litevlm_status_t litevlm_select_cache_attend_workspace(litevlm_select_t h, int32
     int max_rows = 0;
     s = attend_plan(h, batch, q_offsets_h, max_len, weights != 0, &plan, &total, &max_rows);
     if (s == LITEVLM_OK)
-        *bytes = attend_space(plan, total * h->cfg.num_q_heads, h->cfg.head_dim,
+        *bytes = attend_space(plan, total * (h->cfg.num_q_heads / h->cfg.num_kv_heads), h->cfg.head_dim,
                               h->cfg.num_kv_heads, max_rows, batch, max_len, weights != 0)
                      .total;
     return s;
@@ -1495,8 +1495,9 @@ litevlm_status_t litevlm_select_cache_attend(litevlm_select_t h, int32_t batch, 
         if (s != LITEVLM_OK) return s;
         if (!out || !aligned16(out)) return fail(h, LITEVLM_ERR_INVALID_ARG, "out must be 16-byte aligned and not NULL");
     }
-    const AttendSpace space = attend_space(plan, total * c.num_q_heads, c.head_dim,
-                                           c.num_kv_heads, max_rows, batch, max_len, weights_out != nullptr);
+    const int64_t rows = total * (c.num_q_heads / c.num_kv_heads);
+    const AttendSpace space = attend_space(plan, rows, c.head_dim, c.num_kv_heads, max_rows, batch, max_len,
+                                           weights_out != nullptr);
     if (workspace_bytes < space.total || (space.total > 0 && !workspace))
         return fail(h, LITEVLM_ERR_WORKSPACE, "the workspace must hold " + std::to_string(space.total) + " bytes");
     if (reinterpret_cast<uintptr_t>(workspace) & 255u)
@@ -1523,7 +1524,9 @@ litevlm_status_t litevlm_select_cache_attend(litevlm_select_t h, int32_t batch, 
     a.logits = weights_out && plan.logits ? reinterpret_cast<float*>(ws + space.logits) : nullptr;
     a.part_w = weights_out && !plan.logits ? reinterpret_cast<float*>(ws + space.logits) : nullptr;
     a.row_tiles = row_tiles(max_rows);
+    a.head_tiles = lvs::tile_at(rows, batch);
     a.max_rows = max_rows;
+    a.head_rows = rows;
     a.logit_stride = logit_stride(max_len);
     a.weights_in = weights_in;
     a.weights_out = weights_out;

@@ -332,7 +332,7 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
     float boost = kBoost1;
     uint32_t room = 0x78787878u;
 
-    float* logits = a.logits + (((int64_t)b * a.cache.hkv + h) * a.max_rows + rt.row0 + 2 * c) * a.logit_stride;
+    float* logits = a.logits + (h * a.head_rows + (int64_t)q0 * a.group + rt.row0 + 2 * c) * a.logit_stride;
     bool nan_value = false;
 
     // a group of 16 keys from j0 on, for a single row
@@ -829,7 +829,7 @@ __global__ void __launch_bounds__(kFinishThreads) attend_finish_kernel(const __g
             }
             if (!by_warp || lane == 0) {
                 lse_s[x] = lse;
-                row_s[x] = make_int2(h * a.max_rows + r, len - t + i);
+                row_s[x] = make_int2(h * (int)a.head_rows + r, len - t + i);
             }
         }
         __syncthreads();
@@ -849,7 +849,7 @@ __global__ void __launch_bounds__(kFinishThreads) attend_finish_kernel(const __g
             for (int e = 0; e < 4; ++e) before[e] = at >= 0 && j + e < len ? a.weights_in[at + e] : 0.f;
             float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
             if (j < len) {
-                const float* s = a.logits + (int64_t)b * a.cache.hkv * a.max_rows * a.logit_stride + j;
+                const float* s = a.logits + (int64_t)q0 * a.group * a.logit_stride + j;
                 sum = j0 + keys - 1 <= len - t ? add_weights<false>(s, a.logit_stride, row_s, lse_s, x0, x1, j)
                                                       : add_weights<true>(s, a.logit_stride, row_s, lse_s, x0, x1, j);
             }

@@ -23,6 +23,11 @@ LVS_HD int32_t chunk_end(int32_t seen, int32_t k0, int32_t chunk)
     return seen - k0 < chunk ? seen : k0 + chunk;
 }
 
+// First tile of 128 rows of request b, `rows` of whose batch stand before it, where every request's tiles follow the
+// last one's: a request of n rows has at most floor((rows + n) / 128) - floor(rows / 128) + 1. Of the batch's end: the
+// tiles of all.
+LVS_HD int64_t tile_at(int64_t rows, int64_t b) { return rows / 128 + b; }
+
 // Tokens of a request that the kernels may touch: its length cut to
 // [0, limit]. `bad` tells that the length was outside.
 LVS_HD int cache_len(int32_t len, int32_t limit, bool& bad)

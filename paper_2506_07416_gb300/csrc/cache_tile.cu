@@ -733,7 +733,7 @@ __global__ void __launch_bounds__(kTileThreads<1>, 2) attend_weight_kernel(const
 
     if (warp < 4) {
         // ---------------------------------------------------------------- sums: a key a thread
-        float* out = a.part_w + (((int64_t)b * a.cache.hkv + h) * a.row_tiles + tile) * a.logit_stride;
+        float* out = a.part_w + (h * a.head_tiles + tile_at((int64_t)q0 * a.group, b) + tile) * a.logit_stride;
         const uint32_t lanes = (uint32_t)(warp * 32) << 16;
         for (int t = 0; t < n_tiles; ++t) {
             const int st = t & 1, j = k0 + t * kTileKeys + tid;
@@ -846,13 +846,13 @@ __global__ void __launch_bounds__(kFoldThreads) attend_fold_kernel(const __grid_
         // the row tiles from the one on whose last row is the first that sees the key
         const int tiles = (rows + 127) / 128, query = max(0, j - (len - t));
         const int first = (int)((int64_t)query * a.group / 128);
-        const float* p = a.part_w + (int64_t)b * a.cache.hkv * a.row_tiles * a.logit_stride + j;
+        const float* p = a.part_w + tile_at((int64_t)a.q_off[b] * a.group, b) * a.logit_stride + j;
         const int n = max(0, tiles - first), all = n * a.cache.hkv, per = (all + 3) / 4;
         const int x0 = min(all, part * per), x1 = min(all, x0 + per);
         int h = n > 0 ? x0 / n : 0, r = first + (n > 0 ? x0 - h * n : 0);
 #pragma unroll 8
         for (int x = x0; x < x1; ++x) {
-            sum += __ldcg(p + ((int64_t)h * a.row_tiles + r) * a.logit_stride);
+            sum += __ldcg(p + (h * a.head_tiles + r) * a.logit_stride);
             if (++r == tiles) r = first, ++h;
         }
     }

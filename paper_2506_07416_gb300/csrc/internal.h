@@ -170,10 +170,12 @@ struct AttendArgs {
     float2* part_ml;          // [slots][hkv][max_rows] their references and sums of 2^s
     int2* split;              // [batch] chunk length and first slot of each request (slots > 0)
     float* lse;               // [rows * hq] log2 of the sum of 2^s (with weights)
-    float* logits;            // [batch][hkv][max_rows][logit_stride] scores in log2 units, or null
+    float* logits;            // [hkv][rows of the call][logit_stride] scores in log2 units, or null
     int32_t max_rows;         // rows (query x head of a key head) of the longest request
     int64_t logit_stride;
-    float* part_w;            // [batch][hkv][row_tiles][logit_stride] a row tile's weights (calls of many rows)
+    int64_t head_rows;        // rows of the call (query x head of a key head)
+    float* part_w;            // [hkv][head_tiles][logit_stride] a row tile's weights (calls of many rows)
+    int64_t head_tiles;       // tiles of 128 rows of all requests, at most (tile_at)
     int32_t row_tiles;        // tiles of 128 rows of the longest request
     const float* weights_in;  // [num_pages][page_size]
     float* weights_out;       // null: no weights

@@ -1,4 +1,5 @@
-"""The 4-bit cache's sizes at their limits, by the kernels' own header compiled here: chunks of a request's keys."""
+"""The 4-bit cache's sizes at their limits, by the kernels' own header compiled here: chunks of a request's keys, places of
+its tiles of rows."""
 import os
 import subprocess
 
@@ -30,6 +31,19 @@ int main()
         }
         if (k0 != n) return 4;
         if (lvs::chunk_end(n / 2, n, chunk) > n) return 5;  // behind the keys: empty
+    }
+    // the tiles of 128 rows of every request lie behind those of the last one, and inside those of all
+    for (int it = 0; it < 2000; ++it) {
+        const int batch = 1 + rand() % 40;
+        int64_t rows = 0, end = 0;
+        for (int b = 0; b < batch; ++b) {
+            const int64_t n = rand() % 4 == 0 ? 0 : (rand() % 4 == 0 ? 128 * (rand() % 9) : rand() % 1000);
+            const int64_t at = lvs::tile_at(rows, b);
+            if (at < end) return 6;
+            end = at + (n + 127) / 128;
+            rows += n;
+        }
+        if (end > lvs::tile_at(rows, batch)) return 7;
     }
     puts("ok");
     return 0;

@@ -65,3 +65,49 @@ def test_a_handle_keeps_one_workspace_and_gives_it_back(select):  # noqa: F811
     s.check_device()
     s.close()
     assert torch.cuda.memory_allocated() == before
+
+
+def test_the_workspace_follows_the_rows_of_a_call(select):  # noqa: F811
+    """Beside what joins the keys' chunks, weights take 4 bytes a row (up to 32 of the longest request's) or tile of 128
+    rows and key of max_len, of the call's rows and not of as many for every request as the longest has."""
+    most, hq, hkv = 8192, 32, 8
+    s = select.Selector(64, 8, 8, hq, hkv, 128, "bf16")
+    space = lambda counts, w: select.cache_attend_workspace(s.handle, len(counts), offsets(counts), most, w)  # noqa: E731
+    for counts in ([8] + [1] * 31, [1] * 64, [0] * 63 + [8], [8] * 32):
+        rows = sum(counts) * hq // hkv
+        assert space(counts, True) - space(counts, False) <= hkv * rows * (4 * most + 4) + 512, counts
+    for counts in ([1000] + [1] * 31, [0] * 40 + [9], [100] * 8):
+        rows = sum(counts) * hq // hkv
+        assert space(counts, True) - space(counts, False) <= hkv * ((rows // 128 + len(counts)) * 4 * most + 4 * rows) + 512
+    s.close()
+
+
+@pytest.mark.parametrize("counts", [[3, 0, 8, 1, 0], [70, 1, 0, 33, 129], [0, 0, 128, 256, 0], [1, 1, 1, 1, 40]])
+@pytest.mark.parametrize("hq,hkv", [(4, 4), (6, 2)])
+def test_a_request_s_weights_do_not_depend_on_the_others(select, counts, hq, hkv):  # noqa: F811
+    """Requests of different numbers of rows, some of none, in a workspace of just the bytes asked for: each request's
+    outputs and weights are those of the call alone, up to the rounding of other chunks of keys."""
+    rng = np.random.default_rng(sum(counts) + hq)
+    lens = [300, 50, 260, 401, 300]
+    table, pool = tables(rng, lens, 16)
+    w = np.exp(rng.standard_normal((pool, 16)) - 5).astype(np.float32)
+    cache = to_cache(select, random_pool(rng, pool, hkv, 16, 64), w)
+    s = select.Selector(5, 8, 8, hq, hkv, 64, "bf16")
+    off = offsets(counts)
+    q, _, _ = make_q(rng, int(off[-1]), hq, 64, "bf16")
+    bytes_ = select.cache_attend_workspace(s.handle, 5, off, 401)
+    room = torch.full((bytes_ + 4096,), 0xAB, dtype=torch.uint8, device="cuda")
+    nxt = torch.full((pool, 16), -1.0, device="cuda")
+    out = s.cache_attend(cache, i32(table), i32(lens), q, i32(off), 401, weights_out=nxt, offsets_h=off,
+                         workspace=room[:bytes_])
+    assert (room[bytes_:] == 0xAB).all()
+    for b, n in enumerate(lens):
+        one = torch.full((pool, 16), -1.0, device="cuda")
+        rows = slice(int(off[b]), int(off[b + 1]))
+        alone = s.cache_attend(cache, i32(table[b:b + 1]), i32([n]), q[rows], i32([0, counts[b]]), n, weights_out=one)
+        # both are off the exact values by at most 2^-8 + 2^-9 of the value and of the rounding of probabilities
+        assert torch.allclose(out[rows].float(), alone.float(), rtol=2.0 ** -7, atol=2.0 ** -8)
+        live = one >= 0
+        assert torch.allclose(nxt[live], one[live], rtol=2.0 ** -12, atol=0)
+    s.check_device()
+    s.close()
