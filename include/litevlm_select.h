@@ -601,9 +601,10 @@ typedef struct {
  *   weights          device float [num_pages][page_size] or NULL: set to 0 for the new tokens
  *   k_stored, v_stored  device bf16 [sum T_b][num_kv_heads][d] or NULL, 16-byte
  *                    aligned: the values that the cache now holds for the new rows
- *                    (rounded to bf16; exact where the scale is a power of two)
+ *                    (rounded to bf16; exact where the scale is a power of two); neither
+ *                    overlaps k, v or the other
  *   new_lens         device int32 [batch]: seq_lens[b] + T_b (not more than the
- *                    table row holds); not the array seq_lens
+ *                    table row holds); not overlapping seq_lens
  * A row whose position or source row is out of range is skipped (DEVICE_BOUNDS).
  * Errors: INVALID_ARG for sizes, pointers, strides or scales outside the above;
  * WORKSPACE for a batch beyond max_batch.
@@ -636,8 +637,8 @@ litevlm_status_t litevlm_select_cache_append(litevlm_select_t handle, int32_t ba
  *                    array: weights are added up in place. Two arrays: the sums go to
  *                    weights_out for every token of every request of the call, other
  *                    slots are left as they were (a speculative pass whose weights
- *                    may have to be forgotten)
- *   out              device bf16 [sum T_b][Hq][d], 16-byte aligned
+ *                    may have to be forgotten); they do not overlap
+ *   out              device bf16 [sum T_b][Hq][d], 16-byte aligned, not overlapping q
  *   workspace        device, at least the bytes that
  *                    litevlm_select_cache_attend_workspace gives for the same batch,
  *                    offsets and max_len (weights: 1 for a call with weights, which
@@ -680,7 +681,7 @@ litevlm_status_t litevlm_select_cache_attend(litevlm_select_t handle, int32_t ba
  *   weights      device float [num_pages][page_size]
  *   kept_idx     device int32 [batch][budget]: the kept positions, ascending; -1 behind
  *                the last
- *   new_lens     device int32 [batch]: min(n_b, budget); not the array seq_lens
+ *   new_lens     device int32 [batch]: min(n_b, budget); not overlapping seq_lens
  * Errors: as above.
  */
 litevlm_status_t litevlm_select_cache_evict(litevlm_select_t handle, int32_t batch, const litevlm_cache_t* cache,
@@ -708,7 +709,8 @@ litevlm_status_t litevlm_select_cache_evict(litevlm_select_t handle, int32_t bat
  *   u_accept         device float [sum T_b], u_sample device float [batch], in [0, 1)
  *   accepted         device int32 [batch]
  *   tokens           device int32 [sum T_b + batch]: request b's accepted drafts, the
- *                    sampled token, then -1, from row draft_offsets[b] + b on
+ *                    sampled token, then -1, from row draft_offsets[b] + b on; not
+ *                    overlapping draft_tokens
  * A drafted token outside [0, vocab) is refused (DEVICE_BOUNDS). Needs none of the
  * handle's head sizes. Errors: INVALID_ARG / WORKSPACE as above.
  */

@@ -1262,6 +1262,18 @@ struct OnDevice {
     }
 };
 
+// Whether two ranges of memory have a byte in common (an empty or absent one has none).
+bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return a && b && a_bytes > 0 && b_bytes > 0 && x < y + (uint64_t)b_bytes && y < x + (uint64_t)a_bytes;
+}
+// Bytes from the first of `rows` rows of `row` elements, `stride` apart, to the end of the last.
+int64_t span_bytes(int64_t rows, int64_t stride, int64_t row, int64_t esize)
+{
+    return rows > 0 ? ((rows - 1) * stride + row) * esize : 0;
+}
+
 bool in_range(float scale) { return scale >= 0x1p-60f && scale <= 0x1p60f; }
 
 litevlm_status_t start_call(litevlm_select_t h, int32_t batch)
@@ -1403,7 +1415,8 @@ litevlm_status_t litevlm_select_cache_append(litevlm_select_t h, int32_t batch, 
     s = cache_pages(h, cache, table, table_width, seq_lens, &a.cache, &a.limit);
     if (s != LITEVLM_OK) return s;
     if (!new_offsets_d || !new_lens) return fail(h, LITEVLM_ERR_INVALID_ARG, "a device pointer is NULL");
-    if (new_lens == seq_lens) return fail(h, LITEVLM_ERR_INVALID_ARG, "new_lens must not be the array seq_lens");
+    if (overlap(new_lens, (int64_t)batch * 4, seq_lens, (int64_t)batch * 4))
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "new_lens must not overlap seq_lens");
     if (src_rows < 0 || (!row_idx && src_rows < rows))
         return fail(h, LITEVLM_ERR_INVALID_ARG, "k and v have fewer rows than the call appends");
     if (rows > 0) {
@@ -1414,6 +1427,14 @@ litevlm_status_t litevlm_select_cache_append(litevlm_select_t h, int32_t batch, 
             return fail(h, LITEVLM_ERR_INVALID_ARG, "k_in_scale and v_in_scale must be in [2^-60, 2^60]");
         if ((k_stored && !aligned16(k_stored)) || (v_stored && !aligned16(v_stored)))
             return fail(h, LITEVLM_ERR_INVALID_ARG, "k_stored and v_stored must be 16-byte aligned");
+        const int64_t row = (int64_t)h->cfg.num_kv_heads * h->cfg.head_dim, stored = rows * row * 2;
+        const int64_t esize = h->cfg.qk_dtype == LITEVLM_FP8_E4M3 ? 1 : 2;
+        const int64_t k_bytes = span_bytes(src_rows, k_row_stride, row, esize);
+        const int64_t v_bytes = span_bytes(src_rows, v_row_stride, row, esize);
+        if (overlap(k_stored, stored, v_stored, stored) || overlap(k_stored, stored, k, k_bytes) ||
+            overlap(k_stored, stored, v, v_bytes) || overlap(v_stored, stored, k, k_bytes) ||
+            overlap(v_stored, stored, v, v_bytes))
+            return fail(h, LITEVLM_ERR_INVALID_ARG, "k_stored and v_stored must not overlap k, v or one another");
     }
     s = debug_mirror(h, new_offsets_d, new_offsets_h, (int64_t)batch + 1, "new_offsets", stream);
     if (s != LITEVLM_OK) return s;
@@ -1494,7 +1515,14 @@ litevlm_status_t litevlm_select_cache_attend(litevlm_select_t h, int32_t batch, 
         s = check_rows(h, q, q_row_stride, c.num_q_heads, q_scale, "q");
         if (s != LITEVLM_OK) return s;
         if (!out || !aligned16(out)) return fail(h, LITEVLM_ERR_INVALID_ARG, "out must be 16-byte aligned and not NULL");
+        const int64_t row = (int64_t)c.num_q_heads * c.head_dim;
+        if (overlap(out, total * row * 2, q,
+                    span_bytes(total, q_row_stride, row, c.qk_dtype == LITEVLM_FP8_E4M3 ? 1 : 2)))
+            return fail(h, LITEVLM_ERR_INVALID_ARG, "out must not overlap q");
     }
+    const int64_t slots = (int64_t)cache->num_pages * cache->page_size * 4;
+    if (weights_in != weights_out && overlap(weights_in, slots, weights_out, slots))
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "weights_in and weights_out are one array or do not overlap");
     const int64_t rows = total * (c.num_q_heads / c.num_kv_heads);
     const AttendSpace space = attend_space(plan, rows, c.head_dim, c.num_kv_heads, max_rows, batch, max_len,
                                            weights_out != nullptr);
@@ -1567,7 +1595,8 @@ litevlm_status_t litevlm_select_cache_evict(litevlm_select_t h, int32_t batch, c
     if (to_table && (to_width < 1 || (int64_t)to_width * cache->page_size < std::min(budget, max_len)))
         return fail(h, LITEVLM_ERR_INVALID_ARG, "to_width pages must hold min(budget, max_len) tokens");
     if (!weights || !kept_idx || !new_lens) return fail(h, LITEVLM_ERR_INVALID_ARG, "a device pointer is NULL");
-    if (new_lens == seq_lens) return fail(h, LITEVLM_ERR_INVALID_ARG, "new_lens must not be the array seq_lens");
+    if (overlap(new_lens, (int64_t)batch * 4, seq_lens, (int64_t)batch * 4))
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "new_lens must not overlap seq_lens");
     a.lens = seq_lens;
     a.batch = batch;
     a.limit = max_len;
@@ -1608,6 +1637,8 @@ litevlm_status_t litevlm_select_verify(litevlm_select_t h, int32_t batch, int32_
     if (!draft_offsets_d || !target_probs || !u_sample || !accepted || !tokens ||
         (total > 0 && (!draft_tokens || !u_accept)))
         return fail(h, LITEVLM_ERR_INVALID_ARG, "a device pointer is NULL");
+    if (overlap(tokens, (total + batch) * 4, draft_tokens, total * 4))
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "tokens must not overlap draft_tokens");
     s = debug_mirror(h, draft_offsets_d, draft_offsets_h, (int64_t)batch + 1, "draft_offsets", stream);
     if (s != LITEVLM_OK) return s;
     lvs::VerifyArgs a{};

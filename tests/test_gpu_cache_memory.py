@@ -111,3 +111,47 @@ def test_a_request_s_weights_do_not_depend_on_the_others(select, counts, hq, hkv
         assert torch.allclose(nxt[live], one[live], rtol=2.0 ** -12, atol=0)
     s.check_device()
     s.close()
+
+
+def test_arrays_that_overlap_are_refused(select):  # noqa: F811
+    """CTAs read what others write there: queries that a later launch reads again, lengths and drafts of other requests."""
+    rng = np.random.default_rng(4)
+    lens_h = [200, 37, 90]
+    table, pool = tables(rng, [n + 64 for n in lens_h], 16)
+    w = np.zeros((pool, 16), np.float32)
+    cache = to_cache(select, random_pool(rng, pool, 2, 16, 128), w)
+    s = select.Selector(3, 8, 8, 8, 2, 128, "bf16")
+    t, off, off_h = i32(table), i32([0, 1, 2, 3]), offsets([1, 1, 1])
+    buf = i32([0] + lens_h + [0, 0])
+    lens = buf[1:4]
+    k = torch.from_numpy(rng.standard_normal((3, 2, 128))).to(torch.bfloat16).cuda()
+    q, _, _ = make_q(rng, 4, 8, 128, "bf16")
+    bad = "INVALID_ARG"
+    for at in (0, 1, 2, 3):
+        refused(select, bad, lambda: s.cache_append(cache, t, lens, k, k, off, new_lens=buf[at:at + 3]))
+        refused(select, bad, lambda: s.cache_evict(cache, t, lens, 200, 20, new_lens=buf[at:at + 3]))
+    assert buf.tolist() == [0] + lens_h + [0, 0]
+    refused(select, bad, lambda: s.cache_attend(cache, t, lens, q[:3], off, 200, out=q[:3]))
+    refused(select, bad, lambda: s.cache_attend(cache, t, lens, q[:3], off, 200, out=q[1:]))
+    wide = torch.zeros((pool + 1, 16), device="cuda")
+    cache.weights = wide[:pool]
+    refused(select, bad, lambda: s.cache_attend(cache, t, lens, q[:3], off, 200, weights_out=wide[1:]))
+    raw = lambda ks, vs: select.cache_append(s.handle, 3, cache.struct, t, t.shape[1], lens, k, 256, k, 256, 3, None, off,  # noqa: E731
+                                             off_h, 1.0, 1.0, cache.weights, ks, vs, torch.empty_like(lens),
+                                             torch.cuda.current_stream().cuda_stream)
+    room = torch.empty((7, 2, 128), dtype=torch.bfloat16, device="cuda")
+    for ks, vs in ((k, room[:3]), (room[:3], k), (room[:3], room[2:5])):
+        refused(select, bad, lambda: raw(ks, vs))
+    raw(room[:3], room[3:6])
+    x = i32([1, 2, 3, 0, 0, 0, 0])
+    p, u = torch.full((6, 5), 0.2, device="cuda"), torch.zeros(3, device="cuda")
+    refused(select, bad, lambda: s.verify(x[:3], p, u, u, off, tokens=x[:6]))
+    refused(select, bad, lambda: s.verify(x[4:], p, u, u, off, tokens=x[:6]))
+    # beside one another they are taken
+    new = s.cache_append(cache, t, lens, k, k, off, new_lens=torch.cat([buf, buf])[6:9])
+    assert new.tolist() == [n + 1 for n in lens_h]
+    many = torch.cat([q[:3], torch.zeros_like(q[:3])])
+    out = s.cache_attend(cache, t, lens, many[:3], off, 200, out=many[3:], weights_out=torch.zeros_like(cache.weights))
+    assert torch.equal(out, s.cache_attend(cache, t, lens, q[:3], off, 200))
+    s.check_device()
+    s.close()
