@@ -767,20 +767,34 @@ __device__ __forceinline__ float4 add_weights(const float* s, int64_t stride, co
 
 // The first `join_blocks` CTAs of a request join its rows' chunks, `row_warps` warps a row;
 // the others add weights from the kept scores, 256 to 1024 keys at a time, over the rows in order.
+// Where some requests have no queries (`active` > 0: those that have), the grid's first axis holds the join CTAs of
+// these, then the weight CTAs of all; else its second axis is the request.
 // A weight CTA finds the rows' lse from the chunks' statistics by itself, which saves a
 // launch between the two. 7 us of the 128-request step; 18 of the four long requests' (16 Ki to
 // 131 Ki keys x 28 rows of kept scores, 47 MB, and 600 chunks of 28 rows), 20 of the drafts' (80 MB).
 template <int D, int PARTS>
 __global__ void __launch_bounds__(kFinishThreads) attend_finish_kernel(const __grid_constant__ AttendArgs a,
-                                                                       int join_blocks, int row_warps)
+                                                                       int join_blocks, int weight_blocks, int row_warps,
+                                                                       int active)
 {
     extern __shared__ uint8_t rows_s[];
     // the warps' parts: four weights a lane, or a row of outputs a warp (D <= 128)
     __shared__ __align__(16) float join_s[kFinishWarps][128];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int b = blockIdx.y;
+    int b = blockIdx.y, block = blockIdx.x;
     griddep_wait();
     griddep_launch_dependents();
+    if (active > 0) {
+        const int joins = active * join_blocks;
+        if (block < joins) {
+            b = find_active(a, block / join_blocks);
+            block %= join_blocks;
+            if (b == a.batch) return;
+        } else {
+            b = (block - joins) / weight_blocks;
+            block = join_blocks + (block - joins) % weight_blocks;
+        }
+    }
     bool bad;
     const int len = cache_len(a.lens[b], a.limit, bad);
     const int q0 = a.q_off[b], t = a.q_off[b + 1] - q0;
@@ -795,11 +809,11 @@ __global__ void __launch_bounds__(kFinishThreads) attend_finish_kernel(const __g
         const int seen = len - t + i + 1;
         return seen > 0 ? chunks_of(seen, chunk) : 0;
     };
-    if ((int)blockIdx.x >= join_blocks) {
+    if (block >= join_blocks) {
         const int rows = t * a.group, n = rows * a.cache.hkv;
         constexpr int across = kFinishWarps / PARTS, keys = 128 * across;
         const int tiles = (len + keys - 1) / keys;
-        int tile = blockIdx.x - join_blocks;
+        int tile = block - join_blocks;
         if (tile >= tiles) return;
         float* lse_s = reinterpret_cast<float*>(rows_s);
         int2* row_s = reinterpret_cast<int2*>(rows_s + (size_t)((n + 1) & ~1) * 4);  // scores' row, last key seen
@@ -835,7 +849,7 @@ __global__ void __launch_bounds__(kFinishThreads) attend_finish_kernel(const __g
         __syncthreads();
         const int part = warp / across, per = (n + PARTS - 1) / PARTS;
         const int x0 = min(n, part * per), x1 = min(n, x0 + per);
-        for (; tile < tiles; tile += gridDim.x - join_blocks) {
+        for (; tile < tiles; tile += weight_blocks) {
             // four neighbouring keys a lane (the scores' rows are padded to a whole number of them)
             const int j0 = tile * keys, j = j0 + warp % across * 128 + 4 * lane;
             int64_t at = -1;
@@ -903,12 +917,12 @@ __global__ void __launch_bounds__(kFinishThreads) attend_finish_kernel(const __g
         }
     };
     int64_t from = 0;
-    int r = blockIdx.x * join_rows + warp / row_warps, n = place(r, from);
+    int r = block * join_rows + warp / row_warps, n = place(r, from);
     float2 ml[U];
     float v[U][D / 32];
     load(from, n, part, ml, v);
     const int next_r = join_blocks * join_rows;
-    for (int r0 = blockIdx.x * join_rows; r0 < rows; r0 += next_r, r += next_r) {
+    for (int r0 = block * join_rows; r0 < rows; r0 += next_r, r += next_r) {
         // chunks under a running reference
         float M = kNoRef, L = 0.f, O[D / 32];
 #pragma unroll
@@ -990,25 +1004,27 @@ cudaError_t launch_all(const AttendArgs& a, const AttendPlan& plan, int max_rows
         }
     }
     const int most = max_rows / a.group * a.hq;  // rows of the longest request
-    // warps of a row by the chunks that a request has where all are alike
-    const int chunks = (plan.slots + a.batch - 1) / a.batch;
+    // warps of a row by the chunks that a request with queries has where all are alike
+    const int chunks = (plan.slots + plan.active - 1) / std::max(plan.active, 1);
     const int row_warps = chunks <= 4 ? 1 : (chunks <= 16 ? 4 : kFinishWarps);
     const int join_rows = kFinishWarps / row_warps;  // of a CTA
     // (a warp joins row after row, the next one's sums on their way: a chunk of a prompt 234 to 224 us)
     const int join_blocks =
         total_rows > 0 && plan.slots > 0
-            ? std::min((most + join_rows - 1) / join_rows, std::max(1, 4 * a.num_sms / a.batch)) : 0;
+            ? std::min((most + join_rows - 1) / join_rows, std::max(1, 4 * a.num_sms / plan.active)) : 0;
     // weight CTAs: one for the keys that it takes at a time, as many as run in a round or two
     const int parts = weight_parts(most, (int64_t)(max_len + 255) / 256 * a.batch, a.num_sms);
     const int keys = 128 * kFinishWarps / parts;
     const int weight_blocks =
         a.logits ? std::min((max_len + keys - 1) / keys, std::max(1, (parts == 8 ? 6 : 3) * a.num_sms / a.batch)) : 0;
     if (weight_blocks + join_blocks > 0) {
-        cfg.gridDim = dim3((unsigned)(weight_blocks + join_blocks), (unsigned)a.batch, 1);
+        const bool all = plan.active == a.batch;
+        cfg.gridDim = all ? dim3((unsigned)(join_blocks + weight_blocks), (unsigned)a.batch, 1)
+                          : dim3((unsigned)(plan.active * join_blocks + a.batch * weight_blocks), 1, 1);
         cfg.blockDim = dim3(kFinishThreads, 1, 1);
         cfg.dynamicSmemBytes = a.logits ? (size_t)(most + 2) * 12 : 0;
         e = cudaLaunchKernelEx(&cfg, parts == 2 ? attend_finish_kernel<D, 2> : attend_finish_kernel<D, 8>, a, join_blocks,
-                               row_warps);
+                               weight_blocks, row_warps, all ? 0 : plan.active);
         if (e != cudaSuccess) return e;
         ++*launches;
         cfg.dynamicSmemBytes = 0;
@@ -1042,10 +1058,14 @@ bool attend_keeps_scores(int64_t max_rows, int hkv)
 
 AttendPlan plan_cache_attend(int batch, int hkv, int group, const int32_t* q_off, int64_t max_len, int num_sms)
 {
-    int max_t = 0;
-    for (int b = 0; b < batch; ++b) max_t = std::max(max_t, q_off[b + 1] - q_off[b]);
-    const int64_t max_rows = (int64_t)max_t * group;
     AttendPlan p;
+    int max_t = 0;
+    p.active = 0;
+    for (int b = 0; b < batch; ++b) {
+        max_t = std::max(max_t, q_off[b + 1] - q_off[b]);
+        p.active += q_off[b + 1] > q_off[b];
+    }
+    const int64_t max_rows = (int64_t)max_t * group;
     p.row_tile = attend_row_tile(max_rows);
     int64_t items = 0;  // CTAs where each takes all keys of its rows
     for (int b = 0; b < batch; ++b)
@@ -1076,7 +1096,9 @@ AttendPlan plan_cache_attend(int batch, int hkv, int group, const int32_t* q_off
             if (c < cost) cost = c, best = n;
         }
     }
-    p.slots = best > 1 ? (int32_t)std::min<int64_t>(best * batch, 1 << 20) : 0;
+    // (a request without queries has no keys to read: one of 4096 keys beside 255 such takes 18 us, with slots
+    // for each of those too 1780)
+    p.slots = best > 1 ? (int32_t)std::min<int64_t>(best * p.active, 1 << 20) : 0;
     p.logits = attend_keeps_scores(max_rows, hkv);
     return p;
 }

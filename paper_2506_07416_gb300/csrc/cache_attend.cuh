@@ -93,6 +93,21 @@ __device__ __forceinline__ void find_slot(const AttendArgs& a, int slot, int chu
     k0 = 0;
 }
 
+// The n-th request with queries, by a warp.
+__device__ __forceinline__ int find_active(const AttendArgs& a, int n)
+{
+    const int lane = threadIdx.x & 31;
+    for (int b0 = 0; b0 < a.batch; b0 += 32) {
+        const int b = min(b0 + lane, a.batch - 1);
+        const bool there = b0 + lane < a.batch && __ldg(a.q_off + b + 1) > __ldg(a.q_off + b);
+        const uint32_t mask = __ballot_sync(0xffffffffu, there);
+        const uint32_t hit = __ballot_sync(0xffffffffu, there && __popc(mask & ((1u << lane) - 1u)) == n);
+        if (hit) return b0 + __ffs(hit) - 1;
+        n -= __popc(mask);
+    }
+    return a.batch;
+}
+
 // What every CTA of a request's tile needs to know of its rows.
 struct RowTile {
     int len, t, row0, rows, last0;  // last0: position of the first query

@@ -186,6 +186,7 @@ struct AttendArgs {
 struct AttendPlan {
     int32_t row_tile;         // rows (query x head of a key head) of a CTA: 8, 16, 128 or 256
     int32_t slots;
+    int32_t active;           // requests with queries
     bool logits;              // the weights are made from kept scores
 };
 int attend_row_tile(int64_t max_rows);                   // AttendPlan::row_tile for a longest request of so many rows

@@ -155,3 +155,43 @@ def test_arrays_that_overlap_are_refused(select):  # noqa: F811
     assert torch.equal(out, s.cache_attend(cache, t, lens, q[:3], off, 200))
     s.check_device()
     s.close()
+
+
+@pytest.mark.parametrize("hq,hkv,t", [(4, 4, 1), (8, 2, 1), (8, 2, 4), (8, 2, 16), (8, 2, 70)])
+@pytest.mark.parametrize("weights", [False, True])
+def test_requests_without_queries_cost_next_to_nothing(select, hq, hkv, t, weights):  # noqa: F811
+    """A few requests with queries among many without: the keys are split as if the others were not there, into a
+    workspace of the same size but for their weights, and the outputs have the same bits."""
+    rng = np.random.default_rng(hq + t)
+    batch, active, n = 130, (0, 77, 129), 2500
+    lens = np.full(batch, 20)
+    lens[list(active)] = n, 700, n - 333
+    table, pool = tables(rng, lens.tolist(), 64)
+    w = np.exp(rng.standard_normal((pool, 64)) - 5).astype(np.float32)
+    cache = to_cache(select, random_pool(rng, pool, hkv, 64, 128), w)
+    counts = np.zeros(batch, np.int64)
+    counts[list(active)] = t, max(1, t - 2), t
+    few = counts[list(active)]
+    off, off3 = offsets(counts), offsets(few)
+    q, _, _ = make_q(rng, int(off[-1]), hq, 128, "bf16")
+    s = select.Selector(batch, 8, 8, hq, hkv, 128, "bf16")
+    for wanted in (False, weights):
+        many, alone = (select.cache_attend_workspace(s.handle, len(o) - 1, o, n, wanted) for o in (off, off3))
+        more = (batch * 8 + 512) + (wanted and hkv * (batch - 3) * 4 * (n + 32) + 512)
+        assert many <= alone + more, (many, alone)
+    nxt, one = torch.full((pool, 64), -1.0, device="cuda"), torch.full((pool, 64), -1.0, device="cuda")
+    out = s.cache_attend(cache, i32(table), i32(lens), q, i32(off), n, weights_out=nxt if weights else None, offsets_h=off)
+    want = s.cache_attend(cache, i32(table[list(active)]), i32(lens[list(active)]), q, i32(off3), n,
+                          weights_out=one if weights else None, offsets_h=off3)
+    assert torch.equal(out, want)
+    if weights:
+        live = one >= 0
+        # (sums of up to t hq positive terms, which warps share by the call's size: two orders of n terms differ by at
+        # most n 2^-23 of the sum, 560 2^-23 < 2^-13)
+        assert torch.allclose(nxt[live], one[live], rtol=2.0 ** -13, atol=0)
+        for b in (1, 50, 128):  # the others' weights as they are
+            pos = np.arange(20)
+            at = table[b][pos // 64], pos % 64
+            assert (nxt.cpu().numpy()[at] == w[at]).all()
+    s.check_device()
+    s.close()
