@@ -1,4 +1,6 @@
 """Whose memory the 4-bit cache's calls use, and for how long: a cache's tensors, workspaces, arrays that overlap."""
+import gc
+
 import numpy as np
 import pytest
 
@@ -54,6 +56,7 @@ def test_a_handle_keeps_one_workspace_and_gives_it_back(select):  # noqa: F811
     need = select.cache_attend_workspace(s.handle, 1, off_h, n)
     assert need > 10 << 20
     torch.cuda.synchronize()
+    gc.collect()  # (what earlier tests left behind is not counted)
     before = torch.cuda.memory_allocated()
     streams = [torch.cuda.Stream() for _ in range(4)]
     for st in streams + streams:
@@ -64,7 +67,7 @@ def test_a_handle_keeps_one_workspace_and_gives_it_back(select):  # noqa: F811
     assert need <= held < 2 * need
     s.check_device()
     s.close()
-    assert torch.cuda.memory_allocated() == before
+    assert torch.cuda.memory_allocated() <= before
 
 
 def test_the_workspace_follows_the_rows_of_a_call(select):  # noqa: F811
