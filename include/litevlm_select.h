@@ -625,7 +625,9 @@ litevlm_status_t litevlm_select_cache_append(litevlm_select_t handle, int32_t ba
  *     p[h][i][:] = softmax_j;  out[i,h,:] = sum_j p[h][i][j] * v[j, h / G, :]
  *     weights_out[slot of j] = weights_in[slot of j] + (1 / Hq) * sum_h sum_i p[h][i][j]
  * A query that sees no key gives zeros and adds no weight. What lies behind a
- * request's last token does not matter, whatever its bytes are.
+ * request's last token does not matter, whatever its bytes are. Requests without queries
+ * cost next to nothing; one with many queries makes the call run in tiles of 128 or 256
+ * rows for every request, so prompts and single tokens are better two calls.
  *   q                device [sum T_b][Hq][d] of the handle's element type, 16-byte
  *                    aligned, row stride as in litevlm_select_cache_append
  *   q_offsets_d/h    int32 [batch+1] prefix of T_b (T_b = 1: a decoding step; T_b = 0:
@@ -642,17 +644,22 @@ litevlm_status_t litevlm_select_cache_append(litevlm_select_t handle, int32_t ba
  *   workspace        device, at least the bytes that
  *                    litevlm_select_cache_attend_workspace gives for the same batch,
  *                    offsets and max_len (weights: 1 for a call with weights, which
- *                    needs more), 256-byte aligned; used only by this call
+ *                    needs more: 4 bytes x Hkv x max_len for every row, a query with one
+ *                    of the G heads of a key head, in calls of up to 32 rows a request,
+ *                    else for every 128 rows), 256-byte aligned; used only by this call
  *                    until it has run. Calls that may run at the same time (two
  *                    captured graphs among them) need a workspace each.
- * Softmax statistics, sums and weights are fp32; probabilities are rounded to f16 for
- * the product with V. The weights are added in a fixed order (the same inputs give
- * the same bits).
+ * Scores, softmax statistics, sums and weights are fp32, exponentials the GPU's 2^x (off by
+ * 2^-22). Probabilities are rounded to f16 for the product with V (2^-11; below f16's
+ * normal range 2^-32 of the row's largest); where a key head has one row in all of the
+ * call, their products with the values' block scales are instead (2^-11; 2^-34 of the
+ * largest value). Scores beyond fp32's range are brought inside it where any two that differ
+ * are still far apart. The weights are added in a fixed order (the same inputs give the
+ * same bits).
  * Errors: as for litevlm_select_cache_append; WORKSPACE for a workspace that is too
  * small; UNSUPPORTED where the workspace passes 2^60 bytes, or Hkv x tiles of rows of the
- * longest request 65535 (a row is a query with one of the G heads of a key head; a tile has
- * 256 rows in calls of more than 128, with weights 128: 262016 queries at 32 / 32 heads
- * with weights).
+ * longest request 65535 (a tile has 256 rows in calls of more than 128, with weights 128:
+ * 262016 queries at 32 / 32 heads with weights).
  */
 litevlm_status_t litevlm_select_cache_attend_workspace(litevlm_select_t handle, int32_t batch,
                                                        const int32_t* q_offsets_h, int32_t max_len, int32_t weights,

@@ -9,7 +9,7 @@
 // sector of a full page.
 // Bound by memory: 128 prompts of 1100 bf16 rows of 32 heads (5.27 GB read and written)
 // take 824 us, 6.4 TB/s, 0.94 of a plain copy's rate. With picked e4m3 rows and the values
-// written back (12.9 Ki rows, 388 MB) 78 us: 4.2 TB/s at 64% of the issue slots.
+// written back (13 Ki rows, 388 MB) 78 us: 4.2 TB/s at 70% of the issue slots.
 
 #include "cache.cuh"
 

@@ -25,11 +25,11 @@
 // What bounds it: a byte of codes costs instructions (its conversion to f16 pairs, loads,
 // contractions) beside its 1/6780 ns of memory, and registers limit an SM to 16 (one row, 8
 // rows) or 12 (16 rows) warps. By cases, all with weights:
-//   a token of 128 requests of about 1130, 32 heads (669 MB): 118 us and 7 for the weights;
-//     5.75 TB/s, issue and the integer pipe 57%
-//   a token of four requests of 30 Ki to 131 Ki, 28 / 4 heads (217 MB): 50 + 18 us; 4.5 TB/s, issue 47%
-//   1 to 8 e4m3 queries of 32 requests, 32 / 8 heads (139 MB): 88 + 22 us; 2.7 TB/s with the kept
-//     scores, issue 38%: 12 warps do not cover one another's latencies, and requests of different rows
+//   a token of 128 requests of about 1130, 32 heads (669 MB): 126 us, 10 of them for the weights;
+//     5.7 TB/s, issue and the integer pipe 57%
+//   a token of four requests of 40 Ki to 127 Ki, 28 / 4 heads (217 MB): 68 us, 16 for the weights; 4.5 TB/s, issue 47%
+//   1 to 8 e4m3 queries of 32 requests, 32 / 8 heads (139 MB): 110 us, 22 for the weights; 2.7 TB/s with the kept
+//     scores, issue 39%: 12 warps do not cover one another's latencies, and requests of different rows
 //     leave a sixth of the SMs' time idle
 // Dropped: values from codes by masks and shifts (20 pairs a clock and SM; the conversion 50),
 // the weights from K read again (190 us of the first case where the kept scores take 10),
@@ -729,8 +729,9 @@ constexpr int kFinishThreads = 512;
 constexpr int kFinishWarps = kFinishThreads / 32;
 // Warps of a CTA that share a key's rows in adding weights: the fewer, the more keys a CTA takes at a time
 // (128 for each of the others) and the fewer CTAs read the chunks' statistics; the more rows (query and
-// head), the longer a CTA would have. 28 rows (four requests of up to 131 Ki keys): 67 us for the call with 2,
-// 70 with 4, 75 with 8; 32 to 256 rows (32 requests of up to 8191): 125, 119 and 115.5. Where CTAs of 256
+// head), the longer a CTA would have. 28 rows (four requests of up to 127 Ki keys): 67 us for the call with 2,
+// 70 with 4, 75 with 8; 32 to 256 rows (32 requests of up to 8152, before other steps brought 115.5 to 110): 125, 119
+// and 115.5. Where CTAs of 256
 // keys are so few that all run at once, more share too (16 rows, 524 keys: 8.4 us with 2, 7.7 with 8).
 int weight_parts(int rows, int64_t ctas, int num_sms) { return rows <= 64 && ctas > 3 * num_sms ? 2 : 8; }
 constexpr int kLogitRows = 2048;  // rows of a request whose scores are kept for the weights
@@ -770,8 +771,9 @@ __device__ __forceinline__ float4 add_weights(const float* s, int64_t stride, co
 // Where some requests have no queries (`active` > 0: those that have), the grid's first axis holds the join CTAs of
 // these, then the weight CTAs of all; else its second axis is the request.
 // A weight CTA finds the rows' lse from the chunks' statistics by itself, which saves a
-// launch between the two. 7 us of the 128-request step; 18 of the four long requests' (16 Ki to
-// 131 Ki keys x 28 rows of kept scores, 47 MB, and 600 chunks of 28 rows), 20 of the drafts' (80 MB).
+// launch between the two. 10 us of the 128-request step; 16 of the four long requests' (40 Ki to
+// 127 Ki keys x 28 rows of kept scores, 47 MB; each of 568 CTAs finds all 28 rows' lse from about 150 chunks before its
+// first scores), 22 of the drafts' (80 MB).
 template <int D, int PARTS>
 __global__ void __launch_bounds__(kFinishThreads) attend_finish_kernel(const __grid_constant__ AttendArgs a,
                                                                        int join_blocks, int weight_blocks, int row_warps,
@@ -1045,7 +1047,9 @@ cudaError_t launch_all(const AttendArgs& a, const AttendPlan& plan, int max_rows
 // 4096 keys, 32 / 8 heads: 12 rows 53 us (other 50), with weights 63 (95); 20 rows 71 (51), with weights 84
 // (96); 32 rows 79 (51), 97.5 (96). One of 8000 keys: 20 rows 19.6 (19.7). 32 ragged requests of 4 to 32 rows and up to
 // 8200 keys: 88 (128), with weights 111 (243). A call's rows are those of its longest request, so the border
-// lies where ragged calls and those with weights gain more than the others lose.
+// lies where ragged calls and those with weights gain more than the others lose. For the same reason prompts and
+// single tokens are better two calls: 1024 queries beside 63 single ones, 4096 keys each, 28 / 4 heads, take 212 us,
+// each alone 69 and 43.
 constexpr int kFewRows = 32;
 
 // 128 rows a CTA, or two row tiles that share the K and V that it makes: 192 rows 97 (one) and 72 us
@@ -1076,7 +1080,7 @@ AttendPlan plan_cache_attend(int batch, int hkv, int group, const int32_t* q_off
     // keys for every four rows. A CTA of the kernel for many rows, alone on its SM or in a pair, takes as long
     // as 700 keys to start and to end, and its chunks are joined in as long as 2.3 keys a row; its rounds are between
     // the whole number and the fraction, as its CTAs' keys differ. (2 x 700 queries over 2048 keys, 32 / 8
-    // heads: whole 73 us, three chunks, as for few rows, 103; 1024 and 777 over up to 8191, 28 / 4 heads: 195 and
+    // heads: whole 73 us, three chunks, as for few rows, 103; 1023 and 873 over 5928 and 6517, 28 / 4 heads: 195 and
     // 213; 512 over 8192, half the SMs: whole 129, two chunks 80.)
     const int64_t places = (int64_t)num_sms * (p.row_tile == 256 ? 1 : (p.row_tile == 128 ? 2 : (p.row_tile == 16 ? 3 : 4)));
     // (three rounds of smaller chunks for 9 to 32 rows, whose requests have different numbers of rows too)
@@ -1085,7 +1089,10 @@ AttendPlan plan_cache_attend(int batch, int hkv, int group, const int32_t* q_off
     int64_t best = 1;
     if (items > 0 && items < places) {
         best = std::min(units, rounds * places / items);
-    } else if (items < 3 * places) {  // (from three rounds on the last one's idle places matter little)
+    } else if (items < 3 * places) {
+        // (From three rounds on the last one's idle places matter little where the requests are alike. Where one is far
+        // longer than the rest, the CTAs of its heads are left alone with all of its keys: 127 requests of 1000 tokens
+        // and one of 131072, 32 heads, take 1110 us, where 128 of 1000 take 125.)
         double cost = 1e30;
         for (int64_t n = 1; n <= std::min<int64_t>(units, 8); ++n) {
             const bool many = p.row_tile >= 128;

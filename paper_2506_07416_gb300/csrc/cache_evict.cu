@@ -14,9 +14,10 @@
 // every load of a batch ends before its first store, and since the kept rows
 // ascend (row i comes from a position >= i), no store touches a row of a later
 // batch.
-// 64 requests of up to 8191 tokens cut to 2048, 8 heads (300 MB): 79 us, 16 of selecting (cluster
+// 64 requests of up to 8162 tokens cut to 2048, 8 heads (300 MB): 79 us, 16 of selecting (cluster
 // barriers) and 61 of moving at 5.6 TB/s of DRAM traffic: a picked row's scales are 8 of a sector's 32
-// bytes. A request of 560 tokens: 11 us, latency.
+// bytes. A request of 560 tokens: 10 us, latency. The same 64 requests in place: 190 us, one of 8191 tokens and 4 heads
+// 150: a CTA's 128 threads move a head's rows 32 at a time, one round trip to memory after another.
 
 #include <type_traits>
 

@@ -17,9 +17,10 @@
 // another: about 3600 clocks for a tile of 256 rows by 128 keys. So two row tiles are always in flight:
 //   NR = 1, up to 128 rows: two CTAs on an SM, 256 columns and at most 113 KB each, one stage of K and V
 //   NR = 2: one CTA with two row tiles, for which K and V are made once, in two stages
-// (192 rows of 16 requests of 4096 keys: 76 us with NR = 2 and 97 with 1). Start and end of a CTA take about as
-// long as seven of those tiles. A chunk of a prompt, 1024 and 777 queries of 28 / 4 heads over up to 8191 keys
-// (156 GFLOP): 186 us, the tensor pipe active half of the time; with the contractions of the warp-wide instructions 617.
+// (192 rows of 16 requests of 4096 keys: 72 us with NR = 2 and 97 with 1). Start and end of a CTA take about as
+// long as seven of those tiles. A chunk of a prompt, 1023 and 873 queries of 28 / 4 heads over 5928 and 6517 keys
+// (156 GFLOP): 186 us, the tensor pipe active half of the time: its 208 nearly equal tiles of 256 rows take two rounds of
+// 152 SMs where 1.37 would do, and a CTA's own chain the rest; with the contractions of the warp-wide instructions 617.
 // Dropped for that chunk: P and the product by halves of a tile's keys (233 us where the whole took 224), S by
 // halves too (263), two threads a row (245 against 218), a quarter of the exponentials by a polynomial (241 against
 // 217): a warp's own latencies bound the softmax, and the warps share their SM with those that make the values.
@@ -643,7 +644,7 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
 // probabilities of one key over the columns, in order. The sums of a tile of rows are kept
 // for every key; attend_fold_kernel adds those of all tiles and heads, in order. Bound by the
 // exponentials and the contraction, as the first pass, with no second product: the chunk of a
-// prompt above takes 366 us with weights and 186 without (with rows as the contraction's rows and
+// prompt above takes 360 us with weights and 186 without (with rows as the contraction's rows and
 // sums over lanes about 3 ms).
 enum { W_K_FULL = 0, W_K_FREE = 2, W_S_FULL = 4, W_S_FREE = 6, W_DRAIN = 8, W_COUNT };
 
