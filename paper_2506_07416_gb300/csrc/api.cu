@@ -1268,10 +1268,16 @@ bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes)
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
     return a && b && a_bytes > 0 && b_bytes > 0 && x < y + (uint64_t)b_bytes && y < x + (uint64_t)a_bytes;
 }
-// Bytes from the first of `rows` rows of `row` elements, `stride` apart, to the end of the last.
-int64_t span_bytes(int64_t rows, int64_t stride, int64_t row, int64_t esize)
+// The same with rows of `row` elements, `stride` (>= row) apart: what lies between them does not count.
+bool overlap_rows(const void* a, int64_t a_bytes, const void* rows_at, int64_t rows, int64_t stride, int64_t row,
+                  int64_t esize)
 {
-    return rows > 0 ? ((rows - 1) * stride + row) * esize : 0;
+    if (!a || !rows_at || a_bytes <= 0 || rows <= 0) return false;
+    const int64_t ahead = (int64_t)(reinterpret_cast<uintptr_t>(a) - reinterpret_cast<uintptr_t>(rows_at));
+    const int64_t len = row * esize, step = std::min(stride, INT64_MAX / 4) * esize;
+    // the first row that ends behind the start of a
+    const int64_t i = ahead < len ? 0 : (ahead - len) / step + 1;
+    return i < rows && i * step < ahead + a_bytes;
 }
 
 bool in_range(float scale) { return scale >= 0x1p-60f && scale <= 0x1p60f; }
@@ -1429,11 +1435,10 @@ litevlm_status_t litevlm_select_cache_append(litevlm_select_t h, int32_t batch, 
             return fail(h, LITEVLM_ERR_INVALID_ARG, "k_stored and v_stored must be 16-byte aligned");
         const int64_t row = (int64_t)h->cfg.num_kv_heads * h->cfg.head_dim, stored = rows * row * 2;
         const int64_t esize = h->cfg.qk_dtype == LITEVLM_FP8_E4M3 ? 1 : 2;
-        const int64_t k_bytes = span_bytes(src_rows, k_row_stride, row, esize);
-        const int64_t v_bytes = span_bytes(src_rows, v_row_stride, row, esize);
-        if (overlap(k_stored, stored, v_stored, stored) || overlap(k_stored, stored, k, k_bytes) ||
-            overlap(k_stored, stored, v, v_bytes) || overlap(v_stored, stored, k, k_bytes) ||
-            overlap(v_stored, stored, v, v_bytes))
+        const auto in_k = [&](const void* p) { return overlap_rows(p, stored, k, src_rows, k_row_stride, row, esize); };
+        const auto in_v = [&](const void* p) { return overlap_rows(p, stored, v, src_rows, v_row_stride, row, esize); };
+        if (overlap(k_stored, stored, v_stored, stored) || in_k(k_stored) || in_v(k_stored) || in_k(v_stored) ||
+            in_v(v_stored))
             return fail(h, LITEVLM_ERR_INVALID_ARG, "k_stored and v_stored must not overlap k, v or one another");
     }
     s = debug_mirror(h, new_offsets_d, new_offsets_h, (int64_t)batch + 1, "new_offsets", stream);
@@ -1516,8 +1521,7 @@ litevlm_status_t litevlm_select_cache_attend(litevlm_select_t h, int32_t batch, 
         if (s != LITEVLM_OK) return s;
         if (!out || !aligned16(out)) return fail(h, LITEVLM_ERR_INVALID_ARG, "out must be 16-byte aligned and not NULL");
         const int64_t row = (int64_t)c.num_q_heads * c.head_dim;
-        if (overlap(out, total * row * 2, q,
-                    span_bytes(total, q_row_stride, row, c.qk_dtype == LITEVLM_FP8_E4M3 ? 1 : 2)))
+        if (overlap_rows(out, total * row * 2, q, total, q_row_stride, row, c.qk_dtype == LITEVLM_FP8_E4M3 ? 1 : 2))
             return fail(h, LITEVLM_ERR_INVALID_ARG, "out must not overlap q");
     }
     const int64_t slots = (int64_t)cache->num_pages * cache->page_size * 4;

@@ -198,3 +198,38 @@ def test_requests_without_queries_cost_next_to_nothing(select, hq, hkv, t, weigh
             assert (nxt.cpu().numpy()[at] == w[at]).all()
     s.check_device()
     s.close()
+
+
+def test_what_lies_between_rows_does_not_overlap(select):  # noqa: F811
+    """Rows far apart in one buffer: the outputs may lie between two of them, and the sources' number of rows, where an
+    index picks them, may be any bound."""
+    rng = np.random.default_rng(5)
+    table, pool = tables(rng, [100, 40], 16)
+    cache = to_cache(select, random_pool(rng, pool, 2, 16, 64), np.zeros((pool, 16), np.float32))
+    s = select.Selector(2, 8, 8, 4, 2, 64, "bf16")
+    t, lens, off, off_h = i32(table), i32([100, 40]), i32([0, 1, 2]), offsets([1, 1])
+    q, _, _ = make_q(rng, 2, 4, 64, "bf16")
+    room = torch.zeros((2, 64, 4, 64), dtype=torch.bfloat16, device="cuda")
+    room[:, 5] = q
+    want = s.cache_attend(cache, t, lens, q, off, 100)
+    for at in (0, 3, 6, 60):   # beside the first row or between the two
+        assert torch.equal(s.cache_attend(cache, t, lens, room[:, 5], off, 100, out=room[0, at:at + 2]), want)
+    assert torch.equal(s.cache_attend(cache, t, lens, room[:, 5], off, 100, out=room[1, 6:8]), want)  # behind the last
+    for b, at in ((0, 4), (0, 5), (1, 4), (1, 5)):
+        refused(select, "INVALID_ARG", lambda: s.cache_attend(cache, t, lens, room[:, 5], off, 100, out=room[b, at:at + 2]))
+    assert torch.equal(room[:, 5], q)
+    k = torch.from_numpy(rng.standard_normal((2, 2, 64))).to(torch.bfloat16).cuda()
+    new = torch.empty_like(lens)
+    below = torch.empty((4, 2, 64), dtype=torch.bfloat16, device="cuda")
+    below[2:] = k
+    for rows in (2, 2 ** 40, 2 ** 62):
+        # values written below their sources (above them every byte may be a source's)
+        call = lambda a, b: select.cache_append(s.handle, 2, cache.struct, t, t.shape[1], i32([3, 4]), below[2:], 128,  # noqa: E731
+                                                below[2:], 128, rows, i32([1, 0]), off, off_h, 1.0, 1.0, cache.weights, a, b,
+                                                new, torch.cuda.current_stream().cuda_stream)
+        call(below[:2], None)
+        assert torch.equal(below[2:], k)
+        refused(select, "INVALID_ARG", lambda: call(below[1:3], None))
+        refused(select, "INVALID_ARG", lambda: call(None, below[3:]))
+    s.check_device()
+    s.close()
