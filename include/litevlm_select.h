@@ -633,7 +633,7 @@ litevlm_status_t litevlm_select_cache_append(litevlm_select_t handle, int32_t ba
  *   q_offsets_d/h    int32 [batch+1] prefix of T_b (T_b = 1: a decoding step; T_b = 0:
  *                    the request takes no part)
  *   max_len          a bound of the lengths, 0 <= max_len <= table_width * page_size, at
- *                    most 2^30: it sizes the launch and the workspace
+ *                    most 2^30: it sizes the launch and the workspace (best near them)
  *   q_scale          e4m3: the codes' per-tensor scale; bf16: 1
  *   weights_in/out   device float [num_pages][page_size], both or neither. The same
  *                    array: weights are added up in place. Two arrays: the sums go to
