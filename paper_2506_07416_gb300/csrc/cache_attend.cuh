@@ -33,8 +33,8 @@ __device__ __forceinline__ uint32_t pack_h2(float lo, float hi) { return h2_bits
 // How the keys are split, where the plan gives them slots (below three rounds of whole requests, see
 // plan_cache_attend), found by a warp from the lengths on the device: equal chunks, as short as they may be while all
 // requests together have at most a.slots of them (the CTAs that run at once), so that neither lengths that differ
-// nor a max_len far above them leave SMs without work. Of 32 candidate lengths from the mean on, in steps of an eighth of it,
-// the first that fits is taken. Requests without queries take no part.
+// nor a max_len far above them leave SMs without work. Of 32 candidate lengths from the mean on, in steps of an
+// eighth of it, the first that fits is taken. Requests without queries take no part.
 __device__ __forceinline__ int keys_of(const AttendArgs& a, int b)
 {
     bool bad;
