@@ -698,6 +698,116 @@ litevlm_status_t litevlm_select_cache_evict(litevlm_select_t handle, int32_t bat
                                             int32_t* kept_idx, int32_t* new_lens, litevlm_stream_t stream);
 
 /*
+ * Pages for the tokens that requests are to hold, and the slots of their new ones. Free
+ * pages lie in a ring, oldest first: state[0] is the place of the first, state[1] their number. A
+ * request that holds `held` tokens and is to hold `want` has ceil(held / page_size) pages and needs
+ * ceil(want / page_size). In the order of the requests, those that need more take them from the ring's
+ * front into their table row, until the first that finds too few: it and the later ones that need pages
+ * stay as they were (granted = held, slots -1; no error). Those that need fewer put the pages behind their last one
+ * behind the ring's end, in order (free for the next call); their table entries stay. Nothing is taken twice or lost: a
+ * call with want = 0 gives back all that a request has.
+ *   page_size        a power of two in [16, 256]
+ *   table            device int32 [batch][table_width], updated in place
+ *   held, want       device int32 [batch], tokens in [0, table_width * page_size]
+ *   free_pages       device int32 [num_pages], the ring, updated in place
+ *   state, new_state device int32 [2]: the ring's head and count before and after the call
+ *   new_offsets_d/h  int32 [batch+1] prefix of T_b, the new tokens among a request's want: its last ones
+ *   granted          device int32 [batch]: want, or held where there were too few pages
+ *   slots            device int64 [sum T_b], 8-byte aligned: page * page_size + slot of every new token, in order
+ * No two pages of the ring and of the tables are the same. What the call writes overlaps none of its other arrays.
+ * A length outside its range is cut to it, a token before position 0, a page outside [0, num_pages) and one that the
+ * ring has no place for give no slot or are lost, and a state that is none leaves the ring as it is: all set
+ * DEVICE_BOUNDS. Needs none of the handle's head sizes. Errors: INVALID_ARG / WORKSPACE as above.
+ */
+litevlm_status_t litevlm_select_cache_reserve(litevlm_select_t handle, int32_t batch, int32_t page_size,
+                                              int32_t* table, int32_t table_width, const int32_t* held,
+                                              const int32_t* want, int32_t* free_pages, int32_t num_pages,
+                                              const int32_t* state, const int32_t* new_offsets_d,
+                                              const int32_t* new_offsets_h, int32_t* granted, int32_t* new_state,
+                                              int64_t* slots, litevlm_stream_t stream);
+
+/*
+ * The ranges of a pool's keys, by which a query picks pages: for each page, key head and channel the largest and the
+ * smallest of the page's K values (without k_scale), outwards as whole numbers of 2^exps, owned by the caller.
+ *   codes       device int8 [num_pages][num_kv_heads][2][d]: largest, smallest; 16-byte aligned
+ *   exps        device int8 [num_pages][num_kv_heads]
+ *   num_pages, page_size   those of the cache
+ */
+typedef struct {
+    void* codes;
+    void* exps;
+    int32_t num_pages;
+    int32_t page_size;
+} litevlm_key_bounds_t;
+
+/*
+ * Renews the ranges of the pages that hold a request's last T_b tokens (n_b = seq_lens[b], the tokens appended
+ * before), from all tokens of these pages. With m = f * 2^p, 1/2 <= f < 1, the largest magnitude of a head's channels:
+ *     exps = p - 7 (0 where m = 0);  codes = ceil(largest / 2^exps), floor(smallest / 2^exps), at most 126
+ * A value whose scale is NaN counts as 0. After litevlm_select_cache_evict, or for a cache that has no ranges
+ * yet: with T_b = n_b. The V tensors are not read.
+ *   new_offsets_d/h  int32 [batch+1] prefix of T_b (0: the request's ranges stay)
+ * Requests that share a page have the same tokens in it. Lengths and tables are checked as by the other calls; a T_b
+ * beyond n_b is cut to it (DEVICE_BOUNDS). Errors: as above.
+ */
+litevlm_status_t litevlm_select_cache_bounds(litevlm_select_t handle, int32_t batch, const litevlm_cache_t* cache,
+                                             const litevlm_key_bounds_t* bounds, const int32_t* table,
+                                             int32_t table_width, const int32_t* seq_lens,
+                                             const int32_t* new_offsets_d, const int32_t* new_offsets_h,
+                                             litevlm_stream_t stream);
+
+/*
+ * The pages that every query attends to, for each key head. Query i of request b stands at position p = n_b - T_b + i
+ * and sees the pages 0 to P = p / page_size of its request. With r the whole numbers nearest to q / 2^(e - 7) (a tie to
+ * the even one, at most 127), 2^e the least power of two above the magnitudes of the key head's G query heads:
+ *     S(page) = 2^exps * max over the G heads of sum over channels of r * (r > 0 ? largest : smallest)
+ * which no key of the page passes by more than the rounding of q. Where P + 1 <= budget all pages are picked, else the
+ * first `sink`, the last `recent`, and of the others those of the largest S until budget are (ties: the lower page).
+ * The sums are exact, so the same inputs pick the same pages in every batch.
+ *   q                device [sum T_b][Hq][d] as in litevlm_select_cache_attend (its scale does not matter). NaN counts
+ *                    as 0, an infinity as the largest finite value
+ *   q_offsets_d/h    int32 [batch+1] prefix of T_b
+ *   max_len          a bound of the lengths, 0 <= max_len <= table_width * page_size, at most 2^30
+ *   budget           >= 1, its pages hold at most 2^30 tokens; sink, recent >= 0, sink + recent <= budget
+ *   picked           device int32 [sum T_b][Hkv][budget]: pages of the request (0: its first), ascending, then -1
+ *   workspace        device, at least the bytes that litevlm_select_cache_pick_workspace gives for the same sizes (4 for
+ *                    every query, key head and page of max_len; 0 where budget holds max_len), 256-byte aligned; as for
+ *                    litevlm_select_cache_attend
+ * exps are in [-100, 100] (cut to it). A page whose table entry is not in the pool ranks below all others (DEVICE_BOUNDS).
+ * Errors: as above; UNSUPPORTED for more than 128 query heads a key head, or where Hkv x ceil(T_b / (64 / G)) passes
+ * 65535 (G rounded up to 1, 2, 4 or a multiple of 8) or Hkv x sum T_b passes 2^31 - 1.
+ */
+litevlm_status_t litevlm_select_cache_pick_workspace(litevlm_select_t handle, int32_t batch,
+                                                     const int32_t* q_offsets_h, int32_t max_len, int32_t page_size,
+                                                     int32_t budget, int64_t* bytes);
+litevlm_status_t litevlm_select_cache_pick(litevlm_select_t handle, int32_t batch, const litevlm_key_bounds_t* bounds,
+                                           const int32_t* table, int32_t table_width, const int32_t* seq_lens,
+                                           const void* q, int64_t q_row_stride, const int32_t* q_offsets_d,
+                                           const int32_t* q_offsets_h, int32_t max_len, int32_t budget, int32_t sink,
+                                           int32_t recent, int32_t* picked, void* workspace, int64_t workspace_bytes,
+                                           litevlm_stream_t stream);
+
+/*
+ * litevlm_select_cache_attend over picked pages alone: the softmax runs over the positions up to the query's own in the
+ * pages that its list names for the key head, so that a query costs budget * page_size keys whatever the cache's length.
+ *   picked           device int32 [sum T_b][Hkv][budget]: pages of the request, in any order, no page twice for a query
+ *                    and key head (its result is then not defined). Entries that name no page that the query
+ *                    sees (-1 among them) are skipped
+ *   workspace        at least the bytes that litevlm_select_cache_attend_picked_workspace gives for the same sizes
+ * A query whose list has no key that it sees gives zeros. The other arguments, the precision and the errors are those
+ * of litevlm_select_cache_attend without weights (table_width * page_size bounds the lengths).
+ */
+litevlm_status_t litevlm_select_cache_attend_picked_workspace(litevlm_select_t handle, int32_t batch,
+                                                              const int32_t* q_offsets_h, int32_t page_size,
+                                                              int32_t budget, int64_t* bytes);
+litevlm_status_t litevlm_select_cache_attend_picked(litevlm_select_t handle, int32_t batch, const litevlm_cache_t* cache,
+                                                    const int32_t* table, int32_t table_width, const int32_t* seq_lens,
+                                                    const void* q, int64_t q_row_stride, const int32_t* q_offsets_d,
+                                                    const int32_t* q_offsets_h, const int32_t* picked, int32_t budget,
+                                                    float q_scale, void* out, void* workspace, int64_t workspace_bytes,
+                                                    litevlm_stream_t stream);
+
+/*
  * Verification of drafted tokens (Design section, Speculative Decoding Head): draft
  * t of a request, token x with the draft model's probability q and the target's p,
  * is accepted while u_accept * q < p (exact products). Behind the accepted drafts

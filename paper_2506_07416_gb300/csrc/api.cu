@@ -1292,6 +1292,21 @@ litevlm_status_t start_call(litevlm_select_t h, int32_t batch)
     return LITEVLM_OK;
 }
 
+// Checks a page size and a table; gives the page's shift and `limit`, the tokens a table row holds.
+litevlm_status_t page_table(litevlm_select_t h, int32_t ps, int32_t num_pages, int32_t table_width, int32_t* shift,
+                            int32_t* limit)
+{
+    if (num_pages < 1) return fail(h, LITEVLM_ERR_INVALID_ARG, "num_pages must be >= 1");
+    if (ps < 16 || ps > 256 || (ps & (ps - 1)) != 0)
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "page_size must be a power of two in [16, 256]");
+    if (table_width < 1 || (int64_t)table_width * ps > INT32_MAX - 65536)
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "table_width must be >= 1 and its pages hold less than 2^31 - 2^16 tokens");
+    *shift = 0;
+    while ((1 << *shift) < ps) ++*shift;
+    *limit = table_width * ps;
+    return LITEVLM_OK;
+}
+
 // Checks a cache and a table; fills the kernels' view of them and `limit`, the tokens a table row holds.
 litevlm_status_t cache_pages(litevlm_select_t h, const litevlm_cache_t* c, const int32_t* table, int32_t table_width,
                              const int32_t* seq_lens, lvs::CachePages* out, int32_t* limit)
@@ -1301,14 +1316,10 @@ litevlm_status_t cache_pages(litevlm_select_t h, const litevlm_cache_t* c, const
         return fail(h, LITEVLM_ERR_INVALID_ARG, "a device pointer is NULL");
     if (!aligned16(c->k_codes) || !aligned16(c->k_scales) || !aligned16(c->v_codes) || !aligned16(c->v_scales))
         return fail(h, LITEVLM_ERR_INVALID_ARG, "the cache's tensors must be 16-byte aligned");
-    if (c->num_pages < 1) return fail(h, LITEVLM_ERR_INVALID_ARG, "num_pages must be >= 1");
-    const int32_t ps = c->page_size;
-    if (ps < 16 || ps > 256 || (ps & (ps - 1)) != 0)
-        return fail(h, LITEVLM_ERR_INVALID_ARG, "page_size must be a power of two in [16, 256]");
     if (!in_range(c->k_scale) || !in_range(c->v_scale))
         return fail(h, LITEVLM_ERR_INVALID_ARG, "k_scale and v_scale must be in [2^-60, 2^60]");
-    if (table_width < 1 || (int64_t)table_width * ps > INT32_MAX - 65536)
-        return fail(h, LITEVLM_ERR_INVALID_ARG, "table_width must be >= 1 and its pages hold less than 2^31 - 2^16 tokens");
+    const litevlm_status_t s = page_table(h, c->page_size, c->num_pages, table_width, &out->page_shift, limit);
+    if (s != LITEVLM_OK) return s;
     out->codes[0] = static_cast<uint8_t*>(c->k_codes);
     out->codes[1] = static_cast<uint8_t*>(c->v_codes);
     out->scales[0] = static_cast<uint8_t*>(c->k_scales);
@@ -1316,13 +1327,19 @@ litevlm_status_t cache_pages(litevlm_select_t h, const litevlm_cache_t* c, const
     out->scale[0] = c->k_scale;
     out->scale[1] = c->v_scale;
     out->num_pages = c->num_pages;
-    out->page_shift = 0;
-    while ((1 << out->page_shift) < ps) ++out->page_shift;
     out->hkv = h->cfg.num_kv_heads;
     if (out->hkv > 65535) return fail(h, LITEVLM_ERR_UNSUPPORTED, "more than 65535 key heads");
     out->table = table;
     out->width = table_width;
-    *limit = table_width * ps;
+    return LITEVLM_OK;
+}
+
+// Checks the ranges of a pool's keys.
+litevlm_status_t check_bounds(litevlm_select_t h, const litevlm_key_bounds_t* r)
+{
+    if (!r) return fail(h, LITEVLM_ERR_INVALID_ARG, "bounds is NULL");
+    if (!r->codes || !r->exps) return fail(h, LITEVLM_ERR_INVALID_ARG, "a device pointer is NULL");
+    if (!aligned16(r->codes)) return fail(h, LITEVLM_ERR_INVALID_ARG, "the ranges' codes must be 16-byte aligned");
     return LITEVLM_OK;
 }
 
@@ -1398,9 +1415,325 @@ litevlm_status_t attend_plan(litevlm_select_t h, int32_t batch, const int32_t* q
     return LITEVLM_OK;
 }
 
+// Checks the sizes of a selection of pages; gives the stride of a query's keys and the bytes of them all.
+litevlm_status_t pick_plan(litevlm_select_t h, int32_t batch, const int32_t* q_offsets_h, int32_t max_len,
+                           int32_t page_size, int32_t budget, int64_t* total, int* max_t, int64_t* stride, int64_t* bytes)
+{
+    const litevlm_select_config_t& c = h->cfg;
+    litevlm_status_t s = check_offsets(h, q_offsets_h, batch, INT32_MAX, "q_offsets", total);
+    if (s != LITEVLM_OK) return s;
+    if (max_len < 0 || max_len > lvs::kMostKeys)
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "max_len must be in [0, 2^30]");
+    int32_t shift = 0, limit = 0;
+    s = page_table(h, page_size, 1, 1, &shift, &limit);
+    if (s != LITEVLM_OK) return s;
+    if (budget < 1 || (int64_t)budget * page_size > lvs::kMostKeys)
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "budget must be >= 1 and its pages hold at most 2^30 tokens");
+    const int group = c.num_q_heads / c.num_kv_heads;
+    if (group > 128) return fail(h, LITEVLM_ERR_UNSUPPORTED, "more than 128 query heads a key head");
+    *max_t = max_count(q_offsets_h, batch);
+    if ((int64_t)lvs::pick_col_tiles(*max_t, group) * c.num_kv_heads > 65535 || *total * c.num_kv_heads > INT32_MAX)
+        return fail(h, LITEVLM_ERR_UNSUPPORTED, "num_kv_heads x the queries' tiles exceeds the grid");
+    *stride = lvs::pick_key_stride(max_len, shift, budget);
+    if ((double)*total * c.num_kv_heads * (double)*stride * 4.0 > 0x1p60)
+        return fail(h, LITEVLM_ERR_UNSUPPORTED, "the workspace would pass 2^60 bytes");
+    *bytes = round256(*total * c.num_kv_heads * *stride * 4);
+    return LITEVLM_OK;
+}
+
+// The same of attention over picked pages.
+struct PickedSpace {
+    int64_t part_o, part_ml, total;
+};
+litevlm_status_t picked_plan(litevlm_select_t h, int32_t batch, const int32_t* q_offsets_h, int32_t page_size,
+                             int32_t budget, int64_t* total, lvs::PickedPlan* plan, PickedSpace* space)
+{
+    const litevlm_select_config_t& c = h->cfg;
+    litevlm_status_t s = check_offsets(h, q_offsets_h, batch, INT32_MAX, "q_offsets", total);
+    if (s != LITEVLM_OK) return s;
+    int32_t shift = 0, limit = 0;
+    s = page_table(h, page_size, 1, 1, &shift, &limit);
+    if (s != LITEVLM_OK) return s;
+    if (budget < 1 || (int64_t)budget * page_size > lvs::kMostKeys)
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "budget must be >= 1 and its pages hold at most 2^30 tokens");
+    *plan = lvs::plan_attend_picked(*total, c.num_kv_heads, c.num_q_heads / c.num_kv_heads, (int64_t)budget << shift,
+                                    h->num_sms);
+    const int64_t subs = (c.num_q_heads / c.num_kv_heads + plan->row_tile - 1) / plan->row_tile;
+    if (*total * plan->chunks > INT32_MAX || subs * c.num_kv_heads > 65535)
+        return fail(h, LITEVLM_ERR_UNSUPPORTED, "the queries or the heads exceed the grid");
+    const int64_t parts = plan->chunks > 1 ? *total * plan->chunks * c.num_q_heads : 0;
+    space->part_o = 0;
+    space->part_ml = round256(parts * c.head_dim * 4);
+    space->total = space->part_ml + round256(parts * 8);
+    return LITEVLM_OK;
+}
+
+litevlm_status_t check_workspace(litevlm_select_t h, const void* workspace, int64_t bytes, int64_t need)
+{
+    if (bytes < need || (need > 0 && !workspace))
+        return fail(h, LITEVLM_ERR_WORKSPACE, "the workspace must hold " + std::to_string(need) + " bytes");
+    if (reinterpret_cast<uintptr_t>(workspace) & 255u)
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "the workspace must be 256-byte aligned");
+    return LITEVLM_OK;
+}
+
 }  // namespace
 
 extern "C" {
+
+litevlm_status_t litevlm_select_cache_reserve(litevlm_select_t h, int32_t batch, int32_t page_size, int32_t* table,
+                                              int32_t table_width, const int32_t* held, const int32_t* want,
+                                              int32_t* free_pages, int32_t num_pages, const int32_t* state,
+                                              const int32_t* new_offsets_d, const int32_t* new_offsets_h,
+                                              int32_t* granted, int32_t* new_state, int64_t* slots,
+                                              litevlm_stream_t stream)
+{
+    const CallRange range_(__func__);
+    if (!h) return LITEVLM_ERR_INVALID_ARG;
+    litevlm_status_t s = start_call(h, batch);
+    if (s != LITEVLM_OK) return s;
+    lvs::ReserveArgs a{};
+    s = check_offsets(h, new_offsets_h, batch, INT32_MAX, "new_offsets", &a.rows);
+    if (s == LITEVLM_OK) s = page_table(h, page_size, num_pages, table_width, &a.page_shift, &a.limit);
+    if (s != LITEVLM_OK) return s;
+    if (!free_pages || !state || !new_state || (batch > 0 && (!table || !held || !want || !new_offsets_d || !granted)) ||
+        (a.rows > 0 && !slots))
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "a device pointer is NULL");
+    if (reinterpret_cast<uintptr_t>(slots) & 7u)
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "slots must be 8-byte aligned");
+    const int64_t n = (int64_t)batch * 4, pages = (int64_t)num_pages * 4, entries = (int64_t)batch * table_width * 4;
+    const struct {
+        const void* p;
+        int64_t bytes;
+        bool out;
+    } all[] = {{table, entries, true},  {free_pages, pages, true}, {granted, n, true},     {new_state, 8, true},
+               {slots, a.rows * 8, true}, {held, n, false},        {want, n, false},       {state, 8, false},
+               {new_offsets_d, n + 4, false}};
+    for (const auto& x : all)
+        for (const auto& y : all)
+            if (x.out && &x != &y && overlap(x.p, x.bytes, y.p, y.bytes))
+                return fail(h, LITEVLM_ERR_INVALID_ARG, "what the call writes must not overlap its other arrays");
+    s = debug_mirror(h, new_offsets_d, new_offsets_h, (int64_t)batch + 1, "new_offsets", stream);
+    if (s != LITEVLM_OK) return s;
+    a.table = table;
+    a.width = table_width;
+    a.num_pages = num_pages;
+    a.held = held;
+    a.want = want;
+    a.free = free_pages;
+    a.state = state;
+    a.new_state = new_state;
+    a.off = new_offsets_d;
+    a.batch = batch;
+    a.granted = granted;
+    a.slots = slots;
+    a.vec = aligned16(slots);
+    a.err = h->err_d;
+    const OnDevice on(h->device);
+    cudaError_t e = on.e;
+    if (e == cudaSuccess) e = lvs::launch_cache_reserve(a, h->num_sms, (cudaStream_t)stream);
+    if (e != cudaSuccess) return cuda_fail(h, e, "cache_reserve launch");
+    h->last_launches = 1;
+    return LITEVLM_OK;
+}
+
+litevlm_status_t litevlm_select_cache_bounds(litevlm_select_t h, int32_t batch, const litevlm_cache_t* cache,
+                                             const litevlm_key_bounds_t* bounds, const int32_t* table,
+                                             int32_t table_width, const int32_t* seq_lens,
+                                             const int32_t* new_offsets_d, const int32_t* new_offsets_h,
+                                             litevlm_stream_t stream)
+{
+    const CallRange range_(__func__);
+    if (!h) return LITEVLM_ERR_INVALID_ARG;
+    litevlm_status_t s = start_call(h, batch);
+    if (s != LITEVLM_OK) return s;
+    int64_t rows = 0;
+    s = check_offsets(h, new_offsets_h, batch, INT32_MAX, "new_offsets", &rows);
+    if (s != LITEVLM_OK || batch == 0) return s;
+    lvs::BoundsArgs a{};
+    s = cache_pages(h, cache, table, table_width, seq_lens, &a.cache, &a.limit);
+    if (s == LITEVLM_OK) s = check_bounds(h, bounds);
+    if (s != LITEVLM_OK) return s;
+    if (bounds->num_pages != cache->num_pages || bounds->page_size != cache->page_size)
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "the ranges and the cache have different pages");
+    if (!new_offsets_d) return fail(h, LITEVLM_ERR_INVALID_ARG, "a device pointer is NULL");
+    s = debug_mirror(h, new_offsets_d, new_offsets_h, (int64_t)batch + 1, "new_offsets", stream);
+    if (s != LITEVLM_OK || rows == 0) return s;
+    a.codes = static_cast<int8_t*>(bounds->codes);
+    a.exps = static_cast<int8_t*>(bounds->exps);
+    a.lens = seq_lens;
+    a.off = new_offsets_d;
+    a.places = lvs::page_at(rows, batch, a.cache.page_shift);
+    a.batch = batch;
+    a.err = h->err_d;
+    if (a.places * a.cache.hkv > (int64_t)INT32_MAX * 4)
+        return fail(h, LITEVLM_ERR_UNSUPPORTED, "the new tokens' pages x key heads exceed the grid");
+    const OnDevice on(h->device);
+    cudaError_t e = on.e;
+    if (e == cudaSuccess) e = lvs::launch_cache_bounds(a, h->cfg.head_dim, (cudaStream_t)stream);
+    if (e != cudaSuccess) return cuda_fail(h, e, "cache_bounds launch");
+    h->last_launches = 1;
+    return LITEVLM_OK;
+}
+
+litevlm_status_t litevlm_select_cache_pick_workspace(litevlm_select_t h, int32_t batch, const int32_t* q_offsets_h,
+                                                     int32_t max_len, int32_t page_size, int32_t budget, int64_t* bytes)
+{
+    const CallRange range_(__func__);
+    if (!h) return LITEVLM_ERR_INVALID_ARG;
+    litevlm_status_t s = start_call(h, batch);
+    if (s != LITEVLM_OK) return s;
+    if (!bytes) return fail(h, LITEVLM_ERR_INVALID_ARG, "bytes is NULL");
+    int64_t total = 0, stride = 0, need = 0;
+    int max_t = 0;
+    s = pick_plan(h, batch, q_offsets_h, max_len, page_size, budget, &total, &max_t, &stride, &need);
+    if (s == LITEVLM_OK) *bytes = need;
+    return s;
+}
+
+litevlm_status_t litevlm_select_cache_pick(litevlm_select_t h, int32_t batch, const litevlm_key_bounds_t* bounds,
+                                           const int32_t* table, int32_t table_width, const int32_t* seq_lens,
+                                           const void* q, int64_t q_row_stride, const int32_t* q_offsets_d,
+                                           const int32_t* q_offsets_h, int32_t max_len, int32_t budget, int32_t sink,
+                                           int32_t recent, int32_t* picked, void* workspace, int64_t workspace_bytes,
+                                           litevlm_stream_t stream)
+{
+    const CallRange range_(__func__);
+    if (!h) return LITEVLM_ERR_INVALID_ARG;
+    litevlm_status_t s = start_call(h, batch);
+    if (s == LITEVLM_OK) s = check_bounds(h, bounds);
+    if (s != LITEVLM_OK) return s;
+    const litevlm_select_config_t& c = h->cfg;
+    lvs::PickArgs a{};
+    int64_t need = 0;
+    int max_t = 0;
+    s = pick_plan(h, batch, q_offsets_h, max_len, bounds->page_size, budget, &a.rows, &max_t, &a.key_stride, &need);
+    if (s != LITEVLM_OK) return s;
+    if (sink < 0 || recent < 0 || (int64_t)sink + recent > budget)
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "sink and recent must be >= 0 and sink + recent <= budget");
+    if (a.rows == 0) return LITEVLM_OK;
+    int32_t holds = 0;
+    s = page_table(h, bounds->page_size, bounds->num_pages, table_width, &a.page_shift, &holds);
+    if (s != LITEVLM_OK) return s;
+    if (max_len > holds) return fail(h, LITEVLM_ERR_INVALID_ARG, "max_len exceeds table_width * page_size");
+    if (!table || !seq_lens || !q_offsets_d || !picked) return fail(h, LITEVLM_ERR_INVALID_ARG, "a device pointer is NULL");
+    s = check_rows(h, q, q_row_stride, c.num_q_heads, 1.f, "q");
+    if (s == LITEVLM_OK) s = check_workspace(h, workspace, workspace_bytes, need);
+    if (s == LITEVLM_OK) s = debug_mirror(h, q_offsets_d, q_offsets_h, (int64_t)batch + 1, "q_offsets", stream);
+    if (s != LITEVLM_OK) return s;
+    const int64_t row = (int64_t)c.num_q_heads * c.head_dim, lists = a.rows * c.num_kv_heads * budget * 4;
+    if (overlap_rows(picked, lists, q, a.rows, q_row_stride, row, c.qk_dtype == LITEVLM_FP8_E4M3 ? 1 : 2) ||
+        overlap(picked, lists, workspace, need))
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "picked must not overlap q or the workspace");
+    a.codes = static_cast<const int8_t*>(bounds->codes);
+    a.exps = static_cast<const int8_t*>(bounds->exps);
+    a.num_pages = bounds->num_pages;
+    a.hkv = c.num_kv_heads;
+    a.table = table;
+    a.width = table_width;
+    a.lens = seq_lens;
+    a.q = q;
+    a.q_stride = q_row_stride;
+    a.off = q_offsets_d;
+    a.batch = batch;
+    a.hq = c.num_q_heads;
+    a.group = c.num_q_heads / c.num_kv_heads;
+    a.limit = max_len;
+    a.budget = budget;
+    a.sink = sink;
+    a.recent = recent;
+    a.keys = static_cast<uint32_t*>(workspace);
+    a.picked = picked;
+    a.err = h->err_d;
+    const OnDevice on(h->device);
+    cudaError_t e = on.e;
+    int32_t launches = 0;
+    if (e == cudaSuccess)
+        e = lvs::launch_cache_pick(a, c.head_dim, c.qk_dtype == LITEVLM_FP8_E4M3, max_t, max_len, h->num_sms,
+                                   (cudaStream_t)stream, &launches);
+    if (e != cudaSuccess) return cuda_fail(h, e, "cache_pick launch");
+    h->last_launches = launches;
+    return LITEVLM_OK;
+}
+
+litevlm_status_t litevlm_select_cache_attend_picked_workspace(litevlm_select_t h, int32_t batch,
+                                                              const int32_t* q_offsets_h, int32_t page_size,
+                                                              int32_t budget, int64_t* bytes)
+{
+    const CallRange range_(__func__);
+    if (!h) return LITEVLM_ERR_INVALID_ARG;
+    litevlm_status_t s = start_call(h, batch);
+    if (s != LITEVLM_OK) return s;
+    if (!bytes) return fail(h, LITEVLM_ERR_INVALID_ARG, "bytes is NULL");
+    int64_t total = 0;
+    lvs::PickedPlan plan;
+    PickedSpace space;
+    s = picked_plan(h, batch, q_offsets_h, page_size, budget, &total, &plan, &space);
+    if (s == LITEVLM_OK) *bytes = space.total;
+    return s;
+}
+
+litevlm_status_t litevlm_select_cache_attend_picked(litevlm_select_t h, int32_t batch, const litevlm_cache_t* cache,
+                                                    const int32_t* table, int32_t table_width, const int32_t* seq_lens,
+                                                    const void* q, int64_t q_row_stride, const int32_t* q_offsets_d,
+                                                    const int32_t* q_offsets_h, const int32_t* picked, int32_t budget,
+                                                    float q_scale, void* out, void* workspace, int64_t workspace_bytes,
+                                                    litevlm_stream_t stream)
+{
+    const CallRange range_(__func__);
+    if (!h) return LITEVLM_ERR_INVALID_ARG;
+    litevlm_status_t s = start_call(h, batch);
+    if (s != LITEVLM_OK) return s;
+    if (!cache) return fail(h, LITEVLM_ERR_INVALID_ARG, "cache is NULL");
+    const litevlm_select_config_t& c = h->cfg;
+    lvs::PickedPlan plan;
+    PickedSpace space;
+    int64_t total = 0;
+    s = picked_plan(h, batch, q_offsets_h, cache->page_size, budget, &total, &plan, &space);
+    if (s != LITEVLM_OK || total == 0) return s;
+    lvs::AttendArgs a{};
+    s = cache_pages(h, cache, table, table_width, seq_lens, &a.cache, &a.limit);
+    if (s == LITEVLM_OK) s = check_rows(h, q, q_row_stride, c.num_q_heads, q_scale, "q");
+    if (s != LITEVLM_OK) return s;
+    if (!q_offsets_d || !picked) return fail(h, LITEVLM_ERR_INVALID_ARG, "a device pointer is NULL");
+    if (!out || !aligned16(out)) return fail(h, LITEVLM_ERR_INVALID_ARG, "out must be 16-byte aligned and not NULL");
+    const int64_t row = (int64_t)c.num_q_heads * c.head_dim;
+    if (overlap_rows(out, total * row * 2, q, total, q_row_stride, row, c.qk_dtype == LITEVLM_FP8_E4M3 ? 1 : 2) ||
+        overlap(out, total * row * 2, picked, total * c.num_kv_heads * budget * 4))
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "out must not overlap q or picked");
+    s = check_workspace(h, workspace, workspace_bytes, space.total);
+    if (s == LITEVLM_OK) s = debug_mirror(h, q_offsets_d, q_offsets_h, (int64_t)batch + 1, "q_offsets", stream);
+    if (s != LITEVLM_OK) return s;
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    a.q = q;
+    a.q_stride = q_row_stride;
+    a.q_off = q_offsets_d;
+    a.lens = seq_lens;
+    a.batch = batch;
+    a.hq = c.num_q_heads;
+    a.group = c.num_q_heads / c.num_kv_heads;
+    a.c_log2 = (float)((double)q_scale * (double)cache->k_scale / sqrt((double)c.head_dim) * 1.4426950408889634);
+    a.num_sms = h->num_sms;
+    a.out = static_cast<__nv_bfloat16*>(out);
+    a.part_o = reinterpret_cast<float*>(ws + space.part_o);
+    a.part_ml = reinterpret_cast<float2*>(ws + space.part_ml);
+    a.max_rows = a.group;
+    a.picked = picked;
+    a.budget = budget;
+    a.pick_chunk = plan.chunk;
+    a.pick_chunks = plan.chunks;
+    a.err = h->err_d;
+    a.wait_budget = h->wait_budget;
+    const OnDevice on(h->device);
+    cudaError_t e = on.e;
+    int32_t launches = 0;
+    if (e == cudaSuccess)
+        e = lvs::launch_attend_picked(a, plan, c.head_dim, c.qk_dtype == LITEVLM_FP8_E4M3, total, (cudaStream_t)stream,
+                                      &launches);
+    if (e != cudaSuccess) return cuda_fail(h, e, "cache_attend_picked launch");
+    h->last_launches = launches;
+    return LITEVLM_OK;
+}
 
 litevlm_status_t litevlm_select_cache_append(litevlm_select_t h, int32_t batch, const litevlm_cache_t* cache,
                                              const int32_t* table, int32_t table_width, const int32_t* seq_lens,

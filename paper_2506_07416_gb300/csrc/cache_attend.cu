@@ -220,7 +220,9 @@ constexpr int kRingBytes = kAttWarps * kAttStages * 2 * Group<D>::kBytes;
 // which keeps addresses out of the lanes' registers: the sweep's 128 requests take 127 us
 // and not 135).
 // (CTAs of an SM as the plan of the split counts them.)
-template <int D, int NT_, bool FP8, bool WHOLE>
+// PICKED: the keys are those of the pages that the query has in its list, in the list's order; a CTA's rows are heads
+// of one query, and a CTA takes all of the list or a chunk of it.
+template <int D, int NT_, bool FP8, bool WHOLE, bool PICKED = false>
 __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_kernel(const __grid_constant__ AttendArgs a)
 {
     constexpr bool SINGLE = NT_ == 0;
@@ -242,7 +244,13 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
     // the request, and its part of the keys: all, or the chunk of this CTA's slot
     int b = blockIdx.z, chunk = kMostKeys, k0 = 0;
     __shared__ int split_s[3];
-    if (!WHOLE && a.slots > 0) {
+    const int64_t pick_row = PICKED ? blockIdx.x / a.pick_chunks : 0;  // the query
+    const int32_t* list = PICKED ? a.picked + (pick_row * a.cache.hkv + h) * a.budget : nullptr;
+    if constexpr (PICKED) {
+        chunk = a.pick_chunk;
+        k0 = (int)(blockIdx.x % a.pick_chunks) * chunk;
+        b = uniform(find_request(a.q_off, a.batch, pick_row));
+    } else if (!WHOLE && a.slots > 0) {
         if (threadIdx.x < 32) {
             chunk = chunk_keys(a);
             find_slot(a, blockIdx.x, chunk, b, k0);
@@ -254,14 +262,19 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
         // (for the launch that joins the chunks: their length, and the request's first slot)
         if (k0 == 0 && blockIdx.y == 0 && threadIdx.x == 0) a.split[b] = make_int2(chunk, (int)blockIdx.x);
     }
-    const RowTile rt = row_tile(a, b, tile, ROWS);
-    if (rt.rows <= 0) return;
+    RowTile rt = row_tile(a, b, tile, ROWS);
     const int q0 = a.q_off[b];
+    if constexpr (PICKED) {
+        const int i = (int)(pick_row - q0);
+        rt.row0 = i * a.group + tile * ROWS;
+        rt.rows = min(ROWS, a.group - tile * ROWS);
+    }
+    if (rt.rows <= 0) return;
     const int i_last = rt.query(rt.row0 + rt.rows - 1);
-    // keys that the tile's last row sees, and this CTA's part of them
-    const int seen = min(rt.len, rt.last0 + i_last + 1);
+    // keys that the tile's last row sees, and this CTA's part of them (PICKED: keys of the list)
+    const int seen = PICKED ? a.budget << a.cache.page_shift : min(rt.len, rt.last0 + i_last + 1);
     const int k1 = chunk_end(seen, k0, chunk);
-    if (k0 >= k1 && !WHOLE && a.slots > 0) return;  // (without chunks the tile's zeros are written here, else by the join)
+    if (!PICKED && k0 >= k1 && !WHOLE && a.slots > 0) return;  // (without chunks the tile's zeros are written here, else by the join)
     const int all_see = rt.last0 + rt.query(rt.row0);  // the last key that every row sees
 
     constexpr int SPAN = 2 * G::kBytes;
@@ -269,22 +282,38 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
     const uint32_t my_s = smem_u32(my);
     const int spans = k1 > k0 ? (k1 - k0 + 31) / 32 : 0;
     const int n_mine = spans > warp ? (spans - warp + kAttWarps - 1) / kAttWarps : 0;
-    // page of the lane's group of the warp's n-th span (-1: none; no keys from k1 on are copied)
+    // page of the lane's group of the warp's n-th span (-1: none; no keys from k1 on are copied), and of a listed page
+    // how many of the group's keys the query sees
+    int next_sees = 0;
     auto page_of = [&](int n) -> int32_t {
         const int j = k0 + (warp + n * kAttWarps) * 32 + (lane & 16);
+        if constexpr (PICKED) {
+            next_sees = 0;
+            if (j >= k1) return -1;
+            const int32_t o = __ldg(list + (j >> a.cache.page_shift));
+            if (o < 0 || o > all_see >> a.cache.page_shift) return -1;
+            const int64_t at = (int64_t)o << a.cache.page_shift;
+            const int n_see = all_see - (int)at - (j & ((1 << a.cache.page_shift) - 1)) + 1;
+            if (n_see <= 0) return -1;
+            const int32_t p = cache_page(a.cache.table, a.cache.width, a.cache.num_pages, a.cache.page_shift, b, at);
+            if (p >= 0) next_sees = min(n_see, 16);
+            else if ((lane & 15) == 0) atomicOr(a.err, kErrBounds);
+            return p;
+        }
         if (j >= k1) return -1;
         const int32_t p = cache_page(a.cache.table, a.cache.width, a.cache.num_pages, a.cache.page_shift, b, j);
         if (p < 0 && (lane & 15) == 0) atomicOr(a.err, kErrBounds);
         return p;
     };
-    // whether the lane's group has a page, a bit for every span on its way, the last one's lowest
+    // whether the lane's group has a page, a bit for every span on its way, the last one's lowest (PICKED: five bits,
+    // the keys seen)
     uint32_t named = 0;
 #pragma unroll
     for (int i = 0; i < kAttStages - 1; ++i) {
         const int32_t page = page_of(i);
         if (i < n_mine) load_span<D>(a.cache, page, h, k0 + (warp + i * kAttWarps) * 32, my_s + i * SPAN);
         copy_async_commit();
-        named = named << 1 | (page >= 0);
+        named = PICKED ? named << 5 | next_sees : named << 1 | (page >= 0);
     }
     int32_t next_page = page_of(kAttStages - 1);  // (read a span ahead: nothing waits for the table)
 
@@ -336,7 +365,8 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
     bool nan_value = false;
 
     // a group of 16 keys from j0 on, for a single row
-    auto group1 = [&](const uint8_t* grp, int j0, bool there, auto check) {
+    int sees_of[2] = {0, 0};  // PICKED: keys of a span's two groups that the query sees
+    auto group1 = [&](const uint8_t* grp, int j0, bool there, int n_sees, auto check) {
         constexpr bool CHECK = decltype(check)::value;
         constexpr int WORDS = D / 32;
         float s[4] = {0.f, 0.f, 0.f, 0.f};
@@ -377,7 +407,7 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
             z[e] += __shfl_xor_sync(0xffffffffu, z[e], 1);
             z[e] += __shfl_xor_sync(0xffffffffu, z[e], 2);
             z[e] *= fac[0][0];
-            if (CHECK && (!there || j0 + g + 8 * e >= k1)) z[e] = -INFINITY;
+            if (CHECK && (PICKED ? g + 8 * e >= n_sees : !there || j0 + g + 8 * e >= k1)) z[e] = -INFINITY;
         }
         if (a.logits && c == 0) {
             __stcg(logits + j0 + g, z[0]);
@@ -389,7 +419,7 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
         for (int e = 0; e < 4; ++e) {
             const int key = 2 * c + (e & 1) + 8 * (e >> 1);
             uint32_t sc = grp[G::kVs + (D == 128 ? key * 8 + g : key * 4 + g / 2)];
-            if (CHECK && j0 + key >= k1) sc = 0u;  // (bytes behind the last key may be anything)
+            if (CHECK && (PICKED ? key >= n_sees : j0 + key >= k1)) sc = 0u;  // (bytes behind the last key may be anything)
             scales |= sc << (8 * e);
         }
         const bool larger = (((scales + room) | scales) & 0x80808080u) != 0u;
@@ -476,8 +506,9 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     s[x][t][e] *= fac[t][e & 1];
-                    if (CHECK && (!(there >> (16 * x) & 1u) ||
-                                  j0 + 16 * x + g + 8 * (e >> 1) > min(vis[t][e & 1], k1 - 1)))
+                    if (CHECK && (PICKED ? g + 8 * (e >> 1) >= sees_of[x]
+                                         : !(there >> (16 * x) & 1u) ||
+                                               j0 + 16 * x + g + 8 * (e >> 1) > min(vis[t][e & 1], k1 - 1)))
                         s[x][t][e] = -INFINITY;
                 }
         if (a.logits) {
@@ -551,7 +582,9 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
                     w4[e][0] = *reinterpret_cast<const uint32_t*>(grp + G::kV + key * 32 + g * 4);
                     sc[e] = grp[G::kVs + key * 4 + g / 2];
                 }
-                if constexpr (CHECK) {
+                if constexpr (CHECK && PICKED) {
+                    if (key >= sees_of[x]) sc[e] = 0u;
+                } else if constexpr (CHECK) {
                     const int at = j0 + 16 * x + key;
                     // what lies behind the last key may be anything, a NaN scale among it
                     if (at >= k1) sc[e] = 0u;
@@ -591,29 +624,36 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
         copy_async_wait<kAttStages - 2>();
         __syncwarp();  // every lane's copies are there, and the span before is no longer read
         const int j0 = k0 + (warp + n * kAttWarps) * 32;
-        const bool mine = named >> (kAttStages - 2) & 1u;  // the lane's group of this span has a page
+        // the lane's group of this span has a page; the keys that a picked one has for the query
+        const int sees = PICKED ? named >> (5 * (kAttStages - 2)) & 31u : 0;
+        const bool mine = PICKED ? sees > 0 : named >> (kAttStages - 2) & 1u;
         {
             const int nx = n + kAttStages - 1;
             const int to = stage == 0 ? kAttStages - 1 : stage - 1;
             if (nx < n_mine)
                 load_span<D>(a.cache, next_page, h, j0 + (kAttStages - 1) * kAttWarps * 32, my_s + to * SPAN);
             copy_async_commit();
-            named = named << 1 | (next_page >= 0);
+            named = PICKED ? named << 5 | next_sees : named << 1 | (next_page >= 0);
             next_page = page_of(nx + 1);
         }
         const uint8_t* span = my + stage * SPAN;
         stage = stage + 1 == kAttStages ? 0 : stage + 1;
         const uint32_t there = __ballot_sync(0xffffffffu, mine);
-        const bool all = there == 0xFFFFFFFFu && j0 + 31 <= all_see;
+        if (PICKED && there == 0u) continue;
+        const bool all = PICKED ? __all_sync(0xffffffffu, sees == 16) : there == 0xFFFFFFFFu && j0 + 31 <= all_see;
+        if constexpr (PICKED)
+            for (int x = 0; x < 2; ++x) sees_of[x] = __shfl_sync(0xffffffffu, sees, 16 * x);
         if constexpr (SINGLE) {
             if (all) {
 #pragma unroll
-                for (int x = 0; x < 2; ++x) group1(span + x * G::kBytes, j0 + 16 * x, true, std::false_type{});
+                for (int x = 0; x < 2; ++x) group1(span + x * G::kBytes, j0 + 16 * x, true, 16, std::false_type{});
             } else {
 #pragma unroll 1
-                for (int x = 0; x < 2; ++x)
-                    if (j0 + 16 * x < k1)
-                        group1(span + x * G::kBytes, j0 + 16 * x, there >> (16 * x) & 1u, std::true_type{});
+                for (int x = 0; x < 2; ++x) {
+                    const int n_sees = x ? sees_of[1] : sees_of[0];
+                    if (PICKED ? n_sees > 0 : j0 + 16 * x < k1)
+                        group1(span + x * G::kBytes, j0 + 16 * x, there >> (16 * x) & 1u, n_sees, std::true_type{});
+                }
             }
         } else {
             if (all) span_of(span, j0, there, std::false_type{});
@@ -672,7 +712,7 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
             }
             const int rr = rt.row0 + row, i = rt.query(rr);
             const int64_t at = (int64_t)(q0 + i) * a.hq + h * a.group + rr - i * a.group;
-            if (nan_value) {
+            if (!PICKED && nan_value) {
                 for (int j = max(k0, all_see + 1); j < min(k1, rt.last0 + i + 1); ++j) {
                     const int32_t page =
                         cache_page(a.cache.table, a.cache.width, a.cache.num_pages, a.cache.page_shift, b, j);
@@ -682,12 +722,12 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
                     if ((a.cache.scales[1][at_row * (D / 16) + ch / 16] & 0x7Fu) == 0x7Fu) O = __int_as_float(0x7FC00000);
                 }
             }
-            if (WHOLE || a.slots == 0) {
+            if (PICKED ? a.pick_chunks == 1 : WHOLE || a.slots == 0) {
                 // (a row that sees no key is 0; the comparison keeps a NaN sum)
                 a.out[at * D + ch] = __float2bfloat16_rn(L == 0.f ? 0.f : O / L * a.cache.scale[1]);
                 if (a.lse && ch == 0) a.lse[at] = L == 0.f ? INFINITY : M + log2f(L);
             } else {
-                const int64_t part = ((int64_t)blockIdx.x * a.cache.hkv + h) * a.max_rows + rr;
+                const int64_t part = ((int64_t)blockIdx.x * a.cache.hkv + h) * a.max_rows + (PICKED ? rr - i * a.group : rr);
                 a.part_o[part * D + ch] = O;
                 if (ch == 0) a.part_ml[part] = make_float2(M, L);
             }
@@ -1039,7 +1079,116 @@ cudaError_t launch_all(const AttendArgs& a, const AttendPlan& plan, int max_rows
     return e;
 }
 
+// The chunks of a query's list joined, a row (query and head) a warp: chunk x of query r has its sums at
+// ((r * chunks + x) * hkv + key head) * group + head.
+template <int D>
+__global__ void __launch_bounds__(kAttThreads) picked_join_kernel(const __grid_constant__ AttendArgs a, int64_t rows)
+{
+    const int lane = threadIdx.x & 31;
+    const int64_t row = (int64_t)blockIdx.x * kAttWarps + (threadIdx.x >> 5);
+    griddep_wait();
+    griddep_launch_dependents();
+    if (row >= rows) return;
+    const int64_t r = row / a.hq, from = r * a.pick_chunks * a.hq + row % a.hq;
+    float M = kNoRef, L = 0.f, O[D / 32];
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e) O[e] = 0.f;
+    constexpr int U = 4;
+    for (int x0 = 0; x0 < a.pick_chunks; x0 += U) {
+        float2 ml[U];
+        float v[U][D / 32];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t at = from + (int64_t)min(x0 + u, a.pick_chunks - 1) * a.hq;
+            ml[u] = __ldcg(a.part_ml + at);
+            if constexpr (D == 128) {
+                const float4 w = __ldcg(reinterpret_cast<const float4*>(a.part_o + at * D) + lane);
+                v[u][0] = w.x, v[u][1] = w.y, v[u][2] = w.z, v[u][3] = w.w;
+            } else {
+                const float2 w = __ldcg(reinterpret_cast<const float2*>(a.part_o + at * D) + lane);
+                v[u][0] = w.x, v[u][1] = w.y;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (x0 + u >= a.pick_chunks) break;
+            const float top = fmaxf(M, ml[u].x), f = ex2(M - top), f2 = ex2(ml[u].x - top);
+            M = top;
+            L = L * f + ml[u].y * f2;
+#pragma unroll
+            for (int e = 0; e < D / 32; ++e) O[e] = O[e] * f + v[u][e] * f2;
+        }
+    }
+    const float f = a.cache.scale[1] / L;
+#pragma unroll
+    for (int e = 0; e < D / 32; e += 2)
+        *reinterpret_cast<__nv_bfloat162*>(a.out + row * D + lane * (D / 32) + e) =
+            __floats2bfloat162_rn(L == 0.f ? 0.f : O[e] * f, L == 0.f ? 0.f : O[e + 1] * f);
+}
+
+template <int D, bool FP8>
+cudaError_t launch_picked(const AttendArgs& a, const PickedPlan& plan, int64_t queries, cudaStream_t stream, int32_t* launches)
+{
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1] = {pdl_attribute()};
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    cfg.stream = stream;
+    const int subs = (a.group + plan.row_tile - 1) / plan.row_tile;
+    cfg.gridDim = dim3((unsigned)(queries * plan.chunks), (unsigned)(subs * a.cache.hkv), 1);
+    cfg.blockDim = dim3(kAttThreads, 1, 1);
+    cfg.dynamicSmemBytes = kRingBytes<D>;
+    auto kern = a.group == 1 ? attend_split_kernel<D, 0, FP8, false, true>
+                             : (plan.row_tile == 8 ? attend_split_kernel<D, 1, FP8, false, true>
+                                                   : attend_split_kernel<D, 2, FP8, false, true>);
+    cudaError_t e = cudaLaunchKernelEx(&cfg, kern, a);
+    if (e != cudaSuccess) return e;
+    ++*launches;
+    if (plan.chunks > 1) {
+        const int64_t rows = queries * a.hq;
+        cfg.gridDim = dim3((unsigned)((rows + kAttWarps - 1) / kAttWarps), 1, 1);
+        cfg.dynamicSmemBytes = 0;
+        e = cudaLaunchKernelEx(&cfg, picked_join_kernel<D>, a, rows);
+        if (e == cudaSuccess) ++*launches;
+    }
+    return e;
+}
+
 }  // namespace
+
+// The lists are split where the queries alone leave the GPU's places empty: as for whole requests, n chunks take
+// rounds / n of the list and the writing and joining of a chunk's sums.
+PickedPlan plan_attend_picked(int64_t queries, int hkv, int group, int64_t keys, int num_sms)
+{
+    PickedPlan p;
+    p.row_tile = group <= 8 ? 8 : 16;
+    const int64_t subs = (group + p.row_tile - 1) / p.row_tile, items = queries * hkv * subs;
+    const int64_t places = (int64_t)num_sms * (p.row_tile == 16 ? 3 : 4), units = std::max<int64_t>(1, (keys + 127) / 128);
+    int64_t best = 1;
+    if (items > 0 && items < places) {
+        best = std::min(units, places / items);
+    } else if (items < 3 * places) {
+        double cost = 1e30;
+        for (int64_t n = 1; n <= std::min<int64_t>(units, 8); ++n) {
+            const double r = (double)((items * n + places - 1) / places);
+            const double c = r / (double)n + r * (n > 1 ? 1.25 * p.row_tile : 0.0) / (double)std::max<int64_t>(keys, 1);
+            if (c < cost) cost = c, best = n;
+        }
+    }
+    p.chunk = (int32_t)(((keys + best - 1) / best + 31) & ~31ll);
+    p.chunks = (int32_t)std::max<int64_t>(1, (keys + p.chunk - 1) / p.chunk);
+    return p;
+}
+
+cudaError_t launch_attend_picked(const AttendArgs& a, const PickedPlan& plan, int head_dim, bool fp8, int64_t queries,
+                                 cudaStream_t stream, int32_t* launches)
+{
+    *launches = 0;
+    if (queries == 0) return cudaSuccess;
+    if (fp8) return launch_picked<128, true>(a, plan, queries, stream, launches);
+    return head_dim == 128 ? launch_picked<128, false>(a, plan, queries, stream, launches)
+                           : launch_picked<64, false>(a, plan, queries, stream, launches);
+}
 
 // Rows of a request's key head up to which the kernel for few rows is taken. A key costs it less
 // and it splits finer, but it makes a key's values again for every 16 rows; the other makes them once for

@@ -1,0 +1,170 @@
+// The ranges of the keys of a page: for each key head and channel the largest and the
+// smallest value of the page's tokens, outwards as whole numbers of a power of two that
+// the head's channels share.
+//
+// x = e2m1 * e4m3 (exact in f16, NaN counts as 0); m = max |x| over the page's tokens and the head's channels
+// = f * 2^p, f in [1/2, 1). With e = p - 7 the codes ceil(max x / 2^e) and floor(min x / 2^e)
+// lie in [-126, 126]: x has at most six significant bits, so f <= 63/64. A page costs its codes and
+// scales once (page * d * 9/16 bytes a head) and 2 d + 1 bytes written.
+// A warp takes a key head of a page: four lanes a row, 16 bytes of codes each, eight rows
+// at a time, the largest and smallest of 32 channels in half pairs; the eight rows' lanes then
+// halve the channels they hold as they exchange them.
+
+#include <algorithm>
+
+#include "cache.cuh"
+
+namespace lvs {
+
+namespace {
+
+constexpr int kBoundsThreads = 128;
+
+// Scale of a block in both halves; NaN counts as 0.
+__device__ __forceinline__ __half2 block_scale(uint32_t s)
+{
+    s &= 0xFFu;
+    return __low2half2(e4m3x2_value((s & 0x7Fu) == 0x7Fu ? 0u : s));
+}
+
+// Of N half pairs that the lanes d apart (16 down to LAST) hold of the same channels, each keeps the extremes of its own
+// ones: the upper lane the upper half. Returns the first pair that the lane keeps.
+template <int N, int d, int LAST>
+__device__ __forceinline__ int halve(__half2* top, __half2* low, int lane)
+{
+    if constexpr (d < LAST) {
+        return 0;
+    } else {
+        constexpr int n = N / 2;
+        const bool up = lane & d;
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            const __half2 t = __shfl_xor_sync(0xffffffffu, up ? top[i] : top[i + n], d);
+            const __half2 l = __shfl_xor_sync(0xffffffffu, up ? low[i] : low[i + n], d);
+            top[i] = __hmax2(up ? top[i + n] : top[i], t);
+            low[i] = __hmin2(up ? low[i + n] : low[i], l);
+        }
+        return (up ? n : 0) + halve<n, d / 2, LAST>(top, low, lane);
+    }
+}
+
+template <int D>
+__global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(const __grid_constant__ BoundsArgs a)
+{
+    constexpr int LANES = D / 32;     // lanes of a row
+    constexpr int ROWS = 32 / LANES;  // rows of a warp at a time
+    constexpr int PAIRS = 16;         // half pairs of a lane's 32 channels
+    const int lane = threadIdx.x & 31;
+    const int64_t unit = ((int64_t)blockIdx.x * kBoundsThreads + threadIdx.x) >> 5;
+    const int64_t place = unit / a.cache.hkv;
+    const int h = (int)(unit - place * a.cache.hkv);
+    griddep_wait();
+    griddep_launch_dependents();
+    if (place >= a.places) return;
+    // the request: the last whose first place is not behind the unit's
+    int lo = 0, hi = a.batch;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (page_at(__ldg(a.off + mid), mid, a.cache.page_shift) <= place) lo = mid;
+        else hi = mid;
+    }
+    const int q0 = __ldg(a.off + lo), t = __ldg(a.off + lo + 1) - q0;
+    if (t <= 0) return;
+    bool bad;
+    const int len = cache_len(__ldg(a.lens + lo), a.limit, bad);
+    if ((bad || t > len) && lane == 0) atomicOr(a.err, kErrBounds);
+    const int64_t o = (max(len - t, 0) >> a.cache.page_shift) + (place - page_at(q0, lo, a.cache.page_shift));
+    const int64_t first = o << a.cache.page_shift;
+    if (first >= len) return;
+    const int32_t page = cache_page(a.cache.table, a.cache.width, a.cache.num_pages, a.cache.page_shift, lo, first);
+    if (page < 0) {
+        if (lane == 0) atomicOr(a.err, kErrBounds);
+        return;
+    }
+    const int rows = min(1 << a.cache.page_shift, len - (int)first);
+    const int64_t at = cache_row(page, a.cache.hkv, h, a.cache.page_shift, 0);
+    const int c = lane % LANES, g = lane / LANES;
+    const uint4* codes = reinterpret_cast<const uint4*>(a.cache.codes[0] + at * (D / 2)) + c;
+    const uint16_t* scales = reinterpret_cast<const uint16_t*>(a.cache.scales[0] + at * (D / 16)) + c;
+    __half2 top[PAIRS], low[PAIRS];
+    const __half2 inf = bits_h2(0x7C007C00u), ninf = bits_h2(0xFC00FC00u);
+#pragma unroll
+    for (int i = 0; i < PAIRS; ++i) top[i] = ninf, low[i] = inf;
+    constexpr int U = 2;
+    for (int r0 = 0; r0 < rows; r0 += ROWS * U) {
+        uint4 w[U];
+        uint32_t s[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int r = min(r0 + u * ROWS + g, rows - 1);  // (the last row again changes nothing)
+            w[u] = __ldg(codes + r * LANES);
+            s[u] = __ldg(scales + r * LANES);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t words[4] = {w[u].x, w[u].y, w[u].z, w[u].w};
+            const __half2 sc[2] = {block_scale(s[u]), block_scale(s[u] >> 8)};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                __half2 v[4];
+                e2m1x8_value(words[k], v);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const __half2 x = __hmul2(v[i], sc[k / 2]);
+                    top[4 * k + i] = __hmax2(top[4 * k + i], x);
+                    low[4 * k + i] = __hmin2(low[4 * k + i], x);
+                }
+            }
+        }
+    }
+    // lanes of the same channels exchange halves of what they hold, until each has its own 32 / ROWS
+    const int mine = halve<PAIRS, 16, LANES>(top, low, lane);
+    constexpr int KEPT = PAIRS / ROWS;  // pairs of a lane now
+    float m = 0.f;
+    float hi_v[2 * KEPT], lo_v[2 * KEPT];
+#pragma unroll
+    for (int i = 0; i < KEPT; ++i) {
+        const float2 x = __half22float2(top[i]), y = __half22float2(low[i]);
+        hi_v[2 * i] = x.x, hi_v[2 * i + 1] = x.y;
+        lo_v[2 * i] = y.x, lo_v[2 * i + 1] = y.y;
+        m = fmaxf(m, fmaxf(fmaxf(fabsf(x.x), fabsf(x.y)), fmaxf(fabsf(y.x), fabsf(y.y))));
+    }
+    m = warp_max_f32(m);
+    // m = f * 2^p, p = exponent field - 126 (values are normal in fp32); the unit is 2^(p - 7)
+    const int e = m > 0.f ? (int)(__float_as_uint(m) >> 23) - 126 - 7 : 0;
+    const float per = __uint_as_float((uint32_t)(127 - e) << 23);
+    int8_t* to = a.codes + ((int64_t)page * a.cache.hkv + h) * 2 * D + c * 32 + mine * 2;
+    static_assert(KEPT == 1 || KEPT == 2, "two or four channels a lane");
+    uint32_t ch = 0, cl = 0;
+#pragma unroll
+    for (int i = 0; i < 2 * KEPT; ++i) {
+        ch |= ((uint32_t)(int)ceilf(hi_v[i] * per) & 0xFFu) << (8 * i);
+        cl |= ((uint32_t)(int)floorf(lo_v[i] * per) & 0xFFu) << (8 * i);
+    }
+    if constexpr (KEPT == 2) {
+        *reinterpret_cast<uint32_t*>(to) = ch;
+        *reinterpret_cast<uint32_t*>(to + D) = cl;
+    } else {
+        *reinterpret_cast<uint16_t*>(to) = (uint16_t)ch;
+        *reinterpret_cast<uint16_t*>(to + D) = (uint16_t)cl;
+    }
+    if (lane == 0) a.exps[(int64_t)page * a.cache.hkv + h] = (int8_t)e;
+}
+
+}  // namespace
+
+cudaError_t launch_cache_bounds(const BoundsArgs& a, int head_dim, cudaStream_t stream)
+{
+    const int64_t warps = a.places * a.cache.hkv;
+    if (warps <= 0) return cudaSuccess;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((warps * 32 + kBoundsThreads - 1) / kBoundsThreads), 1, 1);
+    cfg.blockDim = dim3(kBoundsThreads, 1, 1);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1] = {pdl_attribute()};
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, head_dim == 128 ? bounds_kernel<128> : bounds_kernel<64>, a);
+}
+
+}  // namespace lvs

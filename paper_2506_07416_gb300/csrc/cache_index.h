@@ -28,6 +28,10 @@ LVS_HD int32_t chunk_end(int32_t seen, int32_t k0, int32_t chunk)
 // tiles of all.
 LVS_HD int64_t tile_at(int64_t rows, int64_t b) { return rows / 128 + b; }
 
+// First place of the pages that request b's new tokens touch, `rows` of the batch's before it, where every request's
+// places follow the last one's: n tokens touch at most floor(n / page) + 2 pages. Of the batch's end: the places of all.
+LVS_HD int64_t page_at(int64_t rows, int64_t b, int32_t page_shift) { return (rows >> page_shift) + 2 * b; }
+
 // Tokens of a request that the kernels may touch: its length cut to
 // [0, limit]. `bad` tells that the length was outside.
 LVS_HD int cache_len(int32_t len, int32_t limit, bool& bad)

@@ -1,0 +1,451 @@
+// The pages that a query attends to, picked by the ranges of their keys.
+//
+// A query's score of a page is the largest product that a key of the page's ranges can have with it: with the query
+// as whole numbers r of a power of two, S(page) = 2^e max over the key head's query heads of sum over channels of
+// r * (r > 0 ? hi : lo). The sums are whole numbers below 2^22, exact in fp32 in any order, so
+// the same inputs pick the same pages whatever kernel adds them up.
+//
+// pick_score_kernel: the product [pages, 2 d] x [2 d, columns] with max(r, 0) against hi and min(r, 0) against lo, a
+// column for each query head of a key head (a query's columns padded to a power of two or whole tiles of eight). A warp
+// keeps 16 pages as the M rows (m16n8k16; codes become f16 in registers, a channel order of the lanes' own) and
+// goes over the columns' tiles in shared memory.
+// pick_select_kernel: the budget-th largest score of a query by halving the bits that its scores differ in, then the
+// pages above it and the lowest of those at it, in order.
+
+#include <algorithm>
+
+#include "cache.cuh"
+
+namespace lvs {
+
+namespace {
+
+constexpr int kScoreThreads = 128;
+constexpr int kScorePages = 16 * kScoreThreads / 32;  // of a CTA at a time
+constexpr int kScoreTiles = 8;                        // tiles of eight columns of a CTA, at most (16 for more heads)
+
+// Columns of a query: its heads padded to 1, 2, 4 or a multiple of 8.
+__host__ __device__ __forceinline__ int padded_group(int group)
+{
+    return group <= 2 ? group : (group <= 4 ? 4 : (group + 7) & ~7);
+}
+// Queries of a CTA.
+__host__ __device__ __forceinline__ int score_queries(int padded)
+{
+    return padded >= 8 * kScoreTiles ? 1 : 8 * kScoreTiles / padded;
+}
+
+__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint2 b)
+{
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+        "{%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b.x), "r"(b.y));
+}
+
+// The four signed bytes of w as f16 (bytes 0, 1 and 2, 3): 1024 + (x + 128) has x's bits as its last ones
+__device__ __forceinline__ void s8x4_value(uint32_t w, uint32_t& a, uint32_t& b)
+{
+    const uint32_t u = w ^ 0x80808080u;
+    const __half2 off = bits_h2(0x64806480u);  // 1152
+    a = h2_bits(__hsub2(bits_h2(__byte_perm(u, 0x64646464u, 0x4140)), off));
+    b = h2_bits(__hsub2(bits_h2(__byte_perm(u, 0x64646464u, 0x4342)), off));
+}
+
+// Order of the scores as whole numbers, above 1 (0: a page that the query does not see, 1: one that the pool has not).
+__device__ __forceinline__ uint32_t score_key(float s)
+{
+    const uint32_t u = __float_as_uint(s);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+// Element x of a row's 16-byte parts as a finite number (NaN: 0, an infinity: the largest).
+template <bool FP8>
+__device__ __forceinline__ void query_values(const uint4& v, float (&x)[FP8 ? 16 : 8])
+{
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    if constexpr (FP8) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            __half2 h[2];
+            e4m3x4_value(w[i], h);
+            const float2 a = __half22float2(h[0]), b = __half22float2(h[1]);
+            x[4 * i] = a.x, x[4 * i + 1] = a.y, x[4 * i + 2] = b.x, x[4 * i + 3] = b.y;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < (FP8 ? 16 : 8); ++i) {
+        if (x[i] != x[i]) x[i] = 0.f;
+        x[i] = fminf(fmaxf(x[i], -0x1.FEp127f), 0x1.FEp127f);
+    }
+}
+
+template <int D, bool FP8>
+__global__ void __launch_bounds__(kScoreThreads) pick_score_kernel(const __grid_constant__ PickArgs a, int blocks)
+{
+    constexpr int STEPS = 2 * D / 16;                       // contractions of 16 channels
+    constexpr int WORDS = D / 16;                           // words of four channels of a lane, of hi and lo each
+    extern __shared__ __align__(16) uint2 frag_s[];         // [tile][step][lane]
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
+    const int h = blockIdx.y % a.hkv, part = blockIdx.y / a.hkv, b = blockIdx.z;
+    griddep_wait();
+    griddep_launch_dependents();
+    const int padded = padded_group(a.group), per = score_queries(padded);
+    const int q0 = __ldg(a.off + b), t = __ldg(a.off + b + 1) - q0;
+    const int i0 = part * per, queries = min(per, t - i0);
+    if (queries <= 0) return;
+    bool bad;
+    const int len = cache_len(__ldg(a.lens + b), a.limit, bad);
+    if (bad && tid == 0) atomicOr(a.err, kErrBounds);
+    // pages that the last of these queries sees; the select kernel reads no scores where all may be picked
+    const int last = len - t + i0 + queries - 1;
+    if (last < 0) return;
+    const int pages = (last >> a.page_shift) + 1;
+    if (pages <= a.budget) return;
+    const int tiles = (queries * padded + 7) / 8;
+
+    // ---- queries into whole numbers, a warp each: the parts that multiply hi and lo in the lanes' order
+    {
+        constexpr int PARTS = D * (FP8 ? 1 : 2) / 16, PER = 32 / PARTS, E = FP8 ? 16 : 8;
+        const int sub = lane % PARTS, row = lane / PARTS;
+        for (int x = warp; x < tiles * 8 / padded; x += kScoreThreads / 32) {  // (zeros behind the last query)
+            const bool real = x < queries;
+            const uint8_t* from = static_cast<const uint8_t*>(a.q) +
+                                  ((int64_t)(q0 + i0 + (real ? x : 0)) * a.q_stride + (int64_t)h * a.group * D) * (FP8 ? 1 : 2);
+            float top = 0.f;
+            for (int y = row; y < a.group; y += PER) {
+                float v[E];
+                query_values<FP8>(__ldg(reinterpret_cast<const uint4*>(from + (int64_t)y * D * (FP8 ? 1 : 2)) + sub), v);
+#pragma unroll
+                for (int e = 0; e < E; ++e) top = fmaxf(top, fabsf(v[e]));
+            }
+            top = warp_max_f32(top);
+            // top = f * 2^p, f in [1/2, 1); the unit is 2^(p - 7)
+            const int p = max((int)(__float_as_uint(top) >> 23) - 126, -119);
+            const float up = __uint_as_float((uint32_t)(127 + 7 - p) << 23);
+            for (int y0 = 0; y0 < padded; y0 += PER) {
+                const int y = y0 + row;
+                if (y >= padded) break;
+                float v[E];
+                query_values<FP8>(
+                    __ldg(reinterpret_cast<const uint4*>(from + (int64_t)min(y, a.group - 1) * D * (FP8 ? 1 : 2)) + sub), v);
+                const int col = x * padded + y, n = col & 7;
+#pragma unroll
+                for (int e = 0; e < E; e += 4) {
+                    float r[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        r[i] = real ? fminf(fmaxf(rintf(v[e + i] * up), -127.f), 127.f) : 0.f;
+                    // channels [ch, ch + 4): word (ch % 16) / 4 of lane (ch / 16) % 4 and load ch / 64 (D = 64: one load)
+                    const int ch = sub * E + e, load = ch / 64, cc = ch / 16 % 4, step = load * 4 + ch % 16 / 4;
+                    uint2* to = frag_s + ((int64_t)(col >> 3) * STEPS + step) * 32 + n * 4 + cc;
+                    const auto pack = [](float s, float u) { return h2_bits(__floats2half2_rn(s, u)); };
+                    to[0] = make_uint2(pack(fmaxf(r[0], 0.f), fmaxf(r[1], 0.f)), pack(fmaxf(r[2], 0.f), fmaxf(r[3], 0.f)));
+                    to[STEPS / 2 * 32] =
+                        make_uint2(pack(fminf(r[0], 0.f), fminf(r[1], 0.f)), pack(fminf(r[2], 0.f), fminf(r[3], 0.f)));
+                }
+            }
+        }
+    }
+    __syncthreads();
+
+    for (int base = blockIdx.x * kScorePages + warp * 16; base < pages; base += blocks * kScorePages) {
+        // ---- 16 pages: lane (g, c) has channels [c * 16, c * 16 + 16) of each 64, of rows g and g + 8
+        uint32_t f[STEPS][4];
+        float unit[2];
+        bool there[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int64_t o = base + g + 8 * e;
+            int32_t page = -1;
+            if (o < pages) {
+                page = cache_page(a.table, a.width, a.num_pages, a.page_shift, b, o << a.page_shift);
+                if (page < 0 && c == 0) atomicOr(a.err, kErrBounds);
+            }
+            there[e] = page >= 0;
+            const int64_t row = (int64_t)max(page, 0) * a.hkv + h;
+            const int x = min(max((int)__ldg(a.exps + row), -100), 100);
+            unit[e] = __uint_as_float((uint32_t)(127 + x) << 23);
+            const uint4* from = reinterpret_cast<const uint4*>(a.codes + row * 2 * D) + c;
+#pragma unroll
+            for (int k = 0; k < 2 * D / 64; ++k) {  // (all loads before the first use)
+                const uint4 w = __ldg(from + k * 4);
+                s8x4_value(w.x, f[4 * k][e], f[4 * k][2 + e]);
+                s8x4_value(w.y, f[4 * k + 1][e], f[4 * k + 1][2 + e]);
+                s8x4_value(w.z, f[4 * k + 2][e], f[4 * k + 2][2 + e]);
+                s8x4_value(w.w, f[4 * k + 3][e], f[4 * k + 3][2 + e]);
+            }
+        }
+        static_assert(WORDS * 2 == STEPS, "a word of four channels is a lane's part of a contraction");
+        float best[2] = {-INFINITY, -INFINITY};  // over the tiles of a query of more than eight heads
+        for (int x = 0; x < tiles; ++x) {
+            float d[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < STEPS; ++k) mma16816(d, f[k], frag_s[((int64_t)x * STEPS + k) * 32 + lane]);
+            // d: page g of columns 2c and 2c + 1, page g + 8 of both
+            auto put = [&](int i, int e, float s) {  // score of the CTA's query i and page g + 8 e
+                const int64_t o = base + g + 8 * e;
+                if (i < queries && o < pages)
+                    a.keys[((int64_t)(q0 + i0 + i) * a.hkv + h) * a.key_stride + o] =
+                        (e ? there[1] : there[0]) ? score_key(s * (e ? unit[1] : unit[0])) : 1u;
+            };
+            if (padded == 1) {
+                const int i = x * 8 + 2 * c;
+                put(i, 0, d[0]), put(i + 1, 0, d[1]);
+                put(i, 1, d[2]), put(i + 1, 1, d[3]);
+                continue;
+            }
+            float s0 = fmaxf(d[0], d[1]), s1 = fmaxf(d[2], d[3]);
+            if (padded >= 4) {
+                s0 = fmaxf(s0, __shfl_xor_sync(0xffffffffu, s0, 1));
+                s1 = fmaxf(s1, __shfl_xor_sync(0xffffffffu, s1, 1));
+            }
+            if (padded >= 8) {
+                s0 = fmaxf(s0, __shfl_xor_sync(0xffffffffu, s0, 2));
+                s1 = fmaxf(s1, __shfl_xor_sync(0xffffffffu, s1, 2));
+                best[0] = fmaxf(best[0], s0), best[1] = fmaxf(best[1], s1);
+                const int tiles_of = padded / 8;
+                if (x % tiles_of != tiles_of - 1) continue;
+                if (c < 2) put(x / tiles_of, c, c ? best[1] : best[0]);
+                best[0] = best[1] = -INFINITY;
+            } else if (padded == 4) {
+                put(x * 2 + (c >> 1), c & 1, c & 1 ? s1 : s0);
+            } else {
+                put(x * 4 + c, 0, s0);
+                put(x * 4 + c, 1, s1);
+            }
+        }
+    }
+}
+
+constexpr int kKeep = 16;  // keys of a thread that stay in registers
+
+// The pages of a query and key head, by WARPS warps (one: four such pairs a CTA).
+template <int WARPS>
+__global__ void __launch_bounds__(WARPS == 1 ? 128 : 32 * WARPS) pick_select_kernel(const __grid_constant__ PickArgs a)
+{
+    constexpr int T = 32 * WARPS;
+    __shared__ int count_s[3][4];
+    __shared__ uint32_t range_s[2][WARPS];
+    __shared__ int before_s[2][WARPS];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tid = WARPS == 1 ? lane : threadIdx.x;
+    griddep_wait();
+    griddep_launch_dependents();
+    const int64_t pair = WARPS == 1 ? (int64_t)blockIdx.x * 4 + warp : (int64_t)blockIdx.x;
+    if (pair >= a.rows * a.hkv) return;
+    const int64_t r = pair / a.hkv;
+    // the request of the query: the last whose first query is not behind it, 32 at a time
+    int b = 0;
+    if (a.rows == a.batch && __ldg(a.off + r) == r && __ldg(a.off + r + 1) == r + 1) {
+        b = (int)r;
+    } else {
+        int lo = 0, hi = a.batch;
+        while (hi - lo > 1) {
+            const int step = (hi - lo + 31) / 32, at = lo + (lane + 1) * step;
+            const uint32_t m = __ballot_sync(0xffffffffu, at < hi && __ldg(a.off + at) <= r);
+            lo += __popc(m) * step;
+            hi = min(hi, lo + step);
+        }
+        b = lo;
+    }
+    const int t1 = __ldg(a.off + b + 1);
+    bool bad;
+    const int len = cache_len(__ldg(a.lens + b), a.limit, bad);
+    if (bad && tid == 0) atomicOr(a.err, kErrBounds);
+    const int64_t pos = min((int64_t)len - t1 + r, (int64_t)len - 1);  // of the query
+    const int pages = pos < 0 ? 0 : (int)(pos >> a.page_shift) + 1;
+    int32_t* out = a.picked + pair * a.budget;
+    if (pages <= a.budget) {
+        for (int x = tid; x < a.budget; x += T) out[x] = x < pages ? x : -1;
+        return;
+    }
+    const uint32_t* keys = a.keys + pair * a.key_stride;
+    auto key_at = [&](int j) -> uint32_t {
+        return j >= pages ? 0u : (j < a.sink || j >= pages - a.recent ? 0xFFFFFFFFu : __ldcg(keys + j));
+    };
+    // pages j = part * chunk + i * 32 + lane of warp `part`
+    const int chunk = WARPS == 1 ? (pages + 31) & ~31 : ((pages + T - 1) / T) * 32;
+    const int first = (WARPS == 1 ? 0 : warp * chunk), steps = chunk / 32;
+    uint32_t k[kKeep];
+    uint32_t top = 0u, low = 0xFFFFFFFFu;
+#pragma unroll
+    for (int i = 0; i < kKeep; ++i) {
+        k[i] = i < steps ? key_at(first + i * 32 + lane) : 0u;
+        if (k[i] != 0u && k[i] != 0xFFFFFFFFu) top = max(top, k[i]), low = min(low, k[i]);
+    }
+    for (int i = kKeep; i < steps; ++i) {
+        const uint32_t v = key_at(first + i * 32 + lane);
+        if (v != 0u && v != 0xFFFFFFFFu) top = max(top, v), low = min(low, v);
+    }
+    top = __reduce_max_sync(0xffffffffu, top);
+    low = __reduce_min_sync(0xffffffffu, low);
+    if constexpr (WARPS > 1) {
+        if (lane == 0) range_s[0][warp] = top, range_s[1][warp] = low;
+        if (tid < 12) count_s[tid / 4][tid & 3] = 0;
+        __syncthreads();
+#pragma unroll 1
+        for (int w = 0; w < WARPS; ++w) top = max(top, range_s[0][w]), low = min(low, range_s[1][w]);
+    }
+    // ---- the largest x that at least `budget` keys reach, two bits a step, from the first bit that they differ in
+    int at_x = 0;  // keys that reach x
+    uint32_t x = low;
+    {
+        const int forced = a.sink + a.recent;
+        int left = 32 - (top > low ? __clz(top ^ low) : 32);  // bits that are open
+        if (forced >= a.budget) x = 0xFFFFFFFFu, left = 0;
+        else x = left < 32 ? low >> left << left : 0u;
+        at_x = forced >= a.budget ? a.budget : pages;
+        int turn = 0;
+        while (left > 0 && at_x != a.budget) {
+            const int bits = left >= 2 ? 2 : 1;
+            left -= bits;
+            const uint32_t x1 = x + (1u << left), x2 = x + (2u << left), x3 = x + (3u << left);
+            int c1 = 0, c2 = 0, c3 = 0;
+#pragma unroll
+            for (int i = 0; i < kKeep; ++i) {
+                if (i >= steps) break;
+                c1 += k[i] >= x1, c2 += k[i] >= x2, c3 += k[i] >= x3;
+            }
+            for (int i = kKeep; i < steps; ++i) {
+                const uint32_t v = key_at(first + i * 32 + lane);
+                c1 += v >= x1, c2 += v >= x2, c3 += v >= x3;
+            }
+            c1 = __reduce_add_sync(0xffffffffu, c1);
+            c2 = __reduce_add_sync(0xffffffffu, c2);
+            c3 = __reduce_add_sync(0xffffffffu, c3);
+            if constexpr (WARPS > 1) {
+                int* to = count_s[turn];
+                if (lane < 3) atomicAdd(to + lane, lane == 0 ? c1 : (lane == 1 ? c2 : c3));
+                const int clear = turn == 2 ? 0 : turn + 1;
+                __syncthreads();
+                c1 = to[0], c2 = to[1], c3 = to[2];
+                if (tid < 3) count_s[clear == 2 ? 0 : clear + 1][tid] = 0;
+                turn = clear;
+            }
+            if (bits == 2 && c3 >= a.budget) x = x3, at_x = c3;
+            else if (bits == 2 && c2 >= a.budget) x = x2, at_x = c2;
+            else if (c1 >= a.budget) x = x1, at_x = c1;
+        }
+    }
+    // ---- keys above x, and the first of those at it (where x was reached by `budget` keys: all that reach it)
+    const bool exact = at_x == a.budget;
+    const uint32_t above = exact ? x - 1u : x;
+    int mine = 0, ties = 0;  // of this warp
+    auto visit = [&](auto f) {
+#pragma unroll
+        for (int i = 0; i < kKeep; ++i) {
+            if (i >= steps) break;
+            f(first + i * 32 + lane, k[i]);
+        }
+        for (int i = kKeep; i < steps; ++i) f(first + i * 32 + lane, key_at(first + i * 32 + lane));
+    };
+    visit([&](int, uint32_t v) {
+        mine += __popc(__ballot_sync(0xffffffffu, v > above));
+        ties += exact ? 0 : __popc(__ballot_sync(0xffffffffu, v == x));
+    });
+    int all = mine, my_at = 0, ties_before = 0;
+    if constexpr (WARPS > 1) {
+        if (lane == 0) before_s[0][warp] = mine, before_s[1][warp] = ties;
+        __syncthreads();
+        all = 0;
+#pragma unroll 1
+        for (int w = 0; w < WARPS; ++w) {
+            if (w < warp) my_at += before_s[0][w], ties_before += before_s[1][w];
+            all += before_s[0][w];
+        }
+    }
+    const int room = a.budget - all;  // of ties
+    my_at += min(ties_before, room);
+    visit([&](int j, uint32_t v) {
+        const uint32_t tie = exact ? 0u : __ballot_sync(0xffffffffu, v == x);
+        const uint32_t below = (1u << lane) - 1u;
+        const bool take = v > above || ((tie >> lane & 1u) && ties_before + __popc(tie & below) < room);
+        const uint32_t m = __ballot_sync(0xffffffffu, take);
+        if (take) out[my_at + __popc(m & below)] = j;
+        my_at += __popc(m);
+        ties_before += __popc(tie);
+    });
+}
+
+template <int D, bool FP8>
+cudaError_t launch_scores(const PickArgs& a, int max_t, int max_pages, int num_sms, cudaLaunchConfig_t cfg)
+{
+    const int padded = padded_group(a.group), per = score_queries(padded);
+    const int parts = (max_t + per - 1) / per;
+    const int tiles = (std::min(per, max_t) * padded + 7) / 8;
+    auto kern = pick_score_kernel<D, FP8>;
+    const size_t smem = (size_t)tiles * (2 * D / 16) * 32 * sizeof(uint2);
+    cudaError_t e = cudaSuccess;
+    if (smem > 48 * 1024) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    // CTAs of a request's pages: as many as fill the GPU, at most one for every 64 pages
+    const int64_t others = (int64_t)parts * a.hkv * a.batch;
+    const int64_t blocks = std::min<int64_t>((max_pages + kScorePages - 1) / kScorePages,
+                                             std::max<int64_t>(1, (8 * (int64_t)num_sms + others - 1) / others));
+    cfg.gridDim = dim3((unsigned)blocks, (unsigned)(parts * a.hkv), (unsigned)a.batch);
+    cfg.blockDim = dim3(kScoreThreads, 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    return cudaLaunchKernelEx(&cfg, kern, a, (int)blocks);
+}
+
+}  // namespace
+
+int64_t pick_key_stride(int64_t max_len, int page_shift, int budget)
+{
+    const int64_t pages = (max_len + (1 << page_shift) - 1) >> page_shift;
+    return pages <= budget ? 0 : (pages + 31) & ~31ll;
+}
+
+int pick_col_tiles(int64_t max_t, int group)
+{
+    const int per = score_queries(padded_group(group));
+    return (int)((max_t + per - 1) / per);
+}
+
+cudaError_t launch_cache_pick(const PickArgs& a, int head_dim, bool fp8, int max_t, int max_len, int num_sms,
+                              cudaStream_t stream, int32_t* launches)
+{
+    *launches = 0;
+    if (a.rows == 0) return cudaSuccess;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1] = {pdl_attribute()};
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    cfg.stream = stream;
+    const int max_pages = (int)(((int64_t)max_len + (1 << a.page_shift) - 1) >> a.page_shift);
+    cudaError_t e = cudaSuccess;
+    if (a.key_stride > 0) {
+        e = fp8 ? launch_scores<128, true>(a, max_t, max_pages, num_sms, cfg)
+                : (head_dim == 128 ? launch_scores<128, false>(a, max_t, max_pages, num_sms, cfg)
+                                   : launch_scores<64, false>(a, max_t, max_pages, num_sms, cfg));
+        if (e != cudaSuccess) return e;
+        ++*launches;
+    }
+    const int64_t pairs = a.rows * a.hkv;
+    cfg.dynamicSmemBytes = 0;
+    if (max_pages <= 32 * kKeep) {
+        cfg.gridDim = dim3((unsigned)((pairs + 3) / 4), 1, 1);
+        cfg.blockDim = dim3(128, 1, 1);
+        e = cudaLaunchKernelEx(&cfg, pick_select_kernel<1>, a);
+    } else {
+        cfg.gridDim = dim3((unsigned)pairs, 1, 1);
+        if (max_pages <= 32 * 8 * kKeep) {
+            cfg.blockDim = dim3(32 * 8, 1, 1);
+            e = cudaLaunchKernelEx(&cfg, pick_select_kernel<8>, a);
+        } else {
+            cfg.blockDim = dim3(32 * 32, 1, 1);
+            e = cudaLaunchKernelEx(&cfg, pick_select_kernel<32>, a);
+        }
+    }
+    if (e == cudaSuccess) ++*launches;
+    return e;
+}
+
+}  // namespace lvs

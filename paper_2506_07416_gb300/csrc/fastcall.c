@@ -18,16 +18,19 @@
 #include <stdint.h>
 
 enum { F_SCORE, F_FULL, F_SCORE_TOPK, F_TOPK, F_COMPACT, F_SPLICE, F_PROJECT, F_KEEP,
-       F_APPEND, F_SPACE, F_ATTEND, F_EVICT, F_VERIFY, F_COUNT };
+       F_APPEND, F_SPACE, F_ATTEND, F_EVICT, F_VERIFY, F_RESERVE, F_BOUNDS, F_PICK_SPACE, F_PICK, F_PICKED_SPACE,
+       F_PICKED, F_COUNT };
 static const char *const kNames[F_COUNT] = {"score", "score_full_keys", "score_topk", "topk",
                                             "compact", "splice", "project", "keep_offsets",
                                             "cache_append", "cache_attend_workspace", "cache_attend", "cache_evict",
-                                            "verify"};
+                                            "verify", "cache_reserve", "cache_bounds", "cache_pick_workspace",
+                                            "cache_pick", "cache_attend_picked_workspace", "cache_attend_picked"};
 /* h handle / stream, i int32, l int64, f float, p pointer, n host int32 array */
 static const char *const kSigs[F_COUNT] = {"hippnppnffph", "hippnppnppnpffph", "hippnppnffppnfppph", "hippnpnfppph",
                                            "", "hippnppnppnppnlpppph", "hliipppfippifph", "",
                                            "hippipplpllppnffpppph", "", "hippipplpnifpppplh", "hippipiiiipippph",
-                                           "hiiippnpppppph"};
+                                           "hiiippnpppppph", "hiipipppippnppph", "hipppippnh", "", "hippipplpniiiipplh", "",
+                                           "hippipplpnpifpplh"};
 static void *g_fn[F_COUNT];
 static PyObject *g_host_i32;      /* the binding's conversion of a host offset array */
 static PyObject *g_ndarray;       /* numpy.ndarray */
@@ -297,6 +300,82 @@ static PyObject *f_verify(PyObject *self, PyObject *const *args, Py_ssize_t n)
     END
 }
 
+static PyObject *f_reserve(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    BEGIN(F_RESERVE)
+    rc = ((int (*)(P, I, I, P, I, P, P, P, I, P, P, P, P, P, P, P))g_fn[F_RESERVE])(
+        a[0].p, a[1].i, a[2].i, a[3].p, a[4].i, a[5].p, a[6].p, a[7].p, a[8].i, a[9].p, a[10].p, a[11].p, a[12].p,
+        a[13].p, a[14].p, a[15].p);
+    END
+}
+
+static PyObject *f_bounds(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    BEGIN(F_BOUNDS)
+    rc = ((int (*)(P, I, P, P, P, I, P, P, P, P))g_fn[F_BOUNDS])(
+        a[0].p, a[1].i, a[2].p, a[3].p, a[4].p, a[5].i, a[6].p, a[7].p, a[8].p, a[9].p);
+    END
+}
+
+static PyObject *f_pick(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    BEGIN(F_PICK)
+    rc = ((int (*)(P, I, P, P, I, P, P, int64_t, P, P, I, I, I, I, P, P, int64_t, P))g_fn[F_PICK])(
+        a[0].p, a[1].i, a[2].p, a[3].p, a[4].i, a[5].p, a[6].p, a[7].l, a[8].p, a[9].p, a[10].i, a[11].i, a[12].i,
+        a[13].i, a[14].p, a[15].p, a[16].l, a[17].p);
+    END
+}
+
+static PyObject *f_picked(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    BEGIN(F_PICKED)
+    rc = ((int (*)(P, I, P, P, I, P, P, int64_t, P, P, P, I, float, P, P, int64_t, P))g_fn[F_PICKED])(
+        a[0].p, a[1].i, a[2].p, a[3].p, a[4].i, a[5].p, a[6].p, a[7].l, a[8].p, a[9].p, a[10].p, a[11].i, a[12].f,
+        a[13].p, a[14].p, a[15].l, a[16].p);
+    END
+}
+
+/* bytes of a workspace from a handle, a batch, its offsets and two or three sizes, or -status */
+static PyObject *bytes_of(int which, int sizes, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 3 + sizes) {
+        PyErr_SetString(PyExc_TypeError, "wrong number of arguments");
+        return NULL;
+    }
+    Held h;
+    h.nbuf = h.nobj = 0;
+    const int32_t *off;
+    uint64_t hd, batch, x[3] = {0, 0, 0};
+    int bad = as_bits(args[0], 'h', &hd) || as_bits(args[1], 'i', &batch) || as_host_i32(args[2], &h, &off, NULL);
+    for (int k = 0; k < sizes && !bad; ++k) bad = as_bits(args[3 + k], 'i', &x[k]);
+    if (bad) {
+        release(&h);
+        return NULL;
+    }
+    int64_t bytes = 0;
+    const I b = (I)(uint32_t)batch, x0 = (I)(uint32_t)x[0], x1 = (I)(uint32_t)x[1], x2 = (I)(uint32_t)x[2];
+    const P handle = (P)(uintptr_t)hd;
+    int rc;
+    if (sizes == 3) rc = ((int (*)(P, I, const int32_t *, I, I, I, int64_t *))g_fn[which])(handle, b, off, x0, x1, x2, &bytes);
+    else rc = ((int (*)(P, I, const int32_t *, I, I, int64_t *))g_fn[which])(handle, b, off, x0, x1, &bytes);
+    release(&h);
+    return PyLong_FromLongLong(rc ? -(long long)rc : (long long)bytes);
+}
+
+/* pick_bytes(handle, batch, q_offsets_h, max_len, page_size, budget) */
+static PyObject *f_pick_bytes(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    (void)self;
+    return bytes_of(F_PICK_SPACE, 3, args, n);
+}
+
+/* picked_bytes(handle, batch, q_offsets_h, page_size, budget) */
+static PyObject *f_picked_bytes(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    (void)self;
+    return bytes_of(F_PICKED_SPACE, 2, args, n);
+}
+
 /* attend_bytes(handle, batch, q_offsets_h, max_len, weights): bytes of an attention call's workspace, or -status */
 static PyObject *f_attend_bytes(PyObject *self, PyObject *const *args, Py_ssize_t n)
 {
@@ -516,6 +595,9 @@ static PyMethodDef kMethods[] = {DEF("bind", f_bind), DEF("score", f_score), DEF
                                  DEF("keep_total", f_keep_total), DEF("cache_append", f_append),
                                  DEF("cache_attend", f_attend), DEF("attend_bytes", f_attend_bytes),
                                  DEF("cache_evict", f_evict), DEF("verify", f_verify),
+                                 DEF("cache_reserve", f_reserve), DEF("cache_bounds", f_bounds),
+                                 DEF("pick_bytes", f_pick_bytes), DEF("cache_pick", f_pick),
+                                 DEF("picked_bytes", f_picked_bytes), DEF("cache_attend_picked", f_picked),
                                  DEF("fits", f_fits), DEF("row_stride", f_row_stride), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_fastcall", NULL, -1, kMethods, NULL, NULL, NULL, NULL};
 

@@ -180,6 +180,10 @@ struct AttendArgs {
     const float* weights_in;  // [num_pages][page_size]
     float* weights_out;       // null: no weights
     int32_t stall;            // debug: the second tile's values are never made
+    const int32_t* picked;    // [rows][hkv][budget] pages of each query's request, or null: all keys
+    int32_t budget;
+    int32_t pick_chunk;       // keys of the picked pages that a CTA takes, and how many such chunks a query has
+    int32_t pick_chunks;
     int32_t* err;
     long long wait_budget;
 };
@@ -195,6 +199,14 @@ AttendPlan plan_cache_attend(int batch, int hkv, int group, const int32_t* q_off
 cudaError_t launch_cache_attend(const AttendArgs& a, const AttendPlan& plan, int head_dim, bool fp8, int max_rows,
                                 int64_t total_rows, int max_len, cudaStream_t stream, int32_t* launches);
 
+struct PickedPlan {
+    int32_t row_tile;         // rows (heads of a key head) of a CTA: 8 or 16
+    int32_t chunk, chunks;
+};
+PickedPlan plan_attend_picked(int64_t queries, int hkv, int group, int64_t keys, int num_sms);
+cudaError_t launch_attend_picked(const AttendArgs& a, const PickedPlan& plan, int head_dim, bool fp8, int64_t queries,
+                                 cudaStream_t stream, int32_t* launches);
+
 // cache_evict.cu
 struct EvictArgs {
     CachePages cache;
@@ -208,6 +220,62 @@ struct EvictArgs {
     int32_t* err;
 };
 cudaError_t launch_cache_evict(const EvictArgs& a, int head_dim, int num_sms, cudaStream_t stream, int32_t* launches);
+
+// cache_reserve.cu
+struct ReserveArgs {
+    int32_t* table;           // [batch][width]
+    int32_t width, page_shift, num_pages;
+    const int32_t* held;      // [batch] tokens that the pages hold, and are to hold
+    const int32_t* want;
+    int32_t* free;            // [num_pages] ring of free pages
+    const int32_t* state;     // its head and count, before and after
+    int32_t* new_state;
+    const int32_t* off;       // [batch+1] prefix of the new tokens
+    int64_t rows;
+    int32_t batch, limit;     // limit: tokens a table row holds
+    int32_t* granted;         // [batch]
+    int64_t* slots;           // [rows]
+    bool vec;                 // slots are 16-byte aligned
+    int32_t* err;
+};
+cudaError_t launch_cache_reserve(const ReserveArgs& a, int num_sms, cudaStream_t stream);
+
+// cache_bounds.cu
+struct BoundsArgs {
+    CachePages cache;         // (K alone)
+    int8_t* codes;            // [num_pages][hkv][2][d]
+    int8_t* exps;             // [num_pages][hkv]
+    const int32_t* lens;
+    const int32_t* off;       // [batch+1] prefix of the new tokens
+    int64_t places;           // page_at of the batch's end
+    int32_t batch, limit;
+    int32_t* err;
+};
+cudaError_t launch_cache_bounds(const BoundsArgs& a, int head_dim, cudaStream_t stream);
+
+// cache_pick.cu
+struct PickArgs {
+    const int8_t* codes;
+    const int8_t* exps;
+    int32_t num_pages, page_shift, hkv;
+    const int32_t* table;
+    int32_t width;
+    const int32_t* lens;
+    const void* q;            // [rows][hq][d] bf16 or e4m3 codes
+    int64_t q_stride;
+    const int32_t* off;       // [batch+1] prefix of the queries
+    int64_t rows;
+    int32_t batch, hq, group, limit;
+    int32_t budget, sink, recent;
+    uint32_t* keys;           // [rows][hkv][key_stride] scores in an order of whole numbers
+    int64_t key_stride;
+    int32_t* picked;          // [rows][hkv][budget]
+    int32_t* err;
+};
+int64_t pick_key_stride(int64_t max_len, int page_shift, int budget);  // 0: no request has more pages than the budget
+int pick_col_tiles(int64_t max_t, int group);                          // CTAs of a request's queries
+cudaError_t launch_cache_pick(const PickArgs& a, int head_dim, bool fp8, int max_t, int max_len, int num_sms,
+                              cudaStream_t stream, int32_t* launches);
 
 // verify.cu
 struct VerifyArgs {

@@ -35,6 +35,12 @@ class Cache(ctypes.Structure):
                 ("k_scale", ctypes.c_float), ("v_scale", ctypes.c_float)]
 
 
+class Bounds(ctypes.Structure):
+    """litevlm_key_bounds_t"""
+    _fields_ = [("codes", ctypes.c_void_p), ("exps", ctypes.c_void_p), ("num_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32)]
+
+
 class LitevlmError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"{STATUS.get(status, status)}: {message}")
@@ -83,12 +89,19 @@ def _load():
     lib.litevlm_select_cache_attend.argtypes = [P, i32, P, P, i32, P, P, i64, P, P, i32, f32, P, P, P, P, i64, P]
     lib.litevlm_select_cache_evict.argtypes = [P, i32, P, P, i32, P, i32, i32, i32, i32, P, i32, P, P, P, P]
     lib.litevlm_select_verify.argtypes = [P, i32, i32, i32, P, P, P, P, P, P, P, P, P, P]
+    lib.litevlm_select_cache_reserve.argtypes = [P, i32, i32, P, i32, P, P, P, i32, P, P, P, P, P, P, P]
+    lib.litevlm_select_cache_bounds.argtypes = [P, i32, P, P, P, i32, P, P, P, P]
+    lib.litevlm_select_cache_pick_workspace.argtypes = [P, i32, P, i32, i32, i32, ctypes.POINTER(i64)]
+    lib.litevlm_select_cache_pick.argtypes = [P, i32, P, P, i32, P, P, i64, P, P, i32, i32, i32, i32, P, P, i64, P]
+    lib.litevlm_select_cache_attend_picked_workspace.argtypes = [P, i32, P, i32, i32, ctypes.POINTER(i64)]
+    lib.litevlm_select_cache_attend_picked.argtypes = [P, i32, P, P, i32, P, P, i64, P, P, P, i32, f32, P, P, i64, P]
     lib.litevlm_select_set_wait_budget.argtypes = [P, i64]
     lib.litevlm_select_set_debug_flags.argtypes = [P, i32]
     for fn in ("create", "destroy", "score", "score_full_keys", "topk", "compact", "check_device", "score_plan",
                "score_noalloc", "splice", "views", "fold_norm", "rope_table", "project", "score_topk", "host_view",
                "keep_offsets", "cache_append", "cache_attend_workspace", "cache_attend", "cache_evict", "verify",
-               "set_wait_budget", "set_debug_flags"):
+               "cache_reserve", "cache_bounds", "cache_pick_workspace", "cache_pick", "cache_attend_picked_workspace",
+               "cache_attend_picked", "set_wait_budget", "set_debug_flags"):
         getattr(lib, "litevlm_select_" + fn).restype = ctypes.c_int
     return lib
 
@@ -104,7 +117,9 @@ EXPORTS = ["litevlm_select_create", "litevlm_select_destroy", "litevlm_select_la
            "litevlm_select_last_launches", "litevlm_select_score_topk", "litevlm_select_host_view",
            "litevlm_select_keep_offsets", "litevlm_select_cache_append", "litevlm_select_cache_attend_workspace",
            "litevlm_select_cache_attend", "litevlm_select_cache_evict", "litevlm_select_verify",
-           "litevlm_select_set_wait_budget", "litevlm_select_set_debug_flags"]
+           "litevlm_select_cache_reserve", "litevlm_select_cache_bounds", "litevlm_select_cache_pick_workspace",
+           "litevlm_select_cache_pick", "litevlm_select_cache_attend_picked_workspace",
+           "litevlm_select_cache_attend_picked", "litevlm_select_set_wait_budget", "litevlm_select_set_debug_flags"]
 FLAGS = {"auto": 0, "reread": 1, "resident": 2, "resident_1buf": 8, "resident_2buf": 16, "resident_flat": 64}
 # LITEVLM_FLAG_SCORE_SPLIT_QUERIES: resident plans for T > 64 run each head's text rows as two pseudo-heads
 QUERY_SPLIT = {"whole": 0, "split": 128}
@@ -175,7 +190,8 @@ def _load_fastcall():
     _fastcall.bind({n: ctypes.cast(getattr(LIB, "litevlm_select_" + n), ctypes.c_void_p).value
                     for n in ("score", "score_full_keys", "score_topk", "topk", "compact", "splice", "project",
                               "keep_offsets", "cache_append", "cache_attend_workspace", "cache_attend", "cache_evict",
-                              "verify")}, _host_i32, np.ndarray, _ctypes_value)
+                              "verify", "cache_reserve", "cache_bounds", "cache_pick_workspace", "cache_pick",
+                              "cache_attend_picked_workspace", "cache_attend_picked")}, _host_i32, np.ndarray, _ctypes_value)
     return _fastcall
 
 
@@ -333,6 +349,58 @@ def cache_evict(handle: int, batch: int, cache, table, table_width: int, seq_len
         _check(rc, handle)
 
 
+def cache_reserve(handle: int, batch: int, page_size: int, table, table_width: int, held, want, free_pages, num_pages: int,
+                  state, new_offsets_d, new_offsets_h, granted, new_state, slots, stream=None) -> None:
+    rc = _FC.cache_reserve(handle, batch, page_size, table, table_width, held, want, free_pages, num_pages, state,
+                           new_offsets_d, new_offsets_h, granted, new_state, slots, _stream_ptr(stream))
+    if rc:
+        _check(rc, handle)
+
+
+def cache_bounds(handle: int, batch: int, cache, bounds, table, table_width: int, seq_lens, new_offsets_d, new_offsets_h,
+                 stream=None) -> None:
+    """litevlm_select_cache_bounds; bounds: the address of a litevlm_key_bounds_t (KeyBounds.struct)."""
+    rc = _FC.cache_bounds(handle, batch, cache, bounds, table, table_width, seq_lens, new_offsets_d, new_offsets_h,
+                          _stream_ptr(stream))
+    if rc:
+        _check(rc, handle)
+
+
+def cache_pick_workspace(handle: int, batch: int, q_offsets_h, max_len: int, page_size: int, budget: int) -> int:
+    """litevlm_select_cache_pick_workspace: bytes of the workspace of a selection of pages."""
+    n = _FC.pick_bytes(handle, batch, q_offsets_h, max_len, page_size, budget)
+    if n < 0:
+        _check(-n, handle)
+    return n
+
+
+def cache_pick(handle: int, batch: int, bounds, table, table_width: int, seq_lens, q, q_row_stride: int, q_offsets_d,
+               q_offsets_h, max_len: int, budget: int, sink: int, recent: int, picked, workspace, workspace_bytes: int,
+               stream=None) -> None:
+    rc = _FC.cache_pick(handle, batch, bounds, table, table_width, seq_lens, q, q_row_stride, q_offsets_d, q_offsets_h,
+                        max_len, budget, sink, recent, picked, workspace, workspace_bytes, _stream_ptr(stream))
+    if rc:
+        _check(rc, handle)
+
+
+def cache_attend_picked_workspace(handle: int, batch: int, q_offsets_h, page_size: int, budget: int) -> int:
+    """litevlm_select_cache_attend_picked_workspace: bytes of the workspace of attention over picked pages."""
+    n = _FC.picked_bytes(handle, batch, q_offsets_h, page_size, budget)
+    if n < 0:
+        _check(-n, handle)
+    return n
+
+
+def cache_attend_picked(handle: int, batch: int, cache, table, table_width: int, seq_lens, q, q_row_stride: int,
+                        q_offsets_d, q_offsets_h, picked, budget: int, q_scale: float, out, workspace,
+                        workspace_bytes: int, stream=None) -> None:
+    rc = _FC.cache_attend_picked(handle, batch, cache, table, table_width, seq_lens, q, q_row_stride, q_offsets_d,
+                                 q_offsets_h, picked, budget, q_scale, out, workspace, workspace_bytes,
+                                 _stream_ptr(stream))
+    if rc:
+        _check(rc, handle)
+
+
 def verify(handle: int, batch: int, vocab: int, prob_bf16: int, draft_tokens, draft_offsets_d, draft_offsets_h,
            target_probs, draft_probs, u_accept, u_sample, accepted, tokens, stream=None) -> None:
     rc = _FC.verify(handle, batch, vocab, prob_bf16, draft_tokens, draft_offsets_d, draft_offsets_h, target_probs,
@@ -465,6 +533,28 @@ class KVCache:
         self.k_scale, self.v_scale, self.weights = float(k_scale), float(v_scale), weights
         self._c = Cache(k_codes.data_ptr(), k_scales.data_ptr(), v_codes.data_ptr(), v_scales.data_ptr(),
                         self.num_pages, self.page_size, self.k_scale, self.v_scale)
+        self.struct = ctypes.addressof(self._c)
+
+
+class KeyBounds:
+    """The ranges of a pool's keys (litevlm_key_bounds_t), int8 CUDA tensors: codes [pages, Hkv, 2, d] (largest, smallest),
+    exps [pages, Hkv]. ``Selector.key_bounds`` makes one for a cache. Like a KVCache's its tensors are fixed."""
+
+    def __setattr__(self, name, value):
+        if "struct" in self.__dict__:
+            _refuse(f"{name} of a KeyBounds is fixed: make another one")
+        object.__setattr__(self, name, value)
+
+    def __init__(self, codes, exps, page_size: int):
+        import torch
+        if not isinstance(codes, torch.Tensor) or codes.dim() != 4 or codes.device.type != "cuda":
+            _refuse("codes must be a CUDA tensor [pages, Hkv, 2, d]")
+        self.num_pages, self.heads, _, self.head_dim = codes.shape
+        self.device, self.page_size = codes.device.index, int(page_size)
+        _want("codes", codes, torch.int8, (self.num_pages, self.heads, 2, self.head_dim), self.device)
+        _want("exps", exps, torch.int8, (self.num_pages, self.heads), self.device)
+        self.codes, self.exps = codes, exps
+        self._c = Bounds(codes.data_ptr(), exps.data_ptr(), self.num_pages, self.page_size)
         self.struct = ctypes.addressof(self._c)
 
 
@@ -683,10 +773,10 @@ class Selector:
 
     # ---- the 4-bit K/V cache
 
-    def _cache_call(self, cache, table, seq_lens, batch: int):
+    def _cache_call(self, cache, table, seq_lens, batch: int, kind=KVCache):
         import torch
-        if not isinstance(cache, KVCache):
-            _refuse("cache must be a KVCache")
+        if not isinstance(cache, kind):
+            _refuse(f"{'cache' if kind is KVCache else 'bounds'} must be a {kind.__name__}")
         if cache.device != self.device:
             _refuse(f"the cache is on cuda:{cache.device}, the handle on cuda:{self.device}")
         if cache.heads != self.kv_heads or cache.head_dim != self.head_dim:
@@ -812,6 +902,116 @@ class Selector:
                     to_table, 0 if to_table is None else to_table.shape[1], cache.weights, kept_idx, new_lens,
                     _stream_on(stream, dev))
         return kept_idx, new_lens
+
+    # ---- its pages: who has them, and attention over some of them
+
+    def cache_reserve(self, table, held, want, free, state, page_size: int, offsets, offsets_h=None, granted=None,
+                      new_state=None, slots=None, stream=None):
+        """Gives pages to requests that hold ``held`` tokens and are to hold ``want``, or takes them back: from and to the
+        ring ``free`` (int32, as long as the pool), whose head and count are ``state``; ``table`` and ``free`` are updated in
+        place. ``offsets``: the prefix of the new tokens among each request's want. Returns (granted: want, or held where the
+        ring had too few pages; the ring's new state; slots int64 of the new tokens, -1 for those that were not granted)."""
+        import torch
+        off_h = _host_i32(offsets if offsets_h is None else offsets_h)
+        batch, total, dev = len(off_h) - 1, int(off_h[-1]), self.device
+        _want("table", table, torch.int32, (batch, -1), dev)
+        _want("held", held, torch.int32, (batch,), dev)
+        _want("want", want, torch.int32, (batch,), dev)
+        _want("free", free, torch.int32, (-1,), dev)
+        _want("state", state, torch.int32, (2,), dev)
+        _want("offsets", offsets, torch.int32, (batch + 1,), dev)
+        with _allocate_on(stream, dev):
+            if granted is None:
+                granted = torch.empty_like(held)
+            else:
+                _want("granted", granted, torch.int32, (batch,), dev)
+            if new_state is None:
+                new_state = torch.empty_like(state)
+            else:
+                _want("new_state", new_state, torch.int32, (2,), dev)
+            if slots is None:
+                slots = torch.empty(total, dtype=torch.int64, device=held.device)
+            else:
+                _want("slots", slots, torch.int64, (total,), dev)
+        cache_reserve(self.handle, batch, page_size, table, table.shape[1], held, want, free, free.shape[0], state, offsets,
+                      off_h, granted, new_state, slots, _stream_on(stream, dev))
+        return granted, new_state, slots
+
+    def key_bounds(self, cache: KVCache) -> KeyBounds:
+        """Empty ranges for a cache's pages (``cache_bounds`` fills them)."""
+        import torch
+        device = cache.k_codes.device
+        return KeyBounds(torch.zeros((cache.num_pages, cache.heads, 2, cache.head_dim), dtype=torch.int8, device=device),
+                         torch.zeros((cache.num_pages, cache.heads), dtype=torch.int8, device=device), cache.page_size)
+
+    def cache_bounds(self, cache: KVCache, bounds: KeyBounds, table, seq_lens, offsets, offsets_h=None, stream=None):
+        """Renews the ranges of the pages that hold each request's last tokens (``offsets``: the prefix of their numbers;
+        ``seq_lens`` with them), from all tokens of these pages."""
+        import torch
+        off_h = _host_i32(offsets if offsets_h is None else offsets_h)
+        batch = len(off_h) - 1
+        dev = self._cache_call(cache, table, seq_lens, batch)
+        self._cache_call(bounds, table, seq_lens, batch, KeyBounds)
+        _want("offsets", offsets, torch.int32, (batch + 1,), dev)
+        cache_bounds(self.handle, batch, cache.struct, bounds.struct, table, table.shape[1], seq_lens, offsets, off_h,
+                     _stream_on(stream, dev))
+        return bounds
+
+    def cache_pick(self, bounds: KeyBounds, table, seq_lens, q, offsets, max_len: int, budget: int, sink: int = 0,
+                   recent: int = 0, offsets_h=None, picked=None, workspace=None, stream=None):
+        """The ``budget`` pages that each query [sum T, Hq, d] attends to, for each key head: the first ``sink``, the last
+        ``recent`` up to its own position, and those whose ranges have the largest product with it. Returns int32
+        [sum T, Hkv, budget]: pages of the request, ascending, -1 behind the last. ``workspace``: a uint8 tensor of at least
+        ``cache_pick_workspace`` bytes that no other call in flight uses."""
+        import torch
+        off_h = _host_i32(offsets if offsets_h is None else offsets_h)
+        batch, total = len(off_h) - 1, int(off_h[-1])
+        dev = self._cache_call(bounds, table, seq_lens, batch, KeyBounds)
+        _want("offsets", offsets, torch.int32, (batch + 1,), dev)
+        stride = _row_stride("q", q, self._element(), self.heads, self.head_dim, dev)
+        if q.shape[0] != total:
+            _refuse(f"q has {q.shape[0]} rows, the offsets {total}")
+        need = cache_pick_workspace(self.handle, batch, off_h, max_len, bounds.page_size, budget)
+        with _allocate_on(stream, dev):
+            if picked is None:
+                picked = torch.empty((total, self.kv_heads, budget), dtype=torch.int32, device=q.device)
+            else:
+                _want("picked", picked, torch.int32, (total, self.kv_heads, budget), dev)
+            if workspace is None:
+                workspace = self._workspace(need, stream, q.device)
+            else:
+                _want("workspace", workspace, torch.uint8, (-1,), dev)
+        cache_pick(self.handle, batch, bounds.struct, table, table.shape[1], seq_lens, q, stride, offsets, off_h, max_len,
+                   budget, sink, recent, picked, workspace, workspace.shape[0], _stream_on(stream, dev))
+        return picked
+
+    def cache_attend_picked(self, cache: KVCache, table, seq_lens, q, offsets, picked, q_scale: float = 1.0,
+                            offsets_h=None, out=None, workspace=None, stream=None):
+        """``cache_attend`` over the pages that ``picked`` (int32 [sum T, Hkv, budget]) names for each query and key head;
+        entries that are no page that the query sees are skipped. Returns the bf16 outputs [sum T, Hq, d]."""
+        import torch
+        off_h = _host_i32(offsets if offsets_h is None else offsets_h)
+        batch, total = len(off_h) - 1, int(off_h[-1])
+        dev = self._cache_call(cache, table, seq_lens, batch)
+        _want("offsets", offsets, torch.int32, (batch + 1,), dev)
+        stride = _row_stride("q", q, self._element(), self.heads, self.head_dim, dev)
+        if q.shape[0] != total:
+            _refuse(f"q has {q.shape[0]} rows, the offsets {total}")
+        _want("picked", picked, torch.int32, (total, self.kv_heads, -1), dev)
+        budget = picked.shape[2]
+        need = cache_attend_picked_workspace(self.handle, batch, off_h, cache.page_size, budget)
+        with _allocate_on(stream, dev):
+            if out is None:
+                out = torch.empty((total, self.heads, self.head_dim), dtype=torch.bfloat16, device=q.device)
+            else:
+                _want("out", out, torch.bfloat16, (total, self.heads, self.head_dim), dev)
+            if workspace is None:
+                workspace = self._workspace(need, stream, q.device)
+            else:
+                _want("workspace", workspace, torch.uint8, (-1,), dev)
+        cache_attend_picked(self.handle, batch, cache.struct, table, table.shape[1], seq_lens, q, stride, offsets, off_h,
+                            picked, budget, q_scale, out, workspace, workspace.shape[0], _stream_on(stream, dev))
+        return out
 
     def verify(self, draft_tokens, target_probs, u_accept, u_sample, offsets, draft_probs=None, offsets_h=None,
                accepted=None, tokens=None, stream=None):
