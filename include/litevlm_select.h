@@ -799,7 +799,7 @@ litevlm_status_t litevlm_select_cache_pick(litevlm_select_t handle, int32_t batc
  */
 litevlm_status_t litevlm_select_cache_attend_picked_workspace(litevlm_select_t handle, int32_t batch,
                                                               const int32_t* q_offsets_h, int32_t page_size,
-                                                              int32_t budget, int64_t* bytes);
+                                                              int32_t table_width, int32_t budget, int64_t* bytes);
 litevlm_status_t litevlm_select_cache_attend_picked(litevlm_select_t handle, int32_t batch, const litevlm_cache_t* cache,
                                                     const int32_t* table, int32_t table_width, const int32_t* seq_lens,
                                                     const void* q, int64_t q_row_stride, const int32_t* q_offsets_d,

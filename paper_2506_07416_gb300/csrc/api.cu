@@ -1443,28 +1443,37 @@ litevlm_status_t pick_plan(litevlm_select_t h, int32_t batch, const int32_t* q_o
 
 // The same of attention over picked pages.
 struct PickedSpace {
-    int64_t part_o, part_ml, total;
+    int64_t part_o, part_ml, lists, list_len, list_bits, total;
 };
 litevlm_status_t picked_plan(litevlm_select_t h, int32_t batch, const int32_t* q_offsets_h, int32_t page_size,
-                             int32_t budget, int64_t* total, lvs::PickedPlan* plan, PickedSpace* space)
+                             int32_t table_width, int32_t budget, int64_t* total, lvs::PickedPlan* plan,
+                             PickedSpace* space)
 {
     const litevlm_select_config_t& c = h->cfg;
     litevlm_status_t s = check_offsets(h, q_offsets_h, batch, INT32_MAX, "q_offsets", total);
     if (s != LITEVLM_OK) return s;
     int32_t shift = 0, limit = 0;
-    s = page_table(h, page_size, 1, 1, &shift, &limit);
+    s = page_table(h, page_size, 1, table_width, &shift, &limit);
     if (s != LITEVLM_OK) return s;
     if (budget < 1 || (int64_t)budget * page_size > lvs::kMostKeys)
         return fail(h, LITEVLM_ERR_INVALID_ARG, "budget must be >= 1 and its pages hold at most 2^30 tokens");
-    *plan = lvs::plan_attend_picked(*total, c.num_kv_heads, c.num_q_heads / c.num_kv_heads, (int64_t)budget << shift,
-                                    h->num_sms);
-    const int64_t subs = (c.num_q_heads / c.num_kv_heads + plan->row_tile - 1) / plan->row_tile;
-    if (*total * plan->chunks > INT32_MAX || subs * c.num_kv_heads > 65535)
+    const int group = c.num_q_heads / c.num_kv_heads;
+    const int64_t hkv = c.num_kv_heads;
+    lvs::PickedPlan& p = *plan;
+    p = lvs::plan_attend_picked(batch, c.num_kv_heads, group, q_offsets_h, shift, table_width, budget, h->num_sms);
+    const int64_t subs = ((int64_t)p.queries * group + p.row_tile - 1) / p.row_tile;
+    if (p.tiles * p.chunks > INT32_MAX || p.tiles * hkv > INT32_MAX || subs * hkv > 65535 ||
+        max_count(q_offsets_h, batch) * (int64_t)group > INT32_MAX / 2)
         return fail(h, LITEVLM_ERR_UNSUPPORTED, "the queries or the heads exceed the grid");
-    const int64_t parts = plan->chunks > 1 ? *total * plan->chunks * c.num_q_heads : 0;
+    if ((double)p.tiles * (double)hkv * ((double)p.list_cap * 16.0 + (double)p.queries * p.list_words * 4.0) > 0x1p60)
+        return fail(h, LITEVLM_ERR_UNSUPPORTED, "the workspace would pass 2^60 bytes");
+    const int64_t parts = p.chunks > 1 ? p.tiles * p.chunks * hkv * p.queries * group : 0, lists = p.lists ? p.tiles * hkv : 0;
     space->part_o = 0;
     space->part_ml = round256(parts * c.head_dim * 4);
-    space->total = space->part_ml + round256(parts * 8);
+    space->lists = space->part_ml + round256(parts * 8);
+    space->list_len = space->lists + round256(lists * p.list_cap * 16);
+    space->list_bits = space->list_len + round256(lists * 4);
+    space->total = space->list_bits + (p.row_tile >= 128 ? round256(lists * p.queries * p.list_words * 4) : 0);
     return LITEVLM_OK;
 }
 
@@ -1658,7 +1667,7 @@ litevlm_status_t litevlm_select_cache_pick(litevlm_select_t h, int32_t batch, co
 
 litevlm_status_t litevlm_select_cache_attend_picked_workspace(litevlm_select_t h, int32_t batch,
                                                               const int32_t* q_offsets_h, int32_t page_size,
-                                                              int32_t budget, int64_t* bytes)
+                                                              int32_t table_width, int32_t budget, int64_t* bytes)
 {
     const CallRange range_(__func__);
     if (!h) return LITEVLM_ERR_INVALID_ARG;
@@ -1668,7 +1677,7 @@ litevlm_status_t litevlm_select_cache_attend_picked_workspace(litevlm_select_t h
     int64_t total = 0;
     lvs::PickedPlan plan;
     PickedSpace space;
-    s = picked_plan(h, batch, q_offsets_h, page_size, budget, &total, &plan, &space);
+    s = picked_plan(h, batch, q_offsets_h, page_size, table_width, budget, &total, &plan, &space);
     if (s == LITEVLM_OK) *bytes = space.total;
     return s;
 }
@@ -1689,7 +1698,7 @@ litevlm_status_t litevlm_select_cache_attend_picked(litevlm_select_t h, int32_t 
     lvs::PickedPlan plan;
     PickedSpace space;
     int64_t total = 0;
-    s = picked_plan(h, batch, q_offsets_h, cache->page_size, budget, &total, &plan, &space);
+    s = picked_plan(h, batch, q_offsets_h, cache->page_size, table_width, budget, &total, &plan, &space);
     if (s != LITEVLM_OK || total == 0) return s;
     lvs::AttendArgs a{};
     s = cache_pages(h, cache, table, table_width, seq_lens, &a.cache, &a.limit);
@@ -1717,11 +1726,20 @@ litevlm_status_t litevlm_select_cache_attend_picked(litevlm_select_t h, int32_t 
     a.out = static_cast<__nv_bfloat16*>(out);
     a.part_o = reinterpret_cast<float*>(ws + space.part_o);
     a.part_ml = reinterpret_cast<float2*>(ws + space.part_ml);
-    a.max_rows = a.group;
+    a.max_rows = plan.queries * a.group;
     a.picked = picked;
     a.budget = budget;
+    a.pick_queries = plan.queries;
     a.pick_chunk = plan.chunk;
     a.pick_chunks = plan.chunks;
+    if (plan.lists) {
+        a.lists = reinterpret_cast<int4*>(ws + space.lists);
+        a.list_len = reinterpret_cast<int32_t*>(ws + space.list_len);
+        a.list_bits = plan.row_tile >= 128 ? reinterpret_cast<uint32_t*>(ws + space.list_bits) : nullptr;
+        a.list_cap = plan.list_cap;
+        a.list_words = plan.list_words;
+    }
+    a.stall = (h->debug_flags & LITEVLM_DEBUG_STALL_ATTEND) != 0;
     a.err = h->err_d;
     a.wait_budget = h->wait_budget;
     const OnDevice on(h->device);

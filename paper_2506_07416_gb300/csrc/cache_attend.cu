@@ -220,8 +220,9 @@ constexpr int kRingBytes = kAttWarps * kAttStages * 2 * Group<D>::kBytes;
 // which keeps addresses out of the lanes' registers: the sweep's 128 requests take 127 us
 // and not 135).
 // (CTAs of an SM as the plan of the split counts them.)
-// PICKED: the keys are those of the pages that the query has in its list, in the list's order; a CTA's rows are heads
-// of one query, and a CTA takes all of the list or a chunk of it.
+// PICKED: the keys are those of picked pages, and a CTA's rows are those of one query, over the pages of its own list, or
+// of a tile of queries, over the list of the pages that any of them has (a key of a page that a row's query has not is as
+// masked); a CTA takes all of the list or a chunk of it.
 template <int D, int NT_, bool FP8, bool WHOLE, bool PICKED = false>
 __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_kernel(const __grid_constant__ AttendArgs a)
 {
@@ -244,12 +245,18 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
     // the request, and its part of the keys: all, or the chunk of this CTA's slot
     int b = blockIdx.z, chunk = kMostKeys, k0 = 0;
     __shared__ int split_s[3];
-    const int64_t pick_row = PICKED ? blockIdx.x / a.pick_chunks : 0;  // the query
-    const int32_t* list = PICKED ? a.picked + (pick_row * a.cache.hkv + h) * a.budget : nullptr;
+    QueryTile qt{0, 0, 1};
+    const int64_t pick_tile = PICKED ? blockIdx.x / a.pick_chunks : 0;
+    const int64_t pick_list = pick_tile * a.cache.hkv + h;
+    int listed = 0;  // keys of the list
     if constexpr (PICKED) {
-        chunk = a.pick_chunk;
-        k0 = (int)(blockIdx.x % a.pick_chunks) * chunk;
-        b = uniform(find_request(a.q_off, a.batch, pick_row));
+        qt = query_tile(a, pick_tile);
+        qt.b = uniform(qt.b), qt.i0 = uniform(qt.i0), qt.queries = uniform(qt.queries);
+        if (qt.queries <= 0) return;
+        b = qt.b;
+        listed = (a.lists ? __ldg(a.list_len + pick_list) : a.budget) << a.cache.page_shift;
+        chunk = a.lists ? list_chunk(listed, a.pick_chunks, 32) : a.pick_chunk;
+        k0 = min((int)(blockIdx.x % a.pick_chunks) * chunk, listed);
     } else if (!WHOLE && a.slots > 0) {
         if (threadIdx.x < 32) {
             chunk = chunk_keys(a);
@@ -265,14 +272,13 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
     RowTile rt = row_tile(a, b, tile, ROWS);
     const int q0 = a.q_off[b];
     if constexpr (PICKED) {
-        const int i = (int)(pick_row - q0);
-        rt.row0 = i * a.group + tile * ROWS;
-        rt.rows = min(ROWS, a.group - tile * ROWS);
+        rt.row0 = qt.i0 * a.group + tile * ROWS;
+        rt.rows = min(ROWS, qt.queries * a.group - tile * ROWS);
     }
     if (rt.rows <= 0) return;
     const int i_last = rt.query(rt.row0 + rt.rows - 1);
     // keys that the tile's last row sees, and this CTA's part of them (PICKED: keys of the list)
-    const int seen = PICKED ? a.budget << a.cache.page_shift : min(rt.len, rt.last0 + i_last + 1);
+    const int seen = PICKED ? listed : min(rt.len, rt.last0 + i_last + 1);
     const int k1 = chunk_end(seen, k0, chunk);
     if (!PICKED && k0 >= k1 && !WHOLE && a.slots > 0) return;  // (without chunks the tile's zeros are written here, else by the join)
     const int all_see = rt.last0 + rt.query(rt.row0);  // the last key that every row sees
@@ -282,39 +288,51 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
     const uint32_t my_s = smem_u32(my);
     const int spans = k1 > k0 ? (k1 - k0 + 31) / 32 : 0;
     const int n_mine = spans > warp ? (spans - warp + kAttWarps - 1) / kAttWarps : 0;
+    const int last_see = rt.last0 + i_last;  // the last key that any row sees
+    const uint32_t all_have = (1u << qt.queries) - 1u;  // PICKED: a bit for every query of the rows
     // page of the lane's group of the warp's n-th span (-1: none; no keys from k1 on are copied), and of a listed page
-    // how many of the group's keys the query sees
-    int next_sees = 0;
+    // the position of the group's first key and the queries that have it
+    int next_pos = 0;
+    uint32_t next_have = 0u;
     auto page_of = [&](int n) -> int32_t {
         const int j = k0 + (warp + n * kAttWarps) * 32 + (lane & 16);
         if constexpr (PICKED) {
-            next_sees = 0;
+            next_have = 0u;
             if (j >= k1) return -1;
-            const int32_t o = __ldg(list + (j >> a.cache.page_shift));
-            if (o < 0 || o > all_see >> a.cache.page_shift) return -1;
-            const int64_t at = (int64_t)o << a.cache.page_shift;
-            const int n_see = all_see - (int)at - (j & ((1 << a.cache.page_shift) - 1)) + 1;
-            if (n_see <= 0) return -1;
-            const int32_t p = cache_page(a.cache.table, a.cache.width, a.cache.num_pages, a.cache.page_shift, b, at);
-            if (p >= 0) next_sees = min(n_see, 16);
-            else if ((lane & 15) == 0) atomicOr(a.err, kErrBounds);
-            return p;
+            int32_t p, o;
+            if (a.lists) {
+                const int4 v = __ldg(a.lists + pick_list * a.list_cap + (j >> a.cache.page_shift));
+                p = v.x, o = v.y;
+                next_have = p >= 0 ? (uint32_t)v.z : 0u;
+            } else {
+                o = __ldg(a.picked + pick_list * a.budget + (j >> a.cache.page_shift));
+                if (o < 0 || o > all_see >> a.cache.page_shift) return -1;
+                p = cache_page(a.cache.table, a.cache.width, a.cache.num_pages, a.cache.page_shift, b,
+                               (int64_t)o << a.cache.page_shift);
+                if (p >= 0) next_have = 1u;
+                else if ((lane & 15) == 0) atomicOr(a.err, kErrBounds);
+            }
+            next_pos = (o << a.cache.page_shift) + (j & ((1 << a.cache.page_shift) - 1));
+            if (next_pos > last_see) next_have = 0u;
+            return next_have ? p : -1;
         }
         if (j >= k1) return -1;
         const int32_t p = cache_page(a.cache.table, a.cache.width, a.cache.num_pages, a.cache.page_shift, b, j);
         if (p < 0 && (lane & 15) == 0) atomicOr(a.err, kErrBounds);
         return p;
     };
-    // whether the lane's group has a page, a bit for every span on its way, the last one's lowest (PICKED: five bits,
-    // the keys seen)
+    // whether the lane's group has a page, a bit for every span on its way, the last one's lowest
     uint32_t named = 0;
 #pragma unroll
     for (int i = 0; i < kAttStages - 1; ++i) {
         const int32_t page = page_of(i);
         if (i < n_mine) load_span<D>(a.cache, page, h, k0 + (warp + i * kAttWarps) * 32, my_s + i * SPAN);
         copy_async_commit();
-        named = PICKED ? named << 5 | next_sees : named << 1 | (page >= 0);
+        named = named << 1 | (page >= 0);
     }
+    static_assert(kAttStages == 2, "one span is on its way beside the one in hand");
+    int pos = next_pos;           // PICKED: of the span in hand
+    uint32_t have = next_have;
     int32_t next_page = page_of(kAttStages - 1);  // (read a span ahead: nothing waits for the table)
 
     // ---- the tile's rows
@@ -365,7 +383,13 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
     bool nan_value = false;
 
     // a group of 16 keys from j0 on, for a single row
-    int sees_of[2] = {0, 0};  // PICKED: keys of a span's two groups that the query sees
+    int pos_of[2] = {0, 0};  // PICKED: of a span's two groups
+    uint32_t have_of[2] = {0u, 0u};
+    uint32_t my_bit[NT][2];  // PICKED: of the queries of rows 2c and 2c + 1
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) my_bit[t][e] = PICKED ? 1u << ((vis[t][e] - all_see) & 31) : 0u;
     auto group1 = [&](const uint8_t* grp, int j0, bool there, int n_sees, auto check) {
         constexpr bool CHECK = decltype(check)::value;
         constexpr int WORDS = D / 32;
@@ -506,7 +530,7 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     s[x][t][e] *= fac[t][e & 1];
-                    if (CHECK && (PICKED ? g + 8 * (e >> 1) >= sees_of[x]
+                    if (CHECK && (PICKED ? !(have_of[x] & my_bit[t][e & 1]) || pos_of[x] + g + 8 * (e >> 1) > vis[t][e & 1]
                                          : !(there >> (16 * x) & 1u) ||
                                                j0 + 16 * x + g + 8 * (e >> 1) > min(vis[t][e & 1], k1 - 1)))
                         s[x][t][e] = -INFINITY;
@@ -582,14 +606,12 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
                     w4[e][0] = *reinterpret_cast<const uint32_t*>(grp + G::kV + key * 32 + g * 4);
                     sc[e] = grp[G::kVs + key * 4 + g / 2];
                 }
-                if constexpr (CHECK && PICKED) {
-                    if (key >= sees_of[x]) sc[e] = 0u;
-                } else if constexpr (CHECK) {
-                    const int at = j0 + 16 * x + key;
+                if constexpr (CHECK) {
+                    const int at = PICKED ? pos_of[x] + key : j0 + 16 * x + key;
                     // what lies behind the last key may be anything, a NaN scale among it
-                    if (at >= k1) sc[e] = 0u;
+                    if (PICKED ? at > last_see || have_of[x] == 0u : at >= k1) sc[e] = 0u;
                     // a NaN value must not reach the rows that do not see it (0 * NaN): put in at the end
-                    if (at > all_see && (sc[e] & 0x7Fu) == 0x7Fu) {
+                    if ((at > all_see || (PICKED && have_of[x] != all_have)) && (sc[e] & 0x7Fu) == 0x7Fu) {
                         sc[e] = 0u;
                         nan_value = true;
                     }
@@ -624,25 +646,32 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
         copy_async_wait<kAttStages - 2>();
         __syncwarp();  // every lane's copies are there, and the span before is no longer read
         const int j0 = k0 + (warp + n * kAttWarps) * 32;
-        // the lane's group of this span has a page; the keys that a picked one has for the query
-        const int sees = PICKED ? named >> (5 * (kAttStages - 2)) & 31u : 0;
-        const bool mine = PICKED ? sees > 0 : named >> (kAttStages - 2) & 1u;
+        const bool mine = named >> (kAttStages - 2) & 1u;  // the lane's group of this span has a page
+        const int now_pos = pos;
+        const uint32_t now_have = have;
+        if constexpr (PICKED) pos = next_pos, have = next_have;  // (those of next_page)
         {
             const int nx = n + kAttStages - 1;
             const int to = stage == 0 ? kAttStages - 1 : stage - 1;
             if (nx < n_mine)
                 load_span<D>(a.cache, next_page, h, j0 + (kAttStages - 1) * kAttWarps * 32, my_s + to * SPAN);
             copy_async_commit();
-            named = PICKED ? named << 5 | next_sees : named << 1 | (next_page >= 0);
+            named = named << 1 | (next_page >= 0);
             next_page = page_of(nx + 1);
         }
         const uint8_t* span = my + stage * SPAN;
         stage = stage + 1 == kAttStages ? 0 : stage + 1;
         const uint32_t there = __ballot_sync(0xffffffffu, mine);
         if (PICKED && there == 0u) continue;
-        const bool all = PICKED ? __all_sync(0xffffffffu, sees == 16) : there == 0xFFFFFFFFu && j0 + 31 <= all_see;
-        if constexpr (PICKED)
-            for (int x = 0; x < 2; ++x) sees_of[x] = __shfl_sync(0xffffffffu, sees, 16 * x);
+        const bool all = PICKED ? __all_sync(0xffffffffu, now_have == all_have && now_pos + 15 <= all_see)
+                                : there == 0xFFFFFFFFu && j0 + 31 <= all_see;
+        if constexpr (PICKED) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                pos_of[x] = __shfl_sync(0xffffffffu, now_pos, 16 * x);
+                have_of[x] = __shfl_sync(0xffffffffu, now_have, 16 * x);
+            }
+        }
         if constexpr (SINGLE) {
             if (all) {
 #pragma unroll
@@ -650,7 +679,7 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
             } else {
 #pragma unroll 1
                 for (int x = 0; x < 2; ++x) {
-                    const int n_sees = x ? sees_of[1] : sees_of[0];
+                    const int n_sees = (x ? have_of[1] : have_of[0]) ? last_see - (x ? pos_of[1] : pos_of[0]) + 1 : 0;
                     if (PICKED ? n_sees > 0 : j0 + 16 * x < k1)
                         group1(span + x * G::kBytes, j0 + 16 * x, there >> (16 * x) & 1u, n_sees, std::true_type{});
                 }
@@ -712,6 +741,16 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
             }
             const int rr = rt.row0 + row, i = rt.query(rr);
             const int64_t at = (int64_t)(q0 + i) * a.hq + h * a.group + rr - i * a.group;
+            if (PICKED && nan_value) {
+                for (int j = k0; j < k1; ++j) {
+                    const int4 v = a.lists ? __ldg(a.lists + pick_list * a.list_cap + (j >> a.cache.page_shift)) : make_int4(-1, 0, 0, 0);
+                    const int slot = j & ((1 << a.cache.page_shift) - 1);
+                    if (v.x < 0 || !((uint32_t)v.z >> (i - qt.i0) & 1u) || (v.y << a.cache.page_shift) + slot > rt.last0 + i)
+                        continue;
+                    const int64_t at_row = cache_row(v.x, a.cache.hkv, h, a.cache.page_shift, slot);
+                    if ((a.cache.scales[1][at_row * (D / 16) + ch / 16] & 0x7Fu) == 0x7Fu) O = __int_as_float(0x7FC00000);
+                }
+            }
             if (!PICKED && nan_value) {
                 for (int j = max(k0, all_see + 1); j < min(k1, rt.last0 + i + 1); ++j) {
                     const int32_t page =
@@ -727,7 +766,7 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
                 a.out[at * D + ch] = __float2bfloat16_rn(L == 0.f ? 0.f : O / L * a.cache.scale[1]);
                 if (a.lse && ch == 0) a.lse[at] = L == 0.f ? INFINITY : M + log2f(L);
             } else {
-                const int64_t part = ((int64_t)blockIdx.x * a.cache.hkv + h) * a.max_rows + (PICKED ? rr - i * a.group : rr);
+                const int64_t part = ((int64_t)blockIdx.x * a.cache.hkv + h) * a.max_rows + (PICKED ? rr - qt.i0 * a.group : rr);
                 a.part_o[part * D + ch] = O;
                 if (ch == 0) a.part_ml[part] = make_float2(M, L);
             }
@@ -1079,8 +1118,103 @@ cudaError_t launch_all(const AttendArgs& a, const AttendPlan& plan, int max_rows
     return e;
 }
 
-// The chunks of a query's list joined, a row (query and head) a warp: chunk x of query r has its sums at
-// ((r * chunks + x) * hkv + key head) * group + head.
+// The list of a tile's queries for a key head: the pages that any of them has and sees, ascending, with the queries that
+// have each. A bit for every page of the request in shared memory (65536 of them at a time), the number of bits before
+// each word, and a second pass over the queries' own lists, which finds every page's place by them. About
+// 2 us, which the next kernel saves many times: of the 37 queries of a tile of 256 rows with 32 pages each, most have
+// the same 120.
+constexpr int kListThreads = 256;
+constexpr int kListWords = 2048;
+__global__ void __launch_bounds__(kListThreads) picked_list_kernel(const __grid_constant__ AttendArgs a)
+{
+    __shared__ uint32_t bits_s[kListWords];
+    __shared__ int before_s[kListWords];
+    __shared__ int warp_s[kListThreads / 32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    griddep_wait();
+    griddep_launch_dependents();
+    const int64_t list = blockIdx.x, tile = list / a.cache.hkv;
+    const int h = (int)(list - tile * a.cache.hkv);
+    const QueryTile qt = query_tile(a, tile);
+    if (qt.queries <= 0) return;
+    bool bad;
+    const int len = cache_len(__ldg(a.lens + qt.b), a.limit, bad);
+    if (bad && tid == 0) atomicOr(a.err, kErrBounds);
+    const int q0 = __ldg(a.q_off + qt.b), t = __ldg(a.q_off + qt.b + 1) - q0;
+    const int first = len - t + qt.i0;                    // position of the first query
+    const int last = first + qt.queries - 1, shift = a.cache.page_shift;
+    const int pages = last < 0 ? 0 : (last >> shift) + 1;  // that the last query sees
+    const int32_t* picked = a.picked + ((int64_t)(q0 + qt.i0) * a.cache.hkv + h) * a.budget;
+    int4* out = a.lists + list * a.list_cap;
+    uint32_t* rows = a.list_bits ? a.list_bits + list * a.pick_queries * a.list_words : nullptr;
+    // calls f(query, page from w0 on) for the lists' pages in [w0, w0 + n) that their queries see
+    auto each = [&](int w0, int n, auto f) {
+        for (int q = warp; q < qt.queries; q += kListThreads / 32) {
+            const int sees = first + q < 0 ? -1 : (first + q) >> shift;
+            const int32_t* from = picked + (int64_t)q * a.cache.hkv * a.budget;
+            for (int x = lane; x < a.budget; x += 32) {
+                const int o = __ldg(from + x);
+                if (o >= 0 && o <= sees && o >= w0 && o - w0 < n) f(q, o - w0);
+            }
+        }
+    };
+    int base = 0;
+    for (int w0 = 0; w0 < pages; w0 += 32 * kListWords) {
+        const int n = min(pages - w0, 32 * kListWords), words = (n + 31) / 32;
+        for (int x = tid; x < words; x += kListThreads) bits_s[x] = 0u;
+        __syncthreads();
+        each(w0, n, [&](int, int o) { atomicOr(bits_s + (o >> 5), 1u << (o & 31)); });
+        __syncthreads();
+        // bits before each word: a thread has `per` neighbouring words
+        const int per = (words + kListThreads - 1) / kListThreads, x0 = min(words, tid * per), x1 = min(words, x0 + per);
+        int mine = 0;
+        for (int x = x0; x < x1; ++x) mine += __popc(bits_s[x]);
+        int sum = mine;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, sum, d);
+            if (lane >= d) sum += y;
+        }
+        if (lane == 31) warp_s[warp] = sum;
+        __syncthreads();
+        int at = base + sum - mine, all = base;
+#pragma unroll
+        for (int w = 0; w < kListThreads / 32; ++w) {
+            if (w < warp) at += warp_s[w];
+            all += warp_s[w];
+        }
+        for (int x = x0; x < x1; ++x) {
+            before_s[x] = at;
+            at += __popc(bits_s[x]);
+        }
+        if (rows) {  // words that only bits of this pass reach
+            const int z0 = (base + 31) / 32, z1 = (all + 31) / 32;
+            for (int q = warp; q < qt.queries; q += kListThreads / 32)
+                for (int z = z0 + lane; z < z1; z += 32) rows[(int64_t)q * a.list_words + z] = 0u;
+        }
+        __syncthreads();
+        for (int x = tid; x < n; x += kListThreads)
+            if (bits_s[x >> 5] >> (x & 31) & 1u) {
+                const int to = before_s[x >> 5] + __popc(bits_s[x >> 5] & ((1u << (x & 31)) - 1u));
+                const int32_t p = cache_page(a.cache.table, a.cache.width, a.cache.num_pages, shift, qt.b,
+                                             (int64_t)(w0 + x) << shift);
+                if (p < 0) atomicOr(a.err, kErrBounds);
+                out[to] = make_int4(p, w0 + x, 0, 0);
+            }
+        __syncthreads();
+        each(w0, n, [&](int q, int o) {
+            const int to = before_s[o >> 5] + __popc(bits_s[o >> 5] & ((1u << (o & 31)) - 1u));
+            if (rows) atomicOr(rows + (int64_t)q * a.list_words + (to >> 5), 1u << (to & 31));
+            else atomicOr(reinterpret_cast<uint32_t*>(&out[to].z), 1u << q);
+        });
+        base = all;
+        __syncthreads();
+    }
+    if (tid == 0) a.list_len[list] = base;
+}
+
+// The chunks of a tile's list joined, a row (query and head) a warp: chunk x of a tile has its sums at
+// ((tile * chunks + x) * hkv + key head) * rows of a tile + row.
 template <int D>
 __global__ void __launch_bounds__(kAttThreads) picked_join_kernel(const __grid_constant__ AttendArgs a, int64_t rows)
 {
@@ -1089,7 +1223,16 @@ __global__ void __launch_bounds__(kAttThreads) picked_join_kernel(const __grid_c
     griddep_wait();
     griddep_launch_dependents();
     if (row >= rows) return;
-    const int64_t r = row / a.hq, from = r * a.pick_chunks * a.hq + row % a.hq;
+    const int64_t r = row / a.hq;
+    const int hq = (int)(row % a.hq), h = hq / a.group;
+    int64_t tile = r;
+    int in = hq % a.group;
+    if (a.lists) {
+        const int b = find_request(a.q_off, a.batch, r), q0 = __ldg(a.q_off + b), i = (int)(r - q0);
+        tile = query_tile_at(q0, b, a.pick_queries) + i / a.pick_queries;
+        in += i % a.pick_queries * a.group;
+    }
+    const int64_t from = (tile * a.pick_chunks * a.cache.hkv + h) * a.max_rows + in, step = (int64_t)a.cache.hkv * a.max_rows;
     float M = kNoRef, L = 0.f, O[D / 32];
 #pragma unroll
     for (int e = 0; e < D / 32; ++e) O[e] = 0.f;
@@ -1099,7 +1242,7 @@ __global__ void __launch_bounds__(kAttThreads) picked_join_kernel(const __grid_c
         float v[U][D / 32];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t at = from + (int64_t)min(x0 + u, a.pick_chunks - 1) * a.hq;
+            const int64_t at = from + min(x0 + u, a.pick_chunks - 1) * step;
             ml[u] = __ldcg(a.part_ml + at);
             if constexpr (D == 128) {
                 const float4 w = __ldcg(reinterpret_cast<const float4*>(a.part_o + at * D) + lane);
@@ -1134,19 +1277,32 @@ cudaError_t launch_picked(const AttendArgs& a, const PickedPlan& plan, int64_t q
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     cfg.stream = stream;
-    const int subs = (a.group + plan.row_tile - 1) / plan.row_tile;
-    cfg.gridDim = dim3((unsigned)(queries * plan.chunks), (unsigned)(subs * a.cache.hkv), 1);
-    cfg.blockDim = dim3(kAttThreads, 1, 1);
-    cfg.dynamicSmemBytes = kRingBytes<D>;
-    auto kern = a.group == 1 ? attend_split_kernel<D, 0, FP8, false, true>
-                             : (plan.row_tile == 8 ? attend_split_kernel<D, 1, FP8, false, true>
-                                                   : attend_split_kernel<D, 2, FP8, false, true>);
-    cudaError_t e = cudaLaunchKernelEx(&cfg, kern, a);
+    cudaError_t e = cudaSuccess;
+    if (plan.lists) {
+        cfg.gridDim = dim3((unsigned)(plan.tiles * a.cache.hkv), 1, 1);
+        cfg.blockDim = dim3(kListThreads, 1, 1);
+        e = cudaLaunchKernelEx(&cfg, picked_list_kernel, a);
+        if (e != cudaSuccess) return e;
+        ++*launches;
+    }
+    if (plan.row_tile >= 128) {
+        e = launch_picked_tiles(a, plan, D, FP8, stream);
+    } else {
+        const int subs = (plan.queries * a.group + plan.row_tile - 1) / plan.row_tile;
+        cfg.gridDim = dim3((unsigned)(plan.tiles * plan.chunks), (unsigned)(subs * a.cache.hkv), 1);
+        cfg.blockDim = dim3(kAttThreads, 1, 1);
+        cfg.dynamicSmemBytes = kRingBytes<D>;
+        auto kern = a.group == 1 && !plan.lists ? attend_split_kernel<D, 0, FP8, false, true>
+                                                : (plan.row_tile == 8 ? attend_split_kernel<D, 1, FP8, false, true>
+                                                                      : attend_split_kernel<D, 2, FP8, false, true>);
+        e = cudaLaunchKernelEx(&cfg, kern, a);
+    }
     if (e != cudaSuccess) return e;
     ++*launches;
     if (plan.chunks > 1) {
         const int64_t rows = queries * a.hq;
         cfg.gridDim = dim3((unsigned)((rows + kAttWarps - 1) / kAttWarps), 1, 1);
+        cfg.blockDim = dim3(kAttThreads, 1, 1);
         cfg.dynamicSmemBytes = 0;
         e = cudaLaunchKernelEx(&cfg, picked_join_kernel<D>, a, rows);
         if (e == cudaSuccess) ++*launches;
@@ -1156,27 +1312,47 @@ cudaError_t launch_picked(const AttendArgs& a, const PickedPlan& plan, int64_t q
 
 }  // namespace
 
-// The lists are split where the queries alone leave the GPU's places empty: as for whole requests, n chunks take
-// rounds / n of the list and the writing and joining of a chunk's sums.
-PickedPlan plan_attend_picked(int64_t queries, int hkv, int group, int64_t keys, int num_sms)
+// A call of single tokens has a tile for each query, with the pages of its own list. Else neighbouring queries of a
+// request, which mostly have the same pages, share a tile of up to 16, 128 or 256 rows and read its pages once.
+// The lists are split where the tiles alone leave the GPU's places empty: as for whole requests, n chunks take
+// rounds / n of the list and the writing and joining of a chunk's sums. A shared list is taken to be twice a query's.
+PickedPlan plan_attend_picked(int batch, int hkv, int group, const int32_t* q_off, int page_shift, int width, int budget,
+                              int num_sms)
 {
-    PickedPlan p;
-    p.row_tile = group <= 8 ? 8 : 16;
-    const int64_t subs = (group + p.row_tile - 1) / p.row_tile, items = queries * hkv * subs;
-    const int64_t places = (int64_t)num_sms * (p.row_tile == 16 ? 3 : 4), units = std::max<int64_t>(1, (keys + 127) / 128);
+    PickedPlan p{};
+    int max_t = 0;
+    for (int b = 0; b < batch; ++b) max_t = std::max(max_t, q_off[b + 1] - q_off[b]);
+    const int64_t max_rows = (int64_t)max_t * group;
+    p.lists = max_t > 1;
+    p.row_tile = p.lists ? attend_row_tile(max_rows) : (group <= 8 ? 8 : 16);
+    p.queries = p.lists ? std::max(1, p.row_tile / group) : 1;
+    int64_t keys = (int64_t)budget << page_shift, items = 0;
+    const int64_t subs = ((int64_t)p.queries * group + p.row_tile - 1) / p.row_tile;
+    for (int b = 0; b < batch; ++b) items += (int64_t)((q_off[b + 1] - q_off[b] + p.queries - 1) / p.queries) * hkv * subs;
+    p.tiles = p.lists ? query_tile_at(q_off[batch], batch, p.queries) : q_off[batch];
+    if (p.lists) {
+        p.list_cap = (int32_t)std::min<int64_t>(width, (int64_t)p.queries * budget);
+        p.list_words = (p.list_cap + 31) / 32;
+        if (p.queries > 1) keys = std::min<int64_t>(2 * keys, (int64_t)p.list_cap << page_shift);
+    }
+    const bool many = p.row_tile >= 128;
+    const int64_t places = (int64_t)num_sms * (p.row_tile == 256 ? 1 : (p.row_tile == 128 ? 2 : (p.row_tile == 16 ? 3 : 4)));
+    const int64_t units = std::max<int64_t>(1, (keys + 127) / 128);
     int64_t best = 1;
     if (items > 0 && items < places) {
         best = std::min(units, places / items);
     } else if (items < 3 * places) {
         double cost = 1e30;
         for (int64_t n = 1; n <= std::min<int64_t>(units, 8); ++n) {
-            const double r = (double)((items * n + places - 1) / places);
-            const double c = r / (double)n + r * (n > 1 ? 1.25 * p.row_tile : 0.0) / (double)std::max<int64_t>(keys, 1);
+            const double whole = (double)((items * n + places - 1) / places);
+            const double r = many ? (whole + (double)(items * n) / (double)places) / 2.0 : whole;
+            const double more = (many ? 700.0 : 0.0) + (n > 1 ? (many ? 2.3 : 1.25) * p.row_tile : 0.0);
+            const double c = r / (double)n + r * more / (double)std::max<int64_t>(keys, 1);
             if (c < cost) cost = c, best = n;
         }
     }
     p.chunk = (int32_t)(((keys + best - 1) / best + 31) & ~31ll);
-    p.chunks = (int32_t)std::max<int64_t>(1, (keys + p.chunk - 1) / p.chunk);
+    p.chunks = (int32_t)(p.lists ? best : std::max<int64_t>(1, (keys + p.chunk - 1) / p.chunk));
     return p;
 }
 

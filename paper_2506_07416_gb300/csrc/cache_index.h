@@ -32,6 +32,9 @@ LVS_HD int64_t tile_at(int64_t rows, int64_t b) { return rows / 128 + b; }
 // places follow the last one's: n tokens touch at most floor(n / page) + 2 pages. Of the batch's end: the places of all.
 LVS_HD int64_t page_at(int64_t rows, int64_t b, int32_t page_shift) { return (rows >> page_shift) + 2 * b; }
 
+// The same of tiles of `per` queries: a request of n queries has at most floor((rows + n) / per) - floor(rows / per) + 1.
+LVS_HD int64_t query_tile_at(int64_t rows, int64_t b, int32_t per) { return rows / per + b; }
+
 // Tokens of a request that the kernels may touch: its length cut to
 // [0, limit]. `bad` tells that the length was outside.
 LVS_HD int cache_len(int32_t len, int32_t limit, bool& bad)

@@ -196,7 +196,10 @@ struct VPart {
     uint32_t scale[8];
 };
 
-template <int D, bool FP8, int NR>
+// PICKED: the rows are whole queries of a tile, and the keys those of the pages that any of them has, in the list's order; a
+// key of a page that a row's query has not is as masked. Of 64 or 32 keys that no row of a warp has, the warp
+// makes no exponentials.
+template <int D, bool FP8, int NR, bool PICKED = false>
 __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile_kernel(const __grid_constant__ AttendArgs a)
 {
     using L = TileLayout<D, NR>;
@@ -218,7 +221,19 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
     griddep_launch_dependents();
     int b = blockIdx.z, chunk = kMostKeys, k0 = 0;
     __shared__ int split_s[3];
-    if (a.slots > 0) {
+    QueryTile qt{0, 0, 0};
+    const int64_t pick_tile = PICKED ? blockIdx.x / a.pick_chunks : 0;
+    const int64_t pick_list = pick_tile * a.cache.hkv + h;
+    int listed = 0;  // keys of the list
+    if constexpr (PICKED) {
+        qt = query_tile(a, pick_tile);
+        qt.b = uniform(qt.b), qt.i0 = uniform(qt.i0), qt.queries = uniform(qt.queries);
+        if (qt.queries <= 0) return;
+        b = qt.b;
+        listed = uniform(__ldg(a.list_len + pick_list) << a.cache.page_shift);
+        chunk = list_chunk(listed, a.pick_chunks, kTileKeys);
+        k0 = min((int)(blockIdx.x % a.pick_chunks) * chunk, listed);
+    } else if (a.slots > 0) {
         if (threadIdx.x < 32) {
             chunk = chunk_keys(a);
             find_slot(a, blockIdx.x, chunk, b, k0);
@@ -230,13 +245,18 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
         // (for the launch that joins the chunks: their length, and the request's first slot)
         if (k0 == 0 && blockIdx.y == 0 && threadIdx.x == 0) a.split[b] = make_int2(chunk, (int)blockIdx.x);
     }
-    const RowTile rt = row_tile(a, b, tile, 128 * NR);
+    RowTile rt = row_tile(a, b, tile, 128 * NR);
+    if constexpr (PICKED) {
+        rt.row0 = qt.i0 * a.group + tile * 128 * NR;
+        rt.rows = min(128 * NR, qt.queries * a.group - tile * 128 * NR);
+    }
     if (rt.rows <= 0) return;
     const int q0 = a.q_off[b];
-    const int seen = min(rt.len, rt.last0 + rt.query(rt.row0 + rt.rows - 1) + 1);
+    const int seen = PICKED ? listed : min(rt.len, rt.last0 + rt.query(rt.row0 + rt.rows - 1) + 1);
     const int k1 = chunk_end(seen, k0, chunk);
-    if (k0 >= k1 && a.slots > 0) return;  // (without chunks the tile's zeros are written here, else by the join)
+    if (!PICKED && k0 >= k1 && a.slots > 0) return;  // (without chunks the tile's zeros are written here, else by the join)
     const int all_see = rt.last0 + rt.query(rt.row0);  // the last key that every row sees
+    const int4* list = PICKED ? a.lists + pick_list * a.list_cap : nullptr;  // page in the pool, page of the request
     const int n_tiles = uniform(k1 > k0 ? (k1 - k0 + kTileKeys - 1) / kTileKeys : 0);
     const int live = (rt.rows + 31) / 32;  // softmax warps with rows
     const int row_tiles = NR > 1 ? uniform((rt.rows + 127) / 128) : 1;
@@ -286,10 +306,22 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
         }
         if (warp < live) {
             const uint32_t ts = tmem + lanes + 256 * rtile, to = ts + 128;
-            const int vis = min(rt.last0 + query, k1 - 1);  // the last key that the row sees here
+            // the last key that the row sees here (PICKED: the last position)
+            const int vis = PICKED ? rt.last0 + query : min(rt.last0 + query, k1 - 1);
+            // the pages that the row's query has, a bit for each of the list, 32 at a time
+            const uint32_t* bits = PICKED ? a.list_bits + (pick_list * a.pick_queries + query - qt.i0) * a.list_words : nullptr;
+            uint32_t bit_word = 0u;
+            int next_pos = 0;  // PICKED: position of the group's first key
             // page of a tile's group of 16 keys (lanes 0 to 7); groups without one are as masked
             auto page_of = [&](int t) -> int32_t {
                 const int j = k0 + t * kTileKeys + lane * 16;
+                if constexpr (PICKED) {
+                    if (lane >= 8) return 0;
+                    if (j >= k1) return -1;
+                    const int4 v = __ldg(list + (j >> a.cache.page_shift));
+                    next_pos = (v.y << a.cache.page_shift) + (j & ((1 << a.cache.page_shift) - 1));
+                    return v.x;
+                }
                 return lane < 8 && j < k1
                            ? cache_page(a.cache.table, a.cache.width, a.cache.num_pages, a.cache.page_shift, b, j)
                            : 0;
@@ -301,17 +333,40 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
                 for (int t = 0; t < n_tiles; ++t) {
                     const int j0 = k0 + t * kTileKeys;
                     const uint32_t gone = __ballot_sync(0xffffffffu, next_page < 0);
+                    const int pos = next_pos;
+                    // PICKED: whether some key is behind a row's position; the groups that the row has, and that any of the warp has
+                    const bool late = PICKED && __any_sync(0xffffffffu, lane < 8 && next_page >= 0 && pos + 15 > all_see);
+                    [[maybe_unused]] uint32_t has = 0u, any_has = 0u;
+                    if constexpr (PICKED) {
+                        const int shift = a.cache.page_shift, x0 = j0 >> shift;
+                        if (t == 0 || (x0 & 31) == 0) bit_word = real ? __ldg(bits + (x0 >> 5)) : 0u;
+                        const uint32_t b8 = bit_word >> (x0 & 31);
+#pragma unroll
+                        for (int g = 0; g < 8; ++g) has |= (b8 >> ((16 * g) >> shift) & 1u) << g;
+                        has &= ~gone;
+                        any_has = __reduce_or_sync(0xffffffffu, has);
+                    }
                     next_page = page_of(t + 1);
-                    const bool check = j0 + kTileKeys > min(k1, all_see + 1) || gone != 0;
+                    const bool check = PICKED ? late : j0 + kTileKeys > min(k1, all_see + 1) || gone != 0;
                     if (!poll_phase_warp(BAR(B_S_FULL + rtile), (uint32_t)t & 1u, ctl)) break;
                     tc_fence_after();
                     // columns of a chunk of 32 that the row sees, as a mask
                     auto mask_of = [&](int c0) -> uint32_t {
-                        const int n = vis - (j0 + c0) + 1;
-                        uint32_t k = n >= 32 ? 0xFFFFFFFFu : (n <= 0 ? 0u : (1u << n) - 1u);
-                        if (gone >> (c0 / 16) & 1u) k &= 0xFFFF0000u;
-                        if (gone >> (c0 / 16 + 1) & 1u) k &= 0x0000FFFFu;
-                        return k;
+                        if constexpr (PICKED) {
+                            uint32_t k = 0u;
+#pragma unroll
+                            for (int x = 0; x < 2; ++x) {
+                                const int n = vis - __shfl_sync(0xffffffffu, pos, c0 / 16 + x) + 1;
+                                k |= (n >= 16 ? 0xFFFFu : (n <= 0 ? 0u : (1u << n) - 1u)) << (16 * x);
+                            }
+                            return k;
+                        } else {
+                            const int n = vis - (j0 + c0) + 1;
+                            uint32_t k = n >= 32 ? 0xFFFFFFFFu : (n <= 0 ? 0u : (1u << n) - 1u);
+                            if (gone >> (c0 / 16) & 1u) k &= 0xFFFF0000u;
+                            if (gone >> (c0 / 16 + 1) & 1u) k &= 0x0000FFFFu;
+                            return k;
+                        }
                     };
                     // the columns, STEP at a time from the last on, read for their maximum; the first STEP
                     // are still there when the exponentials are made
@@ -338,8 +393,17 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
                     };
 #pragma unroll 1
                     for (int c0 = kTileKeys - STEP; c0 >= 0; c0 -= STEP) {
+                        if (PICKED && !(any_has >> (c0 / 16) & ((1u << STEP / 16) - 1u))) continue;
                         read(c0);
-                        mx = fmaxf(mx, row_max<STEP>(v));
+                        if constexpr (PICKED) {
+#pragma unroll
+                            for (int x = 0; x < STEP / 16; ++x) {
+                                const float top = row_max<16>(v + 16 * x);
+                                if (has >> (c0 / 16 + x) & 1u) mx = fmaxf(mx, top);
+                            }
+                        } else {
+                            mx = fmaxf(mx, row_max<STEP>(v));
+                        }
                     }
                     mx *= unit;  // (> 0, see row_factor)
                     if (__any_sync(0xffffffffu, mx > m + kRefSlack)) {
@@ -362,23 +426,50 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
                     }
                     const float2 nm2 = make_float2(-m, -m);
                     float2 s0 = make_float2(0.f, 0.f), s1 = make_float2(0.f, 0.f);
-                    auto chunk_of = [&](int c0, const float* x) {
+                    auto chunk_of = [&](int c0, const float* x_) {
                         float p[16];
+                        if constexpr (PICKED) {
 #pragma unroll
-                        for (int i = 0; i < 32; i += 4) {
-                            const float2 x0 = ffma2(make_float2(x[i], x[i + 1]), fac2, nm2);
-                            const float2 x1 = ffma2(make_float2(x[i + 2], x[i + 3]), fac2, nm2);
-                            const float2 p0 = make_float2(ex2(x0.x), ex2(x0.y)), p1 = make_float2(ex2(x1.x), ex2(x1.y));
-                            s0 = fadd2(s0, p0);
-                            s1 = fadd2(s1, p1);
-                            p[i / 2] = __uint_as_float(pack_h2(p0.x, p0.y));
-                            p[i / 2 + 1] = __uint_as_float(pack_h2(p1.x, p1.y));
+                            for (int x = 0; x < 2; ++x) {
+                                const bool mine = has >> (c0 / 16 + x) & 1u;
+                                const uint32_t keep = mine ? 0xFFFFFFFFu : 0u;
+                                float2 t0 = make_float2(0.f, 0.f), t1 = t0;
+#pragma unroll
+                                for (int i = 16 * x; i < 16 * x + 16; i += 4) {
+                                    const float2 x0 = ffma2(make_float2(x_[i], x_[i + 1]), fac2, nm2);
+                                    const float2 x1 = ffma2(make_float2(x_[i + 2], x_[i + 3]), fac2, nm2);
+                                    const float2 p0 = make_float2(ex2(x0.x), ex2(x0.y)), p1 = make_float2(ex2(x1.x), ex2(x1.y));
+                                    t0 = fadd2(t0, p0);
+                                    t1 = fadd2(t1, p1);
+                                    p[i / 2] = __uint_as_float(pack_h2(p0.x, p0.y) & keep);
+                                    p[i / 2 + 1] = __uint_as_float(pack_h2(p1.x, p1.y) & keep);
+                                }
+                                if (mine) s0 = fadd2(s0, t0), s1 = fadd2(s1, t1);
+                            }
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 32; i += 4) {
+                                const float2 x0 = ffma2(make_float2(x_[i], x_[i + 1]), fac2, nm2);
+                                const float2 x1 = ffma2(make_float2(x_[i + 2], x_[i + 3]), fac2, nm2);
+                                const float2 p0 = make_float2(ex2(x0.x), ex2(x0.y)), p1 = make_float2(ex2(x1.x), ex2(x1.y));
+                                s0 = fadd2(s0, p0);
+                                s1 = fadd2(s1, p1);
+                                p[i / 2] = __uint_as_float(pack_h2(p0.x, p0.y));
+                                p[i / 2 + 1] = __uint_as_float(pack_h2(p1.x, p1.y));
+                            }
                         }
                         tmem_st16(ts + c0 / 2, p);
                     };
                     // (P of columns c is written to the columns from c / 2 on, which have been read)
 #pragma unroll 1
                     for (int c0 = 0; c0 < kTileKeys; c0 += STEP) {
+                        if (PICKED && !(any_has >> (c0 / 16) & ((1u << STEP / 16) - 1u))) {
+                            const float none[16] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f,
+                                                    0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                            for (int x = 0; x < STEP; x += 32) tmem_st16(ts + (c0 + x) / 2, none);
+                            continue;
+                        }
                         if (c0 > 0) read(c0);
 #pragma unroll
                         for (int x = 0; x < STEP; x += 32) chunk_of(c0 + x, v + x);
@@ -405,11 +496,13 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
         const uint32_t v_at = (kg >> 3) * (D * 128) + vb * 16 * 128;
         const uint32_t v_x = (uint32_t)(turn << 7 | ((kg & 7) ^ turn) << 4);
         const bool v_part = vb < D / 16;
+        int pv_pos = 0;  // PICKED: position of the thread's first key of V
         auto page_at = [&](int j) -> int32_t {
-            return j < k1 ? cache_page(C.table, C.width, C.num_pages, C.page_shift, b, j) : -1;
+            if constexpr (PICKED) return j < k1 ? __ldg(&list[j >> C.page_shift].x) : -1;
+            else return j < k1 ? cache_page(C.table, C.width, C.num_pages, C.page_shift, b, j) : -1;
         };
         auto report = [&](int32_t page, int j) {
-            if (page < 0 && j < k1) atomicOr(a.err, kErrBounds);
+            if (!PICKED && page < 0 && j < k1) atomicOr(a.err, kErrBounds);
         };
         auto load_v = [&](VPart& x, int32_t page, int j0) {
             const int64_t at = cache_row(page >= 0 ? page : 0, C.hkv, h, C.page_shift, (j0 + kg * 8) & smask);
@@ -425,10 +518,13 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
         };
         // pages of the thread's keys (a group of 16 lies in one), a tile ahead of the loads of the codes
         int32_t pk0, pk1, pv;
+        int next_pv_pos = 0;
         auto pages = [&](int j0) {
             pk0 = page_at(j0 + w * 32);
             pk1 = page_at(j0 + w * 32 + 16);
             pv = page_at(j0 + kg * 8);
+            if constexpr (PICKED)
+                if (pv >= 0) next_pv_pos = (__ldg(&list[(j0 + kg * 8) >> C.page_shift].y) << C.page_shift) + ((j0 + kg * 8) & smask);
         };
         auto report_pages = [&](int j0) {
             if ((lane & 15) == 0) report(lane ? pk1 : pk0, j0 + w * 32 + lane);
@@ -439,6 +535,7 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
         report_pages(k0);
         kp.load(C, pk0, pk1, h, k0, w);
         load_v(vp, pv, k0);
+        pv_pos = next_pv_pos;
         pages(k0 + kTileKeys);
         for (int t = 0; t < n_tiles; ++t) {
             const int j0 = k0 + t * kTileKeys, jn = j0 + kTileKeys;
@@ -459,7 +556,16 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
             }
             if (t >= ST && !poll_phase_warp(BAR(B_V_FREE + st), past, ctl)) break;
             if (v_part) {
-                if (j0 + kTileKeys - 1 > all_see) {
+                if constexpr (PICKED) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        if (pv_pos + i >= rt.len) vp.scale[i] = 0u;  // behind the last token
+                        if ((vp.scale[i] & 0x7Fu) == 0x7Fu) {        // (some of the rows may not have the page)
+                            vp.scale[i] = 0u;
+                            *nan_flag = 1;
+                        }
+                    }
+                } else if (j0 + kTileKeys - 1 > all_see) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const int j = j0 + kg * 8 + i;
@@ -501,6 +607,7 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
             __syncwarp();
             if (lane == 0) mbar_arrive(BAR(B_V_FULL + st));
             if (more) load_v(vp, pv, jn);
+            pv_pos = next_pv_pos;
             pages(jn + kTileKeys);
         }
     } else {
@@ -566,11 +673,24 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
     // ---- the rows' results
     // values that are NaN, for the rows that see them: whether block x of 16 channels has one
     auto nan_block = [&](int x, int i) -> bool {
-        for (int j = max(k0, all_see + 1); j < min(k1, rt.last0 + i + 1); ++j) {
-            const int32_t page = cache_page(a.cache.table, a.cache.width, a.cache.num_pages, a.cache.page_shift, b, j);
-            if (page < 0) continue;
-            const int64_t r = cache_row(page, a.cache.hkv, h, a.cache.page_shift, j & ((1 << a.cache.page_shift) - 1));
-            if ((a.cache.scales[1][r * (D / 16) + x] & 0x7Fu) == 0x7Fu) return true;
+        if constexpr (PICKED) {
+            const uint32_t* has = a.list_bits + (pick_list * a.pick_queries + i - qt.i0) * a.list_words;
+            const int shift = a.cache.page_shift, smask = (1 << shift) - 1;
+            for (int j = k0; j < k1; ++j) {
+                const int4 v = __ldg(list + (j >> shift));
+                if (v.x < 0 || !(__ldg(has + (j >> shift >> 5)) >> (j >> shift & 31) & 1u) ||
+                    (v.y << shift) + (j & smask) > rt.last0 + i)
+                    continue;
+                const int64_t r = cache_row(v.x, a.cache.hkv, h, shift, j & smask);
+                if ((a.cache.scales[1][r * (D / 16) + x] & 0x7Fu) == 0x7Fu) return true;
+            }
+        } else {
+            for (int j = max(k0, all_see + 1); j < min(k1, rt.last0 + i + 1); ++j) {
+                const int32_t page = cache_page(a.cache.table, a.cache.width, a.cache.num_pages, a.cache.page_shift, b, j);
+                if (page < 0) continue;
+                const int64_t r = cache_row(page, a.cache.hkv, h, a.cache.page_shift, j & ((1 << a.cache.page_shift) - 1));
+                if ((a.cache.scales[1][r * (D / 16) + x] & 0x7Fu) == 0x7Fu) return true;
+            }
         }
         return false;
     };
@@ -601,7 +721,8 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
         }
         __syncwarp();
         const int64_t at = (int64_t)(q0 + query) * a.hq + h * a.group + row - query * a.group;
-        const int64_t part = ((int64_t)blockIdx.x * a.cache.hkv + h) * a.max_rows + row;
+        const int64_t part = ((int64_t)blockIdx.x * a.cache.hkv + h) * a.max_rows + row - (PICKED ? qt.i0 * a.group : 0);
+        const bool split = PICKED ? a.pick_chunks > 1 : a.slots > 0;
         const float f = l == 0.f ? 0.f : a.cache.scale[1] / l;
         const int rows = min(32, rt.rows - warp * 32);
         constexpr int N = D / 32;  // channels of a lane
@@ -611,7 +732,7 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
 #pragma unroll
             for (int i = 0; i < N; i += 2)
                 *reinterpret_cast<float2*>(v + i) = *reinterpret_cast<const float2*>(mine + r * PITCH + lane * N + i);
-            if (a.slots > 0) {
+            if (split) {
                 float* out = a.part_o + __shfl_sync(0xffffffffu, part, r) * D + lane * N;
                 if constexpr (N == 4) __stcg(reinterpret_cast<float4*>(out), make_float4(v[0], v[1], v[2], v[3]));
                 else __stcg(reinterpret_cast<float2*>(out), make_float2(v[0], v[1]));
@@ -626,8 +747,8 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
                         __floats2bfloat162_rn(none ? 0.f : v[i] * fr, none ? 0.f : v[i + 1] * fr);
             }
         }
-        if (real && a.slots > 0) a.part_ml[part] = make_float2(m, l);
-        if (real && a.slots == 0 && a.lse) a.lse[at] = l == 0.f ? INFINITY : m + log2f(l);
+        if (real && split) a.part_ml[part] = make_float2(m, l);
+        if (!PICKED && real && a.slots == 0 && a.lse) a.lse[at] = l == 0.f ? INFINITY : m + log2f(l);
     }
     tc_fence_before();
     __syncthreads();
@@ -886,7 +1007,38 @@ cudaError_t launch_variant(const AttendArgs& a, int tiles, cudaStream_t stream)
     return cudaLaunchKernelEx(&cfg, kern, a);
 }
 
+template <int D, bool FP8, int NR>
+cudaError_t launch_picked_variant(const AttendArgs& a, const PickedPlan& plan, cudaStream_t stream)
+{
+    using L = TileLayout<D, NR>;
+    auto kern = attend_tile_kernel<D, FP8, NR, true>;
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, L::ALLOC);
+    if (e != cudaSuccess) return e;
+    const int subs = (plan.queries * a.group + 128 * NR - 1) / (128 * NR);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(plan.tiles * plan.chunks), (unsigned)(subs * a.cache.hkv), 1);
+    cfg.blockDim = dim3(kTileThreads<NR>, 1, 1);
+    cfg.dynamicSmemBytes = L::ALLOC;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1] = {pdl_attribute()};
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kern, a);
+}
+
 }  // namespace
+
+cudaError_t launch_picked_tiles(const AttendArgs& a, const PickedPlan& plan, int head_dim, bool fp8, cudaStream_t stream)
+{
+    if (plan.row_tile == 256) {
+        if (fp8) return launch_picked_variant<128, true, 2>(a, plan, stream);
+        return head_dim == 128 ? launch_picked_variant<128, false, 2>(a, plan, stream)
+                               : launch_picked_variant<64, false, 2>(a, plan, stream);
+    }
+    if (fp8) return launch_picked_variant<128, true, 1>(a, plan, stream);
+    return head_dim == 128 ? launch_picked_variant<128, false, 1>(a, plan, stream)
+                           : launch_picked_variant<64, false, 1>(a, plan, stream);
+}
 
 cudaError_t launch_attend_tiles(const AttendArgs& a, int head_dim, bool fp8, int row_tile, int tiles, cudaStream_t stream)
 {

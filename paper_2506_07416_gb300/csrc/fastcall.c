@@ -335,10 +335,10 @@ static PyObject *f_picked(PyObject *self, PyObject *const *args, Py_ssize_t n)
     END
 }
 
-/* bytes of a workspace from a handle, a batch, its offsets and two or three sizes, or -status */
-static PyObject *bytes_of(int which, int sizes, PyObject *const *args, Py_ssize_t n)
+/* bytes of a workspace from a handle, a batch, its offsets and three sizes, or -status */
+static PyObject *bytes_of(int which, PyObject *const *args, Py_ssize_t n)
 {
-    if (n != 3 + sizes) {
+    if (n != 6) {
         PyErr_SetString(PyExc_TypeError, "wrong number of arguments");
         return NULL;
     }
@@ -347,7 +347,7 @@ static PyObject *bytes_of(int which, int sizes, PyObject *const *args, Py_ssize_
     const int32_t *off;
     uint64_t hd, batch, x[3] = {0, 0, 0};
     int bad = as_bits(args[0], 'h', &hd) || as_bits(args[1], 'i', &batch) || as_host_i32(args[2], &h, &off, NULL);
-    for (int k = 0; k < sizes && !bad; ++k) bad = as_bits(args[3 + k], 'i', &x[k]);
+    for (int k = 0; k < 3 && !bad; ++k) bad = as_bits(args[3 + k], 'i', &x[k]);
     if (bad) {
         release(&h);
         return NULL;
@@ -355,9 +355,7 @@ static PyObject *bytes_of(int which, int sizes, PyObject *const *args, Py_ssize_
     int64_t bytes = 0;
     const I b = (I)(uint32_t)batch, x0 = (I)(uint32_t)x[0], x1 = (I)(uint32_t)x[1], x2 = (I)(uint32_t)x[2];
     const P handle = (P)(uintptr_t)hd;
-    int rc;
-    if (sizes == 3) rc = ((int (*)(P, I, const int32_t *, I, I, I, int64_t *))g_fn[which])(handle, b, off, x0, x1, x2, &bytes);
-    else rc = ((int (*)(P, I, const int32_t *, I, I, int64_t *))g_fn[which])(handle, b, off, x0, x1, &bytes);
+    const int rc = ((int (*)(P, I, const int32_t *, I, I, I, int64_t *))g_fn[which])(handle, b, off, x0, x1, x2, &bytes);
     release(&h);
     return PyLong_FromLongLong(rc ? -(long long)rc : (long long)bytes);
 }
@@ -366,14 +364,14 @@ static PyObject *bytes_of(int which, int sizes, PyObject *const *args, Py_ssize_
 static PyObject *f_pick_bytes(PyObject *self, PyObject *const *args, Py_ssize_t n)
 {
     (void)self;
-    return bytes_of(F_PICK_SPACE, 3, args, n);
+    return bytes_of(F_PICK_SPACE, args, n);
 }
 
-/* picked_bytes(handle, batch, q_offsets_h, page_size, budget) */
+/* picked_bytes(handle, batch, q_offsets_h, page_size, table_width, budget) */
 static PyObject *f_picked_bytes(PyObject *self, PyObject *const *args, Py_ssize_t n)
 {
     (void)self;
-    return bytes_of(F_PICKED_SPACE, 2, args, n);
+    return bytes_of(F_PICKED_SPACE, args, n);
 }
 
 /* attend_bytes(handle, batch, q_offsets_h, max_len, weights): bytes of an attention call's workspace, or -status */

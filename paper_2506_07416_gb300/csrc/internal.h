@@ -180,10 +180,17 @@ struct AttendArgs {
     const float* weights_in;  // [num_pages][page_size]
     float* weights_out;       // null: no weights
     int32_t stall;            // debug: the second tile's values are never made
+    // attention over picked pages
     const int32_t* picked;    // [rows][hkv][budget] pages of each query's request, or null: all keys
     int32_t budget;
-    int32_t pick_chunk;       // keys of the picked pages that a CTA takes, and how many such chunks a query has
-    int32_t pick_chunks;
+    int32_t pick_queries;     // queries of a tile
+    int32_t pick_chunks;      // chunks of a tile's keys
+    int32_t pick_chunk;       // keys of a chunk (without lists: of a query's own pages)
+    int4* lists;              // [tiles][hkv][list_cap] pages of a tile's queries: in the pool, of the request, a bit for each
+                              // query that has it (up to 16 rows); null: a tile is one query
+    int32_t* list_len;        // [tiles][hkv]
+    uint32_t* list_bits;      // [tiles][hkv][pick_queries][list_words] the pages of each query, a bit each (128 rows and more)
+    int32_t list_cap, list_words;
     int32_t* err;
     long long wait_budget;
 };
@@ -200,10 +207,14 @@ cudaError_t launch_cache_attend(const AttendArgs& a, const AttendPlan& plan, int
                                 int64_t total_rows, int max_len, cudaStream_t stream, int32_t* launches);
 
 struct PickedPlan {
-    int32_t row_tile;         // rows (heads of a key head) of a CTA: 8 or 16
-    int32_t chunk, chunks;
+    int32_t row_tile;         // rows of a CTA: 8, 16, 128 or 256
+    int32_t queries;          // queries of a tile
+    bool lists;               // the queries of a tile share a list
+    int64_t tiles;            // query_tile_at of the batch's end (without lists: the queries)
+    int32_t chunk, chunks, list_cap, list_words;
 };
-PickedPlan plan_attend_picked(int64_t queries, int hkv, int group, int64_t keys, int num_sms);
+PickedPlan plan_attend_picked(int batch, int hkv, int group, const int32_t* q_off, int page_shift, int width, int budget,
+                              int num_sms);
 cudaError_t launch_attend_picked(const AttendArgs& a, const PickedPlan& plan, int head_dim, bool fp8, int64_t queries,
                                  cudaStream_t stream, int32_t* launches);
 

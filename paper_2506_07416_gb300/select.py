@@ -93,7 +93,7 @@ def _load():
     lib.litevlm_select_cache_bounds.argtypes = [P, i32, P, P, P, i32, P, P, P, P]
     lib.litevlm_select_cache_pick_workspace.argtypes = [P, i32, P, i32, i32, i32, ctypes.POINTER(i64)]
     lib.litevlm_select_cache_pick.argtypes = [P, i32, P, P, i32, P, P, i64, P, P, i32, i32, i32, i32, P, P, i64, P]
-    lib.litevlm_select_cache_attend_picked_workspace.argtypes = [P, i32, P, i32, i32, ctypes.POINTER(i64)]
+    lib.litevlm_select_cache_attend_picked_workspace.argtypes = [P, i32, P, i32, i32, i32, ctypes.POINTER(i64)]
     lib.litevlm_select_cache_attend_picked.argtypes = [P, i32, P, P, i32, P, P, i64, P, P, P, i32, f32, P, P, i64, P]
     lib.litevlm_select_set_wait_budget.argtypes = [P, i64]
     lib.litevlm_select_set_debug_flags.argtypes = [P, i32]
@@ -383,9 +383,10 @@ def cache_pick(handle: int, batch: int, bounds, table, table_width: int, seq_len
         _check(rc, handle)
 
 
-def cache_attend_picked_workspace(handle: int, batch: int, q_offsets_h, page_size: int, budget: int) -> int:
+def cache_attend_picked_workspace(handle: int, batch: int, q_offsets_h, page_size: int, table_width: int,
+                                  budget: int) -> int:
     """litevlm_select_cache_attend_picked_workspace: bytes of the workspace of attention over picked pages."""
-    n = _FC.picked_bytes(handle, batch, q_offsets_h, page_size, budget)
+    n = _FC.picked_bytes(handle, batch, q_offsets_h, page_size, table_width, budget)
     if n < 0:
         _check(-n, handle)
     return n
@@ -999,7 +1000,7 @@ class Selector:
             _refuse(f"q has {q.shape[0]} rows, the offsets {total}")
         _want("picked", picked, torch.int32, (total, self.kv_heads, -1), dev)
         budget = picked.shape[2]
-        need = cache_attend_picked_workspace(self.handle, batch, off_h, cache.page_size, budget)
+        need = cache_attend_picked_workspace(self.handle, batch, off_h, cache.page_size, table.shape[1], budget)
         with _allocate_on(stream, dev):
             if out is None:
                 out = torch.empty((total, self.heads, self.head_dim), dtype=torch.bfloat16, device=q.device)

@@ -105,7 +105,7 @@ def test_calls_need_a_handle():
     n = ctypes.c_int64(-7)
     assert L.litevlm_select_cache_pick_workspace(N, 1, N, 1, 16, 1, ctypes.byref(n)) == 1
     assert L.litevlm_select_cache_pick(N, 1, N, N, 1, N, N, 0, N, N, 1, 1, 0, 0, N, N, 0, N) == 1
-    assert L.litevlm_select_cache_attend_picked_workspace(N, 1, N, 16, 1, ctypes.byref(n)) == 1 and n.value == -7
+    assert L.litevlm_select_cache_attend_picked_workspace(N, 1, N, 16, 1, 1, ctypes.byref(n)) == 1 and n.value == -7
     assert L.litevlm_select_cache_attend_picked(N, 1, N, N, 1, N, N, 0, N, N, N, 1, 1.0, N, N, 0, N) == 1
 
 
