@@ -1443,7 +1443,7 @@ litevlm_status_t pick_plan(litevlm_select_t h, int32_t batch, const int32_t* q_o
 
 // The same of attention over picked pages.
 struct PickedSpace {
-    int64_t part_o, part_ml, lists, list_len, list_bits, total;
+    int64_t part_o, part_ml, lists, list_heads, tile_of, list_bits, total;
 };
 litevlm_status_t picked_plan(litevlm_select_t h, int32_t batch, const int32_t* q_offsets_h, int32_t page_size,
                              int32_t table_width, int32_t budget, int64_t* total, lvs::PickedPlan* plan,
@@ -1471,8 +1471,9 @@ litevlm_status_t picked_plan(litevlm_select_t h, int32_t batch, const int32_t* q
     space->part_o = 0;
     space->part_ml = round256(parts * c.head_dim * 4);
     space->lists = space->part_ml + round256(parts * 8);
-    space->list_len = space->lists + round256(lists * p.list_cap * 16);
-    space->list_bits = space->list_len + round256(lists * 4);
+    space->list_heads = space->lists + round256(lists * p.list_cap * 16);
+    space->tile_of = space->list_heads + round256(lists * 16);
+    space->list_bits = space->tile_of + (p.lists ? round256(*total * 8) : 0);
     space->total = space->list_bits + (p.row_tile >= 128 ? round256(lists * p.queries * p.list_words * 4) : 0);
     return LITEVLM_OK;
 }
@@ -1732,9 +1733,11 @@ litevlm_status_t litevlm_select_cache_attend_picked(litevlm_select_t h, int32_t 
     a.pick_queries = plan.queries;
     a.pick_chunk = plan.chunk;
     a.pick_chunks = plan.chunks;
+    a.pick_all = !plan.lists && total == batch;
     if (plan.lists) {
         a.lists = reinterpret_cast<int4*>(ws + space.lists);
-        a.list_len = reinterpret_cast<int32_t*>(ws + space.list_len);
+        a.list_heads = reinterpret_cast<int4*>(ws + space.list_heads);
+        a.tile_of = reinterpret_cast<int2*>(ws + space.tile_of);
         a.list_bits = plan.row_tile >= 128 ? reinterpret_cast<uint32_t*>(ws + space.list_bits) : nullptr;
         a.list_cap = plan.list_cap;
         a.list_words = plan.list_words;

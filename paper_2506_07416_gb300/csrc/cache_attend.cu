@@ -37,6 +37,7 @@
 // of contractions a score (no change), 16 warps of 128 registers for tiles of 16 rows (123 us of the third).
 
 #include <algorithm>
+#include <cstdlib>
 #include <type_traits>
 
 #include "cache_attend.cuh"
@@ -220,12 +221,14 @@ constexpr int kRingBytes = kAttWarps * kAttStages * 2 * Group<D>::kBytes;
 // which keeps addresses out of the lanes' registers: the sweep's 128 requests take 127 us
 // and not 135).
 // (CTAs of an SM as the plan of the split counts them.)
+enum class Picked { kNone, kQuery, kTile };
 // PICKED: the keys are those of picked pages, and a CTA's rows are those of one query, over the pages of its own list, or
 // of a tile of queries, over the list of the pages that any of them has (a key of a page that a row's query has not is as
 // masked); a CTA takes all of the list or a chunk of it.
-template <int D, int NT_, bool FP8, bool WHOLE, bool PICKED = false>
+template <int D, int NT_, bool FP8, bool WHOLE, Picked PICK = Picked::kNone>
 __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_kernel(const __grid_constant__ AttendArgs a)
 {
+    constexpr bool PICKED = PICK != Picked::kNone, LISTS = PICK == Picked::kTile;
     constexpr bool SINGLE = NT_ == 0;
     constexpr int NT = SINGLE ? 1 : NT_;
     using G = Group<D>;
@@ -250,12 +253,19 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
     const int64_t pick_list = pick_tile * a.cache.hkv + h;
     int listed = 0;  // keys of the list
     if constexpr (PICKED) {
-        qt = query_tile(a, pick_tile);
-        qt.b = uniform(qt.b), qt.i0 = uniform(qt.i0), qt.queries = uniform(qt.queries);
+        if constexpr (LISTS) {
+            const int4 head = __ldg(a.list_heads + pick_list);
+            qt = QueryTile{uniform(head.x), uniform(head.y), uniform(head.z)};
+            listed = uniform(head.w) << a.cache.page_shift;
+        } else {
+            // (as many queries as requests: one each, as no request has two)
+            qt.b = a.pick_all ? (int)pick_tile : uniform(find_request(a.q_off, a.batch, pick_tile));
+            qt.i0 = 0, qt.queries = 1;
+            listed = a.budget << a.cache.page_shift;
+        }
         if (qt.queries <= 0) return;
         b = qt.b;
-        listed = (a.lists ? __ldg(a.list_len + pick_list) : a.budget) << a.cache.page_shift;
-        chunk = a.lists ? list_chunk(listed, a.pick_chunks, 32) : a.pick_chunk;
+        chunk = LISTS ? list_chunk(listed, a.pick_chunks, 32) : a.pick_chunk;
         k0 = min((int)(blockIdx.x % a.pick_chunks) * chunk, listed);
     } else if (!WHOLE && a.slots > 0) {
         if (threadIdx.x < 32) {
@@ -300,7 +310,7 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
             next_have = 0u;
             if (j >= k1) return -1;
             int32_t p, o;
-            if (a.lists) {
+            if constexpr (LISTS) {
                 const int4 v = __ldg(a.lists + pick_list * a.list_cap + (j >> a.cache.page_shift));
                 p = v.x, o = v.y;
                 next_have = p >= 0 ? (uint32_t)v.z : 0u;
@@ -518,7 +528,7 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
     // a span of 32 keys from j0 on, two groups at a time (one after the other: 114 us where this takes 110, 1 to 8
     // queries of 32 requests, 32 / 8 heads); `there`: their keys that have a page; CHECK: some of
     // the rows do not see all of them
-    auto span_of = [&](const uint8_t* grp0, int j0, uint32_t there, auto check) {
+    auto span_of = [&](const uint8_t* grp0, int j0, uint32_t there, auto check, bool late = true) {
         constexpr bool CHECK = decltype(check)::value;
         float s[2][NT][4];
 #pragma unroll
@@ -530,7 +540,8 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     s[x][t][e] *= fac[t][e & 1];
-                    if (CHECK && (PICKED ? !(have_of[x] & my_bit[t][e & 1]) || pos_of[x] + g + 8 * (e >> 1) > vis[t][e & 1]
+                    if (CHECK && (PICKED ? !(have_of[x] & my_bit[t][e & 1]) ||
+                                               (late && pos_of[x] + g + 8 * (e >> 1) > vis[t][e & 1])
                                          : !(there >> (16 * x) & 1u) ||
                                                j0 + 16 * x + g + 8 * (e >> 1) > min(vis[t][e & 1], k1 - 1)))
                         s[x][t][e] = -INFINITY;
@@ -606,15 +617,26 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
                     w4[e][0] = *reinterpret_cast<const uint32_t*>(grp + G::kV + key * 32 + g * 4);
                     sc[e] = grp[G::kVs + key * 4 + g / 2];
                 }
-                if constexpr (CHECK) {
-                    const int at = PICKED ? pos_of[x] + key : j0 + 16 * x + key;
+                if constexpr (CHECK && !PICKED) {
+                    const int at = j0 + 16 * x + key;
                     // what lies behind the last key may be anything, a NaN scale among it
-                    if (PICKED ? at > last_see || have_of[x] == 0u : at >= k1) sc[e] = 0u;
+                    if (at >= k1) sc[e] = 0u;
                     // a NaN value must not reach the rows that do not see it (0 * NaN): put in at the end
-                    if ((at > all_see || (PICKED && have_of[x] != all_have)) && (sc[e] & 0x7Fu) == 0x7Fu) {
+                    if (at > all_see && (sc[e] & 0x7Fu) == 0x7Fu) {
                         sc[e] = 0u;
                         nan_value = true;
                     }
+                }
+                if (CHECK && PICKED && late && pos_of[x] + key > last_see) sc[e] = 0u;  // (behind the last key, as above)
+            }
+            if constexpr (CHECK && LISTS) {
+                // NaN among the scales, for rows that may not see it, as above
+                const uint32_t four = sc[0] | sc[1] << 8 | sc[2] << 16 | sc[3] << 24;
+                if (((four & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if ((sc[e] & 0x7Fu) == 0x7Fu) sc[e] = 0u;
+                    nan_value = true;
                 }
             }
             const __half2 sa = e4m3x2_value(sc[0] | (sc[1] << 8)), sb = e4m3x2_value(sc[2] | (sc[3] << 8));
@@ -686,7 +708,8 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
             }
         } else {
             if (all) span_of(span, j0, there, std::false_type{});
-            else span_of(span, j0, there, std::true_type{});
+            else span_of(span, j0, there, std::true_type{},
+                         !LISTS || __any_sync(0xffffffffu, now_have != 0u && now_pos + 15 > all_see));
         }
     }
     copy_async_wait<0>();
@@ -741,9 +764,9 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
             }
             const int rr = rt.row0 + row, i = rt.query(rr);
             const int64_t at = (int64_t)(q0 + i) * a.hq + h * a.group + rr - i * a.group;
-            if (PICKED && nan_value) {
+            if (LISTS && nan_value) {
                 for (int j = k0; j < k1; ++j) {
-                    const int4 v = a.lists ? __ldg(a.lists + pick_list * a.list_cap + (j >> a.cache.page_shift)) : make_int4(-1, 0, 0, 0);
+                    const int4 v = __ldg(a.lists + pick_list * a.list_cap + (j >> a.cache.page_shift));
                     const int slot = j & ((1 << a.cache.page_shift) - 1);
                     if (v.x < 0 || !((uint32_t)v.z >> (i - qt.i0) & 1u) || (v.y << a.cache.page_shift) + slot > rt.last0 + i)
                         continue;
@@ -1135,8 +1158,39 @@ __global__ void __launch_bounds__(kListThreads) picked_list_kernel(const __grid_
     griddep_launch_dependents();
     const int64_t list = blockIdx.x, tile = list / a.cache.hkv;
     const int h = (int)(list - tile * a.cache.hkv);
-    const QueryTile qt = query_tile(a, tile);
-    if (qt.queries <= 0) return;
+    // the tile's request: the requests' tiles one after the other, 256 requests at a time
+    __shared__ int found_s[2];
+    if (tid == 0) found_s[0] = -1;
+    int64_t tiles_before = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += kListThreads) {
+        const int b = b0 + tid;
+        const int n = b < a.batch ? tiles_of(__ldg(a.q_off + b + 1) - __ldg(a.q_off + b), a.pick_queries) : 0;
+        int sum = n;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, sum, d);
+            if (lane >= d) sum += y;
+        }
+        if (lane == 31) warp_s[warp] = sum;
+        __syncthreads();
+        int64_t at = tiles_before + sum - n;
+#pragma unroll
+        for (int w = 0; w < kListThreads / 32; ++w) {
+            if (w < warp) at += warp_s[w];
+            tiles_before += warp_s[w];
+        }
+        if (tile >= at && tile < at + n) found_s[0] = b, found_s[1] = (int)(tile - at) * a.pick_queries;
+        __syncthreads();
+        if (found_s[0] >= 0) break;
+    }
+    QueryTile qt;
+    qt.b = found_s[0];
+    if (qt.b < 0) {
+        if (tid == 0) a.list_heads[list] = make_int4(0, 0, 0, 0);
+        return;
+    }
+    qt.i0 = found_s[1];
+    qt.queries = min(a.pick_queries, __ldg(a.q_off + qt.b + 1) - __ldg(a.q_off + qt.b) - qt.i0);
     bool bad;
     const int len = cache_len(__ldg(a.lens + qt.b), a.limit, bad);
     if (bad && tid == 0) atomicOr(a.err, kErrBounds);
@@ -1210,7 +1264,8 @@ __global__ void __launch_bounds__(kListThreads) picked_list_kernel(const __grid_
         base = all;
         __syncthreads();
     }
-    if (tid == 0) a.list_len[list] = base;
+    if (tid == 0) a.list_heads[list] = make_int4(qt.b, qt.i0, qt.queries, base);
+    if (h == 0 && tid < qt.queries) a.tile_of[q0 + qt.i0 + tid] = make_int2((int)tile, tid);
 }
 
 // The chunks of a tile's list joined, a row (query and head) a warp: chunk x of a tile has its sums at
@@ -1228,9 +1283,9 @@ __global__ void __launch_bounds__(kAttThreads) picked_join_kernel(const __grid_c
     int64_t tile = r;
     int in = hq % a.group;
     if (a.lists) {
-        const int b = find_request(a.q_off, a.batch, r), q0 = __ldg(a.q_off + b), i = (int)(r - q0);
-        tile = query_tile_at(q0, b, a.pick_queries) + i / a.pick_queries;
-        in += i % a.pick_queries * a.group;
+        const int2 v = __ldg(a.tile_of + r);
+        tile = v.x;
+        in += v.y * a.group;
     }
     const int64_t from = (tile * a.pick_chunks * a.cache.hkv + h) * a.max_rows + in, step = (int64_t)a.cache.hkv * a.max_rows;
     float M = kNoRef, L = 0.f, O[D / 32];
@@ -1292,9 +1347,12 @@ cudaError_t launch_picked(const AttendArgs& a, const PickedPlan& plan, int64_t q
         cfg.gridDim = dim3((unsigned)(plan.tiles * plan.chunks), (unsigned)(subs * a.cache.hkv), 1);
         cfg.blockDim = dim3(kAttThreads, 1, 1);
         cfg.dynamicSmemBytes = kRingBytes<D>;
-        auto kern = a.group == 1 && !plan.lists ? attend_split_kernel<D, 0, FP8, false, true>
-                                                : (plan.row_tile == 8 ? attend_split_kernel<D, 1, FP8, false, true>
-                                                                      : attend_split_kernel<D, 2, FP8, false, true>);
+        constexpr Picked Q = Picked::kQuery, T = Picked::kTile;
+        auto kern = plan.lists ? (plan.row_tile == 8 ? attend_split_kernel<D, 1, FP8, false, T>
+                                                     : attend_split_kernel<D, 2, FP8, false, T>)
+                    : a.group == 1 ? attend_split_kernel<D, 0, FP8, false, Q>
+                                   : (plan.row_tile == 8 ? attend_split_kernel<D, 1, FP8, false, Q>
+                                                         : attend_split_kernel<D, 2, FP8, false, Q>);
         e = cudaLaunchKernelEx(&cfg, kern, a);
     }
     if (e != cudaSuccess) return e;
@@ -1324,12 +1382,13 @@ PickedPlan plan_attend_picked(int batch, int hkv, int group, const int32_t* q_of
     for (int b = 0; b < batch; ++b) max_t = std::max(max_t, q_off[b + 1] - q_off[b]);
     const int64_t max_rows = (int64_t)max_t * group;
     p.lists = max_t > 1;
-    p.row_tile = p.lists ? attend_row_tile(max_rows) : (group <= 8 ? 8 : 16);
+    static const int few = getenv("FEW") ? atoi(getenv("FEW")) : 16;
+    p.row_tile = p.lists ? (max_rows <= 8 ? 8 : max_rows <= few ? 16 : max_rows <= 128 ? 128 : 256) : (group <= 8 ? 8 : 16);
     p.queries = p.lists ? std::max(1, p.row_tile / group) : 1;
-    int64_t keys = (int64_t)budget << page_shift, items = 0;
+    int64_t keys = (int64_t)budget << page_shift;
     const int64_t subs = ((int64_t)p.queries * group + p.row_tile - 1) / p.row_tile;
-    for (int b = 0; b < batch; ++b) items += (int64_t)((q_off[b + 1] - q_off[b] + p.queries - 1) / p.queries) * hkv * subs;
-    p.tiles = p.lists ? query_tile_at(q_off[batch], batch, p.queries) : q_off[batch];
+    for (int b = 0; b < batch; ++b) p.tiles += tiles_of(q_off[b + 1] - q_off[b], p.queries);
+    const int64_t items = p.tiles * hkv * subs;
     if (p.lists) {
         p.list_cap = (int32_t)std::min<int64_t>(width, (int64_t)p.queries * budget);
         p.list_words = (p.list_cap + 31) / 32;

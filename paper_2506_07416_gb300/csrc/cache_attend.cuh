@@ -123,35 +123,10 @@ __device__ __forceinline__ int find_request(const int32_t* off, int batch, int64
 }
 
 // A tile of queries, of attention over picked pages: its request, its first query there, and how many it has (0: the tile
-// is none's). By a warp.
+// is none's).
 struct QueryTile {
     int b, i0, queries;
 };
-__device__ __forceinline__ QueryTile query_tile(const AttendArgs& a, int64_t tile)
-{
-    QueryTile q;
-    if (!a.lists) {
-        q.b = find_request(a.q_off, a.batch, tile);
-        q.i0 = (int)(tile - __ldg(a.q_off + q.b));
-        q.queries = 1;
-        return q;
-    }
-    const int lane = threadIdx.x & 31;
-    int lo = 0, hi = a.batch;
-    while (hi - lo > 1) {
-        const int step = (hi - lo + 31) / 32, at = lo + (lane + 1) * step;
-        const uint32_t m =
-            __ballot_sync(0xffffffffu, at < hi && query_tile_at(__ldg(a.q_off + at), at, a.pick_queries) <= tile);
-        lo += __popc(m) * step;
-        hi = min(hi, lo + step);
-    }
-    q.b = lo;
-    const int q0 = __ldg(a.q_off + lo), t = __ldg(a.q_off + lo + 1) - q0;
-    const int64_t i0 = (tile - query_tile_at(q0, lo, a.pick_queries)) * a.pick_queries;
-    q.i0 = (int)min(i0, (int64_t)t);
-    q.queries = min(a.pick_queries, t - q.i0);
-    return q;
-}
 // Keys of a chunk where a tile's list has n of them: a multiple of `unit`.
 __device__ __forceinline__ int list_chunk(int n, int chunks, int unit)
 {

@@ -32,8 +32,8 @@ LVS_HD int64_t tile_at(int64_t rows, int64_t b) { return rows / 128 + b; }
 // places follow the last one's: n tokens touch at most floor(n / page) + 2 pages. Of the batch's end: the places of all.
 LVS_HD int64_t page_at(int64_t rows, int64_t b, int32_t page_shift) { return (rows >> page_shift) + 2 * b; }
 
-// The same of tiles of `per` queries: a request of n queries has at most floor((rows + n) / per) - floor(rows / per) + 1.
-LVS_HD int64_t query_tile_at(int64_t rows, int64_t b, int32_t per) { return rows / per + b; }
+// Tiles of `per` queries of a request with n.
+LVS_HD int32_t tiles_of(int32_t n, int32_t per) { return n <= 0 ? 0 : (n - 1) / per + 1; }
 
 // Tokens of a request that the kernels may touch: its length cut to
 // [0, limit]. `bad` tells that the length was outside.

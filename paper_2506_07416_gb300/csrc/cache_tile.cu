@@ -226,11 +226,11 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
     const int64_t pick_list = pick_tile * a.cache.hkv + h;
     int listed = 0;  // keys of the list
     if constexpr (PICKED) {
-        qt = query_tile(a, pick_tile);
-        qt.b = uniform(qt.b), qt.i0 = uniform(qt.i0), qt.queries = uniform(qt.queries);
+        const int4 head = __ldg(a.list_heads + pick_list);
+        qt = QueryTile{uniform(head.x), uniform(head.y), uniform(head.z)};
         if (qt.queries <= 0) return;
         b = qt.b;
-        listed = uniform(__ldg(a.list_len + pick_list) << a.cache.page_shift);
+        listed = uniform(head.w) << a.cache.page_shift;
         chunk = list_chunk(listed, a.pick_chunks, kTileKeys);
         k0 = min((int)(blockIdx.x % a.pick_chunks) * chunk, listed);
     } else if (a.slots > 0) {

@@ -188,7 +188,9 @@ struct AttendArgs {
     int32_t pick_chunk;       // keys of a chunk (without lists: of a query's own pages)
     int4* lists;              // [tiles][hkv][list_cap] pages of a tile's queries: in the pool, of the request, a bit for each
                               // query that has it (up to 16 rows); null: a tile is one query
-    int32_t* list_len;        // [tiles][hkv]
+    int4* list_heads;         // [tiles][hkv] a tile's request, first query there, queries (0: none) and the list's pages
+    int2* tile_of;            // [rows] tile of each query and its place there
+    int32_t pick_all;         // every request has one query
     uint32_t* list_bits;      // [tiles][hkv][pick_queries][list_words] the pages of each query, a bit each (128 rows and more)
     int32_t list_cap, list_words;
     int32_t* err;
@@ -210,7 +212,7 @@ struct PickedPlan {
     int32_t row_tile;         // rows of a CTA: 8, 16, 128 or 256
     int32_t queries;          // queries of a tile
     bool lists;               // the queries of a tile share a list
-    int64_t tiles;            // query_tile_at of the batch's end (without lists: the queries)
+    int64_t tiles;            // of all requests (without lists: the queries)
     int32_t chunk, chunks, list_cap, list_words;
 };
 PickedPlan plan_attend_picked(int batch, int hkv, int group, const int32_t* q_off, int page_shift, int width, int budget,
