@@ -1580,7 +1580,7 @@ litevlm_status_t litevlm_select_cache_bounds(litevlm_select_t h, int32_t batch, 
         return fail(h, LITEVLM_ERR_UNSUPPORTED, "the new tokens' pages x key heads exceed the grid");
     const OnDevice on(h->device);
     cudaError_t e = on.e;
-    if (e == cudaSuccess) e = lvs::launch_cache_bounds(a, h->cfg.head_dim, (cudaStream_t)stream);
+    if (e == cudaSuccess) e = lvs::launch_cache_bounds(a, h->cfg.head_dim, h->num_sms, (cudaStream_t)stream);
     if (e != cudaSuccess) return cuda_fail(h, e, "cache_bounds launch");
     h->last_launches = 1;
     return LITEVLM_OK;
@@ -1652,6 +1652,7 @@ litevlm_status_t litevlm_select_cache_pick(litevlm_select_t h, int32_t batch, co
     a.budget = budget;
     a.sink = sink;
     a.recent = recent;
+    a.single = max_t == 1 && a.rows == batch;
     a.keys = static_cast<uint32_t*>(workspace);
     a.picked = picked;
     a.err = h->err_d;

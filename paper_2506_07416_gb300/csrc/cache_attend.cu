@@ -37,7 +37,7 @@
 // of contractions a score (no change), 16 warps of 128 registers for tiles of 16 rows (123 us of the third).
 
 #include <algorithm>
-#include <cstdlib>
+#include <cmath>
 #include <type_traits>
 
 #include "cache_attend.cuh"
@@ -1372,8 +1372,13 @@ cudaError_t launch_picked(const AttendArgs& a, const PickedPlan& plan, int64_t q
 
 // A call of single tokens has a tile for each query, with the pages of its own list. Else neighbouring queries of a
 // request, which mostly have the same pages, share a tile of up to 16, 128 or 256 rows and read its pages once.
+// Tiles of 128 rows from 17 rows of the longest request on: 24 and 32 rows of 32 requests, 32 / 8 heads, 48 pages of 32,
+// 85 and 90 us where tiles of 16 take 158 and 174; 12 and 16 rows 76 and 82 with either.
 // The lists are split where the tiles alone leave the GPU's places empty: as for whole requests, n chunks take
-// rounds / n of the list and the writing and joining of a chunk's sums. A shared list is taken to be twice a query's.
+// rounds / n of the list and the writing and joining of a chunk's sums. A shared list is taken to grow by half of a
+// query's own for each doubling of the queries: of 32 pages each, picked as neighbours mostly agree on, 18 queries
+// have 117 and 36 124. A chunk of a prompt (777 to 1024 queries of two requests, 28 / 4 heads, 32 pages of 64): whole
+// 234 us, two chunks 210, three 243.
 PickedPlan plan_attend_picked(int batch, int hkv, int group, const int32_t* q_off, int page_shift, int width, int budget,
                               int num_sms)
 {
@@ -1382,8 +1387,7 @@ PickedPlan plan_attend_picked(int batch, int hkv, int group, const int32_t* q_of
     for (int b = 0; b < batch; ++b) max_t = std::max(max_t, q_off[b + 1] - q_off[b]);
     const int64_t max_rows = (int64_t)max_t * group;
     p.lists = max_t > 1;
-    static const int few = getenv("FEW") ? atoi(getenv("FEW")) : 16;
-    p.row_tile = p.lists ? (max_rows <= 8 ? 8 : max_rows <= few ? 16 : max_rows <= 128 ? 128 : 256) : (group <= 8 ? 8 : 16);
+    p.row_tile = p.lists ? (max_rows <= 8 ? 8 : (max_rows <= 16 ? 16 : (max_rows <= 128 ? 128 : 256))) : (group <= 8 ? 8 : 16);
     p.queries = p.lists ? std::max(1, p.row_tile / group) : 1;
     int64_t keys = (int64_t)budget << page_shift;
     const int64_t subs = ((int64_t)p.queries * group + p.row_tile - 1) / p.row_tile;
@@ -1392,7 +1396,7 @@ PickedPlan plan_attend_picked(int batch, int hkv, int group, const int32_t* q_of
     if (p.lists) {
         p.list_cap = (int32_t)std::min<int64_t>(width, (int64_t)p.queries * budget);
         p.list_words = (p.list_cap + 31) / 32;
-        if (p.queries > 1) keys = std::min<int64_t>(2 * keys, (int64_t)p.list_cap << page_shift);
+        keys = std::min((int64_t)((double)keys * (1.0 + std::log2((double)p.queries) / 2.0)), (int64_t)p.list_cap << page_shift);
     }
     const bool many = p.row_tile >= 128;
     const int64_t places = (int64_t)num_sms * (p.row_tile == 256 ? 1 : (p.row_tile == 128 ? 2 : (p.row_tile == 16 ? 3 : 4)));
@@ -1405,7 +1409,7 @@ PickedPlan plan_attend_picked(int batch, int hkv, int group, const int32_t* q_of
         for (int64_t n = 1; n <= std::min<int64_t>(units, 8); ++n) {
             const double whole = (double)((items * n + places - 1) / places);
             const double r = many ? (whole + (double)(items * n) / (double)places) / 2.0 : whole;
-            const double more = (many ? 700.0 : 0.0) + (n > 1 ? (many ? 2.3 : 1.25) * p.row_tile : 0.0);
+            const double more = (many ? 250.0 : 0.0) + (n > 1 ? (many ? 0.75 : 1.25) * p.row_tile : 0.0);
             const double c = r / (double)n + r * more / (double)std::max<int64_t>(keys, 1);
             if (c < cost) cost = c, best = n;
         }

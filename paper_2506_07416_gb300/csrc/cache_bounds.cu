@@ -49,29 +49,32 @@ __device__ __forceinline__ int halve(__half2* top, __half2* low, int lane)
 }
 
 template <int D>
-__global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(const __grid_constant__ BoundsArgs a)
+__global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(const __grid_constant__ BoundsArgs a, int heads)
 {
     constexpr int LANES = D / 32;     // lanes of a row
     constexpr int ROWS = 32 / LANES;  // rows of a warp at a time
     constexpr int PAIRS = 16;         // half pairs of a lane's 32 channels
     const int lane = threadIdx.x & 31;
     const int64_t unit = ((int64_t)blockIdx.x * kBoundsThreads + threadIdx.x) >> 5;
-    const int64_t place = unit / a.cache.hkv;
-    const int h = (int)(unit - place * a.cache.hkv);
+    const int parts = (a.cache.hkv + heads - 1) / heads;
+    const int64_t place = unit / parts;
+    const int h0 = (int)(unit - place * parts) * heads, h1 = min(a.cache.hkv, h0 + heads);
     griddep_wait();
     griddep_launch_dependents();
     if (place >= a.places) return;
-    // the request: the last whose first place is not behind the unit's
+    // the request: the last whose first place is not behind the unit's, 32 at a time
     int lo = 0, hi = a.batch;
     while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (page_at(__ldg(a.off + mid), mid, a.cache.page_shift) <= place) lo = mid;
-        else hi = mid;
+        const int step = (hi - lo + 31) / 32, at = lo + (lane + 1) * step;
+        const uint32_t m =
+            __ballot_sync(0xffffffffu, at < hi && page_at(__ldg(a.off + at), at, a.cache.page_shift) <= place);
+        lo += __popc(m) * step;
+        hi = min(hi, lo + step);
     }
     const int q0 = __ldg(a.off + lo), t = __ldg(a.off + lo + 1) - q0;
-    if (t <= 0) return;
     bool bad;
     const int len = cache_len(__ldg(a.lens + lo), a.limit, bad);
+    if (t <= 0) return;
     if ((bad || t > len) && lane == 0) atomicOr(a.err, kErrBounds);
     const int64_t o = (max(len - t, 0) >> a.cache.page_shift) + (place - page_at(q0, lo, a.cache.page_shift));
     const int64_t first = o << a.cache.page_shift;
@@ -82,15 +85,18 @@ __global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(const __grid_con
         return;
     }
     const int rows = min(1 << a.cache.page_shift, len - (int)first);
-    const int64_t at = cache_row(page, a.cache.hkv, h, a.cache.page_shift, 0);
     const int c = lane % LANES, g = lane / LANES;
+#pragma unroll 1
+    for (int h = h0; h < h1; ++h) {
+    const int64_t at = cache_row(page, a.cache.hkv, h, a.cache.page_shift, 0);
     const uint4* codes = reinterpret_cast<const uint4*>(a.cache.codes[0] + at * (D / 2)) + c;
     const uint16_t* scales = reinterpret_cast<const uint16_t*>(a.cache.scales[0] + at * (D / 16)) + c;
     __half2 top[PAIRS], low[PAIRS];
     const __half2 inf = bits_h2(0x7C007C00u), ninf = bits_h2(0xFC00FC00u);
 #pragma unroll
     for (int i = 0; i < PAIRS; ++i) top[i] = ninf, low[i] = inf;
-    constexpr int U = 2;
+    constexpr int U = 4;
+#pragma unroll 1
     for (int r0 = 0; r0 < rows; r0 += ROWS * U) {
         uint4 w[U];
         uint32_t s[U];
@@ -102,6 +108,7 @@ __global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(const __grid_con
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
+            if (r0 + u * ROWS >= rows) break;
             const uint32_t words[4] = {w[u].x, w[u].y, w[u].z, w[u].w};
             const __half2 sc[2] = {block_scale(s[u]), block_scale(s[u] >> 8)};
 #pragma unroll
@@ -149,14 +156,18 @@ __global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(const __grid_con
         *reinterpret_cast<uint16_t*>(to + D) = (uint16_t)cl;
     }
     if (lane == 0) a.exps[(int64_t)page * a.cache.hkv + h] = (int8_t)e;
+    }
 }
 
 }  // namespace
 
-cudaError_t launch_cache_bounds(const BoundsArgs& a, int head_dim, cudaStream_t stream)
+cudaError_t launch_cache_bounds(const BoundsArgs& a, int head_dim, int num_sms, cudaStream_t stream)
 {
-    const int64_t warps = a.places * a.cache.hkv;
-    if (warps <= 0) return cudaSuccess;
+    if (a.places <= 0) return cudaSuccess;
+    // heads of a warp, which finds its page once for them: more where the pages alone fill the GPU
+    int heads = 1;
+    while (heads < a.cache.hkv && a.places * a.cache.hkv / (2 * heads) >= (int64_t)num_sms * 128) heads *= 2;
+    const int64_t warps = a.places * ((a.cache.hkv + heads - 1) / heads);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((warps * 32 + kBoundsThreads - 1) / kBoundsThreads), 1, 1);
     cfg.blockDim = dim3(kBoundsThreads, 1, 1);
@@ -164,7 +175,7 @@ cudaError_t launch_cache_bounds(const BoundsArgs& a, int head_dim, cudaStream_t 
     cudaLaunchAttribute attr[1] = {pdl_attribute()};
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, head_dim == 128 ? bounds_kernel<128> : bounds_kernel<64>, a);
+    return cudaLaunchKernelEx(&cfg, head_dim == 128 ? bounds_kernel<128> : bounds_kernel<64>, a, heads);
 }
 
 }  // namespace lvs

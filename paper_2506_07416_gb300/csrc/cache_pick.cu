@@ -87,139 +87,222 @@ __device__ __forceinline__ void query_values(const uint4& v, float (&x)[FP8 ? 16
     }
 }
 
+// A lane's codes of two pages as they are in memory, their units and whether the pool has them.
+template <int D>
+struct PageCodes {
+    uint4 w[2][2 * D / 64];
+    float unit[2];
+    bool there[2];
+
+    // pages p[0] and p[1] of the pool (-1: none): channels [c * 16, c * 16 + 16) of each 64
+    __device__ __forceinline__ void load(const PickArgs& a, const int32_t (&p)[2], int h, int c)
+    {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            there[e] = p[e] >= 0;
+            const int64_t row = (int64_t)max(p[e], 0) * a.hkv + h;
+            const int x = min(max((int)__ldg(a.exps + row), -100), 100);
+            unit[e] = __uint_as_float((uint32_t)(127 + x) << 23);
+            const uint4* from = reinterpret_cast<const uint4*>(a.codes + row * 2 * D) + c;
+#pragma unroll
+            for (int k = 0; k < 2 * D / 64; ++k) w[e][k] = __ldg(from + k * 4);
+        }
+    }
+    // the A operand of contraction k
+    __device__ __forceinline__ void operand(int k, uint32_t (&f)[4]) const
+    {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const uint4 v = w[e][k / 4];
+            s8x4_value(k % 4 == 0 ? v.x : (k % 4 == 1 ? v.y : (k % 4 == 2 ? v.z : v.w)), f[e], f[2 + e]);
+        }
+    }
+};
+
+// The whole numbers of a query (of key head h) into the columns' tiles, by the lanes of `warps` warps, `at` this one's
+// place among them; zeros where !real. The largest magnitude is found over `max_s` where they are more than one.
 template <int D, bool FP8>
-__global__ void __launch_bounds__(kScoreThreads) pick_score_kernel(const __grid_constant__ PickArgs a, int blocks)
+__device__ __forceinline__ void stage_query(const PickArgs& a, int64_t row, int h, bool real, int padded, int col0,
+                                            uint2* frag_s, int at, int warps, float* max_s)
+{
+    constexpr int STEPS = 2 * D / 16, PARTS = D * (FP8 ? 1 : 2) / 16, PER = 32 / PARTS, E = FP8 ? 16 : 8, U = 4;
+    const int lane = threadIdx.x & 31, sub = lane % PARTS, first = at * PER + lane / PARTS, step = warps * PER;
+    const uint8_t* from =
+        static_cast<const uint8_t*>(a.q) + (row * a.q_stride + (int64_t)h * a.group * D) * (FP8 ? 1 : 2);
+    auto load = [&](int y) { return __ldg(reinterpret_cast<const uint4*>(from + (int64_t)y * D * (FP8 ? 1 : 2)) + sub); };
+    uint4 kept[U];  // the first rows stay in registers between the two passes
+    float top = 0.f;
+#pragma unroll
+    for (int u = 0; u < U; ++u) kept[u] = real ? load(min(first + u * step, a.group - 1)) : make_uint4(0u, 0u, 0u, 0u);
+    auto reach = [&](const uint4& w) {
+        float v[E];
+        query_values<FP8>(w, v);
+#pragma unroll
+        for (int e = 0; e < E; ++e) top = fmaxf(top, fabsf(v[e]));
+    };
+#pragma unroll
+    for (int u = 0; u < U; ++u) reach(kept[u]);
+    if (real)
+        for (int y = first + U * step; y < a.group; y += step) reach(load(y));
+    top = warp_max_f32(top);
+    if (warps > 1) {
+        if (lane == 0) max_s[at] = top;
+        __syncthreads();
+        for (int w = 0; w < warps; ++w) top = fmaxf(top, max_s[w]);
+    }
+    // top = f * 2^p, f in [1/2, 1); the unit is 2^(p - 7)
+    const int p = max((int)(__float_as_uint(top) >> 23) - 126, -119);
+    const float up = __uint_as_float((uint32_t)(127 + 7 - p) << 23);
+    auto put = [&](const uint4& w, int y) {
+        float v[E];
+        query_values<FP8>(w, v);
+        const int col = col0 + y, n = col & 7;
+#pragma unroll
+        for (int e = 0; e < E; e += 4) {
+            float r[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r[i] = fminf(fmaxf(rintf(v[e + i] * up), -127.f), 127.f);
+            // channels [ch, ch + 4): word (ch % 16) / 4 of lane (ch / 16) % 4 and load ch / 64
+            const int ch = sub * E + e, cc = ch / 16 % 4, k = ch / 64 * 4 + ch % 16 / 4;
+            uint2* to = frag_s + ((col >> 3) * STEPS + k) * 32 + n * 4 + cc;
+            const auto pack = [](float s, float u) { return h2_bits(__floats2half2_rn(s, u)); };
+            to[0] = make_uint2(pack(fmaxf(r[0], 0.f), fmaxf(r[1], 0.f)), pack(fmaxf(r[2], 0.f), fmaxf(r[3], 0.f)));
+            to[STEPS / 2 * 32] =
+                make_uint2(pack(fminf(r[0], 0.f), fminf(r[1], 0.f)), pack(fminf(r[2], 0.f), fminf(r[3], 0.f)));
+        }
+    };
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (first + u * step < padded) put(kept[u], first + u * step);  // (behind the last head: that one again)
+    for (int y = first + U * step; y < padded; y += step)
+        put(real ? load(min(y, a.group - 1)) : make_uint4(0u, 0u, 0u, 0u), y);
+}
+
+// MULTI: more than one tile of columns (some queries); else one query, or a few of few heads.
+template <int D, bool FP8, bool MULTI>
+__global__ void __launch_bounds__(kScoreThreads, MULTI ? 3 : 4) pick_score_kernel(const __grid_constant__ PickArgs a, int blocks)
 {
     constexpr int STEPS = 2 * D / 16;                       // contractions of 16 channels
-    constexpr int WORDS = D / 16;                           // words of four channels of a lane, of hi and lo each
+    constexpr int GROUP = MULTI ? 4 : 1;                    // tiles of columns at a time: chains that do not wait for one another
     extern __shared__ __align__(16) uint2 frag_s[];         // [tile][step][lane]
+    __shared__ float max_s[kScoreThreads / 32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
     const int h = blockIdx.y % a.hkv, part = blockIdx.y / a.hkv, b = blockIdx.z;
     griddep_wait();
     griddep_launch_dependents();
     const int padded = padded_group(a.group), per = score_queries(padded);
     const int q0 = __ldg(a.off + b), t = __ldg(a.off + b + 1) - q0;
-    const int i0 = part * per, queries = min(per, t - i0);
-    if (queries <= 0) return;
     bool bad;
     const int len = cache_len(__ldg(a.lens + b), a.limit, bad);
+    const int i0 = part * per, queries = min(per, t - i0);
+    if (queries <= 0) return;
     if (bad && tid == 0) atomicOr(a.err, kErrBounds);
     // pages that the last of these queries sees; the select kernel reads no scores where all may be picked
     const int last = len - t + i0 + queries - 1;
     if (last < 0) return;
     const int pages = (last >> a.page_shift) + 1;
-    if (pages <= a.budget) return;
+    const int step = blocks * kScorePages;
+    int base = blockIdx.x * kScorePages + warp * 16;
+    if (pages <= a.budget || blockIdx.x * kScorePages >= pages) return;
     const int tiles = (queries * padded + 7) / 8;
-
-    // ---- queries into whole numbers, a warp each: the parts that multiply hi and lo in the lanes' order
-    {
-        constexpr int PARTS = D * (FP8 ? 1 : 2) / 16, PER = 32 / PARTS, E = FP8 ? 16 : 8;
-        const int sub = lane % PARTS, row = lane / PARTS;
-        for (int x = warp; x < tiles * 8 / padded; x += kScoreThreads / 32) {  // (zeros behind the last query)
-            const bool real = x < queries;
-            const uint8_t* from = static_cast<const uint8_t*>(a.q) +
-                                  ((int64_t)(q0 + i0 + (real ? x : 0)) * a.q_stride + (int64_t)h * a.group * D) * (FP8 ? 1 : 2);
-            float top = 0.f;
-            for (int y = row; y < a.group; y += PER) {
-                float v[E];
-                query_values<FP8>(__ldg(reinterpret_cast<const uint4*>(from + (int64_t)y * D * (FP8 ? 1 : 2)) + sub), v);
+    // a lane's pages are found two steps ahead, their codes loaded one step ahead
+    auto find = [&](int from, int32_t (&p)[2]) {
 #pragma unroll
-                for (int e = 0; e < E; ++e) top = fmaxf(top, fabsf(v[e]));
-            }
-            top = warp_max_f32(top);
-            // top = f * 2^p, f in [1/2, 1); the unit is 2^(p - 7)
-            const int p = max((int)(__float_as_uint(top) >> 23) - 126, -119);
-            const float up = __uint_as_float((uint32_t)(127 + 7 - p) << 23);
-            for (int y0 = 0; y0 < padded; y0 += PER) {
-                const int y = y0 + row;
-                if (y >= padded) break;
-                float v[E];
-                query_values<FP8>(
-                    __ldg(reinterpret_cast<const uint4*>(from + (int64_t)min(y, a.group - 1) * D * (FP8 ? 1 : 2)) + sub), v);
-                const int col = x * padded + y, n = col & 7;
-#pragma unroll
-                for (int e = 0; e < E; e += 4) {
-                    float r[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        r[i] = real ? fminf(fmaxf(rintf(v[e + i] * up), -127.f), 127.f) : 0.f;
-                    // channels [ch, ch + 4): word (ch % 16) / 4 of lane (ch / 16) % 4 and load ch / 64 (D = 64: one load)
-                    const int ch = sub * E + e, load = ch / 64, cc = ch / 16 % 4, step = load * 4 + ch % 16 / 4;
-                    uint2* to = frag_s + ((int64_t)(col >> 3) * STEPS + step) * 32 + n * 4 + cc;
-                    const auto pack = [](float s, float u) { return h2_bits(__floats2half2_rn(s, u)); };
-                    to[0] = make_uint2(pack(fmaxf(r[0], 0.f), fmaxf(r[1], 0.f)), pack(fmaxf(r[2], 0.f), fmaxf(r[3], 0.f)));
-                    to[STEPS / 2 * 32] =
-                        make_uint2(pack(fminf(r[0], 0.f), fminf(r[1], 0.f)), pack(fminf(r[2], 0.f), fminf(r[3], 0.f)));
-                }
+        for (int e = 0; e < 2; ++e) {
+            const int64_t o = from + g + 8 * e;
+            p[e] = -1;
+            if (o < pages) {
+                p[e] = cache_page(a.table, a.width, a.num_pages, a.page_shift, b, o << a.page_shift);
+                if (p[e] < 0 && c == 0) atomicOr(a.err, kErrBounds);
             }
         }
+    };
+    int32_t page[2];
+    PageCodes<D> next;
+    find(base, page);
+    next.load(a, page, h, c);
+    find(base + step, page);
+
+    if (!MULTI && queries == 1) {
+        stage_query<D, FP8>(a, q0 + i0, h, true, padded, 0, frag_s, warp, kScoreThreads / 32, max_s);
+        if (padded < 8 && tid < 32)  // (the tile's other columns)
+            for (int k = 0; k < STEPS; ++k)
+                if (lane >> 2 >= padded) frag_s[k * 32 + lane] = make_uint2(0u, 0u);
+    } else {
+        for (int x = warp; x < tiles * 8 / padded; x += kScoreThreads / 32)  // (zeros behind the last query)
+            stage_query<D, FP8>(a, q0 + i0 + min(x, queries - 1), h, x < queries, padded, x * padded, frag_s, 0, 1, max_s);
     }
     __syncthreads();
 
-    for (int base = blockIdx.x * kScorePages + warp * 16; base < pages; base += blocks * kScorePages) {
-        // ---- 16 pages: lane (g, c) has channels [c * 16, c * 16 + 16) of each 64, of rows g and g + 8
-        uint32_t f[STEPS][4];
-        float unit[2];
-        bool there[2];
+    for (; base < pages; base += step) {
+        const PageCodes<D> now = next;
+        uint32_t f[MULTI ? STEPS : 1][4];
+        if constexpr (MULTI) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int64_t o = base + g + 8 * e;
-            int32_t page = -1;
-            if (o < pages) {
-                page = cache_page(a.table, a.width, a.num_pages, a.page_shift, b, o << a.page_shift);
-                if (page < 0 && c == 0) atomicOr(a.err, kErrBounds);
-            }
-            there[e] = page >= 0;
-            const int64_t row = (int64_t)max(page, 0) * a.hkv + h;
-            const int x = min(max((int)__ldg(a.exps + row), -100), 100);
-            unit[e] = __uint_as_float((uint32_t)(127 + x) << 23);
-            const uint4* from = reinterpret_cast<const uint4*>(a.codes + row * 2 * D) + c;
-#pragma unroll
-            for (int k = 0; k < 2 * D / 64; ++k) {  // (all loads before the first use)
-                const uint4 w = __ldg(from + k * 4);
-                s8x4_value(w.x, f[4 * k][e], f[4 * k][2 + e]);
-                s8x4_value(w.y, f[4 * k + 1][e], f[4 * k + 1][2 + e]);
-                s8x4_value(w.z, f[4 * k + 2][e], f[4 * k + 2][2 + e]);
-                s8x4_value(w.w, f[4 * k + 3][e], f[4 * k + 3][2 + e]);
-            }
+            for (int k = 0; k < STEPS; ++k) now.operand(k, f[k]);
         }
-        static_assert(WORDS * 2 == STEPS, "a word of four channels is a lane's part of a contraction");
+        if (base + step < pages) {
+            next.load(a, page, h, c);
+            find(base + 2 * step, page);
+        }
         float best[2] = {-INFINITY, -INFINITY};  // over the tiles of a query of more than eight heads
-        for (int x = 0; x < tiles; ++x) {
-            float d[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int x0 = 0; x0 < tiles; x0 += GROUP) {
+            float d[GROUP][4], d2[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int k = 0; k < STEPS; ++k) mma16816(d, f[k], frag_s[((int64_t)x * STEPS + k) * 32 + lane]);
-            // d: page g of columns 2c and 2c + 1, page g + 8 of both
-            auto put = [&](int i, int e, float s) {  // score of the CTA's query i and page g + 8 e
-                const int64_t o = base + g + 8 * e;
-                if (i < queries && o < pages)
-                    a.keys[((int64_t)(q0 + i0 + i) * a.hkv + h) * a.key_stride + o] =
-                        (e ? there[1] : there[0]) ? score_key(s * (e ? unit[1] : unit[0])) : 1u;
-            };
-            if (padded == 1) {
-                const int i = x * 8 + 2 * c;
-                put(i, 0, d[0]), put(i + 1, 0, d[1]);
-                put(i, 1, d[2]), put(i + 1, 1, d[3]);
-                continue;
+            for (int u = 0; u < GROUP; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) d[u][i] = 0.f;
+#pragma unroll
+            for (int k = 0; k < STEPS; ++k) {
+                if constexpr (MULTI) {
+#pragma unroll
+                    for (int u = 0; u < GROUP; ++u)  // (a tile behind the last: that one again)
+                        mma16816(d[u], f[k], frag_s[(min(x0 + u, tiles - 1) * STEPS + k) * 32 + lane]);
+                } else {
+                    now.operand(k, f[0]);
+                    mma16816(k & 1 ? d2 : d[0], f[0], frag_s[k * 32 + lane]);
+                }
             }
-            float s0 = fmaxf(d[0], d[1]), s1 = fmaxf(d[2], d[3]);
-            if (padded >= 4) {
-                s0 = fmaxf(s0, __shfl_xor_sync(0xffffffffu, s0, 1));
-                s1 = fmaxf(s1, __shfl_xor_sync(0xffffffffu, s1, 1));
+            if constexpr (!MULTI) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) d[0][i] += d2[i];
             }
-            if (padded >= 8) {
-                s0 = fmaxf(s0, __shfl_xor_sync(0xffffffffu, s0, 2));
-                s1 = fmaxf(s1, __shfl_xor_sync(0xffffffffu, s1, 2));
-                best[0] = fmaxf(best[0], s0), best[1] = fmaxf(best[1], s1);
-                const int tiles_of = padded / 8;
-                if (x % tiles_of != tiles_of - 1) continue;
-                if (c < 2) put(x / tiles_of, c, c ? best[1] : best[0]);
-                best[0] = best[1] = -INFINITY;
-            } else if (padded == 4) {
-                put(x * 2 + (c >> 1), c & 1, c & 1 ? s1 : s0);
-            } else {
-                put(x * 4 + c, 0, s0);
-                put(x * 4 + c, 1, s1);
+#pragma unroll
+            for (int u = 0; u < GROUP; ++u) {
+                const int x = x0 + u;
+                if (x >= tiles) break;
+                // d: page g of columns 2c and 2c + 1, page g + 8 of both
+                auto put = [&](int i, int e, float s) {  // score of the CTA's query i and page g + 8 e
+                    const int64_t o = base + g + 8 * e;
+                    if (i < queries && o < pages)
+                        a.keys[((int64_t)(q0 + i0 + i) * a.hkv + h) * a.key_stride + o] =
+                            (e ? now.there[1] : now.there[0]) ? score_key(s * (e ? now.unit[1] : now.unit[0])) : 1u;
+                };
+                if (padded == 1) {
+                    const int i = x * 8 + 2 * c;
+                    put(i, 0, d[u][0]), put(i + 1, 0, d[u][1]);
+                    put(i, 1, d[u][2]), put(i + 1, 1, d[u][3]);
+                    continue;
+                }
+                float s0 = fmaxf(d[u][0], d[u][1]), s1 = fmaxf(d[u][2], d[u][3]);
+                if (padded >= 4) {
+                    s0 = fmaxf(s0, __shfl_xor_sync(0xffffffffu, s0, 1));
+                    s1 = fmaxf(s1, __shfl_xor_sync(0xffffffffu, s1, 1));
+                }
+                if (padded >= 8) {
+                    s0 = fmaxf(s0, __shfl_xor_sync(0xffffffffu, s0, 2));
+                    s1 = fmaxf(s1, __shfl_xor_sync(0xffffffffu, s1, 2));
+                    best[0] = fmaxf(best[0], s0), best[1] = fmaxf(best[1], s1);
+                    const int tiles_of = padded / 8;
+                    if (x % tiles_of != tiles_of - 1) continue;
+                    if (c < 2) put(x / tiles_of, c, c ? best[1] : best[0]);
+                    best[0] = best[1] = -INFINITY;
+                } else if (padded == 4) {
+                    put(x * 2 + (c >> 1), c & 1, c & 1 ? s1 : s0);
+                } else {
+                    put(x * 4 + c, 0, s0);
+                    put(x * 4 + c, 1, s1);
+                }
             }
         }
     }
@@ -242,10 +325,8 @@ __global__ void __launch_bounds__(WARPS == 1 ? 128 : 32 * WARPS) pick_select_ker
     if (pair >= a.rows * a.hkv) return;
     const int64_t r = pair / a.hkv;
     // the request of the query: the last whose first query is not behind it, 32 at a time
-    int b = 0;
-    if (a.rows == a.batch && __ldg(a.off + r) == r && __ldg(a.off + r + 1) == r + 1) {
-        b = (int)r;
-    } else {
+    int b = (int)r, t1 = (int)r + 1;
+    if (!a.single) {
         int lo = 0, hi = a.batch;
         while (hi - lo > 1) {
             const int step = (hi - lo + 31) / 32, at = lo + (lane + 1) * step;
@@ -254,8 +335,8 @@ __global__ void __launch_bounds__(WARPS == 1 ? 128 : 32 * WARPS) pick_select_ker
             hi = min(hi, lo + step);
         }
         b = lo;
+        t1 = __ldg(a.off + b + 1);
     }
-    const int t1 = __ldg(a.off + b + 1);
     bool bad;
     const int len = cache_len(__ldg(a.lens + b), a.limit, bad);
     if (bad && tid == 0) atomicOr(a.err, kErrBounds);
@@ -304,22 +385,23 @@ __global__ void __launch_bounds__(WARPS == 1 ? 128 : 32 * WARPS) pick_select_ker
         at_x = forced >= a.budget ? a.budget : pages;
         int turn = 0;
         while (left > 0 && at_x != a.budget) {
-            const int bits = left >= 2 ? 2 : 1;
+            const int bits = WARPS > 1 && left >= 2 ? 2 : 1;
             left -= bits;
             const uint32_t x1 = x + (1u << left), x2 = x + (2u << left), x3 = x + (3u << left);
             int c1 = 0, c2 = 0, c3 = 0;
 #pragma unroll
             for (int i = 0; i < kKeep; ++i) {
                 if (i >= steps) break;
-                c1 += k[i] >= x1, c2 += k[i] >= x2, c3 += k[i] >= x3;
+                c1 += k[i] >= x1;
+                if (WARPS > 1) c2 += k[i] >= x2, c3 += k[i] >= x3;
             }
             for (int i = kKeep; i < steps; ++i) {
                 const uint32_t v = key_at(first + i * 32 + lane);
-                c1 += v >= x1, c2 += v >= x2, c3 += v >= x3;
+                c1 += v >= x1;
+                if (WARPS > 1) c2 += v >= x2, c3 += v >= x3;
             }
             c1 = __reduce_add_sync(0xffffffffu, c1);
-            c2 = __reduce_add_sync(0xffffffffu, c2);
-            c3 = __reduce_add_sync(0xffffffffu, c3);
+            if (WARPS > 1) c2 = __reduce_add_sync(0xffffffffu, c2), c3 = __reduce_add_sync(0xffffffffu, c3);
             if constexpr (WARPS > 1) {
                 int* to = count_s[turn];
                 if (lane < 3) atomicAdd(to + lane, lane == 0 ? c1 : (lane == 1 ? c2 : c3));
@@ -380,15 +462,16 @@ cudaError_t launch_scores(const PickArgs& a, int max_t, int max_pages, int num_s
     const int padded = padded_group(a.group), per = score_queries(padded);
     const int parts = (max_t + per - 1) / per;
     const int tiles = (std::min(per, max_t) * padded + 7) / 8;
-    auto kern = pick_score_kernel<D, FP8>;
+    auto kern = tiles > 1 ? pick_score_kernel<D, FP8, true> : pick_score_kernel<D, FP8, false>;
     const size_t smem = (size_t)tiles * (2 * D / 16) * 32 * sizeof(uint2);
     cudaError_t e = cudaSuccess;
-    if (smem > 48 * 1024) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (smem > 47 * 1024) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    // CTAs of a request's pages: as many as fill the GPU, at most one for every 64 pages
-    const int64_t others = (int64_t)parts * a.hkv * a.batch;
-    const int64_t blocks = std::min<int64_t>((max_pages + kScorePages - 1) / kScorePages,
-                                             std::max<int64_t>(1, (8 * (int64_t)num_sms + others - 1) / others));
+    // CTAs of a request's pages: 64 pages at a time, up to four times where the CTAs fill the GPU all the same (eight
+    // times with more than one tile, whose queries take longer to lay out)
+    const int64_t others = (int64_t)parts * a.hkv * a.batch, steps = (max_pages + kScorePages - 1) / kScorePages;
+    const int64_t times = std::max<int64_t>(1, std::min<int64_t>(tiles > 1 ? 8 : 4, others * steps / (8 * (int64_t)num_sms)));
+    const int64_t blocks = (steps + times - 1) / times;
     cfg.gridDim = dim3((unsigned)blocks, (unsigned)(parts * a.hkv), (unsigned)a.batch);
     cfg.blockDim = dim3(kScoreThreads, 1, 1);
     cfg.dynamicSmemBytes = smem;

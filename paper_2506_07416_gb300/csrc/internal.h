@@ -264,7 +264,7 @@ struct BoundsArgs {
     int32_t batch, limit;
     int32_t* err;
 };
-cudaError_t launch_cache_bounds(const BoundsArgs& a, int head_dim, cudaStream_t stream);
+cudaError_t launch_cache_bounds(const BoundsArgs& a, int head_dim, int num_sms, cudaStream_t stream);
 
 // cache_pick.cu
 struct PickArgs {
@@ -280,6 +280,7 @@ struct PickArgs {
     int64_t rows;
     int32_t batch, hq, group, limit;
     int32_t budget, sink, recent;
+    bool single;              // every request has one query
     uint32_t* keys;           // [rows][hkv][key_stride] scores in an order of whole numbers
     int64_t key_stride;
     int32_t* picked;          // [rows][hkv][budget]
