@@ -1537,7 +1537,6 @@ litevlm_status_t litevlm_select_cache_reserve(litevlm_select_t h, int32_t batch,
     a.batch = batch;
     a.granted = granted;
     a.slots = slots;
-    a.vec = aligned16(slots);
     a.err = h->err_d;
     const OnDevice on(h->device);
     cudaError_t e = on.e;

@@ -28,9 +28,10 @@ __device__ __forceinline__ __half2 block_scale(uint32_t s)
 }
 
 // Of N half pairs that the lanes d apart (16 down to LAST) hold of the same channels, each keeps the extremes of its own
-// ones: the upper lane the upper half. Returns the first pair that the lane keeps.
-template <int N, int d, int LAST>
-__device__ __forceinline__ int halve(__half2* top, __half2* low, int lane)
+// ones: the upper lane the upper half. Returns the first pair that the lane keeps. (Values are picked by copies: picked by
+// index they would live in memory.)
+template <int N, int d, int LAST, int A>
+__device__ __forceinline__ int halve(__half2 (&top)[A], __half2 (&low)[A], int lane)
 {
     if constexpr (d < LAST) {
         return 0;
@@ -39,10 +40,11 @@ __device__ __forceinline__ int halve(__half2* top, __half2* low, int lane)
         const bool up = lane & d;
 #pragma unroll
         for (int i = 0; i < n; ++i) {
-            const __half2 t = __shfl_xor_sync(0xffffffffu, up ? top[i] : top[i + n], d);
-            const __half2 l = __shfl_xor_sync(0xffffffffu, up ? low[i] : low[i + n], d);
-            top[i] = __hmax2(up ? top[i + n] : top[i], t);
-            low[i] = __hmin2(up ? low[i + n] : low[i], l);
+            const __half2 t0 = top[i], t1 = top[i + n], l0 = low[i], l1 = low[i + n];
+            const uint32_t tg = up ? h2_bits(t0) : h2_bits(t1), tk = up ? h2_bits(t1) : h2_bits(t0);
+            const uint32_t lg = up ? h2_bits(l0) : h2_bits(l1), lk = up ? h2_bits(l1) : h2_bits(l0);
+            top[i] = __hmax2(bits_h2(tk), bits_h2(__shfl_xor_sync(0xffffffffu, tg, d)));
+            low[i] = __hmin2(bits_h2(lk), bits_h2(__shfl_xor_sync(0xffffffffu, lg, d)));
         }
         return (up ? n : 0) + halve<n, d / 2, LAST>(top, low, lane);
     }

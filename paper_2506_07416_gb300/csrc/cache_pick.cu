@@ -119,14 +119,16 @@ struct PageCodes {
     }
 };
 
-// The whole numbers of a query (of key head h) into the columns' tiles, by the lanes of `warps` warps, `at` this one's
-// place among them; zeros where !real. The largest magnitude is found over `max_s` where they are more than one.
+// Key heads of a CTA of the kernel for few queries, a warp each (or two, or four).
+__host__ __device__ __forceinline__ int score_heads(int hkv) { return hkv % 4 == 0 ? 4 : (hkv % 2 == 0 ? 2 : 1); }
+
+// The whole numbers of a query (of key head h) into the columns' tiles, by a warp; zeros where !real.
 template <int D, bool FP8>
 __device__ __forceinline__ void stage_query(const PickArgs& a, int64_t row, int h, bool real, int padded, int col0,
-                                            uint2* frag_s, int at, int warps, float* max_s)
+                                            uint2* frag_s)
 {
     constexpr int STEPS = 2 * D / 16, PARTS = D * (FP8 ? 1 : 2) / 16, PER = 32 / PARTS, E = FP8 ? 16 : 8, U = 4;
-    const int lane = threadIdx.x & 31, sub = lane % PARTS, first = at * PER + lane / PARTS, step = warps * PER;
+    const int lane = threadIdx.x & 31, sub = lane % PARTS, first = lane / PARTS, step = PER;
     const uint8_t* from =
         static_cast<const uint8_t*>(a.q) + (row * a.q_stride + (int64_t)h * a.group * D) * (FP8 ? 1 : 2);
     auto load = [&](int y) { return __ldg(reinterpret_cast<const uint4*>(from + (int64_t)y * D * (FP8 ? 1 : 2)) + sub); };
@@ -145,11 +147,6 @@ __device__ __forceinline__ void stage_query(const PickArgs& a, int64_t row, int 
     if (real)
         for (int y = first + U * step; y < a.group; y += step) reach(load(y));
     top = warp_max_f32(top);
-    if (warps > 1) {
-        if (lane == 0) max_s[at] = top;
-        __syncthreads();
-        for (int w = 0; w < warps; ++w) top = fmaxf(top, max_s[w]);
-    }
     // top = f * 2^p, f in [1/2, 1); the unit is 2^(p - 7)
     const int p = max((int)(__float_as_uint(top) >> 23) - 126, -119);
     const float up = __uint_as_float((uint32_t)(127 + 7 - p) << 23);
@@ -179,15 +176,17 @@ __device__ __forceinline__ void stage_query(const PickArgs& a, int64_t row, int 
 }
 
 // MULTI: more than one tile of columns (some queries); else one query, or a few of few heads.
+// !MULTI: a warp has a key head of its own where there are enough, so that a CTA reads neighbouring heads' codes of a
+// page, which lie side by side, at the same time.
 template <int D, bool FP8, bool MULTI>
-__global__ void __launch_bounds__(kScoreThreads, MULTI ? 3 : 4) pick_score_kernel(const __grid_constant__ PickArgs a, int blocks)
+__global__ void __launch_bounds__(kScoreThreads, 3) pick_score_kernel(const __grid_constant__ PickArgs a, int blocks)
 {
     constexpr int STEPS = 2 * D / 16;                       // contractions of 16 channels
     constexpr int GROUP = MULTI ? 4 : 1;                    // tiles of columns at a time: chains that do not wait for one another
     extern __shared__ __align__(16) uint2 frag_s[];         // [tile][step][lane]
-    __shared__ float max_s[kScoreThreads / 32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
-    const int h = blockIdx.y % a.hkv, part = blockIdx.y / a.hkv, b = blockIdx.z;
+    const int heads = MULTI ? 1 : score_heads(a.hkv), groups = a.hkv / heads;  // heads of a CTA
+    const int h = blockIdx.y % groups * heads + warp % heads, part = blockIdx.y / groups, b = blockIdx.z;
     griddep_wait();
     griddep_launch_dependents();
     const int padded = padded_group(a.group), per = score_queries(padded);
@@ -201,9 +200,9 @@ __global__ void __launch_bounds__(kScoreThreads, MULTI ? 3 : 4) pick_score_kerne
     const int last = len - t + i0 + queries - 1;
     if (last < 0) return;
     const int pages = (last >> a.page_shift) + 1;
-    const int step = blocks * kScorePages;
-    int base = blockIdx.x * kScorePages + warp * 16;
-    if (pages <= a.budget || blockIdx.x * kScorePages >= pages) return;
+    const int at_once = kScorePages / heads, step = blocks * at_once;
+    int base = blockIdx.x * at_once + warp / heads * 16;
+    if (pages <= a.budget || blockIdx.x * at_once >= pages) return;
     const int tiles = (queries * padded + 7) / 8;
     // a lane's pages are found two steps ahead, their codes loaded one step ahead
     auto find = [&](int from, int32_t (&p)[2]) {
@@ -223,16 +222,16 @@ __global__ void __launch_bounds__(kScoreThreads, MULTI ? 3 : 4) pick_score_kerne
     next.load(a, page, h, c);
     find(base + step, page);
 
-    if (!MULTI && queries == 1) {
-        stage_query<D, FP8>(a, q0 + i0, h, true, padded, 0, frag_s, warp, kScoreThreads / 32, max_s);
-        if (padded < 8 && tid < 32)  // (the tile's other columns)
-            for (int k = 0; k < STEPS; ++k)
-                if (lane >> 2 >= padded) frag_s[k * 32 + lane] = make_uint2(0u, 0u);
-    } else {
+    uint2* frag = MULTI ? frag_s : frag_s + warp * STEPS * 32;  // (!MULTI: a tile for each warp)
+    if constexpr (MULTI) {
         for (int x = warp; x < tiles * 8 / padded; x += kScoreThreads / 32)  // (zeros behind the last query)
-            stage_query<D, FP8>(a, q0 + i0 + min(x, queries - 1), h, x < queries, padded, x * padded, frag_s, 0, 1, max_s);
+            stage_query<D, FP8>(a, q0 + i0 + min(x, queries - 1), h, x < queries, padded, x * padded, frag);
+        __syncthreads();
+    } else {
+        for (int x = 0; x < 8 / padded; ++x)
+            stage_query<D, FP8>(a, q0 + i0 + min(x, queries - 1), h, x < queries, padded, x * padded, frag);
+        __syncwarp();
     }
-    __syncthreads();
 
     for (; base < pages; base += step) {
         const PageCodes<D> now = next;
@@ -257,10 +256,10 @@ __global__ void __launch_bounds__(kScoreThreads, MULTI ? 3 : 4) pick_score_kerne
                 if constexpr (MULTI) {
 #pragma unroll
                     for (int u = 0; u < GROUP; ++u)  // (a tile behind the last: that one again)
-                        mma16816(d[u], f[k], frag_s[(min(x0 + u, tiles - 1) * STEPS + k) * 32 + lane]);
+                        mma16816(d[u], f[k], frag[(min(x0 + u, tiles - 1) * STEPS + k) * 32 + lane]);
                 } else {
                     now.operand(k, f[0]);
-                    mma16816(k & 1 ? d2 : d[0], f[0], frag_s[k * 32 + lane]);
+                    mma16816(k & 1 ? d2 : d[0], f[0], frag[k * 32 + lane]);
                 }
             }
             if constexpr (!MULTI) {
@@ -463,16 +462,18 @@ cudaError_t launch_scores(const PickArgs& a, int max_t, int max_pages, int num_s
     const int parts = (max_t + per - 1) / per;
     const int tiles = (std::min(per, max_t) * padded + 7) / 8;
     auto kern = tiles > 1 ? pick_score_kernel<D, FP8, true> : pick_score_kernel<D, FP8, false>;
-    const size_t smem = (size_t)tiles * (2 * D / 16) * 32 * sizeof(uint2);
+    const int heads = tiles > 1 ? 1 : score_heads(a.hkv), pages_at_once = kScorePages / heads;
+    const size_t smem = (size_t)(tiles > 1 ? tiles : kScoreThreads / 32) * (2 * D / 16) * 32 * sizeof(uint2);
     cudaError_t e = cudaSuccess;
     if (smem > 47 * 1024) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    // CTAs of a request's pages: 64 pages at a time, up to four times where the CTAs fill the GPU all the same (eight
-    // times with more than one tile, whose queries take longer to lay out)
-    const int64_t others = (int64_t)parts * a.hkv * a.batch, steps = (max_pages + kScorePages - 1) / kScorePages;
-    const int64_t times = std::max<int64_t>(1, std::min<int64_t>(tiles > 1 ? 8 : 4, others * steps / (8 * (int64_t)num_sms)));
+    // CTAs of a request's pages: 64 pages (with a head a warp 16) at a time, up to eight times where the CTAs fill the
+    // GPU all the same
+    const int64_t others = (int64_t)parts * (a.hkv / heads) * a.batch;
+    const int64_t steps = (max_pages + pages_at_once - 1) / pages_at_once;
+    const int64_t times = std::max<int64_t>(1, std::min<int64_t>(8, others * steps / (8 * (int64_t)num_sms)));
     const int64_t blocks = (steps + times - 1) / times;
-    cfg.gridDim = dim3((unsigned)blocks, (unsigned)(parts * a.hkv), (unsigned)a.batch);
+    cfg.gridDim = dim3((unsigned)blocks, (unsigned)(parts * (a.hkv / heads)), (unsigned)a.batch);
     cfg.blockDim = dim3(kScoreThreads, 1, 1);
     cfg.dynamicSmemBytes = smem;
     return cudaLaunchKernelEx(&cfg, kern, a, (int)blocks);

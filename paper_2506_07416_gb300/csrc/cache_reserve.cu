@@ -34,14 +34,16 @@ __device__ __forceinline__ longlong2 scan2(long long x, long long y, longlong2* 
     }
     if (lane == 31) warp_s[warp] = make_longlong2(sx, sy);
     __syncthreads();
-    longlong2 before = make_longlong2(0, 0);
-    all = before;
-    for (int w = 0; w < (int)(blockDim.x >> 5); ++w) {
-        const longlong2 v = warp_s[w];
-        if (w < warp) before.x += v.x, before.y += v.y;
-        all.x += v.x, all.y += v.y;
+    // the warps' sums, by every warp
+    longlong2 v = lane < (int)(blockDim.x >> 5) ? warp_s[lane] : make_longlong2(0, 0);
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const long long a = __shfl_up_sync(0xffffffffu, v.x, d), b = __shfl_up_sync(0xffffffffu, v.y, d);
+        if (lane >= d) v.x += a, v.y += b;
     }
-    return make_longlong2(before.x + sx - x, before.y + sy - y);
+    all.x = __shfl_sync(0xffffffffu, v.x, 31), all.y = __shfl_sync(0xffffffffu, v.y, 31);
+    const long long bx = __shfl_sync(0xffffffffu, v.x, max(warp - 1, 0)), by = __shfl_sync(0xffffffffu, v.y, max(warp - 1, 0));
+    return make_longlong2((warp ? bx : 0) + sx - x, (warp ? by : 0) + sy - y);
 }
 
 __global__ void __launch_bounds__(kThreads) reserve_kernel(const __grid_constant__ ReserveArgs a)
@@ -94,7 +96,10 @@ __global__ void __launch_bounds__(kThreads) reserve_kernel(const __grid_constant
             __syncthreads();
             if (lane == 0) warp_s[tid >> 5].x = mine;
             __syncthreads();
-            for (int w = 0; w < threads >> 5; ++w) used = max(used, (int64_t)warp_s[w].x);
+            long long most = lane < threads >> 5 ? warp_s[lane].x : 0;
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, d));
+            used = max(used, (int64_t)most);
         }
         taken += all.x, given += all.y;
         __syncthreads();
@@ -118,42 +123,38 @@ __global__ void __launch_bounds__(kThreads) reserve_kernel(const __grid_constant
                 }
             }
         }
-        // ---- slots, four neighbouring tokens a thread
+        // ---- slots: a warp takes 256 neighbouring tokens, whose pages' numbers are all on their way at once
         const int64_t r0 = max(off_s[0], 0), r1 = min((int64_t)off_s[n], a.rows);
-        const int64_t q0 = (r0 & ~3ll) + 4 * ((int64_t)blockIdx.x * threads + tid), q_step = 4ll * gridDim.x * threads;
-        for (int64_t q = q0; q < r1; q += q_step) {
-            int lo = 0, hi = n;
-            const int64_t first = q > r0 ? q : r0;
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (off_s[mid] <= first) lo = mid;
-                else hi = mid;
+        constexpr int U = 8;
+        for (int64_t q = r0 + 32 * U * ((int64_t)(tid >> 5) * gridDim.x + blockIdx.x); q < r1; q += 32 * U * step) {
+            int x = 0, hi = n;  // the request of the first token: the last that begins at or before it, 32 at a time
+            while (hi - x > 1) {
+                const int d = (hi - x + 31) / 32, at = x + (lane + 1) * d;
+                x += __popc(__ballot_sync(0xffffffffu, at < hi && off_s[at] <= q)) * d;
+                hi = min(hi, x + d);
             }
-            long long s[4];
+            int32_t p[U], in[U];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int64_t r = q + e;
-                s[e] = -1;
-                if (r < r0 || r >= r1) continue;
-                while (off_s[lo + 1] <= r) ++lo;
-                if (need_s[lo] < 0) continue;
-                const int64_t pos = (int64_t)want_s[lo] - off_s[lo + 1] + r;
-                int32_t p = -1;
-                if (pos >= 0) {
-                    const int o = (int)(pos >> a.page_shift);
-                    p = o < has_s[lo] ? __ldg(a.table + (int64_t)(b0 + lo) * a.width + o)
-                                      : __ldg(a.free + (head + from_s[lo] + o - has_s[lo]) % total);
-                }
-                if (p >= 0 && p < total) s[e] = ((int64_t)p << a.page_shift) + (pos & ((1 << a.page_shift) - 1));
-                else atomicOr(a.err, kErrBounds);
+            for (int u = 0; u < U; ++u) {
+                const int64_t r = q + u * 32 + lane;
+                p[u] = -1, in[u] = -1;
+                if (r >= r1) continue;
+                while (off_s[x + 1] <= r) ++x;
+                if (need_s[x] < 0) continue;
+                const int64_t pos = (int64_t)want_s[x] - off_s[x + 1] + r;
+                in[u] = (int)(pos & ((1 << a.page_shift) - 1));
+                if (pos < 0) continue;
+                const int o = (int)(pos >> a.page_shift);
+                p[u] = o < has_s[x] ? __ldg(a.table + (int64_t)(b0 + x) * a.width + o)
+                                    : __ldg(a.free + (head + from_s[x] + o - has_s[x]) % total);
             }
-            if (q >= r0 && q + 4 <= r1 && a.vec) {
-                reinterpret_cast<longlong2*>(a.slots + q)[0] = make_longlong2(s[0], s[1]);
-                reinterpret_cast<longlong2*>(a.slots + q)[1] = make_longlong2(s[2], s[3]);
-            } else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (q + e >= r0 && q + e < r1) a.slots[q + e] = s[e];
+            for (int u = 0; u < U; ++u) {
+                const int64_t r = q + u * 32 + lane;
+                if (r >= r1) continue;
+                const bool there = p[u] >= 0 && p[u] < total;
+                if (!there && in[u] >= 0) atomicOr(a.err, kErrBounds);
+                a.slots[r] = there ? ((int64_t)p[u] << a.page_shift) + in[u] : -1;
             }
         }
         __syncthreads();

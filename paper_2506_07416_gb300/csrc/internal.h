@@ -248,7 +248,6 @@ struct ReserveArgs {
     int32_t batch, limit;     // limit: tokens a table row holds
     int32_t* granted;         // [batch]
     int64_t* slots;           // [rows]
-    bool vec;                 // slots are 16-byte aligned
     int32_t* err;
 };
 cudaError_t launch_cache_reserve(const ReserveArgs& a, int num_sms, cudaStream_t stream);
