@@ -51,7 +51,7 @@ __device__ __forceinline__ int halve(__half2 (&top)[A], __half2 (&low)[A], int l
 }
 
 template <int D>
-__global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(const __grid_constant__ BoundsArgs a, int heads)
+__global__ void __launch_bounds__(kBoundsThreads, 8) bounds_kernel(const __grid_constant__ BoundsArgs a, int heads)
 {
     constexpr int LANES = D / 32;     // lanes of a row
     constexpr int ROWS = 32 / LANES;  // rows of a warp at a time

@@ -123,11 +123,11 @@ struct PageCodes {
 __host__ __device__ __forceinline__ int score_heads(int hkv) { return hkv % 4 == 0 ? 4 : (hkv % 2 == 0 ? 2 : 1); }
 
 // The whole numbers of a query (of key head h) into the columns' tiles, by a warp; zeros where !real.
-template <int D, bool FP8>
-__device__ __forceinline__ void stage_query(const PickArgs& a, int64_t row, int h, bool real, int padded, int col0,
-                                            uint2* frag_s)
+// store(column, channel, r): four neighbouring channels from this one on.
+template <int D, bool FP8, typename F>
+__device__ __forceinline__ void stage_query(const PickArgs& a, int64_t row, int h, bool real, int padded, int col0, F store)
 {
-    constexpr int STEPS = 2 * D / 16, PARTS = D * (FP8 ? 1 : 2) / 16, PER = 32 / PARTS, E = FP8 ? 16 : 8, U = 4;
+    constexpr int PARTS = D * (FP8 ? 1 : 2) / 16, PER = 32 / PARTS, E = FP8 ? 16 : 8, U = 4;
     const int lane = threadIdx.x & 31, sub = lane % PARTS, first = lane / PARTS, step = PER;
     const uint8_t* from =
         static_cast<const uint8_t*>(a.q) + (row * a.q_stride + (int64_t)h * a.group * D) * (FP8 ? 1 : 2);
@@ -153,19 +153,12 @@ __device__ __forceinline__ void stage_query(const PickArgs& a, int64_t row, int 
     auto put = [&](const uint4& w, int y) {
         float v[E];
         query_values<FP8>(w, v);
-        const int col = col0 + y, n = col & 7;
 #pragma unroll
         for (int e = 0; e < E; e += 4) {
             float r[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) r[i] = fminf(fmaxf(rintf(v[e + i] * up), -127.f), 127.f);
-            // channels [ch, ch + 4): word (ch % 16) / 4 of lane (ch / 16) % 4 and load ch / 64
-            const int ch = sub * E + e, cc = ch / 16 % 4, k = ch / 64 * 4 + ch % 16 / 4;
-            uint2* to = frag_s + ((col >> 3) * STEPS + k) * 32 + n * 4 + cc;
-            const auto pack = [](float s, float u) { return h2_bits(__floats2half2_rn(s, u)); };
-            to[0] = make_uint2(pack(fmaxf(r[0], 0.f), fmaxf(r[1], 0.f)), pack(fmaxf(r[2], 0.f), fmaxf(r[3], 0.f)));
-            to[STEPS / 2 * 32] =
-                make_uint2(pack(fminf(r[0], 0.f), fminf(r[1], 0.f)), pack(fminf(r[2], 0.f), fminf(r[3], 0.f)));
+            store(col0 + y, sub * E + e, r);
         }
     };
 #pragma unroll
@@ -175,134 +168,218 @@ __device__ __forceinline__ void stage_query(const PickArgs& a, int64_t row, int 
         put(real ? load(min(y, a.group - 1)) : make_uint4(0u, 0u, 0u, 0u), y);
 }
 
-// MULTI: more than one tile of columns (some queries); else one query, or a few of few heads.
-// !MULTI: a warp has a key head of its own where there are enough, so that a CTA reads neighbouring heads' codes of a
-// page, which lie side by side, at the same time.
-template <int D, bool FP8, bool MULTI>
-__global__ void __launch_bounds__(kScoreThreads, 3) pick_score_kernel(const __grid_constant__ PickArgs a, int blocks)
+// What a CTA scores: queries [i0, i0 + queries) of its request, over the pages that the last of them sees (none: nothing to
+// do, also where the select kernel reads no scores because all pages may be picked).
+struct ScoreTile {
+    int q0, i0, queries, pages;
+};
+__device__ __forceinline__ ScoreTile score_tile(const PickArgs& a, int b, int part, int per)
 {
-    constexpr int STEPS = 2 * D / 16;                       // contractions of 16 channels
-    constexpr int GROUP = MULTI ? 4 : 1;                    // tiles of columns at a time: chains that do not wait for one another
-    extern __shared__ __align__(16) uint2 frag_s[];         // [tile][step][lane]
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
-    const int heads = MULTI ? 1 : score_heads(a.hkv), groups = a.hkv / heads;  // heads of a CTA
+    ScoreTile s;
+    s.q0 = __ldg(a.off + b);
+    const int t = __ldg(a.off + b + 1) - s.q0;
+    bool bad;
+    const int len = cache_len(__ldg(a.lens + b), a.limit, bad);
+    s.i0 = part * per;
+    s.queries = min(per, t - s.i0);
+    if (bad && s.queries > 0 && threadIdx.x == 0) atomicOr(a.err, kErrBounds);
+    const int last = len - t + s.i0 + s.queries - 1;
+    s.pages = s.queries <= 0 || last < 0 ? 0 : (last >> a.page_shift) + 1;
+    if (s.pages <= a.budget) s.pages = 0;
+    return s;
+}
+
+// The lane's pages g and g + 8 from `from` on in the pool (-1: none).
+__device__ __forceinline__ void find_pages(const PickArgs& a, int b, int from, int pages, int32_t (&p)[2])
+{
+    const int g = (threadIdx.x & 31) >> 2;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const int o = from + g + 8 * e;
+        p[e] = -1;
+        if (o < pages) {
+            p[e] = cache_page(a.table, a.width, a.num_pages, a.page_shift, b, (int64_t)o << a.page_shift);
+            if (p[e] < 0 && (threadIdx.x & 3) == 0) atomicOr(a.err, kErrBounds);
+        }
+    }
+}
+
+// Scores of a contraction's 16 pages (from `base` on) and a tile x of eight columns: d of page g and columns 2c and 2c + 1,
+// then of page g + 8. `best` carries the largest over the tiles of a query of more than eight heads.
+template <int D>
+__device__ __forceinline__ void store_scores(const PickArgs& a, const ScoreTile& st, int h, int padded, int base, int x,
+                                             const PageCodes<D>& now, const float (&d)[4], float (&best)[2])
+{
+    const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+    auto put = [&](int i, int e, float s) {  // score of the CTA's query i and page g + 8 e
+        const int o = base + g + 8 * e;
+        if (i < st.queries && o < st.pages)
+            a.keys[((int64_t)(st.q0 + st.i0 + i) * a.hkv + h) * a.key_stride + o] =
+                (e ? now.there[1] : now.there[0]) ? score_key(s * (e ? now.unit[1] : now.unit[0])) : 1u;
+    };
+    if (padded == 1) {
+        const int i = x * 8 + 2 * c;
+        put(i, 0, d[0]), put(i + 1, 0, d[1]);
+        put(i, 1, d[2]), put(i + 1, 1, d[3]);
+        return;
+    }
+    float s0 = fmaxf(d[0], d[1]), s1 = fmaxf(d[2], d[3]);
+    if (padded >= 4) {
+        s0 = fmaxf(s0, __shfl_xor_sync(0xffffffffu, s0, 1));
+        s1 = fmaxf(s1, __shfl_xor_sync(0xffffffffu, s1, 1));
+    }
+    if (padded >= 8) {
+        s0 = fmaxf(s0, __shfl_xor_sync(0xffffffffu, s0, 2));
+        s1 = fmaxf(s1, __shfl_xor_sync(0xffffffffu, s1, 2));
+        best[0] = fmaxf(best[0], s0), best[1] = fmaxf(best[1], s1);
+        const int tiles_of = padded / 8;
+        if (x % tiles_of != tiles_of - 1) return;
+        if (c < 2) put(x / tiles_of, c, c ? best[1] : best[0]);
+        best[0] = best[1] = -INFINITY;
+    } else if (padded == 4) {
+        put(x * 2 + (c >> 1), c & 1, c & 1 ? s1 : s0);
+    } else {
+        put(x * 4 + c, 0, s0);
+        put(x * 4 + c, 1, s1);
+    }
+}
+
+// D += A B in whole numbers: 16 pages x 8 columns, 32 channels
+__device__ __forceinline__ void mma16832(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint2 b)
+{
+    asm volatile(
+        "mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+        "{%0, %1, %2, %3};"
+        : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b.x), "r"(b.y));
+}
+
+// Single tokens, and a few queries of few heads: one tile of columns. The codes go into the contraction as they are in
+// memory (s8: this GPU's slow kind, but a twentieth of the tile's time), the queries' whole numbers stay in
+// registers, and what is left bounds the kernel by memory. A warp has a key head of its own where there are enough, so
+// that a CTA reads neighbouring heads' codes of a page, which lie side by side, at the same time.
+template <int D, bool FP8>
+__global__ void __launch_bounds__(kScoreThreads, 4) pick_token_kernel(const __grid_constant__ PickArgs a, int blocks)
+{
+    constexpr int STEPS = 2 * D / 32;                       // contractions of 32 channels
+    __shared__ uint2 frag_s[kScoreThreads / 32][STEPS][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = lane & 3;
+    const int heads = score_heads(a.hkv), groups = a.hkv / heads;  // heads of a CTA
     const int h = blockIdx.y % groups * heads + warp % heads, part = blockIdx.y / groups, b = blockIdx.z;
     griddep_wait();
     griddep_launch_dependents();
-    const int padded = padded_group(a.group), per = score_queries(padded);
-    const int q0 = __ldg(a.off + b), t = __ldg(a.off + b + 1) - q0;
-    bool bad;
-    const int len = cache_len(__ldg(a.lens + b), a.limit, bad);
-    const int i0 = part * per, queries = min(per, t - i0);
-    if (queries <= 0) return;
-    if (bad && tid == 0) atomicOr(a.err, kErrBounds);
-    // pages that the last of these queries sees; the select kernel reads no scores where all may be picked
-    const int last = len - t + i0 + queries - 1;
-    if (last < 0) return;
-    const int pages = (last >> a.page_shift) + 1;
+    const int padded = padded_group(a.group);
+    const ScoreTile st = score_tile(a, b, part, score_queries(padded));
     const int at_once = kScorePages / heads, step = blocks * at_once;
     int base = blockIdx.x * at_once + warp / heads * 16;
-    if (pages <= a.budget || blockIdx.x * at_once >= pages) return;
-    const int tiles = (queries * padded + 7) / 8;
+    if (base >= st.pages) return;
     // a lane's pages are found two steps ahead, their codes loaded one step ahead
-    auto find = [&](int from, int32_t (&p)[2]) {
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int64_t o = from + g + 8 * e;
-            p[e] = -1;
-            if (o < pages) {
-                p[e] = cache_page(a.table, a.width, a.num_pages, a.page_shift, b, o << a.page_shift);
-                if (p[e] < 0 && c == 0) atomicOr(a.err, kErrBounds);
-            }
-        }
-    };
     int32_t page[2];
     PageCodes<D> next;
-    find(base, page);
+    find_pages(a, b, base, st.pages, page);
     next.load(a, page, h, c);
-    find(base + step, page);
-
-    uint2* frag = MULTI ? frag_s : frag_s + warp * STEPS * 32;  // (!MULTI: a tile for each warp)
-    if constexpr (MULTI) {
-        for (int x = warp; x < tiles * 8 / padded; x += kScoreThreads / 32)  // (zeros behind the last query)
-            stage_query<D, FP8>(a, q0 + i0 + min(x, queries - 1), h, x < queries, padded, x * padded, frag);
-        __syncthreads();
-    } else {
-        for (int x = 0; x < 8 / padded; ++x)
-            stage_query<D, FP8>(a, q0 + i0 + min(x, queries - 1), h, x < queries, padded, x * padded, frag);
-        __syncwarp();
-    }
-
-    for (; base < pages; base += step) {
-        const PageCodes<D> now = next;
-        uint32_t f[MULTI ? STEPS : 1][4];
-        if constexpr (MULTI) {
+    find_pages(a, b, base + step, st.pages, page);
+    for (int x = 0; x < 8 / padded; ++x)
+        stage_query<D, FP8>(a, st.q0 + st.i0 + min(x, st.queries - 1), h, x < st.queries, padded, x * padded,
+                            [&](int col, int ch, const float (&r)[4]) {
+                                // channels [ch, ch + 4): word (ch % 16) / 4 of lane (ch / 16) % 4 and load ch / 64, two
+                                // words a contraction
+                                const int k = ch / 64 * 2 + ch % 16 / 8;
+                                uint32_t up = 0u, down = 0u;
 #pragma unroll
-            for (int k = 0; k < STEPS; ++k) now.operand(k, f[k]);
+                                for (int i = 0; i < 4; ++i) {
+                                    up |= ((uint32_t)(int)fmaxf(r[i], 0.f) & 0xFFu) << (8 * i);
+                                    down |= ((uint32_t)(int)fminf(r[i], 0.f) & 0xFFu) << (8 * i);
+                                }
+                                uint2* to = &frag_s[warp][k][col * 4 + ch / 16 % 4];
+                                if (ch % 8) to[0].y = up, to[STEPS / 2 * 32].y = down;
+                                else to[0].x = up, to[STEPS / 2 * 32].x = down;
+                            });
+    __syncwarp();
+    uint2 q[STEPS];
+#pragma unroll
+    for (int k = 0; k < STEPS; ++k) q[k] = frag_s[warp][k][lane];
+    for (; base < st.pages; base += step) {
+        int d[2][4] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+#pragma unroll
+        for (int k = 0; k < STEPS; k += 2) {
+            const uint4 v = next.w[0][k / 2], w = next.w[1][k / 2];
+            mma16832(d[0], v.x, w.x, v.y, w.y, q[k]);
+            mma16832(d[1], v.z, w.z, v.w, w.w, q[k + 1]);
         }
-        if (base + step < pages) {
+        PageCodes<D> now;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) now.unit[e] = next.unit[e], now.there[e] = next.there[e];
+        if (base + step < st.pages) {
             next.load(a, page, h, c);
-            find(base + 2 * step, page);
+            find_pages(a, b, base + 2 * step, st.pages, page);
         }
-        float best[2] = {-INFINITY, -INFINITY};  // over the tiles of a query of more than eight heads
+        float f[4], best[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = (float)(d[0][i] + d[1][i]);
+        store_scores<D>(a, st, h, padded, base, 0, now, f, best);
+    }
+}
+
+// Some queries: up to eight tiles of columns (more for a query of more than 64 heads), four at a time, chains of
+// contractions that do not wait for one another.
+template <int D, bool FP8>
+__global__ void __launch_bounds__(kScoreThreads, 3) pick_score_kernel(const __grid_constant__ PickArgs a, int blocks)
+{
+    constexpr int STEPS = 2 * D / 16, GROUP = 4;            // contractions of 16 channels
+    extern __shared__ __align__(16) uint2 frag_s[];         // [tile][step][lane]
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = lane & 3;
+    const int h = blockIdx.y % a.hkv, part = blockIdx.y / a.hkv, b = blockIdx.z;
+    griddep_wait();
+    griddep_launch_dependents();
+    const int padded = padded_group(a.group);
+    const ScoreTile st = score_tile(a, b, part, score_queries(padded));
+    const int step = blocks * kScorePages;
+    int base = blockIdx.x * kScorePages + warp * 16;
+    if (blockIdx.x * kScorePages >= st.pages) return;
+    const int tiles = (st.queries * padded + 7) / 8;
+    int32_t page[2];
+    PageCodes<D> next;
+    find_pages(a, b, base, st.pages, page);
+    next.load(a, page, h, c);
+    find_pages(a, b, base + step, st.pages, page);
+    for (int x = warp; x < tiles * 8 / padded; x += kScoreThreads / 32)  // (zeros behind the last query)
+        stage_query<D, FP8>(a, st.q0 + st.i0 + min(x, st.queries - 1), h, x < st.queries, padded, x * padded,
+                            [&](int col, int ch, const float (&r)[4]) {
+                                // channels [ch, ch + 4): word (ch % 16) / 4 of lane (ch / 16) % 4 and load ch / 64
+                                const int k = ch / 64 * 4 + ch % 16 / 4;
+                                uint2* to = frag_s + ((col >> 3) * STEPS + k) * 32 + (col & 7) * 4 + ch / 16 % 4;
+                                const auto pack = [](float s, float u) { return h2_bits(__floats2half2_rn(s, u)); };
+                                to[0] = make_uint2(pack(fmaxf(r[0], 0.f), fmaxf(r[1], 0.f)),
+                                                   pack(fmaxf(r[2], 0.f), fmaxf(r[3], 0.f)));
+                                to[STEPS / 2 * 32] = make_uint2(pack(fminf(r[0], 0.f), fminf(r[1], 0.f)),
+                                                                pack(fminf(r[2], 0.f), fminf(r[3], 0.f)));
+                            });
+    __syncthreads();
+    for (; base < st.pages; base += step) {
+        const PageCodes<D> now = next;
+        uint32_t f[STEPS][4];
+#pragma unroll
+        for (int k = 0; k < STEPS; ++k) now.operand(k, f[k]);
+        if (base + step < st.pages) {
+            next.load(a, page, h, c);
+            find_pages(a, b, base + 2 * step, st.pages, page);
+        }
+        float best[2] = {-INFINITY, -INFINITY};
         for (int x0 = 0; x0 < tiles; x0 += GROUP) {
-            float d[GROUP][4], d2[4] = {0.f, 0.f, 0.f, 0.f};
+            float d[GROUP][4];
 #pragma unroll
             for (int u = 0; u < GROUP; ++u)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) d[u][i] = 0.f;
 #pragma unroll
-            for (int k = 0; k < STEPS; ++k) {
-                if constexpr (MULTI) {
+            for (int k = 0; k < STEPS; ++k)
 #pragma unroll
-                    for (int u = 0; u < GROUP; ++u)  // (a tile behind the last: that one again)
-                        mma16816(d[u], f[k], frag[(min(x0 + u, tiles - 1) * STEPS + k) * 32 + lane]);
-                } else {
-                    now.operand(k, f[0]);
-                    mma16816(k & 1 ? d2 : d[0], f[0], frag[k * 32 + lane]);
-                }
-            }
-            if constexpr (!MULTI) {
+                for (int u = 0; u < GROUP; ++u)  // (a tile behind the last: that one again)
+                    mma16816(d[u], f[k], frag_s[(min(x0 + u, tiles - 1) * STEPS + k) * 32 + lane]);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) d[0][i] += d2[i];
-            }
-#pragma unroll
-            for (int u = 0; u < GROUP; ++u) {
-                const int x = x0 + u;
-                if (x >= tiles) break;
-                // d: page g of columns 2c and 2c + 1, page g + 8 of both
-                auto put = [&](int i, int e, float s) {  // score of the CTA's query i and page g + 8 e
-                    const int64_t o = base + g + 8 * e;
-                    if (i < queries && o < pages)
-                        a.keys[((int64_t)(q0 + i0 + i) * a.hkv + h) * a.key_stride + o] =
-                            (e ? now.there[1] : now.there[0]) ? score_key(s * (e ? now.unit[1] : now.unit[0])) : 1u;
-                };
-                if (padded == 1) {
-                    const int i = x * 8 + 2 * c;
-                    put(i, 0, d[u][0]), put(i + 1, 0, d[u][1]);
-                    put(i, 1, d[u][2]), put(i + 1, 1, d[u][3]);
-                    continue;
-                }
-                float s0 = fmaxf(d[u][0], d[u][1]), s1 = fmaxf(d[u][2], d[u][3]);
-                if (padded >= 4) {
-                    s0 = fmaxf(s0, __shfl_xor_sync(0xffffffffu, s0, 1));
-                    s1 = fmaxf(s1, __shfl_xor_sync(0xffffffffu, s1, 1));
-                }
-                if (padded >= 8) {
-                    s0 = fmaxf(s0, __shfl_xor_sync(0xffffffffu, s0, 2));
-                    s1 = fmaxf(s1, __shfl_xor_sync(0xffffffffu, s1, 2));
-                    best[0] = fmaxf(best[0], s0), best[1] = fmaxf(best[1], s1);
-                    const int tiles_of = padded / 8;
-                    if (x % tiles_of != tiles_of - 1) continue;
-                    if (c < 2) put(x / tiles_of, c, c ? best[1] : best[0]);
-                    best[0] = best[1] = -INFINITY;
-                } else if (padded == 4) {
-                    put(x * 2 + (c >> 1), c & 1, c & 1 ? s1 : s0);
-                } else {
-                    put(x * 4 + c, 0, s0);
-                    put(x * 4 + c, 1, s1);
-                }
-            }
+            for (int u = 0; u < GROUP; ++u)
+                if (x0 + u < tiles) store_scores<D>(a, st, h, padded, base, x0 + u, now, d[u], best);
         }
     }
 }
@@ -461,9 +538,9 @@ cudaError_t launch_scores(const PickArgs& a, int max_t, int max_pages, int num_s
     const int padded = padded_group(a.group), per = score_queries(padded);
     const int parts = (max_t + per - 1) / per;
     const int tiles = (std::min(per, max_t) * padded + 7) / 8;
-    auto kern = tiles > 1 ? pick_score_kernel<D, FP8, true> : pick_score_kernel<D, FP8, false>;
+    auto kern = tiles > 1 ? pick_score_kernel<D, FP8> : pick_token_kernel<D, FP8>;
     const int heads = tiles > 1 ? 1 : score_heads(a.hkv), pages_at_once = kScorePages / heads;
-    const size_t smem = (size_t)(tiles > 1 ? tiles : kScoreThreads / 32) * (2 * D / 16) * 32 * sizeof(uint2);
+    const size_t smem = tiles > 1 ? (size_t)tiles * (2 * D / 16) * 32 * sizeof(uint2) : 0;
     cudaError_t e = cudaSuccess;
     if (smem > 47 * 1024) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
