@@ -26,7 +26,7 @@ OBJ_DEBUG = os.path.join(PKG, "_build_debug")
 LIB_DEBUG = os.path.join(PKG, "liblitevlm_select_debug.so")
 SOURCES = ["api.cu", "score_tc.cu", "score_res.cu", "ctx_stats.cu", "topk.cu", "compact.cu", "splice.cu", "views.cu", "proj.cu",
            "cache_append.cu", "cache_attend.cu", "cache_tile.cu", "cache_evict.cu", "cache_reserve.cu",
-           "cache_bounds.cu", "cache_pick.cu", "verify.cu"]
+           "cache_bounds.cu", "cache_pick.cu", "cache_pick_tile.cu", "verify.cu"]
 FASTCALL = os.path.join(PKG, "_fastcall.so")  # argument marshalling of the binding (CPython extension)
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 

@@ -1655,6 +1655,7 @@ litevlm_status_t litevlm_select_cache_pick(litevlm_select_t h, int32_t batch, co
     a.keys = static_cast<uint32_t*>(workspace);
     a.picked = picked;
     a.err = h->err_d;
+    a.wait_budget = h->wait_budget;
     const OnDevice on(h->device);
     cudaError_t e = on.e;
     int32_t launches = 0;

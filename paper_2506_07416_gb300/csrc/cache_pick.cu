@@ -14,7 +14,7 @@
 
 #include <algorithm>
 
-#include "cache.cuh"
+#include "cache_pick.cuh"
 
 namespace lvs {
 
@@ -24,11 +24,6 @@ constexpr int kScoreThreads = 128;
 constexpr int kScorePages = 16 * kScoreThreads / 32;  // of a CTA at a time
 constexpr int kScoreTiles = 8;                        // tiles of eight columns of a CTA, at most (16 for more heads)
 
-// Columns of a query: its heads padded to 1, 2, 4 or a multiple of 8.
-__host__ __device__ __forceinline__ int padded_group(int group)
-{
-    return group <= 2 ? group : (group <= 4 ? 4 : (group + 7) & ~7);
-}
 // Queries of a CTA.
 __host__ __device__ __forceinline__ int score_queries(int padded)
 {
@@ -42,49 +37,6 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
         "{%0, %1, %2, %3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b.x), "r"(b.y));
-}
-
-// The four signed bytes of w as f16 (bytes 0, 1 and 2, 3): 1024 + (x + 128) has x's bits as its last ones
-__device__ __forceinline__ void s8x4_value(uint32_t w, uint32_t& a, uint32_t& b)
-{
-    const uint32_t u = w ^ 0x80808080u;
-    const __half2 off = bits_h2(0x64806480u);  // 1152
-    a = h2_bits(__hsub2(bits_h2(__byte_perm(u, 0x64646464u, 0x4140)), off));
-    b = h2_bits(__hsub2(bits_h2(__byte_perm(u, 0x64646464u, 0x4342)), off));
-}
-
-// Order of the scores as whole numbers, above 1 (0: a page that the query does not see, 1: one that the pool has not).
-__device__ __forceinline__ uint32_t score_key(float s)
-{
-    const uint32_t u = __float_as_uint(s);
-    return u & 0x80000000u ? ~u : u | 0x80000000u;
-}
-
-// Element x of a row's 16-byte parts as a finite number (NaN: 0, an infinity: the largest).
-template <bool FP8>
-__device__ __forceinline__ void query_values(const uint4& v, float (&x)[FP8 ? 16 : 8])
-{
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    if constexpr (FP8) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            __half2 h[2];
-            e4m3x4_value(w[i], h);
-            const float2 a = __half22float2(h[0]), b = __half22float2(h[1]);
-            x[4 * i] = a.x, x[4 * i + 1] = a.y, x[4 * i + 2] = b.x, x[4 * i + 3] = b.y;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[2 * i] = __uint_as_float(w[i] << 16);
-            x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < (FP8 ? 16 : 8); ++i) {
-        if (x[i] != x[i]) x[i] = 0.f;
-        x[i] = fminf(fmaxf(x[i], -0x1.FEp127f), 0x1.FEp127f);
-    }
 }
 
 // A lane's codes of two pages as they are in memory, their units and whether the pool has them.
@@ -121,73 +73,6 @@ struct PageCodes {
 
 // Key heads of a CTA of the kernel for few queries, a warp each (or two, or four).
 __host__ __device__ __forceinline__ int score_heads(int hkv) { return hkv % 4 == 0 ? 4 : (hkv % 2 == 0 ? 2 : 1); }
-
-// The whole numbers of a query (of key head h) into the columns' tiles, by a warp; zeros where !real.
-// store(column, channel, r): four neighbouring channels from this one on.
-template <int D, bool FP8, typename F>
-__device__ __forceinline__ void stage_query(const PickArgs& a, int64_t row, int h, bool real, int padded, int col0, F store)
-{
-    constexpr int PARTS = D * (FP8 ? 1 : 2) / 16, PER = 32 / PARTS, E = FP8 ? 16 : 8, U = 4;
-    const int lane = threadIdx.x & 31, sub = lane % PARTS, first = lane / PARTS, step = PER;
-    const uint8_t* from =
-        static_cast<const uint8_t*>(a.q) + (row * a.q_stride + (int64_t)h * a.group * D) * (FP8 ? 1 : 2);
-    auto load = [&](int y) { return __ldg(reinterpret_cast<const uint4*>(from + (int64_t)y * D * (FP8 ? 1 : 2)) + sub); };
-    uint4 kept[U];  // the first rows stay in registers between the two passes
-    float top = 0.f;
-#pragma unroll
-    for (int u = 0; u < U; ++u) kept[u] = real ? load(min(first + u * step, a.group - 1)) : make_uint4(0u, 0u, 0u, 0u);
-    auto reach = [&](const uint4& w) {
-        float v[E];
-        query_values<FP8>(w, v);
-#pragma unroll
-        for (int e = 0; e < E; ++e) top = fmaxf(top, fabsf(v[e]));
-    };
-#pragma unroll
-    for (int u = 0; u < U; ++u) reach(kept[u]);
-    if (real)
-        for (int y = first + U * step; y < a.group; y += step) reach(load(y));
-    top = warp_max_f32(top);
-    // top = f * 2^p, f in [1/2, 1); the unit is 2^(p - 7)
-    const int p = max((int)(__float_as_uint(top) >> 23) - 126, -119);
-    const float up = __uint_as_float((uint32_t)(127 + 7 - p) << 23);
-    auto put = [&](const uint4& w, int y) {
-        float v[E];
-        query_values<FP8>(w, v);
-#pragma unroll
-        for (int e = 0; e < E; e += 4) {
-            float r[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) r[i] = fminf(fmaxf(rintf(v[e + i] * up), -127.f), 127.f);
-            store(col0 + y, sub * E + e, r);
-        }
-    };
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-        if (first + u * step < padded) put(kept[u], first + u * step);  // (behind the last head: that one again)
-    for (int y = first + U * step; y < padded; y += step)
-        put(real ? load(min(y, a.group - 1)) : make_uint4(0u, 0u, 0u, 0u), y);
-}
-
-// What a CTA scores: queries [i0, i0 + queries) of its request, over the pages that the last of them sees (none: nothing to
-// do, also where the select kernel reads no scores because all pages may be picked).
-struct ScoreTile {
-    int q0, i0, queries, pages;
-};
-__device__ __forceinline__ ScoreTile score_tile(const PickArgs& a, int b, int part, int per)
-{
-    ScoreTile s;
-    s.q0 = __ldg(a.off + b);
-    const int t = __ldg(a.off + b + 1) - s.q0;
-    bool bad;
-    const int len = cache_len(__ldg(a.lens + b), a.limit, bad);
-    s.i0 = part * per;
-    s.queries = min(per, t - s.i0);
-    if (bad && s.queries > 0 && threadIdx.x == 0) atomicOr(a.err, kErrBounds);
-    const int last = len - t + s.i0 + s.queries - 1;
-    s.pages = s.queries <= 0 || last < 0 ? 0 : (last >> a.page_shift) + 1;
-    if (s.pages <= a.budget) s.pages = 0;
-    return s;
-}
 
 // The lane's pages g and g + 8 from `from` on in the pool (-1: none).
 __device__ __forceinline__ void find_pages(const PickArgs& a, int b, int from, int pages, int32_t (&p)[2])
@@ -259,7 +144,7 @@ __device__ __forceinline__ void mma16832(int (&d)[4], uint32_t a0, uint32_t a1, 
 // registers, and what is left bounds the kernel by memory. A warp has a key head of its own where there are enough, so
 // that a CTA reads neighbouring heads' codes of a page, which lie side by side, at the same time.
 template <int D, bool FP8>
-__global__ void __launch_bounds__(kScoreThreads, 4) pick_token_kernel(const __grid_constant__ PickArgs a, int blocks)
+__global__ void __launch_bounds__(kScoreThreads, 4) pick_token_kernel(const __grid_constant__ PickArgs a, int steps)
 {
     constexpr int STEPS = 2 * D / 32;                       // contractions of 32 channels
     __shared__ uint2 frag_s[kScoreThreads / 32][STEPS][32];
@@ -270,15 +155,18 @@ __global__ void __launch_bounds__(kScoreThreads, 4) pick_token_kernel(const __gr
     griddep_launch_dependents();
     const int padded = padded_group(a.group);
     const ScoreTile st = score_tile(a, b, part, score_queries(padded));
-    const int at_once = kScorePages / heads, step = blocks * at_once;
-    int base = blockIdx.x * at_once + warp / heads * 16;
-    if (base >= st.pages) return;
+    // `steps` times 16 pages a warp: CTAs of neighbouring pages, so that those of short requests end at once and the
+    // others have the same work
+    const int step = kScorePages / heads, first = blockIdx.x * step * steps;
+    const int pages = min(st.pages, first + step * steps);
+    int base = first + warp / heads * 16;
+    if (base >= pages) return;
     // a lane's pages are found two steps ahead, their codes loaded one step ahead
     int32_t page[2];
     PageCodes<D> next;
-    find_pages(a, b, base, st.pages, page);
+    find_pages(a, b, base, pages, page);
     next.load(a, page, h, c);
-    find_pages(a, b, base + step, st.pages, page);
+    find_pages(a, b, base + step, pages, page);
     for (int x = 0; x < 8 / padded; ++x)
         stage_query<D, FP8>(a, st.q0 + st.i0 + min(x, st.queries - 1), h, x < st.queries, padded, x * padded,
                             [&](int col, int ch, const float (&r)[4]) {
@@ -299,7 +187,7 @@ __global__ void __launch_bounds__(kScoreThreads, 4) pick_token_kernel(const __gr
     uint2 q[STEPS];
 #pragma unroll
     for (int k = 0; k < STEPS; ++k) q[k] = frag_s[warp][k][lane];
-    for (; base < st.pages; base += step) {
+    for (; base < pages; base += step) {
         int d[2][4] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
 #pragma unroll
         for (int k = 0; k < STEPS; k += 2) {
@@ -310,9 +198,9 @@ __global__ void __launch_bounds__(kScoreThreads, 4) pick_token_kernel(const __gr
         PageCodes<D> now;
 #pragma unroll
         for (int e = 0; e < 2; ++e) now.unit[e] = next.unit[e], now.there[e] = next.there[e];
-        if (base + step < st.pages) {
+        if (base + step < pages) {
             next.load(a, page, h, c);
-            find_pages(a, b, base + 2 * step, st.pages, page);
+            find_pages(a, b, base + 2 * step, pages, page);
         }
         float f[4], best[2] = {-INFINITY, -INFINITY};
 #pragma unroll
@@ -544,16 +432,18 @@ cudaError_t launch_scores(const PickArgs& a, int max_t, int max_pages, int num_s
     cudaError_t e = cudaSuccess;
     if (smem > 47 * 1024) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    // CTAs of a request's pages: 64 pages (with a head a warp 16) at a time, up to eight times where the CTAs fill the
-    // GPU all the same
+    // CTAs of a request's pages: those that have some are to be a round or two of what fits at once, as each takes as long
+    // to start as for three to five steps (32 caches of 30 Ki to 127 Ki tokens, one step of 64 pages in 32 for each CTA:
+    // 74 us)
     const int64_t others = (int64_t)parts * (a.hkv / heads) * a.batch;
     const int64_t steps = (max_pages + pages_at_once - 1) / pages_at_once;
-    const int64_t times = std::max<int64_t>(1, std::min<int64_t>(8, others * steps / (8 * (int64_t)num_sms)));
+    const int64_t places = (int64_t)num_sms * (tiles > 1 ? 3 : 4);
+    const int64_t times = std::max<int64_t>(1, std::min<int64_t>(steps, others * steps / (2 * places)));
     const int64_t blocks = (steps + times - 1) / times;
     cfg.gridDim = dim3((unsigned)blocks, (unsigned)(parts * (a.hkv / heads)), (unsigned)a.batch);
     cfg.blockDim = dim3(kScoreThreads, 1, 1);
     cfg.dynamicSmemBytes = smem;
-    return cudaLaunchKernelEx(&cfg, kern, a, (int)blocks);
+    return cudaLaunchKernelEx(&cfg, kern, a, (int)(tiles > 1 ? blocks : times));
 }
 
 }  // namespace
@@ -566,7 +456,8 @@ int64_t pick_key_stride(int64_t max_len, int page_shift, int budget)
 
 int pick_col_tiles(int64_t max_t, int group)
 {
-    const int per = score_queries(padded_group(group));
+    const int padded = padded_group(group);
+    const int per = max_t * padded > 64 ? pick_tile_queries(group) : score_queries(padded);
     return (int)((max_t + per - 1) / per);
 }
 
@@ -583,7 +474,9 @@ cudaError_t launch_cache_pick(const PickArgs& a, int head_dim, bool fp8, int max
     const int max_pages = (int)(((int64_t)max_len + (1 << a.page_shift) - 1) >> a.page_shift);
     cudaError_t e = cudaSuccess;
     if (a.key_stride > 0) {
-        e = fp8 ? launch_scores<128, true>(a, max_t, max_pages, num_sms, cfg)
+        const int64_t columns = (int64_t)max_t * padded_group(a.group);
+        if (columns > 64) e = launch_pick_tiles(a, head_dim, fp8, max_t, max_pages, num_sms, stream);
+        else e = fp8 ? launch_scores<128, true>(a, max_t, max_pages, num_sms, cfg)
                 : (head_dim == 128 ? launch_scores<128, false>(a, max_t, max_pages, num_sms, cfg)
                                    : launch_scores<64, false>(a, max_t, max_pages, num_sms, cfg));
         if (e != cudaSuccess) return e;

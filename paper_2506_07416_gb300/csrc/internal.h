@@ -284,6 +284,7 @@ struct PickArgs {
     int64_t key_stride;
     int32_t* picked;          // [rows][hkv][budget]
     int32_t* err;
+    long long wait_budget;
 };
 int64_t pick_key_stride(int64_t max_len, int page_shift, int budget);  // 0: no request has more pages than the budget
 int pick_col_tiles(int64_t max_t, int group);                          // CTAs of a request's queries

@@ -231,6 +231,14 @@ def pick_case(select, hq, hkv, d, dtype, page, lens, counts, budget, sink, recen
     (80, 1, 64, "bf16", 16, [400, 300], [2, 1], 4, 1, 1),                     # eighty: more columns than a CTA's usual
     (128, 1, 128, "bf16", 16, [300], [2], 4, 1, 1),
     (28, 4, 128, "bf16", 64, [9000], [70], 16, 1, 2),                         # a chunk of a prompt
+    (4, 4, 64, "bf16", 16, [3000, 129], [300, 65], 16, 1, 2),                 # ... with one head a key head
+    (4, 2, 128, "e4m3", 16, [5000, 140], [100, 140], 9, 0, 1),                # two, three, four
+    (6, 2, 64, "bf16", 32, [4111], [40], 5, 1, 1),
+    (16, 4, 128, "bf16", 16, [2100, 900], [33, 1], 12, 1, 2),
+    (18, 2, 128, "bf16", 16, [2500], [20], 7, 1, 1),                          # nine, twenty-four, eighty
+    (24, 1, 64, "bf16", 16, [2500, 60], [11, 3], 7, 1, 1),
+    (80, 1, 128, "bf16", 16, [2100], [5], 7, 1, 1),
+    (128, 1, 128, "e4m3", 16, [2100], [3], 7, 1, 1),
     (2, 2, 64, "bf16", 16, [50, 20], [50, 20], 2, 0, 1),                      # a whole prompt, from the first token on
     (8, 8, 128, "bf16", 16, [9000, 600], [1, 2], 20, 1, 2),                   # more than 512 pages
     (8, 2, 128, "bf16", 16, [70000, 100], [1, 1], 64, 1, 4),                  # more than 4096
