@@ -39,22 +39,20 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b.x), "r"(b.y));
 }
 
-// A lane's codes of two pages as they are in memory, their units and whether the pool has them.
+// A lane's codes of two pages as they are in memory, and their units.
 template <int D>
 struct PageCodes {
     uint4 w[2][2 * D / 64];
-    float unit[2];
-    bool there[2];
+    float unit[2];  // 0: none
 
     // pages p[0] and p[1] of the pool (-1: none): channels [c * 16, c * 16 + 16) of each 64
     __device__ __forceinline__ void load(const PickArgs& a, const int32_t (&p)[2], int h, int c)
     {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            there[e] = p[e] >= 0;
             const int64_t row = (int64_t)max(p[e], 0) * a.hkv + h;
             const int x = min(max((int)__ldg(a.exps + row), -100), 100);
-            unit[e] = __uint_as_float((uint32_t)(127 + x) << 23);
+            unit[e] = p[e] >= 0 ? __uint_as_float((uint32_t)(127 + x) << 23) : 0.f;
             const uint4* from = reinterpret_cast<const uint4*>(a.codes + row * 2 * D) + c;
 #pragma unroll
             for (int k = 0; k < 2 * D / 64; ++k) w[e][k] = __ldg(from + k * 4);
@@ -90,17 +88,16 @@ __device__ __forceinline__ void find_pages(const PickArgs& a, int b, int from, i
 }
 
 // Scores of a contraction's 16 pages (from `base` on) and a tile x of eight columns: d of page g and columns 2c and 2c + 1,
-// then of page g + 8. `best` carries the largest over the tiles of a query of more than eight heads.
-template <int D>
+// then of page g + 8; their units (0: the pool has no such page). `best` carries the largest over the tiles of a query of more than eight heads.
 __device__ __forceinline__ void store_scores(const PickArgs& a, const ScoreTile& st, int h, int padded, int base, int x,
-                                             const PageCodes<D>& now, const float (&d)[4], float (&best)[2])
+                                             const float (&unit)[2], const float (&d)[4], float (&best)[2])
 {
     const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
     auto put = [&](int i, int e, float s) {  // score of the CTA's query i and page g + 8 e
         const int o = base + g + 8 * e;
         if (i < st.queries && o < st.pages)
             a.keys[((int64_t)(st.q0 + st.i0 + i) * a.hkv + h) * a.key_stride + o] =
-                (e ? now.there[1] : now.there[0]) ? score_key(s * (e ? now.unit[1] : now.unit[0])) : 1u;
+                (e ? unit[1] : unit[0]) > 0.f ? score_key(s * (e ? unit[1] : unit[0])) : 1u;
     };
     if (padded == 1) {
         const int i = x * 8 + 2 * c;
@@ -139,46 +136,145 @@ __device__ __forceinline__ void mma16832(int (&d)[4], uint32_t a0, uint32_t a1, 
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b.x), "r"(b.y));
 }
 
-// Single tokens, and a few queries of few heads: one tile of columns. The codes go into the contraction as they are in
-// memory (s8: this GPU's slow kind, but a twentieth of the tile's time), the queries' whole numbers stay in
-// registers, and what is left bounds the kernel by memory. A warp has a key head of its own where there are enough, so
-// that a CTA reads neighbouring heads' codes of a page, which lie side by side, at the same time.
-template <int D, bool FP8>
-__global__ void __launch_bounds__(kScoreThreads, 4) pick_token_kernel(const __grid_constant__ PickArgs a, int steps)
+// Pages of request b whose scores are wanted.
+__device__ __forceinline__ int scored_pages(const PickArgs& a, int b)
 {
+    bool bad;
+    const int len = cache_len(__ldg(a.lens + b), a.limit, bad);
+    const int pages = len > 0 ? ((len - 1) >> a.page_shift) + 1 : 0;
+    return pages > a.budget && (a.single || __ldg(a.off + b + 1) > __ldg(a.off + b)) ? pages : 0;
+}
+// The requests' pages in equal chunks, a multiple of `unit`, so that there are no more than `slots` of them however the
+// lengths differ (at least one a request), and the chunk of this CTA: its request (a.batch: none) and its first page. Both
+// by a warp.
+__device__ __forceinline__ int score_chunk(const PickArgs& a, int slots, int unit)
+{
+    if (a.batch == 1) {
+        const int n = (scored_pages(a, 0) + slots - 1) / slots;
+        return max(unit, (n + unit - 1) / unit * unit);
+    }
+    const int lane = threadIdx.x & 31;
+    long long total = 0;
+    int some = 0;  // requests with pages
+    for (int b = lane; b < a.batch; b += 32) {
+        const int n = scored_pages(a, b);
+        total += n, some += n > 0;
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
+    some = __reduce_add_sync(0xffffffffu, some);
+    // sum of ceil(n / chunk) <= total / chunk + some
+    const long long per = (total + max(1, slots - some) - 1) / max(1, slots - some);
+    return (int)min((long long)kMostKeys, (per + unit - 1) / unit * unit);
+}
+__device__ __forceinline__ void find_chunk(const PickArgs& a, int chunk, int& b, int& first)
+{
+    if (a.batch == 1) {
+        b = 0;
+        first = (int)blockIdx.x * chunk;
+        return;
+    }
+    const int lane = threadIdx.x & 31;
+    int before = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += 32) {
+        const int pages = b0 + lane < a.batch ? scored_pages(a, b0 + lane) : 0;
+        const int n = pages > 0 ? (pages - 1) / chunk + 1 : 0;
+        int sum = n;  // inclusive
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, sum, d);
+            if (lane >= d) sum += y;
+        }
+        const uint32_t hit = __ballot_sync(0xffffffffu, (int)blockIdx.x < before + sum);
+        if (hit) {
+            const int x = __ffs(hit) - 1;
+            b = b0 + x;
+            first = ((int)blockIdx.x - before - __shfl_sync(0xffffffffu, sum - n, x)) * chunk;
+            return;
+        }
+        before += __shfl_sync(0xffffffffu, sum, 31);
+    }
+    b = a.batch;
+    first = 0;
+}
+
+// Single tokens, and a few queries of few heads: one tile of columns. The codes go into the contraction as they are in
+// memory (s8: this GPU's slow kind, a third of the time here, but f16 made of them took as many instructions again as
+// all else), the queries' whole numbers stay in registers. A warp has a key head of its own where there are enough, so
+// that a CTA reads neighbouring heads' codes of a page, which lie side by side, at the same time. Codes come by asynchronous
+// copies of whole rows: read into registers, a lane's 16 bytes of each of eight rows at a time, they came at 3 TB/s.
+template <int D>
+struct TokenRing {
+    static constexpr int ROW = 2 * D, STAGE = 16 * ROW, STAGES = 2;
+    // byte of 16-byte part x of row r: odd rows have their halves swapped, so that two rows' parts cover all banks
+    __device__ static __forceinline__ int at(int r, int x) { return r * ROW + (x ^ ((r & 1) << 2)) * 16; }
+};
+template <int D, bool FP8>
+__global__ void __launch_bounds__(kScoreThreads, 5) pick_token_kernel(const __grid_constant__ PickArgs a, int slots)
+{
+    using R = TokenRing<D>;
     constexpr int STEPS = 2 * D / 32;                       // contractions of 32 channels
     __shared__ uint2 frag_s[kScoreThreads / 32][STEPS][32];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = lane & 3;
-    const int heads = score_heads(a.hkv), groups = a.hkv / heads;  // heads of a CTA
-    const int h = blockIdx.y % groups * heads + warp % heads, part = blockIdx.y / groups, b = blockIdx.z;
+    __shared__ __align__(16) uint8_t ring_s[kScoreThreads / 32][R::STAGES * R::STAGE];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
+    const int heads = score_heads(a.hkv);  // of a CTA
+    const int h = blockIdx.y * heads + warp % heads, step = kScorePages / heads;
     griddep_wait();
     griddep_launch_dependents();
     const int padded = padded_group(a.group);
-    const ScoreTile st = score_tile(a, b, part, score_queries(padded));
-    // `steps` times 16 pages a warp: CTAs of neighbouring pages, so that those of short requests end at once and the
-    // others have the same work
-    const int step = kScorePages / heads, first = blockIdx.x * step * steps;
-    const int pages = min(st.pages, first + step * steps);
+    int b, first;
+    const int chunk = score_chunk(a, slots, step);
+    find_chunk(a, chunk, b, first);
+    if (b == a.batch) return;
+    const ScoreTile st = score_tile(a, b, 0, 8 / padded);
+    const int pages = min(st.pages, first + chunk);
     int base = first + warp / heads * 16;
     if (base >= pages) return;
-    // a lane's pages are found two steps ahead, their codes loaded one step ahead
-    int32_t page[2];
-    PageCodes<D> next;
-    find_pages(a, b, base, pages, page);
-    next.load(a, page, h, c);
-    find_pages(a, b, base + step, pages, page);
+
+    // page of row lane % 16 of the 16 pages from `from` on (-1: none), and its unit
+    auto find = [&](int from) -> int32_t {
+        const int o = from + (lane & 15);
+        if (o >= pages) return -1;
+        const int32_t p = cache_page(a.table, a.width, a.num_pages, a.page_shift, b, (int64_t)o << a.page_shift);
+        if (p < 0 && lane < 16) atomicOr(a.err, kErrBounds);
+        return p;
+    };
+    auto load = [&](int32_t page, int stage) -> float {
+        constexpr int LANES = R::ROW / 16, PER = 32 / LANES;
+        const int64_t row = (int64_t)max(page, 0) * a.hkv + h;
+        const uint32_t to = smem_u32(&ring_s[warp][stage * R::STAGE]);
+#pragma unroll
+        for (int i = 0; i < 16 / PER; ++i) {
+            const int r = i * PER + lane / LANES, x = lane % LANES;
+            const int64_t at = __shfl_sync(0xffffffffu, row, r);
+            copy_async16(to + R::at(r, x), a.codes + at * R::ROW + x * 16, true);
+        }
+        const int e = min(max((int)__ldg(a.exps + row), -100), 100);
+        return page >= 0 ? __uint_as_float((uint32_t)(127 + e) << 23) : 0.f;  // (0: none)
+    };
+    // two steps' codes are on their way, the page of the one behind them found
+    float unit[R::STAGES];
+    int32_t page = find(base);
+#pragma unroll
+    for (int u = 0; u < R::STAGES; ++u) {
+        unit[u] = load(page, u);
+        copy_async_commit();
+        page = find(base + (u + 1) * step);
+    }
     for (int x = 0; x < 8 / padded; ++x)
         stage_query<D, FP8>(a, st.q0 + st.i0 + min(x, st.queries - 1), h, x < st.queries, padded, x * padded,
                             [&](int col, int ch, const float (&r)[4]) {
                                 // channels [ch, ch + 4): word (ch % 16) / 4 of lane (ch / 16) % 4 and load ch / 64, two
                                 // words a contraction
                                 const int k = ch / 64 * 2 + ch % 16 / 8;
-                                uint32_t up = 0u, down = 0u;
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) {
-                                    up |= ((uint32_t)(int)fmaxf(r[i], 0.f) & 0xFFu) << (8 * i);
-                                    down |= ((uint32_t)(int)fminf(r[i], 0.f) & 0xFFu) << (8 * i);
-                                }
+                                uint32_t v;  // the four as bytes, then by their signs
+                                asm("{\n\t.reg .b32 t;\n\t"
+                                    "cvt.pack.sat.s8.s32.b32 t, %2, %1, 0;\n\t"
+                                    "cvt.pack.sat.s8.s32.b32 %0, %4, %3, t;\n\t}"
+                                    : "=r"(v)
+                                    : "r"((int)r[2]), "r"((int)r[3]), "r"((int)r[0]), "r"((int)r[1]));
+                                const uint32_t less = (v >> 7 & 0x01010101u) * 255u;
+                                const uint32_t up = v & ~less, down = v & less;
                                 uint2* to = &frag_s[warp][k][col * 4 + ch / 16 % 4];
                                 if (ch % 8) to[0].y = up, to[STEPS / 2 * 32].y = down;
                                 else to[0].x = up, to[STEPS / 2 * 32].x = down;
@@ -187,26 +283,37 @@ __global__ void __launch_bounds__(kScoreThreads, 4) pick_token_kernel(const __gr
     uint2 q[STEPS];
 #pragma unroll
     for (int k = 0; k < STEPS; ++k) q[k] = frag_s[warp][k][lane];
-    for (; base < pages; base += step) {
-        int d[2][4] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+    for (; base < pages; base += 2 * step) {
 #pragma unroll
-        for (int k = 0; k < STEPS; k += 2) {
-            const uint4 v = next.w[0][k / 2], w = next.w[1][k / 2];
-            mma16832(d[0], v.x, w.x, v.y, w.y, q[k]);
-            mma16832(d[1], v.z, w.z, v.w, w.w, q[k + 1]);
+        for (int u = 0; u < R::STAGES; ++u) {
+            const int from = base + u * step;
+            if (from >= pages) break;
+            copy_async_wait<R::STAGES - 1>();
+            __syncwarp();
+            const uint8_t* ring = &ring_s[warp][u * R::STAGE];
+            int d[2][4] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+#pragma unroll
+            for (int k = 0; k < STEPS; k += 2) {
+                const uint4 v = *reinterpret_cast<const uint4*>(ring + R::at(g, k / 2 * 4 + c));
+                const uint4 w = *reinterpret_cast<const uint4*>(ring + R::at(g + 8, k / 2 * 4 + c));
+                mma16832(d[0], v.x, w.x, v.y, w.y, q[k]);
+                mma16832(d[1], v.z, w.z, v.w, w.w, q[k + 1]);
+            }
+            const float now = unit[u];
+            __syncwarp();  // (every lane has read the stage)
+            if (from + 2 * step < pages) {
+                unit[u] = load(page, u);
+                page = find(from + 3 * step);
+            }
+            copy_async_commit();
+            const float units[2] = {__shfl_sync(0xffffffffu, now, g), __shfl_sync(0xffffffffu, now, g + 8)};
+            float f[4], best[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[i] = (float)(d[0][i] + d[1][i]);
+            store_scores(a, st, h, padded, from, 0, units, f, best);
         }
-        PageCodes<D> now;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) now.unit[e] = next.unit[e], now.there[e] = next.there[e];
-        if (base + step < pages) {
-            next.load(a, page, h, c);
-            find_pages(a, b, base + 2 * step, pages, page);
-        }
-        float f[4], best[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) f[i] = (float)(d[0][i] + d[1][i]);
-        store_scores<D>(a, st, h, padded, base, 0, now, f, best);
     }
+    copy_async_wait<0>();
 }
 
 // Some queries: up to eight tiles of columns (more for a query of more than 64 heads), four at a time, chains of
@@ -267,7 +374,7 @@ __global__ void __launch_bounds__(kScoreThreads, 3) pick_score_kernel(const __gr
                     mma16816(d[u], f[k], frag_s[(min(x0 + u, tiles - 1) * STEPS + k) * 32 + lane]);
 #pragma unroll
             for (int u = 0; u < GROUP; ++u)
-                if (x0 + u < tiles) store_scores<D>(a, st, h, padded, base, x0 + u, now, d[u], best);
+                if (x0 + u < tiles) store_scores(a, st, h, padded, base, x0 + u, now.unit, d[u], best);
         }
     }
 }
@@ -423,27 +530,30 @@ __global__ void __launch_bounds__(WARPS == 1 ? 128 : 32 * WARPS) pick_select_ker
 template <int D, bool FP8>
 cudaError_t launch_scores(const PickArgs& a, int max_t, int max_pages, int num_sms, cudaLaunchConfig_t cfg)
 {
-    const int padded = padded_group(a.group), per = score_queries(padded);
-    const int parts = (max_t + per - 1) / per;
-    const int tiles = (std::min(per, max_t) * padded + 7) / 8;
-    auto kern = tiles > 1 ? pick_score_kernel<D, FP8> : pick_token_kernel<D, FP8>;
-    const int heads = tiles > 1 ? 1 : score_heads(a.hkv), pages_at_once = kScorePages / heads;
-    const size_t smem = tiles > 1 ? (size_t)tiles * (2 * D / 16) * 32 * sizeof(uint2) : 0;
-    cudaError_t e = cudaSuccess;
-    if (smem > 47 * 1024) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
-    // CTAs of a request's pages: those that have some are to be a round or two of what fits at once, as each takes as long
-    // to start as for three to five steps (32 caches of 30 Ki to 127 Ki tokens, one step of 64 pages in 32 for each CTA:
-    // 74 us)
-    const int64_t others = (int64_t)parts * (a.hkv / heads) * a.batch;
-    const int64_t steps = (max_pages + pages_at_once - 1) / pages_at_once;
-    const int64_t places = (int64_t)num_sms * (tiles > 1 ? 3 : 4);
-    const int64_t times = std::max<int64_t>(1, std::min<int64_t>(steps, others * steps / (2 * places)));
-    const int64_t blocks = (steps + times - 1) / times;
-    cfg.gridDim = dim3((unsigned)blocks, (unsigned)(parts * (a.hkv / heads)), (unsigned)a.batch);
+    const int padded = padded_group(a.group);
     cfg.blockDim = dim3(kScoreThreads, 1, 1);
-    cfg.dynamicSmemBytes = smem;
-    return cudaLaunchKernelEx(&cfg, kern, a, (int)(tiles > 1 ? blocks : times));
+    if (max_t * padded <= 8) {  // one tile of columns
+        const int groups = a.hkv / score_heads(a.hkv), step = kScorePages / score_heads(a.hkv);
+        // as many CTAs as run at once: each takes as long to start as for ten steps
+        const int64_t slots = std::max<int64_t>(2 * (int64_t)a.batch, (int64_t)num_sms * 5 / groups);
+        cfg.gridDim = dim3((unsigned)std::min<int64_t>(slots, (int64_t)a.batch * ((max_pages + step - 1) / step)),
+                           (unsigned)groups, 1);
+        return cudaLaunchKernelEx(&cfg, pick_token_kernel<D, FP8>, a, (int)cfg.gridDim.x);
+    }
+    const int per = score_queries(padded), parts = (max_t + per - 1) / per;
+    const int tiles = (std::min(per, max_t) * padded + 7) / 8;
+    auto kern = pick_score_kernel<D, FP8>;
+    cfg.dynamicSmemBytes = (size_t)tiles * (2 * D / 16) * 32 * sizeof(uint2);
+    cudaError_t e = cudaSuccess;
+    if (cfg.dynamicSmemBytes > 48 * 1024)
+        e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes);
+    if (e != cudaSuccess) return e;
+    // CTAs of a request's pages: 64 pages at a time, two rounds of what runs at once
+    const int64_t others = (int64_t)parts * a.hkv * a.batch, steps = (max_pages + kScorePages - 1) / kScorePages;
+    const int64_t times = std::max<int64_t>(1, std::min<int64_t>(steps, others * steps / (2 * 3 * (int64_t)num_sms)));
+    const int64_t blocks = (steps + times - 1) / times;
+    cfg.gridDim = dim3((unsigned)blocks, (unsigned)(parts * a.hkv), (unsigned)a.batch);
+    return cudaLaunchKernelEx(&cfg, kern, a, (int)blocks);
 }
 
 }  // namespace

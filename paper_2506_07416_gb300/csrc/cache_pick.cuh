@@ -40,7 +40,7 @@ __device__ __forceinline__ void query_values(const uint4& v, float (&x)[FP8 ? 16
 #pragma unroll
     for (int i = 0; i < (FP8 ? 16 : 8); ++i) {
         if (x[i] != x[i]) x[i] = 0.f;
-        x[i] = fminf(fmaxf(x[i], -0x1.FEp127f), 0x1.FEp127f);
+        if constexpr (!FP8) x[i] = fminf(fmaxf(x[i], -0x1.FEp127f), 0x1.FEp127f);
     }
 }
 
@@ -63,10 +63,18 @@ __device__ __forceinline__ void stage_query(const PickArgs& a, int64_t row, int 
     const uint8_t* from =
         static_cast<const uint8_t*>(a.q) + (row * a.q_stride + (int64_t)h * a.group * D) * (FP8 ? 1 : 2);
     auto load = [&](int y) { return __ldg(reinterpret_cast<const uint4*>(from + (int64_t)y * D * (FP8 ? 1 : 2)) + sub); };
+    if (!real) {
+        const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int y = first; y < padded; y += step)
+#pragma unroll
+            for (int e = 0; e < E; e += 4) store(col0 + y, sub * E + e, zero);
+        return;
+    }
     uint4 kept[U];  // the first rows stay in registers between the two passes
     float top = 0.f;
 #pragma unroll
-    for (int u = 0; u < U; ++u) kept[u] = real ? load(min(first + u * step, a.group - 1)) : make_uint4(0u, 0u, 0u, 0u);
+    for (int u = 0; u < U; ++u)
+        if (u * step < padded) kept[u] = load(min(first + u * step, a.group - 1));
     auto reach = [&](const uint4& w) {
         float v[E];
         query_values<FP8>(w, v);
@@ -74,9 +82,9 @@ __device__ __forceinline__ void stage_query(const PickArgs& a, int64_t row, int 
         for (int e = 0; e < E; ++e) top = fmaxf(top, fabsf(v[e]));
     };
 #pragma unroll
-    for (int u = 0; u < U; ++u) reach(kept[u]);
-    if (real)
-        for (int y = first + U * step; y < a.group; y += step) reach(load(y));
+    for (int u = 0; u < U; ++u)
+        if (u * step < padded) reach(kept[u]);
+    for (int y = first + U * step; y < a.group; y += step) reach(load(y));
     top = warp_max_f32(top);
     // top = f * 2^p, f in [1/2, 1); the unit is 2^(p - 7)
     const int p = max((int)(__float_as_uint(top) >> 23) - 126, -119);
@@ -96,7 +104,7 @@ __device__ __forceinline__ void stage_query(const PickArgs& a, int64_t row, int 
     for (int u = 0; u < U; ++u)
         if (first + u * step < padded) put(kept[u], first + u * step);  // (behind the last head: that one again)
     for (int y = first + U * step; y < padded; y += step)
-        put(real ? load(min(y, a.group - 1)) : make_uint4(0u, 0u, 0u, 0u), y);
+        put(load(min(y, a.group - 1)), y);
 }
 
 // What a CTA scores: queries [i0, i0 + queries) of its request, over the pages that the last of them sees (none: nothing to
