@@ -9,7 +9,7 @@
 // column for each query head of a key head (a query's columns padded to a power of two or whole tiles of eight). A warp
 // keeps 16 pages as the M rows (m16n8k16; codes become f16 in registers, a channel order of the lanes' own) and
 // goes over the columns' tiles in shared memory.
-// pick_select_kernel: the budget-th largest score of a query by halving the bits that its scores differ in, then the
+// pick_select_kernel: the budget-th largest score of a query by counting its scores in buckets, then the
 // pages above it and the lowest of those at it, in order.
 
 #include <algorithm>
@@ -263,7 +263,7 @@ __global__ void __launch_bounds__(kScoreThreads, 5) pick_token_kernel(const __gr
     }
     for (int x = 0; x < 8 / padded; ++x)
         stage_query<D, FP8>(a, st.q0 + st.i0 + min(x, st.queries - 1), h, x < st.queries, padded, x * padded,
-                            [&](int col, int ch, const float (&r)[4]) {
+                            [&](int col, int ch, __half2 r0, __half2 r1) {
                                 // channels [ch, ch + 4): word (ch % 16) / 4 of lane (ch / 16) % 4 and load ch / 64, two
                                 // words a contraction
                                 const int k = ch / 64 * 2 + ch % 16 / 8;
@@ -272,7 +272,8 @@ __global__ void __launch_bounds__(kScoreThreads, 5) pick_token_kernel(const __gr
                                     "cvt.pack.sat.s8.s32.b32 t, %2, %1, 0;\n\t"
                                     "cvt.pack.sat.s8.s32.b32 %0, %4, %3, t;\n\t}"
                                     : "=r"(v)
-                                    : "r"((int)r[2]), "r"((int)r[3]), "r"((int)r[0]), "r"((int)r[1]));
+                                    : "r"(__half2int_rn(__low2half(r1))), "r"(__half2int_rn(__high2half(r1))),
+                                      "r"(__half2int_rn(__low2half(r0))), "r"(__half2int_rn(__high2half(r0))));
                                 const uint32_t less = (v >> 7 & 0x01010101u) * 255u;
                                 const uint32_t up = v & ~less, down = v & less;
                                 uint2* to = &frag_s[warp][k][col * 4 + ch / 16 % 4];
@@ -340,15 +341,13 @@ __global__ void __launch_bounds__(kScoreThreads, 3) pick_score_kernel(const __gr
     find_pages(a, b, base + step, st.pages, page);
     for (int x = warp; x < tiles * 8 / padded; x += kScoreThreads / 32)  // (zeros behind the last query)
         stage_query<D, FP8>(a, st.q0 + st.i0 + min(x, st.queries - 1), h, x < st.queries, padded, x * padded,
-                            [&](int col, int ch, const float (&r)[4]) {
+                            [&](int col, int ch, __half2 r0, __half2 r1) {
                                 // channels [ch, ch + 4): word (ch % 16) / 4 of lane (ch / 16) % 4 and load ch / 64
                                 const int k = ch / 64 * 4 + ch % 16 / 4;
                                 uint2* to = frag_s + ((col >> 3) * STEPS + k) * 32 + (col & 7) * 4 + ch / 16 % 4;
-                                const auto pack = [](float s, float u) { return h2_bits(__floats2half2_rn(s, u)); };
-                                to[0] = make_uint2(pack(fmaxf(r[0], 0.f), fmaxf(r[1], 0.f)),
-                                                   pack(fmaxf(r[2], 0.f), fmaxf(r[3], 0.f)));
-                                to[STEPS / 2 * 32] = make_uint2(pack(fminf(r[0], 0.f), fminf(r[1], 0.f)),
-                                                                pack(fminf(r[2], 0.f), fminf(r[3], 0.f)));
+                                const __half2 zero = bits_h2(0u);
+                                to[0] = make_uint2(h2_bits(__hmax2(r0, zero)), h2_bits(__hmax2(r1, zero)));
+                                to[STEPS / 2 * 32] = make_uint2(h2_bits(__hmin2(r0, zero)), h2_bits(__hmin2(r1, zero)));
                             });
     __syncthreads();
     for (; base < st.pages; base += step) {
@@ -386,7 +385,8 @@ template <int WARPS>
 __global__ void __launch_bounds__(WARPS == 1 ? 128 : 32 * WARPS) pick_select_kernel(const __grid_constant__ PickArgs a)
 {
     constexpr int T = 32 * WARPS;
-    __shared__ int count_s[3][4];
+    constexpr int BITS = WARPS == 1 ? 6 : 8, BUCKETS = 1 << BITS;
+    __shared__ int count_s[WARPS == 1 ? 4 * BUCKETS : BUCKETS];
     __shared__ uint32_t range_s[2][WARPS];
     __shared__ int before_s[2][WARPS];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tid = WARPS == 1 ? lane : threadIdx.x;
@@ -440,57 +440,10 @@ __global__ void __launch_bounds__(WARPS == 1 ? 128 : 32 * WARPS) pick_select_ker
     low = __reduce_min_sync(0xffffffffu, low);
     if constexpr (WARPS > 1) {
         if (lane == 0) range_s[0][warp] = top, range_s[1][warp] = low;
-        if (tid < 12) count_s[tid / 4][tid & 3] = 0;
         __syncthreads();
 #pragma unroll 1
         for (int w = 0; w < WARPS; ++w) top = max(top, range_s[0][w]), low = min(low, range_s[1][w]);
     }
-    // ---- the largest x that at least `budget` keys reach, two bits a step, from the first bit that they differ in
-    int at_x = 0;  // keys that reach x
-    uint32_t x = low;
-    {
-        const int forced = a.sink + a.recent;
-        int left = 32 - (top > low ? __clz(top ^ low) : 32);  // bits that are open
-        if (forced >= a.budget) x = 0xFFFFFFFFu, left = 0;
-        else x = left < 32 ? low >> left << left : 0u;
-        at_x = forced >= a.budget ? a.budget : pages;
-        int turn = 0;
-        while (left > 0 && at_x != a.budget) {
-            const int bits = WARPS > 1 && left >= 2 ? 2 : 1;
-            left -= bits;
-            const uint32_t x1 = x + (1u << left), x2 = x + (2u << left), x3 = x + (3u << left);
-            int c1 = 0, c2 = 0, c3 = 0;
-#pragma unroll
-            for (int i = 0; i < kKeep; ++i) {
-                if (i >= steps) break;
-                c1 += k[i] >= x1;
-                if (WARPS > 1) c2 += k[i] >= x2, c3 += k[i] >= x3;
-            }
-            for (int i = kKeep; i < steps; ++i) {
-                const uint32_t v = key_at(first + i * 32 + lane);
-                c1 += v >= x1;
-                if (WARPS > 1) c2 += v >= x2, c3 += v >= x3;
-            }
-            c1 = __reduce_add_sync(0xffffffffu, c1);
-            if (WARPS > 1) c2 = __reduce_add_sync(0xffffffffu, c2), c3 = __reduce_add_sync(0xffffffffu, c3);
-            if constexpr (WARPS > 1) {
-                int* to = count_s[turn];
-                if (lane < 3) atomicAdd(to + lane, lane == 0 ? c1 : (lane == 1 ? c2 : c3));
-                const int clear = turn == 2 ? 0 : turn + 1;
-                __syncthreads();
-                c1 = to[0], c2 = to[1], c3 = to[2];
-                if (tid < 3) count_s[clear == 2 ? 0 : clear + 1][tid] = 0;
-                turn = clear;
-            }
-            if (bits == 2 && c3 >= a.budget) x = x3, at_x = c3;
-            else if (bits == 2 && c2 >= a.budget) x = x2, at_x = c2;
-            else if (c1 >= a.budget) x = x1, at_x = c1;
-        }
-    }
-    // ---- keys above x, and the first of those at it (where x was reached by `budget` keys: all that reach it)
-    const bool exact = at_x == a.budget;
-    const uint32_t above = exact ? x - 1u : x;
-    int mine = 0, ties = 0;  // of this warp
     auto visit = [&](auto f) {
 #pragma unroll
         for (int i = 0; i < kKeep; ++i) {
@@ -499,6 +452,58 @@ __global__ void __launch_bounds__(WARPS == 1 ? 128 : 32 * WARPS) pick_select_ker
         }
         for (int i = kKeep; i < steps; ++i) f(first + i * 32 + lane, key_at(first + i * 32 + lane));
     };
+    // ---- x, which the budget's keys reach: the keys between the smallest and the largest counted in buckets of a power
+    // of two, the bucket that the budget ends in counted in finer ones, and so on (two or three times)
+    int want = a.budget - a.sink - a.recent;  // of the keys that are not picked anyway
+    uint32_t x = 0xFFFFFFFFu;
+    bool exact = true;  // all that reach x are taken
+    if (want > 0) {
+        uint32_t lo = low, hi = top;
+        int* bucket = count_s + (WARPS == 1 ? warp * BUCKETS : 0);
+        auto sync = [&]() {
+            if constexpr (WARPS == 1) __syncwarp();
+            else __syncthreads();
+        };
+        for (;;) {
+            const int shift = max(0, 32 - __clz(hi - lo) - BITS);
+            for (int i = tid; i < BUCKETS; i += T) bucket[i] = 0;
+            sync();
+            visit([&](int, uint32_t v) {
+                if (v >= lo && v <= hi) atomicAdd(bucket + ((v - lo) >> shift), 1);
+            });
+            sync();
+            // by every warp: lane i has the buckets [i * PER, (i + 1) * PER), counted from the last one down
+            constexpr int PER = BUCKETS / 32;
+            int mine[PER], sum = 0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) mine[i] = bucket[lane * PER + i], sum += mine[i];
+            int from = sum;  // of this lane's buckets and those behind them
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int y = __shfl_down_sync(0xffffffffu, from, d);
+                if (lane + d < 32) from += y;
+            }
+            int above = from - sum, at = -1, in = 0;
+#pragma unroll
+            for (int i = PER - 1; i >= 0; --i) {
+                if (at < 0 && above < want && above + mine[i] >= want) at = lane * PER + i, in = mine[i];
+                if (at < 0) above += mine[i];
+            }
+            const int who = __ffs(__ballot_sync(0xffffffffu, at >= 0)) - 1;
+            at = __shfl_sync(0xffffffffu, at, who);
+            in = __shfl_sync(0xffffffffu, in, who);
+            want -= __shfl_sync(0xffffffffu, above, who);
+            lo += (uint32_t)at << shift;
+            x = lo;
+            exact = in == want;
+            if (exact || shift == 0) break;
+            hi = lo + ((1u << shift) - 1u);
+            sync();  // (the counts have been read)
+        }
+    }
+    // ---- keys above x, and the first of those at it (where x was reached by `budget` keys: all that reach it)
+    const uint32_t above = exact ? x - 1u : x;
+    int mine = 0, ties = 0;  // of this warp
     visit([&](int, uint32_t v) {
         mine += __popc(__ballot_sync(0xffffffffu, v > above));
         ties += exact ? 0 : __popc(__ballot_sync(0xffffffffu, v == x));

@@ -84,14 +84,15 @@ __global__ void __launch_bounds__(kPickThreads, 1) pick_tile_kernel(const __grid
     if (warp < kMmaWarp) {
         for (int x = warp; x < kCols / padded; x += kMmaWarp)  // (zeros behind the last query)
             stage_query<D, FP8>(a, st.q0 + st.i0 + min(x, st.queries - 1), h, x < st.queries, padded, x * padded,
-                                [&](int col, int ch, const float (&r)[4]) {
-                                    const auto put = [&](int k, float r0, float r1, float r2, float r3) {
+                                [&](int col, int ch, __half2 r0, __half2 r1) {
+                                    const auto put = [&](int k, __half2 v0, __half2 v1) {
                                         uint2* to = reinterpret_cast<uint2*>(smem + L::Q + (k >> 6) * kAtom + col * 128 +
                                                                              ((((k >> 3) & 7) ^ (col & 7)) << 4) + (k & 7) * 2);
-                                        *to = make_uint2(h2_bits(__floats2half2_rn(r0, r1)), h2_bits(__floats2half2_rn(r2, r3)));
+                                        *to = make_uint2(h2_bits(v0), h2_bits(v1));
                                     };
-                                    put(ch, fmaxf(r[0], 0.f), fmaxf(r[1], 0.f), fmaxf(r[2], 0.f), fmaxf(r[3], 0.f));
-                                    put(D + ch, fminf(r[0], 0.f), fminf(r[1], 0.f), fminf(r[2], 0.f), fminf(r[3], 0.f));
+                                    const __half2 zero = bits_h2(0u);
+                                    put(ch, __hmax2(r0, zero), __hmax2(r1, zero));
+                                    put(D + ch, __hmin2(r0, zero), __hmin2(r1, zero));
                                 });
         fence_proxy_async_shared();
     }
