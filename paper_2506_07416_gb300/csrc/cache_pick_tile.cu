@@ -80,6 +80,24 @@ __global__ void __launch_bounds__(kPickThreads, 1) pick_tile_kernel(const __grid
     auto find = [&](int64_t o) -> int32_t {
         return o < st.pages ? cache_page(a.table, a.width, a.num_pages, a.page_shift, b, o << a.page_shift) : -1;
     };
+    // ---- of the code warps w the pages [16 w, 16 w + 16) of a tile: a load takes whole pages, 16 channels of largest or
+    // smallest a lane; the first tile's are on their way while the queries are laid out
+    constexpr int LANES = 2 * D / 16, PER = 32 / LANES, LOADS = 16 / PER;  // lanes of a page, pages a load
+    const int w = warp - kOutWarps, sub = lane % LANES, at = lane / LANES;
+    uint4 next[LOADS];
+    int32_t found = -1;  // page of row lane % 16
+    auto load = [&]() {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int32_t p = __shfl_sync(0xffffffffu, found, i * PER + at);
+            next[i] = __ldg(reinterpret_cast<const uint4*>(a.codes + ((int64_t)max(p, 0) * a.hkv + h) * 2 * D) + sub);
+        }
+    };
+    if (warp >= kOutWarps && warp < kMmaWarp) {
+        found = find(first_page(0) + w * 16 + (lane & 15));
+        load();
+        if (mine > 1) found = find(first_page(1) + w * 16 + (lane & 15));
+    }
     // ---- the queries: column n of the operand is row n, channel ch its K index (and D + ch)
     if (warp < kMmaWarp) {
         for (int x = warp; x < kCols / padded; x += kMmaWarp)  // (zeros behind the last query)
@@ -154,20 +172,6 @@ __global__ void __launch_bounds__(kPickThreads, 1) pick_tile_kernel(const __grid
         }
     } else if (warp < kMmaWarp) {
         // ---------------------------------------------------------------- codes to f16
-        // of warp w the pages [16 w, 16 w + 16) of a tile: a load takes whole pages, 16 channels of largest or smallest a lane
-        constexpr int LANES = 2 * D / 16, PER = 32 / LANES, LOADS = 16 / PER;  // lanes of a page, pages a load
-        const int w = warp - kOutWarps, sub = lane % LANES, at = lane / LANES;
-        uint4 next[LOADS];
-        int32_t page = find(first_page(0) + w * 16 + (lane & 15));
-        auto load = [&]() {
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                const int32_t p = __shfl_sync(0xffffffffu, page, i * PER + at);
-                next[i] = __ldg(reinterpret_cast<const uint4*>(a.codes + ((int64_t)max(p, 0) * a.hkv + h) * 2 * D) + sub);
-            }
-        };
-        load();
-        if (mine > 1) page = find(first_page(1) + w * 16 + (lane & 15));
         // (of eight neighbouring lanes the first four write their first 16 bytes first, the others their second, so that
         // they cover all banks)
         const int k0 = sub * 16, unit0 = (k0 >> 3) & 7, swap = (sub >> 2) & 1;
@@ -194,7 +198,7 @@ __global__ void __launch_bounds__(kPickThreads, 1) pick_tile_kernel(const __grid
             __syncwarp();
             if (lane == 0) mbar_arrive(BAR(P_A_FULL + stage));
             if (n + 1 < mine) load();
-            if (n + 2 < mine) page = find(first_page(n + 2) + w * 16 + (lane & 15));
+            if (n + 2 < mine) found = find(first_page(n + 2) + w * 16 + (lane & 15));
         }
     } else {
         // ---------------------------------------------------------------- contractions

@@ -61,6 +61,8 @@ __global__ void __launch_bounds__(kThreads) reserve_kernel(const __grid_constant
         if (blockIdx.x == 0 && tid == 0) atomicOr(a.err, kErrBounds);
         head = 0, count = -1;
     }
+    // place x from the head on, x < total (a 64-bit remainder took 3 us of a decoding step's call)
+    auto ring = [&](int64_t x) { return head + x < total ? head + x : head + x - total; };
     long long taken = 0, given = 0;  // by the requests before
     int64_t used = 0;
     for (int b0 = 0; b0 < a.batch; b0 += threads) {
@@ -103,26 +105,30 @@ __global__ void __launch_bounds__(kThreads) reserve_kernel(const __grid_constant
         }
         taken += all.x, given += all.y;
         __syncthreads();
-        // ---- pages, a request a warp
-        const int step = (threads >> 5) * gridDim.x;
-        for (int x = (tid >> 5) * gridDim.x + blockIdx.x; x < n; x += step) {
+        // ---- pages: the few that most requests of a step take or give by the request's thread, more by a warp
+        const int64_t step = (int64_t)(threads >> 5) * gridDim.x;
+        auto move = [&](int x, int o0, int by) {
             const int hp = has_s[x], np = need_s[x];
             int32_t* row = a.table + (int64_t)(b0 + x) * a.width;
             if (np > hp) {
-                for (int o = hp + lane; o < np; o += 32) {
-                    const int32_t p = __ldg(a.free + (head + from_s[x] + o - hp) % total);
+                for (int o = hp + o0; o < np; o += by) {
+                    const int32_t p = __ldg(a.free + ring(from_s[x] + o - hp));
                     if (p < 0 || p >= total) atomicOr(a.err, kErrBounds);
                     row[o] = p;
                 }
             } else if (np >= 0 && count >= 0) {
-                for (int o = np + lane; o < hp; o += 32) {
+                for (int o = np + o0; o < hp; o += by) {
                     const int64_t to = from_s[x] + o - np;
                     const int32_t p = row[o];
                     if (p < 0 || p >= total || to >= total) atomicOr(a.err, kErrBounds);
-                    if (to < total) a.free[(head + to) % total] = p;
+                    if (to < total) a.free[ring(to)] = p;
                 }
             }
-        }
+        };
+        constexpr int kFewPages = 2;
+        if (tid < n && tid % gridDim.x == blockIdx.x && abs(need_s[tid] - has_s[tid]) <= kFewPages) move(tid, 0, 1);
+        for (int x = (tid >> 5) * gridDim.x + blockIdx.x; x < n; x += (int)step)
+            if (abs(need_s[x] - has_s[x]) > kFewPages) move(x, lane, 32);
         // ---- slots: a warp takes 256 neighbouring tokens, whose pages' numbers are all on their way at once
         const int64_t r0 = max(off_s[0], 0), r1 = min((int64_t)off_s[n], a.rows);
         constexpr int U = 8;
@@ -146,7 +152,7 @@ __global__ void __launch_bounds__(kThreads) reserve_kernel(const __grid_constant
                 if (pos < 0) continue;
                 const int o = (int)(pos >> a.page_shift);
                 p[u] = o < has_s[x] ? __ldg(a.table + (int64_t)(b0 + x) * a.width + o)
-                                    : __ldg(a.free + (head + from_s[x] + o - has_s[x]) % total);
+                                    : __ldg(a.free + ring(from_s[x] + o - has_s[x]));
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
