@@ -1467,7 +1467,7 @@ litevlm_status_t picked_plan(litevlm_select_t h, int32_t batch, const int32_t* q
         return fail(h, LITEVLM_ERR_UNSUPPORTED, "the queries or the heads exceed the grid");
     if ((double)p.tiles * (double)hkv * ((double)p.list_cap * 16.0 + (double)p.queries * p.list_words * 4.0) > 0x1p60)
         return fail(h, LITEVLM_ERR_UNSUPPORTED, "the workspace would pass 2^60 bytes");
-    const int64_t parts = p.chunks > 1 ? p.tiles * p.chunks * hkv * p.queries * group : 0, lists = p.lists ? p.tiles * hkv : 0;
+    const int64_t parts = p.chunks > 1 && !p.cluster ? p.tiles * p.chunks * hkv * p.queries * group : 0, lists = p.lists ? p.tiles * hkv : 0;
     space->part_o = 0;
     space->part_ml = round256(parts * c.head_dim * 4);
     space->lists = space->part_ml + round256(parts * 8);

@@ -221,14 +221,16 @@ constexpr int kRingBytes = kAttWarps * kAttStages * 2 * Group<D>::kBytes;
 // which keeps addresses out of the lanes' registers: the sweep's 128 requests take 127 us
 // and not 135).
 // (CTAs of an SM as the plan of the split counts them.)
-enum class Picked { kNone, kQuery, kTile };
+enum class Picked { kNone, kQuery, kTile, kQueryCluster, kTileCluster };  // (the chunks of a list are a cluster's CTAs)
+constexpr int kPickCluster = 8;  // chunks of a list that a cluster joins, at most
 // PICKED: the keys are those of picked pages, and a CTA's rows are those of one query, over the pages of its own list, or
 // of a tile of queries, over the list of the pages that any of them has (a key of a page that a row's query has not is as
 // masked); a CTA takes all of the list or a chunk of it.
 template <int D, int NT_, bool FP8, bool WHOLE, Picked PICK = Picked::kNone>
 __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_kernel(const __grid_constant__ AttendArgs a)
 {
-    constexpr bool PICKED = PICK != Picked::kNone, LISTS = PICK == Picked::kTile;
+    constexpr bool PICKED = PICK != Picked::kNone, LISTS = PICK == Picked::kTile || PICK == Picked::kTileCluster;
+    constexpr bool CLUSTER = PICK == Picked::kQueryCluster || PICK == Picked::kTileCluster;
     constexpr bool SINGLE = NT_ == 0;
     constexpr int NT = SINGLE ? 1 : NT_;
     using G = Group<D>;
@@ -237,6 +239,10 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
     // the rings; behind the loop the same memory takes a row tile of every warp's sums
     constexpr int kRing = kRingBytes<D>, kJoin = kAttWarps * 8 * (D + 4) * 4;
     static_assert(kRing >= kJoin, "the sums fit the rings");
+    // CLUSTER: the CTA's own sums behind them
+    constexpr int kOut = ROWS * D * 4;
+    static_assert(!CLUSTER || kRing >= kJoin + kOut, "the CTA's sums fit the rings, too");
+    __shared__ float2 ml_s[CLUSTER ? ROWS : 1];
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ float s_m[kAttWarps][ROWS], s_l[kAttWarps][ROWS];
 
@@ -784,7 +790,10 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
                     if ((a.cache.scales[1][at_row * (D / 16) + ch / 16] & 0x7Fu) == 0x7Fu) O = __int_as_float(0x7FC00000);
                 }
             }
-            if (PICKED ? a.pick_chunks == 1 : WHOLE || a.slots == 0) {
+            if (CLUSTER) {
+                jo[kJoin / 4 + row * D + ch] = O;
+                if (ch == 0) ml_s[row] = make_float2(M, L);
+            } else if (PICKED ? a.pick_chunks == 1 : WHOLE || a.slots == 0) {
                 // (a row that sees no key is 0; the comparison keeps a NaN sum)
                 a.out[at * D + ch] = __float2bfloat16_rn(L == 0.f ? 0.f : O / L * a.cache.scale[1]);
                 if (a.lse && ch == 0) a.lse[at] = L == 0.f ? INFINITY : M + log2f(L);
@@ -794,6 +803,38 @@ __global__ void __launch_bounds__(kAttThreads, NT_ == 2 ? 3 : 4) attend_split_ke
                 if (ch == 0) a.part_ml[part] = make_float2(M, L);
             }
         }
+    }
+    if constexpr (CLUSTER) {
+        // the chunks of a list are a cluster's CTAs: each joins a part of the rows from all CTAs' shared memory
+        cluster_sync_all();
+        const uint32_t n = cluster_nctarank();
+        for (int x = (int)cluster_ctarank() * kAttThreads + tid; x < rt.rows * D / 2; x += (int)n * kAttThreads) {
+            const int row = 2 * x / D;
+            const uint32_t at_ml = smem_u32(&ml_s[row]), at_o = smem_u32(jo + kJoin / 4 + 2 * x);
+            float2 ml[kPickCluster], o[kPickCluster];
+            float M = kNoRef;
+#pragma unroll
+            for (uint32_t r = 0; r < kPickCluster; ++r)
+                if (r < n) {
+                    ml[r] = ld_shared_cluster_f2(mapa_shared(at_ml, r));
+                    o[r] = ld_shared_cluster_f2(mapa_shared(at_o, r));
+                    M = fmaxf(M, ml[r].x);
+                }
+            float L = 0.f, O0 = 0.f, O1 = 0.f;
+#pragma unroll
+            for (uint32_t r = 0; r < kPickCluster; ++r)
+                if (r < n) {
+                    const float f = ex2(ml[r].x - M);
+                    L += ml[r].y * f;
+                    O0 += o[r].x * f, O1 += o[r].y * f;
+                }
+            const int rr = rt.row0 + row, i = rt.query(rr);
+            const int64_t to = ((int64_t)(q0 + i) * a.hq + h * a.group + rr - i * a.group) * D + 2 * x % D;
+            const float f = a.cache.scale[1] / L;
+            *reinterpret_cast<__nv_bfloat162*>(a.out + to) =
+                __floats2bfloat162_rn(L == 0.f ? 0.f : O0 * f, L == 0.f ? 0.f : O1 * f);
+        }
+        cluster_sync_all();  // (no CTA ends while another reads its memory)
     }
 }
 
@@ -1328,7 +1369,7 @@ template <int D, bool FP8>
 cudaError_t launch_picked(const AttendArgs& a, const PickedPlan& plan, int64_t queries, cudaStream_t stream, int32_t* launches)
 {
     cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute attr[1] = {pdl_attribute()};
+    cudaLaunchAttribute attr[2] = {pdl_attribute()};
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     cfg.stream = stream;
@@ -1347,17 +1388,30 @@ cudaError_t launch_picked(const AttendArgs& a, const PickedPlan& plan, int64_t q
         cfg.gridDim = dim3((unsigned)(plan.tiles * plan.chunks), (unsigned)(subs * a.cache.hkv), 1);
         cfg.blockDim = dim3(kAttThreads, 1, 1);
         cfg.dynamicSmemBytes = kRingBytes<D>;
-        constexpr Picked Q = Picked::kQuery, T = Picked::kTile;
-        auto kern = plan.lists ? (plan.row_tile == 8 ? attend_split_kernel<D, 1, FP8, false, T>
-                                                     : attend_split_kernel<D, 2, FP8, false, T>)
-                    : a.group == 1 ? attend_split_kernel<D, 0, FP8, false, Q>
-                                   : (plan.row_tile == 8 ? attend_split_kernel<D, 1, FP8, false, Q>
-                                                         : attend_split_kernel<D, 2, FP8, false, Q>);
+        auto pick = [&](auto q, auto t) {
+            constexpr Picked Q = decltype(q)::value, T = decltype(t)::value;
+            return plan.lists ? (plan.row_tile == 8 ? attend_split_kernel<D, 1, FP8, false, T>
+                                                    : attend_split_kernel<D, 2, FP8, false, T>)
+                   : a.group == 1 ? attend_split_kernel<D, 0, FP8, false, Q>
+                                  : (plan.row_tile == 8 ? attend_split_kernel<D, 1, FP8, false, Q>
+                                                        : attend_split_kernel<D, 2, FP8, false, Q>);
+        };
+        using Own = std::integral_constant<Picked, Picked::kQuery>;
+        using Tile = std::integral_constant<Picked, Picked::kTile>;
+        using OwnC = std::integral_constant<Picked, Picked::kQueryCluster>;
+        using TileC = std::integral_constant<Picked, Picked::kTileCluster>;
+        auto kern = plan.cluster ? pick(OwnC{}, TileC{}) : pick(Own{}, Tile{});
+        if (plan.cluster) {
+            attr[1].id = cudaLaunchAttributeClusterDimension;
+            attr[1].val.clusterDim = {(unsigned)plan.chunks, 1, 1};
+            cfg.numAttrs = 2;
+        }
         e = cudaLaunchKernelEx(&cfg, kern, a);
+        cfg.numAttrs = 1;
     }
     if (e != cudaSuccess) return e;
     ++*launches;
-    if (plan.chunks > 1) {
+    if (plan.chunks > 1 && !plan.cluster) {
         const int64_t rows = queries * a.hq;
         cfg.gridDim = dim3((unsigned)((rows + kAttWarps - 1) / kAttWarps), 1, 1);
         cfg.blockDim = dim3(kAttThreads, 1, 1);
@@ -1373,7 +1427,9 @@ cudaError_t launch_picked(const AttendArgs& a, const PickedPlan& plan, int64_t q
 // A call of single tokens has a tile for each query, with the pages of its own list. Else neighbouring queries of a
 // request, which mostly have the same pages, share a tile of up to 16, 128 or 256 rows and read its pages once.
 // Tiles of 128 rows from 17 rows of the longest request on: 24 and 32 rows of 32 requests, 32 / 8 heads, 48 pages of 32,
-// 85 and 90 us where tiles of 16 take 158 and 174; 12 and 16 rows 76 and 82 with either.
+// 84 and 89 us where tiles of 16 take 158 and 174; 12 and 16 rows 76 and 82 with either. Up to 32 rows tiles of 16 all
+// the same where a tile of 128 for each request and head left seven eighths of its places empty: four queries of one
+// request, 28 / 4 heads, 32 pages of 64, 25 us (128 rows: 33), of eight 27 (29); 30 of four, 16 heads, 47 (41).
 // The lists are split where the tiles alone leave the GPU's places empty: as for whole requests, n chunks take
 // rounds / n of the list and the writing and joining of a chunk's sums. A shared list is taken to grow by half of a
 // query's own for each doubling of the queries: of 32 pages each, picked as neighbours mostly agree on, 18 queries
@@ -1387,7 +1443,10 @@ PickedPlan plan_attend_picked(int batch, int hkv, int group, const int32_t* q_of
     for (int b = 0; b < batch; ++b) max_t = std::max(max_t, q_off[b + 1] - q_off[b]);
     const int64_t max_rows = (int64_t)max_t * group;
     p.lists = max_t > 1;
-    p.row_tile = p.lists ? (max_rows <= 8 ? 8 : (max_rows <= 16 ? 16 : (max_rows <= 128 ? 128 : 256))) : (group <= 8 ? 8 : 16);
+    int active = 0;
+    for (int b = 0; b < batch; ++b) active += q_off[b + 1] > q_off[b];
+    const int64_t few = max_rows <= 32 && (int64_t)active * hkv * 4 <= num_sms ? 32 : 16;
+    p.row_tile = p.lists ? (max_rows <= 8 ? 8 : (max_rows <= few ? 16 : (max_rows <= 128 ? 128 : 256))) : (group <= 8 ? 8 : 16);
     p.queries = p.lists ? std::max(1, p.row_tile / group) : 1;
     int64_t keys = (int64_t)budget << page_shift;
     const int64_t subs = ((int64_t)p.queries * group + p.row_tile - 1) / p.row_tile;
@@ -1414,8 +1473,11 @@ PickedPlan plan_attend_picked(int batch, int hkv, int group, const int32_t* q_of
             if (c < cost) cost = c, best = n;
         }
     }
+    // chunks of few rows are joined within a cluster where it holds them: a launch less, and no sums in memory
+    p.cluster = !many && best > 1 && best <= kPickCluster;
     p.chunk = (int32_t)(((keys + best - 1) / best + 31) & ~31ll);
     p.chunks = (int32_t)(p.lists ? best : std::max<int64_t>(1, (keys + p.chunk - 1) / p.chunk));
+    if (p.chunks == 1) p.cluster = false;
     return p;
 }
 

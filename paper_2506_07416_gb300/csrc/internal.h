@@ -214,6 +214,7 @@ struct PickedPlan {
     bool lists;               // the queries of a tile share a list
     int64_t tiles;            // of all requests (without lists: the queries)
     int32_t chunk, chunks, list_cap, list_words;
+    bool cluster;             // the chunks of a tile are joined by a cluster of CTAs
 };
 PickedPlan plan_attend_picked(int batch, int hkv, int group, const int32_t* q_off, int page_shift, int width, int budget,
                               int num_sms);
