@@ -464,6 +464,9 @@ litevlm_status_t litevlm_select_set_wait_budget(litevlm_select_t handle, int64_t
  * LITEVLM_DEBUG_STALL_ATTEND: in the launches of litevlm_select_cache_attend for many
  * rows (more than 32 a key head), the values of the second 128 keys (the only ones) are never made,
  * so that the launch gives up with contractions in flight; the same report.
+ * LITEVLM_DEBUG_STALL_PICK: in the launches of litevlm_select_cache_pick for many columns (more than 64 a request and key
+ * head), the codes of a CTA's second 128 pages (the only ones) are never made; the same report, and the picked pages are
+ * not valid. LITEVLM_DEBUG_STALL_ATTEND also holds for litevlm_select_cache_attend_picked.
  * Nothing faults, traps or hangs: each wait is bounded by the budget. flags = 0
  * restores normal operation. Errors: INVALID_ARG for a NULL handle or an
  * unknown flag.
@@ -471,6 +474,7 @@ litevlm_status_t litevlm_select_set_wait_budget(litevlm_select_t handle, int64_t
 #define LITEVLM_DEBUG_STALL_SCORE 1
 #define LITEVLM_DEBUG_STALL_PROJECT 4
 #define LITEVLM_DEBUG_STALL_ATTEND 8
+#define LITEVLM_DEBUG_STALL_PICK 16
 litevlm_status_t litevlm_select_set_debug_flags(litevlm_select_t handle, int32_t flags);
 
 /*

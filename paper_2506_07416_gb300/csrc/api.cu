@@ -1223,7 +1223,8 @@ litevlm_status_t litevlm_select_set_debug_flags(litevlm_select_t h, int32_t flag
     const CallRange range_(__func__);
     if (!h) return LITEVLM_ERR_INVALID_ARG;
     h->last_error.clear();
-    if (flags & ~(LITEVLM_DEBUG_STALL_SCORE | LITEVLM_DEBUG_STALL_PROJECT | LITEVLM_DEBUG_STALL_ATTEND))
+    if (flags & ~(LITEVLM_DEBUG_STALL_SCORE | LITEVLM_DEBUG_STALL_PROJECT | LITEVLM_DEBUG_STALL_ATTEND |
+                  LITEVLM_DEBUG_STALL_PICK))
         return fail(h, LITEVLM_ERR_INVALID_ARG, "unknown debug flag");
     h->debug_flags = flags;
     return LITEVLM_OK;
@@ -1563,6 +1564,16 @@ litevlm_status_t litevlm_select_cache_bounds(litevlm_select_t h, int32_t batch, 
     s = cache_pages(h, cache, table, table_width, seq_lens, &a.cache, &a.limit);
     if (s == LITEVLM_OK) s = check_bounds(h, bounds);
     if (s != LITEVLM_OK) return s;
+    {
+        const int64_t pages = (int64_t)cache->num_pages * h->cfg.num_kv_heads, row = (int64_t)cache->page_size * h->cfg.head_dim;
+        const int64_t codes = pages * 2 * h->cfg.head_dim;
+        if (overlap(bounds->codes, codes, bounds->exps, pages) ||
+            overlap(bounds->codes, codes, cache->k_codes, pages * row / 2) ||
+            overlap(bounds->codes, codes, cache->k_scales, pages * row / 16) ||
+            overlap(bounds->exps, pages, cache->k_codes, pages * row / 2) ||
+            overlap(bounds->exps, pages, cache->k_scales, pages * row / 16))
+            return fail(h, LITEVLM_ERR_INVALID_ARG, "the ranges must not overlap the cache or one another");
+    }
     if (bounds->num_pages != cache->num_pages || bounds->page_size != cache->page_size)
         return fail(h, LITEVLM_ERR_INVALID_ARG, "the ranges and the cache have different pages");
     if (!new_offsets_d) return fail(h, LITEVLM_ERR_INVALID_ARG, "a device pointer is NULL");
@@ -1654,6 +1665,7 @@ litevlm_status_t litevlm_select_cache_pick(litevlm_select_t h, int32_t batch, co
     a.single = max_t == 1 && a.rows == batch;
     a.keys = static_cast<uint32_t*>(workspace);
     a.picked = picked;
+    a.stall = (h->debug_flags & LITEVLM_DEBUG_STALL_PICK) != 0;
     a.err = h->err_d;
     a.wait_budget = h->wait_budget;
     const OnDevice on(h->device);
@@ -1712,6 +1724,9 @@ litevlm_status_t litevlm_select_cache_attend_picked(litevlm_select_t h, int32_t 
     if (overlap_rows(out, total * row * 2, q, total, q_row_stride, row, c.qk_dtype == LITEVLM_FP8_E4M3 ? 1 : 2) ||
         overlap(out, total * row * 2, picked, total * c.num_kv_heads * budget * 4))
         return fail(h, LITEVLM_ERR_INVALID_ARG, "out must not overlap q or picked");
+    if (overlap(workspace, space.total, out, total * row * 2) ||
+        overlap(workspace, space.total, picked, total * c.num_kv_heads * budget * 4))
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "the workspace must not overlap out or picked");
     s = check_workspace(h, workspace, workspace_bytes, space.total);
     if (s == LITEVLM_OK) s = debug_mirror(h, q_offsets_d, q_offsets_h, (int64_t)batch + 1, "q_offsets", stream);
     if (s != LITEVLM_OK) return s;

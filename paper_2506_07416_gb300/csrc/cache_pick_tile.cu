@@ -177,6 +177,7 @@ __global__ void __launch_bounds__(kPickThreads, 1) pick_tile_kernel(const __grid
         const int k0 = sub * 16, unit0 = (k0 >> 3) & 7, swap = (sub >> 2) & 1;
         for (int n = 0; n < mine; ++n) {
             const int stage = n & 1;
+            if (a.stall && n == min(1, mine - 1)) break;
             if (n >= 2 && !poll_phase_warp(BAR(P_A_FREE + stage), (uint32_t)(n / 2 - 1) & 1u, ctl)) break;
             const uint32_t to = base + L::A + stage * L::ROWS + (k0 >> 6) * kAtom;
 #pragma unroll

@@ -181,7 +181,7 @@ cudaError_t launch_cache_reserve(const ReserveArgs& a, int num_sms, cudaStream_t
 {
     // a CTA for every 2048 slots or 128 requests, no more than one an SM; small batches in small CTAs, whose scan is short
     const int threads = a.batch <= 128 ? 128 : (a.batch <= 256 ? 256 : kThreads);
-    const int64_t ctas = std::max<int64_t>((a.rows + 2047) / 2048, (a.batch + 127) / 128);
+    const int64_t ctas = std::max<int64_t>({1, (a.rows + 2047) / 2048, (a.batch + 127) / 128});
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)std::min<int64_t>(ctas, num_sms), 1, 1);
     cfg.blockDim = dim3((unsigned)threads, 1, 1);

@@ -476,7 +476,8 @@ static PyObject *f_row_stride(PyObject *self, PyObject *const *args, Py_ssize_t 
             v[3 + k] = PyLong_AsLongLong(PyTuple_GET_ITEM(strides, k));
         }
         const long long heads = PyLong_AsLongLong(args[3]), d = PyLong_AsLongLong(args[4]);
-        if (v[1] == heads && v[2] == d && v[5] == 1 && (heads == 1 || v[4] == d)) stride = v[0] > 1 ? v[3] : heads * d;
+        if (v[1] == heads && v[2] == d && (v[0] == 0 || (v[5] == 1 && (heads == 1 || v[4] == d))))
+            stride = v[0] > 1 ? v[3] : heads * d; /* (of no rows any stride will do) */
     }
 done:
     Py_XDECREF(shape);

@@ -284,6 +284,7 @@ struct PickArgs {
     uint32_t* keys;           // [rows][hkv][key_stride] scores in an order of whole numbers
     int64_t key_stride;
     int32_t* picked;          // [rows][hkv][budget]
+    int32_t stall;            // debug: the codes of a CTA's second pages are never made
     int32_t* err;
     long long wait_budget;
 };

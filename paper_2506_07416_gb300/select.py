@@ -446,6 +446,7 @@ def set_wait_budget(handle: int, cycles: int) -> None:
 DEBUG_STALL_SCORE = 1
 DEBUG_STALL_PROJECT = 4
 DEBUG_STALL_ATTEND = 8
+DEBUG_STALL_PICK = 16
 
 
 def set_debug_flags(handle: int, flags: int) -> None:
@@ -978,12 +979,12 @@ class Selector:
                 picked = torch.empty((total, self.kv_heads, budget), dtype=torch.int32, device=q.device)
             else:
                 _want("picked", picked, torch.int32, (total, self.kv_heads, budget), dev)
-            if workspace is None:
+            if workspace is not None:
+                need = _want("workspace", workspace, torch.uint8, (-1,), dev).shape[0]
+            elif need:
                 workspace = self._workspace(need, stream, q.device)
-            else:
-                _want("workspace", workspace, torch.uint8, (-1,), dev)
         cache_pick(self.handle, batch, bounds.struct, table, table.shape[1], seq_lens, q, stride, offsets, off_h, max_len,
-                   budget, sink, recent, picked, workspace, workspace.shape[0], _stream_on(stream, dev))
+                   budget, sink, recent, picked, workspace, need, _stream_on(stream, dev))
         return picked
 
     def cache_attend_picked(self, cache: KVCache, table, seq_lens, q, offsets, picked, q_scale: float = 1.0,
@@ -1006,12 +1007,12 @@ class Selector:
                 out = torch.empty((total, self.heads, self.head_dim), dtype=torch.bfloat16, device=q.device)
             else:
                 _want("out", out, torch.bfloat16, (total, self.heads, self.head_dim), dev)
-            if workspace is None:
+            if workspace is not None:
+                need = _want("workspace", workspace, torch.uint8, (-1,), dev).shape[0]
+            elif need:
                 workspace = self._workspace(need, stream, q.device)
-            else:
-                _want("workspace", workspace, torch.uint8, (-1,), dev)
         cache_attend_picked(self.handle, batch, cache.struct, table, table.shape[1], seq_lens, q, stride, offsets, off_h,
-                            picked, budget, q_scale, out, workspace, workspace.shape[0], _stream_on(stream, dev))
+                            picked, budget, q_scale, out, workspace, need, _stream_on(stream, dev))
         return out
 
     def verify(self, draft_tokens, target_probs, u_accept, u_sample, offsets, draft_probs=None, offsets_h=None,

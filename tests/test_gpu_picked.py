@@ -355,7 +355,7 @@ def attend_case(select, hq, hkv, d, dtype, page, lens, counts, budget, seed=0, s
     s.check_device()
     want, slack = pref.attend(c, table, lens, qv, off, picked)
     assert np.isfinite(got).all()
-    worst = np.max(np.abs(got - want) - slack)
+    worst = np.max(np.abs(got - want) - slack, initial=-np.inf)
     assert worst <= 0, worst
     s.close()
 
@@ -388,6 +388,36 @@ def test_attend_picked_of_lists_that_leave_nothing(select, hq, hkv, counts):
     picked[::2, 0] = [9, 50, 1 << 29, -1]   # no page that a query sees
     picked[1::2, hkv - 1, 2] = 0            # one page
     attend_case(select, hq, hkv, 128, "bf16", 16, lens, counts, budget, seed=3, picked=picked)
+
+
+@pytest.mark.parametrize("hq,hkv,counts", [(8, 2, [0, 3, 0, 1]), (8, 2, [0, 1, 0, 0]), (28, 4, [0, 90, 0, 7]),
+                                           (2, 2, [0, 0, 0, 0])])
+def test_requests_without_queries_take_no_part(select, hq, hkv, counts):
+    lens = [300, 200, 0, 77]
+    attend_case(select, hq, hkv, 64, "bf16", 16, lens, counts, 5, seed=1)
+    pick_case(select, hq, hkv, 64, "bf16", 16, lens, counts, 3, 1, 1, seed=2)
+
+
+@pytest.mark.parametrize("hq,hkv,count", [(4, 4, 1), (4, 4, 3), (14, 2, 3), (16, 2, 30)])
+def test_attend_picked_over_more_pages_than_a_window(select, hq, hkv, count):
+    """More than 65536 pages: the shared lists are made a window of them at a time. The request's pages are the same
+    fifty again and again (shared pages are allowed where they are only read)."""
+    rng = np.random.default_rng(15)
+    page, pages, pool, budget, d = 16, 140000, 50, 6, 64
+    n = pages * page - 5
+    table = rng.integers(0, pool, (1, pages)).astype(np.int32)
+    c, off = random_pool(rng, pool, hkv, page, d), offsets([count])
+    q, qv, _ = make_q(rng, count, hq, d, "bf16")
+    picked = rng.integers(0, pages - 1, (count, hkv, budget)).astype(np.int32)
+    picked[:, :, 0] = pages - 1
+    picked[:, :, 1] = rng.integers(65500, 65600, (count, hkv))
+    picked[:, :, 2] = rng.integers(0, 3, (count, hkv))
+    s = select.Selector(1, 8, 8, hq, hkv, d, "bf16")
+    got = s.cache_attend_picked(to_cache(select, c), i32(table), i32([n]), q, i32(off), i32(picked), offsets_h=off)
+    s.check_device()
+    want, slack = pref.attend(c, table, [n], qv, off, picked)
+    assert (np.abs(got.double().cpu().numpy() - want) <= slack).all()
+    s.close()
 
 
 def test_attend_picked_of_flat_and_of_strong_scores(select):
