@@ -401,6 +401,42 @@ static PyObject *f_attend_bytes(PyObject *self, PyObject *const *args, Py_ssize_
 /* fits(tensor, dtype, device index, sizes...): whether it is a contiguous tensor of this type on this CUDA device with
  * these sizes (-1: any). Written out in Python the checks of a call's tensors took half of its time. */
 static PyObject *g_dtype, *g_get_device, *g_shape, *g_is_contiguous;
+static int tensor_fits(PyObject *t, PyObject *dtype, PyObject *device, PyObject *const *sizes, Py_ssize_t n)
+{
+    int ok = 0;
+    PyObject *r = PyObject_GetAttr(t, g_dtype);
+    if (!r) goto other;
+    ok = r == dtype;
+    Py_DECREF(r);
+    if (!ok) return 0;
+    ok = 0;
+    r = PyObject_CallMethodNoArgs(t, g_get_device);
+    if (!r) goto other;
+    ok = PyLong_Check(r) && PyLong_Check(device) && PyLong_AsLong(r) == PyLong_AsLong(device);
+    Py_DECREF(r);
+    if (!ok) return 0;
+    ok = 0;
+    r = PyObject_GetAttr(t, g_shape);
+    if (!r) goto other;
+    if (PyTuple_Check(r) && PyTuple_GET_SIZE(r) == n) {
+        ok = 1;
+        for (Py_ssize_t k = 0; k < n && ok; ++k) {
+            const long long want = PyLong_AsLongLong(sizes[k]);
+            ok = want < 0 || PyLong_AsLongLong(PyTuple_GET_ITEM(r, k)) == want;
+        }
+    }
+    Py_DECREF(r);
+    if (PyErr_Occurred()) goto other;
+    if (!ok) return 0;
+    r = PyObject_CallMethodNoArgs(t, g_is_contiguous);
+    if (!r) goto other;
+    ok = r == Py_True;
+    Py_DECREF(r);
+    return ok;
+other: /* no tensor: the caller says what is wrong */
+    PyErr_Clear();
+    return 0;
+}
 static PyObject *f_fits(PyObject *self, PyObject *const *args, Py_ssize_t n)
 {
     (void)self;
@@ -408,41 +444,24 @@ static PyObject *f_fits(PyObject *self, PyObject *const *args, Py_ssize_t n)
         PyErr_SetString(PyExc_TypeError, "fits takes a tensor, a type, a device and sizes");
         return NULL;
     }
-    int ok = 0;
-    PyObject *t = args[0], *r = PyObject_GetAttr(t, g_dtype);
-    if (!r) goto other;
-    ok = r == args[1];
-    Py_DECREF(r);
-    if (!ok) goto done;
-    ok = 0;
-    r = PyObject_CallMethodNoArgs(t, g_get_device);
-    if (!r) goto other;
-    ok = PyLong_Check(r) && PyLong_Check(args[2]) && PyLong_AsLong(r) == PyLong_AsLong(args[2]);
-    Py_DECREF(r);
-    if (!ok) goto done;
-    ok = 0;
-    r = PyObject_GetAttr(t, g_shape);
-    if (!r) goto other;
-    if (PyTuple_Check(r) && PyTuple_GET_SIZE(r) == n - 3) {
-        ok = 1;
-        for (Py_ssize_t k = 0; k < n - 3 && ok; ++k) {
-            const long long want = PyLong_AsLongLong(args[3 + k]);
-            ok = want < 0 || PyLong_AsLongLong(PyTuple_GET_ITEM(r, k)) == want;
+    return PyBool_FromLong(tensor_fits(args[0], args[1], args[2], args + 3, n - 3));
+}
+
+/* all_fit(device index, dtype, (tensor, number of sizes, sizes...)...): whether every tensor fits; a decoding step's calls
+ * check four to six */
+static PyObject *f_all_fit(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    (void)self;
+    int ok = n >= 2;
+    for (Py_ssize_t k = 2; k < n && ok;) {
+        const Py_ssize_t sizes = k + 1 < n && PyLong_Check(args[k + 1]) ? PyLong_AsSsize_t(args[k + 1]) : -1;
+        if (sizes < 0 || k + 2 + sizes > n) {
+            PyErr_SetString(PyExc_TypeError, "all_fit takes a device, a type, and tensors with their numbers of sizes");
+            return NULL;
         }
+        ok = tensor_fits(args[k], args[1], args[0], args + k + 2, sizes);
+        k += 2 + sizes;
     }
-    Py_DECREF(r);
-    if (PyErr_Occurred()) goto other;
-    if (!ok) goto done;
-    ok = 0;
-    r = PyObject_CallMethodNoArgs(t, g_is_contiguous);
-    if (!r) goto other;
-    ok = r == Py_True;
-    Py_DECREF(r);
-    goto done;
-other: /* no tensor: the caller says what is wrong */
-    PyErr_Clear();
-    ok = 0;
-done:
     return PyBool_FromLong(ok);
 }
 
@@ -597,7 +616,7 @@ static PyMethodDef kMethods[] = {DEF("bind", f_bind), DEF("score", f_score), DEF
                                  DEF("cache_reserve", f_reserve), DEF("cache_bounds", f_bounds),
                                  DEF("pick_bytes", f_pick_bytes), DEF("cache_pick", f_pick),
                                  DEF("picked_bytes", f_picked_bytes), DEF("cache_attend_picked", f_picked),
-                                 DEF("fits", f_fits), DEF("row_stride", f_row_stride), {NULL, NULL, 0, NULL}};
+                                 DEF("fits", f_fits), DEF("all_fit", f_all_fit), DEF("row_stride", f_row_stride), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_fastcall", NULL, -1, kMethods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__fastcall(void)

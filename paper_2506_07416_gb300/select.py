@@ -905,7 +905,12 @@ class Selector:
                     _stream_on(stream, dev))
         return kept_idx, new_lens
 
-    # ---- its pages: who has them, and attention over some of them
+    # ---- its pages: who has them, and attention over some of them. Their tensors are checked in one call where all fit
+    # (the single checks then say what does not): of a decoding step's calls the host's part is the longer one.
+
+    def _pages_fit(self, pages, kind, dev: int) -> bool:
+        return type(pages) is kind and pages.device == dev and pages.heads == self.kv_heads and \
+            pages.head_dim == self.head_dim
 
     def cache_reserve(self, table, held, want, free, state, page_size: int, offsets, offsets_h=None, granted=None,
                       new_state=None, slots=None, stream=None):
@@ -915,28 +920,28 @@ class Selector:
         ring had too few pages; the ring's new state; slots int64 of the new tokens, -1 for those that were not granted)."""
         import torch
         off_h = _host_i32(offsets if offsets_h is None else offsets_h)
-        batch, total, dev = len(off_h) - 1, int(off_h[-1]), self.device
-        _want("table", table, torch.int32, (batch, -1), dev)
-        _want("held", held, torch.int32, (batch,), dev)
-        _want("want", want, torch.int32, (batch,), dev)
-        _want("free", free, torch.int32, (-1,), dev)
-        _want("state", state, torch.int32, (2,), dev)
-        _want("offsets", offsets, torch.int32, (batch + 1,), dev)
-        with _allocate_on(stream, dev):
-            if granted is None:
-                granted = torch.empty_like(held)
-            else:
-                _want("granted", granted, torch.int32, (batch,), dev)
-            if new_state is None:
-                new_state = torch.empty_like(state)
-            else:
-                _want("new_state", new_state, torch.int32, (2,), dev)
-            if slots is None:
-                slots = torch.empty(total, dtype=torch.int64, device=held.device)
-            else:
-                _want("slots", slots, torch.int64, (total,), dev)
-        cache_reserve(self.handle, batch, page_size, table, table.shape[1], held, want, free, free.shape[0], state, offsets,
-                      off_h, granted, new_state, slots, _stream_on(stream, dev))
+        batch, total, dev, i32 = len(off_h) - 1, int(off_h[-1]), self.device, torch.int32
+        if not _FC.all_fit(dev, i32, table, 2, batch, -1, held, 1, batch, want, 1, batch, free, 1, -1, state, 1, 2, offsets, 1,
+                           batch + 1):
+            _want("table", table, i32, (batch, -1), dev)
+            _want("held", held, i32, (batch,), dev)
+            _want("want", want, i32, (batch,), dev)
+            _want("free", free, i32, (-1,), dev)
+            _want("state", state, i32, (2,), dev)
+            _want("offsets", offsets, i32, (batch + 1,), dev)
+        if granted is None and new_state is None and slots is None and stream is None:
+            granted, new_state = torch.empty_like(held), torch.empty_like(state)
+            slots = torch.empty(total, dtype=torch.int64, device=held.device)
+        else:
+            with _allocate_on(stream, dev):
+                granted = torch.empty_like(held) if granted is None else _want("granted", granted, i32, (batch,), dev)
+                new_state = torch.empty_like(state) if new_state is None else _want("new_state", new_state, i32, (2,), dev)
+                slots = torch.empty(total, dtype=torch.int64, device=held.device) if slots is None else \
+                    _want("slots", slots, torch.int64, (total,), dev)
+        rc = _FC.cache_reserve(self.handle, batch, page_size, table, table.shape[1], held, want, free, free.shape[0], state,
+                               offsets, off_h, granted, new_state, slots, _stream_on(stream, dev))
+        if rc:
+            _check(rc, self.handle)
         return granted, new_state, slots
 
     def key_bounds(self, cache: KVCache) -> KeyBounds:
@@ -951,13 +956,30 @@ class Selector:
         ``seq_lens`` with them), from all tokens of these pages."""
         import torch
         off_h = _host_i32(offsets if offsets_h is None else offsets_h)
-        batch = len(off_h) - 1
-        dev = self._cache_call(cache, table, seq_lens, batch)
-        self._cache_call(bounds, table, seq_lens, batch, KeyBounds)
-        _want("offsets", offsets, torch.int32, (batch + 1,), dev)
-        cache_bounds(self.handle, batch, cache.struct, bounds.struct, table, table.shape[1], seq_lens, offsets, off_h,
-                     _stream_on(stream, dev))
+        batch, dev = len(off_h) - 1, self.device
+        if not (self._pages_fit(cache, KVCache, dev) and self._pages_fit(bounds, KeyBounds, dev) and
+                _FC.all_fit(dev, torch.int32, table, 2, batch, -1, seq_lens, 1, batch, offsets, 1, batch + 1)):
+            self._cache_call(cache, table, seq_lens, batch)
+            self._cache_call(bounds, table, seq_lens, batch, KeyBounds)
+            _want("offsets", offsets, torch.int32, (batch + 1,), dev)
+        rc = _FC.cache_bounds(self.handle, batch, cache.struct, bounds.struct, table, table.shape[1], seq_lens, offsets, off_h,
+                              _stream_on(stream, dev))
+        if rc:
+            _check(rc, self.handle)
         return bounds
+
+    def _queries(self, pages, kind, table, seq_lens, q, offsets, batch: int, total: int, dev: int) -> int:
+        """The row stride of q, the other tensors of a call on cached pages checked."""
+        import torch
+        stride = _FC.row_stride(q, self._element(), dev, self.heads, self.head_dim)
+        if stride < 0 or q.shape[0] != total or not self._pages_fit(pages, kind, dev) or \
+                not _FC.all_fit(dev, torch.int32, table, 2, batch, -1, seq_lens, 1, batch, offsets, 1, batch + 1):
+            self._cache_call(pages, table, seq_lens, batch, kind)
+            _want("offsets", offsets, torch.int32, (batch + 1,), dev)
+            stride = _row_stride("q", q, self._element(), self.heads, self.head_dim, dev)
+            if q.shape[0] != total:
+                _refuse(f"q has {q.shape[0]} rows, the offsets {total}")
+        return stride
 
     def cache_pick(self, bounds: KeyBounds, table, seq_lens, q, offsets, max_len: int, budget: int, sink: int = 0,
                    recent: int = 0, offsets_h=None, picked=None, workspace=None, stream=None):
@@ -967,24 +989,27 @@ class Selector:
         ``cache_pick_workspace`` bytes that no other call in flight uses."""
         import torch
         off_h = _host_i32(offsets if offsets_h is None else offsets_h)
-        batch, total = len(off_h) - 1, int(off_h[-1])
-        dev = self._cache_call(bounds, table, seq_lens, batch, KeyBounds)
-        _want("offsets", offsets, torch.int32, (batch + 1,), dev)
-        stride = _row_stride("q", q, self._element(), self.heads, self.head_dim, dev)
-        if q.shape[0] != total:
-            _refuse(f"q has {q.shape[0]} rows, the offsets {total}")
-        need = cache_pick_workspace(self.handle, batch, off_h, max_len, bounds.page_size, budget)
-        with _allocate_on(stream, dev):
-            if picked is None:
-                picked = torch.empty((total, self.kv_heads, budget), dtype=torch.int32, device=q.device)
-            else:
-                _want("picked", picked, torch.int32, (total, self.kv_heads, budget), dev)
-            if workspace is not None:
-                need = _want("workspace", workspace, torch.uint8, (-1,), dev).shape[0]
-            elif need:
-                workspace = self._workspace(need, stream, q.device)
-        cache_pick(self.handle, batch, bounds.struct, table, table.shape[1], seq_lens, q, stride, offsets, off_h, max_len,
-                   budget, sink, recent, picked, workspace, need, _stream_on(stream, dev))
+        batch, total, dev = len(off_h) - 1, int(off_h[-1]), self.device
+        stride = self._queries(bounds, KeyBounds, table, seq_lens, q, offsets, batch, total, dev)
+        need = _FC.pick_bytes(self.handle, batch, off_h, max_len, bounds.page_size, budget)
+        if need < 0:
+            _check(-need, self.handle)
+        if picked is None and workspace is None and stream is None:
+            picked = torch.empty((total, self.kv_heads, budget), dtype=torch.int32, device=q.device)
+            if need:
+                workspace = self._workspace(need, None, q.device)
+        else:
+            with _allocate_on(stream, dev):
+                picked = torch.empty((total, self.kv_heads, budget), dtype=torch.int32, device=q.device) if picked is None \
+                    else _want("picked", picked, torch.int32, (total, self.kv_heads, budget), dev)
+                if workspace is not None:
+                    need = _want("workspace", workspace, torch.uint8, (-1,), dev).shape[0]
+                elif need:
+                    workspace = self._workspace(need, stream, q.device)
+        rc = _FC.cache_pick(self.handle, batch, bounds.struct, table, table.shape[1], seq_lens, q, stride, offsets, off_h,
+                            max_len, budget, sink, recent, picked, workspace, need, _stream_on(stream, dev))
+        if rc:
+            _check(rc, self.handle)
         return picked
 
     def cache_attend_picked(self, cache: KVCache, table, seq_lens, q, offsets, picked, q_scale: float = 1.0,
@@ -993,26 +1018,29 @@ class Selector:
         entries that are no page that the query sees are skipped. Returns the bf16 outputs [sum T, Hq, d]."""
         import torch
         off_h = _host_i32(offsets if offsets_h is None else offsets_h)
-        batch, total = len(off_h) - 1, int(off_h[-1])
-        dev = self._cache_call(cache, table, seq_lens, batch)
-        _want("offsets", offsets, torch.int32, (batch + 1,), dev)
-        stride = _row_stride("q", q, self._element(), self.heads, self.head_dim, dev)
-        if q.shape[0] != total:
-            _refuse(f"q has {q.shape[0]} rows, the offsets {total}")
+        batch, total, dev = len(off_h) - 1, int(off_h[-1]), self.device
+        stride = self._queries(cache, KVCache, table, seq_lens, q, offsets, batch, total, dev)
         _want("picked", picked, torch.int32, (total, self.kv_heads, -1), dev)
-        budget = picked.shape[2]
-        need = cache_attend_picked_workspace(self.handle, batch, off_h, cache.page_size, table.shape[1], budget)
-        with _allocate_on(stream, dev):
-            if out is None:
-                out = torch.empty((total, self.heads, self.head_dim), dtype=torch.bfloat16, device=q.device)
-            else:
-                _want("out", out, torch.bfloat16, (total, self.heads, self.head_dim), dev)
-            if workspace is not None:
-                need = _want("workspace", workspace, torch.uint8, (-1,), dev).shape[0]
-            elif need:
-                workspace = self._workspace(need, stream, q.device)
-        cache_attend_picked(self.handle, batch, cache.struct, table, table.shape[1], seq_lens, q, stride, offsets, off_h,
-                            picked, budget, q_scale, out, workspace, need, _stream_on(stream, dev))
+        budget, shape = picked.shape[2], (total, self.heads, self.head_dim)
+        need = _FC.picked_bytes(self.handle, batch, off_h, cache.page_size, table.shape[1], budget)
+        if need < 0:
+            _check(-need, self.handle)
+        if out is None and workspace is None and stream is None:
+            out = torch.empty(shape, dtype=torch.bfloat16, device=q.device)
+            if need:
+                workspace = self._workspace(need, None, q.device)
+        else:
+            with _allocate_on(stream, dev):
+                out = torch.empty(shape, dtype=torch.bfloat16, device=q.device) if out is None \
+                    else _want("out", out, torch.bfloat16, shape, dev)
+                if workspace is not None:
+                    need = _want("workspace", workspace, torch.uint8, (-1,), dev).shape[0]
+                elif need:
+                    workspace = self._workspace(need, stream, q.device)
+        rc = _FC.cache_attend_picked(self.handle, batch, cache.struct, table, table.shape[1], seq_lens, q, stride, offsets,
+                                     off_h, picked, budget, q_scale, out, workspace, need, _stream_on(stream, dev))
+        if rc:
+            _check(rc, self.handle)
         return out
 
     def verify(self, draft_tokens, target_probs, u_accept, u_sample, offsets, draft_probs=None, offsets_h=None,
