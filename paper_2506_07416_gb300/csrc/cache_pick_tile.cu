@@ -7,7 +7,7 @@
 //   all lay out the queries once, K-major and swizzled;
 //   eight make f16 of the codes of the next 128 pages (two stages), their bytes on the way one tile ahead;
 //   one issues the contraction into one of two places in tensor memory;
-//   four turn the last one's columns into keys and write them, neighbouring pages by neighbouring lanes.
+//   eight turn the last one's columns into keys and write them, neighbouring pages by neighbouring lanes.
 
 #include <algorithm>
 
@@ -19,7 +19,7 @@ namespace lvs {
 namespace {
 
 constexpr int kCols = 128, kTilePages = 128;
-constexpr int kOutWarps = 4, kCodeWarps = 8, kMmaWarp = kOutWarps + kCodeWarps;
+constexpr int kOutWarps = 8, kCodeWarps = 8, kMmaWarp = kOutWarps + kCodeWarps;
 constexpr int kPickThreads = 32 * (kMmaWarp + 1);
 constexpr int kAtom = 128 * 128;  // 128 rows of 64 f16
 enum { P_A_FULL = 0, P_A_FREE = 2, P_D_FULL = 4, P_D_FREE = 6, P_DRAIN = 8, P_COUNT };
@@ -121,15 +121,25 @@ __global__ void __launch_bounds__(kPickThreads, 1) pick_tile_kernel(const __grid
 
     if (warp < kOutWarps) {
         // ---------------------------------------------------------------- keys: a page a thread
-        const uint32_t lanes = (uint32_t)(warp * 32) << 16;
-        const int cols = st.queries * padded;
+        // (two warps share the 32 pages that their lanes may read, and the columns where a query has one half's alone)
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const bool halves = kCols / 2 % padded == 0;
+        const int row = tid & 127, col0 = halves ? (warp >> 2) * (kCols / 2) : 0;
+        const int cols = halves ? min(kCols / 2, st.queries * padded - col0) : (warp < 4 ? st.queries * padded : 0);
+        // the page and its unit are found a tile ahead
+        auto exps_of = [&](int32_t page) { return (int)__ldg(a.exps + (int64_t)max(page, 0) * a.hkv + h); };
+        int32_t next_page = find(first_page(0) + row);
+        int next_exp = exps_of(next_page);
         for (int n = 0; n < mine; ++n) {
-            const int o = first_page(n) + tid;
-            const int32_t page = find(o);
-            if (page < 0 && o < st.pages) atomicOr(a.err, kErrBounds);
-            const int x = min(max((int)__ldg(a.exps + (int64_t)max(page, 0) * a.hkv + h), -100), 100);
-            const float unit = __uint_as_float((uint32_t)(127 + x) << 23);
-            uint32_t* out = a.keys + ((int64_t)(st.q0 + st.i0) * a.hkv + h) * a.key_stride + o;
+            const int o = first_page(n) + row;
+            const int32_t page = next_page;
+            const float unit = __uint_as_float((uint32_t)(127 + min(max(next_exp, -100), 100)) << 23);
+            if (n + 1 < mine) {
+                next_page = find(first_page(n + 1) + row);
+                next_exp = exps_of(next_page);
+            }
+            if (page < 0 && o < st.pages && warp < 4) atomicOr(a.err, kErrBounds);
+            uint32_t* out = a.keys + ((int64_t)(st.q0 + st.i0 + col0 / padded) * a.hkv + h) * a.key_stride + o;
             const int64_t step = (int64_t)a.hkv * a.key_stride;
             auto put = [&](float s) {  // of the next query
                 if (o < st.pages) *out = page >= 0 ? score_key(s * unit) : 1u;
@@ -142,7 +152,7 @@ __global__ void __launch_bounds__(kPickThreads, 1) pick_tile_kernel(const __grid
 #pragma unroll 1
             for (int c0 = 0; c0 < cols; c0 += 32) {
                 float v[32];
-                tmem_ld32(tmem + lanes + (n & 1) * kCols + c0, v);
+                tmem_ld32(tmem + lanes + (n & 1) * kCols + col0 + c0, v);
                 tmem_wait_ld();
                 if (padded == 8) {
 #pragma unroll
