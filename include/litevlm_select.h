@@ -778,8 +778,9 @@ litevlm_status_t litevlm_select_cache_bounds(litevlm_select_t handle, int32_t ba
  *                    every query, key head and page of max_len; 0 where budget holds max_len), 256-byte aligned; as for
  *                    litevlm_select_cache_attend
  * exps are in [-100, 100] (cut to it). A page whose table entry is not in the pool ranks below all others (DEVICE_BOUNDS).
- * Errors: as above; UNSUPPORTED for more than 128 query heads a key head, or where Hkv x ceil(T_b / (64 / G)) passes
- * 65535 (G rounded up to 1, 2, 4 or a multiple of 8) or Hkv x sum T_b passes 2^31 - 1.
+ * Errors: as above; UNSUPPORTED for more than 128 query heads a key head, where Hkv x the longest request's tiles of columns
+ * (128 of them, 64 in calls of no more; G rounded up to 1, 2, 4 or a multiple of 8 for each query) pass 65535, or
+ * Hkv x sum T_b passes 2^31 - 1.
  */
 litevlm_status_t litevlm_select_cache_pick_workspace(litevlm_select_t handle, int32_t batch,
                                                      const int32_t* q_offsets_h, int32_t max_len, int32_t page_size,

@@ -2,15 +2,19 @@
 //
 // A query's score of a page is the largest product that a key of the page's ranges can have with it: with the query
 // as whole numbers r of a power of two, S(page) = 2^e max over the key head's query heads of sum over channels of
-// r * (r > 0 ? hi : lo). The sums are whole numbers below 2^22, exact in fp32 in any order, so
+// r * (r > 0 ? hi : lo). The sums are whole numbers below 2^22, exact in fp32 and in s32 in any order, so
 // the same inputs pick the same pages whatever kernel adds them up.
 //
-// pick_score_kernel: the product [pages, 2 d] x [2 d, columns] with max(r, 0) against hi and min(r, 0) against lo, a
-// column for each query head of a key head (a query's columns padded to a power of two or whole tiles of eight). A warp
-// keeps 16 pages as the M rows (m16n8k16; codes become f16 in registers, a channel order of the lanes' own) and
-// goes over the columns' tiles in shared memory.
+// The scores are a product [pages, 2 d] x [2 d, columns] with max(r, 0) against hi and min(r, 0) against lo, a
+// column for each query head of a key head (a query's columns padded to a power of two or whole tiles of eight):
+//   pick_token_kernel, one tile of columns: 32 caches of 30 Ki to 127 Ki tokens in pages of 32, 32 / 8 heads (180 MB): 41 us,
+//     4.3 TB/s, a fifth of it the CTAs' start; one of 40 Ki, 28 / 4 heads, 7 us with the launch
+//   pick_score_kernel, up to 64 columns: a warp keeps 16 pages as f16 in registers and goes over the columns' tiles in
+//     shared memory (with it the prompts below took 74 us)
+//   cache_pick_tile.cu, more: 777 to 1024 queries of two requests of 20 Ki to 32 Ki in pages of 64, 28 / 4 heads: 27 us
 // pick_select_kernel: the budget-th largest score of a query by counting its scores in buckets, then the
-// pages above it and the lowest of those at it, in order.
+// pages above it and the lowest of those at it, in order. 256 lists of up to 4096 pages 10.5 us, 7204 of about 400 14
+// (bit by bit 13 and 18).
 
 #include <algorithm>
 
