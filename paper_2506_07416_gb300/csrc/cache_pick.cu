@@ -501,7 +501,7 @@ __global__ void __launch_bounds__(WARPS == 1 ? 128 : 32 * WARPS) pick_select_ker
             x = lo;
             exact = in == want;
             if (exact || shift == 0) break;
-            hi = lo + ((1u << shift) - 1u);
+            hi = lo + ((1u << shift) - 1u);  // (no more than the largest key and a bucket, 2^26: below 2^32)
             sync();  // (the counts have been read)
         }
     }
@@ -523,14 +523,15 @@ __global__ void __launch_bounds__(WARPS == 1 ? 128 : 32 * WARPS) pick_select_ker
             all += before_s[0][w];
         }
     }
-    const int room = a.budget - all;  // of ties
+    // of ties; keys that the scores' kernel gave up on can be anything: then none behind the list, and none before it
+    const int room = max(0, a.budget - all);
     my_at += min(ties_before, room);
     visit([&](int j, uint32_t v) {
         const uint32_t tie = exact ? 0u : __ballot_sync(0xffffffffu, v == x);
         const uint32_t below = (1u << lane) - 1u;
         const bool take = v > above || ((tie >> lane & 1u) && ties_before + __popc(tie & below) < room);
         const uint32_t m = __ballot_sync(0xffffffffu, take);
-        if (take) out[my_at + __popc(m & below)] = j;
+        if (take && my_at + __popc(m & below) < a.budget) out[my_at + __popc(m & below)] = j;
         my_at += __popc(m);
         ties_before += __popc(tie);
     });

@@ -11,6 +11,7 @@ __host__ __device__ __forceinline__ int padded_group(int group)
     return group <= 2 ? group : (group <= 4 ? 4 : (group + 7) & ~7);
 }
 // Order of the scores as whole numbers, above 1 (0: a page that the query does not see, 1: one that the pool has not).
+// Scores are below 2^7 * 2^14 * 2^100, so keys are below 0xFC000000.
 __device__ __forceinline__ uint32_t score_key(float s)
 {
     const uint32_t u = __float_as_uint(s);

@@ -171,6 +171,27 @@ def test_bounds_match_the_definition(select, hkv, d, page, lens, new):
     s.close()
 
 
+def test_bounds_of_many_pages(select):
+    """So many that a warp takes several heads of a page."""
+    rng = np.random.default_rng(3)
+    hkv, d, page = 16, 64, 16
+    lens = rng.integers(700, 1400, 48).tolist()
+    new = [n - int(x) for n, x in zip(lens, rng.integers(0, 40, 48))]
+    table, pool = tables(rng, lens, page)
+    c = random_pool(rng, pool, hkv, page, d)
+    off = offsets(new)
+    s = select.Selector(48, 8, 8, hkv, hkv, d, "bf16")
+    cache = to_cache(select, c)
+    bounds = s.key_bounds(cache)
+    s.cache_bounds(cache, bounds, i32(table), i32(lens), i32(off), offsets_h=off)
+    s.check_device()
+    want_c, want_e = pref.bounds(c, table, lens, new, np.zeros(bounds.codes.shape, np.int8),
+                                 np.zeros(bounds.exps.shape, np.int8))
+    np.testing.assert_array_equal(bounds.exps.cpu().numpy(), want_e)
+    np.testing.assert_array_equal(bounds.codes.cpu().numpy(), want_c)
+    s.close()
+
+
 def test_bounds_report_bad_lengths_and_pages(select):
     rng = np.random.default_rng(1)
     c = random_pool(rng, 3, 1, 16, 64)
@@ -251,6 +272,28 @@ def pick_case(select, hq, hkv, d, dtype, page, lens, counts, budget, sink, recen
 def test_pick_matches_the_definition(select, hq, hkv, d, dtype, page, lens, counts, budget, sink, recent):
     pick_case(select, hq, hkv, d, dtype, page, lens, counts, budget, sink, recent, seed=hq * d + page,
               strided=hq % 4 == 0)
+
+
+@pytest.mark.parametrize("hq,hkv,d,dtype,batch", [(8, 8, 64, "bf16", 70), (14, 2, 64, "bf16", 33), (9, 3, 128, "e4m3", 40),
+                                                  (4, 1, 128, "bf16", 129)])
+def test_pick_of_batches_whose_lengths_differ(select, hq, hkv, d, dtype, batch):
+    rng = np.random.default_rng(batch)
+    lens = np.where(rng.random(batch) < 0.2, rng.integers(0, 40, batch), rng.integers(100, 1500, batch)).tolist()
+    lens[batch // 2] = 9000
+    counts = [1] * batch
+    pick_case(select, hq, hkv, d, dtype, 16, lens, counts, 5, 1, 1, seed=batch)
+    counts = rng.integers(0, 2, batch).tolist()
+    pick_case(select, hq, hkv, d, dtype, 16, lens, counts, 5, 1, 1, seed=batch + 1)
+    counts = rng.integers(0, 4, batch).tolist()
+    pick_case(select, hq, hkv, d, dtype, 16, lens, counts, 5, 1, 1, seed=batch + 2)
+
+
+@pytest.mark.parametrize("hq,hkv,d,dtype,batch", [(8, 8, 64, "bf16", 70), (14, 2, 64, "bf16", 33), (8, 2, 128, "e4m3", 40)])
+def test_attend_picked_of_batches_whose_lengths_differ(select, hq, hkv, d, dtype, batch):
+    rng = np.random.default_rng(batch)
+    lens = np.where(rng.random(batch) < 0.2, rng.integers(0, 40, batch), rng.integers(100, 600, batch)).tolist()
+    for counts in ([1] * batch, rng.integers(0, 2, batch).tolist(), rng.integers(0, 4, batch).tolist()):
+        attend_case(select, hq, hkv, d, dtype, 16, lens, counts, 5, seed=sum(counts))
 
 
 @pytest.mark.parametrize("lens,budget", [([900], 9), ([9000], 33), ([70001], 100)])

@@ -285,6 +285,20 @@ def test_a_wait_that_runs_out_is_reported_and_the_handle_recovers(select):
         a.s.set_wait_budget(0)
         assert torch.equal(call(), want)
         a.s.check_device()
+    # scores that were never made, whatever memory holds in their place, do not lead out of the lists
+    need = select.cache_pick_workspace(a.s.handle, 3, a.off_h, a.most, a.page, a.budget)
+    for byte in (0x00, 0x01, 0x7F, 0xFF):
+        ws = torch.full((need,), byte, dtype=torch.uint8, device="cuda")
+        buf = torch.full((p.shape[0] + 2, *p.shape[1:]), -9, dtype=torch.int32, device="cuda")
+        a.s.set_wait_budget(200000)
+        a.s.set_debug_flags(select.DEBUG_STALL_PICK)
+        a.pick(picked=buf[1:-1], workspace=ws)
+        with pytest.raises(select.LitevlmError):
+            a.s.check_device()
+        assert (buf[0] == -9).all() and (buf[-1] == -9).all()
+        a.s.set_debug_flags(0)
+        a.s.set_wait_budget(0)
+    assert torch.equal(a.pick(), p)
 
 
 def test_lengths_beyond_the_table_are_cut_and_reported(select):
