@@ -1724,11 +1724,12 @@ litevlm_status_t litevlm_select_cache_attend_picked(litevlm_select_t h, int32_t 
     if (overlap_rows(out, total * row * 2, q, total, q_row_stride, row, c.qk_dtype == LITEVLM_FP8_E4M3 ? 1 : 2) ||
         overlap(out, total * row * 2, picked, total * c.num_kv_heads * budget * 4))
         return fail(h, LITEVLM_ERR_INVALID_ARG, "out must not overlap q or picked");
+    s = check_workspace(h, workspace, workspace_bytes, space.total);
+    if (s != LITEVLM_OK) return s;
     if (overlap(workspace, space.total, out, total * row * 2) ||
         overlap(workspace, space.total, picked, total * c.num_kv_heads * budget * 4))
         return fail(h, LITEVLM_ERR_INVALID_ARG, "the workspace must not overlap out or picked");
-    s = check_workspace(h, workspace, workspace_bytes, space.total);
-    if (s == LITEVLM_OK) s = debug_mirror(h, q_offsets_d, q_offsets_h, (int64_t)batch + 1, "q_offsets", stream);
+    s = debug_mirror(h, q_offsets_d, q_offsets_h, (int64_t)batch + 1, "q_offsets", stream);
     if (s != LITEVLM_OK) return s;
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     a.q = q;

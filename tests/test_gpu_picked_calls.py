@@ -359,7 +359,9 @@ def test_refusals(select):
     p2 = two.pick()
     refused("WORKSPACE", lambda: two.attend(p2, workspace=torch.empty(256, **byte)))
     refused(bad, lambda: two.attend(p2, workspace=torch.empty(1 << 24, **byte)[1:]))
-    ws = torch.empty(1 << 24, **byte)
+    ws = torch.empty(1 << 24, **byte)  # too short, whatever lies behind it
+    refused("WORKSPACE", lambda: two.attend(p2, workspace=ws[:256],
+                                            out=ws[256:256 + 4 * 8 * 128 * 2].view(torch.bfloat16).view(4, 8, 128)))
     refused(bad, lambda: two.attend(p2, workspace=ws, out=ws[:4 * 8 * 128 * 2].view(torch.bfloat16).view(4, 8, 128)))
     # ranges
     every, evd = a.off_h, a.off
