@@ -198,7 +198,10 @@ struct VPart {
 
 // PICKED: the rows are whole queries of a tile, and the keys those of the pages that any of them has, in the list's order; a
 // key of a page that a row's query has not is as masked. Of 64 or 32 keys that no row of a warp has, the warp
-// makes no exponentials.
+// makes no exponentials. Few rows stand in the tile more than once, so that all four warps make exponentials: drafts of
+// 32 ragged requests, 4 to 32 rows a head, 48 pages of 32: 83 us without, 77 with. What bounds those: a tile takes 3000
+// clocks of a CTA (1000 are the tensor pipe's, which two CTAs share), half of them the warps that make the values.
+// Dropped there: lines fetched into the L2 three tiles ahead and loads in another order (78 us).
 template <int D, bool FP8, int NR, bool PICKED = false>
 __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile_kernel(const __grid_constant__ AttendArgs a)
 {
@@ -258,7 +261,11 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
     const int all_see = rt.last0 + rt.query(rt.row0);  // the last key that every row sees
     const int4* list = PICKED ? a.lists + pick_list * a.list_cap : nullptr;  // page in the pool, page of the request
     const int n_tiles = uniform(k1 > k0 ? (k1 - k0 + kTileKeys - 1) / kTileKeys : 0);
-    const int live = (rt.rows + 31) / 32;  // softmax warps with rows
+    // PICKED: up to 64 rows stand in the tile twice, up to 32 four times; each copy of a row makes the probabilities of its
+    // own half or quarter of a tile's keys, the others' being 0, and the copies' sums are joined at the end
+    const int copies = PICKED && NR == 1 ? uniform(rt.rows <= 32 ? 4 : (rt.rows <= 64 ? 2 : 1)) : 1;
+    const int copy_rows = 128 * NR / copies;
+    const int live = copies > 1 ? 4 : (rt.rows + 31) / 32;  // softmax warps with rows
     const int row_tiles = NR > 1 ? uniform((rt.rows + 127) / 128) : 1;
 
     if (tid == 0) {
@@ -287,8 +294,9 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
     const uint32_t tmem = uniform(*tmem_slot);
     const Ctl ctl{abort_flag, a.err, a.wait_budget};
     float m = kNoRef, l = 0.f;
-    const bool real = tid < rt.rows;  // (the softmax warps' threads)
-    const int row = rt.row0 + (real ? tid : 0), query = rt.query(row);
+    const int in_copy = copies > 1 ? tid & (copy_rows - 1) : tid;
+    const bool real = tid < 32 * SOFT && in_copy < rt.rows;  // (the softmax warps' threads)
+    const int row = rt.row0 + (real ? in_copy : 0), query = rt.query(row);
 
     const int rtile = warp >> 2;  // the softmax warps' row tile
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
@@ -311,6 +319,8 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
             // the pages that the row's query has, a bit for each of the list, 32 at a time
             const uint32_t* bits = PICKED ? a.list_bits + (pick_list * a.pick_queries + query - qt.i0) * a.list_words : nullptr;
             uint32_t bit_word = 0u;
+            // the groups of 16 keys of a tile that are the copy's
+            const uint32_t own = copies == 4 ? 3u << 2 * warp : (copies == 2 ? 15u << 4 * (warp >> 1) : 255u);
             int next_pos = 0;  // PICKED: position of the group's first key
             // page of a tile's group of 16 keys (lanes 0 to 7); groups without one are as masked
             auto page_of = [&](int t) -> int32_t {
@@ -343,7 +353,7 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
                         const uint32_t b8 = bit_word >> (x0 & 31);
 #pragma unroll
                         for (int g = 0; g < 8; ++g) has |= (b8 >> ((16 * g) >> shift) & 1u) << g;
-                        has &= ~gone;
+                        has &= own & ~gone;
                         any_has = __reduce_or_sync(0xffffffffu, has);
                     }
                     next_page = page_of(t + 1);
@@ -373,6 +383,7 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
                     constexpr int STEP = NR > 1 ? 64 : 32;
                     float mx = -INFINITY;
                     float v[STEP];
+                    int held = PICKED ? -1 : 0;  // the first column of those there
                     auto mask = [&](int c0, float* x) {
                         const uint32_t k = mask_of(c0);
 #pragma unroll
@@ -396,6 +407,7 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
                         if (PICKED && !(any_has >> (c0 / 16) & ((1u << STEP / 16) - 1u))) continue;
                         read(c0);
                         if constexpr (PICKED) {
+                            held = c0;
 #pragma unroll
                             for (int x = 0; x < STEP / 16; ++x) {
                                 const float top = row_max<16>(v + 16 * x);
@@ -470,7 +482,7 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
                             for (int x = 0; x < STEP; x += 32) tmem_st16(ts + (c0 + x) / 2, none);
                             continue;
                         }
-                        if (c0 > 0) read(c0);
+                        if (c0 != held) read(c0);
 #pragma unroll
                         for (int x = 0; x < STEP; x += 32) chunk_of(c0 + x, v + x);
                     }
@@ -518,13 +530,20 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
         };
         // pages of the thread's keys (a group of 16 lies in one), a tile ahead of the loads of the codes
         int32_t pk0, pk1, pv;
-        int next_pv_pos = 0;
+        int next_pv_page = 0;  // PICKED: page of the request of the thread's next keys of V
+        auto pos_of = [&](int j0) { return PICKED ? (next_pv_page << C.page_shift) + ((j0 + kg * 8) & smask) : 0; };
         auto pages = [&](int j0) {
             pk0 = page_at(j0 + w * 32);
             pk1 = page_at(j0 + w * 32 + 16);
-            pv = page_at(j0 + kg * 8);
-            if constexpr (PICKED)
-                if (pv >= 0) next_pv_pos = (__ldg(&list[(j0 + kg * 8) >> C.page_shift].y) << C.page_shift) + ((j0 + kg * 8) & smask);
+            if constexpr (PICKED) {
+                // (both words at once, and nothing that waits for them here)
+                const int j = j0 + kg * 8;
+                const int2 e = j < k1 ? __ldg(reinterpret_cast<const int2*>(list + (j >> C.page_shift))) : make_int2(-1, 0);
+                pv = e.x;
+                next_pv_page = e.y;
+            } else {
+                pv = page_at(j0 + kg * 8);
+            }
         };
         auto report_pages = [&](int j0) {
             if ((lane & 15) == 0) report(lane ? pk1 : pk0, j0 + w * 32 + lane);
@@ -535,7 +554,7 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
         report_pages(k0);
         kp.load(C, pk0, pk1, h, k0, w);
         load_v(vp, pv, k0);
-        pv_pos = next_pv_pos;
+        pv_pos = pos_of(k0);
         pages(k0 + kTileKeys);
         for (int t = 0; t < n_tiles; ++t) {
             const int j0 = k0 + t * kTileKeys, jn = j0 + kTileKeys;
@@ -607,7 +626,7 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
             __syncwarp();
             if (lane == 0) mbar_arrive(BAR(B_V_FULL + st));
             if (more) load_v(vp, pv, jn);
-            pv_pos = next_pv_pos;
+            pv_pos = pos_of(jn);
             pages(jn + kTileKeys);
         }
     } else {
@@ -720,35 +739,78 @@ __global__ void __launch_bounds__(kTileThreads<NR>, NR == 1 ? 2 : 1) attend_tile
                 *reinterpret_cast<float4*>(mine + lane * PITCH + c0 + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
         }
         __syncwarp();
-        const int64_t at = (int64_t)(q0 + query) * a.hq + h * a.group + row - query * a.group;
-        const int64_t part = ((int64_t)blockIdx.x * a.cache.hkv + h) * a.max_rows + row - (PICKED ? qt.i0 * a.group : 0);
-        const bool split = PICKED ? a.pick_chunks > 1 : a.slots > 0;
-        const float f = l == 0.f ? 0.f : a.cache.scale[1] / l;
-        const int rows = min(32, rt.rows - warp * 32);
-        constexpr int N = D / 32;  // channels of a lane
-#pragma unroll 4
-        for (int r = 0; r < rows; ++r) {
-            float v[N];
+        if (PICKED && NR == 1 && copies > 1) {
+            // a row's copies joined: of the four warps each takes every fourth row
+            float2* ml = reinterpret_cast<float2*>(reinterpret_cast<float*>(smem) + 128 * PITCH);
+            static_assert(!(PICKED && NR == 1) || 128 * (PITCH * 4 + 8) <= L::BAR, "the rows fit the operands' memory");
+            ml[tid] = make_float2(m, l);
+            asm volatile("bar.sync 1, 128;" ::: "memory");
+            constexpr int N = D / 32;
+            for (int r = warp; r < rt.rows; r += 4) {
+                float M = kNoRef, L_ = 0.f, O[N];
 #pragma unroll
-            for (int i = 0; i < N; i += 2)
-                *reinterpret_cast<float2*>(v + i) = *reinterpret_cast<const float2*>(mine + r * PITCH + lane * N + i);
-            if (split) {
-                float* out = a.part_o + __shfl_sync(0xffffffffu, part, r) * D + lane * N;
-                if constexpr (N == 4) __stcg(reinterpret_cast<float4*>(out), make_float4(v[0], v[1], v[2], v[3]));
-                else __stcg(reinterpret_cast<float2*>(out), make_float2(v[0], v[1]));
-            } else {
-                // (a row that sees no key is 0, whatever the columns hold)
-                const float fr = __shfl_sync(0xffffffffu, f, r);
-                const bool none = __shfl_sync(0xffffffffu, l, r) == 0.f;
-                __nv_bfloat16* out = a.out + __shfl_sync(0xffffffffu, at, r) * D + lane * N;
+                for (int i = 0; i < N; ++i) O[i] = 0.f;
+                for (int c = 0; c < copies; ++c) M = fmaxf(M, ml[c * copy_rows + r].x);
+                for (int c = 0; c < copies; ++c) {
+                    const int from = c * copy_rows + r;
+                    const float f = ex2(ml[from].x - M);
+                    L_ += ml[from].y * f;
+#pragma unroll
+                    for (int i = 0; i < N; i += 2) {
+                        const float2 x =
+                            *reinterpret_cast<const float2*>(reinterpret_cast<float*>(smem) + from * PITCH + lane * N + i);
+                        O[i] += x.x * f, O[i + 1] += x.y * f;
+                    }
+                }
+                const int i_row = rt.row0 + r, i_query = rt.query(rt.row0 + r);
+                if (a.pick_chunks > 1) {
+                    const int64_t part =
+                        ((int64_t)blockIdx.x * a.cache.hkv + h) * a.max_rows + i_row - qt.i0 * a.group;
+                    float* out = a.part_o + part * D + lane * N;
+#pragma unroll
+                    for (int i = 0; i < N; i += 2) __stcg(reinterpret_cast<float2*>(out + i), make_float2(O[i], O[i + 1]));
+                    if (lane == 0) a.part_ml[part] = make_float2(M, L_);
+                } else {
+                    const int64_t at = (int64_t)(q0 + i_query) * a.hq + h * a.group + i_row - i_query * a.group;
+                    const float f = a.cache.scale[1] / L_;
+                    __nv_bfloat16* out = a.out + at * D + lane * N;
+#pragma unroll
+                    for (int i = 0; i < N; i += 2)
+                        *reinterpret_cast<__nv_bfloat162*>(out + i) =
+                            __floats2bfloat162_rn(L_ == 0.f ? 0.f : O[i] * f, L_ == 0.f ? 0.f : O[i + 1] * f);
+                }
+            }
+        } else {
+            const int64_t at = (int64_t)(q0 + query) * a.hq + h * a.group + row - query * a.group;
+            const int64_t part = ((int64_t)blockIdx.x * a.cache.hkv + h) * a.max_rows + row - (PICKED ? qt.i0 * a.group : 0);
+            const bool split = PICKED ? a.pick_chunks > 1 : a.slots > 0;
+            const float f = l == 0.f ? 0.f : a.cache.scale[1] / l;
+            const int rows = min(32, rt.rows - warp * 32);
+            constexpr int N = D / 32;  // channels of a lane
+#pragma unroll 4
+            for (int r = 0; r < rows; ++r) {
+                float v[N];
 #pragma unroll
                 for (int i = 0; i < N; i += 2)
-                    *reinterpret_cast<__nv_bfloat162*>(out + i) =
-                        __floats2bfloat162_rn(none ? 0.f : v[i] * fr, none ? 0.f : v[i + 1] * fr);
+                    *reinterpret_cast<float2*>(v + i) = *reinterpret_cast<const float2*>(mine + r * PITCH + lane * N + i);
+                if (split) {
+                    float* out = a.part_o + __shfl_sync(0xffffffffu, part, r) * D + lane * N;
+                    if constexpr (N == 4) __stcg(reinterpret_cast<float4*>(out), make_float4(v[0], v[1], v[2], v[3]));
+                    else __stcg(reinterpret_cast<float2*>(out), make_float2(v[0], v[1]));
+                } else {
+                    // (a row that sees no key is 0, whatever the columns hold)
+                    const float fr = __shfl_sync(0xffffffffu, f, r);
+                    const bool none = __shfl_sync(0xffffffffu, l, r) == 0.f;
+                    __nv_bfloat16* out = a.out + __shfl_sync(0xffffffffu, at, r) * D + lane * N;
+#pragma unroll
+                    for (int i = 0; i < N; i += 2)
+                        *reinterpret_cast<__nv_bfloat162*>(out + i) =
+                            __floats2bfloat162_rn(none ? 0.f : v[i] * fr, none ? 0.f : v[i + 1] * fr);
+                }
             }
+            if (real && split) a.part_ml[part] = make_float2(m, l);
+            if (!PICKED && real && a.slots == 0 && a.lse) a.lse[at] = l == 0.f ? INFINITY : m + log2f(l);
         }
-        if (real && split) a.part_ml[part] = make_float2(m, l);
-        if (!PICKED && real && a.slots == 0 && a.lse) a.lse[at] = l == 0.f ? INFINITY : m + log2f(l);
     }
     tc_fence_before();
     __syncthreads();

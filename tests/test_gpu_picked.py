@@ -423,6 +423,17 @@ def test_attend_picked_matches_the_definition(select, hq, hkv, d, dtype, page, l
     attend_case(select, hq, hkv, d, dtype, page, lens, counts, budget, seed=hq + d + page, strided=hq % 8 == 0)
 
 
+@pytest.mark.parametrize("hq,hkv,d,dtype", [(8, 2, 128, "bf16"), (4, 1, 64, "bf16"), (14, 2, 128, "e4m3"), (5, 1, 64, "bf16")])
+@pytest.mark.parametrize("page,budget", [(16, 1), (16, 30), (64, 9)])  # whole lists, and lists in chunks
+def test_attend_picked_of_requests_with_few_and_many_rows(select, hq, hkv, d, dtype, page, budget):
+    """Rows of a request and key head around 32, 64 and 128 in one call."""
+    g = hq // hkv
+    counts = [1, 32 // g, 32 // g + 1, 64 // g, 64 // g + 1, 0, 3, 128 // g, 7]
+    lens = [700, 900, 40, 333, 1200, 5, 2, 800, 64]
+    attend_case(select, hq, hkv, d, dtype, page, lens, counts, budget, seed=budget)
+    attend_case(select, hq, hkv, d, dtype, page, lens[:2], [2, 32 // g + 1], budget, seed=budget + 1, strided=True)
+
+
 @pytest.mark.parametrize("hq,hkv,counts", [(4, 4, [1, 1]), (14, 2, [3, 2]), (28, 4, [50, 30])])
 def test_attend_picked_of_lists_that_leave_nothing(select, hq, hkv, counts):
     off, budget = offsets(counts), 4
@@ -507,6 +518,31 @@ def test_attend_picked_sees_nan_values_only_where_they_are_seen(select):
         want[19:20, :hq // hkv, 48:64] = True  # query i stands at position 70 + i
         np.testing.assert_array_equal(nan, want)
         s.close()
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(2, 2, 128), (4, 2, 64), (8, 2, 128)])
+def test_attend_picked_sees_nan_values_beside_a_request_with_more_rows(select, hq, hkv, d):
+    """The same where a request's 30, 60 or 120 rows stand beside one's with more."""
+    rng = np.random.default_rng(hq)
+    lens, counts, page, g = [100, 90], [30, 128 * hkv // hq], 16, hq // hkv
+    table, pool = tables(rng, lens, page)
+    c, off = random_pool(rng, pool, hkv, page, d), offsets(counts)
+    c["v_scales"][table[0, 5], 0, 9, 3] = 0x7F  # position 89, channels 48 to 63 of key head 0
+    picked = np.tile(np.array([5, 0, 6], np.int32), (sum(counts), hkv, 1))
+    picked[20:30] = [6, 1, 2]
+    picked[30:] = [0, 1, 2]
+    q, qv, _ = make_q(rng, sum(counts), hq, d, "bf16")
+    s = select.Selector(2, 8, 8, hq, hkv, d, "bf16")
+    got = s.cache_attend_picked(to_cache(select, c), i32(table), i32(lens), q, i32(off), i32(picked), offsets_h=off)
+    s.check_device()
+    got = got.double().cpu().numpy()
+    want = np.zeros(got.shape, bool)
+    want[19:20, :g, 48:64] = True  # query i of the first stands at position 70 + i
+    np.testing.assert_array_equal(np.isnan(got), want)
+    c["v_scales"][table[0, 5], 0, 9, 3] = 0x38
+    ref_out, slack = pref.attend(c, table, lens, qv, off, picked)
+    assert (np.abs(got - ref_out) <= slack)[~want].all()
+    s.close()
 
 
 def test_attend_picked_skips_pages_that_the_pool_has_not(select):
