@@ -1184,8 +1184,9 @@ cudaError_t launch_all(const AttendArgs& a, const AttendPlan& plan, int max_rows
 
 // The list of a tile's queries for a key head: the pages that any of them has and sees, ascending, with the queries that
 // have each. A bit for every page of the request in shared memory (65536 of them at a time), the number of bits before
-// each word, and a second pass over the queries' own lists, which finds every page's place by them. About
-// 2 us, which the next kernel saves many times: of the 37 queries of a tile of 256 rows with 32 pages each, most have
+// each word, and a second pass over the queries' own lists, which finds every page's place by them. What bounds it: a chain
+// of loads, offsets - length - lists - table - lists; 9 us of a cold cache for 32 requests of up to 8 queries and 48 pages,
+// which the next kernel saves many times: of the 37 queries of a tile of 256 rows with 32 pages each, most have
 // the same 120.
 constexpr int kListThreads = 256;
 constexpr int kListWords = 2048;
@@ -1242,16 +1243,28 @@ __global__ void __launch_bounds__(kListThreads) picked_list_kernel(const __grid_
     const int32_t* picked = a.picked + ((int64_t)(q0 + qt.i0) * a.cache.hkv + h) * a.budget;
     int4* out = a.lists + list * a.list_cap;
     uint32_t* rows = a.list_bits ? a.list_bits + list * a.pick_queries * a.list_words : nullptr;
-    // calls f(query, page from w0 on) for the lists' pages in [w0, w0 + n) that their queries see
+    // calls f(query, page from w0 on) for the lists' pages in [w0, w0 + n) that their queries see; a warp has 64 entries
+    // of four queries on their way at once
     auto each = [&](int w0, int n, auto f) {
-        for (int q = warp; q < qt.queries; q += kListThreads / 32) {
-            const int sees = first + q < 0 ? -1 : (first + q) >> shift;
-            const int32_t* from = picked + (int64_t)q * a.cache.hkv * a.budget;
-            for (int x = lane; x < a.budget; x += 32) {
-                const int o = __ldg(from + x);
-                if (o >= 0 && o <= sees && o >= w0 && o - w0 < n) f(q, o - w0);
+        constexpr int W = kListThreads / 32, U = 4;
+        for (int q0 = warp; q0 < qt.queries; q0 += W * U)
+            for (int x0 = lane; x0 < a.budget; x0 += 64) {
+                int o[U][2];
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int y = 0; y < 2; ++y)
+                        o[u][y] = q0 + u * W < qt.queries && x0 + 32 * y < a.budget
+                                      ? __ldg(picked + (int64_t)(q0 + u * W) * a.cache.hkv * a.budget + x0 + 32 * y)
+                                      : -1;
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const int q = q0 + u * W, sees = first + q < 0 ? -1 : (first + q) >> shift;
+                        if (o[u][y] >= 0 && o[u][y] <= sees && o[u][y] >= w0 && o[u][y] - w0 < n) f(q, o[u][y] - w0);
+                    }
             }
-        }
     };
     int base = 0;
     for (int w0 = 0; w0 < pages; w0 += 32 * kListWords) {

@@ -8,6 +8,9 @@
 //   eight make f16 of the codes of the next 128 pages (two stages), their bytes on the way one tile ahead;
 //   one issues the contraction into one of two places in tensor memory;
 //   eight turn the last one's columns into keys and write them, neighbouring pages by neighbouring lanes.
+// What bounds it: the chain codes - contraction - keys, and a CTA's start, two fifths of its time. A chunk of a prompt, 777
+// and 1024 queries of 28 / 4 heads over up to 512 pages of 64: 27 us, 38 with the picking (45 with four warps making the
+// codes and the pages of a tile found when it is due); 64 columns a CTA and two CTAs an SM took a microsecond more.
 
 #include <algorithm>
 
