@@ -707,9 +707,10 @@ litevlm_status_t litevlm_select_cache_evict(litevlm_select_t handle, int32_t bat
  * request that holds `held` tokens and is to hold `want` has ceil(held / page_size) pages and needs
  * ceil(want / page_size). In the order of the requests, those that need more take them from the ring's
  * front into their table row, until the first that finds too few: it and the later ones that need pages
- * stay as they were (granted = held, slots -1; no error). Those that need fewer put the pages behind their last one
- * behind the ring's end, in order (free for the next call); their table entries stay. Nothing is taken twice or lost: a
- * call with want = 0 gives back all that a request has.
+ * hold what they held (granted = held, slots -1; no error), and the table entries of the pages that they wanted become -1,
+ * whatever stood there: a page that the request once gave back may be another's by now. Those that need fewer put the pages
+ * behind their last one behind the ring's end, in order (free for the next call); their table entries stay. Nothing is
+ * taken twice or lost: a call with want = 0 gives back all that a request has.
  *   page_size        a power of two in [16, 256]
  *   table            device int32 [batch][table_width], updated in place
  *   held, want       device int32 [batch], tokens in [0, table_width * page_size]

@@ -49,7 +49,7 @@ __device__ __forceinline__ longlong2 scan2(long long x, long long y, longlong2* 
 __global__ void __launch_bounds__(kThreads) reserve_kernel(const __grid_constant__ ReserveArgs a)
 {
     // of the requests in hand, one a thread
-    __shared__ int32_t off_s[kThreads + 1], want_s[kThreads], has_s[kThreads], need_s[kThreads];
+    __shared__ int32_t off_s[kThreads + 1], want_s[kThreads], has_s[kThreads], need_s[kThreads];  // (need_s: ~need: refused)
     __shared__ int64_t from_s[kThreads];  // place in the ring, from its head on, of the first page taken or given back
     __shared__ longlong2 warp_s[kWarps];
     const int tid = threadIdx.x, lane = tid & 31, threads = blockDim.x;
@@ -86,7 +86,7 @@ __global__ void __launch_bounds__(kThreads) reserve_kernel(const __grid_constant
         if (tid < n) {
             want_s[tid] = want;
             has_s[tid] = has;
-            need_s[tid] = served ? need : -1;
+            need_s[tid] = served ? need : ~need;
             from_s[tid] = need > has ? taken + before.x : count + given + before.y;
             if (blockIdx.x == 0) a.granted[b0 + tid] = served ? want : held;
         }
@@ -105,18 +105,22 @@ __global__ void __launch_bounds__(kThreads) reserve_kernel(const __grid_constant
         }
         taken += all.x, given += all.y;
         __syncthreads();
-        // ---- pages: the few that most requests of a step take or give by the request's thread, more by a warp
+        // ---- pages: the few that most requests of a step take or give by the request's thread, more by a warp. Of a request
+        // that is not served the entries of the pages that it wanted become -1: they may name pages that it gave back
+        // and another request has by now
         const int64_t step = (int64_t)(threads >> 5) * gridDim.x;
         auto move = [&](int x, int o0, int by) {
             const int hp = has_s[x], np = need_s[x];
             int32_t* row = a.table + (int64_t)(b0 + x) * a.width;
-            if (np > hp) {
+            if (np < 0) {
+                for (int o = hp + o0; o < ~np; o += by) row[o] = -1;
+            } else if (np > hp) {
                 for (int o = hp + o0; o < np; o += by) {
                     const int32_t p = __ldg(a.free + ring(from_s[x] + o - hp));
                     if (p < 0 || p >= total) atomicOr(a.err, kErrBounds);
                     row[o] = p;
                 }
-            } else if (np >= 0 && count >= 0) {
+            } else if (count >= 0) {
                 for (int o = np + o0; o < hp; o += by) {
                     const int64_t to = from_s[x] + o - np;
                     const int32_t p = row[o];
@@ -126,9 +130,10 @@ __global__ void __launch_bounds__(kThreads) reserve_kernel(const __grid_constant
             }
         };
         constexpr int kFewPages = 2;
-        if (tid < n && tid % gridDim.x == blockIdx.x && abs(need_s[tid] - has_s[tid]) <= kFewPages) move(tid, 0, 1);
+        auto few = [&](int x) { return abs((need_s[x] < 0 ? ~need_s[x] : need_s[x]) - has_s[x]) <= kFewPages; };
+        if (tid < n && tid % gridDim.x == blockIdx.x && few(tid)) move(tid, 0, 1);
         for (int x = (tid >> 5) * gridDim.x + blockIdx.x; x < n; x += (int)step)
-            if (abs(need_s[x] - has_s[x]) > kFewPages) move(x, lane, 32);
+            if (!few(x)) move(x, lane, 32);
         // ---- slots: a warp takes 256 neighbouring tokens, whose pages' numbers are all on their way at once
         const int64_t r0 = max(off_s[0], 0), r1 = min((int64_t)off_s[n], a.rows);
         constexpr int U = 8;
