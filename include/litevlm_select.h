@@ -717,12 +717,14 @@ litevlm_status_t litevlm_select_cache_evict(litevlm_select_t handle, int32_t bat
  *   free_pages       device int32 [num_pages], the ring, updated in place
  *   state, new_state device int32 [2]: the ring's head and count before and after the call
  *   new_offsets_d/h  int32 [batch+1] prefix of T_b, the new tokens among a request's want: its last ones
- *   granted          device int32 [batch]: want, or held where there were too few pages
+ *   granted          device int32 [batch]: want, or held where there were too few pages (or the state is none)
  *   slots            device int64 [sum T_b], 8-byte aligned: page * page_size + slot of every new token, in order
  * No two pages of the ring and of the tables are the same. What the call writes overlaps none of its other arrays.
- * A length outside its range is cut to it, a token before position 0, a page outside [0, num_pages) and one that the
- * ring has no place for give no slot or are lost, and a state that is none leaves the ring as it is: all set
- * DEVICE_BOUNDS. Needs none of the handle's head sizes. Errors: INVALID_ARG / WORKSPACE as above.
+ * A length outside its range is cut to it; a token before position 0 has no slot; a page that the ring has no place for is
+ * lost; a state that is none (head or count outside the ring) leaves ring and state as they are, and nobody whose pages
+ * would change is served: all set DEVICE_BOUNDS. So does an entry outside [0, num_pages), of a table or of the ring; it goes
+ * round as it is: into the ring with the pages that come back, into the table of the request whose turn it is, and the
+ * tokens there have no slot. Needs none of the handle's head sizes. Errors: INVALID_ARG / WORKSPACE as above.
  */
 litevlm_status_t litevlm_select_cache_reserve(litevlm_select_t handle, int32_t batch, int32_t page_size,
                                               int32_t* table, int32_t table_width, const int32_t* held,

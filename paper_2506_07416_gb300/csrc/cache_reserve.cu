@@ -81,8 +81,9 @@ __global__ void __launch_bounds__(kThreads) reserve_kernel(const __grid_constant
         }
         longlong2 all;
         const longlong2 before = scan2(max(need - has, 0), max(has - need, 0), warp_s, all);
-        // (the sum only grows: behind the first request that finds too few none takes a page)
-        const bool served = need <= has || taken + before.x + need - has <= count;
+        // (the sum only grows: behind the first request that finds too few none takes a page; a ring that is none takes
+        // nothing back either, and who wanted to give still holds what it held)
+        const bool served = need == has || (need < has ? count >= 0 : taken + before.x + need - has <= count);
         if (tid < n) {
             want_s[tid] = want;
             has_s[tid] = has;
@@ -120,7 +121,7 @@ __global__ void __launch_bounds__(kThreads) reserve_kernel(const __grid_constant
                     if (p < 0 || p >= total) atomicOr(a.err, kErrBounds);
                     row[o] = p;
                 }
-            } else if (count >= 0) {
+            } else {
                 for (int o = np + o0; o < hp; o += by) {
                     const int64_t to = from_s[x] + o - np;
                     const int32_t p = row[o];
