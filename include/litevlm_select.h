@@ -622,6 +622,25 @@ litevlm_status_t litevlm_select_cache_append(litevlm_select_t handle, int32_t ba
                                              void* v_stored, int32_t* new_lens, litevlm_stream_t stream);
 
 /*
+ * litevlm_select_cache_append behind a litevlm_select_cache_reserve whose answer the host has not seen (in a captured step):
+ * tokens from position granted[b] on are skipped, with no report, and new_lens[b] is seq_lens[b] + the number of
+ * those that were appended. So a refused request (granted[b] = seq_lens[b]) stays as it is, and reserve may be
+ * given its new length as the one held. The calls behind it take the same offsets: the T_b queries of such a
+ * request then stand at its last positions (before its first ones where it has fewer: they see no key), and what comes out
+ * of them, or is added to weights by them, means nothing.
+ *   granted          device int32 [batch], not overlapping new_lens; NULL: all tokens are appended
+ * What k_stored and v_stored hold for a skipped token stays.
+ */
+litevlm_status_t litevlm_select_cache_append_granted(litevlm_select_t handle, int32_t batch, const litevlm_cache_t* cache,
+                                                     const int32_t* table, int32_t table_width, const int32_t* seq_lens,
+                                                     const void* k, int64_t k_row_stride, const void* v,
+                                                     int64_t v_row_stride, int64_t src_rows, const int32_t* row_idx,
+                                                     const int32_t* new_offsets_d, const int32_t* new_offsets_h,
+                                                     float k_in_scale, float v_in_scale, float* weights, void* k_stored,
+                                                     void* v_stored, const int32_t* granted, int32_t* new_lens,
+                                                     litevlm_stream_t stream);
+
+/*
  * Attention of the last tokens of every request over its cache. Query i of the
  * T_b queries of request b stands at position n_b - T_b + i (n_b = seq_lens[b],
  * the queries' own tokens appended before) and sees the positions up to its own:
@@ -755,7 +774,7 @@ typedef struct {
  * yet: with T_b = n_b. The V tensors are not read.
  *   new_offsets_d/h  int32 [batch+1] prefix of T_b (0: the request's ranges stay)
  * Requests that share a page have the same tokens in it. Lengths and tables are checked as by the other calls; a T_b
- * beyond n_b is cut to it (DEVICE_BOUNDS). Errors: as above.
+ * beyond n_b means all tokens of the request. Errors: as above.
  */
 litevlm_status_t litevlm_select_cache_bounds(litevlm_select_t handle, int32_t batch, const litevlm_cache_t* cache,
                                              const litevlm_key_bounds_t* bounds, const int32_t* table,

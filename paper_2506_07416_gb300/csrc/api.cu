@@ -1488,6 +1488,77 @@ litevlm_status_t check_workspace(litevlm_select_t h, const void* workspace, int6
     return LITEVLM_OK;
 }
 
+litevlm_status_t append_rows(litevlm_select_t h, int32_t batch, const litevlm_cache_t* cache,
+                             const int32_t* table, int32_t table_width, const int32_t* seq_lens,
+                             const void* k, int64_t k_row_stride, const void* v,
+                             int64_t v_row_stride, int64_t src_rows, const int32_t* row_idx,
+                             const int32_t* new_offsets_d, const int32_t* new_offsets_h,
+                             float k_in_scale, float v_in_scale, float* weights, void* k_stored,
+                             void* v_stored, const int32_t* granted, int32_t* new_lens, litevlm_stream_t stream)
+{
+    litevlm_status_t s = start_call(h, batch);
+    if (s != LITEVLM_OK) return s;
+    int64_t rows = 0;
+    s = check_offsets(h, new_offsets_h, batch, INT32_MAX, "new_offsets", &rows);
+    if (s != LITEVLM_OK || batch == 0) return s;
+    lvs::AppendArgs a{};
+    s = cache_pages(h, cache, table, table_width, seq_lens, &a.cache, &a.limit);
+    if (s != LITEVLM_OK) return s;
+    if (!new_offsets_d || !new_lens) return fail(h, LITEVLM_ERR_INVALID_ARG, "a device pointer is NULL");
+    if (overlap(new_lens, (int64_t)batch * 4, seq_lens, (int64_t)batch * 4))
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "new_lens must not overlap seq_lens");
+    if (overlap(new_lens, (int64_t)batch * 4, granted, (int64_t)batch * 4))
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "new_lens must not overlap granted");
+    if (src_rows < 0 || (!row_idx && src_rows < rows))
+        return fail(h, LITEVLM_ERR_INVALID_ARG, "k and v have fewer rows than the call appends");
+    if (rows > 0) {
+        s = check_rows(h, k, k_row_stride, h->cfg.num_kv_heads, k_in_scale, "k");
+        if (s == LITEVLM_OK) s = check_rows(h, v, v_row_stride, h->cfg.num_kv_heads, v_in_scale, "v");
+        if (s != LITEVLM_OK) return s;
+        if (!in_range(k_in_scale) || !in_range(v_in_scale))
+            return fail(h, LITEVLM_ERR_INVALID_ARG, "k_in_scale and v_in_scale must be in [2^-60, 2^60]");
+        if ((k_stored && !aligned16(k_stored)) || (v_stored && !aligned16(v_stored)))
+            return fail(h, LITEVLM_ERR_INVALID_ARG, "k_stored and v_stored must be 16-byte aligned");
+        const int64_t row = (int64_t)h->cfg.num_kv_heads * h->cfg.head_dim, stored = rows * row * 2;
+        const int64_t esize = h->cfg.qk_dtype == LITEVLM_FP8_E4M3 ? 1 : 2;
+        const auto in_k = [&](const void* p) { return overlap_rows(p, stored, k, src_rows, k_row_stride, row, esize); };
+        const auto in_v = [&](const void* p) { return overlap_rows(p, stored, v, src_rows, v_row_stride, row, esize); };
+        if (overlap(k_stored, stored, v_stored, stored) || in_k(k_stored) || in_v(k_stored) || in_k(v_stored) ||
+            in_v(v_stored))
+            return fail(h, LITEVLM_ERR_INVALID_ARG, "k_stored and v_stored must not overlap k, v or one another");
+    }
+    s = debug_mirror(h, new_offsets_d, new_offsets_h, (int64_t)batch + 1, "new_offsets", stream);
+    if (s != LITEVLM_OK) return s;
+    a.src[0] = k;
+    a.src[1] = v;
+    a.stride[0] = k_row_stride;
+    a.stride[1] = v_row_stride;
+    a.row_idx = row_idx;
+    a.src_rows = src_rows;
+    a.rows = rows;
+    a.lens = seq_lens;
+    a.off = new_offsets_d;
+    a.batch = batch;
+    a.in_scale[0] = k_in_scale;
+    a.in_scale[1] = v_in_scale;
+    a.inv_scale[0] = 1.f / cache->k_scale;
+    a.inv_scale[1] = 1.f / cache->v_scale;
+    a.stored[0] = static_cast<__nv_bfloat16*>(k_stored);
+    a.stored[1] = static_cast<__nv_bfloat16*>(v_stored);
+    a.weights = weights;
+    a.granted = granted;
+    a.new_lens = new_lens;
+    a.err = h->err_d;
+    const OnDevice on(h->device);
+    cudaError_t e = on.e;
+    if (e == cudaSuccess)
+        e = lvs::launch_cache_append(a, h->cfg.head_dim, h->cfg.qk_dtype == LITEVLM_FP8_E4M3, h->num_sms,
+                                     (cudaStream_t)stream);
+    if (e != cudaSuccess) return cuda_fail(h, e, "cache_append launch");
+    h->last_launches = 1;
+    return LITEVLM_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1783,64 +1854,23 @@ litevlm_status_t litevlm_select_cache_append(litevlm_select_t h, int32_t batch, 
 {
     const CallRange range_(__func__);
     if (!h) return LITEVLM_ERR_INVALID_ARG;
-    litevlm_status_t s = start_call(h, batch);
-    if (s != LITEVLM_OK) return s;
-    int64_t rows = 0;
-    s = check_offsets(h, new_offsets_h, batch, INT32_MAX, "new_offsets", &rows);
-    if (s != LITEVLM_OK || batch == 0) return s;
-    lvs::AppendArgs a{};
-    s = cache_pages(h, cache, table, table_width, seq_lens, &a.cache, &a.limit);
-    if (s != LITEVLM_OK) return s;
-    if (!new_offsets_d || !new_lens) return fail(h, LITEVLM_ERR_INVALID_ARG, "a device pointer is NULL");
-    if (overlap(new_lens, (int64_t)batch * 4, seq_lens, (int64_t)batch * 4))
-        return fail(h, LITEVLM_ERR_INVALID_ARG, "new_lens must not overlap seq_lens");
-    if (src_rows < 0 || (!row_idx && src_rows < rows))
-        return fail(h, LITEVLM_ERR_INVALID_ARG, "k and v have fewer rows than the call appends");
-    if (rows > 0) {
-        s = check_rows(h, k, k_row_stride, h->cfg.num_kv_heads, k_in_scale, "k");
-        if (s == LITEVLM_OK) s = check_rows(h, v, v_row_stride, h->cfg.num_kv_heads, v_in_scale, "v");
-        if (s != LITEVLM_OK) return s;
-        if (!in_range(k_in_scale) || !in_range(v_in_scale))
-            return fail(h, LITEVLM_ERR_INVALID_ARG, "k_in_scale and v_in_scale must be in [2^-60, 2^60]");
-        if ((k_stored && !aligned16(k_stored)) || (v_stored && !aligned16(v_stored)))
-            return fail(h, LITEVLM_ERR_INVALID_ARG, "k_stored and v_stored must be 16-byte aligned");
-        const int64_t row = (int64_t)h->cfg.num_kv_heads * h->cfg.head_dim, stored = rows * row * 2;
-        const int64_t esize = h->cfg.qk_dtype == LITEVLM_FP8_E4M3 ? 1 : 2;
-        const auto in_k = [&](const void* p) { return overlap_rows(p, stored, k, src_rows, k_row_stride, row, esize); };
-        const auto in_v = [&](const void* p) { return overlap_rows(p, stored, v, src_rows, v_row_stride, row, esize); };
-        if (overlap(k_stored, stored, v_stored, stored) || in_k(k_stored) || in_v(k_stored) || in_k(v_stored) ||
-            in_v(v_stored))
-            return fail(h, LITEVLM_ERR_INVALID_ARG, "k_stored and v_stored must not overlap k, v or one another");
-    }
-    s = debug_mirror(h, new_offsets_d, new_offsets_h, (int64_t)batch + 1, "new_offsets", stream);
-    if (s != LITEVLM_OK) return s;
-    a.src[0] = k;
-    a.src[1] = v;
-    a.stride[0] = k_row_stride;
-    a.stride[1] = v_row_stride;
-    a.row_idx = row_idx;
-    a.src_rows = src_rows;
-    a.rows = rows;
-    a.lens = seq_lens;
-    a.off = new_offsets_d;
-    a.batch = batch;
-    a.in_scale[0] = k_in_scale;
-    a.in_scale[1] = v_in_scale;
-    a.inv_scale[0] = 1.f / cache->k_scale;
-    a.inv_scale[1] = 1.f / cache->v_scale;
-    a.stored[0] = static_cast<__nv_bfloat16*>(k_stored);
-    a.stored[1] = static_cast<__nv_bfloat16*>(v_stored);
-    a.weights = weights;
-    a.new_lens = new_lens;
-    a.err = h->err_d;
-    const OnDevice on(h->device);
-    cudaError_t e = on.e;
-    if (e == cudaSuccess)
-        e = lvs::launch_cache_append(a, h->cfg.head_dim, h->cfg.qk_dtype == LITEVLM_FP8_E4M3, h->num_sms,
-                                     (cudaStream_t)stream);
-    if (e != cudaSuccess) return cuda_fail(h, e, "cache_append launch");
-    h->last_launches = 1;
-    return LITEVLM_OK;
+    return append_rows(h, batch, cache, table, table_width, seq_lens, k, k_row_stride, v, v_row_stride, src_rows, row_idx,
+                       new_offsets_d, new_offsets_h, k_in_scale, v_in_scale, weights, k_stored, v_stored, nullptr, new_lens, stream);
+}
+
+litevlm_status_t litevlm_select_cache_append_granted(litevlm_select_t h, int32_t batch, const litevlm_cache_t* cache,
+                                                     const int32_t* table, int32_t table_width, const int32_t* seq_lens,
+                                                     const void* k, int64_t k_row_stride, const void* v,
+                                                     int64_t v_row_stride, int64_t src_rows, const int32_t* row_idx,
+                                                     const int32_t* new_offsets_d, const int32_t* new_offsets_h,
+                                                     float k_in_scale, float v_in_scale, float* weights, void* k_stored,
+                                                     void* v_stored, const int32_t* granted, int32_t* new_lens,
+                                                     litevlm_stream_t stream)
+{
+    const CallRange range_(__func__);
+    if (!h) return LITEVLM_ERR_INVALID_ARG;
+    return append_rows(h, batch, cache, table, table_width, seq_lens, k, k_row_stride, v, v_row_stride, src_rows, row_idx,
+                       new_offsets_d, new_offsets_h, k_in_scale, v_in_scale, weights, k_stored, v_stored, granted, new_lens, stream);
 }
 
 litevlm_status_t litevlm_select_cache_attend_workspace(litevlm_select_t h, int32_t batch, const int32_t* q_offsets_h,

@@ -83,7 +83,7 @@ __global__ void __launch_bounds__(kBoundsThreads, 5) bounds_kernel(const __grid_
     bool bad;
     const int len = cache_len(__ldg(a.lens + lo), a.limit, bad);
     if (t <= 0) return;
-    if ((bad || t > len) && lane == 0) atomicOr(a.err, kErrBounds);
+    if (bad && lane == 0) atomicOr(a.err, kErrBounds);
     const int64_t o = (max(len - t, 0) >> a.cache.page_shift) + (place - page_at(q0, lo, a.cache.page_shift));
     const int64_t first = o << a.cache.page_shift;
     if (first >= len) return;

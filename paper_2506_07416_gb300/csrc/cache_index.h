@@ -35,6 +35,13 @@ LVS_HD int64_t page_at(int64_t rows, int64_t b, int32_t page_shift) { return (ro
 // Tiles of `per` queries of a request with n.
 LVS_HD int32_t tiles_of(int32_t n, int32_t per) { return n <= 0 ? 0 : (n - 1) / per + 1; }
 
+// Length of a request of `len` tokens that would have `n` with its new ones, of which only those before position `granted`
+// are appended.
+LVS_HD int64_t appended_len(int64_t len, int64_t n, int64_t granted)
+{
+    return n <= granted || n <= len ? n : (granted > len ? granted : len);
+}
+
 // Tokens of a request that the kernels may touch: its length cut to
 // [0, limit]. `bad` tells that the length was outside.
 LVS_HD int cache_len(int32_t len, int32_t limit, bool& bad)

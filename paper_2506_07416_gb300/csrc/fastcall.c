@@ -19,18 +19,19 @@
 
 enum { F_SCORE, F_FULL, F_SCORE_TOPK, F_TOPK, F_COMPACT, F_SPLICE, F_PROJECT, F_KEEP,
        F_APPEND, F_SPACE, F_ATTEND, F_EVICT, F_VERIFY, F_RESERVE, F_BOUNDS, F_PICK_SPACE, F_PICK, F_PICKED_SPACE,
-       F_PICKED, F_COUNT };
+       F_PICKED, F_APPEND_GRANTED, F_COUNT };
 static const char *const kNames[F_COUNT] = {"score", "score_full_keys", "score_topk", "topk",
                                             "compact", "splice", "project", "keep_offsets",
                                             "cache_append", "cache_attend_workspace", "cache_attend", "cache_evict",
                                             "verify", "cache_reserve", "cache_bounds", "cache_pick_workspace",
-                                            "cache_pick", "cache_attend_picked_workspace", "cache_attend_picked"};
+                                            "cache_pick", "cache_attend_picked_workspace", "cache_attend_picked",
+                                            "cache_append_granted"};
 /* h handle / stream, i int32, l int64, f float, p pointer, n host int32 array */
 static const char *const kSigs[F_COUNT] = {"hippnppnffph", "hippnppnppnpffph", "hippnppnffppnfppph", "hippnpnfppph",
                                            "", "hippnppnppnppnlpppph", "hliipppfippifph", "",
                                            "hippipplpllppnffpppph", "", "hippipplpnifpppplh", "hippipiiiipippph",
                                            "hiiippnpppppph", "hiipipppippnppph", "hipppippnh", "", "hippipplpniiiipplh", "",
-                                           "hippipplpnpifpplh"};
+                                           "hippipplpnpifpplh", "hippipplpllppnffppppph"};
 static void *g_fn[F_COUNT];
 static PyObject *g_host_i32;      /* the binding's conversion of a host offset array */
 static PyObject *g_ndarray;       /* numpy.ndarray */
@@ -267,6 +268,16 @@ static PyObject *f_append(PyObject *self, PyObject *const *args, Py_ssize_t n)
           g_fn[F_APPEND])(
         a[0].p, a[1].i, a[2].p, a[3].p, a[4].i, a[5].p, a[6].p, a[7].l, a[8].p, a[9].l, a[10].l, a[11].p,
         a[12].p, a[13].p, a[14].f, a[15].f, a[16].p, a[17].p, a[18].p, a[19].p, a[20].p);
+    END
+}
+
+static PyObject *f_append_granted(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    BEGIN(F_APPEND_GRANTED)
+    rc = ((int (*)(P, I, P, P, I, P, P, int64_t, P, int64_t, int64_t, P, P, P, float, float, P, P, P, P, P, P))
+          g_fn[F_APPEND_GRANTED])(
+        a[0].p, a[1].i, a[2].p, a[3].p, a[4].i, a[5].p, a[6].p, a[7].l, a[8].p, a[9].l, a[10].l, a[11].p,
+        a[12].p, a[13].p, a[14].f, a[15].f, a[16].p, a[17].p, a[18].p, a[19].p, a[20].p, a[21].p);
     END
 }
 
@@ -611,6 +622,7 @@ static PyMethodDef kMethods[] = {DEF("bind", f_bind), DEF("score", f_score), DEF
                                  DEF("score_topk", f_score_topk), DEF("topk", f_topk), DEF("compact", f_compact),
                                  DEF("splice", f_splice), DEF("project", f_project),
                                  DEF("keep_total", f_keep_total), DEF("cache_append", f_append),
+                                 DEF("cache_append_granted", f_append_granted),
                                  DEF("cache_attend", f_attend), DEF("attend_bytes", f_attend_bytes),
                                  DEF("cache_evict", f_evict), DEF("verify", f_verify),
                                  DEF("cache_reserve", f_reserve), DEF("cache_bounds", f_bounds),

@@ -148,6 +148,7 @@ struct AppendArgs {
     float in_scale[2], inv_scale[2];
     __nv_bfloat16* stored[2]; // [rows][hkv][d] values that the codes stand for, or null
     float* weights;           // [num_pages][page_size], 0 for the new tokens; or null
+    const int32_t* granted;   // [batch] tokens that the requests' pages hold: none behind them is appended; or null
     int32_t* new_lens;        // [batch]
     int32_t* err;
 };

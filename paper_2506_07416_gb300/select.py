@@ -85,6 +85,7 @@ def _load():
     lib.litevlm_select_keep_offsets.argtypes = [i32, P, P, f32, P]
     lib.litevlm_select_cache_append.argtypes = [P, i32, P, P, i32, P, P, i64, P, i64, i64, P, P, P, f32, f32, P, P, P,
                                                 P, P]
+    lib.litevlm_select_cache_append_granted.argtypes = [*lib.litevlm_select_cache_append.argtypes[:-2], P, P, P]
     lib.litevlm_select_cache_attend_workspace.argtypes = [P, i32, P, i32, i32, ctypes.POINTER(i64)]
     lib.litevlm_select_cache_attend.argtypes = [P, i32, P, P, i32, P, P, i64, P, P, i32, f32, P, P, P, P, i64, P]
     lib.litevlm_select_cache_evict.argtypes = [P, i32, P, P, i32, P, i32, i32, i32, i32, P, i32, P, P, P, P]
@@ -101,7 +102,7 @@ def _load():
                "score_noalloc", "splice", "views", "fold_norm", "rope_table", "project", "score_topk", "host_view",
                "keep_offsets", "cache_append", "cache_attend_workspace", "cache_attend", "cache_evict", "verify",
                "cache_reserve", "cache_bounds", "cache_pick_workspace", "cache_pick", "cache_attend_picked_workspace",
-               "cache_attend_picked", "set_wait_budget", "set_debug_flags"):
+               "cache_attend_picked", "cache_append_granted", "set_wait_budget", "set_debug_flags"):
         getattr(lib, "litevlm_select_" + fn).restype = ctypes.c_int
     return lib
 
@@ -119,7 +120,8 @@ EXPORTS = ["litevlm_select_create", "litevlm_select_destroy", "litevlm_select_la
            "litevlm_select_cache_attend", "litevlm_select_cache_evict", "litevlm_select_verify",
            "litevlm_select_cache_reserve", "litevlm_select_cache_bounds", "litevlm_select_cache_pick_workspace",
            "litevlm_select_cache_pick", "litevlm_select_cache_attend_picked_workspace",
-           "litevlm_select_cache_attend_picked", "litevlm_select_set_wait_budget", "litevlm_select_set_debug_flags"]
+           "litevlm_select_cache_attend_picked", "litevlm_select_cache_append_granted", "litevlm_select_set_wait_budget",
+           "litevlm_select_set_debug_flags"]
 FLAGS = {"auto": 0, "reread": 1, "resident": 2, "resident_1buf": 8, "resident_2buf": 16, "resident_flat": 64}
 # LITEVLM_FLAG_SCORE_SPLIT_QUERIES: resident plans for T > 64 run each head's text rows as two pseudo-heads
 QUERY_SPLIT = {"whole": 0, "split": 128}
@@ -191,7 +193,8 @@ def _load_fastcall():
                     for n in ("score", "score_full_keys", "score_topk", "topk", "compact", "splice", "project",
                               "keep_offsets", "cache_append", "cache_attend_workspace", "cache_attend", "cache_evict",
                               "verify", "cache_reserve", "cache_bounds", "cache_pick_workspace", "cache_pick",
-                              "cache_attend_picked_workspace", "cache_attend_picked")}, _host_i32, np.ndarray, _ctypes_value)
+                              "cache_attend_picked_workspace", "cache_attend_picked", "cache_append_granted")},
+                   _host_i32, np.ndarray, _ctypes_value)
     return _fastcall
 
 
@@ -314,11 +317,17 @@ def splice(handle: int, batch: int, sys_rows, sys_offsets_d, sys_offsets_h, vis_
 
 def cache_append(handle: int, batch: int, cache, table, table_width: int, seq_lens, k, k_row_stride: int, v,
                  v_row_stride: int, src_rows: int, row_idx, new_offsets_d, new_offsets_h, k_in_scale: float,
-                 v_in_scale: float, weights, k_stored, v_stored, new_lens, stream=None) -> None:
-    """litevlm_select_cache_append; cache: the address of a litevlm_cache_t (KVCache.struct)."""
-    rc = _FC.cache_append(handle, batch, cache, table, table_width, seq_lens, k, k_row_stride, v, v_row_stride, src_rows,
-                          row_idx, new_offsets_d, new_offsets_h, k_in_scale, v_in_scale, weights, k_stored, v_stored,
-                          new_lens, _stream_ptr(stream))
+                 v_in_scale: float, weights, k_stored, v_stored, new_lens, stream=None, granted=None) -> None:
+    """litevlm_select_cache_append, or with ``granted`` litevlm_select_cache_append_granted; cache: the address of a
+    litevlm_cache_t (KVCache.struct)."""
+    if granted is None:
+        rc = _FC.cache_append(handle, batch, cache, table, table_width, seq_lens, k, k_row_stride, v, v_row_stride,
+                              src_rows, row_idx, new_offsets_d, new_offsets_h, k_in_scale, v_in_scale, weights, k_stored,
+                              v_stored, new_lens, _stream_ptr(stream))
+    else:
+        rc = _FC.cache_append_granted(handle, batch, cache, table, table_width, seq_lens, k, k_row_stride, v, v_row_stride,
+                                      src_rows, row_idx, new_offsets_d, new_offsets_h, k_in_scale, v_in_scale, weights,
+                                      k_stored, v_stored, granted, new_lens, _stream_ptr(stream))
     if rc:
         _check(rc, handle)
 
@@ -815,10 +824,12 @@ class Selector:
         return KVCache(*c, k_scale=k_scale, v_scale=v_scale, weights=w)
 
     def cache_append(self, cache: KVCache, table, seq_lens, k, v, offsets, rows=None, k_in_scale: float = 1.0,
-                     v_in_scale: float = 1.0, offsets_h=None, stored: bool = False, new_lens=None, stream=None):
+                     v_in_scale: float = 1.0, offsets_h=None, stored: bool = False, new_lens=None, stream=None,
+                     granted=None):
         """Quantises rows into the cache: token t of request b, row offsets[b] + t of k and v [rows, Hkv, d] (or row
-        rows[offsets[b] + t]), to position seq_lens[b] + t of the request's pages; its weight becomes 0. Returns the
-        new lengths, and with ``stored`` also the K and V values that the cache now holds for the rows (bf16)."""
+        rows[offsets[b] + t]), to position seq_lens[b] + t of the request's pages; its weight becomes 0. With ``granted``
+        (what ``cache_reserve`` returned) the tokens behind it are skipped: a refused request stays as it was. Returns
+        the new lengths, and with ``stored`` also the K and V values that the cache now holds for the rows (bf16)."""
         import torch
         off_h = _host_i32(offsets if offsets_h is None else offsets_h)
         batch, total = len(off_h) - 1, int(off_h[-1])
@@ -831,6 +842,8 @@ class Selector:
             _refuse("k and v must have the same number of rows")
         if rows is not None:
             _want("rows", rows, torch.int32, (total,), dev)
+        if granted is not None:
+            _want("granted", granted, torch.int32, (batch,), dev)
         with _allocate_on(stream, dev):
             if new_lens is None:
                 new_lens = torch.empty_like(seq_lens)
@@ -840,7 +853,7 @@ class Selector:
                    for _ in "kv"] if stored else (None, None)
         cache_append(self.handle, batch, cache.struct, table, table.shape[1], seq_lens, k, k_stride, v, v_stride,
                      k.shape[0], rows, offsets, off_h, k_in_scale, v_in_scale, cache.weights, out[0], out[1], new_lens,
-                     _stream_on(stream, dev))
+                     _stream_on(stream, dev), granted)
         return (new_lens, *out) if stored else new_lens
 
     def cache_attend(self, cache: KVCache, table, seq_lens, q, offsets, max_len: int, q_scale: float = 1.0,
