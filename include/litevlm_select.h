@@ -771,7 +771,7 @@ typedef struct {
  * before), from all tokens of these pages. With m = f * 2^p, 1/2 <= f < 1, the largest magnitude of a head's channels:
  *     exps = p - 7 (0 where m = 0);  codes = ceil(largest / 2^exps), floor(smallest / 2^exps), at most 126
  * A value whose scale is NaN counts as 0. After litevlm_select_cache_evict, or for a cache that has no ranges
- * yet: with T_b = n_b. The V tensors are not read.
+ * yet: with T_b = n_b. The V tensors are not read. The ranges overlap no other array of the call, nor each other.
  *   new_offsets_d/h  int32 [batch+1] prefix of T_b (0: the request's ranges stay)
  * Requests that share a page have the same tokens in it. Lengths and tables are checked as by the other calls; a T_b
  * beyond n_b means all tokens of the request. Errors: as above.

@@ -9,6 +9,7 @@
 #include <algorithm>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <limits>
 #include <mutex>
 #include <new>
@@ -1269,6 +1270,16 @@ bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes)
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
     return a && b && a_bytes > 0 && b_bytes > 0 && x < y + (uint64_t)b_bytes && y < x + (uint64_t)a_bytes;
 }
+struct Span {
+    const void* p;
+    int64_t bytes;
+};
+bool overlap_any(const void* a, int64_t a_bytes, std::initializer_list<Span> others)
+{
+    for (const Span& s : others)
+        if (overlap(a, a_bytes, s.p, s.bytes)) return true;
+    return false;
+}
 // The same with rows of `row` elements, `stride` (>= row) apart: what lies between them does not count.
 bool overlap_rows(const void* a, int64_t a_bytes, const void* rows_at, int64_t rows, int64_t stride, int64_t row,
                   int64_t esize)
@@ -1637,13 +1648,13 @@ litevlm_status_t litevlm_select_cache_bounds(litevlm_select_t h, int32_t batch, 
     if (s != LITEVLM_OK) return s;
     {
         const int64_t pages = (int64_t)cache->num_pages * h->cfg.num_kv_heads, row = (int64_t)cache->page_size * h->cfg.head_dim;
-        const int64_t codes = pages * 2 * h->cfg.head_dim;
-        if (overlap(bounds->codes, codes, bounds->exps, pages) ||
-            overlap(bounds->codes, codes, cache->k_codes, pages * row / 2) ||
-            overlap(bounds->codes, codes, cache->k_scales, pages * row / 16) ||
-            overlap(bounds->exps, pages, cache->k_codes, pages * row / 2) ||
-            overlap(bounds->exps, pages, cache->k_scales, pages * row / 16))
-            return fail(h, LITEVLM_ERR_INVALID_ARG, "the ranges must not overlap the cache or one another");
+        const int64_t codes = pages * 2 * h->cfg.head_dim, n = (int64_t)batch * 4;
+        const auto others = {Span{cache->k_codes, pages * row / 2},  Span{cache->v_codes, pages * row / 2},
+                             Span{cache->k_scales, pages * row / 16}, Span{cache->v_scales, pages * row / 16},
+                             Span{table, n * table_width},            Span{seq_lens, n}, Span{new_offsets_d, n + 4}};
+        if (overlap(bounds->codes, codes, bounds->exps, pages) || overlap_any(bounds->codes, codes, others) ||
+            overlap_any(bounds->exps, pages, others))
+            return fail(h, LITEVLM_ERR_INVALID_ARG, "the ranges must not overlap the call's other arrays or one another");
     }
     if (bounds->num_pages != cache->num_pages || bounds->page_size != cache->page_size)
         return fail(h, LITEVLM_ERR_INVALID_ARG, "the ranges and the cache have different pages");

@@ -515,6 +515,11 @@ def _row_stride(name: str, t, dtype, heads: int, d: int, device: int) -> int:
     _refuse(f"{name}'s heads and channels must lie side by side (only the row stride is free)")
 
 
+def _bytes_of(t):
+    """First address of a contiguous tensor's bytes and the one behind them."""
+    return (0, 0) if t is None else (t.data_ptr(), t.data_ptr() + t.numel() * t.element_size())
+
+
 class KVCache:
     """The tensors of a 4-bit K/V cache (litevlm_cache_t), uint8 CUDA tensors: codes [pages, Hkv, page_size, d/2],
     scales [pages, Hkv, page_size, d/16]; weights: float32 [pages, page_size] or None. ``Selector.cache`` makes one.
@@ -525,6 +530,7 @@ class KVCache:
             if value is not None:
                 import torch
                 _want("weights", value, torch.float32, (self.num_pages, self.page_size), self.device)
+            object.__setattr__(self, "weights_at", _bytes_of(value))
         elif "struct" in self.__dict__:
             _refuse(f"{name} of a KVCache is fixed: make another one")
         object.__setattr__(self, name, value)
@@ -565,6 +571,7 @@ class KeyBounds:
         _want("codes", codes, torch.int8, (self.num_pages, self.heads, 2, self.head_dim), self.device)
         _want("exps", exps, torch.int8, (self.num_pages, self.heads), self.device)
         self.codes, self.exps = codes, exps
+        self.at = (_bytes_of(codes), _bytes_of(exps))
         self._c = Bounds(codes.data_ptr(), exps.data_ptr(), self.num_pages, self.page_size)
         self.struct = ctypes.addressof(self._c)
 
@@ -975,6 +982,10 @@ class Selector:
             self._cache_call(cache, table, seq_lens, batch)
             self._cache_call(bounds, table, seq_lens, batch, KeyBounds)
             _want("offsets", offsets, torch.int32, (batch + 1,), dev)
+        first, end = cache.weights_at  # (the C call does not know them)
+        (a0, b0), (a1, b1) = bounds.at
+        if a0 < end and first < b0 or a1 < end and first < b1:
+            _refuse("the ranges must not overlap the cache's weights")
         rc = _FC.cache_bounds(self.handle, batch, cache.struct, bounds.struct, table, table.shape[1], seq_lens, offsets, off_h,
                               _stream_on(stream, dev))
         if rc:
