@@ -799,6 +799,7 @@ litevlm_status_t litevlm_select_cache_bounds(litevlm_select_t handle, int32_t ba
  *   workspace        device, at least the bytes that litevlm_select_cache_pick_workspace gives for the same sizes (4 for
  *                    every query, key head and page of max_len; 0 where budget holds max_len), 256-byte aligned; as for
  *                    litevlm_select_cache_attend
+ * What the call writes (picked, the workspace) overlaps none of its other arrays.
  * exps are in [-100, 100] (cut to it). A page whose table entry is not in the pool ranks below all others (DEVICE_BOUNDS).
  * Errors: as above; UNSUPPORTED for more than 128 query heads a key head, where Hkv x the longest request's tiles of columns
  * (128 of them, 64 in calls of no more; G rounded up to 1, 2, 4 or a multiple of 8 for each query) pass 65535, or
@@ -821,6 +822,7 @@ litevlm_status_t litevlm_select_cache_pick(litevlm_select_t handle, int32_t batc
  *                    and key head (its result is then not defined). Entries that name no page that the query
  *                    sees (-1 among them) are skipped
  *   workspace        at least the bytes that litevlm_select_cache_attend_picked_workspace gives for the same sizes
+ * What the call writes (out, the workspace) overlaps none of its other arrays.
  * A query whose list has no key that it sees gives zeros. The other arguments, the precision and the errors are those
  * of litevlm_select_cache_attend without weights (table_width * page_size bounds the lengths).
  */

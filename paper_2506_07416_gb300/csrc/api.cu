@@ -1723,10 +1723,16 @@ litevlm_status_t litevlm_select_cache_pick(litevlm_select_t h, int32_t batch, co
     if (s == LITEVLM_OK) s = check_workspace(h, workspace, workspace_bytes, need);
     if (s == LITEVLM_OK) s = debug_mirror(h, q_offsets_d, q_offsets_h, (int64_t)batch + 1, "q_offsets", stream);
     if (s != LITEVLM_OK) return s;
-    const int64_t row = (int64_t)c.num_q_heads * c.head_dim, lists = a.rows * c.num_kv_heads * budget * 4;
-    if (overlap_rows(picked, lists, q, a.rows, q_row_stride, row, c.qk_dtype == LITEVLM_FP8_E4M3 ? 1 : 2) ||
-        overlap(picked, lists, workspace, need))
-        return fail(h, LITEVLM_ERR_INVALID_ARG, "picked must not overlap q or the workspace");
+    const int64_t row = (int64_t)c.num_q_heads * c.head_dim, esize = c.qk_dtype == LITEVLM_FP8_E4M3 ? 1 : 2;
+    const int64_t lists = a.rows * c.num_kv_heads * budget * 4, n = (int64_t)batch * 4;
+    const int64_t heads = (int64_t)bounds->num_pages * c.num_kv_heads;
+    const auto others = {Span{bounds->codes, heads * 2 * c.head_dim}, Span{bounds->exps, heads}, Span{table, n * table_width},
+                         Span{seq_lens, n}, Span{q_offsets_d, n + 4}};
+    if (overlap_rows(picked, lists, q, a.rows, q_row_stride, row, esize) || overlap(picked, lists, workspace, need) ||
+        overlap_rows(workspace, need, q, a.rows, q_row_stride, row, esize) || overlap_any(picked, lists, others) ||
+        overlap_any(workspace, need, others))
+        return fail(h, LITEVLM_ERR_INVALID_ARG,
+                    "picked and the workspace must not overlap the call's other arrays or one another");
     a.codes = static_cast<const int8_t*>(bounds->codes);
     a.exps = static_cast<const int8_t*>(bounds->exps);
     a.num_pages = bounds->num_pages;
@@ -1802,15 +1808,19 @@ litevlm_status_t litevlm_select_cache_attend_picked(litevlm_select_t h, int32_t 
     if (s != LITEVLM_OK) return s;
     if (!q_offsets_d || !picked) return fail(h, LITEVLM_ERR_INVALID_ARG, "a device pointer is NULL");
     if (!out || !aligned16(out)) return fail(h, LITEVLM_ERR_INVALID_ARG, "out must be 16-byte aligned and not NULL");
-    const int64_t row = (int64_t)c.num_q_heads * c.head_dim;
-    if (overlap_rows(out, total * row * 2, q, total, q_row_stride, row, c.qk_dtype == LITEVLM_FP8_E4M3 ? 1 : 2) ||
-        overlap(out, total * row * 2, picked, total * c.num_kv_heads * budget * 4))
-        return fail(h, LITEVLM_ERR_INVALID_ARG, "out must not overlap q or picked");
     s = check_workspace(h, workspace, workspace_bytes, space.total);
     if (s != LITEVLM_OK) return s;
-    if (overlap(workspace, space.total, out, total * row * 2) ||
-        overlap(workspace, space.total, picked, total * c.num_kv_heads * budget * 4))
-        return fail(h, LITEVLM_ERR_INVALID_ARG, "the workspace must not overlap out or picked");
+    const int64_t row = (int64_t)c.num_q_heads * c.head_dim, esize = c.qk_dtype == LITEVLM_FP8_E4M3 ? 1 : 2;
+    const int64_t results = total * row * 2, n = (int64_t)batch * 4;
+    const int64_t keys = (int64_t)cache->num_pages * c.num_kv_heads * cache->page_size * c.head_dim;
+    const auto others = {Span{cache->k_codes, keys / 2}, Span{cache->v_codes, keys / 2}, Span{cache->k_scales, keys / 16},
+                         Span{cache->v_scales, keys / 16}, Span{picked, total * c.num_kv_heads * budget * 4},
+                         Span{table, n * table_width}, Span{seq_lens, n}, Span{q_offsets_d, n + 4}};
+    if (overlap_rows(out, results, q, total, q_row_stride, row, esize) || overlap(out, results, workspace, space.total) ||
+        overlap_rows(workspace, space.total, q, total, q_row_stride, row, esize) || overlap_any(out, results, others) ||
+        overlap_any(workspace, space.total, others))
+        return fail(h, LITEVLM_ERR_INVALID_ARG,
+                    "out and the workspace must not overlap the call's other arrays or one another");
     s = debug_mirror(h, q_offsets_d, q_offsets_h, (int64_t)batch + 1, "q_offsets", stream);
     if (s != LITEVLM_OK) return s;
     uint8_t* ws = static_cast<uint8_t*>(workspace);
