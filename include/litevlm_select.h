@@ -801,9 +801,8 @@ litevlm_status_t litevlm_select_cache_bounds(litevlm_select_t handle, int32_t ba
  *                    litevlm_select_cache_attend
  * What the call writes (picked, the workspace) overlaps none of its other arrays.
  * exps are in [-100, 100] (cut to it). A page whose table entry is not in the pool ranks below all others (DEVICE_BOUNDS).
- * Errors: as above; UNSUPPORTED for more than 128 query heads a key head, where Hkv x the longest request's tiles of columns
- * (128 of them, 64 in calls of no more; G rounded up to 1, 2, 4 or a multiple of 8 for each query) pass 65535, or
- * Hkv x sum T_b passes 2^31 - 1.
+ * Errors: as above; UNSUPPORTED for more than 128 query heads a key head, where Hkv x the longest request's tiles of 128
+ * columns (G of them, rounded up to 1, 2, 4 or a multiple of 8, for each query) pass 65535, or Hkv x sum T_b passes 2^31 - 1.
  */
 litevlm_status_t litevlm_select_cache_pick_workspace(litevlm_select_t handle, int32_t batch,
                                                      const int32_t* q_offsets_h, int32_t max_len, int32_t page_size,

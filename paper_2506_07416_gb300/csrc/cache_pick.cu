@@ -9,8 +9,9 @@
 // column for each query head of a key head (a query's columns padded to a power of two or whole tiles of eight):
 //   pick_token_kernel, one tile of columns: 32 caches of 30 Ki to 127 Ki tokens in pages of 32, 32 / 8 heads (180 MB): 41 us,
 //     4.3 TB/s, a fifth of it the CTAs' start; one of 40 Ki, 28 / 4 heads, 7 us with the launch
-//   pick_score_kernel, up to 64 columns: a warp keeps 16 pages as f16 in registers and goes over the columns' tiles in
-//     shared memory (with it the prompts below took 74 us)
+//   pick_score_kernel, up to 64 columns a request: a warp keeps 16 pages as f16 in registers and goes over the columns'
+//     tiles in shared memory. The caches above with 2 to 8 queries each take 96 us, the picking with them; the prompts
+//     below took 74 with it
 //   cache_pick_tile.cu, more: 777 to 1024 queries of two requests of 20 Ki to 32 Ki in pages of 64, 28 / 4 heads: 27 us
 // pick_select_kernel: the budget-th largest score of a query by counting its scores in buckets, then the
 // pages above it and the lowest of those at it, in order. 256 lists of up to 4096 pages 10.5 us, 7204 of about 400 14
@@ -26,13 +27,7 @@ namespace {
 
 constexpr int kScoreThreads = 128;
 constexpr int kScorePages = 16 * kScoreThreads / 32;  // of a CTA at a time
-constexpr int kScoreTiles = 8;                        // tiles of eight columns of a CTA, at most (16 for more heads)
-
-// Queries of a CTA.
-__host__ __device__ __forceinline__ int score_queries(int padded)
-{
-    return padded >= 8 * kScoreTiles ? 1 : 8 * kScoreTiles / padded;
-}
+constexpr int kScoreCols = 64;                        // columns of a request up to which a CTA has them all
 
 __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint2 b)
 {
@@ -97,10 +92,11 @@ __device__ __forceinline__ void store_scores(const PickArgs& a, const ScoreTile&
                                              const float (&unit)[2], const float (&d)[4], float (&best)[2])
 {
     const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+    const int64_t keys_step = (int64_t)a.hkv * a.key_stride, keys_at = (int64_t)(st.q0 + st.i0) * keys_step + h * a.key_stride;
     auto put = [&](int i, int e, float s) {  // score of the CTA's query i and page g + 8 e
         const int o = base + g + 8 * e;
         if (i < st.queries && o < st.pages)
-            a.keys[((int64_t)(st.q0 + st.i0 + i) * a.hkv + h) * a.key_stride + o] =
+            a.keys[keys_at + i * keys_step + o] =
                 (e ? unit[1] : unit[0]) > 0.f ? score_key(s * (e ? unit[1] : unit[0])) : 1u;
     };
     if (padded == 1) {
@@ -321,19 +317,18 @@ __global__ void __launch_bounds__(kScoreThreads, 5) pick_token_kernel(const __gr
     copy_async_wait<0>();
 }
 
-// Some queries: up to eight tiles of columns (more for a query of more than 64 heads), four at a time, chains of
-// contractions that do not wait for one another.
+// Some queries: up to eight tiles of columns, four at a time, chains of contractions that do not wait for one another.
 template <int D, bool FP8>
 __global__ void __launch_bounds__(kScoreThreads, 3) pick_score_kernel(const __grid_constant__ PickArgs a, int blocks)
 {
     constexpr int STEPS = 2 * D / 16, GROUP = 4;            // contractions of 16 channels
     extern __shared__ __align__(16) uint2 frag_s[];         // [tile][step][lane]
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = lane & 3;
-    const int h = blockIdx.y % a.hkv, part = blockIdx.y / a.hkv, b = blockIdx.z;
+    const int h = blockIdx.y, b = blockIdx.z;
     griddep_wait();
     griddep_launch_dependents();
     const int padded = padded_group(a.group);
-    const ScoreTile st = score_tile(a, b, part, score_queries(padded));
+    const ScoreTile st = score_tile(a, b, 0, kScoreCols / padded);
     const int step = blocks * kScorePages;
     int base = blockIdx.x * kScorePages + warp * 16;
     if (blockIdx.x * kScorePages >= st.pages) return;
@@ -550,20 +545,15 @@ cudaError_t launch_scores(const PickArgs& a, int max_t, int max_pages, int num_s
                            (unsigned)groups, 1);
         return cudaLaunchKernelEx(&cfg, pick_token_kernel<D, FP8>, a, (int)cfg.gridDim.x);
     }
-    const int per = score_queries(padded), parts = (max_t + per - 1) / per;
-    const int tiles = (std::min(per, max_t) * padded + 7) / 8;
-    auto kern = pick_score_kernel<D, FP8>;
-    cfg.dynamicSmemBytes = (size_t)tiles * (2 * D / 16) * 32 * sizeof(uint2);
-    cudaError_t e = cudaSuccess;
-    if (cfg.dynamicSmemBytes > 48 * 1024)
-        e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes);
-    if (e != cudaSuccess) return e;
+    constexpr int kTileBytes = 2 * D / 16 * 32 * (int)sizeof(uint2);
+    static_assert(kScoreCols / 8 * kTileBytes <= 48 * 1024, "the columns fit shared memory as it is");
+    cfg.dynamicSmemBytes = (size_t)((max_t * padded + 7) / 8) * kTileBytes;
     // CTAs of a request's pages: 64 pages at a time, two rounds of what runs at once
-    const int64_t others = (int64_t)parts * a.hkv * a.batch, steps = (max_pages + kScorePages - 1) / kScorePages;
+    const int64_t others = (int64_t)a.hkv * a.batch, steps = (max_pages + kScorePages - 1) / kScorePages;
     const int64_t times = std::max<int64_t>(1, std::min<int64_t>(steps, others * steps / (2 * 3 * (int64_t)num_sms)));
     const int64_t blocks = (steps + times - 1) / times;
-    cfg.gridDim = dim3((unsigned)blocks, (unsigned)(parts * a.hkv), (unsigned)a.batch);
-    return cudaLaunchKernelEx(&cfg, kern, a, (int)blocks);
+    cfg.gridDim = dim3((unsigned)blocks, (unsigned)a.hkv, (unsigned)a.batch);
+    return cudaLaunchKernelEx(&cfg, pick_score_kernel<D, FP8>, a, (int)blocks);
 }
 
 }  // namespace
@@ -576,8 +566,8 @@ int64_t pick_key_stride(int64_t max_len, int page_shift, int budget)
 
 int pick_col_tiles(int64_t max_t, int group)
 {
-    const int padded = padded_group(group);
-    const int per = max_t * padded > 64 ? pick_tile_queries(group) : score_queries(padded);
+    if (max_t * padded_group(group) <= kScoreCols) return max_t > 0;
+    const int per = pick_tile_queries(group);
     return (int)((max_t + per - 1) / per);
 }
 
@@ -595,7 +585,7 @@ cudaError_t launch_cache_pick(const PickArgs& a, int head_dim, bool fp8, int max
     cudaError_t e = cudaSuccess;
     if (a.key_stride > 0) {
         const int64_t columns = (int64_t)max_t * padded_group(a.group);
-        if (columns > 64) e = launch_pick_tiles(a, head_dim, fp8, max_t, max_pages, num_sms, stream);
+        if (columns > kScoreCols) e = launch_pick_tiles(a, head_dim, fp8, max_t, max_pages, num_sms, stream);
         else e = fp8 ? launch_scores<128, true>(a, max_t, max_pages, num_sms, cfg)
                 : (head_dim == 128 ? launch_scores<128, false>(a, max_t, max_pages, num_sms, cfg)
                                    : launch_scores<64, false>(a, max_t, max_pages, num_sms, cfg));
