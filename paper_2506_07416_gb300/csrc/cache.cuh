@@ -57,6 +57,27 @@ __device__ __forceinline__ void e4m3x4_value(uint32_t w, __half2 (&v)[2])
     v[0] = bits_h2(o[0]), v[1] = bits_h2(o[1]);
 }
 
+// The last of n items in order that is not behind what is sought, as before(x) says of item x (item 0 is not asked); by a
+// warp, 32 items at a time.
+template <typename F>
+__device__ __forceinline__ int last_before(int n, F before)
+{
+    const int lane = threadIdx.x & 31;
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 31) / 32, at = lo + (lane + 1) * step;
+        lo += __popc(__ballot_sync(0xffffffffu, at < hi && before(at))) * step;
+        hi = min(hi, lo + step);
+    }
+    return lo;
+}
+
+// The request of row r of a batch whose rows begin at off: the last whose first row is not behind it, by a warp.
+__device__ __forceinline__ int find_request(const int32_t* off, int batch, int64_t r)
+{
+    return last_before(batch, [&](int x) { return __ldg(off + x) <= r; });
+}
+
 // 16 bytes from global to shared memory, asynchronously; zeros where !valid.
 __device__ __forceinline__ void copy_async16(uint32_t dst, const void* src, bool valid)
 {

@@ -108,20 +108,6 @@ __device__ __forceinline__ int find_active(const AttendArgs& a, int n)
     return a.batch;
 }
 
-// The request of query r: the last whose first query is not behind it, by a warp, 32 at a time.
-__device__ __forceinline__ int find_request(const int32_t* off, int batch, int64_t r)
-{
-    const int lane = threadIdx.x & 31;
-    int lo = 0, hi = batch;
-    while (hi - lo > 1) {
-        const int step = (hi - lo + 31) / 32, at = lo + (lane + 1) * step;
-        const uint32_t m = __ballot_sync(0xffffffffu, at < hi && __ldg(off + at) <= r);
-        lo += __popc(m) * step;
-        hi = min(hi, lo + step);
-    }
-    return lo;
-}
-
 // A tile of queries, of attention over picked pages: its request, its first query there, and how many it has (0: the tile
 // is none's).
 struct QueryTile {

@@ -70,15 +70,8 @@ __global__ void __launch_bounds__(kBoundsThreads, 5) bounds_kernel(const __grid_
     griddep_wait();
     griddep_launch_dependents();
     if (place >= a.places) return;
-    // the request: the last whose first place is not behind the unit's, 32 at a time
-    int lo = 0, hi = a.batch;
-    while (hi - lo > 1) {
-        const int step = (hi - lo + 31) / 32, at = lo + (lane + 1) * step;
-        const uint32_t m =
-            __ballot_sync(0xffffffffu, at < hi && page_at(__ldg(a.off + at), at, a.cache.page_shift) <= place);
-        lo += __popc(m) * step;
-        hi = min(hi, lo + step);
-    }
+    const int lo =  // the request
+        last_before(a.batch, [&](int x) { return page_at(__ldg(a.off + x), x, a.cache.page_shift) <= place; });
     const int q0 = __ldg(a.off + lo), t = __ldg(a.off + lo + 1) - q0;
     bool bad;
     const int len = cache_len(__ldg(a.lens + lo), a.limit, bad);

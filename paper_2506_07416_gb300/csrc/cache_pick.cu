@@ -394,17 +394,9 @@ __global__ void __launch_bounds__(WARPS == 1 ? 128 : 32 * WARPS) pick_select_ker
     const int64_t pair = WARPS == 1 ? (int64_t)blockIdx.x * 4 + warp : (int64_t)blockIdx.x;
     if (pair >= a.rows * a.hkv) return;
     const int64_t r = pair / a.hkv;
-    // the request of the query: the last whose first query is not behind it, 32 at a time
     int b = (int)r, t1 = (int)r + 1;
     if (!a.single) {
-        int lo = 0, hi = a.batch;
-        while (hi - lo > 1) {
-            const int step = (hi - lo + 31) / 32, at = lo + (lane + 1) * step;
-            const uint32_t m = __ballot_sync(0xffffffffu, at < hi && __ldg(a.off + at) <= r);
-            lo += __popc(m) * step;
-            hi = min(hi, lo + step);
-        }
-        b = lo;
+        b = find_request(a.off, a.batch, r);
         t1 = __ldg(a.off + b + 1);
     }
     bool bad;

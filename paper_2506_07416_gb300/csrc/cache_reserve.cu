@@ -12,9 +12,7 @@
 
 #include <algorithm>
 
-#include "cache_index.h"
-#include "internal.h"
-#include "ptx.cuh"
+#include "cache.cuh"
 
 namespace lvs {
 
@@ -139,12 +137,7 @@ __global__ void __launch_bounds__(kThreads) reserve_kernel(const __grid_constant
         const int64_t r0 = max(off_s[0], 0), r1 = min((int64_t)off_s[n], a.rows);
         constexpr int U = 8;
         for (int64_t q = r0 + 32 * U * ((int64_t)(tid >> 5) * gridDim.x + blockIdx.x); q < r1; q += 32 * U * step) {
-            int x = 0, hi = n;  // the request of the first token: the last that begins at or before it, 32 at a time
-            while (hi - x > 1) {
-                const int d = (hi - x + 31) / 32, at = x + (lane + 1) * d;
-                x += __popc(__ballot_sync(0xffffffffu, at < hi && off_s[at] <= q)) * d;
-                hi = min(hi, x + d);
-            }
+            int x = last_before(n, [&](int y) { return off_s[y] <= q; });  // the request of the first token
             int32_t p[U], in[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
