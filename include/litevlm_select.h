@@ -785,7 +785,8 @@ litevlm_status_t litevlm_select_cache_bounds(litevlm_select_t handle, int32_t ba
 /*
  * The pages that every query attends to, for each key head. Query i of request b stands at position p = n_b - T_b + i
  * and sees the pages 0 to P = p / page_size of its request. With r the whole numbers nearest to q / 2^(e - 7) (a tie to
- * the even one, at most 127), 2^e the least power of two above the magnitudes of the key head's G query heads:
+ * the even one, at most 127), 2^e the least power of two above the magnitudes of the key head's G query heads (e at
+ * least -119):
  *     S(page) = 2^exps * max over the G heads of sum over channels of r * (r > 0 ? largest : smallest)
  * which no key of the page passes by more than the rounding of q. Where P + 1 <= budget all pages are picked, else the
  * first `sink`, the last `recent`, and of the others those of the largest S until budget are (ties: the lower page).

@@ -1447,7 +1447,7 @@ cudaError_t launch_picked(const AttendArgs& a, const PickedPlan& plan, int64_t q
 // rounds / n of the list and the writing and joining of a chunk's sums. A shared list is taken to grow by half of a
 // query's own for each doubling of the queries: of 32 pages each, picked as neighbours mostly agree on, 18 queries
 // have 117 and 36 124. A chunk of a prompt (777 to 1024 queries of two requests, 28 / 4 heads, 32 pages of 64): whole
-// 234 us, two chunks 210, three 243.
+// 237 us, two chunks 216, three 252.
 PickedPlan plan_attend_picked(int batch, int hkv, int group, const int32_t* q_off, int page_shift, int width, int budget,
                               int num_sms)
 {

@@ -199,7 +199,7 @@ struct VPart {
 // PICKED: the rows are whole queries of a tile, and the keys those of the pages that any of them has, in the list's order; a
 // key of a page that a row's query has not is as masked. Of 64 or 32 keys that no row of a warp has, the warp
 // makes no exponentials. Few rows stand in the tile more than once, so that all four warps make exponentials: drafts of
-// 32 ragged requests, 4 to 32 rows a head, 48 pages of 32: 83 us without, 77 with. What bounds those: a tile takes 3000
+// 32 ragged requests, 4 to 32 rows a head, 48 pages of 32: 82 us without, 77 with. What bounds those: a tile takes 3000
 // clocks of a CTA (1000 are the tensor pipe's, which two CTAs share), half of them the warps that make the values.
 // Dropped there: lines fetched into the L2 three tiles ahead and loads in another order (78 us).
 template <int D, bool FP8, int NR, bool PICKED = false>

@@ -1010,7 +1010,8 @@ class Selector:
         """The ``budget`` pages that each query [sum T, Hq, d] attends to, for each key head: the first ``sink``, the last
         ``recent`` up to its own position, and those whose ranges have the largest product with it. Returns int32
         [sum T, Hkv, budget]: pages of the request, ascending, -1 behind the last. ``workspace``: a uint8 tensor of at least
-        ``cache_pick_workspace`` bytes that no other call in flight uses."""
+        ``cache_pick_workspace`` bytes (4 for every query, key head and page of ``max_len``, whatever the lengths are) that
+        no other call in flight uses; without one the handle keeps its own, of the largest call so far."""
         import torch
         off_h = _host_i32(offsets if offsets_h is None else offsets_h)
         batch, total, dev = len(off_h) - 1, int(off_h[-1]), self.device
